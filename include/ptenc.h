@@ -181,6 +181,60 @@ PTENC_API int ptenc_lora_apply(ptenc_cache* c, int layer, const void* A, const v
 PTENC_API int ptenc_decode_step(ptenc_cache* c, int layer, const void* q, const void* k_new, const void* v_new,
                       const uint8_t* active, void* out, void* stream);
 
+/* Speculative decoding under the fixed-size cache.  (The paper decodes one token per step; a rollout is bound by reading the
+ * window, and a draft that is verified many tokens at a time reads it once for all of them.)  A draft of a sequence is a
+ * tree of up to max_nodes <= PTENC_MAX_TREE nodes in topological order: parent[b][i] in [-1, i) is the node that node i
+ * continues, -1 for a root, which continues the cached sequence itself.  One round: ptenc_tree_attn on every layer (the
+ * target model's queries, keys and values of all nodes), ptenc_verify_tree on the resulting probabilities,
+ * ptenc_commit_path on every layer.
+ *
+ * ptenc_tree_attn: attention of every node over the cache and over its own ancestors.
+ *   out[b,i,h,:] = softmax(q[b,i,h,:] . K^T / sqrt(D)) V  over what ptenc_decode_attn would see after the tokens on node i's
+ * path (its ancestors, then itself) had been appended one by one: the pinned entries, the ring without the tokens that
+ * those appends would have evicted, and the nodes of the path that would still be there.  The cache is not changed.
+ *   q, out [B, max_nodes, H_q, D]; k_tree, v_tree [B, max_nodes, H_kv, D] (leading [L] when layer == -1); parent
+ * [B, max_nodes] and n_nodes [B] int32, the same for every layer (n_nodes nullable = max_nodes for all); lse_out
+ * [B, max_nodes, H_q] fp32, nullable.  Rows of nodes at or past n_nodes[b] (0 allowed) and of inactive sequences are neither
+ * read nor written.  What a node does not see does not reach its rows, whatever it holds (NaN and infinities included).
+ * A sequence whose n_nodes, parents or ring words are out of range is left alone and the device status word gets
+ * PTENC_ST_BAD_INDEX (2).  max_nodes outside 1..PTENC_MAX_TREE: PTENC_ESHAPE.  PTENC_EINVAL under PTENC_POLICY_SCORE, whose
+ * evictions depend on the attention of every single step. */
+#define PTENC_MAX_TREE 64
+PTENC_API int ptenc_tree_attn(ptenc_cache* c, int layer, const void* q, const void* k_tree, const void* v_tree,
+                              const int32_t* parent, const int32_t* n_nodes, int32_t max_nodes, const uint8_t* active,
+                              void* out, float* lse_out, void* stream);
+
+/* Rejection sampling of a draft tree; needs no cache.  p[b,i,:] is the target's distribution after node i, q[b,i,:] the
+ * draft's distribution from which the children of node i were drawn (q NULL: the drafted tokens were certain, q is one at
+ * the token and zero elsewhere); [B, max_nodes, vocab], both fp32 or both bf16 (dtype).  Node 0 is the only root: the token
+ * the sequence ends with.  tokens [B, max_nodes] int32, drafted token of node i >= 1 (entry 0 is not read); u
+ * [B, max_nodes] fp32 uniform random numbers in [0, 1): u[b,i] judges node i >= 1, u[b,0] draws the next token.
+ *   cur = 0, r = p[0].  For i = 1 .. n_nodes-1 with parent[i] == cur, in this order: accepted when
+ *   u[i] * q[cur][tokens[i]] < r[tokens[i]]: cur = i, r = p[i].  Otherwise r = max(r - q[cur], 0) / sum (r = p[cur] when
+ *   nothing is left).  Then next_token = the first x with r[0] + .. + r[x] > u[0] * (sum of r).
+ * The sequence of accepted tokens and next_token is distributed as if sampled from p token by token.  Evaluated in 64 bits.
+ *   path [B, max_nodes] int32: node 0, the accepted nodes, then -1; n_path [B]: how many (1 + accepted); next_token [B].
+ * These are what ptenc_commit_path takes.  Entries of p and q are finite and not negative; a row of p that sums to zero gives
+ * next_token -1.  A sequence with n_nodes outside 1..max_nodes, a parent or a token out of range gets path -1, n_path 0,
+ * next_token -1.  Outputs of inactive sequences are not written.  n_nodes, active nullable.  p and q 16-byte aligned, the
+ * others 4.  PTENC_ESHAPE: max_nodes > PTENC_MAX_TREE. */
+PTENC_API int ptenc_verify_tree(const void* p, const void* q, int dtype, const int32_t* tokens, const int32_t* parent,
+                                const int32_t* n_nodes, const float* u, const uint8_t* active, int32_t batch,
+                                int32_t max_nodes, int32_t vocab, int32_t* path, int32_t* n_path, int32_t* next_token,
+                                void* stream);
+
+/* The accepted path enters the cache: for each active sequence the same result as ptenc_append_evict followed by
+ * ptenc_encode of the staged rows, once for each of the tokens path[b][0 .. n_path[b]-1] in order (rows of k_tree, v_tree
+ * [B, max_nodes, H_kv, D], leading [L] when layer == -1).  path [B, max_nodes], n_path [B] int32 (0: nothing is appended),
+ * the same for every layer; a node may not have been drafted in order, any indices in [0, max_nodes) are taken as they come.
+ * n_evicted_out [B] (nullable, leading [L] when layer == -1): tokens evicted altogether.  What the last append evicted stays
+ * staged, as after ptenc_append_evict, and has been folded.  A sequence with n_path outside 0..max_nodes, a node or ring
+ * words out of range is left alone (n_evicted_out 0) and the status word gets PTENC_ST_BAD_INDEX (2).  PTENC_EINVAL under
+ * PTENC_POLICY_SCORE; PTENC_ESHAPE for max_nodes outside 1..PTENC_MAX_TREE. */
+PTENC_API int ptenc_commit_path(ptenc_cache* c, int layer, const void* k_tree, const void* v_tree, int32_t max_nodes,
+                                const int32_t* path, const int32_t* n_path, const uint8_t* active,
+                                int32_t* n_evicted_out, void* stream);
+
 /* a4 with HOST buffers: the same step as ptenc_decode_step, with q, k_new, v_new, active read from host
  * memory and out written to host memory.  The call enqueues the host-to-device copies into `dev_staging`
  * (device, 256-byte aligned, at least ptenc_host_staging_bytes), the step, and the device-to-host copy of out,

@@ -28,7 +28,8 @@ EXPORTS = ["ptenc_workspace_bytes", "ptenc_cache_create", "ptenc_cache_destroy",
            "ptenc_host_staging_bytes", "ptenc_decode_step_host",
            "ptenc_get_ring", "ptenc_get_state", "ptenc_get_evicted", "ptenc_get_scores", "ptenc_cache_status", "ptenc_cache_info", "ptenc_attn_launch_info",
            "ptenc_workspace_region", "ptenc_time_next_attn", "ptenc_attn_rings_static", "ptenc_launch_count",
-           "ptenc_strerror"]
+           "ptenc_tree_attn", "ptenc_verify_tree", "ptenc_commit_path", "ptenc_strerror"]
+MAX_TREE = 64
 
 
 class PtencConfig(ctypes.Structure):
@@ -75,6 +76,10 @@ def _load() -> ctypes.CDLL:
     lib.ptenc_workspace_region.argtypes = [vp, i32, ctypes.POINTER(u64), ctypes.POINTER(u64)]
     lib.ptenc_time_next_attn.argtypes = [vp, vp, vp]
     lib.ptenc_attn_rings_static.argtypes = [cfgp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.ptenc_tree_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp]
+    lib.ptenc_verify_tree.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                      vp, vp, vp, vp]
+    lib.ptenc_commit_path.argtypes = [vp, i32, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp]
     lib.ptenc_launch_count.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
     lib.ptenc_strerror.argtypes = [i32]
     lib.ptenc_strerror.restype = ctypes.c_char_p
@@ -106,6 +111,17 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _want(where: str, device, *wanted) -> None:
+    """Refuses tensors the C side could not tell from valid ones: (name, tensor or None, shape, dtype) each."""
+    for name, t, shape, dtype in wanted:
+        if t is None:
+            continue
+        if t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a contiguous {dtype} tensor on {device}")
+        if t.shape != shape:
+            raise PtencError(PTENC_ESHAPE, f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+
+
 def make_config(*, n_layers, batch, n_q_heads, n_kv_heads, head_dim, window, evict_chunk=1, n_global=32,
                 rank=32, dtype="bf16", normalize_mode=0, encode_enabled=1, device=0, attn_consumer_warps=0,
                 policy=POLICY_FIFO, recent=0) -> PtencConfig:
@@ -130,6 +146,25 @@ def attn_rings_static(cfg: PtencConfig, K, V, head, count, q, out, active=None, 
     _check(lib.ptenc_attn_rings_static(ctypes.byref(cfg), _ptr(K), _ptr(V), _ptr(head), _ptr(count), _ptr(q),
                                        _ptr(active), _ptr(out), _ptr(lse_out), _ptr(status_out), _stream()),
            "ptenc_attn_rings_static")
+
+
+def verify_tree(p, q, tokens, parent, u, path, n_path, next_token, n_nodes=None, active=None):
+    """ptenc_verify_tree: rejection sampling of a draft tree.  p, q [B, T, V] (q None: certain drafts), fp32 or bf16; tokens,
+    parent [B, T] int32; u [B, T] fp32; out: path [B, T], n_path [B], next_token [B] int32."""
+    where = "ptenc_verify_tree"
+    if p.dim() != 3 or p.dtype not in (torch.float32, torch.bfloat16):
+        raise PtencError(PTENC_EINVAL, f"{where}: p is to be a [B, T, V] tensor of fp32 or bf16")
+    B, T, V = p.shape
+    i32 = torch.int32
+    _want(where, p.device, ("p", p, p.shape, p.dtype), ("q", q, p.shape, p.dtype), ("tokens", tokens, (B, T), i32),
+          ("parent", parent, (B, T), i32), ("u", u, (B, T), torch.float32), ("path", path, (B, T), i32),
+          ("n_path", n_path, (B,), i32), ("next_token", next_token, (B,), i32), ("n_nodes", n_nodes, (B,), i32),
+          ("active", active, (B,), torch.uint8))
+    if p.device.type != "cuda" or p.device.index != torch.cuda.current_device():
+        raise PtencError(PTENC_EINVAL, f"{where}: the tensors' device is to be the current CUDA device")
+    _check(lib.ptenc_verify_tree(_ptr(p), _ptr(q), DTYPE_BF16 if p.dtype == torch.bfloat16 else DTYPE_FP32, _ptr(tokens),
+                                 _ptr(parent), _ptr(n_nodes), _ptr(u), _ptr(active), B, T, V, _ptr(path), _ptr(n_path),
+                                 _ptr(next_token), _stream()), where)
 
 
 class Cache:
@@ -201,6 +236,40 @@ class Cache:
     def decode_step(self, layer, q, k_new, v_new, out, active=None):
         _check(lib.ptenc_decode_step(self._h, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(active), _ptr(out),
                                      _stream()), "ptenc_decode_step")
+
+    def _tree_shape(self, layer, k_tree, where):
+        """Leading dimensions [L, B, T] or [B, T] of the tree tensors of a call."""
+        lead = k_tree.shape[:-2]
+        want = 3 if layer == -1 else 2
+        if len(lead) != want or lead[-2] != self.cfg.batch or (layer == -1 and lead[0] != self.cfg.n_layers):
+            raise PtencError(PTENC_ESHAPE, f"{where}: k_tree has shape {tuple(k_tree.shape)}")
+        return lead
+
+    def tree_attn(self, layer, q, k_tree, v_tree, parent, out, n_nodes=None, active=None, lse_out=None):
+        """Attention of draft-tree nodes over the cache and their ancestors.  q, out [.., B, T, Hq, D]; k_tree, v_tree
+        [.., B, T, Hkv, D]; parent [B, T], n_nodes [B] int32; lse_out [.., B, T, Hq] fp32 (leading [L] when layer == -1)."""
+        where, c, dt = "ptenc_tree_attn", self.cfg, self.torch_dtype
+        lead = self._tree_shape(layer, k_tree, where)
+        B, T = lead[-2:]
+        _want(where, self.device, ("q", q, (*lead, c.n_q_heads, c.head_dim), dt),
+              ("k_tree", k_tree, (*lead, c.n_kv_heads, c.head_dim), dt),
+              ("v_tree", v_tree, (*lead, c.n_kv_heads, c.head_dim), dt), ("parent", parent, (B, T), torch.int32),
+              ("out", out, (*lead, c.n_q_heads, c.head_dim), dt), ("n_nodes", n_nodes, (B,), torch.int32),
+              ("active", active, (B,), torch.uint8), ("lse_out", lse_out, (*lead, c.n_q_heads), torch.float32))
+        _check(lib.ptenc_tree_attn(self._h, layer, _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(n_nodes), T,
+                                   _ptr(active), _ptr(out), _ptr(lse_out), _stream()), where)
+
+    def commit_path(self, layer, k_tree, v_tree, path, n_path, active=None, n_evicted_out=None):
+        """Appends the path's tokens in order, evicting and encoding as decode steps would.  path [B, T], n_path [B] int32."""
+        where, c, dt = "ptenc_commit_path", self.cfg, self.torch_dtype
+        lead = self._tree_shape(layer, k_tree, where)
+        B, T = lead[-2:]
+        _want(where, self.device, ("k_tree", k_tree, (*lead, c.n_kv_heads, c.head_dim), dt),
+              ("v_tree", v_tree, (*lead, c.n_kv_heads, c.head_dim), dt), ("path", path, (B, T), torch.int32),
+              ("n_path", n_path, (B,), torch.int32), ("active", active, (B,), torch.uint8),
+              ("n_evicted_out", n_evicted_out, lead[:-1], torch.int32))
+        _check(lib.ptenc_commit_path(self._h, layer, _ptr(k_tree), _ptr(v_tree), T, _ptr(path), _ptr(n_path),
+                                     _ptr(active), _ptr(n_evicted_out), _stream()), where)
 
     def host_staging_bytes(self, layer) -> int:
         n = ctypes.c_size_t(0)

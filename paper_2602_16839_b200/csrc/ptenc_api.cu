@@ -389,6 +389,53 @@ int ptenc_lora_apply(ptenc_cache* c, int layer, const void* A, const void* Bm, c
              ? PTENC_OK : PTENC_ECUDA;
 }
 
+namespace {
+// What the two calls of the speculative step that take a cache check alike.
+int check_tree_call(const ptenc_cache* c, int layer, int32_t max_nodes, int* l0, int* nl) {
+  const int rc = check_layer(c, layer, l0, nl);
+  if (rc != PTENC_OK) return rc;
+  if (c->cfg.policy != PTENC_POLICY_FIFO) return PTENC_EINVAL;
+  if (max_nodes < 1 || max_nodes > PTENC_MAX_TREE) return PTENC_ESHAPE;
+  return PTENC_OK;
+}
+int check_device(const ptenc_cache* c) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return PTENC_ECUDA;
+  return dev == c->cfg.device ? PTENC_OK : PTENC_EINVAL;
+}
+inline bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) != 0; }
+}  // namespace
+
+int ptenc_tree_attn(ptenc_cache* c, int layer, const void* q, const void* k_tree, const void* v_tree,
+                    const int32_t* parent, const int32_t* n_nodes, int32_t max_nodes, const uint8_t* active, void* out,
+                    float* lse_out, void* stream) {
+  int l0, nl;
+  int rc = check_tree_call(c, layer, max_nodes, &l0, &nl);
+  if (rc != PTENC_OK) return rc;
+  if (q == nullptr || k_tree == nullptr || v_tree == nullptr || parent == nullptr || out == nullptr) return PTENC_EINVAL;
+  if (misaligned(q) || misaligned(k_tree) || misaligned(v_tree) || misaligned(out) || off4(parent) || off4(n_nodes) ||
+      off4(lse_out))
+    return PTENC_EALIGN;
+  if ((rc = check_device(c)) != PTENC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return ok(ptenc_launch_tree_generic(c, l0, nl, q, k_tree, v_tree, parent, n_nodes, max_nodes, active, out, lse_out, st),
+            "tree_attn", st) ? PTENC_OK : PTENC_ECUDA;
+}
+
+int ptenc_commit_path(ptenc_cache* c, int layer, const void* k_tree, const void* v_tree, int32_t max_nodes,
+                      const int32_t* path, const int32_t* n_path, const uint8_t* active, int32_t* n_evicted_out,
+                      void* stream) {
+  int l0, nl;
+  int rc = check_tree_call(c, layer, max_nodes, &l0, &nl);
+  if (rc != PTENC_OK) return rc;
+  if (k_tree == nullptr || v_tree == nullptr || path == nullptr || n_path == nullptr) return PTENC_EINVAL;
+  if (misaligned(k_tree) || misaligned(v_tree) || off4(path) || off4(n_path) || off4(n_evicted_out)) return PTENC_EALIGN;
+  if ((rc = check_device(c)) != PTENC_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return ok(ptenc_launch_commit(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, st),
+            "commit_path", st) ? PTENC_OK : PTENC_ECUDA;
+}
+
 int ptenc_decode_step(ptenc_cache* c, int layer, const void* q, const void* k_new, const void* v_new,
                       const uint8_t* active, void* out, void* stream) {
   int l0, nl;

@@ -128,6 +128,13 @@ cudaError_t ptenc_launch_lora_apply(ptenc_cache* c, int l0, int nl, const void* 
 bool ptenc_encode_tc_prepare(ptenc_cache* c);
 cudaError_t ptenc_launch_encode_tc(ptenc_cache* c, int l0, int nl, const void* Ke, const void* Ve,
                                    const int32_t* n_ev, int m_max, cudaStream_t st);
+// Speculative step: attention of a draft tree over the cache, and the append / evict / fold of an accepted path.
+cudaError_t ptenc_launch_tree_generic(ptenc_cache* c, int l0, int nl, const void* q, const void* k_tree,
+                                      const void* v_tree, const int32_t* parent, const int32_t* n_nodes, int max_nodes,
+                                      const uint8_t* active, void* out, float* lse, cudaStream_t st);
+cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tree, const void* v_tree, int max_nodes,
+                                const int32_t* path, const int32_t* n_path, const uint8_t* active,
+                                int32_t* n_evicted_out, cudaStream_t st);
 // Host-side preparation of the fast attention path (tensor maps, attributes).  Returns false when the
 // shape is not covered, in which case the generic kernel serves it.
 bool ptenc_attn_bf16_prepare(ptenc_cache* c, cudaError_t* err);
