@@ -83,6 +83,11 @@ struct ptenc_cache {
   CUtensorMap tmWk, tmWv;       // 2-D maps over the encoder weights: rows = L*r, cols = d_kv
   CUtensorMap tmStageK, tmStageV;   // 2-D maps over the staged evicted rows: rows = L*B*E, cols = d_kv
   int tc_stage_box;             // token rows per TMA box of the staged maps
+  bool tree_tc;                 // tensor-core kernel usable for draft trees
+  CUtensorMap tmTreeK, tmTreeV; // 3-D maps over the rings: units x W x D, boxes of up to 128 slots
+  float* tree_part;             // partial rows of split blocks of a tree call, their (m, l) and arrival counters
+  float* tree_ml;
+  int* tree_tickets;
   float* lora_u;                // [PTENC_LORA_MAX_PART][L][B][r] partial sums of B x (scratch of ptenc_lora_apply)
   __nv_bfloat16* lora_w;        // [2][L][B][G] S (B x) split into two bf16 terms (scratch of ptenc_lora_apply)
 };
@@ -132,6 +137,14 @@ cudaError_t ptenc_launch_encode_tc(ptenc_cache* c, int l0, int nl, const void* K
 cudaError_t ptenc_launch_tree_generic(ptenc_cache* c, int l0, int nl, const void* q, const void* k_tree,
                                       const void* v_tree, const int32_t* parent, const int32_t* n_nodes, int max_nodes,
                                       const uint8_t* active, void* out, float* lse, cudaStream_t st);
+cudaError_t ptenc_launch_tree(ptenc_cache* c, int l0, int nl, const void* q, const void* k_tree, const void* v_tree,
+                              const int32_t* parent, const int32_t* n_nodes, int max_nodes, const uint8_t* active, void* out,
+                              float* lse, cudaStream_t st);
+constexpr int PTENC_TREE_SLOTS = 320;     // partial row tiles of a tree call
+bool ptenc_tree_tc_shape(const ptenc_config* c);
+size_t ptenc_tree_part_bytes(const ptenc_config* c);
+size_t ptenc_tree_ml_bytes(const ptenc_config* c);
+bool ptenc_tree_tc_prepare(ptenc_cache* c);
 cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tree, const void* v_tree, int max_nodes,
                                 const int32_t* path, const int32_t* n_path, const uint8_t* active,
                                 int32_t* n_evicted_out, cudaStream_t st);

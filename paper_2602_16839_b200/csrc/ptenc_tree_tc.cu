@@ -1,0 +1,975 @@
+// Attention of a draft tree over the cache on the sm_100a tensor cores (bf16, head_dim 64 or 128).
+//
+// The T nodes of a tree times the g heads that share a KV head are R = T g query rows over the same K and V: R flop per
+// byte read.  Up to about 250 rows HBM is the bound (6.5 TB/s against 1.65 PFLOP/s), above it the tensor cores, so both
+// products run on tcgen05 with accumulators in tensor memory and every K/V byte is read once per 2 x 128 rows.
+//
+// A row tile is the nodes that fit 128 rows (128 / g nodes, row = node * g + head).  A work item is a block of one or two
+// row tiles of a (layer, sequence, KV head) against a stretch of its K/V tiles of 128 slots; the draft's own K/V rows are
+// one more tile at the end.  Per CTA (one per SM, persistent, items handed out by a counter):
+//  * warp 0, one lane: producer.  Describes the item, then TMA-loads its Q tiles and the K and V tiles (128-byte swizzle;
+//    plain loads of this GPU's own memory) into a ring of stages.
+//  * warp 1, one lane: issues the MMAs.  Two streams, each with its own S, P and O in tensor memory: with two row tiles a
+//    stream per row tile; with one, the K/V tiles alternate between the streams and the two results are merged at the end.
+//    One stream's products always run under the other's softmax.  S = Q K^T (both K-major in shared memory),
+//    O += P V (P bf16 in tensor memory over the S it came from, V as it lies: tokens x head_dim, MN-major).
+//  * warp 2: patches.  Works out what each node sees (ptenc_tree.cuh), and passes every stage on; in the tiles where some
+//    slot is not seen by some node it clears the V rows that nobody sees and takes non-finite values out of the V rows
+//    that only some nodes see, since 0 * NaN would carry them into the other nodes' rows.
+//  * warps 4..11: softmax, a row per thread: S from tensor memory, mask, running maximum and sum in fp32 (base 2), P
+//    rounded to bf16 back to tensor memory.  O is rescaled only when the maximum has grown by more than 2^8, which for
+//    most rows is never after the first tiles.  Non-finite values that were taken out are added to the rows that see them.
+//  * Items that are a part of a block's tiles leave fp32 partials; the CTA that arrives last (ticket) joins them in order.
+//  * Every wait is bounded: one that runs out raises a status bit and an abort flag, every role then leaves, copies and
+//    MMAs in flight are drained and tensor memory is freed.
+#include <string.h>
+
+#include "ptenc_tree.cuh"
+
+namespace {
+
+constexpr uint32_t TT_POLLS = 4000000;
+constexpr int TN = 128;                        // slots per K/V tile
+constexpr int TM = 128;                        // rows of a row tile = TMEM lanes
+constexpr int TT_THREADS = 384;                // producer, MMA, patch, (none), 2 x 4 softmax warps
+constexpr int TT_SOFT = 256;
+constexpr int TT_LEAD = 128;                   // the softmax thread that speaks for all of them
+// Registers: 384 threads are launched with 168 each (64512); the first four warps give up 88 so that a softmax thread can
+// hold a row of 128 scores: 128 * 80 + 256 * 208 = 63488.
+constexpr int TT_REGS_LOW = 80, TT_REGS_HIGH = 208;
+static_assert(128 * TT_REGS_LOW + 256 * TT_REGS_HIGH <= 384 * 168, "the split waits for registers that do not exist");
+constexpr int HALF = TN * 128;                 // 64 columns of a 128-row tile
+constexpr int TT_MAX_PIECES = 16;
+
+// ------------------------------------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t tt_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+  return ok;
+}
+// Bounded wait that also gives up when another role has raised the abort flag.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (uint32_t i = 0; i < TT_POLLS; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if ((i & 15) == 15 && *abort_flag != 0) return false;
+  }
+  return false;
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// A and B from shared memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// A from tensor memory.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// 32 consecutive 32-bit columns of this thread's lane.
+__device__ __forceinline__ void ld32(uint32_t t, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(t) : "memory");
+}
+__device__ __forceinline__ void st32(uint32_t t, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(t), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t t, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(t), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ float tt_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TT_SOFT) : "memory"); }
+
+// Shared-memory descriptors of bf16 tiles of 128-byte rows with the 128-byte swizzle.
+// K-major (the contraction index runs along the row): groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_k(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)2 << 61);
+}
+// MN-major (the contraction index counts rows): the next 64 columns one HALF on, the next 8 rows 1024 bytes on.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// D fp32, A and B bf16, M = 128; b_mn: B is MN-major.
+__host__ __device__ constexpr uint32_t tt_idesc(int n, int b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(TM >> 4) << 24);
+}
+
+// ------------------------------------------------------------------------------------------------ layout
+template <int D>
+struct TSmem {
+  static constexpr int TILE = (D / 64) * HALF;                       // bytes of a 128-row tile
+  static constexpr int STAGES = D == 128 ? 5 : 10;
+  static constexpr int OFF_Q = STAGES * TILE;                        // two Q tiles
+  static constexpr int OFF_VIS = OFF_Q + 2 * TILE;                   // u64 [64] what each node sees of the draft
+  static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // float2 [128]
+  static constexpr int OFF_DESC = OFF_ML + TM * 8;                   // int [2][32] items
+  static constexpr int OFF_BAR = OFF_DESC + 2 * 32 * 4;
+  static constexpr int N_BAR = 3 * STAGES + 20;
+  static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]
+  static constexpr int OFF_JUMP = OFF_DEPTH + TREE_MAX;              // s8 [64]
+  static constexpr int OFF_MISC = OFF_JUMP + TREE_MAX;
+  static constexpr int TOTAL = OFF_MISC + 32;
+  static_assert(TOTAL <= 232448, "shared memory of one CTA");
+};
+
+struct TreeTcArgs {
+  int l0, NT;                      // first layer; nodes per sequence in the call's tensors
+  int npt, tpb, nqp;               // nodes per row tile, row tiles per block (1 or 2), row blocks per unit
+  int nb;                          // rows of the draft tile: NT rounded up to 16
+  int ring_box;                    // rows of a ring box
+  int n_full, n_items, P;          // items that are whole blocks; all items; pieces of the other blocks
+  const int32_t* parent;
+  const int32_t* n_nodes;
+  const uint8_t* active;
+  __nv_bfloat16* out;
+  float* lse;
+  const __nv_bfloat16* v_tree;
+  float* part;                     // [slot][2][D / 4][128][4]
+  float2* part_ml;                 // [slot][2][128]
+  int* tickets;                    // [block that is split]
+};
+
+// Item description words in shared memory.
+enum { I_KIND, I_LI, I_B, I_H, I_NODE0, I_N, I_TWO, I_HEAD, I_COUNT, I_SINK, I_E, I_T0, I_LEN2, I_LO, I_CNT, I_NT, I_PIECES,
+       I_PIECE, I_SPLIT, I_EVMAX, I_VALID, I_ODD };
+
+// Tiles of a ring that hold slots some node sees: the pinned entries [0, sink) and `count` slots from sink + head on, wrapping
+// inside [sink, W).  Enumerated from the tile of the first sliding slot upwards, then from tile 0.
+__device__ __forceinline__ int tt_tiles(int sink, int head, int count, int W, int* t0, int* len2) {
+  int low = sink, high = 0;                              // slots [0, low) and [sink + head, sink + head + high)
+  const int first = W - sink - head;
+  if (count > first) { low = sink + count - first; high = first; } else { high = count; }
+  *t0 = 0;
+  *len2 = 0;
+  const int e1 = (low + TN - 1) / TN;                    // tiles of the low part
+  if (high == 0) return e1;
+  *t0 = (sink + head) / TN;
+  *len2 = (sink + head + high - 1) / TN - *t0 + 1;
+  return *len2 + min(e1, *t0);
+}
+
+// ------------------------------------------------------------------------------------------------ kernel
+template <int D>
+__global__ void __launch_bounds__(TT_THREADS, 1)
+k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+          const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKt,
+          const __grid_constant__ CUtensorMap tmVt, const TreeTcArgs a) {
+  using SM = TSmem<D>;
+  constexpr int NS = SM::STAGES, TILE = SM::TILE, DH = D / 64;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sb = tt_u32(smem);
+  volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
+  unsigned long long* s_vis = reinterpret_cast<unsigned long long*>(smem + SM::OFF_VIS);
+  float2* s_ml = reinterpret_cast<float2*>(smem + SM::OFF_ML);
+  uint8_t* s_depth = smem + SM::OFF_DEPTH;
+  int8_t* s_jump = reinterpret_cast<int8_t*>(smem + SM::OFF_JUMP);
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
+  volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict, misc[3]: last arriver
+  const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
+  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16,
+                 q_empty = q_full + 16, item_full = q_empty + 16, item_empty = item_full + 16,
+                 o_empty = item_empty + 16, info_full = o_empty + 8, info_empty = info_full + 8, drain = info_empty + 8;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int W = p.W, B = p.B, Hkv = p.Hkv, g = p.g;
+
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 2); bar_init(ready + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) {
+      bar_init(s_full + 8 * s, 1);
+      bar_init(p_full + 8 * s, 4);
+      bar_init(o_full + 8 * s, 1);
+      bar_init(q_full + 8 * s, 1);
+      bar_init(q_empty + 8 * s, 1);
+      bar_init(item_full + 8 * s, 1);
+      bar_init(item_empty + 8 * s, 2 + 8);               // MMA lane, patch warp, softmax warps
+    }
+    bar_init(o_empty, 8);
+    bar_init(info_full, 1);
+    bar_init(info_empty, 8);
+    bar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sb + SM::OFF_MISC + 4), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = (uint32_t)misc[1];
+  const uint32_t tS[2] = {tmem, tmem + TN}, tO[2] = {tmem + 2 * TN, tmem + 2 * TN + D};
+
+  // Ring position of an item's K and V tiles, counted from its first: with two row tiles K0 V0 K1 V1 ..; with one, the next
+  // K tile of a stream is wanted before the V tile of the other: K0 K1 V0 K2 V1 K3 ..
+  auto pos_k = [](int i, bool two) -> int { return two ? 2 * i : (i < 2 ? i : 2 * i - 1); };
+  auto pos_v = [](int i, int n, bool two) -> int { return two ? 2 * i + 1 : (i == n - 1 ? 2 * n - 1 : 2 * i + 2); };
+
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TT_REGS_LOW));
+  if (warp == 0) {
+    // ================================================================ producer
+    if (lane == 0) {
+      uint32_t pos = 0, qn = 0, seq = 0;                 // ring entries, Q tiles and items so far
+      bool okay = true;
+      int item = (int)blockIdx.x;
+      while (okay) {
+        const int last_grab = a.n_items + (int)gridDim.x - 1;
+        if (item >= a.n_items) {
+          if (item == last_grab) *p.work = 0;            // the launch's last grab rewinds the counter
+          if (bar_wait(item_empty + 8 * (seq & 1), ((seq >> 1) & 1) ^ 1, abort_flag)) {
+            desc[(seq & 1) * 32 + I_KIND] = 0;
+            bar_arrive(item_full + 8 * (seq & 1));
+          } else {
+            okay = false;
+          }
+          break;
+        }
+        const int next = atomicAdd(p.work, 1) + (int)gridDim.x;
+        int blk, piece = 0, pieces = 1, split = -1;
+        if (item < a.n_full) {
+          blk = item;
+        } else {
+          split = (item - a.n_full) / a.P;
+          piece = item - a.n_full - split * a.P;
+          pieces = a.P;
+          blk = a.n_full + split;
+        }
+        item = next;
+        const int unit = blk / a.nqp, qp = blk - unit * a.nqp;
+        const int e = unit / Hkv, h = unit - e * Hkv;
+        const int li = e / B, b = e - li * B;
+        const size_t lb = (size_t)(a.l0 + li) * B + b;
+        const int act = a.active != nullptr ? a.active[b] : 1;
+        const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
+        TreeRing r;
+        const bool ring_ok = tree_ring(p, lb, &r);
+        if (act == 0) continue;
+        if (!ring_ok || n < 0 || n > a.NT) {
+          atomicOr(p.status, PTENC_ST_BAD_INDEX);
+          continue;
+        }
+        const int node0 = qp * 2 * a.npt;
+        if (node0 >= n) continue;
+        const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
+        int t0, len2;
+        int head2 = r.head + ev0;
+        if (head2 >= r.cap) head2 -= r.cap;
+        const int nt = tt_tiles(r.sink, head2, r.count - ev0, W, &t0, &len2) + 1;     // the draft's own tile is the last
+        if (pieces > nt) pieces = nt;
+        if (piece >= pieces) continue;
+        const int lo = (int)((long long)piece * nt / pieces);
+        const int cnt = (int)((long long)(piece + 1) * nt / pieces) - lo;
+        const bool two = n - node0 > a.npt;
+        const uint32_t slot = seq & 1;
+        if (!bar_wait(item_empty + 8 * slot, ((seq >> 1) & 1) ^ 1, abort_flag)) { okay = false; break; }
+        volatile int* d = desc + slot * 32;
+        d[I_LI] = li; d[I_B] = b; d[I_H] = h; d[I_NODE0] = node0; d[I_N] = n; d[I_TWO] = two ? 1 : 0;
+        d[I_HEAD] = r.head; d[I_COUNT] = r.count; d[I_SINK] = r.sink; d[I_E] = r.e; d[I_T0] = t0; d[I_LEN2] = len2;
+        d[I_LO] = lo; d[I_CNT] = cnt; d[I_NT] = nt; d[I_PIECES] = pieces; d[I_PIECE] = piece;
+        d[I_SPLIT] = pieces > 1 ? split : -1;
+        d[I_KIND] = 1;
+        bar_arrive(item_full + 8 * slot);
+        ++seq;
+        const int row = (li * B + b) * a.NT;             // first node of the sequence in the call's tensors
+        for (int t = 0; t < (two ? 2 : 1); ++t, ++qn) {
+          const uint32_t qs = qn & 1;
+          if (!bar_wait(q_empty + 8 * qs, ((qn >> 1) & 1) ^ 1, abort_flag)) { okay = false; break; }
+          bar_expect(q_full + 8 * qs, (uint32_t)(DH * g * a.npt * 128));
+          for (int hf = 0; hf < DH; ++hf)
+            tma_3d(sb + SM::OFF_Q + qs * TILE + hf * HALF, &tmQ, hf * 64, h * g, row + node0 + t * a.npt, q_full + 8 * qs);
+        }
+        if (!okay) break;
+        const int z = (int)(lb * Hkv + h);
+        for (int k = 0; k < 2 * cnt; ++k, ++pos) {
+          // entry k of the item: which tile, and whether its K or its V
+          int i;
+          bool is_v;
+          if (two) { i = k >> 1; is_v = k & 1; }
+          else if (k < 2 && cnt > 1) { i = k; is_v = false; }
+          else if (k == 2 * cnt - 1) { i = cnt - 1; is_v = true; }
+          else if (k & 1) { i = (k + 1) >> 1; is_v = false; }
+          else { i = cnt > 1 ? (k - 2) >> 1 : 0; is_v = cnt > 1; }
+          const uint32_t s = pos % NS, bar = full + 8 * s, dst = sb + s * TILE;
+          if (!bar_wait(empty + 8 * s, ((pos / NS) & 1) ^ 1, abort_flag)) { okay = false; break; }
+          if (lo + i == nt - 1) {
+            bar_expect(bar, (uint32_t)(DH * a.nb * 128));
+            for (int hf = 0; hf < DH; ++hf) tma_3d(dst + hf * HALF, is_v ? &tmVt : &tmKt, hf * 64, h, row, bar);
+          } else {
+            const int u = lo + i;
+            const int j = u < len2 ? t0 + u : u - len2;
+            bar_expect(bar, (uint32_t)(DH * a.ring_box * 128));
+            for (int hf = 0; hf < DH; ++hf) tma_3d(dst + hf * HALF, is_v ? &tmV : &tmK, hf * 64, j * TN, z, bar);
+          }
+        }
+      }
+      if (!okay) { atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT); *abort_flag = 1; }
+      // whatever the other roles did, copies in flight land before the shared memory goes away
+      for (uint32_t i = 1; i <= (uint32_t)NS && i <= pos; ++i)
+        for (uint32_t k = 0; k < TT_POLLS; ++k)
+          if (bar_try(full + 8 * ((pos - i) % NS), ((pos - i) / NS) & 1)) break;
+      for (uint32_t i = 1; i <= 2 && i <= qn; ++i)
+        for (uint32_t k = 0; k < TT_POLLS; ++k)
+          if (bar_try(q_full + 8 * ((qn - i) & 1), ((qn - i) >> 1) & 1)) break;
+    }
+  } else if (warp == 1) {
+    // ================================================================ MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t ID_QK = tt_idesc(TN, 0), ID_PV = tt_idesc(D, 1);
+      const uint32_t ID_QKD = tt_idesc(a.nb, 0);
+      uint32_t base = 0, qn = 0, seq = 0, items = 0;
+      uint32_t np = 0;                                   // bit st: parity of the softmax results consumed of stream st
+      bool okay = true;
+      while (okay) {
+        if (!bar_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag)) { okay = false; break; }
+        volatile int* d = desc + (seq & 1) * 32;
+        if (d[I_KIND] == 0) break;
+        const bool two = d[I_TWO] != 0;
+        const int n = d[I_CNT];
+        const int draft = d[I_NT] - 1 - d[I_LO];         // the draft's tile, if it is among the item's
+        bar_arrive(item_empty + 8 * (seq & 1));
+        ++seq;
+        const uint32_t q0 = qn, nq = two ? 2 : 1;
+        auto issue_s = [&](int i, int st, int qt, bool release) -> bool {
+          const uint32_t ps = base + pos_k(i, two), s = ps % NS;
+          if (!bar_wait(full + 8 * s, (ps / NS) & 1, abort_flag)) return false;
+          fence_after();
+          const uint32_t qa = sb + SM::OFF_Q + ((q0 + qt) & 1) * TILE, ka = sb + s * TILE;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k >> 2) * HALF + (k & 3) * 32;
+            mma_ss(tS[st], desc_k(qa + off), desc_k(ka + off), i == draft ? ID_QKD : ID_QK, k > 0);
+          }
+          commit(s_full + 8 * st);
+          if (release) commit(empty + 8 * s);
+          return true;
+        };
+        bool first = true;
+        auto issue_pv = [&](int i, int st, bool start, bool end, bool release) -> bool {
+          if (!bar_wait(p_full + 8 * st, (np >> st) & 1, abort_flag)) return false;
+          np ^= 1u << st;
+          if (first && !bar_wait(o_empty, (items & 1) ^ 1, abort_flag)) return false;   // O of the item before is out
+          first = false;
+          const uint32_t ps = base + pos_v(i, n, two), s = ps % NS;
+          if (!bar_wait(full + 8 * s, (ps / NS) & 1, abort_flag)) return false;
+          if (!bar_wait(ready + 8 * s, (ps / NS) & 1, abort_flag)) return false;
+          fence_after();
+          const int ks = i == draft ? a.nb / 16 : TN / 16;
+          for (int k = 0; k < ks; ++k)
+            mma_ts(tO[st], tS[st] + 8 * k, desc_mn(sb + s * TILE + k * 2048), ID_PV, (!start || k > 0) ? 1u : 0u);
+          if (release) commit(empty + 8 * s);
+          if (end) commit(o_full + 8 * st);
+          return true;
+        };
+        for (uint32_t t = 0; t < nq && okay; ++t)
+          okay = bar_wait(q_full + 8 * ((q0 + t) & 1), ((q0 + t) >> 1) & 1, abort_flag);
+        if (two) {
+          okay = okay && issue_s(0, 0, 0, false) && issue_s(0, 1, 1, true);
+          for (int i = 0; i < n && okay; ++i) {
+            okay = issue_pv(i, 0, i == 0, i == n - 1, false) && (i + 1 >= n || issue_s(i + 1, 0, 0, false)) &&
+                   issue_pv(i, 1, i == 0, i == n - 1, true) && (i + 1 >= n || issue_s(i + 1, 1, 1, true));
+          }
+        } else {
+          okay = okay && issue_s(0, 0, 0, true) && (n < 2 || issue_s(1, 1, 0, true));
+          for (int i = 0; i < n && okay; ++i)
+            okay = issue_pv(i, i & 1, i < 2, i >= n - 2, true) && (i + 2 >= n || issue_s(i + 2, i & 1, 0, true));
+        }
+        if (okay)
+          for (uint32_t t = 0; t < nq; ++t) commit(q_empty + 8 * ((q0 + t) & 1));
+        qn += nq;
+        base += 2 * n;
+        ++items;
+      }
+      if (!okay) { atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT); *abort_flag = 1; }
+      commit(drain);                                     // MMAs still in flight finish before tensor memory is freed
+      for (uint32_t k = 0; k < TT_POLLS; ++k)
+        if (bar_try(drain, 0)) break;
+    }
+  } else if (warp == 2) {
+    // ================================================================ patch warp
+    uint32_t base = 0, seq = 0;
+    bool okay = true;
+    // the lanes give up together, or not at all
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+      return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag));
+    };
+    while (okay) {
+      if (!wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + (seq & 1) * 32;
+      if (d[I_KIND] == 0) break;
+      const bool two = d[I_TWO] != 0;
+      const int n = d[I_CNT], nodes = d[I_N], lo = d[I_LO], nt = d[I_NT], t0 = d[I_T0], len2 = d[I_LEN2];
+      TreeRing r;
+      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_E];
+      // ---- what each node sees: the parent relation closed by pointer doubling, two nodes per lane -----------------------
+      const int32_t* par = a.parent + (size_t)d[I_B] * a.NT;
+      int pa[2];
+      unsigned long long anc[2] = {0ull, 0ull};
+      int bad = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int i = lane + 32 * x;
+        pa[x] = -1;
+        if (i < nodes) {
+          const int v = par[i];
+          if (v < -1 || v >= i) bad = 1; else pa[x] = v;
+          anc[x] = 1ull << i;
+        }
+      }
+      bad = __any_sync(0xffffffffu, bad);
+      if (bad) { pa[0] = pa[1] = -1; }
+      if (!wait(info_empty, (seq & 1) ^ 1)) { okay = false; break; }   // the rows have what they need of the last
+      for (int s = 1; s < nodes; s <<= 1) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          s_vis[lane + 32 * x] = anc[x];
+          s_jump[lane + 32 * x] = (int8_t)pa[x];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (pa[x] >= 0) { anc[x] |= s_vis[pa[x]]; pa[x] = s_jump[pa[x]]; }
+        __syncwarp();
+      }
+      int deepest = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int depth = __popcll(anc[x]) - 1;
+        s_depth[lane + 32 * x] = (uint8_t)(depth < 0 ? 0 : depth);
+        deepest = max(deepest, depth);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int gone = tree_evicted(r.count, r.cap, r.e, __popcll(anc[x]));
+        unsigned long long v = anc[x];
+        if (gone > r.count) {                            // a path longer than the ring: its first tokens have left again
+          v = 0;
+          for (unsigned long long m = anc[x]; m != 0; m &= m - 1) {
+            const int j = __ffsll((long long)m) - 1;
+            if (r.count + s_depth[j] >= gone) v |= 1ull << j;
+          }
+        }
+        s_vis[lane + 32 * x] = v;
+      }
+      deepest = __reduce_max_sync(0xffffffffu, deepest);
+      const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
+      const int ev_max = tree_evicted(r.count, r.cap, r.e, deepest + 1);
+      if (lane == 0) {
+        if (bad) atomicOr(p.status, PTENC_ST_BAD_INDEX);
+        d[I_EVMAX] = ev_max;
+        d[I_VALID] = bad ? 0 : 1;
+        d[I_ODD] = 0;
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(info_full);
+      // ---- pass the stages on, in ring order --------------------------------------------------------------------------------
+      for (int k = 0; k < 2 * n; ++k) {
+        int i = -1;                                      // the tile whose V this entry is, if it is one
+        if (two) { if (k & 1) i = k >> 1; }
+        else if (k == 2 * n - 1) i = n - 1;
+        else if (k >= 2 && (k & 1) == 0) i = (k - 2) >> 1;
+        const uint32_t ps = base + k, s = ps % NS;
+        if (!wait(full + 8 * s, (ps / NS) & 1)) { okay = false; break; }
+        if (i >= 0) {
+          const int u = lo + i;
+          const bool draft = u == nt - 1;
+          const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
+          bool clean = false;
+          if (!draft) {
+            int d0 = slot0 - r.sink - r.head;
+            if (d0 < 0) d0 += r.cap;
+            clean = slot0 + TN <= r.sink ||
+                    (slot0 >= r.sink && slot0 + TN <= W &&
+                     ((d0 >= ev_max && d0 + TN <= r.count) || (ev_max == 0 && r.count == r.cap)));
+          }
+          if (!clean) {
+            uint8_t* v = smem + s * TILE;
+            constexpr int VPR = DH * 8;                  // 16-byte vectors of a row
+            const int rows = draft ? a.nb : TN;
+            int odd = 0;
+            for (int x = lane; x < rows * VPR; x += 32) {
+              const int t = x / VPR, c = x - t * VPR;
+              bool dead, some;
+              if (draft) {
+                dead = t >= nodes;
+                some = !dead;
+              } else {
+                const int slot = slot0 + t;
+                int dd = slot - r.sink - r.head;
+                if (dd < 0) dd += r.cap;
+                dead = slot >= r.sink && (slot >= W || dd < ev0 || dd >= r.count);
+                some = !dead && slot >= r.sink && dd < ev_max;
+              }
+              uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * HALF + t * 128 + (c & 7) * 16);
+              if (dead) {
+                *at = make_uint4(0u, 0u, 0u, 0u);
+              } else if (some) {
+                uint4 w = *at;
+                uint32_t* e = reinterpret_cast<uint32_t*>(&w);
+                int hit = 0;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {            // exponent bits all set: infinity or NaN
+                  if ((e[y] & 0x7f80u) == 0x7f80u) { e[y] &= 0xffff0000u; hit = 1; }
+                  if ((e[y] & 0x7f800000u) == 0x7f800000u) { e[y] &= 0x0000ffffu; hit = 1; }
+                }
+                if (hit) { *at = w; odd = 1; }
+              }
+            }
+            if (__any_sync(0xffffffffu, odd) && lane == 0) d[I_ODD] = 1;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+        }
+        if (lane == 0) { bar_arrive(ready + 8 * s); bar_arrive(empty + 8 * s); }
+      }
+      if (!okay) break;
+      __syncwarp();
+      if (lane == 0) bar_arrive(item_empty + 8 * (seq & 1));
+      ++seq;
+      base += 2 * n;
+    }
+    if (!okay && lane == 0) { atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT); *abort_flag = 1; }
+  }
+  } else {
+    // ================================================================ softmax: stream st, a row per thread
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TT_REGS_HIGH));
+    const int st = (warp - 4) >> 2, quarter = warp & 3;
+    const int lrow = 32 * quarter + lane;
+    const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
+    const float sl2 = 1.4426950408889634f / sqrtf((float)D);
+    uint32_t seq = 0, ns = 0;                            // items; tiles of this stream
+    uint32_t no0 = 0, no1 = 0;                           // items in which the streams had tiles
+    bool fine = true;                                    // a wait that ran out: go through the motions, never wait again
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (fine && !bar_wait(bar, parity, abort_flag)) {
+        fine = false;
+        atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT);
+        *abort_flag = 1;
+      }
+    };
+    while (true) {
+      // one thread waits for the item and posts what all warps then read, so that they agree on going on
+      if (tid == TT_LEAD) {
+        int v = 0;
+        if (*abort_flag == 0 && bar_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag)) v = desc[(seq & 1) * 32 + I_KIND];
+        misc[2] = v;
+      }
+      soft_sync();
+      if (misc[2] != 1) break;
+      wait(item_full + 8 * (seq & 1), (seq >> 1) & 1);
+      wait(info_full, seq & 1);
+      volatile int* d = desc + (seq & 1) * 32;
+      const bool two = d[I_TWO] != 0;
+      const int n = d[I_CNT], nodes = d[I_N], lo = d[I_LO], nt = d[I_NT], t0 = d[I_T0], len2 = d[I_LEN2];
+      const int ev_max = d[I_EVMAX], valid = d[I_VALID];
+      TreeRing r;
+      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_E];
+      const int node_l = lrow / g, hh = lrow - node_l * g;
+      const int node = d[I_NODE0] + (two ? st * a.npt : 0) + node_l;
+      const bool real = node_l < a.npt && node < nodes;
+      const unsigned long long vis = real ? s_vis[node] : 0ull;
+      const int ev = real ? tree_evicted(r.count, r.cap, r.e, s_depth[node] + 1) : 0;
+      const bool idle = __all_sync(0xffffffffu, !real);  // a warp without rows only keeps the barriers going
+      __syncwarp();
+      if (lane == 0) bar_arrive(info_empty);
+      auto sees = [&](int slot) -> bool {
+        int dd = slot - r.sink - r.head;
+        if (dd < 0) dd += r.cap;
+        return slot < r.sink || (slot < W && dd >= ev && dd < r.count);
+      };
+      float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and sum
+      bool started = false;
+      for (int i = two ? 0 : st; i < n; i += two ? 1 : 2, ++ns) {
+        const int u = lo + i;
+        const bool draft = u == nt - 1;
+        const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
+        bool clean = false;
+        if (!draft) {
+          int d0 = slot0 - r.sink - r.head;
+          if (d0 < 0) d0 += r.cap;
+          clean = slot0 + TN <= r.sink ||
+                  (slot0 >= r.sink && slot0 + TN <= W &&
+                   ((d0 >= ev_max && d0 + TN <= r.count) || (ev_max == 0 && r.count == r.cap)));
+        }
+        wait(s_full + 8 * st, ns & 1);
+        fence_after();
+        if (!idle) {
+          float x[TN];
+          const uint32_t ts = tS[st] + lane_off;
+          const int chunks = draft ? (a.nb + 31) / 32 : 4;             // 32-column chunks in use
+          ld32(ts, x);
+          ld32(ts + 32, x + 32);
+          ld32(ts + 64, x + 64);
+          ld32(ts + 96, x + 96);
+          wait_ld();
+          if (draft) {
+#pragma unroll
+            for (int c = 0; c < TN; ++c)
+              if (c >= TREE_MAX || !((vis >> (c & 63)) & 1ull)) x[c] = -INFINITY;
+          } else if (!clean) {
+#pragma unroll
+            for (int c = 0; c < TN; ++c)
+              if (!sees(slot0 + c)) x[c] = -INFINITY;
+          }
+          float mx[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+          for (int c = 4; c < TN; c += 4) {
+            mx[0] = fmaxf(mx[0], x[c]); mx[1] = fmaxf(mx[1], x[c + 1]);
+            mx[2] = fmaxf(mx[2], x[c + 2]); mx[3] = fmaxf(mx[3], x[c + 3]);
+          }
+          const float mnew = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+          if (!started) {
+            m = mnew;
+          } else {
+            const bool grown = (mnew - m) * sl2 > 8.f;   // false while nothing has been seen (NaN)
+            if (__any_sync(0xffffffffu, grown)) {
+              const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
+              if (grown) m = mnew;
+              l *= corr;
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                float o[32];
+                ld32(tO[st] + lane_off + c, o);
+                wait_ld();
+#pragma unroll
+                for (int y = 0; y < 32; ++y) o[y] *= corr;
+                st32(tO[st] + lane_off + c, reinterpret_cast<uint32_t*>(o));
+              }
+            }
+          }
+          const float neg = m == -INFINITY ? 0.f : -m * sl2;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < TN; c += 32) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int y = 0; y < 32; y += 2) {
+              const float p0 = tt_ex2(fmaf(x[c + y], sl2, neg)), p1 = tt_ex2(fmaf(x[c + y + 1], sl2, neg));
+              sum[(y >> 1) & 3] += p0 + p1;
+              pk[y >> 1] = tt_pack(p0, p1);
+            }
+            if (c < 32 * chunks) st16(ts + c / 2, pk);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          wait_st();
+        }
+        started = true;
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_full + 8 * st);
+      }
+      // ---- the item's rows ------------------------------------------------------------------------------------------------
+      const bool both = two || n > 1;                    // the second stream had tiles
+      if (!two || st == 0) wait(o_full, no0 & 1);
+      if (both && (!two || st == 1)) wait(o_full + 8, no1 & 1);
+      ++no0;
+      if (both) ++no1;
+      fence_after();
+      const bool odd = d[I_ODD] != 0;
+      const int split = d[I_SPLIT], pieces = d[I_PIECES], piece = d[I_PIECE];
+      const int li = d[I_LI], b = d[I_B], h = d[I_H];
+      const size_t lb = (size_t)(a.l0 + li) * B + b;
+      m *= sl2;                                          // base-2 units from here on (-inf stays)
+      // with one row tile both streams hold parts of the same rows: join (m, l), each half of the threads takes half of
+      // the columns of both
+      float w0 = 1.f, w1 = 0.f;
+      int c_lo = 0, c_hi = D;
+      if (!two) {
+        if (st == 1) s_ml[lrow] = make_float2(m, l);
+        soft_sync();
+        if (st == 0) {
+          const float2 o = s_ml[lrow];
+          const float mm = fmaxf(m, o.x);
+          w0 = m == -INFINITY ? 0.f : tt_ex2(m - mm);
+          w1 = o.x == -INFINITY ? 0.f : tt_ex2(o.x - mm);
+          l = w0 * l + w1 * o.y;
+          m = mm;
+          s_ml[lrow] = make_float2(w0, w1);
+        }
+        soft_sync();
+        if (st == 1) { const float2 o = s_ml[lrow]; w0 = o.x; w1 = o.y; }
+        soft_sync();
+        if (st == 0) s_ml[lrow] = make_float2(m, l);
+        soft_sync();
+        if (st == 1) { const float2 o = s_ml[lrow]; m = o.x; l = o.y; }
+        c_lo = st * (D / 2);
+        c_hi = c_lo + D / 2;
+      }
+      const size_t orow = ((size_t)(li * B + b) * a.NT + node) * p.Hq + (size_t)h * g + hh;
+      const float inv = 1.f / l;
+      const int tile_i = two ? st : 0;
+      const size_t pslot = split >= 0 ? (((size_t)split * a.P + piece) * a.tpb + tile_i) : 0;
+      float4* part = reinterpret_cast<float4*>(a.part) + pslot * (D / 4) * TM;
+#pragma unroll 1
+      for (int c = c_lo; c < c_hi; c += 32) {
+        float o[32];
+        if (idle) continue;
+        if (two) {
+          ld32(tO[st] + lane_off + c, o);
+          wait_ld();
+        } else {
+          float o1[32];
+          ld32(tO[0] + lane_off + c, o);
+          if (both) ld32(tO[1] + lane_off + c, o1);
+          wait_ld();
+#pragma unroll
+          for (int y = 0; y < 32; ++y) o[y] = both ? fmaf(o1[y], w1, o[y] * w0) : o[y] * w0;
+        }
+        if (odd && real) {
+          // V values that are not finite were left out of the products: they reach the rows that see their token
+          for (int i = 0; i < n; ++i) {
+            const int u = lo + i;
+            const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
+            const bool draft = u == nt - 1;
+            for (int t = 0; t < (draft ? nodes : TN); ++t) {
+              const __nv_bfloat16* vr;
+              if (draft) {
+                if (!((vis >> t) & 1ull)) continue;
+                vr = a.v_tree + (((size_t)(li * B + b) * a.NT + t) * Hkv + h) * D;
+              } else {
+                int dd = slot0 + t - r.sink - r.head;
+                if (dd < 0) dd += r.cap;
+                if (slot0 + t < r.sink || slot0 + t >= W || dd < ev || dd >= ev_max || dd >= r.count) continue;
+                vr = reinterpret_cast<const __nv_bfloat16*>(p.V) + ((lb * Hkv + h) * W + slot0 + t) * D;
+              }
+#pragma unroll
+              for (int y = 0; y < 32; ++y) {
+                const float v = __bfloat162float(vr[c + y]);
+                if (!isfinite(v)) o[y] += v;
+              }
+            }
+          }
+        }
+        if (split >= 0) {
+          if (real)
+#pragma unroll
+            for (int y = 0; y < 32; y += 4)
+              part[((c + y) >> 2) * TM + lrow] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+        } else if (real && valid) {
+          uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
+#pragma unroll
+          for (int y = 0; y < 32; y += 8)
+            dst[y >> 3] = make_uint4(tt_pack(o[y] * inv, o[y + 1] * inv), tt_pack(o[y + 2] * inv, o[y + 3] * inv),
+                                     tt_pack(o[y + 4] * inv, o[y + 5] * inv), tt_pack(o[y + 6] * inv, o[y + 7] * inv));
+        }
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) { bar_arrive(o_empty); bar_arrive(item_empty + 8 * (seq & 1)); }
+      const bool writes_lse = real && valid && (two || st == 0);
+      if (split < 0) {
+        if (writes_lse && a.lse != nullptr) a.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
+      } else {
+        // ---- a part of the block's tiles: the CTA that arrives last joins the parts in order ----------------------------
+        if (real && (two || st == 0)) a.part_ml[pslot * TM + lrow] = make_float2(m, l);
+        __threadfence();
+        soft_sync();
+        if (tid == TT_LEAD) {
+          const int old = atomicAdd(&a.tickets[split], 1);
+          const int last = old == pieces - 1;
+          if (last) a.tickets[split] = 0;
+          misc[3] = last;
+        }
+        soft_sync();
+        if (misc[3] && real) {
+          __threadfence();
+          const size_t ps0 = (size_t)split * a.P * a.tpb + tile_i, step = a.tpb;
+          float mm = -INFINITY;
+          for (int q = 0; q < pieces; ++q) mm = fmaxf(mm, __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]).x);
+          float ll = 0.f;
+          for (int q = 0; q < pieces; ++q) {
+            const float2 v = __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]);
+            ll += (v.x == -INFINITY ? 0.f : tt_ex2(v.x - mm)) * v.y;
+          }
+          const float linv = 1.f / ll;
+#pragma unroll 1
+          for (int c = c_lo; c < c_hi; c += 8) {
+            float acc[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) acc[y] = 0.f;
+            for (int q = 0; q < pieces; ++q) {
+              const float mq = __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]).x;
+              if (mq == -INFINITY) continue;             // a part in which the row sees nothing
+              const float w = tt_ex2(mq - mm);
+              const float4* src = reinterpret_cast<const float4*>(a.part) + (ps0 + q * step) * (D / 4) * TM + (c >> 2) * TM + lrow;
+              const float4 v0 = __ldcg(src), v1 = __ldcg(src + TM);
+              acc[0] = fmaf(w, v0.x, acc[0]); acc[1] = fmaf(w, v0.y, acc[1]); acc[2] = fmaf(w, v0.z, acc[2]);
+              acc[3] = fmaf(w, v0.w, acc[3]); acc[4] = fmaf(w, v1.x, acc[4]); acc[5] = fmaf(w, v1.y, acc[5]);
+              acc[6] = fmaf(w, v1.z, acc[6]); acc[7] = fmaf(w, v1.w, acc[7]);
+            }
+            if (valid)
+              *reinterpret_cast<uint4*>(a.out + orow * D + c) =
+                  make_uint4(tt_pack(acc[0] * linv, acc[1] * linv), tt_pack(acc[2] * linv, acc[3] * linv),
+                             tt_pack(acc[4] * linv, acc[5] * linv), tt_pack(acc[6] * linv, acc[7] * linv));
+          }
+          if (writes_lse && a.lse != nullptr) a.lse[orow] = (mm + log2f(ll)) * 0.6931471805599453f;
+        }
+      }
+      ++seq;
+      soft_sync();                                       // misc and the exchange buffer are free again
+    }
+  }
+
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+typedef CUresult (*TtEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+TtEncodeFn tt_encode_fn() {
+  static TtEncodeFn fn = nullptr;
+  if (fn != nullptr) return fn;
+  void* ptr = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) != cudaSuccess ||
+      qres != cudaDriverEntryPointSuccess)
+    return nullptr;
+  fn = reinterpret_cast<TtEncodeFn>(ptr);
+  return fn;
+}
+
+// bf16 [n2][n1][D], box [b2][b1][64], 128-byte swizzle; what lies outside the tensor reads as zero.
+bool tt_map(CUtensorMap* map, const void* base, int D, long long n1, long long n2, int b1, int b2) {
+  TtEncodeFn fn = tt_encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)n1, (cuuint64_t)n2};
+  cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)n1 * D * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)b1, (cuuint32_t)b2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t tt_launch(ptenc_cache* c, const CUtensorMap& q, const CUtensorMap& kt, const CUtensorMap& vt,
+                      const TreeTcArgs& a, int grid, cudaStream_t st) {
+  static bool attr_done[PTENC_MAX_DEVICES] = {};
+  if (ptenc_first_use(attr_done, c->cfg.device)) {
+    cudaError_t e = cudaFuncSetAttribute(k_tree_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
+    if (e != cudaSuccess) return e;
+  }
+  k_tree_tc<D><<<grid, TT_THREADS, TSmem<D>::TOTAL, st>>>(c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
+  c->launches++;
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+// Bytes of the scratch that the parts of split blocks need: partial rows, their (m, l), arrival tickets.
+bool ptenc_tree_tc_shape(const ptenc_config* c) {
+  return c->dtype == PTENC_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128) && c->policy == PTENC_POLICY_FIFO &&
+         c->n_q_heads / c->n_kv_heads <= TM;
+}
+size_t ptenc_tree_part_bytes(const ptenc_config* c) { return (size_t)PTENC_TREE_SLOTS * TM * c->head_dim * 4; }
+size_t ptenc_tree_ml_bytes(const ptenc_config*) { return (size_t)PTENC_TREE_SLOTS * TM * 8; }
+
+bool ptenc_tree_tc_prepare(ptenc_cache* c) {
+  c->tree_tc = false;
+  if (!ptenc_tree_tc_shape(&c->cfg)) return false;
+  const PtencDev& p = c->dev;
+  const long long units = (long long)p.L * p.B * p.Hkv;
+  const int box = p.W < TN ? p.W : TN;
+  c->tree_tc = tt_map(&c->tmTreeK, p.K, p.D, p.W, units, box, 1) && tt_map(&c->tmTreeV, p.V, p.D, p.W, units, box, 1);
+  return c->tree_tc;
+}
+
+cudaError_t ptenc_launch_tree(ptenc_cache* c, int l0, int nl, const void* q, const void* k_tree, const void* v_tree,
+                              const int32_t* parent, const int32_t* n_nodes, int max_nodes, const uint8_t* active, void* out,
+                              float* lse, cudaStream_t st) {
+  const PtencDev& p = c->dev;
+  CUtensorMap mq, mk, mv;
+  const long long nodes = (long long)nl * p.B * max_nodes;
+  const int npt = c->tree_tc ? TM / p.g : 0, nb = (max_nodes + 15) / 16 * 16;
+  if (!c->tree_tc || nodes >= (1ll << 31) || !tt_map(&mq, q, p.D, p.Hq, nodes, p.g, npt) ||
+      !tt_map(&mk, k_tree, p.D, p.Hkv, nodes, 1, nb) || !tt_map(&mv, v_tree, p.D, p.Hkv, nodes, 1, nb))
+    return ptenc_launch_tree_generic(c, l0, nl, q, k_tree, v_tree, parent, n_nodes, max_nodes, active, out, lse, st);
+  TreeTcArgs a;
+  memset(&a, 0, sizeof(a));
+  a.l0 = l0; a.NT = max_nodes; a.npt = npt; a.tpb = max_nodes > npt ? 2 : 1;
+  a.nqp = (max_nodes + 2 * npt - 1) / (2 * npt);
+  a.nb = nb;
+  a.ring_box = p.W < TN ? p.W : TN;
+  a.parent = parent; a.n_nodes = n_nodes; a.active = active;
+  a.out = static_cast<__nv_bfloat16*>(out); a.lse = lse; a.v_tree = static_cast<const __nv_bfloat16*>(v_tree);
+  a.part = c->tree_part; a.part_ml = reinterpret_cast<float2*>(c->tree_ml); a.tickets = c->tree_tickets;
+  // Whole rounds of blocks, one block per SM; the blocks of the last, partial round are cut into P parts each, so that
+  // they fill the SMs too.  Cost in K/V tiles: a part pays about two for its start and end, a joined block about two more
+  // and a fraction per part.
+  const long long blocks = (long long)nl * p.B * p.Hkv * a.nqp;
+  if (blocks > (1ll << 30)) return cudaErrorInvalidValue;
+  const int sms = c->sm_count, rem = (int)(blocks % sms), nt = (p.W + TN - 1) / TN + 1;
+  a.n_full = (int)(blocks - rem);
+  a.P = 1;
+  float best = 1e30f;
+  for (int P = 1; P <= TT_MAX_PIECES && P <= nt && (rem * P * a.tpb <= PTENC_TREE_SLOTS || P == 1); ++P) {
+    const float cost = (float)((rem * P + sms - 1) / sms) * ((float)((nt + P - 1) / P) + 2.f) + (P > 1 ? 2.f + 0.15f * P : 0.f);
+    if (cost < best) { best = cost; a.P = P; }
+  }
+  a.n_items = a.n_full + rem * a.P;
+  const int grid = a.n_items < sms ? a.n_items : sms;
+  return p.D == 128 ? tt_launch<128>(c, mq, mk, mv, a, grid, st) : tt_launch<64>(c, mq, mk, mv, a, grid, st);
+}
