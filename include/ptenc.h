@@ -217,7 +217,7 @@ PTENC_API int ptenc_tree_attn(ptenc_cache* c, int layer, const void* q, const vo
  * These are what ptenc_commit_path takes.  Entries of p and q are finite and not negative; a row of p that sums to zero gives
  * next_token -1.  A sequence with n_nodes outside 1..max_nodes, a parent or a token out of range gets path -1, n_path 0,
  * next_token -1.  Outputs of inactive sequences are not written.  n_nodes, active nullable.  p and q 16-byte aligned, the
- * others 4.  PTENC_ESHAPE: max_nodes > PTENC_MAX_TREE. */
+ * others 4.  PTENC_ESHAPE: max_nodes > PTENC_MAX_TREE, batch > 2^24, vocab > 2^28. */
 PTENC_API int ptenc_verify_tree(const void* p, const void* q, int dtype, const int32_t* tokens, const int32_t* parent,
                                 const int32_t* n_nodes, const float* u, const uint8_t* active, int32_t batch,
                                 int32_t max_nodes, int32_t vocab, int32_t* path, int32_t* n_path, int32_t* next_token,

@@ -8,11 +8,16 @@
 //
 // What it costs.  Judging a first child needs two numbers of a row; only a rejection or the last draw needs whole rows,
 // and those are rows of one node.  So a sequence reads its tree, one number of p and q per node (all requested together),
-// and then one row of p, and of q if a child was rejected there, once per rejected child that has a younger sibling and
-// once for the draw; the repeats come from the caches.  The rows are spread over a cluster of CTAs.
+// and then, per rejection, one row of p and q (of p alone at a node without a rejection); the repeats at a node come from
+// the caches.  A row is spread over a cluster of CTAs, a stretch per warp; the draw finds the CTA, the warp and the vector
+// that hold the border from the sums of the last pass, so it re-reads one warp's stretch, a vector per thread.
 //
-// Arithmetic: r, its sums and the border of the draw are held in 64 bits.  Neighbouring borders of a row of 10^5 entries
-// are about as close as a 32-bit sum of them is wrong, so a 32-bit cumulative sum would draw another token now and then.
+// Arithmetic: with c_0 = 1 and q >= 0, k rejections of the same row leave r = w / c_k with
+//   w = max(p - C q, 0),  C = c_0 + .. + c_(k-1),  c_k = sum of w
+// (max(max(a - b, 0) - c, 0) = max(a - b - c, 0)), so a pass costs one multiply-add per entry however many siblings have
+// been rejected, and no division.  w, its sums and the border of the draw are held in 64 bits: neighbouring borders of a
+// row of 10^5 entries are about as close as a 32-bit sum of them is wrong, so a 32-bit cumulative sum would draw another
+// token now and then.
 #include <cooperative_groups.h>
 #include <string.h>
 
@@ -46,21 +51,33 @@ template <typename T> struct VfVec {
   static constexpr int N = 16 / (int)sizeof(T);
   T e[N];
 };
-// Entries [at, at + N) of a tensor of `total` entries; at is a multiple of N, at >= 0.
+// Vector v of a row whose storage starts at `base` (16-byte aligned, up to N - 1 entries before the row's first); `room`
+// entries of the tensor lie from there on.
 template <typename T>
-__device__ __forceinline__ VfVec<T> vf_load(const T* base, long long at, long long total) {
-  VfVec<T> v;
-  if (at + VfVec<T>::N <= total) {
-    *reinterpret_cast<uint4*>(v.e) = __ldg(reinterpret_cast<const uint4*>(base + at));
+__device__ __forceinline__ VfVec<T> vf_load(const T* base, int v, long long room) {
+  constexpr int N = VfVec<T>::N;
+  VfVec<T> x;
+  const long long at = (long long)v * N;
+  if (at + N <= room) {
+    *reinterpret_cast<uint4*>(x.e) = __ldg(reinterpret_cast<const uint4*>(base) + v);
   } else {
 #pragma unroll
-    for (int i = 0; i < VfVec<T>::N; ++i) v.e[i] = at + i < total ? base[at + i] : ptenc_from_float<T>(0.f);
+    for (int i = 0; i < N; ++i) x.e[i] = at + i < room ? base[at + i] : ptenc_from_float<T>(0.f);
   }
-  return v;
+  return x;
+}
+// Inclusive sums over the lanes of a warp.
+__device__ __forceinline__ double vf_scan(double x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double t = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += t;
+  }
+  return x;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(VF_THREADS)
+__global__ void __launch_bounds__(VF_THREADS, 2)
 k_verify_tree(const VerifyArgs a) {
   constexpr int N = VfVec<T>::N;
   cg::cluster_group cluster = cg::this_cluster();
@@ -68,33 +85,38 @@ k_verify_tree(const VerifyArgs a) {
   const int rank = (int)cluster.block_rank();
   const int b = blockIdx.x / CS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ int s_par[TREE_MAX], s_tok[TREE_MAX], s_path[TREE_MAX];
-  __shared__ double s_pv[TREE_MAX], s_qv[TREE_MAX], s_u[TREE_MAX];
-  __shared__ double s_norm[TREE_MAX];              // sums of the levels of r at the current node
-  __shared__ int s_rej[TREE_MAX];                  // tokens rejected at the current node
+  __shared__ int s_par[TREE_MAX], s_tok[TREE_MAX];
+  __shared__ double s_pv[TREE_MAX], s_qv[TREE_MAX];
+  __shared__ float s_u[TREE_MAX];
+  __shared__ int s_rej[TREE_MAX];                  // certain drafts: tokens rejected at the current node,
+  __shared__ double s_left[TREE_MAX];              // and what is left of their entries
   __shared__ double s_warp[VF_WARPS];
   __shared__ double s_cta[2];                      // this CTA's sum, read by the other CTAs; passes alternate
   __shared__ double s_all[VF_CLUSTER];
+  __shared__ int s_hit, s_tail;
 
   if (a.active != nullptr && a.active[b] == 0) return;            // the whole cluster
-  const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.T;
   const T* P = static_cast<const T*>(a.p);
   const T* Q = static_cast<const T*>(a.q);
-  int bad = n < 1 || n > a.T;
-  if (!bad && tid < n) {
+  const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.T;
+  int bad = 0;
+  if (tid < a.T) {
     const size_t at = (size_t)b * a.T + tid;
-    const int par = a.parent[at];
-    const int tok = a.tokens[at];
+    const int par = a.parent[at], tok = a.tokens[at];
+    s_u[tid] = a.u[at];
     s_par[tid] = par;
     s_tok[tid] = tok;
-    s_u[tid] = (double)a.u[at];
-    bad = tid == 0 ? par != -1 : (par < 0 || par >= tid || tok < 0 || tok >= a.V);
-    if (!bad && tid > 0) {
-      const long long x = ((long long)b * a.T + par) * a.V + tok;
-      s_pv[tid] = (double)ptenc_to_float(P[x]);
-      s_qv[tid] = Q != nullptr ? (double)ptenc_to_float(Q[x]) : 1.0;
+    if (tid < n) {
+      bad = tid == 0 ? par != -1 : (par < 0 || par >= tid || tok < 0 || tok >= a.V);
+      if (!bad && tid > 0) {
+        const long long x = ((long long)b * a.T + par) * a.V + tok;
+        const T pv = P[x], qv = Q != nullptr ? Q[x] : ptenc_from_float<T>(1.f);
+        s_pv[tid] = (double)ptenc_to_float(pv);
+        s_qv[tid] = (double)ptenc_to_float(qv);
+      }
     }
   }
+  bad |= n < 1 || n > a.T;
   if (__syncthreads_or(bad)) {                                    // the same verdict in every CTA of the cluster
     if (rank == 0) {
       for (int i = tid; i < a.T; i += VF_THREADS) a.path[(size_t)b * a.T + i] = -1;
@@ -103,46 +125,69 @@ k_verify_tree(const VerifyArgs a) {
     return;
   }
 
-  // r after `levels` rejections at the current node, for an entry with p, q and index x; a level whose sum was not
-  // positive starts over from p
-  int levels = 0;
-  auto level = [&](double pv, double qv, long long x, int upto) -> double {
-    double r = pv;
-    for (int k = 0; k < upto; ++k) {
-      const double qk = Q != nullptr ? qv : (x == (long long)s_rej[k] ? 1.0 : 0.0);
-      const double s = s_norm[k];
-      r = s > 0.0 ? fmax(r - qk, 0.0) / s : pv;
-    }
-    return r;
-  };
-  // weight of an entry in a pass: the last rejection's subtraction is not normalised yet
-  auto weight = [&](double pv, double qv, long long x, bool open) -> double {
-    if (!open) return level(pv, qv, x, levels);
-    const double qk = Q != nullptr ? qv : (x == (long long)s_rej[levels - 1] ? 1.0 : 0.0);
-    return fmax(level(pv, qv, x, levels - 1) - qk, 0.0);
-  };
-
-  int cur = 0;
-  int pass = 0;
-  const long long wslot = (long long)rank * VF_WARPS + warp, wslots = (long long)CS * VF_WARPS;
-  // One pass over the current node's row: every warp sums a stretch of its own, the sums of all CTAs end up in s_all.
-  // Vectors are aligned in memory, so the row's first one may begin inside the row before it.
-  auto row_total = [&](bool open) -> double {
+  // ---- a pass over the current node's row: weights max(p - C q, 0), a stretch of vectors per warp -----------------------
+  const int V = (int)a.V;
+  int cur = 0, pass = 0, nrej = 0;
+  double C = 0.0;
+  const T *pr = nullptr, *qr = nullptr;
+  int off = 0, nv = 0, per = 0;
+  long long room = 0;
+  auto take_row = [&]() {
     const long long row = ((long long)b * a.T + cur) * a.V;
-    const long long v0 = row / N, v1 = (row + a.V + N - 1) / N;
-    const long long per = (v1 - v0 + wslots - 1) / wslots;
-    const long long lo = v0 + wslot * per, hi = min(lo + per, v1);
-    const bool need_q = Q != nullptr && levels > 0;
-    double sum = 0.0;
-#pragma unroll 4
-    for (long long v = lo + lane; v < hi; v += 32) {
-      const VfVec<T> pv = vf_load(P, v * N, a.total);
-      VfVec<T> qv = pv;
-      if (need_q) qv = vf_load(Q, v * N, a.total);
+    off = (int)(row % N);                                         // entries of the first vector that belong to the row before
+    pr = P + (row - off);
+    qr = Q != nullptr ? Q + (row - off) : nullptr;
+    room = a.total - (row - off);
+    nv = (off + V + N - 1) / N;
+    per = (nv + CS * VF_WARPS - 1) / (CS * VF_WARPS);
+  };
+  // weights of vector v; x0: index of its first entry in the row
+  auto weigh = [&](const VfVec<T>& pv, const VfVec<T>& qv, int v, double (&w)[N]) {
+    const int x0 = v * N - off;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const long long x = v * N + i - row;
-        if (x >= 0 && x < a.V) sum += weight((double)ptenc_to_float(pv.e[i]), (double)ptenc_to_float(qv.e[i]), x, open);
+    for (int i = 0; i < N; ++i) w[i] = (double)ptenc_to_float(pv.e[i]);
+    if (C != 0.0) {
+      if (Q != nullptr) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const double d = fma(-C, (double)ptenc_to_float(qv.e[i]), w[i]);
+          w[i] = d > 0.0 ? d : 0.0;
+        }
+      } else {
+        for (int k = 0; k < nrej; ++k) {
+          const int at = s_rej[k] - x0;
+#pragma unroll
+          for (int i = 0; i < N; ++i) if (at == i) w[i] = s_left[k];
+        }
+      }
+    }
+    if (x0 < 0 || x0 + N > V) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) if (x0 + i < 0 || x0 + i >= V) w[i] = 0.0;
+    }
+  };
+  auto row_total = [&]() -> double {
+    const int lo = (rank * VF_WARPS + warp) * per, hi = min(lo + per, nv);
+    const bool need_q = Q != nullptr && C != 0.0;
+    double sum = 0.0;
+    constexpr int U = N == 4 ? 4 : 2;                             // vectors of p and of q in flight per lane: what 64 registers hold
+    for (int v0 = lo + lane; v0 < hi; v0 += 32 * U) {
+      VfVec<T> pv[U], qv[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int v = min(v0 + 32 * j, hi - 1);
+        pv[j] = vf_load(pr, v, room);
+        qv[j] = pv[j];
+        if (need_q) qv[j] = vf_load(qr, v, room);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (v0 + 32 * j < hi) {
+          double w[N];
+          weigh(pv[j], qv[j], v0 + 32 * j, w);
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum += w[i];
+        }
       }
     }
 #pragma unroll
@@ -150,13 +195,18 @@ k_verify_tree(const VerifyArgs a) {
     __syncthreads();                                              // the pass before is done with s_warp and s_all
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();
-    if (tid == 0) {
-      double t = 0.0;
-      for (int w = 0; w < VF_WARPS; ++w) t += s_warp[w];
-      s_cta[pass & 1] = t;
+    if (warp == 0) {
+      double t = lane < VF_WARPS ? s_warp[lane] : 0.0;
+#pragma unroll
+      for (int o = VF_WARPS / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+      if (lane == 0) s_cta[pass & 1] = t;
     }
-    cluster.sync();
-    if (tid < CS) s_all[tid] = *cluster.map_shared_rank(&s_cta[pass & 1], tid);
+    if (CS > 1) {
+      cluster.sync();
+      if (tid < CS) s_all[tid] = *cluster.map_shared_rank(&s_cta[pass & 1], tid);
+    } else if (tid == 0) {
+      s_all[0] = s_cta[pass & 1];
+    }
     __syncthreads();
     ++pass;
     double t = 0.0;
@@ -164,117 +214,130 @@ k_verify_tree(const VerifyArgs a) {
     return t;
   };
 
-  // ---- the walk: every thread of the cluster takes the same one --------------------------------------------------------
-  int len = 1;
-  bool open = false;                                              // a rejection whose sum has not been formed
-  if (tid == 0) s_path[0] = 0;
-  for (int i = 1; i < n; ++i) {
-    if (s_par[i] != cur) continue;
-    if (open) {
-      const double t = row_total(true);
-      if (tid == 0) s_norm[levels - 1] = t;
-      __syncthreads();
-      open = false;
-    }
-    const double r = level(s_pv[i], s_qv[i], s_tok[i], levels);
-    if (s_u[i] * s_qv[i] < r) {
-      if (tid == 0) s_path[len] = i;
-      ++len;
-      cur = i;
-      levels = 0;
-    } else {
-      __syncthreads();
-      if (tid == 0) s_rej[levels] = s_tok[i];
-      __syncthreads();
-      ++levels;
-      open = true;
+  // ---- the walk: every warp of the cluster takes the same one ------------------------------------------------------------
+  const int par0 = lane < n ? s_par[lane] : -2, par1 = lane + 32 < n ? s_par[lane + 32] : -2;
+  unsigned long long line = 1ull;                                 // the path's nodes; they come in rising order
+  double c = 1.0;                                                 // r = w / c
+  bool moved = true, summed = false;
+  while (moved) {
+    moved = false;
+    summed = false;
+    C = 0.0;
+    c = 1.0;
+    nrej = 0;
+    unsigned long long kids = (unsigned long long)__ballot_sync(0xffffffffu, par0 == cur) |
+                              (unsigned long long)__ballot_sync(0xffffffffu, par1 == cur) << 32;
+    for (; kids != 0 && !moved; kids &= kids - 1) {
+      const int i = __ffsll((long long)kids) - 1;
+      double w = s_pv[i];
+      int same = -1;                                              // certain drafts: the token was rejected before, as entry `same`
+      if (Q != nullptr) {
+        w = fmax(fma(-C, s_qv[i], w), 0.0);
+      } else {
+        for (int k = 0; k < nrej; ++k) if (s_rej[k] == s_tok[i]) { same = k; w = s_left[k]; }
+      }
+      if ((double)s_u[i] * s_qv[i] < w / c) {
+        line |= 1ull << i;
+        cur = i;
+        moved = true;
+        break;
+      }
+      take_row();
+      C += c;
+      if (Q == nullptr) {
+        __syncthreads();
+        if (tid == 0) {
+          const int k = same >= 0 ? same : nrej;
+          s_rej[k] = s_tok[i];
+          s_left[k] = fmax(w - c, 0.0);
+        }
+        if (same < 0) ++nrej;
+        __syncthreads();
+      }
+      c = row_total();
+      summed = c > 0.0;
+      if (!summed) { C = 0.0; c = 1.0; nrej = 0; }                // nothing left: the target's own row
     }
   }
   // ---- the draw ------------------------------------------------------------------------------------------------------------
-  double total = row_total(open);
-  if (open && !(total > 0.0)) {                                   // nothing left of r: the target's own row
-    levels = 0;
-    open = false;
-    total = row_total(false);
+  if (!summed) {
+    take_row();
+    c = row_total();
   }
-  const double border = s_u[0] * total;
+  const double border = (double)s_u[0] * c;
+  const int len = __popcll(line);
   if (rank == 0) {
-    for (int i = tid; i < a.T; i += VF_THREADS) a.path[(size_t)b * a.T + i] = i < len ? s_path[i] : -1;
+    if (tid < a.T) {
+      a.path[(size_t)b * a.T + tid] = -1;
+    }
+    __syncthreads();
+    if (tid < a.T && ((line >> tid) & 1ull)) a.path[(size_t)b * a.T + __popcll(line & ((1ull << tid) - 1))] = tid;
     if (tid == 0) {
       a.n_path[b] = len;
-      if (!(total > 0.0)) a.next[b] = -1;
+      if (!(c > 0.0)) a.next[b] = -1;
     }
   }
-  if (total > 0.0) {
+  if (c > 0.0) {
     // the CTA and the warp whose stretch holds the border; the last one with any weight if rounding puts it past the end
-    int owner = -1, last = 0;
-    double before = 0.0, cum = 0.0, before_last = 0.0;
-    for (int c = 0; c < CS; ++c) {
-      if (s_all[c] > 0.0) { last = c; before_last = cum; }
-      if (owner < 0 && cum + s_all[c] > border) { owner = c; before = cum; }
-      cum += s_all[c];
-    }
-    if (owner < 0) { owner = last; before = before_last; }
+    auto holder = [&](double x, double start, double* before) -> int {
+      const double inc = start + vf_scan(x, lane);
+      unsigned m = __ballot_sync(0xffffffffu, x > 0.0 && inc > border);
+      const unsigned some = __ballot_sync(0xffffffffu, x > 0.0);
+      const int at = m != 0 ? __ffs(m) - 1 : 31 - __clz(some);
+      *before = __shfl_sync(0xffffffffu, inc - x, at);
+      return at;
+    };
+    double before;
+    const int owner = holder(lane < CS ? s_all[lane] : 0.0, 0.0, &before);
     if (owner == rank) {
-      int mine = -1;
-      last = 0;
-      cum = before_last = before;
-      for (int w = 0; w < VF_WARPS; ++w) {
-        if (s_warp[w] > 0.0) { last = w; before_last = cum; }
-        if (mine < 0 && cum + s_warp[w] > border) { mine = w; before = cum; }
-        cum += s_warp[w];
-      }
-      if (mine < 0) { mine = last; before = before_last; }
-      if (mine == warp) {
-        const long long row = ((long long)b * a.T + cur) * a.V;
-        const long long v0 = row / N, v1 = (row + a.V + N - 1) / N;
-        const long long per = (v1 - v0 + wslots - 1) / wslots;
-        const long long lo = v0 + wslot * per, hi = min(lo + per, v1);
-        const bool need_q = Q != nullptr && levels > 0;
-        long long found = -1, tail = -1;                          // tail: the last entry with any weight so far
-        for (long long vb = lo; vb < hi && found < 0; vb += 32) {
-          const long long v = vb + lane;
-          double w[N], sum = 0.0;
-          long long my_tail = -1;
-          VfVec<T> pv, qv;
-          if (v < hi) {
-            pv = vf_load(P, v * N, a.total);
-            qv = pv;
-            if (need_q) qv = vf_load(Q, v * N, a.total);
-          }
+      const int mine = holder(lane < VF_WARPS ? s_warp[lane] : 0.0, before, &before);
+      const int lo = (rank * VF_WARPS + mine) * per, hi = min(lo + per, nv);
+      const bool need_q = Q != nullptr && C != 0.0;
+      if (tid == 0) { s_hit = 0x7fffffff; s_tail = -1; }
+      __syncthreads();                                            // s_warp is free too
+      for (int vb = lo; vb < hi; vb += VF_THREADS) {
+        const int v = vb + tid;
+        double w[N], sum = 0.0;
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const long long x = v * N + i - row;
-            w[i] = 0.0;
-            if (v < hi && x >= 0 && x < a.V)
-              w[i] = weight((double)ptenc_to_float(pv.e[i]), (double)ptenc_to_float(qv.e[i]), x, open);
-            if (w[i] > 0.0) my_tail = x;
-            sum += w[i];
-          }
-          double inc = sum;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double t = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += t;
-          }
-          double c = before + (inc - sum);
-          long long x_hit = -1;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            c += w[i];
-            if (x_hit < 0 && w[i] > 0.0 && c > border) x_hit = v * N + i - row;
-          }
-          const unsigned hit = __ballot_sync(0xffffffffu, x_hit >= 0);
-          if (hit != 0) found = __shfl_sync(0xffffffffu, x_hit, __ffs(hit) - 1);
-          const unsigned some = __ballot_sync(0xffffffffu, my_tail >= 0);
-          if (some != 0) tail = __shfl_sync(0xffffffffu, my_tail, 31 - __clz(some));
-          before += __shfl_sync(0xffffffffu, inc, 31);
+        for (int i = 0; i < N; ++i) w[i] = 0.0;
+        if (v < hi) {
+          const VfVec<T> pv = vf_load(pr, v, room);
+          VfVec<T> qv = pv;
+          if (need_q) qv = vf_load(qr, v, room);
+          weigh(pv, qv, v, w);
         }
-        if (lane == 0) a.next[b] = (int32_t)(found >= 0 ? found : tail);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += w[i];
+        const double inc = vf_scan(sum, lane);
+        if (lane == 31) s_warp[warp] = inc;
+        __syncthreads();
+        const double wsum = vf_scan(lane < VF_WARPS ? s_warp[lane] : 0.0, lane);
+        double at = before + (inc - sum);
+        const double prev = __shfl_sync(0xffffffffu, wsum, warp > 0 ? warp - 1 : 0);
+        if (warp > 0) at += prev;
+        int hit = 0x7fffffff, tail = -1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          at += w[i];
+          if (w[i] > 0.0) {
+            tail = v * N + i - off;
+            if (at > border && hit == 0x7fffffff) hit = tail;
+          }
+        }
+        hit = __reduce_min_sync(0xffffffffu, hit);
+        tail = __reduce_max_sync(0xffffffffu, tail);
+        if (lane == 0) {
+          if (hit != 0x7fffffff) atomicMin(&s_hit, hit);
+          if (tail >= 0) atomicMax(&s_tail, tail);
+        }
+        before += __shfl_sync(0xffffffffu, wsum, 31);
+        __syncthreads();
+        if (s_hit != 0x7fffffff) break;                           // uniform: nobody writes it before the next barrier
       }
+      if (tid == 0) a.next[b] = s_hit != 0x7fffffff ? s_hit : s_tail;
     }
   }
-  cluster.sync();                                                 // nobody leaves while its sum may still be read
+  if (CS > 1) cluster.sync();                                     // nobody leaves while its sum may still be read
 }
 
 template <typename T>
@@ -312,7 +375,7 @@ extern "C" int ptenc_verify_tree(const void* p, const void* q, int dtype, const 
     return PTENC_EINVAL;
   if (dtype != PTENC_DTYPE_FP32 && dtype != PTENC_DTYPE_BF16) return PTENC_EINVAL;
   if (batch < 1 || max_nodes < 1 || vocab < 1) return PTENC_EINVAL;
-  if (max_nodes > PTENC_MAX_TREE || batch > (1 << 24)) return PTENC_ESHAPE;
+  if (max_nodes > PTENC_MAX_TREE || batch > (1 << 24) || vocab > (1 << 28)) return PTENC_ESHAPE;
   if (off16(p) || off16(q) || off4(tokens) || off4(parent) || off4(n_nodes) || off4(u) || off4(path) || off4(n_path) ||
       off4(next_token))
     return PTENC_EALIGN;

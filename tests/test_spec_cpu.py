@@ -126,7 +126,7 @@ def _verify(**patch):
     (dict(u=None), bd.PTENC_EINVAL), (dict(path=None), bd.PTENC_EINVAL), (dict(n_path=None), bd.PTENC_EINVAL),
     (dict(next_token=None), bd.PTENC_EINVAL), (dict(dtype=2), bd.PTENC_EINVAL), (dict(dtype=-1), bd.PTENC_EINVAL),
     (dict(batch=0), bd.PTENC_EINVAL), (dict(max_nodes=0), bd.PTENC_EINVAL), (dict(vocab=0), bd.PTENC_EINVAL),
-    (dict(max_nodes=65), bd.PTENC_ESHAPE), (dict(batch=(1 << 24) + 1), bd.PTENC_ESHAPE),
+    (dict(max_nodes=65), bd.PTENC_ESHAPE), (dict(batch=(1 << 24) + 1), bd.PTENC_ESHAPE), (dict(vocab=(1 << 28) + 1), bd.PTENC_ESHAPE),
     (dict(p=24), bd.PTENC_EALIGN), (dict(q=8), bd.PTENC_EALIGN), (dict(u=6), bd.PTENC_EALIGN),
     (dict(path=5), bd.PTENC_EALIGN), (dict(n_nodes=2), bd.PTENC_EALIGN),
 ])
