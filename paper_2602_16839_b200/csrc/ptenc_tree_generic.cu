@@ -1,41 +1,74 @@
 // Attention of a draft tree over the cache, shape-generic kernel: fp32 or bf16 storage, any head_dim <= 256 that is a
 // multiple of 8, any query group size.
 //
-// out[i,h] = softmax(q[i,h] . K^T / sqrt(D)) V over the tokens node i sees (ptenc_tree.cuh).  A CTA takes 16 query rows
-// (row = node * g + head of the group) of one (layer, sequence, KV head) and walks the tokens 32 at a time: K and V rows
-// as fp32 in shared memory, a score per (lane = token, four rows per warp), the running maximum and sum of the softmax
-// per row, and the outputs of a row in the registers of eight threads.  fp32 FMA throughout (no TF32).
+// out[i,h] = softmax(q[i,h] . K^T / sqrt(D)) V over the tokens node i sees (ptenc_tree.cuh).  A CTA takes 32 query rows
+// (row = node * g + head of the group) of one (layer, sequence, KV head) and walks its tokens 64 at a time, the next tile
+// on its way (cp.async) while one is worked on.  A warp owns eight rows: a thread scores 4 rows x 4 tokens, the running
+// maximum and sum of the softmax stay in registers, and the outputs are 4 rows x 4 D / 64 dims per thread, so that every
+// 16-byte read of shared memory feeds 8 (scores) to 16 (outputs) multiply-adds.  fp32 FMA throughout (no TF32): the bound
+// is the FMA pipe for many rows and latency for few, so when the call has fewer CTAs than the machine has room for, the
+// tokens are split over a cluster of CTAs that join their rows through distributed shared memory.
+#include <cooperative_groups.h>
+#include <string.h>
+
 #include "ptenc_tree.cuh"
 
 namespace {
 
-constexpr int TG_THREADS = 128;
-constexpr int TG_ROWS = 16;
-constexpr int TG_TOK = 32;
-constexpr int TG_MAXJ = 32;          // head_dim <= 8 * TG_MAXJ
+namespace cg = cooperative_groups;
 
+constexpr int TG_THREADS = 128;
+constexpr int TG_ROWS = 32;
+constexpr int TG_TOK = 64;
+constexpr int TG_PP = TG_TOK + 4;    // pitch of the probabilities
+constexpr int TG_CLUSTER = 8;
+
+__device__ __forceinline__ float4 tg_ld4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 tg_ld4(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+__device__ __forceinline__ void tg_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+               ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src) : "memory");
+}
+__device__ __forceinline__ void tg_fma4(float4& a, float s, const float4& v) {
+  a.x = fmaf(s, v.x, a.x); a.y = fmaf(s, v.y, a.y); a.z = fmaf(s, v.z, a.z); a.w = fmaf(s, v.w, a.w);
+}
+
+// Shared memory in bytes: two K and V tiles (one where two do not fit), Q rows, probabilities.
 template <typename T>
+__host__ __device__ inline int tg_pitch(int D) { return D + 16 / (int)sizeof(T); }
+template <typename T>
+inline size_t tg_smem(int D, int stages) {
+  return (size_t)stages * 2 * TG_TOK * tg_pitch<T>(D) * sizeof(T) + sizeof(float) * (TG_ROWS * (D + 4) + TG_ROWS * TG_PP);
+}
+
+// J = 64-dim blocks of a row (D <= 64 J).
+template <typename T, int J>
 __global__ void __launch_bounds__(TG_THREADS)
 k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict__ k_tree, const T* __restrict__ v_tree,
                const int32_t* __restrict__ parent, const int32_t* __restrict__ n_nodes, int NT,
-               const uint8_t* __restrict__ active, T* __restrict__ out, float* __restrict__ lse, int n_groups) {
-  extern __shared__ float tg_sm[];
+               const uint8_t* __restrict__ active, T* __restrict__ out, float* __restrict__ lse, int n_groups, int stages) {
+  extern __shared__ __align__(16) uint8_t tg_sm[];
   const int D = p.D, g = p.g, W = p.W, Hkv = p.Hkv;
-  const int KP = D + 4;                                  // K row pitch: 16-byte loads of 32 rows without bank conflicts
-  float* s_k = tg_sm;                                    // [TG_TOK][KP]
-  float* s_v = s_k + TG_TOK * KP;                        // [TG_TOK][D]
-  float* s_q = s_v + TG_TOK * D;                         // [TG_ROWS][D]
-  __shared__ float s_p[TG_ROWS][TG_TOK + 1];
-  __shared__ float s_m[TG_ROWS], s_l[TG_ROWS], s_c[TG_ROWS];
+  const int KP = tg_pitch<T>(D), QP = D + 4;
+  T* s_kv = reinterpret_cast<T*>(tg_sm);                  // [stages][K, V][TG_TOK][KP]
+  float* s_q = reinterpret_cast<float*>(tg_sm + (size_t)stages * 2 * TG_TOK * KP * sizeof(T));   // [TG_ROWS][QP]
+  float* s_p = s_q + TG_ROWS * QP;                        // [TG_ROWS][TG_PP]
+  __shared__ float2 s_ml[TG_ROWS];
   __shared__ unsigned long long s_anc[TREE_MAX], s_vis[TREE_MAX];
   __shared__ int s_ev[TREE_MAX], s_jump[TREE_MAX];
 
-  int idx = blockIdx.x;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int CS = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  int idx = blockIdx.x / CS;
   const int grp = idx % n_groups; idx /= n_groups;
   const int hkv = idx % Hkv; idx /= Hkv;
   const int b = idx % p.B;
   const int li = idx / p.B;
-  if (active != nullptr && active[b] == 0) return;
+  if (active != nullptr && active[b] == 0) return;        // these verdicts are alike for the CTAs of a cluster
   const int n = n_nodes != nullptr ? n_nodes[b] : NT;
   const size_t lb = (size_t)(l0 + li) * p.B + b;
   const size_t ob = (size_t)li * p.B + b;
@@ -46,142 +79,285 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     return;
   }
   const int row0 = grp * TG_ROWS;
-  if (row0 >= n * g) return;                             // rows of nodes that do not exist stay as they are
+  if (row0 >= n * g) return;                              // rows of nodes that do not exist stay as they are
   if (!tree_setup(parent + (size_t)b * NT, n, r, s_anc, s_vis, s_ev, s_jump)) {
     if (threadIdx.x == 0) atomicOr(p.status, PTENC_ST_BAD_INDEX);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (int i = tid; i < TG_ROWS * D; i += TG_THREADS) {
-    const int rr = i / D, d = i - rr * D, row = row0 + rr;
-    const int node = row / g, h = row - node * g;
-    s_q[i] = node < n ? ptenc_to_float(q[((ob * NT + node) * p.Hq + (size_t)hkv * g + h) * D + d]) : 0.f;
-  }
-  if (tid < TG_ROWS) { s_m[tid] = -INFINITY; s_l[tid] = 0.f; }
 
   // tokens of the unit: pinned entries, then the ring from the oldest token that any node sees, then the nodes
   const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
-  const int n_ring = r.count - ev0;
-  const int n_cache = r.sink + n_ring;
+  const int n_cache = r.sink + r.count - ev0;
   const int n_tok = n_cache + n;
+  const int tiles = (n_tok + TG_TOK - 1) / TG_TOK;
+  const int t_lo = (int)((long long)rank * tiles / CS), t_hi = (int)((long long)(rank + 1) * tiles / CS);
   const T* Kb = reinterpret_cast<const T*>(p.K) + (lb * Hkv + hkv) * (size_t)W * D;
   const T* Vb = reinterpret_cast<const T*>(p.V) + (lb * Hkv + hkv) * (size_t)W * D;
-  const float scale = 1.0f / sqrtf((float)D);
-  const int orow = tid >> 3, od = tid & 7;
-  float acc[TG_MAXJ];
-#pragma unroll
-  for (int j = 0; j < TG_MAXJ; ++j) acc[j] = 0.f;
-
-  for (int t0 = 0; t0 < n_tok; t0 += TG_TOK) {
-    __syncthreads();
-    for (int tt = warp; tt < TG_TOK; tt += TG_THREADS / 32) {
-      const int i = t0 + tt;
-      const T *kr = nullptr, *vr = nullptr;
+  const int vpr = D * (int)sizeof(T) / 16;                // 16-byte vectors of a row
+  auto fetch = [&](int tile, int stage) {
+    T* dk = s_kv + (size_t)stage * 2 * TG_TOK * KP;
+    T* dv = dk + TG_TOK * KP;
+    for (int x = tid; x < TG_TOK * vpr; x += TG_THREADS) {
+      const int t = x / vpr, v = x - t * vpr, i = tile * TG_TOK + t;
+      if (i >= n_tok) {                                   // past the end: zeros, so that the products stay finite
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dk + t * KP) + 16 * v) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dv + t * KP) + 16 * v) = make_uint4(0u, 0u, 0u, 0u);
+        continue;
+      }
+      const T *kr, *vr;
       if (i < n_cache) {
-        const int slot = i < r.sink ? i : tree_slot(r, ev0 + (i - r.sink));
+        int slot = i;
+        if (i >= r.sink) {
+          slot = r.head + ev0 + (i - r.sink);
+          while (slot >= r.cap) slot -= r.cap;
+          slot += r.sink;
+        }
         kr = Kb + (size_t)slot * D;
         vr = Vb + (size_t)slot * D;
-      } else if (i < n_tok) {
+      } else {
         const size_t at = ((ob * NT + (i - n_cache)) * Hkv + hkv) * (size_t)D;
         kr = k_tree + at;
         vr = v_tree + at;
       }
-      for (int d = lane; d < D; d += 32) {
-        s_k[tt * KP + d] = kr != nullptr ? ptenc_to_float(kr[d]) : 0.f;
-        s_v[tt * D + d] = kr != nullptr ? ptenc_to_float(vr[d]) : 0.f;
-      }
+      tg_async16(reinterpret_cast<uint8_t*>(dk + t * KP) + 16 * v, reinterpret_cast<const uint8_t*>(kr) + 16 * v);
+      tg_async16(reinterpret_cast<uint8_t*>(dv + t * KP) + 16 * v, reinterpret_cast<const uint8_t*>(vr) + 16 * v);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (t_lo < t_hi) fetch(t_lo, 0);
+  for (int i = tid; i < TG_ROWS * D; i += TG_THREADS) {
+    const int rr = i / D, d = i - rr * D, row = row0 + rr;
+    const int node = row / g, h = row - node * g;
+    s_q[rr * QP + d] = node < n ? ptenc_to_float(q[((ob * NT + node) * p.Hq + (size_t)hkv * g + h) * D + d]) : 0.f;
+  }
+
+  const float scale = 1.0f / sqrtf((float)D);
+  const int rb = 8 * warp + 4 * (lane >> 4);              // this thread's four rows
+  const int tk = lane & 15;
+  float m[4], l[4];
+  float4 acc[4][J];
+  int ev[4], node_of[4];
+  int ev_max = ev0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    m[x] = -INFINITY;
+    l[x] = 0.f;
+    const int node = (row0 + rb + x) / g;
+    node_of[x] = node < n ? node : -1;
+    ev[x] = node < n ? s_ev[node] : ev0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[x][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  for (int i = 0; i < n; ++i) ev_max = max(ev_max, s_ev[i]);
+
+  for (int tile = t_lo; tile < t_hi; ++tile) {
+    const int stage = stages == 2 ? (tile - t_lo) & 1 : 0;
+    if (stages == 2 && tile + 1 < t_hi) {
+      fetch(tile + 1, stage ^ 1);
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    } else {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
     __syncthreads();
-    // scores: lane = token, rows 4 warp .. 4 warp + 3
-    {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-      const float4* kr = reinterpret_cast<const float4*>(s_k + lane * KP);
-      for (int d4 = 0; d4 < D / 4; ++d4) {
-        const float4 kk = kr[d4];
+    const T* sk = s_kv + (size_t)stage * 2 * TG_TOK * KP;
+    const T* sv = sk + TG_TOK * KP;
+    const int t0 = tile * TG_TOK;
+    // every row sees every token of the tile
+    const bool clean = t0 + TG_TOK <= n_cache && (ev_max == ev0 || t0 >= r.sink + ev_max - ev0 || t0 + TG_TOK <= r.sink);
+    // ---- scores: 4 rows x tokens tk, tk + 16, .. -----------------------------------------------------------------------
+    float s[4][4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float4 qq = *reinterpret_cast<const float4*>(s_q + (4 * warp + x) * D + 4 * d4);
-          s[x] = fmaf(qq.x, kk.x, fmaf(qq.y, kk.y, fmaf(qq.z, kk.z, fmaf(qq.w, kk.w, s[x]))));
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) s[x][y] = 0.f;
+    for (int d = 0; d < D; d += 4) {
+      float4 qq[4], kk[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) qq[x] = tg_ld4(s_q + (rb + x) * QP + d);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) kk[y] = tg_ld4(sk + (tk + 16 * y) * KP + d);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          s[x][y] = fmaf(qq[x].x, kk[y].x, fmaf(qq[x].y, kk[y].y, fmaf(qq[x].z, kk[y].z, fmaf(qq[x].w, kk[y].w, s[x][y]))));
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      unsigned seen = 0xfu;
+      if (!clean) {
+        const unsigned long long vis = node_of[x] >= 0 ? s_vis[node_of[x]] : ~0ull;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int i = t0 + tk + 16 * y;
+          const bool is = i < r.sink || (i < n_cache ? ev0 + (i - r.sink) >= ev[x] : (i < n_tok && ((vis >> ((i - n_cache) & 63)) & 1ull)));
+          if (!is) seen &= ~(1u << y);
         }
       }
-      const int i = t0 + lane;
+      float mx = -INFINITY;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int rr = 4 * warp + x;
-        const int node = (row0 + rr) / g;
-        bool seen = false;
-        if (node < n && i < n_tok) {
-          if (i < r.sink) seen = true;
-          else if (i < n_cache) seen = ev0 + (i - r.sink) >= s_ev[node];
-          else seen = (s_vis[node] >> (i - n_cache)) & 1ull;
-        }
-        const float v = seen ? s[x] * scale : -INFINITY;
-        float mx = v;
+      for (int y = 0; y < 4; ++y) {
+        s[x][y] = ((seen >> y) & 1u) ? s[x][y] * scale : -INFINITY;
+        mx = fmaxf(mx, s[x][y]);
+      }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float m_old = s_m[rr], m_new = fmaxf(m_old, mx);
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float e = seen ? expf(v - m_use) : 0.f;
-        float sum = e;
+      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float m_new = fmaxf(m[x], mx);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float corr = m[x] == -INFINITY ? 0.f : expf(m[x] - m_use);
+      float sum = 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        s_p[rr][lane] = e;
-        __syncwarp();                                     // every lane has read the row's old maximum
-        if (lane == 0) {
-          const float corr = m_old == -INFINITY ? 0.f : expf(m_old - m_use);
-          s_c[rr] = corr;
-          s_l[rr] = s_l[rr] * corr + sum;
-          s_m[rr] = m_new;
+      for (int y = 0; y < 4; ++y) {
+        const float e = ((seen >> y) & 1u) ? expf(s[x][y] - m_use) : 0.f;
+        sum += e;
+        s_p[(rb + x) * TG_PP + tk + 16 * y] = e;
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l[x] = l[x] * corr + sum;
+      m[x] = m_new;
+#pragma unroll
+      for (int j = 0; j < J; ++j) { acc[x][j].x *= corr; acc[x][j].y *= corr; acc[x][j].z *= corr; acc[x][j].w *= corr; }
+    }
+    __syncwarp();                                         // a warp reads the probabilities it wrote
+    // ---- outputs: 4 rows x dims 4 tk + 64 j -----------------------------------------------------------------------------
+    for (int t = 0; t < TG_TOK; t += 4) {
+      float4 pp[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) pp[x] = tg_ld4(s_p + (rb + x) * TG_PP + t);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int d = 4 * tk + 64 * j;
+        if (d < D) {
+          float4 vv[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) vv[y] = tg_ld4(sv + (t + y) * KP + d);
+          if (clean) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              tg_fma4(acc[x][j], pp[x].x, vv[0]); tg_fma4(acc[x][j], pp[x].y, vv[1]);
+              tg_fma4(acc[x][j], pp[x].z, vv[2]); tg_fma4(acc[x][j], pp[x].w, vv[3]);
+            }
+          } else {                                        // a token the row does not see may hold anything, NaN included
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if (pp[x].x != 0.f) tg_fma4(acc[x][j], pp[x].x, vv[0]);
+              if (pp[x].y != 0.f) tg_fma4(acc[x][j], pp[x].y, vv[1]);
+              if (pp[x].z != 0.f) tg_fma4(acc[x][j], pp[x].z, vv[2]);
+              if (pp[x].w != 0.f) tg_fma4(acc[x][j], pp[x].w, vv[3]);
+            }
+          }
         }
       }
     }
-    __syncthreads();
-    // outputs: eight threads per row, every eighth dim
-    {
-      const float corr = s_c[orow];
+    __syncthreads();                                      // the tile's buffer is free
+    if (stages == 1 && tile + 1 < t_hi) fetch(tile + 1, 0);
+  }
+
+  if (CS == 1) {
 #pragma unroll
-      for (int j = 0; j < TG_MAXJ; ++j) acc[j] *= corr;
-      const int last = min(TG_TOK, n_tok - t0);
-      for (int tt = 0; tt < last; ++tt) {
-        const float e = s_p[orow][tt];
-        if (e != 0.f) {                                   // a token the row does not see may hold anything, NaN included
+    for (int x = 0; x < 4; ++x) {
+      if (node_of[x] < 0) continue;
+      const size_t at = (ob * NT + node_of[x]) * p.Hq + (size_t)hkv * g + (row0 + rb + x) % g;
 #pragma unroll
-          for (int j = 0; j < TG_MAXJ; ++j)
-            if (od + 8 * j < D) acc[j] = fmaf(e, s_v[tt * D + od + 8 * j], acc[j]);
+      for (int j = 0; j < J; ++j) {
+        const int d = 4 * tk + 64 * j;
+        if (d < D) {
+          T* o = out + at * D + d;
+          o[0] = ptenc_from_float<T>(acc[x][j].x / l[x]); o[1] = ptenc_from_float<T>(acc[x][j].y / l[x]);
+          o[2] = ptenc_from_float<T>(acc[x][j].z / l[x]); o[3] = ptenc_from_float<T>(acc[x][j].w / l[x]);
         }
       }
+      if (lse != nullptr && tk == 0) lse[at] = m[x] + logf(l[x]);
     }
+    return;
   }
-  const int row = row0 + orow;
-  const int node = row / g, h = row - node * g;
-  if (node < n) {
-    const float l = s_l[orow];
-    const size_t at = (ob * NT + node) * p.Hq + (size_t)hkv * g + h;
+  // ---- the CTAs of the cluster join their rows: sums in the Q rows' place, (m, l) beside them ------------------------------
 #pragma unroll
-    for (int j = 0; j < TG_MAXJ; ++j)
-      if (od + 8 * j < D) out[at * D + od + 8 * j] = ptenc_from_float<T>(acc[j] / l);
-    if (lse != nullptr && od == 0) lse[at] = s_m[orow] + logf(l);
+  for (int x = 0; x < 4; ++x) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int d = 4 * tk + 64 * j;
+      if (d < D) *reinterpret_cast<float4*>(s_q + (rb + x) * QP + d) = acc[x][j];
+    }
+    if (tk == 0) s_ml[rb + x] = make_float2(m[x], l[x]);
   }
+  cluster.sync();
+  const int dv = D / 4;
+  for (int i = tid + rank * TG_THREADS; i < TG_ROWS * dv; i += TG_THREADS * CS) {
+    const int rr = i / dv, d = 4 * (i - rr * dv), row = row0 + rr;
+    const int node = row / g;
+    if (node >= n) continue;
+    float2 ml[TG_CLUSTER];
+    float mt = -INFINITY, lt = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int c = 0; c < TG_CLUSTER; ++c) {
+      ml[c] = c < CS ? cluster.map_shared_rank(s_ml, c)[rr] : make_float2(-INFINITY, 0.f);
+      mt = fmaxf(mt, ml[c].x);
+    }
+#pragma unroll
+    for (int c = 0; c < TG_CLUSTER; ++c) {
+      if (c < CS && ml[c].x != -INFINITY) {
+        const float w = expf(ml[c].x - mt);
+        lt = fmaf(w, ml[c].y, lt);
+        tg_fma4(o, w, *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_q, c) + rr * QP + d));
+      }
+    }
+    const size_t at = (ob * NT + node) * p.Hq + (size_t)hkv * g + row % g;
+    T* dst = out + at * D + d;
+    dst[0] = ptenc_from_float<T>(o.x / lt); dst[1] = ptenc_from_float<T>(o.y / lt);
+    dst[2] = ptenc_from_float<T>(o.z / lt); dst[3] = ptenc_from_float<T>(o.w / lt);
+    if (lse != nullptr && d == 0) lse[at] = mt + logf(lt);
+  }
+  cluster.sync();                                         // nobody leaves while its rows may still be read
 }
 
-template <typename T>
-cudaError_t launch_tree_t(ptenc_cache* c, int l0, int nl, const void* q, const void* kt, const void* vt,
+template <typename T, int J>
+cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const void* kt, const void* vt,
                           const int32_t* parent, const int32_t* n_nodes, int NT, const uint8_t* active, void* out,
                           float* lse, cudaStream_t st) {
   const PtencDev& p = c->dev;
   const int n_groups = (NT * p.g + TG_ROWS - 1) / TG_ROWS;
-  const long long grid = (long long)nl * p.B * p.Hkv * n_groups;
-  if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-  const size_t smem = sizeof(float) * ((size_t)TG_TOK * (2 * p.D + 4) + (size_t)TG_ROWS * p.D);
+  const long long blocks = (long long)nl * p.B * p.Hkv * n_groups;
+  // Tokens over up to eight CTAs while that does not exceed two CTAs per SM and each still has a tile of 64.
+  int cs = 1;
+  while (cs < TG_CLUSTER && blocks * cs * 2 <= 2 * c->sm_count && cs * 2 * TG_TOK <= p.W) cs *= 2;
+  if (blocks * cs > 0x7fffffffll) return cudaErrorInvalidValue;
+  int stages = 2;
+  if (tg_smem<T>(p.D, 2) > 200 * 1024) stages = 1;
+  const size_t smem = tg_smem<T>(p.D, stages);
   static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (smem > 40 * 1024 && ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_tree_generic<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+  if (ptenc_first_use(attr_done, c->cfg.device)) {
+    cudaError_t e = cudaFuncSetAttribute(k_tree_generic<T, J>, cudaFuncAttributeMaxDynamicSharedMemorySize, 216 * 1024);
     if (e != cudaSuccess) return e;
   }
-  k_tree_generic<T><<<(unsigned)grid, TG_THREADS, smem, st>>>(p, l0, (const T*)q, (const T*)kt, (const T*)vt, parent,
-                                                              n_nodes, NT, active, (T*)out, lse, n_groups);
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(blocks * cs));
+  cfg.blockDim = dim3(TG_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cs;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, k_tree_generic<T, J>, p, l0, (const T*)q, (const T*)kt, (const T*)vt, parent,
+                                     n_nodes, NT, active, (T*)out, lse, n_groups, stages);
   c->launches++;
-  return cudaGetLastError();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_tree_t(ptenc_cache* c, int l0, int nl, const void* q, const void* kt, const void* vt,
+                          const int32_t* parent, const int32_t* n_nodes, int NT, const uint8_t* active, void* out,
+                          float* lse, cudaStream_t st) {
+  if (c->dev.D <= 64) return launch_tree_j<T, 1>(c, l0, nl, q, kt, vt, parent, n_nodes, NT, active, out, lse, st);
+  if (c->dev.D <= 128) return launch_tree_j<T, 2>(c, l0, nl, q, kt, vt, parent, n_nodes, NT, active, out, lse, st);
+  return launch_tree_j<T, 4>(c, l0, nl, q, kt, vt, parent, n_nodes, NT, active, out, lse, st);
 }
 
 }  // namespace
