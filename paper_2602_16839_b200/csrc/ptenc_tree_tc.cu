@@ -114,12 +114,6 @@ __device__ __forceinline__ void st32(uint32_t t, const uint32_t* r) {
         "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
         "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
-__device__ __forceinline__ void st16(uint32_t t, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-      ::"r"(t), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
 __device__ __forceinline__ float tt_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -200,6 +194,12 @@ __device__ __forceinline__ int tt_tiles(int sink, int head, int count, int W, in
   *t0 = (sink + head) / TN;
   *len2 = (sink + head + high - 1) / TN - *t0 + 1;
   return *len2 + min(e1, *t0);
+}
+
+// Bits of columns [lo, hi) in the word of columns [at, at + 32).
+__device__ __forceinline__ uint32_t run_mask(int lo, int hi, int at) {
+  const int a = max(lo - at, 0), b = min(hi - at, 32);
+  return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
 }
 
 // ------------------------------------------------------------------------------------------------ kernel
@@ -628,11 +628,6 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       const bool idle = __all_sync(0xffffffffu, !real);  // a warp without rows only keeps the barriers going
       __syncwarp();
       if (lane == 0) bar_arrive(info_empty);
-      auto sees = [&](int slot) -> bool {
-        int dd = slot - r.sink - r.head;
-        if (dd < 0) dd += r.cap;
-        return slot < r.sink || (slot < W && dd >= ev && dd < r.count);
-      };
       float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and sum
       bool started = false;
       for (int i = two ? 0 : st; i < n; i += two ? 1 : 2, ++ns) {
@@ -650,28 +645,41 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
         wait(s_full + 8 * st, ns & 1);
         fence_after();
         if (!idle) {
-          float x[TN];
+          // The row is read from tensor memory twice, 64 columns at a time, once for its maximum and once for P: the loop
+          // bodies stay small (at the start of a launch every instruction comes from cold memory, and a row unrolled over
+          // 128 columns took microseconds there) and the registers hold half a row.
           const uint32_t ts = tS[st] + lane_off;
-          const int chunks = draft ? (a.nb + 31) / 32 : 4;             // 32-column chunks in use
-          ld32(ts, x);
-          ld32(ts + 32, x + 32);
-          ld32(ts + 64, x + 64);
-          ld32(ts + 96, x + 96);
-          wait_ld();
+          const int cols = draft ? a.nb : TN;
+          uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};       // columns the row sees
           if (draft) {
-#pragma unroll
-            for (int c = 0; c < TN; ++c)
-              if (c >= TREE_MAX || !((vis >> (c & 63)) & 1ull)) x[c] = -INFINITY;
+            keep[0] = (uint32_t)vis;
+            keep[1] = (uint32_t)(vis >> 32);
           } else if (!clean) {
+            // three runs of slots: pinned; from the oldest one seen to the end of the ring; what has wrapped round
+            const int z = r.sink + r.head - slot0;
+            const int lo1 = z + ev, hi1 = min(z + r.count, W - slot0);
+            const int lo2 = max(z - r.cap + ev, r.sink - slot0), hi2 = min(z - r.cap + r.count, z);
 #pragma unroll
-            for (int c = 0; c < TN; ++c)
-              if (!sees(slot0 + c)) x[c] = -INFINITY;
+            for (int w = 0; w < 4; ++w)
+              keep[w] = run_mask(-slot0, r.sink - slot0, 32 * w) | run_mask(lo1, hi1, 32 * w) | run_mask(lo2, hi2, 32 * w);
           }
-          float mx[4] = {x[0], x[1], x[2], x[3]};
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int c = 0; c < cols; c += 64) {
+            float x[64];
+            ld32(ts + c, x);
+            ld32(ts + c + 32, x + 32);
+            wait_ld();
+            if (!clean) {
+              const uint32_t k0 = c == 0 ? keep[0] : keep[2], k1 = c == 0 ? keep[1] : keep[3];
 #pragma unroll
-          for (int c = 4; c < TN; c += 4) {
-            mx[0] = fmaxf(mx[0], x[c]); mx[1] = fmaxf(mx[1], x[c + 1]);
-            mx[2] = fmaxf(mx[2], x[c + 2]); mx[3] = fmaxf(mx[3], x[c + 3]);
+              for (int y = 0; y < 32; ++y) {
+                if (!(k0 & (1u << y))) x[y] = -INFINITY;
+                if (!(k1 & (1u << y))) x[y + 32] = -INFINITY;
+              }
+            }
+#pragma unroll
+            for (int y = 0; y < 64; ++y) mx[y & 3] = fmaxf(mx[y & 3], x[y]);
           }
           const float mnew = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
           if (!started) {
@@ -695,16 +703,28 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
           }
           const float neg = m == -INFINITY ? 0.f : -m * sl2;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          for (int c = 0; c < cols; c += 64) {
+            float x[64];
+            uint32_t pk[32];
+            ld32(ts + c, x);
+            ld32(ts + c + 32, x + 32);
+            wait_ld();
+            if (!clean) {
+              const uint32_t k0 = c == 0 ? keep[0] : keep[2], k1 = c == 0 ? keep[1] : keep[3];
 #pragma unroll
-          for (int c = 0; c < TN; c += 32) {
-            uint32_t pk[16];
+              for (int y = 0; y < 32; ++y) {
+                if (!(k0 & (1u << y))) x[y] = -INFINITY;
+                if (!(k1 & (1u << y))) x[y + 32] = -INFINITY;
+              }
+            }
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-              const float p0 = tt_ex2(fmaf(x[c + y], sl2, neg)), p1 = tt_ex2(fmaf(x[c + y + 1], sl2, neg));
+            for (int y = 0; y < 64; y += 2) {
+              const float p0 = tt_ex2(fmaf(x[y], sl2, neg)), p1 = tt_ex2(fmaf(x[y + 1], sl2, neg));
               sum[(y >> 1) & 3] += p0 + p1;
               pk[y >> 1] = tt_pack(p0, p1);
             }
-            if (c < 32 * chunks) st16(ts + c / 2, pk);
+            st32(ts + c / 2, pk);                        // over columns that have been read: c / 2 + 32 <= c + 64
           }
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           wait_st();
@@ -829,34 +849,60 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
         soft_sync();
         if (misc[3] && real) {
           __threadfence();
-          const size_t ps0 = (size_t)split * a.P * a.tpb + tile_i, step = a.tpb;
-          float mm = -INFINITY;
-          for (int q = 0; q < pieces; ++q) mm = fmaxf(mm, __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]).x);
-          float ll = 0.f;
+          // Two parts' 32 columns are requested together: the join is the tail of the call, and a vector at a time it is a
+          // chain of round trips through L2.
+          const size_t step = (size_t)a.tpb * TM;
+          const float2* ml = a.part_ml + ((size_t)split * a.P * a.tpb + tile_i) * TM + lrow;
+          const float4* src = reinterpret_cast<const float4*>(a.part) + ((size_t)split * a.P * a.tpb + tile_i) * (D / 4) * TM + lrow;
+          float mm = -INFINITY, ll = 0.f;
+#pragma unroll 4
+          for (int q = 0; q < pieces; ++q) mm = fmaxf(mm, __ldcg(ml + q * step).x);
+#pragma unroll 4
           for (int q = 0; q < pieces; ++q) {
-            const float2 v = __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]);
-            ll += (v.x == -INFINITY ? 0.f : tt_ex2(v.x - mm)) * v.y;
+            const float2 v = __ldcg(ml + q * step);
+            ll = fmaf(v.x == -INFINITY ? 0.f : tt_ex2(v.x - mm), v.y, ll);
           }
           const float linv = 1.f / ll;
 #pragma unroll 1
-          for (int c = c_lo; c < c_hi; c += 8) {
-            float acc[8];
+          for (int c = c_lo; c < c_hi; c += 32) {
+            float4 acc[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) acc[y] = 0.f;
-            for (int q = 0; q < pieces; ++q) {
-              const float mq = __ldcg(&a.part_ml[(ps0 + q * step) * TM + lrow]).x;
-              if (mq == -INFINITY) continue;             // a part in which the row sees nothing
-              const float w = tt_ex2(mq - mm);
-              const float4* src = reinterpret_cast<const float4*>(a.part) + (ps0 + q * step) * (D / 4) * TM + (c >> 2) * TM + lrow;
-              const float4 v0 = __ldcg(src), v1 = __ldcg(src + TM);
-              acc[0] = fmaf(w, v0.x, acc[0]); acc[1] = fmaf(w, v0.y, acc[1]); acc[2] = fmaf(w, v0.z, acc[2]);
-              acc[3] = fmaf(w, v0.w, acc[3]); acc[4] = fmaf(w, v1.x, acc[4]); acc[5] = fmaf(w, v1.y, acc[5]);
-              acc[6] = fmaf(w, v1.z, acc[6]); acc[7] = fmaf(w, v1.w, acc[7]);
+            for (int y = 0; y < 8; ++y) acc[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int q = 0; q < pieces; q += 2) {
+              const int q1 = min(q + 1, pieces - 1);
+              const float4* s0 = src + (q * step * (D / 4) + (c >> 2) * TM);
+              const float4* s1 = src + (q1 * step * (D / 4) + (c >> 2) * TM);
+              const float m0 = __ldcg(ml + q * step).x, m1 = __ldcg(ml + q1 * step).x;
+              float4 v0[8], v1[8];
+#pragma unroll
+              for (int y = 0; y < 8; ++y) { v0[y] = __ldcg(s0 + y * TM); v1[y] = __ldcg(s1 + y * TM); }
+              // a part in which the row sees nothing does not count, whatever it holds
+              if (m0 != -INFINITY) {
+                const float w = tt_ex2(m0 - mm);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                  acc[y].x = fmaf(w, v0[y].x, acc[y].x); acc[y].y = fmaf(w, v0[y].y, acc[y].y);
+                  acc[y].z = fmaf(w, v0[y].z, acc[y].z); acc[y].w = fmaf(w, v0[y].w, acc[y].w);
+                }
+              }
+              if (q1 != q && m1 != -INFINITY) {
+                const float w = tt_ex2(m1 - mm);
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                  acc[y].x = fmaf(w, v1[y].x, acc[y].x); acc[y].y = fmaf(w, v1[y].y, acc[y].y);
+                  acc[y].z = fmaf(w, v1[y].z, acc[y].z); acc[y].w = fmaf(w, v1[y].w, acc[y].w);
+                }
+              }
             }
-            if (valid)
-              *reinterpret_cast<uint4*>(a.out + orow * D + c) =
-                  make_uint4(tt_pack(acc[0] * linv, acc[1] * linv), tt_pack(acc[2] * linv, acc[3] * linv),
-                             tt_pack(acc[4] * linv, acc[5] * linv), tt_pack(acc[6] * linv, acc[7] * linv));
+            if (valid) {
+              uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
+#pragma unroll
+              for (int y = 0; y < 4; ++y)
+                dst[y] = make_uint4(tt_pack(acc[2 * y].x * linv, acc[2 * y].y * linv), tt_pack(acc[2 * y].z * linv, acc[2 * y].w * linv),
+                                    tt_pack(acc[2 * y + 1].x * linv, acc[2 * y + 1].y * linv),
+                                    tt_pack(acc[2 * y + 1].z * linv, acc[2 * y + 1].w * linv));
+            }
           }
           if (writes_lse && a.lse != nullptr) a.lse[orow] = (mm + log2f(ll)) * 0.6931471805599453f;
         }
