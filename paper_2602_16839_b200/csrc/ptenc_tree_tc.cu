@@ -11,8 +11,9 @@
 //    plain loads of this GPU's own memory) into a ring of stages.
 //  * warp 1, one lane: issues the MMAs.  Two streams, each with its own S, P and O in tensor memory: with two row tiles a
 //    stream per row tile; with one, the K/V tiles alternate between the streams and the two results are merged at the end.
-//    One stream's products always run under the other's softmax.  S = Q K^T (both K-major in shared memory),
-//    O += P V (P bf16 in tensor memory over the S it came from, V as it lies: tokens x head_dim, MN-major).
+//    One stream's products run under the other's softmax, and the product with the first half of a tile's V under the
+//    softmax of the second half.  S = Q K^T (both K-major in shared memory), O += P V (P bf16 in tensor memory over the
+//    S it came from, V as it lies: tokens x head_dim, MN-major).
 //  * warp 2: patches.  Works out what each node sees (ptenc_tree.cuh), and passes every stage on; in the tiles where some
 //    slot is not seen by some node it clears the V rows that nobody sees and takes non-finite values out of the V rows
 //    that only some nodes see, since 0 * NaN would carry them into the other nodes' rows.
@@ -23,13 +24,15 @@
 //  * Every wait is bounded: one that runs out raises a status bit and an abort flag, every role then leaves, copies and
 //    MMAs in flight are drained and tensor memory is freed.
 #include <string.h>
+#include <type_traits>
 
 #include "ptenc_tree.cuh"
 
 namespace {
 
-constexpr uint32_t TT_POLLS = 4000000;
+constexpr long long TT_CLOCKS = 4000000000ll;  // longest wait: two seconds
 constexpr int TN = 128;                        // slots per K/V tile
+constexpr int TH = 64;                         // tokens per softmax block: half a tile
 constexpr int TM = 128;                        // rows of a row tile = TMEM lanes
 constexpr int TT_THREADS = 384;                // producer, MMA, patch, (none), 2 x 4 softmax warps
 constexpr int TT_SOFT = 256;
@@ -56,18 +59,31 @@ __device__ __forceinline__ uint32_t bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
 // Bounded wait that also gives up when another role has raised the abort flag.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t i = 0; i < TT_POLLS; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if ((i & 15) == 15 && *abort_flag != 0) return false;
+  if (bar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (clock64() - t0 < TT_CLOCKS) {
+    if (bar_try(bar, parity) || bar_try(bar, parity)) return true;
+    if (*abort_flag != 0) return false;
   }
   return false;
+}
+// Bounded wait for what completes by itself: copies and products in flight.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (!bar_try(bar, parity) && clock64() - t0 < TT_CLOCKS) {}
+}
+// True in one lane of the (converged) warp.
+__device__ __forceinline__ bool tt_elect() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
 }
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
@@ -119,6 +135,30 @@ __device__ __forceinline__ float tt_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t tt_two(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void tt_both(uint64_t d, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
+}
+__device__ __forceinline__ uint64_t tt_fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t tt_add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float tt_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
@@ -152,7 +192,7 @@ struct TSmem {
   static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // float2 [128]
   static constexpr int OFF_DESC = OFF_ML + TM * 8;                   // int [2][32] items
   static constexpr int OFF_BAR = OFF_DESC + 2 * 32 * 4;
-  static constexpr int N_BAR = 3 * STAGES + 20;
+  static constexpr int N_BAR = 3 * STAGES + 24;
   static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]
   static constexpr int OFF_JUMP = OFF_DEPTH + TREE_MAX;              // s8 [64]
   static constexpr int OFF_MISC = OFF_JUMP + TREE_MAX;
@@ -220,17 +260,19 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
   volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict, misc[3]: last arriver
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
-  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16,
-                 q_empty = q_full + 16, item_full = q_empty + 16, item_empty = item_full + 16,
+  // p_full: [stream][half]; the others with two entries: [stream], [Q tile] or [item slot]
+  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, pv_done = p_full + 32, o_full = pv_done + 16,
+                 q_full = o_full + 16, q_empty = q_full + 16, item_full = q_empty + 16, item_empty = item_full + 16,
                  o_empty = item_empty + 16, info_full = o_empty + 8, info_empty = info_full + 8, drain = info_empty + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int W = p.W, B = p.B, Hkv = p.Hkv, g = p.g;
 
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 2); bar_init(ready + 8 * s, 1); }
+    for (int s = 0; s < 4; ++s) bar_init(p_full + 8 * s, 4);
     for (int s = 0; s < 2; ++s) {
       bar_init(s_full + 8 * s, 1);
-      bar_init(p_full + 8 * s, 4);
+      bar_init(pv_done + 8 * s, 1);
       bar_init(o_full + 8 * s, 1);
       bar_init(q_full + 8 * s, 1);
       bar_init(q_empty + 8 * s, 1);
@@ -253,7 +295,7 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
   __syncthreads();
   fence_after();
   const uint32_t tmem = (uint32_t)misc[1];
-  const uint32_t tS[2] = {tmem, tmem + TN}, tO[2] = {tmem + 2 * TN, tmem + 2 * TN + D};
+  const uint32_t tS = tmem, tO = tmem + 2 * TN;          // S [stream] of 128 columns, O [stream] of D columns
 
   // Ring position of an item's K and V tiles, counted from its first: with two row tiles K0 V0 K1 V1 ..; with one, the next
   // K tile of a stream is wanted before the V tile of the other: K0 K1 V0 K2 V1 K3 ..
@@ -360,86 +402,116 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       }
       if (!okay) { atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT); *abort_flag = 1; }
       // whatever the other roles did, copies in flight land before the shared memory goes away
-      for (uint32_t i = 1; i <= (uint32_t)NS && i <= pos; ++i)
-        for (uint32_t k = 0; k < TT_POLLS; ++k)
-          if (bar_try(full + 8 * ((pos - i) % NS), ((pos - i) / NS) & 1)) break;
-      for (uint32_t i = 1; i <= 2 && i <= qn; ++i)
-        for (uint32_t k = 0; k < TT_POLLS; ++k)
-          if (bar_try(q_full + 8 * ((qn - i) & 1), ((qn - i) >> 1) & 1)) break;
+      for (uint32_t i = 1; i <= (uint32_t)NS && i <= pos; ++i) bar_drain(full + 8 * ((pos - i) % NS), ((pos - i) / NS) & 1);
+      for (uint32_t i = 1; i <= 2 && i <= qn; ++i) bar_drain(q_full + 8 * ((qn - i) & 1), ((qn - i) >> 1) & 1);
     }
   } else if (warp == 1) {
     // ================================================================ MMA issuer
-    if (lane == 0) {
-      constexpr uint32_t ID_QK = tt_idesc(TN, 0), ID_PV = tt_idesc(D, 1);
-      const uint32_t ID_QKD = tt_idesc(a.nb, 0);
-      uint32_t base = 0, qn = 0, seq = 0, items = 0;
-      uint32_t np = 0;                                   // bit st: parity of the softmax results consumed of stream st
-      bool okay = true;
-      while (okay) {
-        if (!bar_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag)) { okay = false; break; }
-        volatile int* d = desc + (seq & 1) * 32;
-        if (d[I_KIND] == 0) break;
-        const bool two = d[I_TWO] != 0;
-        const int n = d[I_CNT];
-        const int draft = d[I_NT] - 1 - d[I_LO];         // the draft's tile, if it is among the item's
-        bar_arrive(item_empty + 8 * (seq & 1));
-        ++seq;
-        const uint32_t q0 = qn, nq = two ? 2 : 1;
-        auto issue_s = [&](int i, int st, int qt, bool release) -> bool {
-          const uint32_t ps = base + pos_k(i, two), s = ps % NS;
-          if (!bar_wait(full + 8 * s, (ps / NS) & 1, abort_flag)) return false;
-          fence_after();
-          const uint32_t qa = sb + SM::OFF_Q + ((q0 + qt) & 1) * TILE, ka = sb + s * TILE;
+    // The whole warp takes every step, so that addresses, descriptors and counters are alike in all lanes and can live in
+    // uniform registers, which the MMA instruction takes its operands from; one elected lane issues.  With the steps
+    // behind `lane == 0` an MMA cost about 100 cycles to issue, more than it takes to run.
+    const bool leader = tt_elect();
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+      return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag));
+    };
+    constexpr uint32_t ID_QK = tt_idesc(TN, 0), ID_PV = tt_idesc(D, 1);
+    const uint32_t ID_QKD = tt_idesc(a.nb, 0);
+    uint32_t base = 0, qn = 0, seq = 0, items = 0;
+    uint32_t np0 = 0, np1 = 0;                           // bits 0 and 1: parity of the halves consumed per stream
+    bool okay = true;
+    while (okay) {
+      if (!wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + (seq & 1) * 32;
+      const int kind = __shfl_sync(0xffffffffu, d[I_KIND], 0);
+      if (kind == 0) break;
+      const bool two = __shfl_sync(0xffffffffu, d[I_TWO], 0) != 0;
+      const int n = __shfl_sync(0xffffffffu, d[I_CNT], 0);
+      const int draft = __shfl_sync(0xffffffffu, d[I_NT] - 1 - d[I_LO], 0);   // the draft's tile, if the item has it: one half
+      __syncwarp();
+      if (leader) bar_arrive(item_empty + 8 * (seq & 1));
+      ++seq;
+      const uint32_t q0 = qn, nq = two ? 2 : 1;
+      const int stride = two ? 1 : 2;                    // a stream's next tile
+      auto issue_s = [&](auto ST, int i) -> bool {       // S = Q K^T of the stream's tile i
+        constexpr int st = decltype(ST)::value;
+        if (i >= n) return true;
+        const uint32_t ps = base + pos_k(i, two), s = ps % NS;
+        if (!wait(full + 8 * s, (ps / NS) & 1)) return false;
+        fence_after();
+        const uint64_t dq = desc_k(sb + SM::OFF_Q + ((q0 + (two ? st : 0)) & 1) * TILE), dk = desc_k(sb + s * TILE);
+        const uint32_t id = i == draft ? ID_QKD : ID_QK;
+        if (leader) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = (k >> 2) * HALF + (k & 3) * 32;
-            mma_ss(tS[st], desc_k(qa + off), desc_k(ka + off), i == draft ? ID_QKD : ID_QK, k > 0);
+            const uint64_t off = ((k >> 2) * HALF + (k & 3) * 32) >> 4;        // the address field counts 16 bytes
+            mma_ss(tS + st * TN, dq + off, dk + off, id, k > 0);
           }
           commit(s_full + 8 * st);
-          if (release) commit(empty + 8 * s);
-          return true;
-        };
-        bool first = true;
-        auto issue_pv = [&](int i, int st, bool start, bool end, bool release) -> bool {
-          if (!bar_wait(p_full + 8 * st, (np >> st) & 1, abort_flag)) return false;
-          np ^= 1u << st;
-          if (first && !bar_wait(o_empty, (items & 1) ^ 1, abort_flag)) return false;   // O of the item before is out
-          first = false;
-          const uint32_t ps = base + pos_v(i, n, two), s = ps % NS;
-          if (!bar_wait(full + 8 * s, (ps / NS) & 1, abort_flag)) return false;
-          if (!bar_wait(ready + 8 * s, (ps / NS) & 1, abort_flag)) return false;
-          fence_after();
-          const int ks = i == draft ? a.nb / 16 : TN / 16;
-          for (int k = 0; k < ks; ++k)
-            mma_ts(tO[st], tS[st] + 8 * k, desc_mn(sb + s * TILE + k * 2048), ID_PV, (!start || k > 0) ? 1u : 0u);
-          if (release) commit(empty + 8 * s);
-          if (end) commit(o_full + 8 * st);
-          return true;
-        };
-        for (uint32_t t = 0; t < nq && okay; ++t)
-          okay = bar_wait(q_full + 8 * ((q0 + t) & 1), ((q0 + t) >> 1) & 1, abort_flag);
-        if (two) {
-          okay = okay && issue_s(0, 0, 0, false) && issue_s(0, 1, 1, true);
-          for (int i = 0; i < n && okay; ++i) {
-            okay = issue_pv(i, 0, i == 0, i == n - 1, false) && (i + 1 >= n || issue_s(i + 1, 0, 0, false)) &&
-                   issue_pv(i, 1, i == 0, i == n - 1, true) && (i + 1 >= n || issue_s(i + 1, 1, 1, true));
-          }
-        } else {
-          okay = okay && issue_s(0, 0, 0, true) && (n < 2 || issue_s(1, 1, 0, true));
-          for (int i = 0; i < n && okay; ++i)
-            okay = issue_pv(i, i & 1, i < 2, i >= n - 2, true) && (i + 2 >= n || issue_s(i + 2, i & 1, 0, true));
+          if (!two || st == 1) commit(empty + 8 * s);
         }
-        if (okay)
-          for (uint32_t t = 0; t < nq; ++t) commit(q_empty + 8 * ((q0 + t) & 1));
-        qn += nq;
-        base += 2 * n;
-        ++items;
-      }
+        __syncwarp();
+        return true;
+      };
+      bool first = true;
+      auto issue_pv = [&](auto ST, int i, uint32_t& np) -> bool {              // O += P V of the stream's tile i
+        constexpr int st = decltype(ST)::value;
+        if (i >= n) return true;
+        const uint32_t ps = base + pos_v(i, n, two), s = ps % NS;
+        const uint32_t start = i < stride ? 0u : 1u;                           // 0: the product replaces what O holds
+        const uint64_t dv = desc_mn(sb + s * TILE);
+        const int ks = i == draft ? a.nb / 16 : TH / 16;
+        if (!wait(p_full + 16 * st, np & 1)) return false;
+        np ^= 1;
+        if (first && !wait(o_empty, (items & 1) ^ 1)) return false;            // O of the item before is out
+        first = false;
+        if (!wait(ready + 8 * s, (ps / NS) & 1)) return false;
+        fence_after();
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < TH / 16; ++k)
+            if (k < ks) mma_ts(tO + st * D, tS + st * TN + 8 * k, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : start);
+          commit(pv_done + 8 * st);
+        }
+        __syncwarp();
+        if (i != draft) {
+          if (!wait(p_full + 16 * st + 8, (np >> 1) & 1)) return false;
+          np ^= 2;
+          fence_after();
+          if (leader) {
+#pragma unroll
+            for (int k = TH / 16; k < TN / 16; ++k)
+              mma_ts(tO + st * D, tS + st * TN + 8 * k, dv + (k * 2048 >> 4), ID_PV, 1u);
+            commit(pv_done + 8 * st);
+          }
+        }
+        if (leader) {
+          if (!two || st == 1) commit(empty + 8 * s);
+          if (i + stride >= n) commit(o_full + 8 * st);
+        }
+        __syncwarp();
+        return true;
+      };
+      using S0 = std::integral_constant<int, 0>;
+      using S1 = std::integral_constant<int, 1>;
+      for (uint32_t t = 0; t < nq && okay; ++t) okay = wait(q_full + 8 * ((q0 + t) & 1), ((q0 + t) >> 1) & 1);
+      const int off1 = two ? 0 : 1;                      // with one row tile the second stream takes the odd tiles
+      okay = okay && issue_s(S0(), 0) && issue_s(S1(), off1);
+      for (int i = 0; i < n && okay; i += stride)
+        okay = issue_pv(S0(), i, np0) && issue_s(S0(), i + stride) && issue_pv(S1(), i + off1, np1) &&
+               issue_s(S1(), i + off1 + stride);
+      if (okay && leader)
+        for (uint32_t t = 0; t < nq; ++t) commit(q_empty + 8 * ((q0 + t) & 1));
+      __syncwarp();
+      qn += nq;
+      base += 2 * n;
+      ++items;
+    }
+    if (leader) {
       if (!okay) { atomicOr(p.status, PTENC_ST_WAIT_TIMEOUT); *abort_flag = 1; }
       commit(drain);                                     // MMAs still in flight finish before tensor memory is freed
-      for (uint32_t k = 0; k < TT_POLLS; ++k)
-        if (bar_try(drain, 0)) break;
+      bar_drain(drain, 0);
     }
+    __syncwarp();
   } else if (warp == 2) {
     // ================================================================ patch warp
     uint32_t base = 0, seq = 0;
@@ -539,12 +611,13 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
                      ((d0 >= ev_max && d0 + TN <= r.count) || (ev_max == 0 && r.count == r.cap)));
           }
           if (!clean) {
+            // which rows nobody sees and which only some nodes see, 32 at a time; then 16 bytes per lane of those rows
             uint8_t* v = smem + s * TILE;
             constexpr int VPR = DH * 8;                  // 16-byte vectors of a row
             const int rows = draft ? a.nb : TN;
             int odd = 0;
-            for (int x = lane; x < rows * VPR; x += 32) {
-              const int t = x / VPR, c = x - t * VPR;
+            for (int rb = 0; rb < rows; rb += 32) {
+              const int t = rb + lane;
               bool dead, some;
               if (draft) {
                 dead = t >= nodes;
@@ -556,19 +629,34 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
                 dead = slot >= r.sink && (slot >= W || dd < ev0 || dd >= r.count);
                 some = !dead && slot >= r.sink && dd < ev_max;
               }
-              uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * HALF + t * 128 + (c & 7) * 16);
-              if (dead) {
-                *at = make_uint4(0u, 0u, 0u, 0u);
-              } else if (some) {
-                uint4 w = *at;
-                uint32_t* e = reinterpret_cast<uint32_t*>(&w);
-                int hit = 0;
+              const unsigned m_dead = __ballot_sync(0xffffffffu, dead && t < rows);
+              unsigned todo = m_dead | __ballot_sync(0xffffffffu, some && t < rows);
+              while (todo != 0) {
+                // 32 / VPR rows at a time: this lane's is the (lane / VPR)-th of those left
+                int at = __ffs(todo) - 1;
+                unsigned rest = todo & (todo - 1);
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {            // exponent bits all set: infinity or NaN
-                  if ((e[y] & 0x7f80u) == 0x7f80u) { e[y] &= 0xffff0000u; hit = 1; }
-                  if ((e[y] & 0x7f800000u) == 0x7f800000u) { e[y] &= 0x0000ffffu; hit = 1; }
+                for (int y = 1; y < 32 / VPR; ++y) {
+                  if (lane / VPR >= y) at = rest != 0 ? __ffs(rest) - 1 : -1;
+                  rest &= rest - 1;
                 }
-                if (hit) { *at = w; odd = 1; }
+                todo = rest;
+                if (at < 0) continue;
+                const int c = lane % VPR;
+                uint4* vec = reinterpret_cast<uint4*>(v + (c >> 3) * HALF + (rb + at) * 128 + (c & 7) * 16);
+                if ((m_dead >> at) & 1u) {
+                  *vec = make_uint4(0u, 0u, 0u, 0u);
+                } else {
+                  uint4 w = *vec;
+                  uint32_t* e = reinterpret_cast<uint32_t*>(&w);
+                  int hit = 0;
+#pragma unroll
+                  for (int y = 0; y < 4; ++y) {          // exponent bits all set: infinity or NaN
+                    if ((e[y] & 0x7f80u) == 0x7f80u) { e[y] &= 0xffff0000u; hit = 1; }
+                    if ((e[y] & 0x7f800000u) == 0x7f800000u) { e[y] &= 0x0000ffffu; hit = 1; }
+                  }
+                  if (hit) { *vec = w; odd = 1; }
+                }
               }
             }
             if (__any_sync(0xffffffffu, odd) && lane == 0) d[I_ODD] = 1;
@@ -593,7 +681,7 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
     const int lrow = 32 * quarter + lane;
     const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
     const float sl2 = 1.4426950408889634f / sqrtf((float)D);
-    uint32_t seq = 0, ns = 0;                            // items; tiles of this stream
+    uint32_t seq = 0, ns = 0, ntile = 0;                 // items; blocks and tiles of this stream
     uint32_t no0 = 0, no1 = 0;                           // items in which the streams had tiles
     bool fine = true;                                    // a wait that ran out: go through the motions, never wait again
     auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -630,109 +718,101 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       if (lane == 0) bar_arrive(info_empty);
       float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and sum
       bool started = false;
-      for (int i = two ? 0 : st; i < n; i += two ? 1 : 2, ++ns) {
+#pragma unroll 1
+      for (int i = two ? 0 : st; i < n; i += two ? 1 : 2) {
         const int u = lo + i;
         const bool draft = u == nt - 1;
-        const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
-        bool clean = false;
-        if (!draft) {
-          int d0 = slot0 - r.sink - r.head;
-          if (d0 < 0) d0 += r.cap;
-          clean = slot0 + TN <= r.sink ||
-                  (slot0 >= r.sink && slot0 + TN <= W &&
-                   ((d0 >= ev_max && d0 + TN <= r.count) || (ev_max == 0 && r.count == r.cap)));
-        }
-        wait(s_full + 8 * st, ns & 1);
-        fence_after();
-        if (!idle) {
-          // The row is read from tensor memory twice, 64 columns at a time, once for its maximum and once for P: the loop
-          // bodies stay small (at the start of a launch every instruction comes from cold memory, and a row unrolled over
-          // 128 columns took microseconds there) and the registers hold half a row.
-          const uint32_t ts = tS[st] + lane_off;
-          const int cols = draft ? a.nb : TN;
-          uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};       // columns the row sees
+        const int tile0 = (u < len2 ? t0 + u : u - len2) * TN;
+#pragma unroll 1
+        for (int h = 0; h < (draft ? 1 : 2); ++h, ++ns) {
+          const int slot0 = tile0 + h * TH;
+          bool clean = false;
+          uint32_t keep0 = ~0u, keep1 = ~0u;             // columns the row sees
           if (draft) {
-            keep[0] = (uint32_t)vis;
-            keep[1] = (uint32_t)(vis >> 32);
-          } else if (!clean) {
-            // three runs of slots: pinned; from the oldest one seen to the end of the ring; what has wrapped round
-            const int z = r.sink + r.head - slot0;
-            const int lo1 = z + ev, hi1 = min(z + r.count, W - slot0);
-            const int lo2 = max(z - r.cap + ev, r.sink - slot0), hi2 = min(z - r.cap + r.count, z);
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-              keep[w] = run_mask(-slot0, r.sink - slot0, 32 * w) | run_mask(lo1, hi1, 32 * w) | run_mask(lo2, hi2, 32 * w);
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int c = 0; c < cols; c += 64) {
-            float x[64];
-            ld32(ts + c, x);
-            ld32(ts + c + 32, x + 32);
-            wait_ld();
-            if (!clean) {
-              const uint32_t k0 = c == 0 ? keep[0] : keep[2], k1 = c == 0 ? keep[1] : keep[3];
-#pragma unroll
-              for (int y = 0; y < 32; ++y) {
-                if (!(k0 & (1u << y))) x[y] = -INFINITY;
-                if (!(k1 & (1u << y))) x[y + 32] = -INFINITY;
-              }
-            }
-#pragma unroll
-            for (int y = 0; y < 64; ++y) mx[y & 3] = fmaxf(mx[y & 3], x[y]);
-          }
-          const float mnew = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
-          if (!started) {
-            m = mnew;
+            keep0 = (uint32_t)vis;
+            keep1 = (uint32_t)(vis >> 32);
           } else {
-            const bool grown = (mnew - m) * sl2 > 8.f;   // false while nothing has been seen (NaN)
-            if (__any_sync(0xffffffffu, grown)) {
-              const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
-              if (grown) m = mnew;
-              l *= corr;
-#pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                float o[32];
-                ld32(tO[st] + lane_off + c, o);
-                wait_ld();
-#pragma unroll
-                for (int y = 0; y < 32; ++y) o[y] *= corr;
-                st32(tO[st] + lane_off + c, reinterpret_cast<uint32_t*>(o));
-              }
+            int d0 = slot0 - r.sink - r.head;
+            if (d0 < 0) d0 += r.cap;
+            clean = slot0 + TH <= r.sink ||
+                    (slot0 >= r.sink && slot0 + TH <= W &&
+                     ((d0 >= ev_max && d0 + TH <= r.count) || (ev_max == 0 && r.count == r.cap)));
+            if (!clean) {
+              // three runs of slots: pinned; from the oldest one seen to the end of the ring; what has wrapped round
+              const int z = r.sink + r.head - slot0;
+              const int lo1 = z + ev, hi1 = min(z + r.count, W - slot0);
+              const int lo2 = max(z - r.cap + ev, r.sink - slot0), hi2 = min(z - r.cap + r.count, z);
+              keep0 = run_mask(-slot0, r.sink - slot0, 0) | run_mask(lo1, hi1, 0) | run_mask(lo2, hi2, 0);
+              keep1 = run_mask(-slot0, r.sink - slot0, 32) | run_mask(lo1, hi1, 32) | run_mask(lo2, hi2, 32);
             }
           }
-          const float neg = m == -INFINITY ? 0.f : -m * sl2;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-          for (int c = 0; c < cols; c += 64) {
-            float x[64];
-            uint32_t pk[32];
-            ld32(ts + c, x);
-            ld32(ts + c + 32, x + 32);
+          if (h == 0) {
+            wait(s_full + 8 * st, ntile & 1);
+            fence_after();
+          }
+          if (!idle) {
+            const uint32_t ts = tS + st * TN + h * TH + lane_off;
+            float x[TH];
+            ld32(ts, x);
+            ld32(ts + 32, x + 32);
             wait_ld();
             if (!clean) {
-              const uint32_t k0 = c == 0 ? keep[0] : keep[2], k1 = c == 0 ? keep[1] : keep[3];
 #pragma unroll
               for (int y = 0; y < 32; ++y) {
-                if (!(k0 & (1u << y))) x[y] = -INFINITY;
-                if (!(k1 & (1u << y))) x[y + 32] = -INFINITY;
+                if (!(keep0 & (1u << y))) x[y] = -INFINITY;
+                if (!(keep1 & (1u << y))) x[y + 32] = -INFINITY;
               }
             }
+            float mx[4] = {m, x[0], x[1], x[2]};
 #pragma unroll
-            for (int y = 0; y < 64; y += 2) {
-              const float p0 = tt_ex2(fmaf(x[y], sl2, neg)), p1 = tt_ex2(fmaf(x[y + 1], sl2, neg));
-              sum[(y >> 1) & 3] += p0 + p1;
-              pk[y >> 1] = tt_pack(p0, p1);
+            for (int y = 3; y + 1 < TH; y += 2) mx[(y >> 1) & 3] = tt_max3(mx[(y >> 1) & 3], x[y], x[y + 1]);
+            const float mnew = tt_max3(tt_max3(mx[0], mx[1], mx[2]), mx[3], x[TH - 1]);
+            if (!started) {
+              m = mnew;
+            } else {
+              const bool grown = (mnew - m) * sl2 > 8.f;         // false while nothing has been seen (NaN)
+              if (__any_sync(0xffffffffu, grown)) {
+                const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
+                if (grown) m = mnew;
+                l *= corr;
+                wait(pv_done + 8 * st, (ns - 1) & 1);    // O is at rest: the product before this block's has been added
+                fence_after();
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                  float o[32];
+                  ld32(tO + st * D + lane_off + c, o);
+                  wait_ld();
+#pragma unroll
+                  for (int y = 0; y < 32; ++y) o[y] *= corr;
+                  st32(tO + st * D + lane_off + c, reinterpret_cast<uint32_t*>(o));
+                }
+              }
             }
-            st32(ts + c / 2, pk);                        // over columns that have been read: c / 2 + 32 <= c + 64
+            const float neg = m == -INFINITY ? 0.f : -m * sl2;
+            const uint64_t neg2 = tt_two(neg, neg), scl2 = tt_two(sl2, sl2);
+            uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
+            uint32_t pk[32];
+#pragma unroll
+            for (int y = 0; y < TH; y += 2) {
+              float e0, e1;
+              tt_both(tt_fma2(tt_two(x[y], x[y + 1]), scl2, neg2), e0, e1);
+              e0 = tt_ex2(e0);
+              e1 = tt_ex2(e1);
+              sum[(y >> 1) & 3] = tt_add2(sum[(y >> 1) & 3], tt_two(e0, e1));
+              pk[y >> 1] = tt_pack(e0, e1);
+            }
+            st32(tS + st * TN + h * (TH / 2) + lane_off, pk);     // over columns that have been read
+            float s0, s1;
+            tt_both(tt_add2(tt_add2(sum[0], sum[1]), tt_add2(sum[2], sum[3])), s0, s1);
+            l += s0 + s1;
+            wait_st();
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          wait_st();
+          started = true;
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(p_full + 16 * st + 8 * h);
         }
-        started = true;
-        fence_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(p_full + 8 * st);
+        ++ntile;
       }
       // ---- the item's rows ------------------------------------------------------------------------------------------------
       const bool both = two || n > 1;                    // the second stream had tiles
@@ -781,12 +861,12 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
         float o[32];
         if (idle) continue;
         if (two) {
-          ld32(tO[st] + lane_off + c, o);
+          ld32(tO + st * D + lane_off + c, o);
           wait_ld();
         } else {
           float o1[32];
-          ld32(tO[0] + lane_off + c, o);
-          if (both) ld32(tO[1] + lane_off + c, o1);
+          ld32(tO + lane_off + c, o);
+          if (both) ld32(tO + D + lane_off + c, o1);
           wait_ld();
 #pragma unroll
           for (int y = 0; y < 32; ++y) o[y] = both ? fmaf(o1[y], w1, o[y] * w0) : o[y] * w0;
