@@ -15,7 +15,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Layout {
   size_t K, V, head, count, n_app, n_sink, stageK, stageV, n_staged, evict_first, S, S0, Qa, Wk, Wv, enc_set,
-      part_acc, part_ml, tickets, status, lora_u, lora_w, tree_part, tree_ml, tree_tickets, total;
+      part_acc, part_ml, tickets, status, lora_u, lora_w, tree_part, tree_ml, tree_pieces, total;
   // importance-aware policy only
   size_t slot_tok, score, live_bits, logits, lse2, pending, fq, fq_head, fq_count, ev_tok, ev_slot;
 };
@@ -95,11 +95,11 @@ Layout make_layout(const ptenc_config* c) {
     o.ev_tok = take(L * B * E * 8);
     o.ev_slot = take(L * B * E * 4);
   }
-  o.tree_part = o.tree_ml = o.tree_tickets = 0;
+  o.tree_part = o.tree_ml = o.tree_pieces = 0;
   if (ptenc_tree_tc_shape(c)) {
     o.tree_part = take(ptenc_tree_part_bytes(c));
     o.tree_ml = take(ptenc_tree_ml_bytes(c));
-    o.tree_tickets = take(PTENC_TREE_SLOTS * 4);
+    o.tree_pieces = take(PTENC_TREE_SLOTS * 4);
   }
   o.total = off;
   return o;
@@ -265,7 +265,7 @@ int ptenc_cache_create(const ptenc_config* cfg, void* ws, size_t bytes, void* st
   c->lora_w = reinterpret_cast<__nv_bfloat16*>(base + lay.lora_w);
   c->tree_part = reinterpret_cast<float*>(base + lay.tree_part);
   c->tree_ml = reinterpret_cast<float*>(base + lay.tree_ml);
-  c->tree_tickets = reinterpret_cast<int*>(base + lay.tree_tickets);
+  c->tree_pieces = reinterpret_cast<int*>(base + lay.tree_pieces);
   d.policy = cfg->policy; d.recent = cfg->recent; d.wb = 0;
   d.slot_tok = nullptr; d.score = nullptr; d.live_bits = nullptr; d.logits = nullptr; d.lse2 = nullptr;
   d.pending = nullptr; d.fq = nullptr; d.fq_head = nullptr; d.fq_count = nullptr; d.ev_tok = nullptr; d.ev_slot = nullptr;
@@ -311,7 +311,6 @@ int ptenc_cache_reset(ptenc_cache* c, const uint8_t* seq_mask, void* stream) {
     // of split units behind; the full reset is the documented way back, so it clears them with the status word.
     const PtencDev& d = c->dev;
     if (cudaMemsetAsync(d.tickets, 0, (size_t)d.L * d.B * d.Hkv * 4, st) != cudaSuccess) return PTENC_ECUDA;
-    if (c->tree_tc && cudaMemsetAsync(c->tree_tickets, 0, PTENC_TREE_SLOTS * 4, st) != cudaSuccess) return PTENC_ECUDA;
   }
   return ptenc_launch_reset(c, seq_mask, st) == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
 }

@@ -85,9 +85,9 @@ struct ptenc_cache {
   int tc_stage_box;             // token rows per TMA box of the staged maps
   bool tree_tc;                 // tensor-core kernel usable for draft trees
   CUtensorMap tmTreeK, tmTreeV; // 3-D maps over the rings: units x W x D, boxes of up to 128 slots
-  float* tree_part;             // partial rows of split blocks of a tree call, their (m, l) and arrival counters
+  float* tree_part;             // partial rows of split blocks of a tree call, their (m, l) and numbers of parts
   float* tree_ml;
-  int* tree_tickets;
+  int* tree_pieces;
   float* lora_u;                // [PTENC_LORA_MAX_PART][L][B][r] partial sums of B x (scratch of ptenc_lora_apply)
   __nv_bfloat16* lora_w;        // [2][L][B][G] S (B x) split into two bf16 terms (scratch of ptenc_lora_apply)
 };

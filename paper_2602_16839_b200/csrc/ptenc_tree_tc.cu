@@ -9,18 +9,20 @@
 // one more tile at the end.  Per CTA (one per SM, persistent, items handed out by a counter):
 //  * warp 0, one lane: producer.  Describes the item, then TMA-loads its Q tiles and the K and V tiles (128-byte swizzle;
 //    plain loads of this GPU's own memory) into a ring of stages.
-//  * warp 1, one lane: issues the MMAs.  Two streams, each with its own S, P and O in tensor memory: with two row tiles a
-//    stream per row tile; with one, the K/V tiles alternate between the streams and the two results are merged at the end.
-//    One stream's products run under the other's softmax, and the product with the first half of a tile's V under the
-//    softmax of the second half.  S = Q K^T (both K-major in shared memory), O += P V (P bf16 in tensor memory over the
-//    S it came from, V as it lies: tokens x head_dim, MN-major).
-//  * warp 2: patches.  Works out what each node sees (ptenc_tree.cuh), and passes every stage on; in the tiles where some
-//    slot is not seen by some node it clears the V rows that nobody sees and takes non-finite values out of the V rows
-//    that only some nodes see, since 0 * NaN would carry them into the other nodes' rows.
-//  * warps 4..11: softmax, a row per thread: S from tensor memory, mask, running maximum and sum in fp32 (base 2), P
-//    rounded to bf16 back to tensor memory.  O is rescaled only when the maximum has grown by more than 2^8, which for
-//    most rows is never after the first tiles.  Non-finite values that were taken out are added to the rows that see them.
-//  * Items that are a part of a block's tiles leave fp32 partials; the CTA that arrives last (ticket) joins them in order.
+//  * warp 1: issues the MMAs (one elected lane).  Two streams, each with its own S, P and O in tensor memory: with two row
+//    tiles a stream per row tile; with one, the K/V tiles alternate between the streams and the two results are merged at
+//    the end.  One stream's products run under the other's softmax.  S = Q K^T (both K-major in shared memory), O += P V (P
+//    bf16 in tensor memory over the S it came from, V as it lies: tokens x head_dim, MN-major).
+//  * warps 2 and 3: patches.  Warp 2 works out what each node sees (ptenc_tree.cuh); both pass every stage on, and in the
+//    tiles where some slot is not seen by some node they clear the V rows that nobody sees and take non-finite values out of
+//    the V rows that only some nodes see, since 0 * NaN would carry them into the other nodes' rows.
+//  * warps 4..19: softmax, eight warps per stream, a row per thread and half of a tile's tokens: S from tensor memory, mask,
+//    maximum (the two halves exchange theirs through shared memory), running sum in fp32 (base 2), P rounded to bf16 back to
+//    tensor memory.  A warp alone is bound by its own latencies, so four warps share a scheduler.  O is rescaled only when
+//    the maximum has grown by more than 2^8, which for most rows is never after the first tiles.  Non-finite values that
+//    were taken out of V are added to the rows that see them.
+//  * Items that are a part of a block's tiles leave fp32 partials, which k_tree_join, chained by programmatic dependent
+//    launch, joins in order: a thread per row and eight columns, so the join is spread over the machine.
 //  * Every wait is bounded: one that runs out raises a status bit and an abort flag, every role then leaves, copies and
 //    MMAs in flight are drained and tensor memory is freed.
 #include <string.h>
@@ -30,17 +32,17 @@
 
 namespace {
 
-constexpr long long TT_CLOCKS = 4000000000ll;  // longest wait: two seconds
+constexpr uint32_t TT_POLLS = 2000;             // bounded wait: tries of up to a millisecond each before giving up
 constexpr int TN = 128;                        // slots per K/V tile
-constexpr int TH = 64;                         // tokens per softmax block: half a tile
+constexpr int TH = 64;                         // tokens of a softmax thread: half a tile
 constexpr int TM = 128;                        // rows of a row tile = TMEM lanes
-constexpr int TT_THREADS = 384;                // producer, MMA, patch, (none), 2 x 4 softmax warps
-constexpr int TT_SOFT = 256;
+constexpr int TT_THREADS = 640;                // producer, MMA, two patch warps, 2 x 8 softmax warps
+constexpr int TT_SOFT = 512;
 constexpr int TT_LEAD = 128;                   // the softmax thread that speaks for all of them
-// Registers: 384 threads are launched with 168 each (64512); the first four warps give up 88 so that a softmax thread can
-// hold a row of 128 scores: 128 * 80 + 256 * 208 = 63488.
-constexpr int TT_REGS_LOW = 80, TT_REGS_HIGH = 208;
-static_assert(128 * TT_REGS_LOW + 256 * TT_REGS_HIGH <= 384 * 168, "the split waits for registers that do not exist");
+// Registers: 640 threads are launched with 96 each (61440); the first four warps give up 32 so that a softmax thread can hold
+// its 64 scores: 128 * 64 + 512 * 104 = 61440.
+constexpr int TT_REGS_LOW = 64, TT_REGS_HIGH = 104;
+static_assert(128 * TT_REGS_LOW + 512 * TT_REGS_HIGH <= 640 * 96, "the split waits for registers that do not exist");
 constexpr int HALF = TN * 128;                 // 64 columns of a 128-row tile
 constexpr int TT_MAX_PIECES = 16;
 
@@ -55,29 +57,30 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Lets the hardware park the thread for up to a millisecond instead of spinning: the waiting warps share their schedulers
+// with the softmax warps.
 __device__ __forceinline__ uint32_t bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
   return ok;
 }
 // Bounded wait that also gives up when another role has raised the abort flag.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   if (bar_try(bar, parity)) return true;
-  const long long t0 = clock64();
-  while (clock64() - t0 < TT_CLOCKS) {
-    if (bar_try(bar, parity) || bar_try(bar, parity)) return true;
+  for (uint32_t i = 0; i < TT_POLLS; ++i) {
+    if (bar_try(bar, parity)) return true;
     if (*abort_flag != 0) return false;
   }
   return false;
 }
 // Bounded wait for what completes by itself: copies and products in flight.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
-  const long long t0 = clock64();
-  while (!bar_try(bar, parity) && clock64() - t0 < TT_CLOCKS) {}
+  for (uint32_t i = 0; i < TT_POLLS; ++i)
+    if (bar_try(bar, parity)) return;
 }
 // True in one lane of the (converged) warp.
 __device__ __forceinline__ bool tt_elect() {
@@ -121,14 +124,19 @@ __device__ __forceinline__ void ld32(uint32_t t, float* v) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(t) : "memory");
 }
-__device__ __forceinline__ void st32(uint32_t t, const uint32_t* r) {
+__device__ __forceinline__ void ld16(uint32_t t, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(t) : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t t, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
       ::"r"(t), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ float tt_ex2(float x) {
   float y;
@@ -154,9 +162,10 @@ __device__ __forceinline__ uint64_t tt_add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+// NaN if any of the three is.
 __device__ __forceinline__ float tt_max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
@@ -164,6 +173,9 @@ __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TT_SOFT) : "memory"); }
+__device__ __forceinline__ void stream_sync(int st) {                        // the eight warps of a stream
+  asm volatile("bar.sync %0, %1;" ::"r"(2 + st), "n"(TT_SOFT / 2) : "memory");
+}
 
 // Shared-memory descriptors of bf16 tiles of 128-byte rows with the 128-byte swizzle.
 // K-major (the contraction index runs along the row): groups of 8 rows 1024 bytes apart.
@@ -189,10 +201,10 @@ struct TSmem {
   static constexpr int STAGES = D == 128 ? 5 : 10;
   static constexpr int OFF_Q = STAGES * TILE;                        // two Q tiles
   static constexpr int OFF_VIS = OFF_Q + 2 * TILE;                   // u64 [64] what each node sees of the draft
-  static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // float2 [128]
+  static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // exchange: bf16 [2][2][128] maxima, float2 [128]
   static constexpr int OFF_DESC = OFF_ML + TM * 8;                   // int [2][32] items
   static constexpr int OFF_BAR = OFF_DESC + 2 * 32 * 4;
-  static constexpr int N_BAR = 3 * STAGES + 24;
+  static constexpr int N_BAR = 3 * STAGES + 20;
   static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]
   static constexpr int OFF_JUMP = OFF_DEPTH + TREE_MAX;              // s8 [64]
   static constexpr int OFF_MISC = OFF_JUMP + TREE_MAX;
@@ -214,7 +226,7 @@ struct TreeTcArgs {
   const __nv_bfloat16* v_tree;
   float* part;                     // [slot][2][D / 4][128][4]
   float2* part_ml;                 // [slot][2][128]
-  int* tickets;                    // [block that is split]
+  int* pieces;                     // [block that is split]: its parts, 0 if there is nothing to join
 };
 
 // Item description words in shared memory.
@@ -242,12 +254,40 @@ __device__ __forceinline__ uint32_t run_mask(int lo, int hi, int at) {
   return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
 }
 
+// Adds the non-finite values of the V rows that this row sees and others do not (they were taken out of the products) to 16 of
+// its columns.
+__device__ __noinline__ void add_not_finite(float* o, int c, const PtencDev& p, const __nv_bfloat16* vt, size_t ring, TreeRing r,
+                                            int ev, int ev_max, unsigned long long vis, int nodes, int lo, int n, int nt, int t0,
+                                            int len2) {
+  for (int i = 0; i < n; ++i) {
+    const int u = lo + i;
+    const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
+    const bool draft = u == nt - 1;
+    for (int t = 0; t < (draft ? nodes : TN); ++t) {
+      const __nv_bfloat16* v;
+      if (draft) {
+        if (!((vis >> t) & 1ull)) continue;
+        v = vt + (size_t)t * p.Hkv * p.D;
+      } else {
+        int dd = slot0 + t - r.sink - r.head;
+        if (dd < 0) dd += r.cap;
+        if (slot0 + t < r.sink || slot0 + t >= p.W || dd < ev || dd >= ev_max || dd >= r.count) continue;
+        v = reinterpret_cast<const __nv_bfloat16*>(p.V) + ring + (size_t)(slot0 + t) * p.D;
+      }
+      for (int y = 0; y < 16; ++y) {
+        const float x = __bfloat162float(v[c + y]);
+        if (!isfinite(x)) o[y] += x;
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ kernel
 template <int D>
 __global__ void __launch_bounds__(TT_THREADS, 1)
-k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
           const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKt,
-          const __grid_constant__ CUtensorMap tmVt, const TreeTcArgs a) {
+          const __grid_constant__ CUtensorMap tmVt, const __grid_constant__ TreeTcArgs a) {
   using SM = TSmem<D>;
   constexpr int NS = SM::STAGES, TILE = SM::TILE, DH = D / 64;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -255,33 +295,33 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
   volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
   unsigned long long* s_vis = reinterpret_cast<unsigned long long*>(smem + SM::OFF_VIS);
   float2* s_ml = reinterpret_cast<float2*>(smem + SM::OFF_ML);
+  __nv_bfloat16* s_mx = reinterpret_cast<__nv_bfloat16*>(smem + SM::OFF_ML);
   uint8_t* s_depth = smem + SM::OFF_DEPTH;
   int8_t* s_jump = reinterpret_cast<int8_t*>(smem + SM::OFF_JUMP);
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
-  volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict, misc[3]: last arriver
+  volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict on the next item
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
-  // p_full: [stream][half]; the others with two entries: [stream], [Q tile] or [item slot]
-  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, pv_done = p_full + 32, o_full = pv_done + 16,
-                 q_full = o_full + 16, q_empty = q_full + 16, item_full = q_empty + 16, item_empty = item_full + 16,
-                 o_empty = item_empty + 16, info_full = o_empty + 8, info_empty = info_full + 8, drain = info_empty + 8;
+  // barriers with two entries: [stream], [Q tile] or [item slot]
+  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16,
+                 q_empty = q_full + 16, item_full = q_empty + 16, item_empty = item_full + 16, o_empty = item_empty + 16,
+                 info_full = o_empty + 8, info_empty = info_full + 8, drain = info_empty + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int W = p.W, B = p.B, Hkv = p.Hkv, g = p.g;
 
   if (tid == 0) {
-    for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 2); bar_init(ready + 8 * s, 1); }
-    for (int s = 0; s < 4; ++s) bar_init(p_full + 8 * s, 4);
+    for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 3); bar_init(ready + 8 * s, 2); }
     for (int s = 0; s < 2; ++s) {
       bar_init(s_full + 8 * s, 1);
-      bar_init(pv_done + 8 * s, 1);
+      bar_init(p_full + 8 * s, 8);
       bar_init(o_full + 8 * s, 1);
       bar_init(q_full + 8 * s, 1);
       bar_init(q_empty + 8 * s, 1);
       bar_init(item_full + 8 * s, 1);
-      bar_init(item_empty + 8 * s, 2 + 8);               // MMA lane, patch warp, softmax warps
+      bar_init(item_empty + 8 * s, 1 + 2 + 16);          // MMA, patch and softmax warps
     }
-    bar_init(o_empty, 8);
+    bar_init(o_empty, 16);
     bar_init(info_full, 1);
-    bar_init(info_empty, 8);
+    bar_init(info_empty, 1 + 16);
     bar_init(drain, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -291,6 +331,23 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // What the producer has to know of an item's sequence; the first item's is requested while tensor memory is allocated.
+  struct Words { int act, n, head, count, sink; };
+  auto words_of = [&](int item) -> Words {
+    const int blk = item < a.n_full ? item : a.n_full + (item - a.n_full) / a.P;
+    const int e = blk / a.nqp / Hkv, li = e / B, b = e - li * B;
+    const size_t lb = (size_t)(a.l0 + li) * B + b;
+    Words w;
+    w.act = a.active != nullptr ? a.active[b] : 1;
+    w.n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
+    w.head = p.head[lb];
+    w.count = p.count[lb];
+    w.sink = p.n_sink[lb];
+    return w;
+  };
+  Words words = {0, 0, 0, 0, 0};
+  if (tid == 0) words = words_of((int)blockIdx.x);       // gridDim.x <= n_items
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   fence_before();
   __syncthreads();
   fence_after();
@@ -310,6 +367,7 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       uint32_t pos = 0, qn = 0, seq = 0;                 // ring entries, Q tiles and items so far
       bool okay = true;
       int item = (int)blockIdx.x;
+      bool fresh = true;
       while (okay) {
         const int last_grab = a.n_items + (int)gridDim.x - 1;
         if (item >= a.n_items) {
@@ -332,17 +390,19 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
           pieces = a.P;
           blk = a.n_full + split;
         }
+        const Words w = fresh ? words : words_of(item);
+        fresh = false;
         item = next;
         const int unit = blk / a.nqp, qp = blk - unit * a.nqp;
         const int e = unit / Hkv, h = unit - e * Hkv;
         const int li = e / B, b = e - li * B;
         const size_t lb = (size_t)(a.l0 + li) * B + b;
-        const int act = a.active != nullptr ? a.active[b] : 1;
-        const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
+        const int n = w.n;
         TreeRing r;
-        const bool ring_ok = tree_ring(p, lb, &r);
-        if (act == 0) continue;
-        if (!ring_ok || n < 0 || n > a.NT) {
+        r.head = w.head; r.count = w.count; r.sink = w.sink; r.cap = W - w.sink; r.e = min(p.E, r.cap);
+        if (split >= 0 && piece == 0) a.pieces[split] = 0;           // until its rows say otherwise
+        if (w.act == 0) continue;
+        if (r.sink < 0 || r.cap < 1 || r.head < 0 || r.head >= r.cap || r.count < 0 || r.count > r.cap || n < 0 || n > a.NT) {
           atomicOr(p.status, PTENC_ST_BAD_INDEX);
           continue;
         }
@@ -417,7 +477,7 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
     constexpr uint32_t ID_QK = tt_idesc(TN, 0), ID_PV = tt_idesc(D, 1);
     const uint32_t ID_QKD = tt_idesc(a.nb, 0);
     uint32_t base = 0, qn = 0, seq = 0, items = 0;
-    uint32_t np0 = 0, np1 = 0;                           // bits 0 and 1: parity of the halves consumed per stream
+    uint32_t np0 = 0, np1 = 0;                           // tiles of the streams whose P has been taken
     bool okay = true;
     while (okay) {
       if (!wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { okay = false; break; }
@@ -426,18 +486,17 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       if (kind == 0) break;
       const bool two = __shfl_sync(0xffffffffu, d[I_TWO], 0) != 0;
       const int n = __shfl_sync(0xffffffffu, d[I_CNT], 0);
-      const int draft = __shfl_sync(0xffffffffu, d[I_NT] - 1 - d[I_LO], 0);   // the draft's tile, if the item has it: one half
+      const int draft = __shfl_sync(0xffffffffu, d[I_NT] - 1 - d[I_LO], 0);   // the draft's tile, if the item has it
       __syncwarp();
       if (leader) bar_arrive(item_empty + 8 * (seq & 1));
       ++seq;
       const uint32_t q0 = qn, nq = two ? 2 : 1;
       const int stride = two ? 1 : 2;                    // a stream's next tile
-      auto issue_s = [&](auto ST, int i) -> bool {       // S = Q K^T of the stream's tile i
+      const int off1 = two ? 0 : 1;                      // with one row tile the second stream takes the odd tiles
+      // S = Q K^T of tile i; whoever sees it done knows that the stream's products before it are done too
+      auto issue_s = [&](auto ST, int i) {
         constexpr int st = decltype(ST)::value;
-        if (i >= n) return true;
-        const uint32_t ps = base + pos_k(i, two), s = ps % NS;
-        if (!wait(full + 8 * s, (ps / NS) & 1)) return false;
-        fence_after();
+        const uint32_t s = (base + pos_k(i, two)) % NS;
         const uint64_t dq = desc_k(sb + SM::OFF_Q + ((q0 + (two ? st : 0)) & 1) * TILE), dk = desc_k(sb + s * TILE);
         const uint32_t id = i == draft ? ID_QKD : ID_QK;
         if (leader) {
@@ -447,58 +506,52 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
             mma_ss(tS + st * TN, dq + off, dk + off, id, k > 0);
           }
           commit(s_full + 8 * st);
-          if (!two || st == 1) commit(empty + 8 * s);
         }
         __syncwarp();
-        return true;
+      };
+      auto wait_k = [&](int i) -> bool {
+        if (i >= n) return true;
+        const uint32_t ps = base + pos_k(i, two);
+        return wait(full + 8 * (ps % NS), (ps / NS) & 1);
       };
       bool first = true;
-      auto issue_pv = [&](auto ST, int i, uint32_t& np) -> bool {              // O += P V of the stream's tile i
+      // O += P V of the stream's tile i, then S of its next tile.  What does not depend on P is waited for first.
+      auto step = [&](auto ST, int i, uint32_t& np) -> bool {
         constexpr int st = decltype(ST)::value;
         if (i >= n) return true;
         const uint32_t ps = base + pos_v(i, n, two), s = ps % NS;
-        const uint32_t start = i < stride ? 0u : 1u;                           // 0: the product replaces what O holds
         const uint64_t dv = desc_mn(sb + s * TILE);
-        const int ks = i == draft ? a.nb / 16 : TH / 16;
-        if (!wait(p_full + 16 * st, np & 1)) return false;
-        np ^= 1;
+        const uint32_t start = i < stride ? 0u : 1u;                           // 0: the product replaces what O holds
+        const int ks = i == draft ? a.nb / 16 : TN / 16;
         if (first && !wait(o_empty, (items & 1) ^ 1)) return false;            // O of the item before is out
         first = false;
-        if (!wait(ready + 8 * s, (ps / NS) & 1)) return false;
+        if (!wait(ready + 8 * s, (ps / NS) & 1) || !wait_k(i + stride)) return false;
+        if (!wait(p_full + 8 * st, np & 1)) return false;
+        ++np;
         fence_after();
         if (leader) {
 #pragma unroll
-          for (int k = 0; k < TH / 16; ++k)
-            if (k < ks) mma_ts(tO + st * D, tS + st * TN + 8 * k, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : start);
-          commit(pv_done + 8 * st);
-        }
-        __syncwarp();
-        if (i != draft) {
-          if (!wait(p_full + 16 * st + 8, (np >> 1) & 1)) return false;
-          np ^= 2;
-          fence_after();
-          if (leader) {
-#pragma unroll
-            for (int k = TH / 16; k < TN / 16; ++k)
-              mma_ts(tO + st * D, tS + st * TN + 8 * k, dv + (k * 2048 >> 4), ID_PV, 1u);
-            commit(pv_done + 8 * st);
-          }
-        }
-        if (leader) {
-          if (!two || st == 1) commit(empty + 8 * s);
+          for (int k = 0; k < TN / 16; ++k)
+            if (k < ks)                                  // P lies at the start of each half of S
+              mma_ts(tO + st * D, tS + st * TN + (k >> 2) * TH + (k & 3) * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : start);
           if (i + stride >= n) commit(o_full + 8 * st);
         }
         __syncwarp();
+        if (i + stride < n) issue_s(ST, i + stride);
         return true;
       };
       using S0 = std::integral_constant<int, 0>;
       using S1 = std::integral_constant<int, 1>;
       for (uint32_t t = 0; t < nq && okay; ++t) okay = wait(q_full + 8 * ((q0 + t) & 1), ((q0 + t) >> 1) & 1);
-      const int off1 = two ? 0 : 1;                      // with one row tile the second stream takes the odd tiles
-      okay = okay && issue_s(S0(), 0) && issue_s(S1(), off1);
-      for (int i = 0; i < n && okay; i += stride)
-        okay = issue_pv(S0(), i, np0) && issue_s(S0(), i + stride) && issue_pv(S1(), i + off1, np1) &&
-               issue_s(S1(), i + off1 + stride);
+      okay = okay && wait_k(0);
+      fence_after();
+      if (okay) issue_s(S0(), 0);
+      if (okay && off1 < n) {
+        okay = wait_k(off1);
+        fence_after();
+        if (okay) issue_s(S1(), off1);
+      }
+      for (int i = 0; i < n && okay; i += stride) okay = step(S0(), i, np0) && step(S1(), i + off1, np1);
       if (okay && leader)
         for (uint32_t t = 0; t < nq; ++t) commit(q_empty + 8 * ((q0 + t) & 1));
       __syncwarp();
@@ -512,8 +565,9 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       bar_drain(drain, 0);
     }
     __syncwarp();
-  } else if (warp == 2) {
-    // ================================================================ patch warp
+  } else {
+    // ================================================================ patch warps
+    const int me = warp - 2;
     uint32_t base = 0, seq = 0;
     bool okay = true;
     // the lanes give up together, or not at all
@@ -528,68 +582,76 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       const int n = d[I_CNT], nodes = d[I_N], lo = d[I_LO], nt = d[I_NT], t0 = d[I_T0], len2 = d[I_LEN2];
       TreeRing r;
       r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_E];
-      // ---- what each node sees: the parent relation closed by pointer doubling, two nodes per lane -----------------------
-      const int32_t* par = a.parent + (size_t)d[I_B] * a.NT;
-      int pa[2];
-      unsigned long long anc[2] = {0ull, 0ull};
-      int bad = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int i = lane + 32 * x;
-        pa[x] = -1;
-        if (i < nodes) {
-          const int v = par[i];
-          if (v < -1 || v >= i) bad = 1; else pa[x] = v;
-          anc[x] = 1ull << i;
-        }
-      }
-      bad = __any_sync(0xffffffffu, bad);
-      if (bad) { pa[0] = pa[1] = -1; }
-      if (!wait(info_empty, (seq & 1) ^ 1)) { okay = false; break; }   // the rows have what they need of the last
-      for (int s = 1; s < nodes; s <<= 1) {
+      const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
+      int ev_max;
+      if (me == 0) {
+        // ---- what each node sees: the parent relation closed by pointer doubling, two nodes per lane ---------------------
+        const int32_t* par = a.parent + (size_t)d[I_B] * a.NT;
+        int pa[2];
+        unsigned long long anc[2] = {0ull, 0ull};
+        int bad = 0;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          s_vis[lane + 32 * x] = anc[x];
-          s_jump[lane + 32 * x] = (int8_t)pa[x];
-        }
-        __syncwarp();
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if (pa[x] >= 0) { anc[x] |= s_vis[pa[x]]; pa[x] = s_jump[pa[x]]; }
-        __syncwarp();
-      }
-      int deepest = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int depth = __popcll(anc[x]) - 1;
-        s_depth[lane + 32 * x] = (uint8_t)(depth < 0 ? 0 : depth);
-        deepest = max(deepest, depth);
-      }
-      __syncwarp();
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int gone = tree_evicted(r.count, r.cap, r.e, __popcll(anc[x]));
-        unsigned long long v = anc[x];
-        if (gone > r.count) {                            // a path longer than the ring: its first tokens have left again
-          v = 0;
-          for (unsigned long long m = anc[x]; m != 0; m &= m - 1) {
-            const int j = __ffsll((long long)m) - 1;
-            if (r.count + s_depth[j] >= gone) v |= 1ull << j;
+          const int i = lane + 32 * x;
+          pa[x] = -1;
+          if (i < nodes) {
+            const int v = par[i];
+            if (v < -1 || v >= i) bad = 1; else pa[x] = v;
+            anc[x] = 1ull << i;
           }
         }
-        s_vis[lane + 32 * x] = v;
+        bad = __any_sync(0xffffffffu, bad);
+        if (bad) { pa[0] = pa[1] = -1; }
+        if (!wait(info_empty, (seq & 1) ^ 1)) { okay = false; break; }   // the rows have what they need of the last item
+        for (int s = 1; s < nodes; s <<= 1) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            s_vis[lane + 32 * x] = anc[x];
+            s_jump[lane + 32 * x] = (int8_t)pa[x];
+          }
+          __syncwarp();
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            if (pa[x] >= 0) { anc[x] |= s_vis[pa[x]]; pa[x] = s_jump[pa[x]]; }
+          __syncwarp();
+        }
+        int deepest = 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int depth = __popcll(anc[x]) - 1;
+          s_depth[lane + 32 * x] = (uint8_t)(depth < 0 ? 0 : depth);
+          deepest = max(deepest, depth);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int gone = tree_evicted(r.count, r.cap, r.e, __popcll(anc[x]));
+          unsigned long long v = anc[x];
+          if (gone > r.count) {                          // a path longer than the ring: its first tokens have left again
+            v = 0;
+            for (unsigned long long m = anc[x]; m != 0; m &= m - 1) {
+              const int j = __ffsll((long long)m) - 1;
+              if (r.count + s_depth[j] >= gone) v |= 1ull << j;
+            }
+          }
+          s_vis[lane + 32 * x] = v;
+        }
+        deepest = __reduce_max_sync(0xffffffffu, deepest);
+        ev_max = tree_evicted(r.count, r.cap, r.e, deepest + 1);
+        if (lane == 0) {
+          if (bad) atomicOr(p.status, PTENC_ST_BAD_INDEX);
+          d[I_EVMAX] = ev_max;
+          d[I_VALID] = bad ? 0 : 1;
+          d[I_ODD] = 0;
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(info_full);
+      } else {
+        if (!wait(info_full, seq & 1)) { okay = false; break; }
+        ev_max = d[I_EVMAX];
+        __syncwarp();
+        if (lane == 0) bar_arrive(info_empty);
       }
-      deepest = __reduce_max_sync(0xffffffffu, deepest);
-      const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
-      const int ev_max = tree_evicted(r.count, r.cap, r.e, deepest + 1);
-      if (lane == 0) {
-        if (bad) atomicOr(p.status, PTENC_ST_BAD_INDEX);
-        d[I_EVMAX] = ev_max;
-        d[I_VALID] = bad ? 0 : 1;
-        d[I_ODD] = 0;
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(info_full);
       // ---- pass the stages on, in ring order --------------------------------------------------------------------------------
       for (int k = 0; k < 2 * n; ++k) {
         int i = -1;                                      // the tile whose V this entry is, if it is one
@@ -616,7 +678,7 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
             constexpr int VPR = DH * 8;                  // 16-byte vectors of a row
             const int rows = draft ? a.nb : TN;
             int odd = 0;
-            for (int rb = 0; rb < rows; rb += 32) {
+            for (int rb = 32 * me; rb < rows; rb += 64) {          // the two warps take turns
               const int t = rb + lane;
               bool dead, some;
               if (draft) {
@@ -649,11 +711,17 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
                 } else {
                   uint4 w = *vec;
                   uint32_t* e = reinterpret_cast<uint32_t*>(&w);
-                  int hit = 0;
+                  uint32_t top = 0;                      // exponent bits all set, infinity or NaN, carry into the sign's place
 #pragma unroll
-                  for (int y = 0; y < 4; ++y) {          // exponent bits all set: infinity or NaN
-                    if ((e[y] & 0x7f80u) == 0x7f80u) { e[y] &= 0xffff0000u; hit = 1; }
-                    if ((e[y] & 0x7f800000u) == 0x7f800000u) { e[y] &= 0x0000ffffu; hit = 1; }
+                  for (int y = 0; y < 4; ++y) top |= (e[y] & 0x7fff7fffu) + 0x00800080u;
+                  int hit = 0;
+                  if ((top & 0x80008000u) != 0) {
+                    hit = 1;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                      if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
+                      if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0x0000ffffu;
+                    }
                   }
                   if (hit) { *vec = w; odd = 1; }
                 }
@@ -677,11 +745,12 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
   } else {
     // ================================================================ softmax: stream st, a row per thread
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TT_REGS_HIGH));
-    const int st = (warp - 4) >> 2, quarter = warp & 3;
+    const int st = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1, quarter = warp & 3;
     const int lrow = 32 * quarter + lane;
     const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
-    const float sl2 = 1.4426950408889634f / sqrtf((float)D);
-    uint32_t seq = 0, ns = 0, ntile = 0;                 // items; blocks and tiles of this stream
+    const bool passes = tid == TT_LEAD + 256 * st;       // the thread of the stream that gives stages back
+    const float sl2 = 1.4426950408889634f / sqrtf((float)D), slack = 8.f / sl2;
+    uint32_t seq = 0, ntile = 0, base = 0;               // items; tiles of this stream; ring entries
     uint32_t no0 = 0, no1 = 0;                           // items in which the streams had tiles
     bool fine = true;                                    // a wait that ran out: go through the motions, never wait again
     auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -716,103 +785,121 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       const bool idle = __all_sync(0xffffffffu, !real);  // a warp without rows only keeps the barriers going
       __syncwarp();
       if (lane == 0) bar_arrive(info_empty);
-      float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and sum
-      bool started = false;
+      float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and this half's sum
+      const int stride = two ? 1 : 2;
 #pragma unroll 1
-      for (int i = two ? 0 : st; i < n; i += two ? 1 : 2) {
+      for (int i = two ? 0 : st; i < n; i += stride, ++ntile) {
         const int u = lo + i;
         const bool draft = u == nt - 1;
-        const int tile0 = (u < len2 ? t0 + u : u - len2) * TN;
+        const int slot0 = (u < len2 ? t0 + u : u - len2) * TN + half * TH;
+        bool clean = false;
+        uint32_t keep0 = 0, keep1 = 0;                   // columns the row sees
+        if (draft) {
+          if (half == 0) { keep0 = (uint32_t)vis; keep1 = (uint32_t)(vis >> 32); }
+        } else {
+          int d0 = slot0 - r.sink - r.head;
+          if (d0 < 0) d0 += r.cap;
+          clean = slot0 + TH <= r.sink ||
+                  (slot0 >= r.sink && slot0 + TH <= W &&
+                   ((d0 >= ev_max && d0 + TH <= r.count) || (ev_max == 0 && r.count == r.cap)));
+          if (!clean) {
+            // three runs of slots: pinned; from the oldest one seen to the end of the ring; what has wrapped round
+            const int z = r.sink + r.head - slot0;
+            const int lo1 = z + ev, hi1 = min(z + r.count, W - slot0);
+            const int lo2 = max(z - r.cap + ev, r.sink - slot0), hi2 = min(z - r.cap + r.count, z);
+            keep0 = run_mask(-slot0, r.sink - slot0, 0) | run_mask(lo1, hi1, 0) | run_mask(lo2, hi2, 0);
+            keep1 = run_mask(-slot0, r.sink - slot0, 32) | run_mask(lo1, hi1, 32) | run_mask(lo2, hi2, 32);
+          }
+        }
+        wait(s_full + 8 * st, ntile & 1);
+        fence_after();
+        if (passes && (!two || st == 1)) {               // this S and the products before it are done: their stages are free
+          bar_arrive(empty + 8 * ((base + pos_k(i, two)) % NS));
+          if (i >= stride) bar_arrive(empty + 8 * ((base + pos_v(i - stride, n, two)) % NS));
+        }
+        const bool some = !idle && !(draft && half == 1);          // uniform over the warp
+        // The scores are read from tensor memory twice, 32 at a time, once for the maximum and once for P: held in registers
+        // they would push everything else out of them.
+        const uint32_t ts = tS + st * TN + half * TH + lane_off;
+        float mine = -INFINITY;
+        if (some) {
 #pragma unroll 1
-        for (int h = 0; h < (draft ? 1 : 2); ++h, ++ns) {
-          const int slot0 = tile0 + h * TH;
-          bool clean = false;
-          uint32_t keep0 = ~0u, keep1 = ~0u;             // columns the row sees
-          if (draft) {
-            keep0 = (uint32_t)vis;
-            keep1 = (uint32_t)(vis >> 32);
-          } else {
-            int d0 = slot0 - r.sink - r.head;
-            if (d0 < 0) d0 += r.cap;
-            clean = slot0 + TH <= r.sink ||
-                    (slot0 >= r.sink && slot0 + TH <= W &&
-                     ((d0 >= ev_max && d0 + TH <= r.count) || (ev_max == 0 && r.count == r.cap)));
-            if (!clean) {
-              // three runs of slots: pinned; from the oldest one seen to the end of the ring; what has wrapped round
-              const int z = r.sink + r.head - slot0;
-              const int lo1 = z + ev, hi1 = min(z + r.count, W - slot0);
-              const int lo2 = max(z - r.cap + ev, r.sink - slot0), hi2 = min(z - r.cap + r.count, z);
-              keep0 = run_mask(-slot0, r.sink - slot0, 0) | run_mask(lo1, hi1, 0) | run_mask(lo2, hi2, 0);
-              keep1 = run_mask(-slot0, r.sink - slot0, 32) | run_mask(lo1, hi1, 32) | run_mask(lo2, hi2, 32);
-            }
-          }
-          if (h == 0) {
-            wait(s_full + 8 * st, ntile & 1);
-            fence_after();
-          }
-          if (!idle) {
-            const uint32_t ts = tS + st * TN + h * TH + lane_off;
-            float x[TH];
-            ld32(ts, x);
-            ld32(ts + 32, x + 32);
+          for (int c = 0; c < TH; c += 32) {
+            float x[32];
+            ld32(ts + c, x);
             wait_ld();
             if (!clean) {
+              const uint32_t keep = c == 0 ? keep0 : keep1;
 #pragma unroll
-              for (int y = 0; y < 32; ++y) {
-                if (!(keep0 & (1u << y))) x[y] = -INFINITY;
-                if (!(keep1 & (1u << y))) x[y + 32] = -INFINITY;
-              }
+              for (int y = 0; y < 32; ++y)
+                if (!(keep & (1u << y))) x[y] = -INFINITY;
             }
-            float mx[4] = {m, x[0], x[1], x[2]};
+            float mx[4] = {mine, x[0], x[1], x[2]};
 #pragma unroll
-            for (int y = 3; y + 1 < TH; y += 2) mx[(y >> 1) & 3] = tt_max3(mx[(y >> 1) & 3], x[y], x[y + 1]);
-            const float mnew = tt_max3(tt_max3(mx[0], mx[1], mx[2]), mx[3], x[TH - 1]);
-            if (!started) {
-              m = mnew;
-            } else {
-              const bool grown = (mnew - m) * sl2 > 8.f;         // false while nothing has been seen (NaN)
-              if (__any_sync(0xffffffffu, grown)) {
-                const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
-                if (grown) m = mnew;
-                l *= corr;
-                wait(pv_done + 8 * st, (ns - 1) & 1);    // O is at rest: the product before this block's has been added
-                fence_after();
+            for (int y = 3; y < 31; y += 2) mx[(y >> 1) & 3] = tt_max3(mx[(y >> 1) & 3], x[y], x[y + 1]);
+            mine = tt_max3(tt_max3(mx[0], mx[1], mx[2]), mx[3], x[31]);
+          }
+        }
+        // The halves agree on a maximum; bf16 will do, any common reference near the maximum serves.
+        s_mx[(2 * st + half) * TM + lrow] = __float2bfloat16_rn(mine);
+        stream_sync(st);
+        const float mnew = tt_max3(m, __bfloat162float(s_mx[2 * st * TM + lrow]), __bfloat162float(s_mx[(2 * st + 1) * TM + lrow]));
+        if (i < stride) {
+          m = mnew;
+        } else {
+          const bool grown = !(mnew <= m + slack);       // NaN counts; nothing seen yet and nothing now (-inf) does not
+          if (!idle && __any_sync(0xffffffffu, grown)) {
+            const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
+            if (grown) m = mnew;
+            l *= corr;
+            // O is at rest; each half of the threads rescales half of the columns
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                  float o[32];
-                  ld32(tO + st * D + lane_off + c, o);
-                  wait_ld();
+            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
+              float o[16];
+              ld16(tO + st * D + lane_off + c, o);
+              wait_ld();
 #pragma unroll
-                  for (int y = 0; y < 32; ++y) o[y] *= corr;
-                  st32(tO + st * D + lane_off + c, reinterpret_cast<uint32_t*>(o));
-                }
-              }
+              for (int y = 0; y < 16; ++y) o[y] *= corr;
+              st16(tO + st * D + lane_off + c, reinterpret_cast<uint32_t*>(o));
             }
-            const float neg = m == -INFINITY ? 0.f : -m * sl2;
-            const uint64_t neg2 = tt_two(neg, neg), scl2 = tt_two(sl2, sl2);
-            uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
-            uint32_t pk[32];
+          }
+        }
+        if (some) {
+          // an infinite maximum makes the row NaN, as inf - inf does
+          const float neg = m == -INFINITY ? 0.f : m == INFINITY ? __int_as_float(0x7fffffff) : -m * sl2;
+          const uint64_t neg2 = tt_two(neg, neg), scl2 = tt_two(sl2, sl2);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll 1
+          for (int c = 0; c < TH; c += 32) {
+            float x[32];
+            uint32_t pk[16];
+            ld32(ts + c, x);
+            wait_ld();
+            if (!clean) {
+              const uint32_t keep = c == 0 ? keep0 : keep1;
 #pragma unroll
-            for (int y = 0; y < TH; y += 2) {
+              for (int y = 0; y < 32; ++y)
+                if (!(keep & (1u << y))) x[y] = -INFINITY;
+            }
+#pragma unroll
+            for (int y = 0; y < 32; y += 2) {
               float e0, e1;
               tt_both(tt_fma2(tt_two(x[y], x[y + 1]), scl2, neg2), e0, e1);
               e0 = tt_ex2(e0);
               e1 = tt_ex2(e1);
-              sum[(y >> 1) & 3] = tt_add2(sum[(y >> 1) & 3], tt_two(e0, e1));
+              sum[(y >> 1) & 1] = tt_add2(sum[(y >> 1) & 1], tt_two(e0, e1));
               pk[y >> 1] = tt_pack(e0, e1);
             }
-            st32(tS + st * TN + h * (TH / 2) + lane_off, pk);     // over columns that have been read
-            float s0, s1;
-            tt_both(tt_add2(tt_add2(sum[0], sum[1]), tt_add2(sum[2], sum[3])), s0, s1);
-            l += s0 + s1;
-            wait_st();
+            st16(ts + c / 2, pk);                        // over this half's own scores, those that have been read
           }
-          started = true;
-          fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(p_full + 16 * st + 8 * h);
+          float s0, s1;
+          tt_both(tt_add2(sum[0], sum[1]), s0, s1);
+          l += s0 + s1;
         }
-        ++ntile;
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_full + 8 * st);
       }
       // ---- the item's rows ------------------------------------------------------------------------------------------------
       const bool both = two || n > 1;                    // the second stream had tiles
@@ -821,90 +908,89 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       ++no0;
       if (both) ++no1;
       fence_after();
+      if (passes && (!two || st == 1)) {
+        const int last = two ? n - 1 : ((n - 1 - st) & ~1) + st;   // the stream's last tile, -1 or less if it had none
+        if (last >= 0) bar_arrive(empty + 8 * ((base + pos_v(last, n, two)) % NS));
+      }
+      base += 2 * n;
+      // (m, l) of both streams for everybody: first the halves' sums, then the streams' values
+      float m0, l0, m1, l1;
+      m *= sl2;                                          // base-2 units from here on (-inf stays)
+      {
+        float* s_l = reinterpret_cast<float*>(s_ml);
+        stream_sync(st);                                 // the maxima of the last tile have been read
+        soft_sync();
+        if (half == 1) s_l[2 * lrow + st] = l;
+        soft_sync();
+        if (half == 0) l += s_l[2 * lrow + st];
+        soft_sync();
+        if (half == 0 && st == 1) s_ml[lrow] = make_float2(m, l);
+        soft_sync();
+        { const float2 v = s_ml[lrow]; m1 = v.x; l1 = v.y; }
+        soft_sync();
+        if (half == 0 && st == 0) s_ml[lrow] = make_float2(m, l);
+        soft_sync();
+        { const float2 v = s_ml[lrow]; m0 = v.x; l0 = v.y; }
+      }
       const bool odd = d[I_ODD] != 0;
       const int split = d[I_SPLIT], pieces = d[I_PIECES], piece = d[I_PIECE];
-      const int li = d[I_LI], b = d[I_B], h = d[I_H];
+      const int li = d[I_LI], b = d[I_B], h = d[I_H], node0 = d[I_NODE0];
       const size_t lb = (size_t)(a.l0 + li) * B + b;
-      m *= sl2;                                          // base-2 units from here on (-inf stays)
-      // with one row tile both streams hold parts of the same rows: join (m, l), each half of the threads takes half of
-      // the columns of both
+      // With one row tile both streams hold parts of the same rows; the columns are dealt to the groups of warps.
       float w0 = 1.f, w1 = 0.f;
-      int c_lo = 0, c_hi = D;
-      if (!two) {
-        if (st == 1) s_ml[lrow] = make_float2(m, l);
-        soft_sync();
-        if (st == 0) {
-          const float2 o = s_ml[lrow];
-          const float mm = fmaxf(m, o.x);
-          w0 = m == -INFINITY ? 0.f : tt_ex2(m - mm);
-          w1 = o.x == -INFINITY ? 0.f : tt_ex2(o.x - mm);
-          l = w0 * l + w1 * o.y;
-          m = mm;
-          s_ml[lrow] = make_float2(w0, w1);
-        }
-        soft_sync();
-        if (st == 1) { const float2 o = s_ml[lrow]; w0 = o.x; w1 = o.y; }
-        soft_sync();
-        if (st == 0) s_ml[lrow] = make_float2(m, l);
-        soft_sync();
-        if (st == 1) { const float2 o = s_ml[lrow]; m = o.x; l = o.y; }
-        c_lo = st * (D / 2);
+      int c_lo, c_hi;
+      if (two) {
+        m = st == 0 ? m0 : m1;
+        l = st == 0 ? l0 : l1;
+        c_lo = half * (D / 2);
         c_hi = c_lo + D / 2;
+      } else {
+        m = fmaxf(m0, m1);
+        w0 = m0 == -INFINITY ? 0.f : tt_ex2(m0 - m);
+        w1 = m1 == -INFINITY ? 0.f : tt_ex2(m1 - m);
+        l = w0 * l0 + w1 * l1;
+        if (m0 != m0 || m1 != m1) m = l = __int_as_float(0x7fffffff);
+        c_lo = D == 128 ? (2 * st + half) * 32 : (half == 0 ? st * 32 : D);
+        c_hi = D == 128 ? c_lo + 32 : min(c_lo + 32, D);
       }
       const size_t orow = ((size_t)(li * B + b) * a.NT + node) * p.Hq + (size_t)h * g + hh;
-      const float inv = 1.f / l;
+      const float inv = m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;      // every score -inf: NaN
       const int tile_i = two ? st : 0;
       const size_t pslot = split >= 0 ? (((size_t)split * a.P + piece) * a.tpb + tile_i) : 0;
       float4* part = reinterpret_cast<float4*>(a.part) + pslot * (D / 4) * TM;
 #pragma unroll 1
-      for (int c = c_lo; c < c_hi; c += 32) {
-        float o[32];
+      for (int c = c_lo; c < c_hi; c += 16) {
+        float o[16];
         if (idle) continue;
         if (two) {
-          ld32(tO + st * D + lane_off + c, o);
+          ld16(tO + st * D + lane_off + c, o);
           wait_ld();
         } else {
-          float o1[32];
-          ld32(tO + lane_off + c, o);
-          if (both) ld32(tO + D + lane_off + c, o1);
+          float o1[16];
+          ld16(tO + lane_off + c, o);
+          if (both) ld16(tO + D + lane_off + c, o1);
           wait_ld();
 #pragma unroll
-          for (int y = 0; y < 32; ++y) o[y] = both ? fmaf(o1[y], w1, o[y] * w0) : o[y] * w0;
+          for (int y = 0; y < 16; ++y) o[y] = both ? fmaf(o1[y], w1, o[y] * w0) : o[y] * w0;
         }
-        if (odd && real) {
-          // V values that are not finite were left out of the products: they reach the rows that see their token
-          for (int i = 0; i < n; ++i) {
-            const int u = lo + i;
-            const int slot0 = (u < len2 ? t0 + u : u - len2) * TN;
-            const bool draft = u == nt - 1;
-            for (int t = 0; t < (draft ? nodes : TN); ++t) {
-              const __nv_bfloat16* vr;
-              if (draft) {
-                if (!((vis >> t) & 1ull)) continue;
-                vr = a.v_tree + (((size_t)(li * B + b) * a.NT + t) * Hkv + h) * D;
-              } else {
-                int dd = slot0 + t - r.sink - r.head;
-                if (dd < 0) dd += r.cap;
-                if (slot0 + t < r.sink || slot0 + t >= W || dd < ev || dd >= ev_max || dd >= r.count) continue;
-                vr = reinterpret_cast<const __nv_bfloat16*>(p.V) + ((lb * Hkv + h) * W + slot0 + t) * D;
-              }
+        if (odd && real) {                               // rare, and out of line: it would cost the tile loop its registers
+          float x[16];
 #pragma unroll
-              for (int y = 0; y < 32; ++y) {
-                const float v = __bfloat162float(vr[c + y]);
-                if (!isfinite(v)) o[y] += v;
-              }
-            }
-          }
+          for (int y = 0; y < 16; ++y) x[y] = o[y];
+          add_not_finite(x, c, p, a.v_tree + ((size_t)(li * B + b) * a.NT * Hkv + h) * D, (lb * Hkv + h) * (size_t)W * D, r, ev, ev_max,
+                         vis, nodes, lo, n, nt, t0, len2);
+#pragma unroll
+          for (int y = 0; y < 16; ++y) o[y] = x[y];
         }
         if (split >= 0) {
           if (real)
 #pragma unroll
-            for (int y = 0; y < 32; y += 4)
+            for (int y = 0; y < 16; y += 4)
               part[((c + y) >> 2) * TM + lrow] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
         } else if (real && valid) {
           uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
 #pragma unroll
-          for (int y = 0; y < 32; y += 8)
+          for (int y = 0; y < 16; y += 8)
             dst[y >> 3] = make_uint4(tt_pack(o[y] * inv, o[y + 1] * inv), tt_pack(o[y + 2] * inv, o[y + 3] * inv),
                                      tt_pack(o[y + 4] * inv, o[y + 5] * inv), tt_pack(o[y + 6] * inv, o[y + 7] * inv));
         }
@@ -912,83 +998,13 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
       fence_before();
       __syncwarp();
       if (lane == 0) { bar_arrive(o_empty); bar_arrive(item_empty + 8 * (seq & 1)); }
-      const bool writes_lse = real && valid && (two || st == 0);
-      if (split < 0) {
-        if (writes_lse && a.lse != nullptr) a.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
-      } else {
-        // ---- a part of the block's tiles: the CTA that arrives last joins the parts in order ----------------------------
-        if (real && (two || st == 0)) a.part_ml[pslot * TM + lrow] = make_float2(m, l);
-        __threadfence();
-        soft_sync();
-        if (tid == TT_LEAD) {
-          const int old = atomicAdd(&a.tickets[split], 1);
-          const int last = old == pieces - 1;
-          if (last) a.tickets[split] = 0;
-          misc[3] = last;
-        }
-        soft_sync();
-        if (misc[3] && real) {
-          __threadfence();
-          // Two parts' 32 columns are requested together: the join is the tail of the call, and a vector at a time it is a
-          // chain of round trips through L2.
-          const size_t step = (size_t)a.tpb * TM;
-          const float2* ml = a.part_ml + ((size_t)split * a.P * a.tpb + tile_i) * TM + lrow;
-          const float4* src = reinterpret_cast<const float4*>(a.part) + ((size_t)split * a.P * a.tpb + tile_i) * (D / 4) * TM + lrow;
-          float mm = -INFINITY, ll = 0.f;
-#pragma unroll 4
-          for (int q = 0; q < pieces; ++q) mm = fmaxf(mm, __ldcg(ml + q * step).x);
-#pragma unroll 4
-          for (int q = 0; q < pieces; ++q) {
-            const float2 v = __ldcg(ml + q * step);
-            ll = fmaf(v.x == -INFINITY ? 0.f : tt_ex2(v.x - mm), v.y, ll);
-          }
-          const float linv = 1.f / ll;
-#pragma unroll 1
-          for (int c = c_lo; c < c_hi; c += 32) {
-            float4 acc[8];
-#pragma unroll
-            for (int y = 0; y < 8; ++y) acc[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-            for (int q = 0; q < pieces; q += 2) {
-              const int q1 = min(q + 1, pieces - 1);
-              const float4* s0 = src + (q * step * (D / 4) + (c >> 2) * TM);
-              const float4* s1 = src + (q1 * step * (D / 4) + (c >> 2) * TM);
-              const float m0 = __ldcg(ml + q * step).x, m1 = __ldcg(ml + q1 * step).x;
-              float4 v0[8], v1[8];
-#pragma unroll
-              for (int y = 0; y < 8; ++y) { v0[y] = __ldcg(s0 + y * TM); v1[y] = __ldcg(s1 + y * TM); }
-              // a part in which the row sees nothing does not count, whatever it holds
-              if (m0 != -INFINITY) {
-                const float w = tt_ex2(m0 - mm);
-#pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                  acc[y].x = fmaf(w, v0[y].x, acc[y].x); acc[y].y = fmaf(w, v0[y].y, acc[y].y);
-                  acc[y].z = fmaf(w, v0[y].z, acc[y].z); acc[y].w = fmaf(w, v0[y].w, acc[y].w);
-                }
-              }
-              if (q1 != q && m1 != -INFINITY) {
-                const float w = tt_ex2(m1 - mm);
-#pragma unroll
-                for (int y = 0; y < 8; ++y) {
-                  acc[y].x = fmaf(w, v1[y].x, acc[y].x); acc[y].y = fmaf(w, v1[y].y, acc[y].y);
-                  acc[y].z = fmaf(w, v1[y].z, acc[y].z); acc[y].w = fmaf(w, v1[y].w, acc[y].w);
-                }
-              }
-            }
-            if (valid) {
-              uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
-#pragma unroll
-              for (int y = 0; y < 4; ++y)
-                dst[y] = make_uint4(tt_pack(acc[2 * y].x * linv, acc[2 * y].y * linv), tt_pack(acc[2 * y].z * linv, acc[2 * y].w * linv),
-                                    tt_pack(acc[2 * y + 1].x * linv, acc[2 * y + 1].y * linv),
-                                    tt_pack(acc[2 * y + 1].z * linv, acc[2 * y + 1].w * linv));
-            }
-          }
-          if (writes_lse && a.lse != nullptr) a.lse[orow] = (mm + log2f(ll)) * 0.6931471805599453f;
-        }
+      if (real && half == 0 && (two || st == 0)) {       // once per row
+        if (split >= 0) a.part_ml[pslot * TM + lrow] = make_float2(m, l);
+        else if (valid && a.lse != nullptr) a.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
       }
+      if (tid == TT_LEAD && split >= 0 && piece == 0) a.pieces[split] = valid ? pieces : 0;
       ++seq;
-      soft_sync();                                       // misc and the exchange buffer are free again
+      soft_sync();                                       // misc[2] and the exchange buffer are free again
     }
   }
 
@@ -998,6 +1014,71 @@ k_tree_tc(const PtencDev p, const __grid_constant__ CUtensorMap tmK, const __gri
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
+}
+
+constexpr int TJ_THREADS = 256;
+
+// Joins the parts of the blocks that were split: rows' partial sums weighted by 2^(m - max), four parts requested together.
+template <int D>
+__global__ void __launch_bounds__(TJ_THREADS)
+k_tree_join(const __grid_constant__ TreeTcArgs a, int B, int Hkv, int g) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the parts are written
+  const int per = a.tpb * TM * (D / 8) / TJ_THREADS;     // CTAs per block
+  const int split = blockIdx.x / per;
+  const int pieces = a.pieces[split];
+  if (pieces <= 1) return;
+  const int x = (blockIdx.x - split * per) * TJ_THREADS + threadIdx.x;
+  const int row = x % TM, c = 8 * (x / TM % (D / 8)), tile = x / (TM * (D / 8));
+  const int blk = a.n_full + split;
+  const int unit = blk / a.nqp, qp = blk - unit * a.nqp;
+  const int e = unit / Hkv, h = unit - e * Hkv, b = e % B;
+  const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
+  const int node = qp * 2 * a.npt + tile * a.npt + row / g;
+  if (row >= a.npt * g || node >= n) return;
+  const size_t ps = (size_t)split * a.P * a.tpb + tile;
+  const float4* part = reinterpret_cast<const float4*>(a.part);
+  float mm = -INFINITY, ll = 0.f;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int q = 0; q < pieces; q += 4) {
+    float2 v[4];
+    float4 f[4][2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const size_t at = ps + (size_t)min(q + k, pieces - 1) * a.tpb;
+      v[k] = __ldcg(a.part_ml + at * TM + row);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) f[k][y] = __ldcg(part + (at * (D / 4) + (c >> 2) + y) * TM + row);
+    }
+    float mn = mm;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (q + k < pieces) mn = tt_max3(mn, v[k].x, v[k].x);
+    const float corr = mm == -INFINITY ? 0.f : tt_ex2(mm - mn);
+    ll *= corr;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) acc[y] *= corr;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (q + k < pieces && v[k].x != -INFINITY) {       // a part in which the row sees nothing does not count
+        const float w = tt_ex2(v[k].x - mn);
+        ll = fmaf(w, v[k].y, ll);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          acc[4 * y] = fmaf(w, f[k][y].x, acc[4 * y]);
+          acc[4 * y + 1] = fmaf(w, f[k][y].y, acc[4 * y + 1]);
+          acc[4 * y + 2] = fmaf(w, f[k][y].z, acc[4 * y + 2]);
+          acc[4 * y + 3] = fmaf(w, f[k][y].w, acc[4 * y + 3]);
+        }
+      }
+    }
+    mm = mn;
+  }
+  const size_t o = ((size_t)e * a.NT + node) * (size_t)(Hkv * g) + (size_t)h * g + row % g;
+  const float linv = 1.f / ll;                           // nothing but -inf: 0 * inf, NaN
+  *reinterpret_cast<uint4*>(a.out + o * D + c) = make_uint4(tt_pack(acc[0] * linv, acc[1] * linv), tt_pack(acc[2] * linv, acc[3] * linv),
+                                                            tt_pack(acc[4] * linv, acc[5] * linv), tt_pack(acc[6] * linv, acc[7] * linv));
+  if (c == 0 && a.lse != nullptr) a.lse[o] = (mm + log2f(ll)) * 0.6931471805599453f;
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -1040,12 +1121,26 @@ cudaError_t tt_launch(ptenc_cache* c, const CUtensorMap& q, const CUtensorMap& k
   }
   k_tree_tc<D><<<grid, TT_THREADS, TSmem<D>::TOTAL, st>>>(c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
   c->launches++;
-  return cudaGetLastError();
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || a.P == 1 || a.n_items == a.n_full) return e;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)((a.n_items - a.n_full) / a.P * (a.tpb * TM * (D / 8) / TJ_THREADS)));
+  cfg.blockDim = dim3(TJ_THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, k_tree_join<D>, a, c->dev.B, c->dev.Hkv, c->dev.g);
+  c->launches++;
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-// Bytes of the scratch that the parts of split blocks need: partial rows, their (m, l), arrival tickets.
+// Bytes of the scratch that the parts of split blocks need: partial rows and their (m, l).
 bool ptenc_tree_tc_shape(const ptenc_config* c) {
   return c->dtype == PTENC_DTYPE_BF16 && (c->head_dim == 64 || c->head_dim == 128) && c->policy == PTENC_POLICY_FIFO &&
          c->n_q_heads / c->n_kv_heads <= TM;
@@ -1081,10 +1176,9 @@ cudaError_t ptenc_launch_tree(ptenc_cache* c, int l0, int nl, const void* q, con
   a.ring_box = p.W < TN ? p.W : TN;
   a.parent = parent; a.n_nodes = n_nodes; a.active = active;
   a.out = static_cast<__nv_bfloat16*>(out); a.lse = lse; a.v_tree = static_cast<const __nv_bfloat16*>(v_tree);
-  a.part = c->tree_part; a.part_ml = reinterpret_cast<float2*>(c->tree_ml); a.tickets = c->tree_tickets;
+  a.part = c->tree_part; a.part_ml = reinterpret_cast<float2*>(c->tree_ml); a.pieces = c->tree_pieces;
   // Whole rounds of blocks, one block per SM; the blocks of the last, partial round are cut into P parts each, so that
-  // they fill the SMs too.  Cost in K/V tiles: a part pays about two for its start and end, a joined block about two more
-  // and a fraction per part.
+  // they fill the SMs too.  Microseconds: an item costs about 4 and 1.2 per tile (1.6 with two row tiles), the join 3.
   const long long blocks = (long long)nl * p.B * p.Hkv * a.nqp;
   if (blocks > (1ll << 30)) return cudaErrorInvalidValue;
   const int sms = c->sm_count, rem = (int)(blocks % sms), nt = (p.W + TN - 1) / TN + 1;
@@ -1092,7 +1186,7 @@ cudaError_t ptenc_launch_tree(ptenc_cache* c, int l0, int nl, const void* q, con
   a.P = 1;
   float best = 1e30f;
   for (int P = 1; P <= TT_MAX_PIECES && P <= nt && (rem * P * a.tpb <= PTENC_TREE_SLOTS || P == 1); ++P) {
-    const float cost = (float)((rem * P + sms - 1) / sms) * ((float)((nt + P - 1) / P) + 2.f) + (P > 1 ? 2.f + 0.15f * P : 0.f);
+    const float cost = (float)((rem * P + sms - 1) / sms) * (4.f + (a.tpb == 2 ? 1.6f : 1.2f) * (float)((nt + P - 1) / P)) + (P > 1 ? 3.f : 0.f);
     if (cost < best) { best = cost; a.P = P; }
   }
   a.n_items = a.n_full + rem * a.P;
