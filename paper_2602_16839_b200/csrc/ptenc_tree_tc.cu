@@ -534,6 +534,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
           for (int k = 0; k < TN / 16; ++k)
             if (k < ks)                                  // P lies at the start of each half of S
               mma_ts(tO + st * D, tS + st * TN + (k >> 2) * TH + (k & 3) * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : start);
+          if (!two) commit(empty + 8 * s);               // the V tile is this stream's alone and free when that is done
           if (i + stride >= n) commit(o_full + 8 * st);
         }
         __syncwarp();
@@ -813,9 +814,9 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         }
         wait(s_full + 8 * st, ntile & 1);
         fence_after();
-        if (passes && (!two || st == 1)) {               // this S and the products before it are done: their stages are free
+        if (passes && (!two || st == 1)) {               // S is done, and with two row tiles both streams' products with the V before it
           bar_arrive(empty + 8 * ((base + pos_k(i, two)) % NS));
-          if (i >= stride) bar_arrive(empty + 8 * ((base + pos_v(i - stride, n, two)) % NS));
+          if (two && i > 0) bar_arrive(empty + 8 * ((base + pos_v(i - 1, n, two)) % NS));
         }
         const bool some = !idle && !(draft && half == 1);          // uniform over the warp
         // The scores are read from tensor memory twice, 32 at a time, once for the maximum and once for P: held in registers
@@ -908,10 +909,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       ++no0;
       if (both) ++no1;
       fence_after();
-      if (passes && (!two || st == 1)) {
-        const int last = two ? n - 1 : ((n - 1 - st) & ~1) + st;   // the stream's last tile, -1 or less if it had none
-        if (last >= 0) bar_arrive(empty + 8 * ((base + pos_v(last, n, two)) % NS));
-      }
+      if (passes && two && st == 1) bar_arrive(empty + 8 * ((base + pos_v(n - 1, n, two)) % NS));
       base += 2 * n;
       // (m, l) of both streams for everybody: first the halves' sums, then the streams' values
       float m0, l0, m1, l1;
