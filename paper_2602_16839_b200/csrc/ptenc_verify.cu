@@ -9,8 +9,10 @@
 // What it costs.  Judging a first child needs two numbers of a row; only a rejection or the last draw needs whole rows,
 // and those are rows of one node.  So a sequence reads its tree, one number of p and q per node (all requested together),
 // and then, per rejection, one row of p and q (of p alone at a node without a rejection); the repeats at a node come from
-// the caches.  A row is spread over a cluster of CTAs, a stretch per warp; the draw finds the CTA, the warp and the vector
-// that hold the border from the sums of the last pass, so it re-reads one warp's stretch, a vector per thread.
+// the caches.  A row is spread over a cluster of CTAs, a stretch per warp.  Every warp stores its sum into the shared memory
+// of all the cluster's CTAs, so that behind one cluster barrier each CTA has all sums and finds the total, the warp and
+// (re-reading that warp's stretch, a vector per thread) the entry that hold the border.  The code is kept short: a launch
+// starts from cold instruction memory, and a pass unrolled for throughput cost 5 us in a call for one sequence.
 //
 // Arithmetic: with c_0 = 1 and q >= 0, k rejections of the same row leave r = w / c_k with
 //   w = max(p - C q, 0),  C = c_0 + .. + c_(k-1),  c_k = sum of w
@@ -27,9 +29,11 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int VF_THREADS = 512;
+constexpr int VF_THREADS = 256;
 constexpr int VF_WARPS = VF_THREADS / 32;
 constexpr int VF_CLUSTER = 8;
+constexpr int VF_DEPTH = 4;          // vectors of p and of q that a thread keeps in flight
+constexpr int VF_SMEM = VF_DEPTH * 2 * VF_THREADS * 16;
 
 struct VerifyArgs {
   const void* p;
@@ -66,6 +70,10 @@ __device__ __forceinline__ VfVec<T> vf_load(const T* base, int v, long long room
   }
   return x;
 }
+__device__ __forceinline__ void vf_async(uint4* dst, const void* src, int bytes) {        // the rest of the 16 bytes reads as zero
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+               ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src), "r"(bytes) : "memory");
+}
 // Inclusive sums over the lanes of a warp.
 __device__ __forceinline__ double vf_scan(double x, int lane) {
 #pragma unroll
@@ -76,8 +84,9 @@ __device__ __forceinline__ double vf_scan(double x, int lane) {
   return x;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(VF_THREADS, 2)
+// QROWS: the draft's rows are given; otherwise the drafted tokens were certain.
+template <typename T, bool QROWS>
+__global__ void __launch_bounds__(VF_THREADS, 4)
 k_verify_tree(const VerifyArgs a) {
   constexpr int N = VfVec<T>::N;
   cg::cluster_group cluster = cg::this_cluster();
@@ -85,14 +94,14 @@ k_verify_tree(const VerifyArgs a) {
   const int rank = (int)cluster.block_rank();
   const int b = blockIdx.x / CS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  extern __shared__ __align__(16) uint4 s_ring[];  // [VF_DEPTH][p, q][VF_THREADS]
   __shared__ int s_par[TREE_MAX], s_tok[TREE_MAX];
   __shared__ double s_pv[TREE_MAX], s_qv[TREE_MAX];
   __shared__ float s_u[TREE_MAX];
   __shared__ int s_rej[TREE_MAX];                  // certain drafts: tokens rejected at the current node,
   __shared__ double s_left[TREE_MAX];              // and what is left of their entries
+  __shared__ double s_sum[2][VF_CLUSTER * VF_WARPS];              // the warps' sums of a pass; passes alternate
   __shared__ double s_warp[VF_WARPS];
-  __shared__ double s_cta[2];                      // this CTA's sum, read by the other CTAs; passes alternate
-  __shared__ double s_all[VF_CLUSTER];
   __shared__ int s_hit, s_tail;
 
   if (a.active != nullptr && a.active[b] == 0) return;            // the whole cluster
@@ -110,14 +119,17 @@ k_verify_tree(const VerifyArgs a) {
       bad = tid == 0 ? par != -1 : (par < 0 || par >= tid || tok < 0 || tok >= a.V);
       if (!bad && tid > 0) {
         const long long x = ((long long)b * a.T + par) * a.V + tok;
-        const T pv = P[x], qv = Q != nullptr ? Q[x] : ptenc_from_float<T>(1.f);
+        const T pv = P[x], qv = QROWS ? Q[x] : ptenc_from_float<T>(1.f);
         s_pv[tid] = (double)ptenc_to_float(pv);
         s_qv[tid] = (double)ptenc_to_float(qv);
       }
     }
   }
+  for (int i = tid; i < 2 * VF_CLUSTER * VF_WARPS; i += VF_THREADS) (&s_sum[0][0])[i] = 0.0;
   bad |= n < 1 || n > a.T;
-  if (__syncthreads_or(bad)) {                                    // the same verdict in every CTA of the cluster
+  bad = __syncthreads_or(bad);                                    // the same verdict in every CTA of the cluster
+  if (CS > 1) cluster.sync();                                     // all CTAs run and their sums are clear before any is stored
+  if (bad) {
     if (rank == 0) {
       for (int i = tid; i < a.T; i += VF_THREADS) a.path[(size_t)b * a.T + i] = -1;
       if (tid == 0) { a.n_path[b] = 0; a.next[b] = -1; }
@@ -136,29 +148,30 @@ k_verify_tree(const VerifyArgs a) {
     const long long row = ((long long)b * a.T + cur) * a.V;
     off = (int)(row % N);                                         // entries of the first vector that belong to the row before
     pr = P + (row - off);
-    qr = Q != nullptr ? Q + (row - off) : nullptr;
+    if (QROWS) qr = Q + (row - off);
     room = a.total - (row - off);
     nv = (off + V + N - 1) / N;
     per = (nv + CS * VF_WARPS - 1) / (CS * VF_WARPS);
   };
-  // weights of vector v; x0: index of its first entry in the row
+  // weights of vector v
   auto weigh = [&](const VfVec<T>& pv, const VfVec<T>& qv, int v, double (&w)[N]) {
-    const int x0 = v * N - off;
+    const int x0 = v * N - off;                                   // index of its first entry in the row
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = (double)ptenc_to_float(pv.e[i]);
-    if (C != 0.0) {
-      if (Q != nullptr) {
+    if (QROWS) {
+      if (C != 0.0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const double d = fma(-C, (double)ptenc_to_float(qv.e[i]), w[i]);
           w[i] = d > 0.0 ? d : 0.0;
         }
-      } else {
-        for (int k = 0; k < nrej; ++k) {
-          const int at = s_rej[k] - x0;
+      }
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < nrej; ++k) {
+        const int at = s_rej[k] - x0;
 #pragma unroll
-          for (int i = 0; i < N; ++i) if (at == i) w[i] = s_left[k];
-        }
+        for (int i = 0; i < N; ++i) if (at == i) w[i] = s_left[k];
       }
     }
     if (x0 < 0 || x0 + N > V) {
@@ -168,49 +181,75 @@ k_verify_tree(const VerifyArgs a) {
   };
   auto row_total = [&]() -> double {
     const int lo = (rank * VF_WARPS + warp) * per, hi = min(lo + per, nv);
-    const bool need_q = Q != nullptr && C != 0.0;
+    const bool need_q = QROWS && C != 0.0;
     double sum = 0.0;
-    constexpr int U = N == 4 ? 4 : 2;                             // vectors of p and of q in flight per lane: what 64 registers hold
-    for (int v0 = lo + lane; v0 < hi; v0 += 32 * U) {
-      VfVec<T> pv[U], qv[U];
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int v = min(v0 + 32 * j, hi - 1);
-        pv[j] = vf_load(pr, v, room);
-        qv[j] = pv[j];
-        if (need_q) qv[j] = vf_load(qr, v, room);
+    // Every thread keeps VF_DEPTH vectors of its own on their way through shared memory: with two or three in registers a row
+    // alone on the machine took 9 us a pass.
+    auto fetch = [&](int v, int slot) {
+      if (v < hi) {
+        const int bytes = (int)min(16ll, (room - (long long)v * N) * (long long)sizeof(T));
+        vf_async(s_ring + slot * 2 * VF_THREADS + tid, pr + (size_t)v * N, bytes);
+        if (need_q) vf_async(s_ring + (slot * 2 + 1) * VF_THREADS + tid, qr + (size_t)v * N, bytes);
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // this lane's next vector that holds a rejected token of a certain draft
+    auto next_rejected = [&](int from) -> int {
+      int best = 0x7fffffff;
+      for (int k = 0; k < nrej; ++k) {
+        const int v = (s_rej[k] + off) / N;
+        if (v >= from && v < best && ((v - lo) & 31) == lane) best = v;
+      }
+      return best;
+    };
+    int rejected = QROWS ? 0x7fffffff : next_rejected(lo);
+#pragma unroll 1
+    for (int k = 0; k < VF_DEPTH; ++k) fetch(lo + lane + 32 * k, k);
+    int slot = 0;
+#pragma unroll 1
+    for (int v = lo + lane; v < hi; v += 32) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(VF_DEPTH - 1) : "memory");
+      VfVec<T> p0, q0;
+      *reinterpret_cast<uint4*>(p0.e) = s_ring[slot * 2 * VF_THREADS + tid];
+      q0 = p0;
+      if (need_q) *reinterpret_cast<uint4*>(q0.e) = s_ring[(slot * 2 + 1) * VF_THREADS + tid];
+      fetch(v + 32 * VF_DEPTH, slot);
+      slot = slot + 1 == VF_DEPTH ? 0 : slot + 1;
+      if (v == 0 || v == nv - 1 || v == rejected) {               // the ends of the row, entries to replace
+        double w[N];
+        weigh(p0, q0, v, w);
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        if (v0 + 32 * j < hi) {
-          double w[N];
-          weigh(pv[j], qv[j], v0 + 32 * j, w);
+        for (int i = 0; i < N; ++i) sum += w[i];
+        if (!QROWS && v == rejected) rejected = next_rejected(v + 1);
+      } else if (need_q) {
 #pragma unroll
-          for (int i = 0; i < N; ++i) sum += w[i];
+        for (int i = 0; i < N; ++i) {
+          const double d = fma(-C, (double)ptenc_to_float(q0.e[i]), (double)ptenc_to_float(p0.e[i]));
+          if (__double2hiint(d) >= 0) sum += d;                   // max(d, 0) joins the sum
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += (double)ptenc_to_float(p0.e[i]);
       }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    __syncthreads();                                              // the pass before is done with s_warp and s_all
-    if (lane == 0) s_warp[warp] = sum;
-    __syncthreads();
-    if (warp == 0) {
-      double t = lane < VF_WARPS ? s_warp[lane] : 0.0;
-#pragma unroll
-      for (int o = VF_WARPS / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-      if (lane == 0) s_cta[pass & 1] = t;
-    }
+    double* to = &s_sum[pass & 1][rank * VF_WARPS + warp];
     if (CS > 1) {
+      if (lane < CS) *cluster.map_shared_rank(to, lane) = sum;
       cluster.sync();
-      if (tid < CS) s_all[tid] = *cluster.map_shared_rank(&s_cta[pass & 1], tid);
-    } else if (tid == 0) {
-      s_all[0] = s_cta[pass & 1];
+    } else {
+      if (lane == 0) *to = sum;
+      __syncthreads();
     }
-    __syncthreads();
+    const double* all = s_sum[pass & 1];
     ++pass;
-    double t = 0.0;
-    for (int c = 0; c < CS; ++c) t += s_all[c];
+    double t = 0.0;                                               // every lane adds the same four warps' sums everywhere
+#pragma unroll
+    for (int i = 0; i < VF_CLUSTER * VF_WARPS / 32; ++i) t += all[lane * (VF_CLUSTER * VF_WARPS / 32) + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
     return t;
   };
 
@@ -218,20 +257,23 @@ k_verify_tree(const VerifyArgs a) {
   const int par0 = lane < n ? s_par[lane] : -2, par1 = lane + 32 < n ? s_par[lane + 32] : -2;
   unsigned long long line = 1ull;                                 // the path's nodes; they come in rising order
   double c = 1.0;                                                 // r = w / c
-  bool moved = true, summed = false;
-  while (moved) {
-    moved = false;
-    summed = false;
-    C = 0.0;
-    c = 1.0;
-    nrej = 0;
-    unsigned long long kids = (unsigned long long)__ballot_sync(0xffffffffu, par0 == cur) |
-                              (unsigned long long)__ballot_sync(0xffffffffu, par1 == cur) << 32;
-    for (; kids != 0 && !moved; kids &= kids - 1) {
+  double raw = 0.0, mass = 0.0;                                   // certain drafts: sums of the row as it is, and of w
+  bool summed = false;
+  unsigned long long kids = 0;
+  auto children = [&]() {
+    kids = (unsigned long long)__ballot_sync(0xffffffffu, par0 == cur) |
+           (unsigned long long)__ballot_sync(0xffffffffu, par1 == cur) << 32;
+  };
+  children();
+  // one step: the next child is judged, or there is none left and the last pass is made
+#pragma unroll 1
+  while (true) {
+    if (kids != 0) {
       const int i = __ffsll((long long)kids) - 1;
+      kids &= kids - 1;
       double w = s_pv[i];
       int same = -1;                                              // certain drafts: the token was rejected before, as entry `same`
-      if (Q != nullptr) {
+      if (QROWS) {
         w = fmax(fma(-C, s_qv[i], w), 0.0);
       } else {
         for (int k = 0; k < nrej; ++k) if (s_rej[k] == s_tok[i]) { same = k; w = s_left[k]; }
@@ -239,62 +281,94 @@ k_verify_tree(const VerifyArgs a) {
       if ((double)s_u[i] * s_qv[i] < w / c) {
         line |= 1ull << i;
         cur = i;
-        moved = true;
-        break;
+        C = raw = 0.0;
+        c = 1.0;
+        nrej = 0;
+        summed = false;
+        children();
+        continue;
       }
-      take_row();
       C += c;
-      if (Q == nullptr) {
+      if (!QROWS) {
+        // A certain draft changes one entry, so the sums follow from those of the row as it is, as long as what is left is
+        // no small part of it (1e-3 leaves thirteen digits); otherwise the row is summed again without the entries.
+        if (raw == 0.0) {
+          take_row();
+          raw = mass = row_total();
+        }
+        const double left = fmax(w - c, 0.0);
         __syncthreads();
         if (tid == 0) {
           const int k = same >= 0 ? same : nrej;
           s_rej[k] = s_tok[i];
-          s_left[k] = fmax(w - c, 0.0);
+          s_left[k] = left;
         }
         if (same < 0) ++nrej;
+        mass -= w - left;
+        if (mass > 1e-3 * raw) {
+          if (tid == 0) s_sum[(pass - 1) & 1][(s_tok[i] + off) / N / per] -= w - left;
+          c = mass;
+          summed = true;
+          __syncthreads();
+          continue;
+        }
         __syncthreads();
       }
-      c = row_total();
-      summed = c > 0.0;
-      if (!summed) { C = 0.0; c = 1.0; nrej = 0; }                // nothing left: the target's own row
+    } else if (summed) {
+      break;
     }
+    const bool last = kids == 0 && C == 0.0;                      // no rejection to account for: the row as it is, for the draw
+    take_row();
+    c = mass = row_total();
+    summed = true;
+    if (last) break;
+    if (!(c > 0.0)) { C = raw = 0.0; c = 1.0; nrej = 0; summed = false; } // nothing left: the target's own row
   }
   // ---- the draw ------------------------------------------------------------------------------------------------------------
-  if (!summed) {
-    take_row();
-    c = row_total();
-  }
   const double border = (double)s_u[0] * c;
-  const int len = __popcll(line);
-  if (rank == 0) {
-    if (tid < a.T) {
-      a.path[(size_t)b * a.T + tid] = -1;
+  if (rank == 0 && tid < a.T) {
+    const int len = __popcll(line);
+    // the path, node by node, and -1 behind it
+    int node = -1;
+    if (tid < len) {
+      unsigned long long m = line;
+      for (int k = 0; k < tid; ++k) m &= m - 1;
+      node = __ffsll((long long)m) - 1;
     }
-    __syncthreads();
-    if (tid < a.T && ((line >> tid) & 1ull)) a.path[(size_t)b * a.T + __popcll(line & ((1ull << tid) - 1))] = tid;
+    a.path[(size_t)b * a.T + tid] = node;
     if (tid == 0) {
       a.n_path[b] = len;
       if (!(c > 0.0)) a.next[b] = -1;
     }
   }
   if (c > 0.0) {
-    // the CTA and the warp whose stretch holds the border; the last one with any weight if rounding puts it past the end
-    auto holder = [&](double x, double start, double* before) -> int {
-      const double inc = start + vf_scan(x, lane);
-      unsigned m = __ballot_sync(0xffffffffu, x > 0.0 && inc > border);
-      const unsigned some = __ballot_sync(0xffffffffu, x > 0.0);
-      const int at = m != 0 ? __ffs(m) - 1 : 31 - __clz(some);
-      *before = __shfl_sync(0xffffffffu, inc - x, at);
-      return at;
-    };
-    double before;
-    const int owner = holder(lane < CS ? s_all[lane] : 0.0, 0.0, &before);
-    if (owner == rank) {
-      const int mine = holder(lane < VF_WARPS ? s_warp[lane] : 0.0, before, &before);
-      const int lo = (rank * VF_WARPS + mine) * per, hi = min(lo + per, nv);
-      const bool need_q = Q != nullptr && C != 0.0;
+    // the warp whose stretch holds the border; the last one with any weight if rounding puts it past the end
+    constexpr int PL = VF_CLUSTER * VF_WARPS / 32;
+    const double* all = s_sum[(pass - 1) & 1];
+    double x[PL], mine = 0.0;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) { x[i] = all[lane * PL + i]; mine += x[i]; }
+    double at = vf_scan(mine, lane) - mine;
+    int hit = 0x7fffffff, tail = -1;
+    double before_hit = 0.0, before_tail = 0.0;
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      if (x[i] > 0.0) {
+        tail = lane * PL + i;
+        before_tail = at;
+        if (hit == 0x7fffffff && at + x[i] > border) { hit = tail; before_hit = at; }
+      }
+      at += x[i];
+    }
+    const int h = __reduce_min_sync(0xffffffffu, hit), tl = __reduce_max_sync(0xffffffffu, tail);
+    const int holder = h != 0x7fffffff ? h : tl;
+    double before = __shfl_sync(0xffffffffu, h != 0x7fffffff ? before_hit : before_tail, holder / PL);
+    if (holder / VF_WARPS == rank) {
+      const int lo = holder * per, hi = min(lo + per, nv);
+      const bool need_q = QROWS && C != 0.0;
       if (tid == 0) { s_hit = 0x7fffffff; s_tail = -1; }
-      __syncthreads();                                            // s_warp is free too
+      __syncthreads();
+#pragma unroll 1
       for (int vb = lo; vb < hi; vb += VF_THREADS) {
         const int v = vb + tid;
         double w[N], sum = 0.0;
@@ -312,23 +386,23 @@ k_verify_tree(const VerifyArgs a) {
         if (lane == 31) s_warp[warp] = inc;
         __syncthreads();
         const double wsum = vf_scan(lane < VF_WARPS ? s_warp[lane] : 0.0, lane);
-        double at = before + (inc - sum);
+        double pos = before + (inc - sum);
         const double prev = __shfl_sync(0xffffffffu, wsum, warp > 0 ? warp - 1 : 0);
-        if (warp > 0) at += prev;
-        int hit = 0x7fffffff, tail = -1;
+        if (warp > 0) pos += prev;
+        int first = 0x7fffffff, some = -1;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          at += w[i];
+          pos += w[i];
           if (w[i] > 0.0) {
-            tail = v * N + i - off;
-            if (at > border && hit == 0x7fffffff) hit = tail;
+            some = v * N + i - off;
+            if (pos > border && first == 0x7fffffff) first = some;
           }
         }
-        hit = __reduce_min_sync(0xffffffffu, hit);
-        tail = __reduce_max_sync(0xffffffffu, tail);
+        first = __reduce_min_sync(0xffffffffu, first);
+        some = __reduce_max_sync(0xffffffffu, some);
         if (lane == 0) {
-          if (hit != 0x7fffffff) atomicMin(&s_hit, hit);
-          if (tail >= 0) atomicMax(&s_tail, tail);
+          if (first != 0x7fffffff) atomicMin(&s_hit, first);
+          if (some >= 0) atomicMax(&s_tail, some);
         }
         before += __shfl_sync(0xffffffffu, wsum, 31);
         __syncthreads();
@@ -337,18 +411,20 @@ k_verify_tree(const VerifyArgs a) {
       if (tid == 0) a.next[b] = s_hit != 0x7fffffff ? s_hit : s_tail;
     }
   }
-  if (CS > 1) cluster.sync();                                     // nobody leaves while its sum may still be read
 }
 
 template <typename T>
-cudaError_t launch_verify_t(const VerifyArgs& a, int batch, cudaStream_t st) {
-  // A CTA's share of a row should be worth its start: at least 4096 entries, eight CTAs at most.
+cudaError_t launch_verify_t(const VerifyArgs& a, int batch, int dev, int sms, cudaStream_t st) {
+  // A row over up to eight CTAs: a CTA's share should be worth its start, 2048 entries at least, and the batch should not
+  // need more than two rounds of the eight CTAs that an SM holds.  128 rows of 152000 entries: 53 us with eight CTAs each,
+  // 65 us with four.
   int cs = 1;
-  while (cs < VF_CLUSTER && a.V >= 8192ll * cs) cs *= 2;
+  while (cs < VF_CLUSTER && a.V >= 4096ll * cs && (long long)batch * cs * 2 <= 8 * sms) cs *= 2;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((unsigned)batch * cs);
   cfg.blockDim = dim3(VF_THREADS);
+  cfg.dynamicSmemBytes = VF_SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -357,7 +433,13 @@ cudaError_t launch_verify_t(const VerifyArgs& a, int batch, cudaStream_t st) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, k_verify_tree<T>, a);
+  static bool attr_done[PTENC_MAX_DEVICES] = {};
+  if (ptenc_first_use(attr_done, dev)) {
+    cudaError_t e = cudaFuncSetAttribute(k_verify_tree<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_verify_tree<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
+    if (e != cudaSuccess) return e;
+  }
+  cudaError_t e = a.q != nullptr ? cudaLaunchKernelEx(&cfg, k_verify_tree<T, true>, a) : cudaLaunchKernelEx(&cfg, k_verify_tree<T, false>, a);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -384,7 +466,11 @@ extern "C" int ptenc_verify_tree(const void* p, const void* q, int dtype, const 
   a.T = max_nodes; a.V = vocab; a.total = (long long)batch * max_nodes * vocab;
   a.path = path; a.n_path = n_path; a.next = next_token;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dtype == PTENC_DTYPE_FP32 ? launch_verify_t<float>(a, batch, st)
-                                                  : launch_verify_t<__nv_bfloat16>(a, batch, st);
+  int dev = -1, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return PTENC_ECUDA;
+  const cudaError_t e = dtype == PTENC_DTYPE_FP32 ? launch_verify_t<float>(a, batch, dev, sms, st)
+                                                  : launch_verify_t<__nv_bfloat16>(a, batch, dev, sms, st);
   return e == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
 }
