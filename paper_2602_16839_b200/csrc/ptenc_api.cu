@@ -15,7 +15,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Layout {
   size_t K, V, head, count, n_app, n_sink, stageK, stageV, n_staged, evict_first, S, S0, Qa, Wk, Wv, enc_set,
-      part_acc, part_ml, tickets, status, lora_u, lora_w, tree_part, tree_ml, tree_pieces, total;
+      part_acc, part_ml, tickets, status, lora_u, lora_w, tree_part, tree_ml, tree_pieces, commit_rows, total;
   // importance-aware policy only
   size_t slot_tok, score, live_bits, logits, lse2, pending, fq, fq_head, fq_count, ev_tok, ev_slot;
 };
@@ -95,6 +95,7 @@ Layout make_layout(const ptenc_config* c) {
     o.ev_tok = take(L * B * E * 8);
     o.ev_slot = take(L * B * E * 4);
   }
+  o.commit_rows = take(L * B * 4);
   o.tree_part = o.tree_ml = o.tree_pieces = 0;
   if (ptenc_tree_tc_shape(c)) {
     o.tree_part = take(ptenc_tree_part_bytes(c));
@@ -263,6 +264,7 @@ int ptenc_cache_create(const ptenc_config* cfg, void* ws, size_t bytes, void* st
   d.work = d.status + 4;                               // same 64-byte block as the status word
   c->lora_u = reinterpret_cast<float*>(base + lay.lora_u);
   c->lora_w = reinterpret_cast<__nv_bfloat16*>(base + lay.lora_w);
+  c->commit_rows = reinterpret_cast<int32_t*>(base + lay.commit_rows);
   c->tree_part = reinterpret_cast<float*>(base + lay.tree_part);
   c->tree_ml = reinterpret_cast<float*>(base + lay.tree_ml);
   c->tree_pieces = reinterpret_cast<int*>(base + lay.tree_pieces);

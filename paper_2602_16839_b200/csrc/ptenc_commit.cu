@@ -5,13 +5,13 @@
 // [k e, (k + 1) e), which are cache tokens or, when the ring is shorter than the path, the path's own first tokens.  The
 // state is normalised after every event, so events are folded in order; the rows of an event are summed,
 //   S <- Normalize(S + sum_i (Q_a k_a,i) v_a,i^T)   (Sec. 3.3, Eq. (3) and the sentence after it).
-#include <type_traits>
-
 #include "ptenc_tree.cuh"
 
 namespace {
 
 constexpr int CM_THREADS = 256;
+constexpr int CM_KC = 512;             // columns of the evicted rows in shared memory at a time
+constexpr int CM_KP = CM_KC + 8;       // and their pitch: 16-byte reads of eight rows fall into distinct banks
 
 template <typename T> struct CmVec;
 template <> struct CmVec<float> { static constexpr int N = 4; };
@@ -28,46 +28,81 @@ __device__ __forceinline__ float cm_dot16(const T* __restrict__ w, const float* 
   return s;
 }
 
-// The end of a commit, alike for every kernel: the last event's rows to the staging area, the tokens that stay into the
-// slots the evicted ones left, the ring words.  All threads of the CTA; every row has been folded before.
+// Rows [r0, r1) of the last event to the staging area, oldest first and KV heads concatenated.  All threads of the CTA.
 template <typename T>
-__device__ __forceinline__ void cm_store(const PtencDev& p, size_t lb, size_t ob, const TreeRing& rg, int m, int gone,
-                                         int events, long long n0, const T* __restrict__ k_tree,
-                                         const T* __restrict__ v_tree, int NT, const int* s_path, int32_t* n_evicted_out) {
+__device__ __forceinline__ void cm_stage(const PtencDev& p, size_t lb, size_t ob, const TreeRing& rg, int events, int r0, int r1,
+                                         const T* __restrict__ k_tree, const T* __restrict__ v_tree, int NT,
+                                         const int* s_path) {
   const int D = p.D, Hkv = p.Hkv, W = p.W, tid = threadIdx.x;
-  const T* ringK = reinterpret_cast<const T*>(p.K);
-  const T* ringV = reinterpret_cast<const T*>(p.V);
-  auto row = [&](int o, const T* ring, const T* fresh, size_t* stride) -> const T* {
-    if (o < rg.count) { *stride = (size_t)W * D; return ring + (lb * Hkv * (size_t)W + tree_slot(rg, o)) * D; }
+  const int vph = D * (int)sizeof(T) / 16, vpr = Hkv * vph;
+  auto row = [&](int o, const char* ring, const T* fresh, size_t* stride) -> const T* {
+    if (o < rg.count) {
+      *stride = (size_t)W * D;
+      return reinterpret_cast<const T*>(ring) + (lb * Hkv * (size_t)W + tree_slot(rg, o)) * D;
+    }
     *stride = D;
     return fresh + (ob * NT + s_path[o - rg.count]) * (size_t)Hkv * D;
   };
-  // ---- what the last arrival evicted stays staged, as after ptenc_append_evict ---------------------------------------
-  const int vph = D * (int)sizeof(T) / 16, vpr = Hkv * vph;
-  const bool last_evicts = events > 0 && rg.cap - rg.count + (events - 1) * rg.e == m - 1;
-  if (last_evicts) {
-    for (int i = tid; i < rg.e * vpr; i += CM_THREADS) {
-      const int rr = i / vpr, v = i - rr * vpr, h = v / vph, vv = v - h * vph;
+  // four vectors of K and of V per thread and turn, all requested before any is stored
+  constexpr int U = 4;
+  const int total = r1 * vpr, o0 = (events - 1) * rg.e;
+  for (int i0 = r0 * vpr + tid; i0 < total; i0 += U * CM_THREADS) {
+    uint4 kv[U], vv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + u * CM_THREADS, total - 1);
+      const int rr = i / vpr, v = i - rr * vpr, h = v / vph;
       size_t ks, vs;
-      const int o = (events - 1) * rg.e + rr;
-      const T* kr = row(o, ringK, k_tree, &ks);
-      const T* vr = row(o, ringV, v_tree, &vs);
-      kr += h * ks;
-      vr += h * vs;
-      const size_t dst = ((lb * p.E + rr) * Hkv + h) * (size_t)D * sizeof(T) + (size_t)vv * 16;
-      *reinterpret_cast<uint4*>(p.stageK + dst) = reinterpret_cast<const uint4*>(kr)[vv];
-      *reinterpret_cast<uint4*>(p.stageV + dst) = reinterpret_cast<const uint4*>(vr)[vv];
+      const T* kr = row(o0 + rr, p.K, k_tree, &ks);
+      const T* vr = row(o0 + rr, p.V, v_tree, &vs);
+      kv[u] = reinterpret_cast<const uint4*>(kr + h * ks)[v - h * vph];
+      vv[u] = reinterpret_cast<const uint4*>(vr + h * vs)[v - h * vph];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * CM_THREADS;
+      if (i < total) {                                     // rows of the staging area are Hkv D long: row rr at rr * vpr
+        reinterpret_cast<uint4*>(p.stageK)[lb * p.E * vpr + i] = kv[u];
+        reinterpret_cast<uint4*>(p.stageV)[lb * p.E * vpr + i] = vv[u];
+      }
     }
   }
+}
+
+// The end of a commit, alike for every kernel: the last event's rows to the staging area, the tokens that stay into the
+// slots the evicted ones left, the ring words.  All threads of the CTA; every row has been folded before, and with `staged`
+// the last event's rows are in the staging area already.
+template <typename T>
+__device__ __forceinline__ void cm_store(const PtencDev& p, size_t lb, size_t ob, const TreeRing& rg, int m, int gone,
+                                         int events, long long n0, const T* __restrict__ k_tree,
+                                         const T* __restrict__ v_tree, int NT, const int* s_path, int32_t* n_evicted_out,
+                                         bool staged = false) {
+  const int D = p.D, Hkv = p.Hkv, W = p.W, tid = threadIdx.x;
+  const int vph = D * (int)sizeof(T) / 16, vpr = Hkv * vph;
+  const bool last_evicts = events > 0 && rg.cap - rg.count + (events - 1) * rg.e == m - 1;
+  if (last_evicts && !staged) cm_stage(p, lb, ob, rg, events, 0, rg.e, k_tree, v_tree, NT, s_path);
   // ---- the tokens that stay, into the slots the evicted ones left (all of those have been read above) ------------------
   __syncthreads();
   const int first = gone > rg.count ? gone - rg.count : 0;         // a path longer than the ring keeps its newest tokens
-  for (int i = first * vpr + tid; i < m * vpr; i += CM_THREADS) {
-    const int j = i / vpr, v = i - j * vpr, h = v / vph, vv = v - h * vph;
-    const size_t src = ((ob * NT + s_path[j]) * Hkv + h) * (size_t)D * sizeof(T) + (size_t)vv * 16;
-    const size_t dst = ((lb * Hkv + h) * (size_t)W + tree_slot(rg, rg.count + j)) * D * sizeof(T) + (size_t)vv * 16;
-    *reinterpret_cast<uint4*>(p.K + dst) = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(k_tree) + src);
-    *reinterpret_cast<uint4*>(p.V + dst) = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(v_tree) + src);
+  for (int i0 = first * vpr + tid; i0 < m * vpr; i0 += 2 * CM_THREADS) {
+    uint4 kv[2], vv[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = min(i0 + u * CM_THREADS, m * vpr - 1), j = i / vpr;
+      const size_t src = (ob * NT + s_path[j]) * (size_t)vpr + (i - j * vpr);
+      kv[u] = reinterpret_cast<const uint4*>(k_tree)[src];
+      vv[u] = reinterpret_cast<const uint4*>(v_tree)[src];
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = i0 + u * CM_THREADS;
+      if (i < m * vpr) {
+        const int j = i / vpr, v = i - j * vpr, h = v / vph;
+        const size_t dst = ((lb * Hkv + h) * (size_t)W + tree_slot(rg, rg.count + j)) * vph + (v - h * vph);
+        reinterpret_cast<uint4*>(p.K)[dst] = kv[u];
+        reinterpret_cast<uint4*>(p.V)[dst] = vv[u];
+      }
+    }
   }
   if (tid == 0) {
     p.head[lb] = (int)(((long long)rg.head + gone) % rg.cap);
@@ -212,21 +247,25 @@ __device__ __forceinline__ void cm_async16(void* dst, const void* src) {
 }
 
 // The same for bf16 storage, row-normalised or unnormalised states, r a multiple of 8, H_kv D a multiple of 32: a CTA per
-// (layer, sequence), the evicted rows 16 MT at a time in order of arrival.
-//  * k_a and v_a of a tile come from mma.m16n8k16, a warp per eight outputs.  A lane reads its pieces of rows and weights as
-//    16-byte vectors straight from memory: eight consecutive values serve two mma steps, the contraction index permuted
-//    alike on both operands, so nothing is staged.
-//  * p = Q_a k_a for all rows of the tile, then S += p v_a^T row by row, a warp per four state rows and a lane per
-//    column, with the state rows in registers; behind the last row of an event the rows are normalised.
-//  RJ = columns per lane (r <= 32 RJ), MT = 16-row blocks per tile.
-template <int RJ, int MT>
-__global__ void __launch_bounds__(CM_THREADS, MT == 1 ? 3 : 2)
+// (layer, sequence), the evicted rows 16 at a time in order of arrival.  A commit is a chain of round trips (ring words, rows
+// and weights, the events one after another, the stores), so each link asks for all it needs at once:
+//  * rows come to shared memory by asynchronous copies while the first weights are requested; k_a and v_a of the 16 rows are
+//    mma.m16n8k16 products, a warp per eight outputs.  A lane reads 16-byte vectors of rows and weights: eight consecutive
+//    values serve two mma steps, the contraction index permuted alike on both operands.
+//  * p = Q_a k_a for all rows, then S += p v_a^T row by row, a warp per four state rows and a lane per column, with the
+//    state rows in registers; behind the last row of an event the rows are normalised, four at a time.
+// With `defer` the last event is left out: its rows are in the staging area (k_commit_stage) for the chunk encoder.
+//  RJ = columns per lane (r <= 32 RJ).
+template <int RJ>
+__global__ void __launch_bounds__(CM_THREADS, 3)
 k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, const __nv_bfloat16* __restrict__ v_tree, int NT,
               const int32_t* __restrict__ path, const int32_t* __restrict__ n_path, const uint8_t* __restrict__ active,
-              int32_t* n_evicted_out) {
+              int32_t* n_evicted_out, bool defer) {
   extern __shared__ __align__(16) float cm_sm[];
   __shared__ int s_path[TREE_MAX];
-  constexpr int RT = 16 * MT;
+  __shared__ const __nv_bfloat16* s_src[32];
+  __shared__ size_t s_hs[32];
+  constexpr int RT = 16;
   const int G = p.G, r = p.r, d_kv = p.d_kv, D = p.D, Hkv = p.Hkv, W = p.W;
   const int li = blockIdx.x / p.B;
   const int b = blockIdx.x - li * p.B;
@@ -239,6 +278,7 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
   float* s_p = s_kv + RT * KP;                             // [RT][GP] Q_a k_a
   float* s_q = s_p + RT * GP;                              // [G][QP] Q_a
   float* s_s = s_q + G * QP;                               // [G][r] state
+  __nv_bfloat16* s_row = reinterpret_cast<__nv_bfloat16*>(s_s + G * r);    // [K, V][RT][CM_KP] columns of the evicted rows
   const bool enc = p.encode_enabled != 0;
   float* S = p.S + lb * G * r;
   if (enc) {                                               // Q_a and the state travel while the ring words are looked at
@@ -285,78 +325,92 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
     return fresh + (ob * NT + s_path[o - rg.count]) * (size_t)Hkv * D;
   };
 
-  if (folds && gone > 0) {
+  const int fold = defer && events > 0 ? gone - rg.e : gone;       // rows to fold here
+  if (folds && fold > 0) {
     const int tiles_n = r >> 2;                            // 8-output tiles of W^a_K and W^a_V
     const int fr = lane >> 2, fq = lane & 3;               // fragment row and quarter
-    for (int t0 = 0; t0 < gone; t0 += RT) {
-      for (int x = warp; x < tiles_n; x += CM_THREADS / 32) {
-        const bool is_v = x >= (r >> 3);
-        const int j0 = (is_v ? x - (r >> 3) : x) * 8;
-        const __nv_bfloat16* w = reinterpret_cast<const __nv_bfloat16*>(is_v ? p.Wv : p.Wk) +
-                                 ((size_t)l * r + j0 + fr) * d_kv + 8 * fq;
-        const __nv_bfloat16* src[2 * MT];
-        size_t hs[2 * MT];
-#pragma unroll
-        for (int y = 0; y < 2 * MT; ++y) {
-          const int o = t0 + fr + 8 * y;
-          src[y] = nullptr;
-          hs[y] = 0;
-          if (o < gone) src[y] = row(o, is_v ? ringV : ringK, is_v ? v_tree : k_tree, &hs[y]);
-        }
-        float acc[MT][4];
-#pragma unroll
-        for (int y = 0; y < MT; ++y) { acc[y][0] = acc[y][1] = acc[y][2] = acc[y][3] = 0.f; }
-        constexpr int U = MT == 1 ? 4 : 2;                 // 32-value steps whose loads are in flight together
-        int h = (8 * fq) / D, dd = 8 * fq - h * D;
-        for (int k0 = 0; k0 < d_kv; k0 += 32 * U) {
-          uint4 bw[U], aw[U][2 * MT];
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const bool in = k0 + 32 * u < d_kv;
-            bw[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (in) bw[u] = __ldg(reinterpret_cast<const uint4*>(w + k0 + 32 * u));
-#pragma unroll
-            for (int y = 0; y < 2 * MT; ++y) {
-              aw[u][y] = make_uint4(0u, 0u, 0u, 0u);
-              if (in && src[y] != nullptr) aw[u][y] = *reinterpret_cast<const uint4*>(src[y] + h * hs[y] + dd);
-            }
-            dd += 32;
-            while (dd >= D) { dd -= D; ++h; }
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int y = 0; y < MT; ++y) {
-              cm_mma(acc[y], aw[u][2 * y].x, aw[u][2 * y + 1].x, aw[u][2 * y].y, aw[u][2 * y + 1].y, bw[u].x, bw[u].y);
-              cm_mma(acc[y], aw[u][2 * y].z, aw[u][2 * y + 1].z, aw[u][2 * y].w, aw[u][2 * y + 1].w, bw[u].z, bw[u].w);
-            }
-        }
-        float* dst = s_kv + (is_v ? r : 0) + j0 + 2 * fq;
-#pragma unroll
-        for (int y = 0; y < MT; ++y) {
-          *reinterpret_cast<float2*>(dst + (16 * y + fr) * KP) = make_float2(acc[y][0], acc[y][1]);
-          *reinterpret_cast<float2*>(dst + (16 * y + fr + 8) * KP) = make_float2(acc[y][2], acc[y][3]);
-        }
+    for (int t0 = 0; t0 < fold; t0 += RT) {
+      const int here = min(RT, fold - t0);
+      if (tid < 2 * RT) {                                  // where the tile's rows lie
+        size_t hs = 0;
+        const __nv_bfloat16* src = nullptr;
+        const int o = t0 + tid % RT;
+        if (o < fold) src = row(o, tid < RT ? ringK : ringV, tid < RT ? k_tree : v_tree, &hs);
+        s_src[tid] = src;
+        s_hs[tid] = hs;
       }
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncthreads();
-      const int rows = min(RT, gone - t0);
-      // p[i][g] = Q_a[g] . k_a[i]: a lane per state row, 2 MT rows of the tile per warp
+      for (int kc = 0; kc < d_kv; kc += CM_KC) {
+        const int kn = min(CM_KC, d_kv - kc);
+        // the columns [kc, kc + kn) of the tile's rows, a row of K or V per warp and turn; what lies behind the last row is
+        // whatever it was: it reaches only the products of rows that nobody reads
+        for (int w = warp; w < 2 * here; w += CM_THREADS / 32) {
+          const int is_v = w >= here, rr = is_v ? w - here : w;
+          const __nv_bfloat16* src = s_src[is_v * RT + rr];
+          const size_t hs = s_hs[is_v * RT + rr];
+          __nv_bfloat16* dst = s_row + (is_v * RT + rr) * CM_KP;
+          for (int d = 8 * lane; d < kn; d += 256) {
+            const int h = (kc + d) / D;
+            cm_async16(dst + d, src + h * hs + (kc + d - h * D));
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        bool there = false;
+        for (int x = warp; x < tiles_n; x += CM_THREADS / 32) {
+          const bool is_v = x >= (r >> 3);
+          const int j0 = (is_v ? x - (r >> 3) : x) * 8;
+          const __nv_bfloat16* w = reinterpret_cast<const __nv_bfloat16*>(is_v ? p.Wv : p.Wk) +
+                                   ((size_t)l * r + j0 + fr) * d_kv + kc + 8 * fq;
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+          float* dst = s_kv + fr * KP + (is_v ? r : 0) + j0 + 2 * fq;
+          if (kc > 0) { acc[0] = dst[0]; acc[1] = dst[1]; acc[2] = dst[8 * KP]; acc[3] = dst[8 * KP + 1]; }
+          constexpr int U = 8;                             // 32-value steps whose weights are in flight together
+          for (int k0 = 0; k0 < kn; k0 += 32 * U) {
+            uint4 bw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              bw[u] = k0 + 32 * u < kn ? __ldg(reinterpret_cast<const uint4*>(w + k0 + 32 * u)) : make_uint4(0u, 0u, 0u, 0u);
+            if (!there) {                                  // the first weights are on their way: now wait for the rows
+              there = true;
+              asm volatile("cp.async.wait_group 0;" ::: "memory");
+              asm volatile("bar.sync 0;" ::: "memory");
+            }
+            const __nv_bfloat16* ar = s_row + ((is_v ? RT : 0) + fr) * CM_KP + k0 + 8 * fq;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (k0 + 32 * u < kn) {
+                const uint4 lo = *reinterpret_cast<const uint4*>(ar + 32 * u);
+                const uint4 hi = *reinterpret_cast<const uint4*>(ar + 8 * CM_KP + 32 * u);
+                cm_mma(acc, lo.x, hi.x, lo.y, hi.y, bw[u].x, bw[u].y);
+                cm_mma(acc, lo.z, hi.z, lo.w, hi.w, bw[u].z, bw[u].w);
+              }
+            }
+          }
+          *reinterpret_cast<float2*>(dst) = make_float2(acc[0], acc[1]);
+          *reinterpret_cast<float2*>(dst + 8 * KP) = make_float2(acc[2], acc[3]);
+        }
+        if (!there) {                                      // a warp without outputs still takes part
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          asm volatile("bar.sync 0;" ::: "memory");
+        }
+        __syncthreads();                                   // products stored, row buffer free
+      }
+      // p[i][g] = Q_a[g] . k_a[i]: a lane per state row, two rows of the tile per warp
       for (int g0 = 0; g0 < G; g0 += 32) {
         const int g = min(g0 + lane, G - 1);
-        float acc[2 * MT];
+        float acc[2];
 #pragma unroll
-        for (int y = 0; y < 2 * MT; ++y) acc[y] = 0.f;
+        for (int y = 0; y < 2; ++y) acc[y] = 0.f;
         for (int j = 0; j < r; j += 4) {
           const float4 q4 = *reinterpret_cast<const float4*>(s_q + g * QP + j);
 #pragma unroll
-          for (int y = 0; y < 2 * MT; ++y) {
+          for (int y = 0; y < 2; ++y) {
             const float4 k4 = *reinterpret_cast<const float4*>(s_kv + (warp + 8 * y) * KP + j);
             acc[y] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, acc[y]))));
           }
         }
 #pragma unroll
-        for (int y = 0; y < 2 * MT; ++y) s_p[(warp + 8 * y) * GP + g0 + lane] = acc[y];
+        for (int y = 0; y < 2; ++y) s_p[(warp + 8 * y) * GP + g0 + lane] = acc[y];
       }
       __syncthreads();
       // S += p v_a^T, normalised behind each event's last row; warp w holds state rows g0 + 4 w .. + 3
@@ -372,7 +426,7 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
             s[x][jj] = (gw + x < G && j < r) ? s_s[(gw + x) * r + j] : 0.f;
           }
         int left = rg.e - t0 % rg.e;                       // rows until the current event is complete
-        for (int i = 0; i < rows; ++i) {
+        for (int i = 0; i < here; ++i) {
           const float4 pv = *reinterpret_cast<const float4*>(s_p + i * GP + gw);
 #pragma unroll
           for (int jj = 0; jj < RJ; ++jj) {
@@ -397,14 +451,14 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
                 for (int x = 0; x < 4; ++x) q2[x] += __shfl_xor_sync(0xffffffffu, q2[x], o);
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                const float sc = 1.f / fmaxf(sqrtf(q2[x]), 1e-12f);
+                const float sc = rsqrtf(fmaxf(q2[x], 1e-24f));      // 1 / max(|row|, 1e-12)
 #pragma unroll
                 for (int jj = 0; jj < RJ; ++jj) s[x][jj] *= sc;
               }
             }
           }
         }
-        const bool done = t0 + RT >= gone;
+        const bool done = t0 + RT >= fold;
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -420,7 +474,33 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
     }
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
-  cm_store(p, lb, ob, rg, m, gone, events, n0, k_tree, v_tree, NT, s_path, n_evicted_out);
+  cm_store(p, lb, ob, rg, m, gone, events, n0, k_tree, v_tree, NT, s_path, n_evicted_out, defer);
+}
+
+// The staging of a chunk in front of the commit itself, 16 rows per CTA: one CTA per sequence would copy 129 rows of 512
+// columns in 18 us.  deferred[] receives the number of rows staged; paths that the commit refuses are left alone here.
+constexpr int CM_STAGE = 16;
+__global__ void __launch_bounds__(CM_THREADS)
+k_commit_stage(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, const __nv_bfloat16* __restrict__ v_tree, int NT,
+               const int32_t* __restrict__ path, const int32_t* __restrict__ n_path, const uint8_t* __restrict__ active,
+               int32_t* __restrict__ deferred) {
+  __shared__ int s_path[TREE_MAX];
+  const int li = blockIdx.x / p.B, b = blockIdx.x - li * p.B, tid = threadIdx.x;
+  const size_t lb = (size_t)(l0 + li) * p.B + b, ob = (size_t)li * p.B + b;
+  const int m = (active != nullptr && active[b] == 0) ? 0 : n_path[b];
+  TreeRing rg;
+  int bad = !tree_ring(p, lb, &rg) || m < 0 || m > NT;
+  if (tid < NT) {
+    const int at = path[(size_t)b * NT + tid];
+    s_path[tid] = at;
+    bad |= tid < m && (at < 0 || at >= NT);
+  }
+  bad = __syncthreads_or(bad);
+  const int events = bad ? 0 : tree_evicted(rg.count, rg.cap, rg.e, m) / rg.e;
+  if (blockIdx.y == 0 && tid == 0) deferred[ob] = events > 0 ? rg.e : 0;
+  const int r0 = blockIdx.y * CM_STAGE;
+  if (events == 0 || r0 >= rg.e) return;
+  cm_stage(p, lb, ob, rg, events, r0, min(r0 + CM_STAGE, rg.e), k_tree, v_tree, NT, s_path);
 }
 
 template <typename T>
@@ -440,22 +520,24 @@ cudaError_t launch_commit_t(ptenc_cache* c, int l0, int nl, const void* kt, cons
 }
 
 constexpr size_t CM_SMEM = 220 * 1024;
-size_t commit_smem(const PtencDev& p, int mt) {
-  const size_t rt = 16 * (size_t)mt, gp = (p.G + 31) / 32 * 32 + 4;
-  return sizeof(float) * (rt * (2 * p.r + 4) + rt * gp + (size_t)p.G * (p.r + 4) + (size_t)p.G * p.r);
+size_t commit_smem(const PtencDev& p) {
+  const size_t gp = (p.G + 31) / 32 * 32 + 4;
+  return sizeof(float) * (16 * (size_t)(2 * p.r + 4) + 16 * gp + (size_t)p.G * (p.r + 4) + (size_t)p.G * p.r) +
+         (size_t)2 * 16 * CM_KP * 2;
 }
 
-template <int RJ, int MT>
+template <int RJ>
 cudaError_t launch_commit_bf16(ptenc_cache* c, int l0, int nl, const void* kt, const void* vt, int NT, const int32_t* path,
-                               const int32_t* n_path, const uint8_t* active, int32_t* n_evicted_out, cudaStream_t st) {
-  const size_t smem = commit_smem(c->dev, MT);
+                               const int32_t* n_path, const uint8_t* active, int32_t* n_evicted_out, bool defer,
+                               cudaStream_t st) {
+  const size_t smem = commit_smem(c->dev);
   static bool attr_done[PTENC_MAX_DEVICES] = {};
   if (smem > 40 * 1024 && ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_commit_bf16<RJ, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)CM_SMEM);
+    cudaError_t e = cudaFuncSetAttribute(k_commit_bf16<RJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)CM_SMEM);
     if (e != cudaSuccess) return e;
   }
-  k_commit_bf16<RJ, MT><<<nl * c->cfg.batch, CM_THREADS, smem, st>>>(
-      c->dev, l0, (const __nv_bfloat16*)kt, (const __nv_bfloat16*)vt, NT, path, n_path, active, n_evicted_out);
+  k_commit_bf16<RJ><<<nl * c->cfg.batch, CM_THREADS, smem, st>>>(
+      c->dev, l0, (const __nv_bfloat16*)kt, (const __nv_bfloat16*)vt, NT, path, n_path, active, n_evicted_out, defer);
   c->launches++;
   return cudaGetLastError();
 }
@@ -467,21 +549,23 @@ cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tr
                                 int32_t* n_evicted_out, cudaStream_t st) {
   const PtencDev& p = c->dev;
   if (c->cfg.dtype == PTENC_DTYPE_BF16 && p.r % 8 == 0 && p.d_kv % 32 == 0 && p.norm_mode != PTENC_NORM_FROBENIUS) {
-    // one token per event: 16 rows cover most paths; chunks: 64 rows share each weight vector
-    const bool many = p.E > 1 && commit_smem(p, 4) <= CM_SMEM;
-    const int rj = p.r <= 32 ? 1 : p.r <= 64 ? 2 : 4;
-    auto go = [&](auto RJ, auto MT) {
-      return launch_commit_bf16<decltype(RJ)::value, decltype(MT)::value>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path,
-                                                                          active, n_evicted_out, st);
-    };
-    using std::integral_constant;
-    if (many)
-      return rj == 1 ? go(integral_constant<int, 1>(), integral_constant<int, 4>())
-             : rj == 2 ? go(integral_constant<int, 2>(), integral_constant<int, 4>())
-                       : go(integral_constant<int, 4>(), integral_constant<int, 4>());
-    return rj == 1 ? go(integral_constant<int, 1>(), integral_constant<int, 1>())
-           : rj == 2 ? go(integral_constant<int, 2>(), integral_constant<int, 1>())
-                     : go(integral_constant<int, 4>(), integral_constant<int, 1>());
+    // Chunks of evicted tokens (E >= 16, a tile of the fold here) are folded by the chunk encoder, which reads them from the
+    // staging area: 192 sequences of which 40 % evict 129 rows 56 us by k_commit_bf16 alone, XX us with the encoder.
+    const bool chunks = p.E >= 16 && c->tc_encode && c->cfg.encode_enabled && (long long)nl * p.B * p.E >= 128;
+    int32_t* deferred = c->commit_rows;
+    cudaError_t e;
+    if (chunks) {
+      k_commit_stage<<<dim3(nl * p.B, (p.E + CM_STAGE - 1) / CM_STAGE), CM_THREADS, 0, st>>>(
+          p, l0, (const __nv_bfloat16*)k_tree, (const __nv_bfloat16*)v_tree, max_nodes, path, n_path, active, deferred);
+      c->launches++;
+      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    if (p.r <= 32) e = launch_commit_bf16<1>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);
+    else if (p.r <= 64) e = launch_commit_bf16<2>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);
+    else e = launch_commit_bf16<4>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);
+    if (e != cudaSuccess || !chunks) return e;
+    const size_t rows = (size_t)l0 * p.B * p.E * p.d_kv * p.elt;
+    return ptenc_launch_encode_tc(c, l0, nl, p.stageK + rows, p.stageV + rows, deferred, p.E, st);
   }
   if (c->cfg.dtype == PTENC_DTYPE_FP32)
     return launch_commit_t<float>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, st);

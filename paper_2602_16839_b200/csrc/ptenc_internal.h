@@ -88,6 +88,7 @@ struct ptenc_cache {
   float* tree_part;             // partial rows of split blocks of a tree call, their (m, l) and numbers of parts
   float* tree_ml;
   int* tree_pieces;
+  int32_t* commit_rows;         // [L][B] rows of a commit's last chunk that the chunk encoder is to fold
   float* lora_u;                // [PTENC_LORA_MAX_PART][L][B][r] partial sums of B x (scratch of ptenc_lora_apply)
   __nv_bfloat16* lora_w;        // [2][L][B][G] S (B x) split into two bf16 terms (scratch of ptenc_lora_apply)
 };

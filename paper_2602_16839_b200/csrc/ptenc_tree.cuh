@@ -35,7 +35,10 @@ __device__ __forceinline__ bool tree_ring(const PtencDev& p, size_t lb, TreeRing
 
 // Slot of the token with arrival number o (counted from the oldest sliding token).
 __device__ __forceinline__ int tree_slot(const TreeRing& r, int o) {
-  return r.sink + (int)(((long long)r.head + o) % r.cap);
+  int s = r.head + o;                                    // o is below cap + TREE_MAX, so a few turns at most where cap is small
+  if (s >= 2 * r.cap) s %= r.cap;
+  else if (s >= r.cap) s -= r.cap;
+  return r.sink + s;
 }
 
 // Fills, for the n nodes of a sequence, anc[i] (bit j: node j is on node i's path, i included), ev[i] (tokens gone when
