@@ -111,10 +111,20 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _stream_of(device: int) -> int:
+    """The current stream of a device.  The calls of a speculative step take a few microseconds on the GPU, less than building
+    a stream object and asking it for its handle adds to each of them."""
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _want(where: str, device, *wanted) -> None:
     """Refuses tensors the C side could not tell from valid ones: (name, tensor or None, shape, dtype) each."""
+    index = device.index if device.type == "cuda" else -1
     for name, t, shape, dtype in wanted:
-        if t is None:
+        if t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
             continue
         if t.dtype != dtype or t.device != device or not t.is_contiguous():
             raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a contiguous {dtype} tensor on {device}")
@@ -154,17 +164,20 @@ def verify_tree(p, q, tokens, parent, u, path, n_path, next_token, n_nodes=None,
     where = "ptenc_verify_tree"
     if p.dim() != 3 or p.dtype not in (torch.float32, torch.bfloat16):
         raise PtencError(PTENC_EINVAL, f"{where}: p is to be a [B, T, V] tensor of fp32 or bf16")
-    B, T, V = p.shape
-    i32 = torch.int32
-    _want(where, p.device, ("p", p, p.shape, p.dtype), ("q", q, p.shape, p.dtype), ("tokens", tokens, (B, T), i32),
-          ("parent", parent, (B, T), i32), ("u", u, (B, T), torch.float32), ("path", path, (B, T), i32),
-          ("n_path", n_path, (B,), i32), ("next_token", next_token, (B,), i32), ("n_nodes", n_nodes, (B,), i32),
-          ("active", active, (B,), torch.uint8))
-    if p.device.type != "cuda" or p.device.index != torch.cuda.current_device():
+    shape, i32 = p.shape, torch.int32
+    B, T, V = shape
+    bt, b1 = shape[:2], shape[:1]
+    _want(where, p.device, ("p", p, shape, p.dtype), ("q", q, shape, p.dtype), ("tokens", tokens, bt, i32),
+          ("parent", parent, bt, i32), ("u", u, bt, torch.float32), ("path", path, bt, i32), ("n_path", n_path, b1, i32),
+          ("next_token", next_token, b1, i32), ("n_nodes", n_nodes, b1, i32), ("active", active, b1, torch.uint8))
+    dev = p.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise PtencError(PTENC_EINVAL, f"{where}: the tensors' device is to be the current CUDA device")
-    _check(lib.ptenc_verify_tree(_ptr(p), _ptr(q), DTYPE_BF16 if p.dtype == torch.bfloat16 else DTYPE_FP32, _ptr(tokens),
-                                 _ptr(parent), _ptr(n_nodes), _ptr(u), _ptr(active), B, T, V, _ptr(path), _ptr(n_path),
-                                 _ptr(next_token), _stream()), where)
+    rc = lib.ptenc_verify_tree(p.data_ptr(), _ptr(q), DTYPE_BF16 if p.dtype is torch.bfloat16 else DTYPE_FP32,
+                               tokens.data_ptr(), parent.data_ptr(), _ptr(n_nodes), u.data_ptr(), _ptr(active), B, T, V,
+                               path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
 
 
 class Cache:
@@ -243,33 +256,36 @@ class Cache:
         want = 3 if layer == -1 else 2
         if len(lead) != want or lead[-2] != self.cfg.batch or (layer == -1 and lead[0] != self.cfg.n_layers):
             raise PtencError(PTENC_ESHAPE, f"{where}: k_tree has shape {tuple(k_tree.shape)}")
-        return lead
+        return tuple(lead)
 
     def tree_attn(self, layer, q, k_tree, v_tree, parent, out, n_nodes=None, active=None, lse_out=None):
         """Attention of draft-tree nodes over the cache and their ancestors.  q, out [.., B, T, Hq, D]; k_tree, v_tree
         [.., B, T, Hkv, D]; parent [B, T], n_nodes [B] int32; lse_out [.., B, T, Hq] fp32 (leading [L] when layer == -1)."""
         where, c, dt = "ptenc_tree_attn", self.cfg, self.torch_dtype
         lead = self._tree_shape(layer, k_tree, where)
-        B, T = lead[-2:]
-        _want(where, self.device, ("q", q, (*lead, c.n_q_heads, c.head_dim), dt),
-              ("k_tree", k_tree, (*lead, c.n_kv_heads, c.head_dim), dt),
-              ("v_tree", v_tree, (*lead, c.n_kv_heads, c.head_dim), dt), ("parent", parent, (B, T), torch.int32),
-              ("out", out, (*lead, c.n_q_heads, c.head_dim), dt), ("n_nodes", n_nodes, (B,), torch.int32),
-              ("active", active, (B,), torch.uint8), ("lse_out", lse_out, (*lead, c.n_q_heads), torch.float32))
-        _check(lib.ptenc_tree_attn(self._h, layer, _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(n_nodes), T,
-                                   _ptr(active), _ptr(out), _ptr(lse_out), _stream()), where)
+        bt, Hq, D = lead[-2:], c.n_q_heads, c.head_dim
+        qs, ks, b1 = (*lead, Hq, D), (*lead, c.n_kv_heads, D), bt[:1]
+        _want(where, self.device, ("q", q, qs, dt), ("k_tree", k_tree, ks, dt), ("v_tree", v_tree, ks, dt),
+              ("parent", parent, bt, torch.int32), ("out", out, qs, dt), ("n_nodes", n_nodes, b1, torch.int32),
+              ("active", active, b1, torch.uint8), ("lse_out", lse_out, (*lead, Hq), torch.float32))
+        rc = lib.ptenc_tree_attn(self._h, layer, q.data_ptr(), k_tree.data_ptr(), v_tree.data_ptr(), parent.data_ptr(),
+                                 _ptr(n_nodes), bt[1], _ptr(active), out.data_ptr(), _ptr(lse_out), _stream_of(c.device))
+        if rc != PTENC_OK:
+            raise PtencError(rc, where)
 
     def commit_path(self, layer, k_tree, v_tree, path, n_path, active=None, n_evicted_out=None):
         """Appends the path's tokens in order, evicting and encoding as decode steps would.  path [B, T], n_path [B] int32."""
         where, c, dt = "ptenc_commit_path", self.cfg, self.torch_dtype
         lead = self._tree_shape(layer, k_tree, where)
-        B, T = lead[-2:]
-        _want(where, self.device, ("k_tree", k_tree, (*lead, c.n_kv_heads, c.head_dim), dt),
-              ("v_tree", v_tree, (*lead, c.n_kv_heads, c.head_dim), dt), ("path", path, (B, T), torch.int32),
-              ("n_path", n_path, (B,), torch.int32), ("active", active, (B,), torch.uint8),
+        bt = lead[-2:]
+        ks, b1 = (*lead, c.n_kv_heads, c.head_dim), bt[:1]
+        _want(where, self.device, ("k_tree", k_tree, ks, dt), ("v_tree", v_tree, ks, dt), ("path", path, bt, torch.int32),
+              ("n_path", n_path, b1, torch.int32), ("active", active, b1, torch.uint8),
               ("n_evicted_out", n_evicted_out, lead[:-1], torch.int32))
-        _check(lib.ptenc_commit_path(self._h, layer, _ptr(k_tree), _ptr(v_tree), T, _ptr(path), _ptr(n_path),
-                                     _ptr(active), _ptr(n_evicted_out), _stream()), where)
+        rc = lib.ptenc_commit_path(self._h, layer, k_tree.data_ptr(), v_tree.data_ptr(), bt[1], path.data_ptr(),
+                                   n_path.data_ptr(), _ptr(active), _ptr(n_evicted_out), _stream_of(c.device))
+        if rc != PTENC_OK:
+            raise PtencError(rc, where)
 
     def host_staging_bytes(self, layer) -> int:
         n = ctypes.c_size_t(0)

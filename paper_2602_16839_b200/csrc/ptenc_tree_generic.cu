@@ -2,12 +2,14 @@
 // multiple of 8, any query group size.
 //
 // out[i,h] = softmax(q[i,h] . K^T / sqrt(D)) V over the tokens node i sees (ptenc_tree.cuh).  A CTA takes 32 query rows
-// (row = node * g + head of the group) of one (layer, sequence, KV head) and walks its tokens 64 at a time, the next tile
-// on its way (cp.async) while one is worked on.  A warp owns eight rows: a thread scores 4 rows x 4 tokens, the running
-// maximum and sum of the softmax stay in registers, and the outputs are 4 rows x 4 D / 64 dims per thread, so that every
-// 16-byte read of shared memory feeds 8 (scores) to 16 (outputs) multiply-adds.  fp32 FMA throughout (no TF32): the bound
-// is the FMA pipe for many rows and latency for few, so when the call has fewer CTAs than the machine has room for, the
-// tokens are split over a cluster of CTAs that join their rows through distributed shared memory.
+// (row = node * g + head of the group) of one (layer, sequence, KV head).  Two sets of four warps walk its tokens in turn, 64 at
+// a time, each set with a tile buffer of its own, so that one set's copies run under the other's arithmetic (one set where
+// two buffers do not fit).  A warp owns eight rows: a thread scores 4 rows x 4 tokens, the running maximum and sum of the
+// softmax stay in registers, and the outputs are 4 rows x 4 D / 64 dims per thread, so that every 16-byte read of shared
+// memory feeds 8 (scores) to 16 (outputs) multiply-adds.  fp32 FMA throughout (no TF32): the bound is the FMA pipe for many
+// rows and latency for few, so when the call has fewer CTAs than the machine has room for, the tokens are split over a cluster
+// of CTAs as well; sets and CTAs join their rows through (distributed) shared memory.  Loops stay rolled: a small call runs
+// from cold instruction memory.
 #include <cooperative_groups.h>
 #include <string.h>
 
@@ -17,7 +19,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int TG_THREADS = 128;
+constexpr int TG_SET = 128;          // threads of a set
+constexpr int TG_SETS = 2;
 constexpr int TG_ROWS = 32;
 constexpr int TG_TOK = 64;
 constexpr int TG_PP = TG_TOK + 4;    // pitch of the probabilities
@@ -37,27 +40,34 @@ __device__ __forceinline__ void tg_fma4(float4& a, float s, const float4& v) {
   a.x = fmaf(s, v.x, a.x); a.y = fmaf(s, v.y, a.y); a.z = fmaf(s, v.z, a.z); a.w = fmaf(s, v.w, a.w);
 }
 
-// Shared memory in bytes: two K and V tiles (one where two do not fit), Q rows, probabilities.
+__device__ __forceinline__ void tg_set_sync(int set) { asm volatile("bar.sync %0, %1;" ::"r"(1 + set), "n"(TG_SET) : "memory"); }
+
+// Shared memory in bytes: a K and a V tile and probabilities per set, Q rows.
 template <typename T>
 __host__ __device__ inline int tg_pitch(int D) { return D + 16 / (int)sizeof(T); }
 template <typename T>
-inline size_t tg_smem(int D, int stages) {
-  return (size_t)stages * 2 * TG_TOK * tg_pitch<T>(D) * sizeof(T) + sizeof(float) * (TG_ROWS * (D + 4) + TG_ROWS * TG_PP);
+inline size_t tg_smem(int D, int sets) {
+  return (size_t)sets * (2 * TG_TOK * tg_pitch<T>(D) * sizeof(T) + sizeof(float) * TG_ROWS * TG_PP) +
+         sizeof(float) * TG_ROWS * (D + 4);
 }
 
 // J = 64-dim blocks of a row (D <= 64 J).
 template <typename T, int J>
-__global__ void __launch_bounds__(TG_THREADS)
+__global__ void __launch_bounds__(TG_SET * TG_SETS)
 k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict__ k_tree, const T* __restrict__ v_tree,
                const int32_t* __restrict__ parent, const int32_t* __restrict__ n_nodes, int NT,
-               const uint8_t* __restrict__ active, T* __restrict__ out, float* __restrict__ lse, int n_groups, int stages) {
+               const uint8_t* __restrict__ active, T* __restrict__ out, float* __restrict__ lse, int n_groups) {
   extern __shared__ __align__(16) uint8_t tg_sm[];
   const int D = p.D, g = p.g, W = p.W, Hkv = p.Hkv;
   const int KP = tg_pitch<T>(D), QP = D + 4;
-  T* s_kv = reinterpret_cast<T*>(tg_sm);                  // [stages][K, V][TG_TOK][KP]
-  float* s_q = reinterpret_cast<float*>(tg_sm + (size_t)stages * 2 * TG_TOK * KP * sizeof(T));   // [TG_ROWS][QP]
-  float* s_p = s_q + TG_ROWS * QP;                        // [TG_ROWS][TG_PP]
-  __shared__ float2 s_ml[TG_ROWS];
+  const int sets = (int)blockDim.x / TG_SET, threads = (int)blockDim.x;
+  const int tid = threadIdx.x, lane = tid & 31, set = tid / TG_SET, st = tid - set * TG_SET, warp = st >> 5;
+  const size_t kv_bytes = (size_t)2 * TG_TOK * KP * sizeof(T);
+  float* s_q = reinterpret_cast<float*>(tg_sm + sets * kv_bytes);                                // [TG_ROWS][QP]
+  float* s_p = s_q + TG_ROWS * QP + set * TG_ROWS * TG_PP;                                       // [sets][TG_ROWS][TG_PP]
+  T* s_k = reinterpret_cast<T*>(tg_sm + set * kv_bytes);                                         // [sets][K, V][TG_TOK][KP]
+  T* s_v = s_k + TG_TOK * KP;
+  __shared__ float2 s_ml[TG_SETS][TG_ROWS];
   __shared__ unsigned long long s_anc[TREE_MAX], s_vis[TREE_MAX];
   __shared__ int s_ev[TREE_MAX], s_jump[TREE_MAX];
 
@@ -84,35 +94,32 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     if (threadIdx.x == 0) atomicOr(p.status, PTENC_ST_BAD_INDEX);
     return;
   }
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   // tokens of the unit: pinned entries, then the ring from the oldest token that any node sees, then the nodes
   const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
   const int n_cache = r.sink + r.count - ev0;
   const int n_tok = n_cache + n;
   const int tiles = (n_tok + TG_TOK - 1) / TG_TOK;
-  const int t_lo = (int)((long long)rank * tiles / CS), t_hi = (int)((long long)(rank + 1) * tiles / CS);
+  // this set's tiles: rank * sets + set of CS * sets shares
+  const int share = rank * sets + set, shares = CS * sets;
+  const int t_lo = (int)((long long)share * tiles / shares), t_hi = (int)((long long)(share + 1) * tiles / shares);
   const T* Kb = reinterpret_cast<const T*>(p.K) + (lb * Hkv + hkv) * (size_t)W * D;
   const T* Vb = reinterpret_cast<const T*>(p.V) + (lb * Hkv + hkv) * (size_t)W * D;
   const int vpr = D * (int)sizeof(T) / 16;                // 16-byte vectors of a row
-  auto fetch = [&](int tile, int stage) {
-    T* dk = s_kv + (size_t)stage * 2 * TG_TOK * KP;
-    T* dv = dk + TG_TOK * KP;
-    for (int x = tid; x < TG_TOK * vpr; x += TG_THREADS) {
+  auto fetch = [&](int tile) {
+#pragma unroll 2
+    for (int x = st; x < TG_TOK * vpr; x += TG_SET) {
       const int t = x / vpr, v = x - t * vpr, i = tile * TG_TOK + t;
+      uint8_t* dk = reinterpret_cast<uint8_t*>(s_k + t * KP) + 16 * v;
+      uint8_t* dv = reinterpret_cast<uint8_t*>(s_v + t * KP) + 16 * v;
       if (i >= n_tok) {                                   // past the end: zeros, so that the products stay finite
-        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dk + t * KP) + 16 * v) = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(dv + t * KP) + 16 * v) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(dk) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(dv) = make_uint4(0u, 0u, 0u, 0u);
         continue;
       }
       const T *kr, *vr;
       if (i < n_cache) {
-        int slot = i;
-        if (i >= r.sink) {
-          slot = r.head + ev0 + (i - r.sink);
-          while (slot >= r.cap) slot -= r.cap;
-          slot += r.sink;
-        }
+        const int slot = i < r.sink ? i : tree_slot(r, ev0 + (i - r.sink));
         kr = Kb + (size_t)slot * D;
         vr = Vb + (size_t)slot * D;
       } else {
@@ -120,17 +127,19 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
         kr = k_tree + at;
         vr = v_tree + at;
       }
-      tg_async16(reinterpret_cast<uint8_t*>(dk + t * KP) + 16 * v, reinterpret_cast<const uint8_t*>(kr) + 16 * v);
-      tg_async16(reinterpret_cast<uint8_t*>(dv + t * KP) + 16 * v, reinterpret_cast<const uint8_t*>(vr) + 16 * v);
+      tg_async16(dk, reinterpret_cast<const uint8_t*>(kr) + 16 * v);
+      tg_async16(dv, reinterpret_cast<const uint8_t*>(vr) + 16 * v);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (t_lo < t_hi) fetch(t_lo, 0);
-  for (int i = tid; i < TG_ROWS * D; i += TG_THREADS) {
+  if (t_lo < t_hi) fetch(t_lo);
+#pragma unroll 2
+  for (int i = tid; i < TG_ROWS * D; i += threads) {
     const int rr = i / D, d = i - rr * D, row = row0 + rr;
     const int node = row / g, h = row - node * g;
     s_q[rr * QP + d] = node < n ? ptenc_to_float(q[((ob * NT + node) * p.Hq + (size_t)hkv * g + h) * D + d]) : 0.f;
   }
+  __syncthreads();
 
   const float scale = 1.0f / sqrtf((float)D);
   const int rb = 8 * warp + 4 * (lane >> 4);              // this thread's four rows
@@ -149,19 +158,14 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[x][j] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
+#pragma unroll 1
   for (int i = 0; i < n; ++i) ev_max = max(ev_max, s_ev[i]);
 
+#pragma unroll 1
   for (int tile = t_lo; tile < t_hi; ++tile) {
-    const int stage = stages == 2 ? (tile - t_lo) & 1 : 0;
-    if (stages == 2 && tile + 1 < t_hi) {
-      fetch(tile + 1, stage ^ 1);
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-    } else {
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-    }
-    __syncthreads();
-    const T* sk = s_kv + (size_t)stage * 2 * TG_TOK * KP;
-    const T* sv = sk + TG_TOK * KP;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    tg_set_sync(set);
+    const T *sk = s_k, *sv = s_v;
     const int t0 = tile * TG_TOK;
     // every row sees every token of the tile
     const bool clean = t0 + TG_TOK <= n_cache && (ev_max == ev0 || t0 >= r.sink + ev_max - ev0 || t0 + TG_TOK <= r.sink);
@@ -171,6 +175,7 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int y = 0; y < 4; ++y) s[x][y] = 0.f;
+#pragma unroll 1
     for (int d = 0; d < D; d += 4) {
       float4 qq[4], kk[4];
 #pragma unroll
@@ -222,6 +227,7 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     }
     __syncwarp();                                         // a warp reads the probabilities it wrote
     // ---- outputs: 4 rows x dims 4 tk + 64 j -----------------------------------------------------------------------------
+#pragma unroll 1
     for (int t = 0; t < TG_TOK; t += 4) {
       float4 pp[4];
 #pragma unroll
@@ -251,11 +257,11 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
         }
       }
     }
-    __syncthreads();                                      // the tile's buffer is free
-    if (stages == 1 && tile + 1 < t_hi) fetch(tile + 1, 0);
+    tg_set_sync(set);                                     // the tile's buffer is free
+    if (tile + 1 < t_hi) fetch(tile + 1);
   }
 
-  if (CS == 1) {
+  if (shares == 1) {
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       if (node_of[x] < 0) continue;
@@ -273,36 +279,38 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     }
     return;
   }
-  // ---- the CTAs of the cluster join their rows: sums in the Q rows' place, (m, l) beside them ------------------------------
+  // ---- the sets and CTAs join their rows: sums in the place of the set's tile, (m, l) beside them -----------------------------
+  float* s_o = reinterpret_cast<float*>(s_k);             // [TG_ROWS][QP], no larger than the tiles
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int d = 4 * tk + 64 * j;
-      if (d < D) *reinterpret_cast<float4*>(s_q + (rb + x) * QP + d) = acc[x][j];
+      if (d < D) *reinterpret_cast<float4*>(s_o + (rb + x) * QP + d) = acc[x][j];
     }
-    if (tk == 0) s_ml[rb + x] = make_float2(m[x], l[x]);
+    if (tk == 0) s_ml[set][rb + x] = make_float2(m[x], l[x]);
   }
-  cluster.sync();
+  if (CS > 1) cluster.sync(); else __syncthreads();
   const int dv = D / 4;
-  for (int i = tid + rank * TG_THREADS; i < TG_ROWS * dv; i += TG_THREADS * CS) {
+#pragma unroll 1
+  for (int i = tid + rank * threads; i < TG_ROWS * dv; i += threads * CS) {
     const int rr = i / dv, d = 4 * (i - rr * dv), row = row0 + rr;
     const int node = row / g;
     if (node >= n) continue;
-    float2 ml[TG_CLUSTER];
     float mt = -INFINITY, lt = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int c = 0; c < TG_CLUSTER; ++c) {
-      ml[c] = c < CS ? cluster.map_shared_rank(s_ml, c)[rr] : make_float2(-INFINITY, 0.f);
-      mt = fmaxf(mt, ml[c].x);
-    }
-#pragma unroll
-    for (int c = 0; c < TG_CLUSTER; ++c) {
-      if (c < CS && ml[c].x != -INFINITY) {
-        const float w = expf(ml[c].x - mt);
-        lt = fmaf(w, ml[c].y, lt);
-        tg_fma4(o, w, *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_q, c) + rr * QP + d));
+#pragma unroll 4
+    for (int c = 0; c < shares; ++c) {
+      const int from = c / sets, ss = c - from * sets;
+      const float2 ml = cluster.map_shared_rank(&s_ml[ss][0], from)[rr];
+      const float4 v = *reinterpret_cast<const float4*>(
+          cluster.map_shared_rank(reinterpret_cast<float*>(tg_sm + ss * kv_bytes), from) + rr * QP + d);
+      if (ml.x != -INFINITY) {
+        const float mn = fmaxf(mt, ml.x), w = expf(ml.x - mn), corr = mt == -INFINITY ? 0.f : expf(mt - mn);
+        lt = fmaf(w, ml.y, lt * corr);
+        o.x *= corr; o.y *= corr; o.z *= corr; o.w *= corr;
+        tg_fma4(o, w, v);
+        mt = mn;
       }
     }
     const size_t at = (ob * NT + node) * p.Hq + (size_t)hkv * g + row % g;
@@ -311,7 +319,7 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     dst[2] = ptenc_from_float<T>(o.z / lt); dst[3] = ptenc_from_float<T>(o.w / lt);
     if (lse != nullptr && d == 0) lse[at] = mt + logf(lt);
   }
-  cluster.sync();                                         // nobody leaves while its rows may still be read
+  if (CS > 1) cluster.sync();                             // nobody leaves while its rows may still be read
 }
 
 template <typename T, int J>
@@ -325,9 +333,8 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
   int cs = 1;
   while (cs < TG_CLUSTER && blocks * cs * 2 <= 2 * c->sm_count && cs * 2 * TG_TOK <= p.W) cs *= 2;
   if (blocks * cs > 0x7fffffffll) return cudaErrorInvalidValue;
-  int stages = 2;
-  if (tg_smem<T>(p.D, 2) > 200 * 1024) stages = 1;
-  const size_t smem = tg_smem<T>(p.D, stages);
+  const int sets = tg_smem<T>(p.D, 2) > 200 * 1024 ? 1 : 2;
+  const size_t smem = tg_smem<T>(p.D, sets);
   static bool attr_done[PTENC_MAX_DEVICES] = {};
   if (ptenc_first_use(attr_done, c->cfg.device)) {
     cudaError_t e = cudaFuncSetAttribute(k_tree_generic<T, J>, cudaFuncAttributeMaxDynamicSharedMemorySize, 216 * 1024);
@@ -336,7 +343,7 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((unsigned)(blocks * cs));
-  cfg.blockDim = dim3(TG_THREADS);
+  cfg.blockDim = dim3(TG_SET * sets);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -347,7 +354,7 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, k_tree_generic<T, J>, p, l0, (const T*)q, (const T*)kt, (const T*)vt, parent,
-                                     n_nodes, NT, active, (T*)out, lse, n_groups, stages);
+                                     n_nodes, NT, active, (T*)out, lse, n_groups);
   c->launches++;
   return e != cudaSuccess ? e : cudaGetLastError();
 }
