@@ -102,42 +102,46 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
   const int tiles = (n_tok + TG_TOK - 1) / TG_TOK;
   // this set's tiles: rank * sets + set of CS * sets shares
   const int share = rank * sets + set, shares = CS * sets;
-  const int t_lo = (int)((long long)share * tiles / shares), t_hi = (int)((long long)(share + 1) * tiles / shares);
+  const int t_lo = share * tiles / shares, t_hi = (share + 1) * tiles / shares;      // tiles < 2^19, shares <= 16
   const T* Kb = reinterpret_cast<const T*>(p.K) + (lb * Hkv + hkv) * (size_t)W * D;
   const T* Vb = reinterpret_cast<const T*>(p.V) + (lb * Hkv + hkv) * (size_t)W * D;
   const int vpr = D * (int)sizeof(T) / 16;                // 16-byte vectors of a row
+  // Where the tile's tokens lie is worked out a token per lane (slot, or -1 - node, or nothing); then a token per warp and
+  // turn, the lanes taking the vectors of its K row and of its V row.
+  auto place = [&](int i) -> int {
+    if (i < r.sink) return i;
+    if (i < n_cache) return tree_slot(r, ev0 + (i - r.sink));
+    return i < n_tok ? -1 - (i - n_cache) : -1000;
+  };
+  const T* Kt = k_tree + (ob * NT * Hkv + hkv) * (size_t)D;
+  const T* Vt = v_tree + (ob * NT * Hkv + hkv) * (size_t)D;
   auto fetch = [&](int tile) {
-#pragma unroll 2
-    for (int x = st; x < TG_TOK * vpr; x += TG_SET) {
-      const int t = x / vpr, v = x - t * vpr, i = tile * TG_TOK + t;
-      uint8_t* dk = reinterpret_cast<uint8_t*>(s_k + t * KP) + 16 * v;
-      uint8_t* dv = reinterpret_cast<uint8_t*>(s_v + t * KP) + 16 * v;
-      if (i >= n_tok) {                                   // past the end: zeros, so that the products stay finite
-        *reinterpret_cast<uint4*>(dk) = make_uint4(0u, 0u, 0u, 0u);
-        *reinterpret_cast<uint4*>(dv) = make_uint4(0u, 0u, 0u, 0u);
-        continue;
+    const int pl0 = place(tile * TG_TOK + lane), pl1 = place(tile * TG_TOK + 32 + lane);
+#pragma unroll 4
+    for (int t = warp; t < TG_TOK; t += TG_SET / 32) {
+      const int at = __shfl_sync(0xffffffffu, t < 32 ? pl0 : pl1, t & 31);
+      const size_t off = at >= 0 ? (size_t)at * D : (size_t)(-1 - at) * Hkv * D;
+      for (int x = lane; x < 2 * vpr; x += 32) {
+        const bool is_v = x >= vpr;
+        const int v = 16 * (is_v ? x - vpr : x);
+        uint8_t* dst = reinterpret_cast<uint8_t*>((is_v ? s_v : s_k) + t * KP) + v;
+        const T* src = (at >= 0 ? (is_v ? Vb : Kb) : (is_v ? Vt : Kt)) + off;
+        if (at != -1000) tg_async16(dst, reinterpret_cast<const uint8_t*>(src) + v);
+        else *reinterpret_cast<uint4*>(dst) = make_uint4(0u, 0u, 0u, 0u);      // past the end: the products stay finite
       }
-      const T *kr, *vr;
-      if (i < n_cache) {
-        const int slot = i < r.sink ? i : tree_slot(r, ev0 + (i - r.sink));
-        kr = Kb + (size_t)slot * D;
-        vr = Vb + (size_t)slot * D;
-      } else {
-        const size_t at = ((ob * NT + (i - n_cache)) * Hkv + hkv) * (size_t)D;
-        kr = k_tree + at;
-        vr = v_tree + at;
-      }
-      tg_async16(dk, reinterpret_cast<const uint8_t*>(kr) + 16 * v);
-      tg_async16(dv, reinterpret_cast<const uint8_t*>(vr) + 16 * v);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (t_lo < t_hi) fetch(t_lo);
-#pragma unroll 2
-  for (int i = tid; i < TG_ROWS * D; i += threads) {
-    const int rr = i / D, d = i - rr * D, row = row0 + rr;
-    const int node = row / g, h = row - node * g;
-    s_q[rr * QP + d] = node < n ? ptenc_to_float(q[((ob * NT + node) * p.Hq + (size_t)hkv * g + h) * D + d]) : 0.f;
+#pragma unroll 4
+  for (int rr = tid >> 5; rr < TG_ROWS; rr += threads >> 5) {
+    const int row = row0 + rr, node = row / g, h = row - node * g;
+    const T* src = q + ((ob * NT + node) * p.Hq + (size_t)hkv * g + h) * D;
+#pragma unroll
+    for (int j = 0; j < (64 * J + 127) / 128; ++j) {
+      const int d = 4 * lane + 128 * j;
+      if (d < D) *reinterpret_cast<float4*>(s_q + rr * QP + d) = node < n ? tg_ld4(src + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
   }
   __syncthreads();
 
@@ -175,7 +179,7 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int y = 0; y < 4; ++y) s[x][y] = 0.f;
-#pragma unroll 1
+#pragma unroll 2
     for (int d = 0; d < D; d += 4) {
       float4 qq[4], kk[4];
 #pragma unroll
@@ -291,33 +295,39 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
     if (tk == 0) s_ml[set][rb + x] = make_float2(m[x], l[x]);
   }
   if (CS > 1) cluster.sync(); else __syncthreads();
-  const int dv = D / 4;
-#pragma unroll 1
-  for (int i = tid + rank * threads; i < TG_ROWS * dv; i += threads * CS) {
-    const int rr = i / dv, d = 4 * (i - rr * dv), row = row0 + rr;
-    const int node = row / g;
-    if (node >= n) continue;
-    float mt = -INFINITY, lt = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  // a row per warp: a lane per share looks at its (m, l), then a lane per four dims adds the shares' sums
+  for (int rr = rank * (threads >> 5) + (tid >> 5); rr < TG_ROWS; rr += CS * (threads >> 5)) {
+    const int row = row0 + rr, node = row / g;
+    if (node >= n) continue;                              // uniform over the warp
+    const int from = lane / sets, ss = lane - from * sets;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < shares) ml = cluster.map_shared_rank(&s_ml[ss][0], from)[rr];
+    float mt = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, o));
+    const float w = ml.x == -INFINITY ? 0.f : expf(ml.x - mt);
+    float lt = w * ml.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
+    const size_t at = (ob * NT + node) * p.Hq + (size_t)hkv * g + row % g;
+    for (int d0 = 0; d0 < D; d0 += 128) {
+      const int d = min(d0 + 4 * lane, D - 4);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int c = 0; c < shares; ++c) {
-      const int from = c / sets, ss = c - from * sets;
-      const float2 ml = cluster.map_shared_rank(&s_ml[ss][0], from)[rr];
-      const float4 v = *reinterpret_cast<const float4*>(
-          cluster.map_shared_rank(reinterpret_cast<float*>(tg_sm + ss * kv_bytes), from) + rr * QP + d);
-      if (ml.x != -INFINITY) {
-        const float mn = fmaxf(mt, ml.x), w = expf(ml.x - mn), corr = mt == -INFINITY ? 0.f : expf(mt - mn);
-        lt = fmaf(w, ml.y, lt * corr);
-        o.x *= corr; o.y *= corr; o.z *= corr; o.w *= corr;
-        tg_fma4(o, w, v);
-        mt = mn;
+      for (int c = 0; c < shares; ++c) {
+        const int cf = c / sets, cs = c - cf * sets;
+        const float4 v = *reinterpret_cast<const float4*>(
+            cluster.map_shared_rank(reinterpret_cast<float*>(tg_sm + cs * kv_bytes), cf) + rr * QP + d);
+        const float wc = __shfl_sync(0xffffffffu, w, c);
+        if (wc != 0.f) tg_fma4(o, wc, v);                 // a share in which the row sees nothing does not count
+      }
+      if (d0 + 4 * lane < D) {
+        T* dst = out + at * D + d;
+        dst[0] = ptenc_from_float<T>(o.x / lt); dst[1] = ptenc_from_float<T>(o.y / lt);
+        dst[2] = ptenc_from_float<T>(o.z / lt); dst[3] = ptenc_from_float<T>(o.w / lt);
       }
     }
-    const size_t at = (ob * NT + node) * p.Hq + (size_t)hkv * g + row % g;
-    T* dst = out + at * D + d;
-    dst[0] = ptenc_from_float<T>(o.x / lt); dst[1] = ptenc_from_float<T>(o.y / lt);
-    dst[2] = ptenc_from_float<T>(o.z / lt); dst[3] = ptenc_from_float<T>(o.w / lt);
-    if (lse != nullptr && d == 0) lse[at] = mt + logf(lt);
+    if (lse != nullptr && lane == 0) lse[at] = mt + logf(lt);
   }
   if (CS > 1) cluster.sync();                             // nobody leaves while its rows may still be read
 }
