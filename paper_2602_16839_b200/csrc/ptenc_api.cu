@@ -213,15 +213,15 @@ int ptenc_cache_create(const ptenc_config* cfg, void* ws, size_t bytes, void* st
   if (bytes < lay.total) return PTENC_EWORKSPACE;
 
   if (cudaSetDevice(cfg->device) != cudaSuccess) return PTENC_ECUDA;
-  cudaDeviceProp prop;
-  if (cudaGetDeviceProperties(&prop, cfg->device) != cudaSuccess) return PTENC_ECUDA;
+  int sm_count = 0;
+  if (cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess) return PTENC_ECUDA;
 
   ptenc_cache* c = new (std::nothrow) ptenc_cache();
   if (c == nullptr) return PTENC_EINVAL;
   c->cfg = *cfg;
   c->ws = ws;
   c->ws_bytes = lay.total;
-  c->sm_count = prop.multiProcessorCount;
+  c->sm_count = sm_count;
   c->launches = 0;
   c->fast_attn = false;
   c->tc_encode = false;

@@ -195,20 +195,23 @@ __host__ __device__ constexpr uint32_t tt_idesc(int n, int b_mn) {
 }
 
 // ------------------------------------------------------------------------------------------------ layout
+// Item description words in shared memory; I_LB is layer of the call * batch + sequence.
+enum { I_KIND, I_LB, I_H, I_NODE0, I_N, I_TWO, I_HEAD, I_COUNT, I_SINK, I_CHUNK, I_T0, I_LEN2, I_LO, I_CNT, I_NT, I_PIECES,
+       I_PIECE, I_SPLIT, I_EVMAX, I_VALID, I_ODD, I_WORDS };
 template <int D>
 struct TSmem {
   static constexpr int TILE = (D / 64) * HALF;                       // bytes of a 128-row tile
   static constexpr int STAGES = D == 128 ? 5 : 10;
   static constexpr int OFF_Q = STAGES * TILE;                        // two Q tiles
   static constexpr int OFF_VIS = OFF_Q + 2 * TILE;                   // u64 [64] what each node sees of the draft
-  static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // exchange: bf16 [2][2][128] maxima, float2 [128]
-  static constexpr int OFF_DESC = OFF_ML + TM * 8;                   // int [2][32] items
-  static constexpr int OFF_BAR = OFF_DESC + 2 * 32 * 4;
-  static constexpr int N_BAR = 3 * STAGES + 20;
-  static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]
-  static constexpr int OFF_JUMP = OFF_DEPTH + TREE_MAX;              // s8 [64]
-  static constexpr int OFF_MISC = OFF_JUMP + TREE_MAX;
-  static constexpr int TOTAL = OFF_MISC + 32;
+  static constexpr int OFF_ML = OFF_VIS + TREE_MAX * 8;              // exchange: float [2][2][128] maxima, float2 [128]
+  static constexpr int OFF_DESC = OFF_ML + 4 * TM * 4;               // int [2][I_WORDS] items
+  static constexpr int OFF_BAR = OFF_DESC + 2 * I_WORDS * 4;
+  static constexpr int N_BAR = 3 * STAGES + 18;
+  static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]: first the doubled parents, then the depths
+  static constexpr int OFF_MISC = OFF_DEPTH + TREE_MAX;              // int [3]
+  static constexpr int TOTAL = OFF_MISC + 12;
+  static_assert(OFF_BAR % 8 == 0 && OFF_MISC % 4 == 0, "alignment");
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
 };
 
@@ -228,10 +231,6 @@ struct TreeTcArgs {
   float2* part_ml;                 // [slot][2][128]
   int* pieces;                     // [block that is split]: its parts, 0 if there is nothing to join
 };
-
-// Item description words in shared memory.
-enum { I_KIND, I_LI, I_B, I_H, I_NODE0, I_N, I_TWO, I_HEAD, I_COUNT, I_SINK, I_E, I_T0, I_LEN2, I_LO, I_CNT, I_NT, I_PIECES,
-       I_PIECE, I_SPLIT, I_EVMAX, I_VALID, I_ODD };
 
 // Tiles of a ring that hold slots some node sees: the pinned entries [0, sink) and `count` slots from sink + head on, wrapping
 // inside [sink, W).  Enumerated from the tile of the first sliding slot upwards, then from tile 0.
@@ -295,9 +294,9 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
   volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
   unsigned long long* s_vis = reinterpret_cast<unsigned long long*>(smem + SM::OFF_VIS);
   float2* s_ml = reinterpret_cast<float2*>(smem + SM::OFF_ML);
-  __nv_bfloat16* s_mx = reinterpret_cast<__nv_bfloat16*>(smem + SM::OFF_ML);
+  float* s_mx = reinterpret_cast<float*>(smem + SM::OFF_ML);
   uint8_t* s_depth = smem + SM::OFF_DEPTH;
-  int8_t* s_jump = reinterpret_cast<int8_t*>(smem + SM::OFF_JUMP);
+  int8_t* s_jump = reinterpret_cast<int8_t*>(smem + SM::OFF_DEPTH);
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
   volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict on the next item
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
@@ -373,7 +372,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         if (item >= a.n_items) {
           if (item == last_grab) *p.work = 0;            // the launch's last grab rewinds the counter
           if (bar_wait(item_empty + 8 * (seq & 1), ((seq >> 1) & 1) ^ 1, abort_flag)) {
-            desc[(seq & 1) * 32 + I_KIND] = 0;
+            desc[(seq & 1) * I_WORDS + I_KIND] = 0;
             bar_arrive(item_full + 8 * (seq & 1));
           } else {
             okay = false;
@@ -420,9 +419,9 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         const bool two = n - node0 > a.npt;
         const uint32_t slot = seq & 1;
         if (!bar_wait(item_empty + 8 * slot, ((seq >> 1) & 1) ^ 1, abort_flag)) { okay = false; break; }
-        volatile int* d = desc + slot * 32;
-        d[I_LI] = li; d[I_B] = b; d[I_H] = h; d[I_NODE0] = node0; d[I_N] = n; d[I_TWO] = two ? 1 : 0;
-        d[I_HEAD] = r.head; d[I_COUNT] = r.count; d[I_SINK] = r.sink; d[I_E] = r.e; d[I_T0] = t0; d[I_LEN2] = len2;
+        volatile int* d = desc + slot * I_WORDS;
+        d[I_LB] = li * B + b; d[I_H] = h; d[I_NODE0] = node0; d[I_N] = n; d[I_TWO] = two ? 1 : 0;
+        d[I_HEAD] = r.head; d[I_COUNT] = r.count; d[I_SINK] = r.sink; d[I_CHUNK] = r.e; d[I_T0] = t0; d[I_LEN2] = len2;
         d[I_LO] = lo; d[I_CNT] = cnt; d[I_NT] = nt; d[I_PIECES] = pieces; d[I_PIECE] = piece;
         d[I_SPLIT] = pieces > 1 ? split : -1;
         d[I_KIND] = 1;
@@ -481,7 +480,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
     bool okay = true;
     while (okay) {
       if (!wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { okay = false; break; }
-      volatile int* d = desc + (seq & 1) * 32;
+      volatile int* d = desc + (seq & 1) * I_WORDS;
       const int kind = __shfl_sync(0xffffffffu, d[I_KIND], 0);
       if (kind == 0) break;
       const bool two = __shfl_sync(0xffffffffu, d[I_TWO], 0) != 0;
@@ -577,17 +576,17 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
     };
     while (okay) {
       if (!wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { okay = false; break; }
-      volatile int* d = desc + (seq & 1) * 32;
+      volatile int* d = desc + (seq & 1) * I_WORDS;
       if (d[I_KIND] == 0) break;
       const bool two = d[I_TWO] != 0;
       const int n = d[I_CNT], nodes = d[I_N], lo = d[I_LO], nt = d[I_NT], t0 = d[I_T0], len2 = d[I_LEN2];
       TreeRing r;
-      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_E];
+      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_CHUNK];
       const int ev0 = min(tree_evicted(r.count, r.cap, r.e, 1), r.count);
       int ev_max;
       if (me == 0) {
         // ---- what each node sees: the parent relation closed by pointer doubling, two nodes per lane ---------------------
-        const int32_t* par = a.parent + (size_t)d[I_B] * a.NT;
+        const int32_t* par = a.parent + (size_t)(d[I_LB] % B) * a.NT;
         int pa[2];
         unsigned long long anc[2] = {0ull, 0ull};
         int bad = 0;
@@ -765,19 +764,19 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       // one thread waits for the item and posts what all warps then read, so that they agree on going on
       if (tid == TT_LEAD) {
         int v = 0;
-        if (*abort_flag == 0 && bar_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag)) v = desc[(seq & 1) * 32 + I_KIND];
+        if (*abort_flag == 0 && bar_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag)) v = desc[(seq & 1) * I_WORDS + I_KIND];
         misc[2] = v;
       }
       soft_sync();
       if (misc[2] != 1) break;
       wait(item_full + 8 * (seq & 1), (seq >> 1) & 1);
       wait(info_full, seq & 1);
-      volatile int* d = desc + (seq & 1) * 32;
+      volatile int* d = desc + (seq & 1) * I_WORDS;
       const bool two = d[I_TWO] != 0;
       const int n = d[I_CNT], nodes = d[I_N], lo = d[I_LO], nt = d[I_NT], t0 = d[I_T0], len2 = d[I_LEN2];
       const int ev_max = d[I_EVMAX], valid = d[I_VALID];
       TreeRing r;
-      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_E];
+      r.head = d[I_HEAD]; r.count = d[I_COUNT]; r.sink = d[I_SINK]; r.cap = W - r.sink; r.e = d[I_CHUNK];
       const int node_l = lrow / g, hh = lrow - node_l * g;
       const int node = d[I_NODE0] + (two ? st * a.npt : 0) + node_l;
       const bool real = node_l < a.npt && node < nodes;
@@ -841,10 +840,9 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
             mine = tt_max3(tt_max3(mx[0], mx[1], mx[2]), mx[3], x[31]);
           }
         }
-        // The halves agree on a maximum; bf16 will do, any common reference near the maximum serves.
-        s_mx[(2 * st + half) * TM + lrow] = __float2bfloat16_rn(mine);
+        s_mx[(2 * st + half) * TM + lrow] = mine;        // the halves agree on a maximum
         stream_sync(st);
-        const float mnew = tt_max3(m, __bfloat162float(s_mx[2 * st * TM + lrow]), __bfloat162float(s_mx[(2 * st + 1) * TM + lrow]));
+        const float mnew = tt_max3(m, mine, s_mx[(2 * st + 1 - half) * TM + lrow]);
         if (i < stride) {
           m = mnew;
         } else {
@@ -932,8 +930,8 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       }
       const bool odd = d[I_ODD] != 0;
       const int split = d[I_SPLIT], pieces = d[I_PIECES], piece = d[I_PIECE];
-      const int li = d[I_LI], b = d[I_B], h = d[I_H], node0 = d[I_NODE0];
-      const size_t lb = (size_t)(a.l0 + li) * B + b;
+      const int e = d[I_LB], h = d[I_H];
+      const size_t lb = (size_t)a.l0 * B + e;
       // With one row tile both streams hold parts of the same rows; the columns are dealt to the groups of warps.
       float w0 = 1.f, w1 = 0.f;
       int c_lo, c_hi;
@@ -951,7 +949,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         c_lo = D == 128 ? (2 * st + half) * 32 : (half == 0 ? st * 32 : D);
         c_hi = D == 128 ? c_lo + 32 : min(c_lo + 32, D);
       }
-      const size_t orow = ((size_t)(li * B + b) * a.NT + node) * p.Hq + (size_t)h * g + hh;
+      const size_t orow = ((size_t)e * a.NT + node) * p.Hq + (size_t)h * g + hh;
       const float inv = m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;      // every score -inf: NaN
       const int tile_i = two ? st : 0;
       const size_t pslot = split >= 0 ? (((size_t)split * a.P + piece) * a.tpb + tile_i) : 0;
@@ -975,7 +973,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
           float x[16];
 #pragma unroll
           for (int y = 0; y < 16; ++y) x[y] = o[y];
-          add_not_finite(x, c, p, a.v_tree + ((size_t)(li * B + b) * a.NT * Hkv + h) * D, (lb * Hkv + h) * (size_t)W * D, r, ev, ev_max,
+          add_not_finite(x, c, p, a.v_tree + ((size_t)e * a.NT * Hkv + h) * D, (lb * Hkv + h) * (size_t)W * D, r, ev, ev_max,
                          vis, nodes, lo, n, nt, t0, len2);
 #pragma unroll
           for (int y = 0; y < 16; ++y) o[y] = x[y];
