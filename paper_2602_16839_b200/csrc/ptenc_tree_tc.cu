@@ -848,7 +848,8 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         } else {
           const bool grown = !(mnew <= m + slack);       // NaN counts; nothing seen yet and nothing now (-inf) does not
           if (!idle && __any_sync(0xffffffffu, grown)) {
-            const float corr = grown ? tt_ex2((m - mnew) * sl2) : 1.f;
+            // between the references as they were rounded, which for large scores is not their distance
+            const float corr = grown ? tt_ex2(__fmul_rn(m, sl2) - __fmul_rn(mnew, sl2)) : 1.f;
             if (grown) m = mnew;
             l *= corr;
             // O is at rest; each half of the threads rescales half of the columns
@@ -865,7 +866,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         }
         if (some) {
           // an infinite maximum makes the row NaN, as inf - inf does
-          const float neg = m == -INFINITY ? 0.f : m == INFINITY ? __int_as_float(0x7fffffff) : -m * sl2;
+          const float neg = m == -INFINITY ? 0.f : m == INFINITY ? __int_as_float(0x7fffffff) : -__fmul_rn(m, sl2);
           const uint64_t neg2 = tt_two(neg, neg), scl2 = tt_two(sl2, sl2);
           uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll 1
@@ -911,7 +912,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       base += 2 * n;
       // (m, l) of both streams for everybody: first the halves' sums, then the streams' values
       float m0, l0, m1, l1;
-      m *= sl2;                                          // base-2 units from here on (-inf stays)
+      m = __fmul_rn(m, sl2);                             // base-2 units from here on (-inf stays)
       {
         float* s_l = reinterpret_cast<float*>(s_ml);
         stream_sync(st);                                 // the maxima of the last tile have been read

@@ -217,6 +217,104 @@ def test_what_a_node_does_not_see_does_not_reach_it(dtype, D):
     p.close()
 
 
+@pytest.mark.parametrize("D,Hq,T,E", [(128, 8, 9, 1), (64, 8, 9, 40), (128, 32, 33, 1), (64, 32, 20, 1)])
+def test_tree_attention_of_more_blocks_than_the_device_holds(D, Hq, T, E):
+    """160 pairs of sequence and KV head: most are worked off whole, one after another, the last ones in parts.  Lengths, trees
+    and finished sequences vary, and each call leaves the next one a fresh count of its work."""
+    rng = np.random.default_rng(D + T)
+    p = Pair(pt, n_layers=1, batch=40, n_q_heads=Hq, n_kv_heads=4, head_dim=D, window=150, evict_chunk=E, seed=14)
+    _fill(p, 170, rng)
+    parent = _trees(rng, 40, T, "tree")
+    _check_tree(p, T, parent)
+    n = rng.integers(0, T + 1, 40)
+    active = (rng.random(40) < 0.8).astype(np.uint8)
+    _check_tree(p, T, parent, n, active)
+    _check_tree(p, T, parent, n)
+    p.close()
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("bf16", 16), ("fp32", 64)])
+def test_scores_of_any_size(dtype, D):
+    """Scores from -2e5 to 2e5 and more.  Products and sums are whole numbers below 2^24, and 1/sqrt(D) is a power of two for
+    D = 16 and 64, so the scores are exact there.  For D = 128 the factor to base 2 is off by 2^-24 relative, which counts for a
+    score's distance from the row's largest alone: 24 units at most where the weight is above 2^-24.  The row's reference may be
+    off by half a step of 4e5, the same for all its weights."""
+    W, T, n = 300, 9, 320
+    p = Pair(pt, n_layers=1, batch=2, n_q_heads=8, n_kv_heads=2, head_dim=D, window=W, dtype=dtype, seed=15)
+    rng = np.random.default_rng(D)
+
+    def rows(*shape):                                        # large in one place; a last place that tells ties apart by units
+        x = np.zeros(shape, np.float32)
+        x[..., 0] = rng.integers(-255, 256, shape[:-1])
+        x[..., 1] = rng.integers(-3, 4, shape[:-1])
+        return x
+
+    for t in range(n):
+        k, v = rows(1, 2, 2, D), rng.standard_normal((1, 2, 2, D)).astype(np.float32)
+        kt, vt = _cuda(k, p.cache.torch_dtype), _cuda(v, p.cache.torch_dtype)
+        p.cache.append_evict(-1, kt, vt)
+        p.orc.append_evict(0, np64(kt[0]), np64(vt[0]))
+    q = rows(1, 2, T, 8, D)
+    q[..., 0] *= 32                                          # 2^13 * 2^8 / sqrt(D): up to 2.6e5 at D = 64
+    q = _cuda(q, p.cache.torch_dtype)
+    k, v = _cuda(rows(1, 2, T, 2, D), p.cache.torch_dtype), _cuda(rng.standard_normal((1, 2, T, 2, D)), p.cache.torch_dtype)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, T, 8, device="cuda")
+    parent = _trees(rng, 2, T, "tree")
+    p.cache.tree_attn(-1, q, k, v, _cuda(parent), out, lse_out=lse)
+    o, s, _ = so.tree_attn(p.orc, 0, np64(q[0]), np64(k[0]), np64(v[0]), parent)
+    assert np.abs(s).max() > 5e4
+    # the sum's logarithm joins a reference of up to 2.6e5 in natural units, held in fp32 in base 2 and scaled: three roundings
+    assert (np.abs(np64(lse)[0] - s) <= 3 * 2.0 ** -23 * np.abs(s) + 1e-4).all()
+    # fp32: exponents up to 24 that count, off by 2^-24 relative each for the factor, and exp2 itself
+    _close(np64(out)[0], o, "bf16" if dtype == "bf16" else "fp32", 4.5)
+    p.close()
+
+
+@pytest.mark.parametrize("D,B", [(128, 40), (256, 24)])
+def test_a_cache_whose_offsets_pass_32_bits(D, B):
+    """5 to 6 GB of K and of V: the last sequence of a large batch gives what the same ring gives in a cache of its own, in
+    attention and after a commit, and the first sequence's rows stay as they were."""
+    Hkv, W, T = 8, 65536, 6
+    kw = dict(n_layers=1, n_q_heads=8, n_kv_heads=Hkv, head_dim=D, window=W, n_global=8, rank=8, encode_enabled=0)
+    big, small = pt.Cache(pt.make_config(batch=B, **kw)), pt.Cache(pt.make_config(batch=1, **kw))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def word(c, region, dtype):
+        at, n = c.workspace_region(region)
+        at -= c.workspace.data_ptr()
+        return c.workspace[at:at + n].view(dtype)
+
+    for x, y in zip(_rings(big), _rings(small)):
+        assert x.numel() > 2 ** 31
+        y.normal_(generator=gen)
+        x[0, 0].fill_(float("nan"))
+        x[0, B - 1].copy_(y[0, 0])
+    for c, b in ((big, B - 1), (small, 0)):
+        word(c, pt.binding.REGION_COUNT, torch.int32)[b] = W
+        word(c, pt.binding.REGION_HEAD, torch.int32)[b] = W - 3
+        word(c, pt.binding.REGION_NAPP, torch.int64)[b] = 2 * W - 3
+    q, k, v = (torch.randn(1, B, T, h, D, generator=gen, device="cuda").bfloat16() for h in (8, Hkv, Hkv))
+    parent = torch.tensor([[-1, 0, 0, 1, 3, 2]] * B, dtype=torch.int32, device="cuda")
+    act = torch.zeros(B, dtype=torch.uint8, device="cuda")
+    act[B - 1] = 1
+    a, b = torch.zeros_like(q), torch.zeros_like(q[:, :1])
+    big.tree_attn(-1, q, k, v, parent, a, active=act)
+    last = [t[:, B - 1:].contiguous() for t in (q, k, v)]
+    small.tree_attn(-1, *last, parent[:1], b)
+    assert (a[:, :B - 1] == 0).all()
+    # weights of 65536 nearly equal tokens: outputs near 1 / 256, in other orders of summation
+    assert float((a[:, B - 1:].float() - b.float()).abs().max()) <= 2.0 ** -8 * float(b.float().abs().max()) + 1e-4
+    assert float(b.float().abs().max()) > 2e-3
+    path = torch.tensor([[0, 1, 3, 4, -1, -1]] * B, dtype=torch.int32, device="cuda")
+    n = torch.full((B,), 4, dtype=torch.int32, device="cuda")
+    big.commit_path(-1, k, v, path, n, act)
+    small.commit_path(-1, last[1], last[2], path[:1], n[:1])
+    for x, y in zip(_rings(big), _rings(small)):
+        assert torch.equal(x[0, B - 1], y[0, 0]) and bool(x[0, 0].isnan().all())
+    assert big.status() == 0 and small.status() == 0
+    big.close(), small.close()
+
+
 def test_bad_trees_are_left_alone():
     """Parents out of order, counts out of range: that sequence is skipped and the status word says so; the others are served."""
     for D in (128, 32):
@@ -318,6 +416,16 @@ def test_commit_against_the_oracle(dtype, Hkv, D, W, E, T, prompt, steps, norm, 
         _check_rows(p)
     assert p.cache.status() == 0
     p.close()
+
+
+@pytest.mark.parametrize("W,E,T,prompt,steps,G,r", [
+    (20, 16, 20, 12, 40, 32, 32),                            # pinned prompts leave a ring shorter than the chunk: several events
+    (64, 64, 64, 0, 70, 32, 32),                             # the whole ring leaves at once
+    (300, 129, 40, 0, 290, 16, 64),                          # a chunk that fills no tile evenly
+])
+def test_commit_of_chunks_against_the_oracle(W, E, T, prompt, steps, G, r):
+    test_commit_against_the_oracle("bf16", 2, 64, W, E, T, prompt, steps, 0, G, r)
+    test_commit_against_the_oracle("bf16", 8, 128, W, E, T, prompt, steps, 0, G, r)
 
 
 def _rings(c):
