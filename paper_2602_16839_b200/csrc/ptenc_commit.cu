@@ -11,7 +11,7 @@ namespace {
 
 constexpr int CM_THREADS = 256;
 constexpr int CM_KC = 512;             // columns of the evicted rows in shared memory at a time
-constexpr int CM_KP = CM_KC + 8;       // and their pitch: 16-byte reads of eight rows fall into distinct banks
+constexpr int CM_KP = CM_KC + 32;      // and their pitch, 64 bytes past whole rounds of the banks: 64-byte pieces of two rows side by side
 
 template <typename T> struct CmVec;
 template <> struct CmVec<float> { static constexpr int N = 4; };
@@ -84,28 +84,31 @@ __device__ __forceinline__ void cm_store(const PtencDev& p, size_t lb, size_t ob
   // ---- the tokens that stay, into the slots the evicted ones left (all of those have been read above) ------------------
   __syncthreads();
   const int first = gone > rg.count ? gone - rg.count : 0;         // a path longer than the ring keeps its newest tokens
-  for (int i0 = first * vpr + tid; i0 < m * vpr; i0 += 2 * CM_THREADS) {
-    uint4 kv[2], vv[2];
+  constexpr int NW = CM_THREADS / 32;
+  for (int v = tid & 31; v < vpr; v += 32) {               // a lane per 16 bytes of a row, a token per warp, two at a time
+    const int h = v / vph;
+    const size_t at = ((lb * Hkv + h) * (size_t)W) * vph + (v - h * vph);
+    for (int j0 = first + (tid >> 5); j0 < m; j0 += 2 * NW) {
+      uint4 kv[2], vv[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int i = min(i0 + u * CM_THREADS, m * vpr - 1), j = i / vpr;
-      const size_t src = (ob * NT + s_path[j]) * (size_t)vpr + (i - j * vpr);
-      kv[u] = reinterpret_cast<const uint4*>(k_tree)[src];
-      vv[u] = reinterpret_cast<const uint4*>(v_tree)[src];
-    }
+      for (int u = 0; u < 2; ++u) {
+        const size_t src = (ob * NT + s_path[min(j0 + u * NW, m - 1)]) * (size_t)vpr + v;
+        kv[u] = reinterpret_cast<const uint4*>(k_tree)[src];
+        vv[u] = reinterpret_cast<const uint4*>(v_tree)[src];
+      }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int i = i0 + u * CM_THREADS;
-      if (i < m * vpr) {
-        const int j = i / vpr, v = i - j * vpr, h = v / vph;
-        const size_t dst = ((lb * Hkv + h) * (size_t)W + tree_slot(rg, rg.count + j)) * vph + (v - h * vph);
-        reinterpret_cast<uint4*>(p.K)[dst] = kv[u];
-        reinterpret_cast<uint4*>(p.V)[dst] = vv[u];
+      for (int u = 0; u < 2; ++u) {
+        const int j = j0 + u * NW;
+        if (j < m) {
+          const size_t dst = at + (size_t)tree_slot(rg, rg.count + j) * vph;
+          reinterpret_cast<uint4*>(p.K)[dst] = kv[u];
+          reinterpret_cast<uint4*>(p.V)[dst] = vv[u];
+        }
       }
     }
   }
   if (tid == 0) {
-    p.head[lb] = (int)(((long long)rg.head + gone) % rg.cap);
+    p.head[lb] = (rg.head + gone) % rg.cap;              // gone <= window + nodes
     p.count[lb] = rg.count + m - gone;
     p.n_app[lb] = n0 + m;
     p.n_staged[lb] = last_evicts ? rg.e : 0;
@@ -380,7 +383,8 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
             for (int u = 0; u < U; ++u) {
               if (k0 + 32 * u < kn) {
                 const uint4 lo = *reinterpret_cast<const uint4*>(ar + 32 * u);
-                const uint4 hi = *reinterpret_cast<const uint4*>(ar + 8 * CM_KP + 32 * u);
+                uint4 hi = make_uint4(0u, 0u, 0u, 0u);
+                if (here > 8) hi = *reinterpret_cast<const uint4*>(ar + 8 * CM_KP + 32 * u);
                 cm_mma(acc, lo.x, hi.x, lo.y, hi.y, bw[u].x, bw[u].y);
                 cm_mma(acc, lo.z, hi.z, lo.w, hi.w, bw[u].z, bw[u].w);
               }
