@@ -396,6 +396,51 @@ def job_tokens_per_s(world: int, batch_per_rank: int, steps: int, ms_total: floa
     return world * batch_per_rank * steps / (ms_total * 1e-3)
 
 
+# ======================================================================================== speculative round
+def draft_round(args, c: dict, cache, dev) -> dict:
+    """One round of speculative decoding on the cache as the timed steps left it: attention of a random tree of
+    `--draft-tree` nodes per sequence over all layers, verification against `--draft-vocab` probabilities per node,
+    commit of the accepted paths into every layer.  Medians of 20 rounds, CUDA events; not part of `value`."""
+    import paper_2602_16839_b200 as pt
+
+    L, B, Hq, Hkv, D = c["n_layers"], c["batch"], c["n_q_heads"], c["n_kv_heads"], c["head_dim"]
+    T, V = args.draft_tree, args.draft_vocab
+    gen = torch.Generator(device=dev).manual_seed(0)
+    q, k, v = (torch.randn(L, B, T, h, D, generator=gen, device=dev).to(cache.torch_dtype) for h in (Hq, Hkv, Hkv))
+    out = torch.empty_like(q)
+    i32 = dict(dtype=torch.int32, device=dev)
+    parent = torch.full((B, T), -1, **i32)
+    for i in range(1, T):                            # half of the nodes continue the node before them
+        back = torch.randint(0, i, (B,), generator=gen, **i32)
+        parent[:, i] = torch.where(torch.rand(B, generator=gen, device=dev) < 0.5, torch.full_like(back, i - 1), back)
+    z = 2.5 * torch.randn(B, T, V, generator=gen, device=dev)
+    target = torch.softmax(z, -1)
+    draft = torch.softmax(0.9 * z + 0.6 * torch.randn(B, T, V, generator=gen, device=dev), -1)
+    del z
+    tokens = torch.zeros(B, T, **i32)
+    for i in range(1, T):
+        row = draft[torch.arange(B, device=dev), parent[:, i].long()]
+        tokens[:, i] = torch.multinomial(row, 1, generator=gen)[:, 0]
+    u = torch.rand(B, T, generator=gen, device=dev)
+    path, n_path, following = torch.empty(B, T, **i32), torch.empty(B, **i32), torch.empty(B, **i32)
+    parts = (("tree_attn", lambda: cache.tree_attn(-1, q, k, v, parent, out)),
+             ("verify_tree", lambda: pt.verify_tree(target, draft, tokens, parent, u, path, n_path, following)),
+             ("commit_path", lambda: cache.commit_path(-1, k, v, path, n_path)))
+    times = {name: [] for name, _ in parts}
+    for _ in range(23):
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+        ev[0].record()
+        for j, (_, call) in enumerate(parts):
+            call()
+            ev[j + 1].record()
+        torch.cuda.synchronize()
+        for j, (name, _) in enumerate(parts):
+            times[name].append(ev[j].elapsed_time(ev[j + 1]))
+    med = {name + "_ms": statistics.median(ts[3:]) for name, ts in times.items()}
+    return {"nodes": T, "vocab": V, "accepted_per_sequence": float(n_path.float().mean()), **med,
+            "how": "medians of 20 rounds, every call over all layers, CUDA events"}
+
+
 # ======================================================================================== GPU leg
 def run_gpu(args, c: dict):
     import paper_2602_16839_b200 as pt
@@ -553,6 +598,8 @@ def run_gpu(args, c: dict):
         extras["lora_apply"] = {"ms": ms, "algorithmic_gbs": by / ms / 1e6, "d_in": d_q, "d_out": d_q,
                                 "how": "median of 20 ptenc_lora_apply(layer=-1) calls, L2 flushed, CUDA events"}
         del Am, Bw, xin, yio, flush
+    if rank == 0 and args.draft_tree > 0:
+        extras["draft_round"] = draft_round(args, c, cache, dev)
 
     # ---- max over ranks -------------------------------------------------------------------------------------
     ms_total, ms_e2e = max_over_ranks([ms_total, ms_e2e], dist, dev)
@@ -632,7 +679,13 @@ def main():
     ap.add_argument("--extras", action="store_true",
                     help="also time the encoder's burst on a staged chunk (with --evict-chunk > 1) and the dynamic "
                          "weight update, each alone")
+    ap.add_argument("--draft-tree", type=int, default=0,
+                    help="also time a round of speculative decoding with a tree of this many nodes per sequence (1..64; "
+                         "sliding-window policy): attention of the tree, verification, commit of the accepted path")
+    ap.add_argument("--draft-vocab", type=int, default=32768, help="--draft-tree: probabilities per node")
     args = ap.parse_args()
+    if args.draft_tree and (not 1 <= args.draft_tree <= 64 or args.policy != "fifo"):
+        ap.error("--draft-tree takes 1 to 64 nodes under the sliding-window policy")
     c = workload_cfg(args.workload)
     if args.n_global > 0:
         c["n_global"] = args.n_global
