@@ -363,7 +363,9 @@ k_verify_tree(const VerifyArgs a) {
     const int h = __reduce_min_sync(0xffffffffu, hit), tl = __reduce_max_sync(0xffffffffu, tail);
     const int holder = h != 0x7fffffff ? h : tl;
     double before = __shfl_sync(0xffffffffu, h != 0x7fffffff ? before_hit : before_tail, holder / PL);
-    if (holder / VF_WARPS == rank) {
+    if (holder < 0) {                                             // only with sums that are no numbers
+      if (rank == 0 && tid == 0) a.next[b] = -1;
+    } else if (holder / VF_WARPS == rank) {
       const int lo = holder * per, hi = min(lo + per, nv);
       const bool need_q = QROWS && C != 0.0;
       if (tid == 0) { s_hit = 0x7fffffff; s_tail = -1; }

@@ -625,6 +625,61 @@ def test_verify_bad_trees_give_no_path():
     assert n_path[7] >= 1 and 0 <= nxt[7] < 64
 
 
+def test_rubbish_in_finished_sequences_is_not_looked_at():
+    """What belongs to inactive sequences may hold anything: parents, counts, paths, tokens, probabilities.  Nothing is written
+    for them and the status word stays clean; sequences without nodes or path likewise keep what they have."""
+    B, T, V = 6, 9, 300
+    for dtype, D in (("bf16", 128), ("bf16", 32), ("fp32", 64)):
+        p = Pair(pt, n_layers=2, batch=B, n_q_heads=8, n_kv_heads=2, head_dim=D, window=40, dtype=dtype, seed=16)
+        _fill(p, 50)
+        q, k, v = _drafts(p, T)
+        rng = np.random.default_rng(D)
+        parent, n = _trees(rng, B, T, "tree"), np.full(B, T)
+        active = np.array([1, 0, 1, 0, 1, 1], np.uint8)
+        good = torch.full_like(q, 3.0)
+        p.cache.tree_attn(-1, q, k, v, _cuda(parent), good, n_nodes=_cuda(n), active=_cuda(active, torch.uint8))
+        n[5] = 0
+        parent[[1, 3, 5]], n[[1, 3]] = 99, [-5, 1000]
+        for x in (q, k, v):
+            x[:, [1, 3, 5]] = float("nan")
+        out = torch.full_like(q, 3.0)
+        p.cache.tree_attn(-1, q, k, v, _cuda(parent), out, n_nodes=_cuda(n), active=_cuda(active, torch.uint8))
+        assert p.cache.status() == 0
+        assert torch.equal(out[:, [0, 2, 4]], good[:, [0, 2, 4]]) and (out[:, [1, 3, 5]] == 3.0).all()
+        before, states = [r.clone() for r in _rings(p.cache)], [p.cache.get_state(l) for l in range(2)]
+        path, m = np.tile(np.arange(T), (B, 1)), np.full(B, T)
+        path[[1, 3, 5]], m[[1, 3, 5]] = -7, [1000, -3, 0]
+        p.cache.commit_path(-1, k, v, _cuda(path), _cuda(m), _cuda(active, torch.uint8))
+        assert p.cache.status() == 0
+        for x, y in zip(before, _rings(p.cache)):
+            assert torch.equal(x[:, [1, 3, 5]], y[:, [1, 3, 5]]) and not torch.equal(x[:, 0], y[:, 0])
+        for l in range(2):
+            assert torch.equal(states[l][[1, 3, 5]], p.cache.get_state(l)[[1, 3, 5]])
+            assert bool(torch.isfinite(p.cache.get_state(l)).all())
+        p.close()
+    case = _verify_case(np.random.default_rng(1), B, T, V, "fp32", "tree")
+    want = _run_verify(*case, active=active)
+    p, dq, tok, parent, u = case
+    p[[1, 3]], dq[[1, 3]], tok[[1, 3]], parent[[1, 3]] = float("nan"), float("inf"), -9, 77
+    for x, y in zip(want, _run_verify(p, dq, tok, parent, u, active=active)):
+        assert np.array_equal(x, y)
+
+
+def test_verify_survives_rows_that_are_no_numbers():
+    """The documentation asks for finite rows; others give some answer in range and leave the other sequences alone."""
+    rng = np.random.default_rng(2)
+    p, q, tok, parent, u = _verify_case(rng, 6, 5, 2051, "fp32", "tree")
+    for dq in (q, None):
+        want = _run_verify(p, dq, tok, parent, u)
+        p2 = p.clone()
+        p2[0], p2[1], p2[2, :, ::7] = float("nan"), float("inf"), float("inf")
+        p2[3, :, 5] = -1.0
+        got = _run_verify(p2, dq, tok, parent, u)
+        for x, y in zip(want, got):
+            assert np.array_equal(x[4:], y[4:])
+        assert ((got[2] >= -1) & (got[2] < 2051)).all() and ((got[1] >= 1) & (got[1] <= 5)).all()
+
+
 # ------------------------------------------------------------------------------------------------------------ together
 class _Round:
     """One speculative round of a stand-in model: every node's output of the last layer, projected to a vocabulary."""
