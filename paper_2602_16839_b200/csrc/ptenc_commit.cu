@@ -259,8 +259,12 @@ __device__ __forceinline__ void cm_async16(void* dst, const void* src) {
 //    state rows in registers; behind the last row of an event the rows are normalised, four at a time.
 // With `defer` the last event is left out: its rows are in the staging area (k_commit_stage) for the chunk encoder.
 //  RJ = columns per lane (r <= 32 RJ).
+// Measured (G = r = 32, four KV heads of 128): 28 layers x 32 sequences, paths of up to 8 tokens that each evict one, 30 us
+// (34 MB that have to move, 5 us of copy bandwidth); one layer of 8 sequences 8 us.  The bound is the chain of round trips
+// and the instructions of many small steps (issue slots 40 % busy, DRAM 8 %), so four CTAs share an SM: three, with twice the
+// weights in flight, 32 us.
 template <int RJ>
-__global__ void __launch_bounds__(CM_THREADS, 3)
+__global__ void __launch_bounds__(CM_THREADS, 4)
 k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, const __nv_bfloat16* __restrict__ v_tree, int NT,
               const int32_t* __restrict__ path, const int32_t* __restrict__ n_path, const uint8_t* __restrict__ active,
               int32_t* n_evicted_out, bool defer) {
@@ -367,7 +371,7 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
           float acc[4] = {0.f, 0.f, 0.f, 0.f};
           float* dst = s_kv + fr * KP + (is_v ? r : 0) + j0 + 2 * fq;
           if (kc > 0) { acc[0] = dst[0]; acc[1] = dst[1]; acc[2] = dst[8 * KP]; acc[3] = dst[8 * KP + 1]; }
-          constexpr int U = 8;                             // 32-value steps whose weights are in flight together
+          constexpr int U = 4;                             // 32-value steps whose weights are in flight together
           for (int k0 = 0; k0 < kn; k0 += 32 * U) {
             uint4 bw[U];
 #pragma unroll
@@ -449,13 +453,17 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
               for (int x = 0; x < 4; ++x)
 #pragma unroll
                 for (int jj = 0; jj < RJ; ++jj) q2[x] = fmaf(s[x][jj], s[x][jj], q2[x]);
+              // four sums over the warp: each exchange halves the values a lane carries, eight lanes finish a row
+              const bool up = lane & 16, right = lane & 8;
+              const float a = (up ? q2[2] : q2[0]) + __shfl_xor_sync(0xffffffffu, up ? q2[0] : q2[2], 16);
+              const float b = (up ? q2[3] : q2[1]) + __shfl_xor_sync(0xffffffffu, up ? q2[1] : q2[3], 16);
+              float n2 = (right ? b : a) + __shfl_xor_sync(0xffffffffu, right ? a : b, 8);
 #pragma unroll
-              for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) q2[x] += __shfl_xor_sync(0xffffffffu, q2[x], o);
+              for (int o = 4; o > 0; o >>= 1) n2 += __shfl_xor_sync(0xffffffffu, n2, o);
+              n2 = rsqrtf(fmaxf(n2, 1e-24f));              // 1 / max(|row|, 1e-12)
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                const float sc = rsqrtf(fmaxf(q2[x], 1e-24f));      // 1 / max(|row|, 1e-12)
+                const float sc = __shfl_sync(0xffffffffu, n2, 8 * x);
 #pragma unroll
                 for (int jj = 0; jj < RJ; ++jj) s[x][jj] *= sc;
               }
