@@ -93,7 +93,9 @@ typedef struct {
 /* Bytes of device workspace a cache with this configuration needs.  Host only, launches nothing.
  * Layout (all inside the workspace): K and V rings [L][B][H_kv][W][D]; ring state head/count (int32)
  * and n_appended (int64) [L][B], pinned-entry counts (int32) [L][B]; evicted-row staging [L][B][E][H_kv*D] for K and for V; state S
- * [L][B][G][r] fp32; per layer Q_a [G][r] fp32 and copies of W^a_K, W^a_V; split-K partials; status.  Under
+ * [L][B][G][r] fp32; per layer Q_a [G][r] fp32 and copies of W^a_K, W^a_V; split-K partials; status; the number of
+ * rows staged by ptenc_commit_path [L][B] int32; for bf16, head_dim 64 or 128 and PTENC_POLICY_FIFO the partials of
+ * ptenc_tree_attn (320 tiles of 128 rows, 21 MB at head_dim 128).  Under
  * PTENC_POLICY_SCORE also per-slot scores and token indices, a liveness bitmap, the freed-slot queue, and the logits
  * of the latest attention launch [L][B][H_kv][W][8] fp32 (6 % of the rings at head_dim 128). */
 PTENC_API int ptenc_workspace_bytes(const ptenc_config* cfg /*host*/, size_t* bytes /*host, out*/);
@@ -198,7 +200,8 @@ PTENC_API int ptenc_decode_step(ptenc_cache* c, int layer, const void* q, const 
  * read nor written.  What a node does not see does not reach its rows, whatever it holds (NaN and infinities included).
  * A sequence whose n_nodes, parents or ring words are out of range is left alone and the device status word gets
  * PTENC_ST_BAD_INDEX (2).  max_nodes outside 1..PTENC_MAX_TREE: PTENC_ESHAPE.  PTENC_EINVAL under PTENC_POLICY_SCORE, whose
- * evictions depend on the attention of every single step. */
+ * evictions depend on the attention of every single step.  The handle's scratch is used: calls and graphs that hold calls on
+ * one handle do not overlap on the GPU. */
 #define PTENC_MAX_TREE 64
 PTENC_API int ptenc_tree_attn(ptenc_cache* c, int layer, const void* q, const void* k_tree, const void* v_tree,
                               const int32_t* parent, const int32_t* n_nodes, int32_t max_nodes, const uint8_t* active,
