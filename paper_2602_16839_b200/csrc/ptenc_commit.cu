@@ -132,6 +132,7 @@ k_commit(PtencDev p, int l0, const T* __restrict__ k_tree, const T* __restrict__
   const size_t lb = (size_t)l * p.B + b;
   const size_t ob = (size_t)li * p.B + b;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = CM_THREADS / 32;
+  tree_after_previous();
   const int m = (active != nullptr && active[b] == 0) ? 0 : n_path[b];
   TreeRing rg;
   int bad = !tree_ring(p, lb, &rg) || m < 0 || m > NT;
@@ -288,6 +289,7 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
   __nv_bfloat16* s_row = reinterpret_cast<__nv_bfloat16*>(s_s + G * r);    // [K, V][RT][CM_KP] columns of the evicted rows
   const bool enc = p.encode_enabled != 0;
   float* S = p.S + lb * G * r;
+  tree_after_previous();
   if (enc) {                                               // Q_a and the state travel while the ring words are looked at
     for (int i = tid; i < G * r / 4; i += CM_THREADS) {
       cm_async16(s_q + (4 * i / r) * QP + 4 * i % r, p.Qa + (size_t)l * G * r + 4 * i);
@@ -499,6 +501,7 @@ k_commit_stage(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, con
   __shared__ int s_path[TREE_MAX];
   const int li = blockIdx.x / p.B, b = blockIdx.x - li * p.B, tid = threadIdx.x;
   const size_t lb = (size_t)(l0 + li) * p.B + b, ob = (size_t)li * p.B + b;
+  tree_after_previous();
   const int m = (active != nullptr && active[b] == 0) ? 0 : n_path[b];
   TreeRing rg;
   int bad = !tree_ring(p, lb, &rg) || m < 0 || m > NT;
@@ -525,10 +528,9 @@ cudaError_t launch_commit_t(ptenc_cache* c, int l0, int nl, const void* kt, cons
     cudaError_t e = cudaFuncSetAttribute(k_commit<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
     if (e != cudaSuccess) return e;
   }
-  k_commit<T><<<nl * c->cfg.batch, CM_THREADS, smem, st>>>(p, l0, (const T*)kt, (const T*)vt, NT, path, n_path, active,
-                                                           n_evicted_out);
   c->launches++;
-  return cudaGetLastError();
+  return tree_launch(k_commit<T>, dim3(nl * c->cfg.batch), CM_THREADS, smem, 0, st, p, l0, (const T*)kt, (const T*)vt, NT, path,
+                     n_path, active, n_evicted_out);
 }
 
 constexpr size_t CM_SMEM = 220 * 1024;
@@ -548,10 +550,9 @@ cudaError_t launch_commit_bf16(ptenc_cache* c, int l0, int nl, const void* kt, c
     cudaError_t e = cudaFuncSetAttribute(k_commit_bf16<RJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)CM_SMEM);
     if (e != cudaSuccess) return e;
   }
-  k_commit_bf16<RJ><<<nl * c->cfg.batch, CM_THREADS, smem, st>>>(
-      c->dev, l0, (const __nv_bfloat16*)kt, (const __nv_bfloat16*)vt, NT, path, n_path, active, n_evicted_out, defer);
   c->launches++;
-  return cudaGetLastError();
+  return tree_launch(k_commit_bf16<RJ>, dim3(nl * c->cfg.batch), CM_THREADS, smem, 0, st, c->dev, l0, (const __nv_bfloat16*)kt,
+                     (const __nv_bfloat16*)vt, NT, path, n_path, active, n_evicted_out, defer);
 }
 
 }  // namespace
@@ -567,10 +568,10 @@ cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tr
     int32_t* deferred = c->commit_rows;
     cudaError_t e;
     if (chunks) {
-      k_commit_stage<<<dim3(nl * p.B, (p.E + CM_STAGE - 1) / CM_STAGE), CM_THREADS, 0, st>>>(
-          p, l0, (const __nv_bfloat16*)k_tree, (const __nv_bfloat16*)v_tree, max_nodes, path, n_path, active, deferred);
       c->launches++;
-      if ((e = cudaGetLastError()) != cudaSuccess) return e;
+      e = tree_launch(k_commit_stage, dim3(nl * p.B, (p.E + CM_STAGE - 1) / CM_STAGE), CM_THREADS, 0, 0, st, p, l0,
+                      (const __nv_bfloat16*)k_tree, (const __nv_bfloat16*)v_tree, max_nodes, path, n_path, active, deferred);
+      if (e != cudaSuccess) return e;
     }
     if (p.r <= 32) e = launch_commit_bf16<1>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);
     else if (p.r <= 64) e = launch_commit_bf16<2>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);

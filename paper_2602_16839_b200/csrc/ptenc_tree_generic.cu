@@ -82,6 +82,7 @@ k_tree_generic(PtencDev p, int l0, const T* __restrict__ q, const T* __restrict_
   const int hkv = idx % Hkv; idx /= Hkv;
   const int b = idx % p.B;
   const int li = idx / p.B;
+  tree_after_previous();
   if (active != nullptr && active[b] == 0) return;        // these verdicts are alike for the CTAs of a cluster
   const int n = n_nodes != nullptr ? n_nodes[b] : NT;
   const size_t lb = (size_t)(l0 + li) * p.B + b;
@@ -354,23 +355,9 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
     cudaError_t e = cudaFuncSetAttribute(k_tree_generic<T, J>, cudaFuncAttributeMaxDynamicSharedMemorySize, 216 * 1024);
     if (e != cudaSuccess) return e;
   }
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)(blocks * cs));
-  cfg.blockDim = dim3(TG_SET * sets);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cs;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, k_tree_generic<T, J>, p, l0, (const T*)q, (const T*)kt, (const T*)vt, parent,
-                                     n_nodes, NT, active, (T*)out, lse, n_groups);
   c->launches++;
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return tree_launch(k_tree_generic<T, J>, dim3((unsigned)(blocks * cs)), TG_SET * sets, smem, cs, st, p, l0, (const T*)q,
+                     (const T*)kt, (const T*)vt, parent, n_nodes, NT, active, (T*)out, lse, n_groups);
 }
 template <typename T>
 cudaError_t launch_tree_t(ptenc_cache* c, int l0, int nl, const void* q, const void* kt, const void* vt,

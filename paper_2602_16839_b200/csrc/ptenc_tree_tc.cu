@@ -355,8 +355,9 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
     return w;
   };
   Words words = {0, 0, 0, 0, 0};
+  tree_after_previous();
+  tree_let_next_start();
   if (tid == 0) words = words_of((int)blockIdx.x);       // gridDim.x <= n_items
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   fence_before();
   __syncthreads();
   fence_after();
@@ -1029,7 +1030,8 @@ constexpr int TJ_THREADS = 256;
 template <int D>
 __global__ void __launch_bounds__(TJ_THREADS)
 k_tree_join(const __grid_constant__ TreeTcArgs a, int B, int Hkv, int g) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // the parts are written
+  tree_after_previous();                                 // the parts are written
+  tree_let_next_start();
   const int per = a.tpb * TM * (D / 8) / TJ_THREADS;     // CTAs per block
   const int split = blockIdx.x / per;
   const int pieces = a.pieces[split];
@@ -1126,23 +1128,12 @@ cudaError_t tt_launch(ptenc_cache* c, const CUtensorMap& q, const CUtensorMap& k
     cudaError_t e = cudaFuncSetAttribute(k_tree_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
     if (e != cudaSuccess) return e;
   }
-  k_tree_tc<D><<<grid, TT_THREADS, TSmem<D>::TOTAL, st>>>(c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
   c->launches++;
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = tree_launch(k_tree_tc<D>, dim3(grid), TT_THREADS, TSmem<D>::TOTAL, 0, st, c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
   if (e != cudaSuccess || a.P == 1 || a.n_items == a.n_full) return e;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)((a.n_items - a.n_full) / a.P * (a.tpb * TM * (D / 8) / TJ_THREADS)));
-  cfg.blockDim = dim3(TJ_THREADS);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, k_tree_join<D>, a, c->dev.B, c->dev.Hkv, c->dev.g);
   c->launches++;
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return tree_launch(k_tree_join<D>, dim3((unsigned)((a.n_items - a.n_full) / a.P * (a.tpb * TM * (D / 8) / TJ_THREADS))), TJ_THREADS,
+                     0, 0, st, a, c->dev.B, c->dev.Hkv, c->dev.g);
 }
 
 }  // namespace

@@ -109,6 +109,7 @@ k_verify_tree(const VerifyArgs a) {
   __shared__ double s_warp[VF_WARPS];
   __shared__ int s_hit, s_tail;
 
+  tree_after_previous();
   if (a.active != nullptr && a.active[b] == 0) return;            // the whole cluster
   const T* P = static_cast<const T*>(a.p);
   const T* Q = static_cast<const T*>(a.q);
@@ -427,27 +428,14 @@ cudaError_t launch_verify_t(const VerifyArgs& a, int batch, int dev, int sms, cu
   // 65 us with four.
   int cs = 1;
   while (cs < VF_CLUSTER && a.V >= 4096ll * cs && (long long)batch * cs * 2 <= 8 * sms) cs *= 2;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)batch * cs);
-  cfg.blockDim = dim3(VF_THREADS);
-  cfg.dynamicSmemBytes = VF_SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cs;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   static bool attr_done[PTENC_MAX_DEVICES] = {};
   if (ptenc_first_use(attr_done, dev)) {
     cudaError_t e = cudaFuncSetAttribute(k_verify_tree<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_verify_tree<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
     if (e != cudaSuccess) return e;
   }
-  cudaError_t e = a.q != nullptr ? cudaLaunchKernelEx(&cfg, k_verify_tree<T, true>, a) : cudaLaunchKernelEx(&cfg, k_verify_tree<T, false>, a);
-  return e != cudaSuccess ? e : cudaGetLastError();
+  return tree_launch(a.q != nullptr ? k_verify_tree<T, true> : k_verify_tree<T, false>, dim3((unsigned)batch * cs), VF_THREADS,
+                     VF_SMEM, cs, st, a);
 }
 
 inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
