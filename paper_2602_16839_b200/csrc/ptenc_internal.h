@@ -84,6 +84,7 @@ struct ptenc_cache {
   CUtensorMap tmStageK, tmStageV;   // 2-D maps over the staged evicted rows: rows = L*B*E, cols = d_kv
   int tc_stage_box;             // token rows per TMA box of the staged maps
   bool tree_tc;                 // tensor-core kernel usable for draft trees
+  int tree_clusters[3];         // its clusters of 2, 4 and 8 CTAs that the device holds at a time
   CUtensorMap tmTreeK, tmTreeV; // 3-D maps over the rings: units x W x D, boxes of up to 128 slots
   float* tree_part;             // partial rows of split blocks of a tree call, their (m, l) and numbers of parts
   float* tree_ml;

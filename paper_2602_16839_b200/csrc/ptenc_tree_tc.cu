@@ -21,8 +21,11 @@
 //    tensor memory.  A warp alone is bound by its own latencies, so four warps share a scheduler.  O is rescaled only when
 //    the maximum has grown by more than 2^8, which for most rows is never after the first tiles.  Non-finite values that
 //    were taken out of V are added to the rows that see them.
-//  * Items that are a part of a block's tiles leave fp32 partials, which k_tree_join, chained by programmatic dependent
-//    launch, joins in order: a thread per row and eight columns, so the join is spread over the machine.
+//  * Items that are a part of a block's tiles leave fp32 partials.  When the call has so few blocks that clusters of two, four
+//    or eight CTAs can hold all their parts, a block's parts are a cluster: they stay in shared memory and every CTA joins
+//    some of the rows (one chain of 5 nodes: 12.0 us, from Python 12.9).  Otherwise k_tree_join, chained by programmatic
+//    dependent launch, joins them in order from memory, a thread per row and eight columns (the same chain 12.5, from Python
+//    17.3, the second launch's time on the host).
 //  * Every wait is bounded: one that runs out raises a status bit and an abort flag, every role then leaves, copies and
 //    MMAs in flight are drained and tensor memory is freed.
 //
@@ -30,17 +33,20 @@
 // 5.2 TB/s.  64 sequences of 64 nodes, groups of 4, eight rings of 4096 slots: 277 GFLOP in 310 us, 0.9 PFLOP/s; there the
 // tensor pipe is 44 % busy, the exponentials' unit 45 %, the issue slots 46 %: the bound is a stream's chain, about 3800
 // cycles a tile, of which both products take 1100, the maximum 630, its exchange 180, P 1650 and handing over the rest.  One
-// chain of 5 nodes over 1024 slots: 13 us, most of it set-up and the join.  What did not shorten the chain: tiles of 64
+// chain of 5 nodes over 1024 slots: 12 us, most of it set-up and the join.  What did not shorten the chain: tiles of 64
 // tokens (a 64-column product costs as much as one of 128), a second warp issuing products (334 us), part of the exponentials
 // on the FMA pipe, reading the scores 16 at a time with the next ones in flight, exchanging between the two warps of a row
 // alone, and the weights in one pass against the running maximum (twice the time: P in registers until the maximum is known
 // spills).
+#include <cooperative_groups.h>
 #include <string.h>
 #include <type_traits>
 
 #include "ptenc_tree.cuh"
 
 namespace {
+
+namespace cg = cooperative_groups;
 
 constexpr uint32_t TT_POLLS = 2000;             // bounded wait: tries of up to a millisecond each before giving up
 constexpr int TN = 128;                        // slots per K/V tile
@@ -219,8 +225,8 @@ struct TSmem {
   static constexpr int OFF_BAR = OFF_DESC + 2 * I_WORDS * 4;
   static constexpr int N_BAR = 3 * STAGES + 18;
   static constexpr int OFF_DEPTH = OFF_BAR + N_BAR * 8;              // u8 [64]: first the doubled parents, then the depths
-  static constexpr int OFF_MISC = OFF_DEPTH + TREE_MAX;              // int [3]
-  static constexpr int TOTAL = OFF_MISC + 12;
+  static constexpr int OFF_MISC = OFF_DEPTH + TREE_MAX;              // int [4]
+  static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(OFF_BAR % 8 == 0 && OFF_MISC % 4 == 0, "alignment");
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
 };
@@ -291,8 +297,63 @@ __device__ __noinline__ void add_not_finite(float* o, int c, const PtencDev& p, 
   }
 }
 
+// Eight columns of one row of block n_full + split, x counting rows, then columns, then row tiles: the parts' sums weighted by
+// 2^(m - max), four parts requested together.  ml(part, tile, row) and sums(part, tile, column / 4 * 128 + row) fetch them.
+template <int D, typename ML, typename SUMS>
+__device__ __forceinline__ void join_row(const TreeTcArgs& a, int B, int Hkv, int g, int split, int x, int pieces, ML ml, SUMS sums) {
+  const int row = x % TM, c = 8 * (x / TM % (D / 8)), tile = x / (TM * (D / 8));
+  const int blk = a.n_full + split;
+  const int unit = blk / a.nqp, qp = blk - unit * a.nqp;
+  const int e = unit / Hkv, h = unit - e * Hkv, b = e % B;
+  const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
+  const int node = qp * 2 * a.npt + tile * a.npt + row / g;
+  if (row >= a.npt * g || node >= n) return;
+  float mm = -INFINITY, ll = 0.f;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int q = 0; q < pieces; q += 4) {
+    float2 v[4];
+    float4 f[4][2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = min(q + k, pieces - 1);
+      v[k] = ml(at, tile, row);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) f[k][y] = sums(at, tile, ((c >> 2) + y) * TM + row);
+    }
+    float mn = mm;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (q + k < pieces) mn = tt_max3(mn, v[k].x, v[k].x);
+    const float corr = mm == -INFINITY ? 0.f : tt_ex2(mm - mn);
+    ll *= corr;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) acc[y] *= corr;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (q + k < pieces && v[k].x != -INFINITY) {       // a part in which the row sees nothing does not count
+        const float w = tt_ex2(v[k].x - mn);
+        ll = fmaf(w, v[k].y, ll);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          acc[4 * y] = fmaf(w, f[k][y].x, acc[4 * y]);
+          acc[4 * y + 1] = fmaf(w, f[k][y].y, acc[4 * y + 1]);
+          acc[4 * y + 2] = fmaf(w, f[k][y].z, acc[4 * y + 2]);
+          acc[4 * y + 3] = fmaf(w, f[k][y].w, acc[4 * y + 3]);
+        }
+      }
+    }
+    mm = mn;
+  }
+  const size_t o = ((size_t)e * a.NT + node) * (size_t)(Hkv * g) + (size_t)h * g + row % g;
+  const float linv = 1.f / ll;                           // nothing but -inf: 0 * inf, NaN
+  *reinterpret_cast<uint4*>(a.out + o * D + c) = make_uint4(tt_pack(acc[0] * linv, acc[1] * linv), tt_pack(acc[2] * linv, acc[3] * linv),
+                                                            tt_pack(acc[4] * linv, acc[5] * linv), tt_pack(acc[6] * linv, acc[7] * linv));
+  if (c == 0 && a.lse != nullptr) a.lse[o] = (mm + log2f(ll)) * 0.6931471805599453f;
+}
+
 // ------------------------------------------------------------------------------------------------ kernel
-template <int D>
+template <int D, bool CL>
 __global__ void __launch_bounds__(TT_THREADS, 1)
 k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
           const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmKt,
@@ -308,7 +369,8 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
   uint8_t* s_depth = smem + SM::OFF_DEPTH;
   int8_t* s_jump = reinterpret_cast<int8_t*>(smem + SM::OFF_DEPTH);
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
-  volatile int* abort_flag = misc;                       // misc[1]: TMEM base, misc[2]: verdict on the next item
+  // misc[1]: TMEM base, misc[2]: verdict on the next item, misc[3]: with CL, the parts that make up the block
+  volatile int* abort_flag = misc;
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
   // barriers with two entries: [stream], [Q tile] or [item slot]
   const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, q_full = o_full + 16,
@@ -333,6 +395,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
     bar_init(info_empty, 1 + 16);
     bar_init(drain, 1);
     *abort_flag = 0;
+    misc[3] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -381,7 +444,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       while (okay) {
         const int last_grab = a.n_items + (int)gridDim.x - 1;
         if (item >= a.n_items) {
-          if (item == last_grab) *p.work = 0;            // the launch's last grab rewinds the counter
+          if (!CL && item == last_grab) *p.work = 0;            // the launch's last grab rewinds the counter
           if (bar_wait(item_empty + 8 * (seq & 1), ((seq >> 1) & 1) ^ 1, abort_flag)) {
             desc[(seq & 1) * I_WORDS + I_KIND] = 0;
             bar_arrive(item_full + 8 * (seq & 1));
@@ -390,7 +453,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
           }
           break;
         }
-        const int next = atomicAdd(p.work, 1) + (int)gridDim.x;
+        const int next = CL ? a.n_items : atomicAdd(p.work, 1) + (int)gridDim.x;     // a CTA of a cluster has one part
         int blk, piece = 0, pieces = 1, split = -1;
         if (item < a.n_full) {
           blk = item;
@@ -410,7 +473,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
         const int n = w.n;
         TreeRing r;
         r.head = w.head; r.count = w.count; r.sink = w.sink; r.cap = W - w.sink; r.e = min(p.E, r.cap);
-        if (split >= 0 && piece == 0) a.pieces[split] = 0;           // until its rows say otherwise
+        if (!CL && split >= 0 && piece == 0) a.pieces[split] = 0;           // until its rows say otherwise
         if (w.act == 0) continue;
         if (r.sink < 0 || r.cap < 1 || r.head < 0 || r.head >= r.cap || r.count < 0 || r.count > r.cap || n < 0 || n > a.NT) {
           atomicOr(p.status, PTENC_ST_BAD_INDEX);
@@ -966,6 +1029,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       const int tile_i = two ? st : 0;
       const size_t pslot = split >= 0 ? (((size_t)split * a.P + piece) * a.tpb + tile_i) : 0;
       float4* part = reinterpret_cast<float4*>(a.part) + pslot * (D / 4) * TM;
+      float4* s_part = reinterpret_cast<float4*>(smem);  // over the stages, whose products are done
 #pragma unroll 1
       for (int c = c_lo; c < c_hi; c += 16) {
         float o[16];
@@ -994,7 +1058,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
           if (real)
 #pragma unroll
             for (int y = 0; y < 16; y += 4)
-              part[((c + y) >> 2) * TM + lrow] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+              (CL ? s_part + tile_i * (D / 4) * TM : part)[((c + y) >> 2) * TM + lrow] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
         } else if (real && valid) {
           uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
 #pragma unroll
@@ -1006,11 +1070,12 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       fence_before();
       __syncwarp();
       if (lane == 0) { bar_arrive(o_empty); bar_arrive(item_empty + 8 * (seq & 1)); }
+      if (CL) soft_sync();                               // the exchange is over
       if (real && half == 0 && (two || st == 0)) {       // once per row
-        if (split >= 0) a.part_ml[pslot * TM + lrow] = make_float2(m, l);
+        if (split >= 0) (CL ? s_ml + tile_i * TM : a.part_ml + pslot * TM)[lrow] = make_float2(m, l);
         else if (valid && a.lse != nullptr) a.lse[orow] = (m + log2f(l)) * 0.6931471805599453f;
       }
-      if (tid == TT_LEAD && split >= 0 && piece == 0) a.pieces[split] = valid ? pieces : 0;
+      if (tid == TT_LEAD && split >= 0 && piece == 0) (CL ? misc + 3 : a.pieces + split)[0] = valid ? pieces : 0;
       ++seq;
       soft_sync();                                       // misc[2] and the exchange buffer are free again
     }
@@ -1022,11 +1087,26 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
   }
+  if (CL) {
+    // the parts of the block lie in the CTAs of the cluster: everybody adds some of the rows
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    if (warp >= 4) {
+      const int pieces = *cluster.map_shared_rank(const_cast<const int*>(misc) + 3, 0);
+      const int total = pieces > 1 ? a.tpb * TM * (D / 8) : 0;
+      for (int x = (int)cluster.block_rank() * TT_SOFT + tid - TT_LEAD; x < total; x += (int)cluster.num_blocks() * TT_SOFT)
+        join_row<D>(a, p.B, Hkv, g, (int)blockIdx.x / a.P, x, pieces,
+                    [&](int q, int tile, int at) { return *cluster.map_shared_rank(s_ml + tile * TM + at, q); },
+                    [&](int q, int tile, int at) { return *cluster.map_shared_rank(reinterpret_cast<float4*>(smem) + tile * (D / 4) * TM + at, q); });
+    }
+    __syncwarp();
+    cluster.sync();                                      // nobody leaves while its rows may still be read
+  }
 }
 
 constexpr int TJ_THREADS = 256;
 
-// Joins the parts of the blocks that were split: rows' partial sums weighted by 2^(m - max), four parts requested together.
+// Joins the parts of the blocks that were split.
 template <int D>
 __global__ void __launch_bounds__(TJ_THREADS)
 k_tree_join(const __grid_constant__ TreeTcArgs a, int B, int Hkv, int g) {
@@ -1036,58 +1116,11 @@ k_tree_join(const __grid_constant__ TreeTcArgs a, int B, int Hkv, int g) {
   const int split = blockIdx.x / per;
   const int pieces = a.pieces[split];
   if (pieces <= 1) return;
-  const int x = (blockIdx.x - split * per) * TJ_THREADS + threadIdx.x;
-  const int row = x % TM, c = 8 * (x / TM % (D / 8)), tile = x / (TM * (D / 8));
-  const int blk = a.n_full + split;
-  const int unit = blk / a.nqp, qp = blk - unit * a.nqp;
-  const int e = unit / Hkv, h = unit - e * Hkv, b = e % B;
-  const int n = a.n_nodes != nullptr ? a.n_nodes[b] : a.NT;
-  const int node = qp * 2 * a.npt + tile * a.npt + row / g;
-  if (row >= a.npt * g || node >= n) return;
-  const size_t ps = (size_t)split * a.P * a.tpb + tile;
-  const float4* part = reinterpret_cast<const float4*>(a.part);
-  float mm = -INFINITY, ll = 0.f;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-  for (int q = 0; q < pieces; q += 4) {
-    float2 v[4];
-    float4 f[4][2];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const size_t at = ps + (size_t)min(q + k, pieces - 1) * a.tpb;
-      v[k] = __ldcg(a.part_ml + at * TM + row);
-#pragma unroll
-      for (int y = 0; y < 2; ++y) f[k][y] = __ldcg(part + (at * (D / 4) + (c >> 2) + y) * TM + row);
-    }
-    float mn = mm;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (q + k < pieces) mn = tt_max3(mn, v[k].x, v[k].x);
-    const float corr = mm == -INFINITY ? 0.f : tt_ex2(mm - mn);
-    ll *= corr;
-#pragma unroll
-    for (int y = 0; y < 8; ++y) acc[y] *= corr;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (q + k < pieces && v[k].x != -INFINITY) {       // a part in which the row sees nothing does not count
-        const float w = tt_ex2(v[k].x - mn);
-        ll = fmaf(w, v[k].y, ll);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          acc[4 * y] = fmaf(w, f[k][y].x, acc[4 * y]);
-          acc[4 * y + 1] = fmaf(w, f[k][y].y, acc[4 * y + 1]);
-          acc[4 * y + 2] = fmaf(w, f[k][y].z, acc[4 * y + 2]);
-          acc[4 * y + 3] = fmaf(w, f[k][y].w, acc[4 * y + 3]);
-        }
-      }
-    }
-    mm = mn;
-  }
-  const size_t o = ((size_t)e * a.NT + node) * (size_t)(Hkv * g) + (size_t)h * g + row % g;
-  const float linv = 1.f / ll;                           // nothing but -inf: 0 * inf, NaN
-  *reinterpret_cast<uint4*>(a.out + o * D + c) = make_uint4(tt_pack(acc[0] * linv, acc[1] * linv), tt_pack(acc[2] * linv, acc[3] * linv),
-                                                            tt_pack(acc[4] * linv, acc[5] * linv), tt_pack(acc[6] * linv, acc[7] * linv));
-  if (c == 0 && a.lse != nullptr) a.lse[o] = (mm + log2f(ll)) * 0.6931471805599453f;
+  const float4* part = reinterpret_cast<const float4*>(a.part) + (size_t)split * a.P * a.tpb * (D / 4) * TM;
+  const float2* ml = a.part_ml + (size_t)split * a.P * a.tpb * TM;
+  join_row<D>(a, B, Hkv, g, split, (blockIdx.x - split * per) * TJ_THREADS + threadIdx.x, pieces,
+              [&](int q, int tile, int at) { return __ldcg(ml + (q * a.tpb + tile) * TM + at); },
+              [&](int q, int tile, int at) { return __ldcg(part + (q * a.tpb + tile) * (D / 4) * TM + at); });
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -1121,19 +1154,50 @@ bool tt_map(CUtensorMap* map, const void* base, int D, long long n1, long long n
 }
 
 template <int D>
+cudaError_t tt_attributes(int device) {
+  static bool done[PTENC_MAX_DEVICES] = {};
+  if (!ptenc_first_use(done, device)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(k_tree_tc<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_tree_tc<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
+}
+
+template <int D>
 cudaError_t tt_launch(ptenc_cache* c, const CUtensorMap& q, const CUtensorMap& kt, const CUtensorMap& vt,
-                      const TreeTcArgs& a, int grid, cudaStream_t st) {
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_tree_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
-    if (e != cudaSuccess) return e;
-  }
+                      const TreeTcArgs& a, int grid, bool clusters, cudaStream_t st) {
+  cudaError_t e = tt_attributes<D>(c->cfg.device);
+  if (e != cudaSuccess) return e;
   c->launches++;
-  cudaError_t e = tree_launch(k_tree_tc<D>, dim3(grid), TT_THREADS, TSmem<D>::TOTAL, 0, st, c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
+  if (clusters)
+    return tree_launch(k_tree_tc<D, true>, dim3(grid), TT_THREADS, TSmem<D>::TOTAL, a.P, st, c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
+  e = tree_launch(k_tree_tc<D, false>, dim3(grid), TT_THREADS, TSmem<D>::TOTAL, 0, st, c->dev, c->tmTreeK, c->tmTreeV, q, kt, vt, a);
   if (e != cudaSuccess || a.P == 1 || a.n_items == a.n_full) return e;
   c->launches++;
   return tree_launch(k_tree_join<D>, dim3((unsigned)((a.n_items - a.n_full) / a.P * (a.tpb * TM * (D / 8) / TJ_THREADS))), TJ_THREADS,
                      0, 0, st, a, c->dev.B, c->dev.Hkv, c->dev.g);
+}
+
+// Clusters of `size` CTAs that the device holds at a time (one CTA per SM), 0 if it cannot say.
+template <int D>
+int tt_clusters(int device, int size) {
+  if (tt_attributes<D>(device) != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(size);
+  cfg.blockDim = dim3(TT_THREADS);
+  cfg.dynamicSmemBytes = TSmem<D>::TOTAL;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, k_tree_tc<D, true>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return n;
 }
 
 }  // namespace
@@ -1153,6 +1217,15 @@ bool ptenc_tree_tc_prepare(ptenc_cache* c) {
   const long long units = (long long)p.L * p.B * p.Hkv;
   const int box = p.W < TN ? p.W : TN;
   c->tree_tc = tt_map(&c->tmTreeK, p.K, p.D, p.W, units, box, 1) && tt_map(&c->tmTreeV, p.V, p.D, p.W, units, box, 1);
+  static int held[PTENC_MAX_DEVICES][2][3];              // 1 + clusters of 2, 4, 8 CTAs; alike for every handle on the device
+  for (int i = 0; i < 3; ++i) {
+    int x = 0;
+    const bool keep = c->cfg.device < PTENC_MAX_DEVICES;
+    if (keep) x = held[c->cfg.device][p.D == 128][i];
+    if (x == 0) x = 1 + (p.D == 128 ? tt_clusters<128>(c->cfg.device, 2 << i) : tt_clusters<64>(c->cfg.device, 2 << i));
+    if (keep) held[c->cfg.device][p.D == 128][i] = x;
+    c->tree_clusters[i] = x - 1;
+  }
   return c->tree_tc;
 }
 
@@ -1187,7 +1260,15 @@ cudaError_t ptenc_launch_tree(ptenc_cache* c, int l0, int nl, const void* q, con
     const float cost = (float)((rem * P + sms - 1) / sms) * (4.f + (a.tpb == 2 ? 1.6f : 1.2f) * (float)((nt + P - 1) / P)) + (P > 1 ? 3.f : 0.f);
     if (cost < best) { best = cost; a.P = P; }
   }
+  // Where a cluster can hold every block's parts, they are joined in its shared memory instead, without a second kernel.
+  bool clusters = false;
+  for (int i = 0; i < 3 && a.n_full == 0; ++i) {
+    const int P = 2 << i;
+    if (P > nt || rem > c->tree_clusters[i]) continue;
+    const float cost = 4.f + (a.tpb == 2 ? 1.6f : 1.2f) * (float)((nt + P - 1) / P) + 1.f;
+    if (cost < best) { best = cost; a.P = P; clusters = true; }
+  }
   a.n_items = a.n_full + rem * a.P;
-  const int grid = a.n_items < sms ? a.n_items : sms;
-  return p.D == 128 ? tt_launch<128>(c, mq, mk, mv, a, grid, st) : tt_launch<64>(c, mq, mk, mv, a, grid, st);
+  const int grid = clusters || a.n_items < sms ? a.n_items : sms;
+  return p.D == 128 ? tt_launch<128>(c, mq, mk, mv, a, grid, clusters, st) : tt_launch<64>(c, mq, mk, mv, a, grid, clusters, st);
 }
