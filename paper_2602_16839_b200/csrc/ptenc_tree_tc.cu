@@ -29,8 +29,9 @@
 //  * Every wait is bounded: one that runs out raises a status bit and an abort flag, every role then leaves, copies and
 //    MMAs in flight are drained and tensor memory is freed.
 //
-// Measured (head size 128, full rings).  128 sequences of 16 nodes, groups of 7, four rings of 2048 slots: 571 MB in 110 us,
-// 5.2 TB/s.  64 sequences of 64 nodes, groups of 4, eight rings of 4096 slots: 277 GFLOP in 310 us, 0.9 PFLOP/s; there the
+// Measured (head size 128, full rings).  128 sequences of 16 nodes, groups of 7, four rings of 2048 slots: 571 MB in 107 us,
+// 5.3 TB/s; an item costs about 10000 cycles beside the 33000 of its tiles (description, set-up, the last product, the rows' way
+// out).  64 sequences of 64 nodes, groups of 4, eight rings of 4096 slots: 277 GFLOP in 303 us, 0.9 PFLOP/s; there the
 // tensor pipe is 44 % busy, the exponentials' unit 45 %, the issue slots 46 %: the bound is a stream's chain, about 3800
 // cycles a tile, of which both products take 1100, the maximum 630, its exchange 180, P 1650 and handing over the rest.  One
 // chain of 5 nodes over 1024 slots: 12 us, most of it set-up and the join.  What did not shorten the chain: tiles of 64
@@ -187,6 +188,17 @@ __device__ __forceinline__ float tt_max3(float a, float b, float c) {
 __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+// Sixteen outputs of a row.  The rows of a warp lie apart, so a store costs a cycle per row whatever its width: 32 bytes at a
+// time where the tensor is aligned for it.
+__device__ __forceinline__ void tt_store(__nv_bfloat16* to, const uint32_t (&r)[8], bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
 }
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TT_SOFT) : "memory"); }
 __device__ __forceinline__ void stream_sync(int st) {                        // the eight warps of a stream
@@ -1029,6 +1041,7 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
       const int tile_i = two ? st : 0;
       const size_t pslot = split >= 0 ? (((size_t)split * a.P + piece) * a.tpb + tile_i) : 0;
       float4* part = reinterpret_cast<float4*>(a.part) + pslot * (D / 4) * TM;
+      const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
       float4* s_part = reinterpret_cast<float4*>(smem);  // over the stages, whose products are done
 #pragma unroll 1
       for (int c = c_lo; c < c_hi; c += 16) {
@@ -1060,11 +1073,10 @@ k_tree_tc(const __grid_constant__ PtencDev p, const __grid_constant__ CUtensorMa
             for (int y = 0; y < 16; y += 4)
               (CL ? s_part + tile_i * (D / 4) * TM : part)[((c + y) >> 2) * TM + lrow] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
         } else if (real && valid) {
-          uint4* dst = reinterpret_cast<uint4*>(a.out + orow * D + c);
+          uint32_t pk[8];
 #pragma unroll
-          for (int y = 0; y < 16; y += 8)
-            dst[y >> 3] = make_uint4(tt_pack(o[y] * inv, o[y + 1] * inv), tt_pack(o[y + 2] * inv, o[y + 3] * inv),
-                                     tt_pack(o[y + 4] * inv, o[y + 5] * inv), tt_pack(o[y + 6] * inv, o[y + 7] * inv));
+          for (int y = 0; y < 16; y += 2) pk[y >> 1] = tt_pack(o[y] * inv, o[y + 1] * inv);
+          tt_store(a.out + orow * D + c, pk, wide);
         }
       }
       fence_before();

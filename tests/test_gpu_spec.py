@@ -315,6 +315,33 @@ def test_a_cache_whose_offsets_pass_32_bits(D, B):
     big.close(), small.close()
 
 
+@pytest.mark.parametrize("dtype,D,B", [("bf16", 128, 2), ("bf16", 64, 90), ("fp32", 64, 2)])
+def test_tensors_at_the_least_alignment(dtype, D, B):
+    """Every tensor 16 bytes (whole numbers 4) behind a 256-byte boundary: the same bits as aligned ones."""
+    T = 6
+    p = Pair(pt, n_layers=1, batch=B, n_q_heads=8, n_kv_heads=2, head_dim=D, window=70, dtype=dtype, seed=17)
+    for t in range(75):
+        k, v = p.gen.step_kv(t)
+        p.cache.append_evict(-1, k, v)
+    q, k, v = _drafts(p, T)
+    parent, n = _cuda(_trees(np.random.default_rng(0), B, T, "tree")), torch.full((B,), T, dtype=torch.int32, device="cuda")
+
+    def off(x, nbytes):
+        room = torch.zeros(x.numel() * x.element_size() + 256 + nbytes, dtype=torch.uint8, device="cuda")
+        start = -room.data_ptr() % 256 + nbytes
+        y = room[start:start + x.numel() * x.element_size()].view(x.dtype).view(x.shape)
+        y.copy_(x)
+        assert y.data_ptr() % 256 == nbytes
+        return y
+
+    a, la = torch.zeros_like(q), torch.zeros(1, B, T, 8, device="cuda")
+    b, lb = off(a, 16), off(la, 4)
+    p.cache.tree_attn(-1, q, k, v, parent, a, n_nodes=n, lse_out=la)
+    p.cache.tree_attn(-1, off(q, 16), off(k, 16), off(v, 16), off(parent, 4), b, n_nodes=off(n, 4), lse_out=lb)
+    assert torch.equal(a, b) and torch.equal(la, lb) and float(a.abs().max()) > 0
+    p.close()
+
+
 def test_bad_trees_are_left_alone():
     """Parents out of order, counts out of range: that sequence is skipped and the status word says so; the others are served."""
     for D in (128, 32):
