@@ -707,6 +707,31 @@ def test_verify_survives_rows_that_are_no_numbers():
         assert ((got[2] >= -1) & (got[2] < 2051)).all() and ((got[1] >= 1) & (got[1] <= 5)).all()
 
 
+@pytest.mark.parametrize("with_q", [True, False])
+def test_verify_rows_past_32_bits(with_q):
+    """2.4e9 entries: the last sequence gives what it gives alone, in rows of 1.3e8 entries and of an odd width."""
+    B, T, V = 6, 3, 2 ** 27 + 1
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    p = torch.rand(B, T, V, generator=gen, device="cuda", dtype=torch.bfloat16)
+    q = torch.rand(B, T, V, generator=gen, device="cuda", dtype=torch.bfloat16) if with_q else None
+    assert p.numel() > 2 ** 31
+    tok = torch.randint(0, V, (B, T), generator=gen, device="cuda", dtype=torch.int32)
+    parent = torch.tensor([[-1, 0, 0]] * B, dtype=torch.int32, device="cuda")
+    u = torch.rand(B, T, generator=gen, device="cuda")
+    u[:, 1:] = 1 - 2.0 ** -24                                 # rejected but where the target's entry is the larger one
+
+    def run(lo):
+        n, i32 = B - lo, dict(dtype=torch.int32, device="cuda")
+        path, n_path, nxt = torch.empty(n, T, **i32), torch.empty(n, **i32), torch.empty(n, **i32)
+        pt.verify_tree(p[lo:].clone(), None if q is None else q[lo:].clone(), tok[lo:].clone(), parent[lo:].clone(), u[lo:].clone(),
+                       path, n_path, nxt)
+        return path, n_path, nxt
+
+    for x, y in zip(run(0), run(B - 1)):
+        assert torch.equal(x[-1], y[-1])
+    assert int(run(0)[2].min()) >= 0 and int(run(0)[2].max()) > 2 ** 20
+
+
 # ------------------------------------------------------------------------------------------------------------ together
 class _Round:
     """One speculative round of a stand-in model: every node's output of the last layer, projected to a vocabulary."""
