@@ -840,3 +840,51 @@ def test_a_captured_round_replays_on_another_stream():
     del graph
     for x in (a, b):
         x.close()
+
+
+def test_two_caches_on_two_streams_at_once():
+    """Rounds on two handles, queued on two streams without a wait between them, give the bits of the same rounds one by one."""
+    T, turns = 7, 12
+    kws = [dict(n_layers=2, batch=24, n_q_heads=8, n_kv_heads=4, head_dim=128, window=300, evict_chunk=1),
+           dict(n_layers=2, batch=6, n_q_heads=8, n_kv_heads=2, head_dim=64, window=96, evict_chunk=16)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    pairs = [Pair(pt, seed=18, n_global=32, rank=32, **kw) for kw in kws]
+    drafts = [[_drafts(p, T, seed=t) for t in range(turns)] for p in pairs]
+    rng = np.random.default_rng(4)
+    parents = [_cuda(_trees(rng, kw["batch"], T, "tree")) for kw in kws]
+    paths = [[_cuda(np.sort(rng.permuted(np.tile(np.arange(T), (kw["batch"], 1)), axis=1)[:, :4], axis=1)) for _ in range(turns)]
+             for kw in kws]
+    count = [torch.full((kw["batch"],), 4, dtype=torch.int32, device="cuda") for kw in kws]
+    full = [[torch.cat([x, x[:, :3]], 1).contiguous() for x in ps] for ps in paths]
+
+    def turn(i, t, out):
+        q, k, v = drafts[i][t]
+        pairs[i].cache.tree_attn(-1, q, k, v, parents[i], out)
+        pairs[i].cache.commit_path(-1, k, v, full[i][t], count[i])
+
+    for p in pairs:
+        for t in range(p.W + 3):
+            k, v = p.gen.step_kv(t)
+            p.cache.append_evict(-1, k, v)
+    start = [p.cache.workspace.clone() for p in pairs]
+    results = []
+    for together in (False, True):
+        for p, ws in zip(pairs, start):
+            p.cache.workspace.copy_(ws)
+        outs = [[torch.zeros_like(d[0]) for d in ds] for ds in drafts]
+        torch.cuda.synchronize()
+        for t in range(turns):
+            for i in (0, 1):
+                with torch.cuda.stream(streams[i]):
+                    turn(i, t, outs[i][t])
+                if not together:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert all(p.cache.status() == 0 for p in pairs)
+        results.append((outs, [r.clone() for p in pairs for r in _rings(p.cache)], [p.cache.get_state(l) for p in pairs for l in (0, 1)]))
+    for x, y in zip(results[0][0], results[1][0]):
+        assert all(torch.equal(a, b) and float(a.float().abs().max()) > 0 for a, b in zip(x, y))
+    for part in (1, 2):
+        assert all(torch.equal(a, b) for a, b in zip(results[0][part], results[1][part]))
+    for p in pairs:
+        p.close()
