@@ -106,6 +106,7 @@ k_verify_tree(const VerifyArgs a) {
   __shared__ int s_rej[TREE_MAX];                  // certain drafts: tokens rejected at the current node,
   __shared__ double s_left[TREE_MAX];              // and what is left of their entries
   __shared__ double s_sum[2][VF_CLUSTER * VF_WARPS];              // the warps' sums of a pass; passes alternate
+  __shared__ double s_raw[VF_CLUSTER * VF_WARPS];  // certain drafts: the warps' sums of the row as it is
   __shared__ double s_warp[VF_WARPS];
   __shared__ int s_hit, s_tail;
 
@@ -264,7 +265,7 @@ k_verify_tree(const VerifyArgs a) {
   unsigned long long line = 1ull;                                 // the path's nodes; they come in rising order
   double c = 1.0;                                                 // r = w / c
   double raw = 0.0, mass = 0.0;                                   // certain drafts: sums of the row as it is, and of w
-  bool summed = false;
+  bool summed = false, stale = false;                             // stale: some warp's sum is to be taken again before the draw
   unsigned long long kids = 0;
   auto children = [&]() {
     kids = (unsigned long long)__ballot_sync(0xffffffffu, par0 == cur) |
@@ -290,17 +291,21 @@ k_verify_tree(const VerifyArgs a) {
         C = raw = 0.0;
         c = 1.0;
         nrej = 0;
-        summed = false;
+        summed = stale = false;
         children();
         continue;
       }
       C += c;
       if (!QROWS) {
         // A certain draft changes one entry, so the sums follow from those of the row as it is, as long as what is left is
-        // no small part of it (1e-3 leaves thirteen digits); otherwise the row is summed again without the entries.
+        // no small part of it (1e-3 leaves thirteen digits); otherwise the row is summed again without the entries.  The same
+        // holds of the sum of the warp that had the entry, which only the draw looks at: where little is left of it, down
+        // to a residue of the rounding or nothing beside entries that were too small to count, the row is summed once more before
+        // the draw.
         if (raw == 0.0) {
           take_row();
           raw = mass = row_total();
+          if (tid < VF_CLUSTER * VF_WARPS) s_raw[tid] = s_sum[(pass - 1) & 1][tid];
         }
         const double left = fmax(w - c, 0.0);
         __syncthreads();
@@ -312,17 +317,20 @@ k_verify_tree(const VerifyArgs a) {
         if (same < 0) ++nrej;
         mass -= w - left;
         if (mass > 1e-3 * raw) {
-          if (tid == 0) s_sum[(pass - 1) & 1][(s_tok[i] + off) / N / per] -= w - left;
+          const int at = (s_tok[i] + off) / N / per;
+          if (tid == 0) s_sum[(pass - 1) & 1][at] -= w - left;
           c = mass;
           summed = true;
           __syncthreads();
+          stale |= w > left && !(s_sum[(pass - 1) & 1][at] > 1e-3 * s_raw[at]);
           continue;
         }
         __syncthreads();
       }
-    } else if (summed) {
+    } else if (summed && !stale) {
       break;
     }
+    stale = false;
     const bool last = kids == 0 && C == 0.0;                      // no rejection to account for: the row as it is, for the draw
     take_row();
     c = mass = row_total();

@@ -732,6 +732,77 @@ def test_verify_rows_past_32_bits(with_q):
     assert int(run(0)[2].min()) >= 0 and int(run(0)[2].max()) > 2 ** 20
 
 
+def _stretch_rows(dtype):
+    """Rows of 50001 entries, of which a cluster's warps sum about 800 each, with two certain drafts at the start of the row that
+    are rejected there: (entry 3, entry 7, entry 11); the rest of the row's weight lies from entry 30000 on.  Taking the two
+    out of the stretch's sum leaves a residue above zero, one below zero, or hides the third entry altogether."""
+    small = dict(fp32=(1e-12, 1e-10, 3e-11), bf16=(1e-16, 1.1e-15, 3e-15))[dtype]
+    rows = [(0.3, small[0], 0.0), (0.3, small[1], 0.0), (small[1], 0.3, 0.0), (0.4, small[2], 0.0), (0.3, 0.0, 1e-20),
+            (0.3, small[1], 1e-20), (1e-10, 0.3, 1e-25), (0.3, 0.2, 1e-6)]
+    p = torch.zeros(len(rows), 50001)
+    for x, (a, b, c) in zip(p, rows):
+        x[3], x[7], x[11] = a, b, c
+        x[30000:30010] = (1 - a - b - c) / 10
+    return p.to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_certain_drafts_that_take_nearly_all_of_a_stretch(dtype):
+    """u[0] = 0 draws the first token with any weight left, however little it is beside what the rejected drafts held; at a root and
+    at a node that was accepted after rejections.  With u[0] = 0 the definition has no rounding: every sum up to the drawn
+    token is zero or not."""
+    rows = _stretch_rows(dtype)
+    B, V = rows.shape
+    first = torch.zeros(V)
+    first[[3, 40, 49000]] = torch.tensor([0.25, 0.25, 0.5])
+    for order in ((3, 7), (7, 3)):
+        # at the root: both siblings rejected
+        p = rows[:, None].expand(B, 3, V).contiguous()
+        tok, par = np.tile([0, *order], (B, 1)), np.tile([-1, 0, 0], (B, 1))
+        u = np.tile(np.float32([0.0, 0.99, 0.99]), (B, 1))
+        # behind an accepted sibling: entries 3 and 40 of another row come first, the second of them is taken
+        deep = torch.stack([first.to(rows.dtype).expand(B, V), rows, rows, rows, rows], 1).contiguous()
+        tok2, par2 = np.tile([0, 3, 40, *order], (B, 1)), np.tile([-1, 0, 0, 2, 2], (B, 1))
+        u2 = np.tile(np.float32([0.0, 0.9, 0.1, 0.99, 0.99]), (B, 1))
+        for q, t, pa, uu, line in ((p, tok, par, u, [0]), (deep, tok2, par2, u2, [0, 2])):
+            path, n_path, nxt = _run_verify(q, None, t, pa, uu)
+            for b in range(B):
+                want = so.verify_tree(q[b].double().numpy(), None, t[b], pa[b], uu[b])
+                assert want[0] == line
+                assert list(path[b, :n_path[b]]) == line and nxt[b] == want[1], (order, b, nxt[b], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_certain_drafts_on_peaked_rows(dtype):
+    """Rows with a few tokens of weight and zeros elsewhere (what a top-k filter leaves), siblings drawn among those tokens, the same
+    token twice included."""
+    rng = np.random.default_rng(8)
+    B, T, V = 48, 12, 20011
+    p = torch.zeros(B, T, V, dtype=torch.float64)
+    tok = np.zeros((B, T), np.int32)
+    for b in range(B):
+        k = int(rng.integers(2, 30))
+        where = np.sort(rng.choice(V, k, replace=False)) if b % 2 else int(rng.integers(0, V - 64)) + np.sort(rng.choice(64, k, replace=False))
+        for i in range(T):
+            w = np.exp(rng.standard_normal(k) * rng.choice([1.0, 8.0, 16.0]))
+            p[b, i, where] = torch.as_tensor(w / w.sum())
+        tok[b] = where[rng.integers(0, k, T)]
+    p = p.to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+    parent = np.full((B, T), -1, np.int32)
+    for i in range(1, T):
+        parent[:, i] = np.where(rng.random(B) < 0.8, 0, rng.integers(0, i, B))
+    u = rng.random((B, T)).astype(np.float32)
+    for zero in (False, True):
+        if zero:
+            u[:, 0] = 0.0
+        path, n_path, nxt = _run_verify(p, None, tok, parent, u)
+        for b in range(B):
+            line, x, margin = so.verify_tree(p[b].double().numpy(), None, tok[b], parent[b], u[b])
+            if margin <= 1e-12 and not zero:
+                continue                                      # on a border up to rounding: both neighbours are right
+            assert list(path[b, :n_path[b]]) == line and nxt[b] == x, (zero, b, nxt[b], x)
+
+
 # ------------------------------------------------------------------------------------------------------------ together
 class _Round:
     """One speculative round of a stand-in model: every node's output of the last layer, projected to a vocabulary."""
