@@ -972,9 +972,10 @@ bool make_ring_map(CUtensorMap* map, void* base, long long rows, int D, int tile
   cuuint64_t strides[1] = {(cuuint64_t)D * 2};
   cuuint32_t box[2] = {64, (cuuint32_t)tile_n};
   cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, PTENC_ATTN_L2PROMO,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return ptenc_encode_map([&] {
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, PTENC_ATTN_L2PROMO, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  });
 }
 
 constexpr int NW_DEFAULT = PTENC_ATTN_NW;

@@ -156,6 +156,16 @@ bool ptenc_attn_bf16_prepare(ptenc_cache* c, cudaError_t* err);
 // The instantiation a launch over `nl` layers would use: consumer warps, tokens per tile, pipeline stages.
 void ptenc_attn_bf16_plan(const ptenc_cache* c, int nl, int* consumer_warps, int* tile_tokens, int* stages);
 
+// Describing a tensor to the TMA unit is a driver call that wants a current context, and a host thread whose first CUDA call
+// this is has none: the runtime binds one when it is asked for something that needs it.  Encodes; if that fails, makes the
+// thread's current device's context current and encodes once more.
+template <typename Encode>
+inline bool ptenc_encode_map(Encode encode) {
+  if (encode() == CUDA_SUCCESS) return true;
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode() == CUDA_SUCCESS;
+}
+
 // Kernel attributes are per device: a launcher sets them the first time it runs on a device.
 constexpr int PTENC_MAX_DEVICES = 64;
 inline bool ptenc_first_use(bool (&done)[PTENC_MAX_DEVICES], int device) {
