@@ -109,9 +109,8 @@ Layout make_layout(const ptenc_config* c) {
 // With PTENC_DEBUG set in the environment, failed CUDA calls are reported on stderr (and every launch is
 // followed by a synchronise so the report names the right step).
 bool debug_on() {
-  static int on = -1;
-  if (on < 0) { const char* e = getenv("PTENC_DEBUG"); on = (e != nullptr && e[0] != '\0' && e[0] != '0') ? 1 : 0; }
-  return on == 1;
+  static const bool on = [] { const char* e = getenv("PTENC_DEBUG"); return e != nullptr && e[0] != '\0' && e[0] != '0'; }();
+  return on;
 }
 bool ok(cudaError_t e, const char* where, cudaStream_t st = nullptr) {
   if (e == cudaSuccess && debug_on()) e = cudaStreamSynchronize(st);

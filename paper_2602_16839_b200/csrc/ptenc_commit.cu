@@ -523,9 +523,9 @@ cudaError_t launch_commit_t(ptenc_cache* c, int l0, int nl, const void* kt, cons
                             const int32_t* n_path, const uint8_t* active, int32_t* n_evicted_out, cudaStream_t st) {
   const PtencDev& p = c->dev;
   const size_t smem = sizeof(float) * (size_t)(2 * p.d_kv + 2 * p.r + p.G + 2 * p.G * p.r + p.G + 1);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (smem > 40 * 1024 && ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_commit<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  static PtencOnce once;
+  if (smem > 40 * 1024) {
+    const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_commit<T>, 200 * 1024); });
     if (e != cudaSuccess) return e;
   }
   c->launches++;
@@ -545,9 +545,9 @@ cudaError_t launch_commit_bf16(ptenc_cache* c, int l0, int nl, const void* kt, c
                                const int32_t* n_path, const uint8_t* active, int32_t* n_evicted_out, bool defer,
                                cudaStream_t st) {
   const size_t smem = commit_smem(c->dev);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (smem > 40 * 1024 && ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_commit_bf16<RJ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)CM_SMEM);
+  static PtencOnce once;
+  if (smem > 40 * 1024) {
+    const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_commit_bf16<RJ>, CM_SMEM); });
     if (e != cudaSuccess) return e;
   }
   c->launches++;

@@ -192,9 +192,9 @@ template <typename T>
 cudaError_t launch_encode_t(ptenc_cache* c, int l0, int nl, const void* Ke, const void* Ve,
                             const int32_t* n_ev, int m_max, int mode, cudaStream_t st) {
   const size_t smem = encode_smem(c->dev);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};          // one per instantiation of this template
-  if (smem > 48 * 1024 && ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_encode_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  static PtencOnce once;                                  // one per instantiation of this template
+  if (smem > 48 * 1024) {
+    const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_encode_rows<T>, 200 * 1024); });
     if (e != cudaSuccess) return e;
   }
   const int grid = mode == 1 ? 1 : nl * c->cfg.batch;

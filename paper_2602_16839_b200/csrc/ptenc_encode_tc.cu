@@ -534,7 +534,7 @@ typedef CUresult (*TcEncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_
                                     CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 TcEncodeTiledFn tc_encode_fn() {
-  static TcEncodeTiledFn fn = nullptr;
+  static std::atomic<TcEncodeTiledFn> fn;
   if (fn != nullptr) return fn;
   void* ptr = nullptr;
   cudaDriverEntryPointQueryResult qres;
@@ -569,12 +569,9 @@ template <int R>
 cudaError_t tc_launch(ptenc_cache* c, const CUtensorMap& tmK, const CUtensorMap& tmV, const TcArgs& a, int nl,
                       cudaStream_t st) {
   const size_t smem = TcSmem<R>::total(c->dev.G);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_encode_chunk_tc<R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)TcSmem<R>::total(128));
-    if (e != cudaSuccess) return e;
-  }
+  static PtencOnce once;
+  const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_encode_chunk_tc<R>, TcSmem<R>::total(128)); });
+  if (e != cudaSuccess) return e;
   // persistent: two CTAs per SM walk the (layer, sequence) units, so barriers and tensor memory are set up once per
   // CTA and the loads of a unit's first tile overlap the epilogue of the unit before
   int grid = nl * c->cfg.batch;

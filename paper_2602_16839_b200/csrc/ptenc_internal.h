@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "ptenc.h"
+#include "ptenc_once.h"
 
 // Device status bits (sticky, OR-ed into *status).
 #define PTENC_ST_WAIT_TIMEOUT 1   // a bounded mbarrier wait ran out
@@ -166,13 +167,10 @@ inline bool ptenc_encode_map(Encode encode) {
   return cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess && encode() == CUDA_SUCCESS;
 }
 
-// Kernel attributes are per device: a launcher sets them the first time it runs on a device.
-constexpr int PTENC_MAX_DEVICES = 64;
-inline bool ptenc_first_use(bool (&done)[PTENC_MAX_DEVICES], int device) {
-  if (device < 0 || device >= PTENC_MAX_DEVICES) return true;     // unknown ordinal: set the attribute every time
-  if (done[device]) return false;
-  done[device] = true;
-  return true;
+// Kernel attributes are per device: a launcher sets them through ptenc_first_use (ptenc_once.h).
+template <typename Kernel>
+inline cudaError_t ptenc_allow_smem(Kernel kernel, size_t bytes) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
 // ---- small device helpers --------------------------------------------------------------------------

@@ -507,16 +507,15 @@ cudaError_t ls_apply(ptenc_cache* c, int l0, int nl, const __nv_bfloat16* A, con
   if (c->cfg.dtype != PTENC_DTYPE_BF16 || (p.r != 16 && p.r != 32 && p.r != 64) || (p.G & 31) != 0 || p.G > 128 ||
       (d_in & 31) != 0 || (d_out & 7) != 0 || nl > 65535)
     return cudaSuccess;
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaSuccess;
-    auto big = [&](const void* f) {
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)LS_SMEM_MAX);
-    };
+  static PtencOnce once;
+  cudaError_t e = ptenc_first_use(once, c->cfg.device, [] {
+    cudaError_t err = cudaSuccess;
+    auto big = [&](const void* f) { if (err == cudaSuccess) err = ptenc_allow_smem(f, LS_SMEM_MAX); };
     big((const void*)k_lora_u<2>); big((const void*)k_lora_u<4>); big((const void*)k_lora_u<8>);
     big((const void*)k_lora_y<1>); big((const void*)k_lora_y<2>); big((const void*)k_lora_y<3>); big((const void*)k_lora_y<4>);
-    if (e != cudaSuccess) return e;
-  }
+    return err;
+  });
+  if (e != cudaSuccess) return e;
   const int n_mt = (p.B + 15) / 16;
   const int want = PTENC_LORA_CTAS_PER_SM * c->sm_count;        // CTAs of a streaming kernel: all resident at once
   // slices of d_in: enough CTAs, a slice of B that fits shared memory, no more partial sums than the scratch holds
@@ -547,7 +546,6 @@ cudaError_t ls_apply(ptenc_cache* c, int l0, int nl, const __nv_bfloat16* A, con
   __nv_bfloat16* w_hi = c->lora_w;
   __nv_bfloat16* w_lo = c->lora_w + (size_t)p.L * p.B * p.G;
   const float* u_c = c->lora_u;
-  cudaError_t e;
   switch (p.r) {
     case 16: e = ls_launch(k_lora_u<2>, dim3(SL, nl), smem_u, false, st, p, Bm, x, c->lora_u, d_in, SL, KS); break;
     case 32: e = ls_launch(k_lora_u<4>, dim3(SL, nl), smem_u, false, st, p, Bm, x, c->lora_u, d_in, SL, KS); break;
@@ -590,13 +588,12 @@ cudaError_t ptenc_launch_lora_apply(ptenc_cache* c, int l0, int nl, const void* 
                                        (((size_t)LR_SEQ * p.G * (p.r + 1) + 3) & ~(size_t)3)) +
                       (size_t)LR_SEQ * d_in * p.elt;
   if (smem > 200 * 1024) return cudaErrorInvalidValue;
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_lora_apply<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(k_lora_apply<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    if (e != cudaSuccess) return e;
-  }
+  static PtencOnce once;
+  const cudaError_t set = ptenc_first_use(once, c->cfg.device, [] {
+    const cudaError_t e = ptenc_allow_smem(k_lora_apply<float>, 200 * 1024);
+    return e != cudaSuccess ? e : ptenc_allow_smem(k_lora_apply<__nv_bfloat16>, 200 * 1024);
+  });
+  if (set != cudaSuccess) return set;
   const int nblk = (p.B + LR_SEQ - 1) / LR_SEQ;
   if (c->cfg.dtype == PTENC_DTYPE_FP32)
     k_lora_apply<float><<<nl * nblk, LR_THREADS, smem, st>>>(p, l0, (const float*)A, (const float*)Bm,

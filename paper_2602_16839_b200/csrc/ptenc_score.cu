@@ -265,11 +265,9 @@ cudaError_t ptenc_launch_score_step(ptenc_cache* c, int l0, int nl, const void* 
                                     const uint8_t* active, int32_t* slot_out, int64_t* evict_first_out,
                                     int32_t* n_evicted_out, cudaStream_t st) {
   const size_t smem = ptenc_score_step_smem(&c->cfg);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_score_step, cudaFuncAttributeMaxDynamicSharedMemorySize, 8192 * 12);
-    if (e != cudaSuccess) return e;
-  }
+  static PtencOnce once;
+  const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_score_step, 8192 * 12); });
+  if (e != cudaSuccess) return e;
   const int n2 = c->cfg.evict_chunk > 1 ? pow2_at_least(c->cfg.window) : 1;
   k_score_step<<<nl * c->cfg.batch, SC_THREADS, smem, st>>>(c->dev, l0, (const char*)k_new, (const char*)v_new, active,
                                                            slot_out, (long long*)evict_first_out, n_evicted_out, n2);

@@ -350,11 +350,9 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
   if (blocks * cs > 0x7fffffffll) return cudaErrorInvalidValue;
   const int sets = tg_smem<T>(p.D, 2) > 200 * 1024 ? 1 : 2;
   const size_t smem = tg_smem<T>(p.D, sets);
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, c->cfg.device)) {
-    cudaError_t e = cudaFuncSetAttribute(k_tree_generic<T, J>, cudaFuncAttributeMaxDynamicSharedMemorySize, 216 * 1024);
-    if (e != cudaSuccess) return e;
-  }
+  static PtencOnce once;
+  const cudaError_t e = ptenc_first_use(once, c->cfg.device, [] { return ptenc_allow_smem(k_tree_generic<T, J>, 216 * 1024); });
+  if (e != cudaSuccess) return e;
   c->launches++;
   return tree_launch(k_tree_generic<T, J>, dim3((unsigned)(blocks * cs)), TG_SET * sets, smem, cs, st, p, l0, (const T*)q,
                      (const T*)kt, (const T*)vt, parent, n_nodes, NT, active, (T*)out, lse, n_groups);

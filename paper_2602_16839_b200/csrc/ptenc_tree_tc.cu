@@ -1141,7 +1141,7 @@ typedef CUresult (*TtEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, vo
                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 TtEncodeFn tt_encode_fn() {
-  static TtEncodeFn fn = nullptr;
+  static std::atomic<TtEncodeFn> fn;
   if (fn != nullptr) return fn;
   void* ptr = nullptr;
   cudaDriverEntryPointQueryResult qres;
@@ -1169,10 +1169,11 @@ bool tt_map(CUtensorMap* map, const void* base, int D, long long n1, long long n
 
 template <int D>
 cudaError_t tt_attributes(int device) {
-  static bool done[PTENC_MAX_DEVICES] = {};
-  if (!ptenc_first_use(done, device)) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(k_tree_tc<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_tree_tc<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, TSmem<D>::TOTAL);
+  static PtencOnce once;
+  return ptenc_first_use(once, device, [] {
+    const cudaError_t e = ptenc_allow_smem(k_tree_tc<D, false>, TSmem<D>::TOTAL);
+    return e != cudaSuccess ? e : ptenc_allow_smem(k_tree_tc<D, true>, TSmem<D>::TOTAL);
+  });
 }
 
 template <int D>
@@ -1190,10 +1191,13 @@ cudaError_t tt_launch(ptenc_cache* c, const CUtensorMap& q, const CUtensorMap& k
                      0, 0, st, a, c->dev.B, c->dev.Hkv, c->dev.g);
 }
 
-// Clusters of `size` CTAs that the device holds at a time (one CTA per SM), 0 if it cannot say.
+// Clusters of `size` CTAs that the device holds at a time (one CTA per SM), -1 if it cannot say.
 template <int D>
 int tt_clusters(int device, int size) {
-  if (tt_attributes<D>(device) != cudaSuccess) return 0;
+  if (tt_attributes<D>(device) != cudaSuccess) {
+    cudaGetLastError();
+    return -1;
+  }
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(size);
@@ -1209,7 +1213,7 @@ int tt_clusters(int device, int size) {
   int n = 0;
   if (cudaOccupancyMaxActiveClusters(&n, k_tree_tc<D, true>, &cfg) != cudaSuccess) {
     cudaGetLastError();
-    return 0;
+    return -1;
   }
   return n;
 }
@@ -1231,14 +1235,15 @@ bool ptenc_tree_tc_prepare(ptenc_cache* c) {
   const long long units = (long long)p.L * p.B * p.Hkv;
   const int box = p.W < TN ? p.W : TN;
   c->tree_tc = tt_map(&c->tmTreeK, p.K, p.D, p.W, units, box, 1) && tt_map(&c->tmTreeV, p.V, p.D, p.W, units, box, 1);
-  static int held[PTENC_MAX_DEVICES][2][3];              // 1 + clusters of 2, 4, 8 CTAs; alike for every handle on the device
+  // 1 + clusters of 2, 4, 8 CTAs; alike for every handle on the device, so threads that find none ask for the same
+  static std::atomic<int> held[PTENC_MAX_DEVICES][2][3];
   for (int i = 0; i < 3; ++i) {
     int x = 0;
     const bool keep = c->cfg.device < PTENC_MAX_DEVICES;
     if (keep) x = held[c->cfg.device][p.D == 128][i];
     if (x == 0) x = 1 + (p.D == 128 ? tt_clusters<128>(c->cfg.device, 2 << i) : tt_clusters<64>(c->cfg.device, 2 << i));
-    if (keep) held[c->cfg.device][p.D == 128][i] = x;
-    c->tree_clusters[i] = x - 1;
+    if (keep) held[c->cfg.device][p.D == 128][i] = x;    // 0: the next handle asks again
+    c->tree_clusters[i] = x > 0 ? x - 1 : 0;
   }
   return c->tree_tc;
 }

@@ -436,12 +436,12 @@ cudaError_t launch_verify_t(const VerifyArgs& a, int batch, int dev, int sms, cu
   // 65 us with four.
   int cs = 1;
   while (cs < VF_CLUSTER && a.V >= 4096ll * cs && (long long)batch * cs * 2 <= 8 * sms) cs *= 2;
-  static bool attr_done[PTENC_MAX_DEVICES] = {};
-  if (ptenc_first_use(attr_done, dev)) {
-    cudaError_t e = cudaFuncSetAttribute(k_verify_tree<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_verify_tree<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, VF_SMEM);
-    if (e != cudaSuccess) return e;
-  }
+  static PtencOnce once;
+  const cudaError_t e = ptenc_first_use(once, dev, [] {
+    const cudaError_t err = ptenc_allow_smem(k_verify_tree<T, true>, VF_SMEM);
+    return err != cudaSuccess ? err : ptenc_allow_smem(k_verify_tree<T, false>, VF_SMEM);
+  });
+  if (e != cudaSuccess) return e;
   return tree_launch(a.q != nullptr ? k_verify_tree<T, true> : k_verify_tree<T, false>, dim3((unsigned)batch * cs), VF_THREADS,
                      VF_SMEM, cs, st, a);
 }
