@@ -492,14 +492,16 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
 }
 
 // The staging of a chunk in front of the commit itself, 16 rows per CTA: one CTA per sequence would copy 129 rows of 512
-// columns in 18 us.  deferred[] receives the number of rows staged; paths that the commit refuses are left alone here.
+// columns in 18 us.  deferred[] receives the number of rows staged; paths that the commit refuses are left alone here.  `groups`
+// CTAs per sequence, all in the grid's first direction, since a chunk may have more groups than the second one has places.
 constexpr int CM_STAGE = 16;
 __global__ void __launch_bounds__(CM_THREADS)
 k_commit_stage(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, const __nv_bfloat16* __restrict__ v_tree, int NT,
                const int32_t* __restrict__ path, const int32_t* __restrict__ n_path, const uint8_t* __restrict__ active,
-               int32_t* __restrict__ deferred) {
+               int32_t* __restrict__ deferred, int groups) {
   __shared__ int s_path[TREE_MAX];
-  const int li = blockIdx.x / p.B, b = blockIdx.x - li * p.B, tid = threadIdx.x;
+  const int seq = blockIdx.x / groups, group = blockIdx.x - seq * groups;
+  const int li = seq / p.B, b = seq - li * p.B, tid = threadIdx.x;
   const size_t lb = (size_t)(l0 + li) * p.B + b, ob = (size_t)li * p.B + b;
   tree_after_previous();
   const int m = (active != nullptr && active[b] == 0) ? 0 : n_path[b];
@@ -512,8 +514,8 @@ k_commit_stage(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, con
   }
   bad = __syncthreads_or(bad);
   const int events = bad ? 0 : tree_evicted(rg.count, rg.cap, rg.e, m) / rg.e;
-  if (blockIdx.y == 0 && tid == 0) deferred[ob] = events > 0 ? rg.e : 0;
-  const int r0 = blockIdx.y * CM_STAGE;
+  if (group == 0 && tid == 0) deferred[ob] = events > 0 ? rg.e : 0;
+  const int r0 = group * CM_STAGE;
   if (events == 0 || r0 >= rg.e) return;
   cm_stage(p, lb, ob, rg, events, r0, min(r0 + CM_STAGE, rg.e), k_tree, v_tree, NT, s_path);
 }
@@ -569,8 +571,9 @@ cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tr
     cudaError_t e;
     if (chunks) {
       c->launches++;
-      e = tree_launch(k_commit_stage, dim3(nl * p.B, (p.E + CM_STAGE - 1) / CM_STAGE), CM_THREADS, 0, 0, st, p, l0,
-                      (const __nv_bfloat16*)k_tree, (const __nv_bfloat16*)v_tree, max_nodes, path, n_path, active, deferred);
+      const int groups = (p.E + CM_STAGE - 1) / CM_STAGE;          // nl B E < 2^31: the grid's size fits
+      e = tree_launch(k_commit_stage, dim3(nl * p.B * groups), CM_THREADS, 0, 0, st, p, l0, (const __nv_bfloat16*)k_tree,
+                      (const __nv_bfloat16*)v_tree, max_nodes, path, n_path, active, deferred, groups);
       if (e != cudaSuccess) return e;
     }
     if (p.r <= 32) e = launch_commit_bf16<1>(c, l0, nl, k_tree, v_tree, max_nodes, path, n_path, active, n_evicted_out, chunks, st);

@@ -514,6 +514,117 @@ def test_commit_equals_appends_and_encodes(dtype, E):
         x.close()
 
 
+def _staging(c):
+    """The staging area where the header's workspace layout puts it: evicted K and V rows [L, B, E, H_kv D], their number and the
+    first one's token index [L, B]; it ends where the states begin."""
+    f, ws = c.cfg, c.workspace
+    at, n = c.workspace_region(pt.binding.REGION_NPINNED)
+    off, views = at - ws.data_ptr() + n, []
+    dims = (f.n_layers, f.batch)
+    for shape, dtype in (((*dims, f.evict_chunk, f.n_kv_heads * f.head_dim), c.torch_dtype),) * 2 + ((dims, torch.int32), (dims, torch.int64)):
+        off = (off + 1023) // 1024 * 1024
+        size = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        views.append(ws[off:off + size].view(dtype).view(shape))
+        off += size
+    assert (off + 1023) // 1024 * 1024 == c.workspace_region(pt.binding.REGION_STATE)[0] - ws.data_ptr()
+    return views
+
+
+@pytest.mark.parametrize("dtype,E,B,norm", [("bf16", 1, 5, 0), ("bf16", 5, 5, 0), ("bf16", 16, 5, 0), ("bf16", 16, 4, 2), ("bf16", 29, 5, 0),
+                                            ("bf16", 29, 1, 0), ("bf16", 16, 5, 1), ("fp32", 1, 5, 0), ("fp32", 29, 5, 0)])
+def test_what_a_commit_leaves_staged(dtype, E, B, norm):
+    """Staged rows, their number and their first token after every commit, bit for bit what appending the same tokens one by one
+    leaves: the last arrival evicts in some sequences and not in others, and some evict in the middle of their path only."""
+    kw = dict(n_layers=2, batch=B, n_q_heads=4, n_kv_heads=2, head_dim=64, window=30, evict_chunk=E, dtype=dtype, seed=20,
+              n_global=32, rank=32, normalize_mode=norm)
+    a, b = Pair(pt, **kw), Pair(pt, **kw)
+    for x in (a, b):
+        _fill(x, 34, np.random.default_rng(2))
+    rng = np.random.default_rng(E)
+    T, seen = 9, set()
+    for turn in range(12):
+        _, k, v = _drafts(a, T, seed=turn)
+        n = rng.integers(0, T + 1, B)
+        path = np.tile(np.arange(T), (B, 1))
+        a.cache.commit_path(-1, k, v, _cuda(path), _cuda(n))
+        want = None
+        for j in range(T):
+            act = j < n
+            b.cache.append_evict(-1, k[:, :, j].contiguous(), v[:, :, j].contiguous(), _cuda(act, torch.uint8))
+            b.cache.encode(-1)
+            now = [t.clone() for t in _staging(b.cache)]
+            if want is None:
+                want = now
+            else:                                             # a sequence keeps what its own last arrival left
+                for w, x in zip(want, now):
+                    w[:, torch.as_tensor(act)] = x[:, torch.as_tensor(act)]
+        got = _staging(a.cache)
+        assert torch.equal(got[2], want[2]) and torch.equal(got[3], want[3])
+        for l in range(2):
+            for s in range(B):
+                m = int(want[2][l, s])
+                seen.add((m > 0, int(n[s]) > 0))
+                assert torch.equal(got[0][l, s, :m], want[0][l, s, :m]) and torch.equal(got[1][l, s, :m], want[1][l, s, :m])
+            for x, y in zip(a.cache.get_ring(l), b.cache.get_ring(l)):
+                assert torch.equal(x, y)
+            assert float((a.cache.get_state(l) - b.cache.get_state(l)).abs().max()) <= (2 * TOL_STATE if norm != 2 else 2 * TOL_STATE * max(1.0, float(b.cache.get_state(l).abs().max())))
+    assert B == 1 or seen >= {(True, True), (False, True), (False, False)}
+    assert a.cache.status() == 0 and b.cache.status() == 0
+    for x in (a, b):
+        x.close()
+
+
+def _fill_rings(c, gen):
+    """Full rings of random rows, the words of which say that the window's tokens came in order."""
+    f, ws = c.cfg, c.workspace
+    for region in (pt.binding.REGION_K, pt.binding.REGION_V):
+        at, n = c.workspace_region(region)
+        flat = ws[at - ws.data_ptr():at - ws.data_ptr() + n].view(c.torch_dtype)
+        for lo in range(0, flat.numel(), 1 << 30):
+            flat[lo:lo + (1 << 30)].normal_(generator=gen)
+    for region, dtype in ((pt.binding.REGION_COUNT, torch.int32), (pt.binding.REGION_NAPP, torch.int64)):
+        at, n = c.workspace_region(region)
+        ws[at - ws.data_ptr():at - ws.data_ptr() + n].view(dtype).fill_(f.window)
+
+
+def _commit_takes_the_whole_window(c, k, v):
+    """One token more than a full window of evict_chunk == window holds: everything leaves, oldest first, and is staged."""
+    f, b1 = c.cfg, dict(dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    _fill_rings(c, gen)
+    rows = torch.cat([torch.arange(0, f.window, max(1, f.window // 97)), torch.arange(f.window - 3, f.window)])
+    rings = [r[0, 0][:, rows].clone() for r in _rings(c)]      # [Hkv, rows, D]
+    evicted = torch.zeros(1, 1, **b1)
+    c.commit_path(-1, k, v, torch.zeros(1, 1, **b1), torch.ones(1, **b1), n_evicted_out=evicted)
+    assert evicted.tolist() == [[f.window]] and c.status() == 0
+    staged = _staging(c)
+    assert int(staged[2]) == f.window and int(staged[3]) == 0
+    for ring, stage in zip(rings, staged):
+        assert torch.equal(ring.transpose(0, 1).reshape(len(rows), -1), stage[0, 0, rows])
+    head, count, n_app = c.get_ring(0)
+    assert count.tolist() == [1] and n_app.tolist() == [f.window + 1]
+    for r, x in zip(_rings(c), (k, v)):
+        assert torch.equal(r[0, 0, :, int(head)], x[0, 0, 0])
+
+
+def test_commit_of_a_chunk_of_a_million_tokens():
+    """evict_chunk 1048577: more groups of sixteen rows than a grid has places in its second direction.  The state after it is
+    that of encoding the rows that were staged."""
+    W, D, r = (1 << 20) + 1, 64, 16
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    c = pt.Cache(pt.make_config(n_layers=1, batch=1, n_q_heads=1, n_kv_heads=1, head_dim=D, window=W, evict_chunk=W, n_global=16, rank=r))
+    bf = lambda *shape: torch.randn(*shape, generator=gen, device="cuda").to(torch.bfloat16)
+    c.set_encoder(0, bf(r, D), bf(r, D), bf(r, D), bf(16, D), bf(16, D), bf(16, D))
+    before = c.get_state(0).clone()
+    _commit_takes_the_whole_window(c, bf(1, 1, 1, 1, D), bf(1, 1, 1, 1, D))
+    after = c.get_state(0).clone()
+    at, n = c.workspace_region(pt.binding.REGION_STATE)
+    c.workspace[at - c.workspace.data_ptr():at - c.workspace.data_ptr() + n].view(torch.float32).view(before.shape).copy_(before)
+    c.encode(-1)                                               # the rows that the commit left staged
+    assert float((c.get_state(0) - after).abs().max()) <= 2 * TOL_STATE and not torch.equal(before, after)
+    c.close()
+
+
 def test_commit_without_encoder_and_bad_paths():
     p = Pair(pt, n_layers=1, batch=4, n_q_heads=4, n_kv_heads=2, head_dim=64, window=10, seed=11, set_encoder=False)
     _fill(p, 12)
