@@ -45,25 +45,28 @@ __device__ __forceinline__ void cm_stage(const PtencDev& p, size_t lb, size_t ob
   };
   // four vectors of K and of V per thread and turn, all requested before any is stored
   constexpr int U = 4;
-  const int total = r1 * vpr, o0 = (events - 1) * rg.e;
-  for (int i0 = r0 * vpr + tid; i0 < total; i0 += U * CM_THREADS) {
-    uint4 kv[U], vv[U];
+  for (int rb = r0; rb < r1; rb += PTENC_ROW_BLOCK) {
+    const int total = min(r1 - rb, PTENC_ROW_BLOCK) * vpr, o0 = (events - 1) * rg.e + rb;
+    const size_t to = (lb * p.E + rb) * vpr;               // rows of the staging area are Hkv D long
+    for (int i0 = tid; i0 < total; i0 += U * CM_THREADS) {
+      uint4 kv[U], vv[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + u * CM_THREADS, total - 1);
-      const int rr = i / vpr, v = i - rr * vpr, h = v / vph;
-      size_t ks, vs;
-      const T* kr = row(o0 + rr, p.K, k_tree, &ks);
-      const T* vr = row(o0 + rr, p.V, v_tree, &vs);
-      kv[u] = reinterpret_cast<const uint4*>(kr + h * ks)[v - h * vph];
-      vv[u] = reinterpret_cast<const uint4*>(vr + h * vs)[v - h * vph];
-    }
+      for (int u = 0; u < U; ++u) {
+        const int i = min(i0 + u * CM_THREADS, total - 1);
+        const int rr = i / vpr, v = i - rr * vpr, h = v / vph;
+        size_t ks, vs;
+        const T* kr = row(o0 + rr, p.K, k_tree, &ks);
+        const T* vr = row(o0 + rr, p.V, v_tree, &vs);
+        kv[u] = reinterpret_cast<const uint4*>(kr + h * ks)[v - h * vph];
+        vv[u] = reinterpret_cast<const uint4*>(vr + h * vs)[v - h * vph];
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * CM_THREADS;
-      if (i < total) {                                     // rows of the staging area are Hkv D long: row rr at rr * vpr
-        reinterpret_cast<uint4*>(p.stageK)[lb * p.E * vpr + i] = kv[u];
-        reinterpret_cast<uint4*>(p.stageV)[lb * p.E * vpr + i] = vv[u];
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * CM_THREADS;
+        if (i < total) {
+          reinterpret_cast<uint4*>(p.stageK)[to + i] = kv[u];
+          reinterpret_cast<uint4*>(p.stageV)[to + i] = vv[u];
+        }
       }
     }
   }

@@ -59,6 +59,11 @@ struct PtencDev {
   int* ev_slot;                 // [L][B][E] their slots
 };
 
+// Evicted rows are copied in blocks of this many, so that a block's 16-byte vectors can be counted in 32 bits: a row has at most
+// 8192 fp32 values, 2048 vectors, and a chunk up to 2^24 rows.
+constexpr int PTENC_ROW_BLOCK = 1 << 16;
+static_assert((long long)PTENC_ROW_BLOCK * 2048 <= (1ll << 30), "room for a thread's last step");
+
 constexpr int PTENC_LORA_MAX_PART = 16;   // most partial sums of B x per sequence (slices of d_in x parts of a slice)
 
 struct ptenc_cache {

@@ -51,19 +51,22 @@ k_append_evict(PtencDev p, int l0, const char* __restrict__ k_new, const char* _
     m = E;
     first = n - count;
     const int per_tok = Hkv * vpr;
-    const int total = m * per_tok;
-    for (int idx = tid; idx < total; idx += blockDim.x) {
-      const int i = idx / per_tok;
-      const int rem = idx - i * per_tok;
-      const int h = rem / vpr;
-      const int v = rem - h * vpr;
-      int slot = head + i;
-      if (slot >= cap) slot -= cap;
-      slot += ns;
-      const size_t src = (((size_t)lb * Hkv + h) * W + slot) * rb + (size_t)v * 16;
-      const size_t dst = (((size_t)lb * p.E + i) * Hkv + h) * rb + (size_t)v * 16;
-      *reinterpret_cast<uint4*>(p.stageK + dst) = *reinterpret_cast<const uint4*>(p.K + src);
-      *reinterpret_cast<uint4*>(p.stageV + dst) = *reinterpret_cast<const uint4*>(p.V + src);
+    for (int row0 = 0; row0 < m; row0 += PTENC_ROW_BLOCK) {
+      const int total = min(m - row0, PTENC_ROW_BLOCK) * per_tok;
+      for (int idx = tid; idx < total; idx += blockDim.x) {
+        const int rr = idx / per_tok;
+        const int rem = idx - rr * per_tok;
+        const int h = rem / vpr;
+        const int v = rem - h * vpr;
+        const int i = row0 + rr;
+        int slot = head + i;
+        if (slot >= cap) slot -= cap;
+        slot += ns;
+        const size_t src = (((size_t)lb * Hkv + h) * W + slot) * rb + (size_t)v * 16;
+        const size_t dst = (((size_t)lb * p.E + i) * Hkv + h) * rb + (size_t)v * 16;
+        *reinterpret_cast<uint4*>(p.stageK + dst) = *reinterpret_cast<const uint4*>(p.K + src);
+        *reinterpret_cast<uint4*>(p.stageV + dst) = *reinterpret_cast<const uint4*>(p.V + src);
+      }
     }
     head += E;
     if (head >= cap) head -= cap;

@@ -587,7 +587,7 @@ def _fill_rings(c, gen):
         ws[at - ws.data_ptr():at - ws.data_ptr() + n].view(dtype).fill_(f.window)
 
 
-def _commit_takes_the_whole_window(c, k, v):
+def _commit_takes_the_whole_window(c, k, v, append=False):
     """One token more than a full window of evict_chunk == window holds: everything leaves, oldest first, and is staged."""
     f, b1 = c.cfg, dict(dtype=torch.int32, device="cuda")
     gen = torch.Generator(device="cuda").manual_seed(5)
@@ -595,7 +595,10 @@ def _commit_takes_the_whole_window(c, k, v):
     rows = torch.cat([torch.arange(0, f.window, max(1, f.window // 97)), torch.arange(f.window - 3, f.window)])
     rings = [r[0, 0][:, rows].clone() for r in _rings(c)]      # [Hkv, rows, D]
     evicted = torch.zeros(1, 1, **b1)
-    c.commit_path(-1, k, v, torch.zeros(1, 1, **b1), torch.ones(1, **b1), n_evicted_out=evicted)
+    if append:
+        c.append_evict(-1, k[:, :, 0], v[:, :, 0], n_evicted_out=evicted)
+    else:
+        c.commit_path(-1, k, v, torch.zeros(1, 1, **b1), torch.ones(1, **b1), n_evicted_out=evicted)
     assert evicted.tolist() == [[f.window]] and c.status() == 0
     staged = _staging(c)
     assert int(staged[2]) == f.window and int(staged[3]) == 0
@@ -623,6 +626,35 @@ def test_commit_of_a_chunk_of_a_million_tokens():
     c.encode(-1)                                               # the rows that the commit left staged
     assert float((c.get_state(0) - after).abs().max()) <= 2 * TOL_STATE and not torch.equal(before, after)
     c.close()
+
+
+@pytest.mark.parametrize("dtype,E,D", [("fp32", 65536, 8), ("fp32", 65537, 8), ("bf16", 131079, 8), ("bf16", 65551, 64)])
+def test_chunks_of_more_rows_than_are_counted_together(dtype, E, D):
+    """Evicted rows are copied 65536 at a time: chunks of one block, one row more, and three; by an append alike."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    for append in (False, True):
+        c = pt.Cache(pt.make_config(n_layers=1, batch=1, n_q_heads=2, n_kv_heads=2, head_dim=D, window=E, evict_chunk=E, dtype=dtype,
+                                    encode_enabled=0))
+        k, v = (torch.randn(1, 1, 1, 2, D, generator=gen, device="cuda").to(c.torch_dtype) for _ in range(2))
+        _commit_takes_the_whole_window(c, k, v, append)
+        c.close()
+
+
+def test_commit_of_a_chunk_of_32_gigabytes():
+    """2^31 vectors of 16 bytes in one chunk: rings and staging area fill 137 GB."""
+    torch.cuda.empty_cache()
+    E = 1 << 20
+    cfg = pt.make_config(n_layers=1, batch=1, n_q_heads=32, n_kv_heads=32, head_dim=256, window=E, evict_chunk=E, dtype="fp32",
+                         encode_enabled=0)
+    if torch.cuda.mem_get_info()[0] < pt.ptenc_workspace_bytes(cfg) + (6 << 30):
+        pytest.skip("the device has no room for it")
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    c = pt.Cache(cfg)
+    k, v = (torch.randn(1, 1, 1, 32, 256, generator=gen, device="cuda") for _ in range(2))
+    _commit_takes_the_whole_window(c, k, v)
+    c.close()
+    del c
+    torch.cuda.empty_cache()
 
 
 def test_commit_without_encoder_and_bad_paths():
