@@ -120,6 +120,26 @@ def test_tree_attention_against_the_oracle(dtype, Hq, Hkv, D, W, E, T, prompt, s
     p.close()
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,W,E,T,prompt,steps,kind", [
+    ("bf16", 34, 2, 128, 150, 1, 9, 0, 160, "tree"),         # groups of 17: seven nodes to a row tile, rows left over
+    ("bf16", 40, 1, 64, 40, 8, 7, 0, 45, "tree"),            # of 40: three nodes to a row tile
+    ("bf16", 96, 2, 64, 130, 1, 6, 0, 140, "chain"),         # of 48: two
+    ("bf16", 65, 1, 128, 40, 1, 3, 4, 50, "tree"),           # of 65: one, half the rows of a tile empty
+    ("bf16", 100, 1, 128, 33, 1, 5, 0, 40, "star"),
+    ("bf16", 128, 1, 128, 20, 1, 64, 0, 25, "tree"),         # of 128, the widest: 32 blocks of rows
+    ("bf16", 128, 1, 64, 260, 60, 11, 9, 250, "tree"),
+    ("bf16", 129, 1, 64, 20, 1, 3, 0, 25, "tree"),           # wider: the shape-generic kernel
+    ("bf16", 8, 2, 96, 130, 1, 9, 0, 140, "tree"),           # head sizes that are no power of two
+    ("bf16", 6, 3, 200, 70, 9, 6, 3, 75, "chain"),
+    ("bf16", 4, 2, 256, 70, 1, 12, 0, 75, "tree"),
+    ("fp32", 8, 2, 96, 130, 1, 9, 0, 140, "tree"),
+    ("fp32", 3, 1, 136, 70, 9, 6, 3, 75, "forest"),
+    ("fp32", 40, 1, 40, 40, 1, 7, 0, 45, "tree"),
+])
+def test_tree_attention_of_wide_groups_and_odd_head_sizes(dtype, Hq, Hkv, D, W, E, T, prompt, steps, kind):
+    test_tree_attention_against_the_oracle(dtype, Hq, Hkv, D, W, E, T, prompt, steps, kind)
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("fp32", 64)])
 @pytest.mark.parametrize("E", [1, 24])
 def test_tree_attention_ragged(dtype, D, E):
@@ -746,6 +766,24 @@ def test_verify_against_the_oracle(dtype, B, T, V, kind):
         active = (rng.random(B) < 0.7).astype(np.uint8)
         _check_verify(p, q, tok, parent, u, n, active)
         _check_verify(p, None, tok, parent, u, n)
+
+
+def test_verify_where_the_clusters_shrink():
+    """Batches around those at which a sequence gets half as many CTAs on a device of 148 SMs: the same answers as sequence by
+    sequence, which has the most."""
+    rng = np.random.default_rng(6)
+    B, T, V = 593, 4, 33001
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    p, q = (torch.softmax(2.5 * torch.randn(B, T, V, generator=gen, device="cuda"), -1) for _ in range(2))
+    parent = np.tile([-1, 0, 0, 1], (B, 1))
+    tok, u = rng.integers(0, V, (B, T)), rng.random((B, T)).astype(np.float32)
+    tok[:, 1] = p[:, 0].argmax(-1).cpu().numpy()
+    for dq in (q, None):
+        one = [_run_verify(p[b:b + 1], None if dq is None else dq[b:b + 1], tok[b:b + 1], parent[b:b + 1], u[b:b + 1]) for b in range(B)]
+        for n in (74, 75, 148, 149, 296, 297, 592, 593):
+            got = _run_verify(p[:n], None if dq is None else dq[:n], tok[:n], parent[:n], u[:n])
+            for i, x in enumerate(got):
+                assert np.array_equal(x, np.concatenate([o[i] for o in one[:n]]))
 
 
 def test_verify_flat_rows_draw_the_right_neighbour():
