@@ -122,6 +122,7 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 
 int check_layer(const ptenc_cache* c, int layer, int* l0, int* nl) {
   if (c == nullptr) return PTENC_EINVAL;
+  ptenc_drop_old_error();
   if (layer == -1) { *l0 = 0; *nl = c->cfg.n_layers; return PTENC_OK; }
   if (layer < 0 || layer >= c->cfg.n_layers) return PTENC_EINVAL;
   *l0 = layer; *nl = 1;
@@ -211,6 +212,7 @@ int ptenc_cache_create(const ptenc_config* cfg, void* ws, size_t bytes, void* st
   const Layout lay = make_layout(cfg);
   if (bytes < lay.total) return PTENC_EWORKSPACE;
 
+  ptenc_drop_old_error();
   if (cudaSetDevice(cfg->device) != cudaSuccess) return PTENC_ECUDA;
   int sm_count = 0;
   if (cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess) return PTENC_ECUDA;
@@ -306,6 +308,7 @@ int ptenc_cache_destroy(ptenc_cache* c) {
 
 int ptenc_cache_reset(ptenc_cache* c, const uint8_t* seq_mask, void* stream) {
   if (c == nullptr) return PTENC_EINVAL;
+  ptenc_drop_old_error();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (seq_mask == nullptr) {
     // A launch that gave up part-way (a bounded wait ran out, the schedule did not add up) can leave arrival counts
@@ -323,6 +326,7 @@ int ptenc_set_encoder(ptenc_cache* c, int layer, const void* Wq_a, const void* W
   if (misaligned(Wq_a) || misaligned(Wk_a) || misaligned(Wv_a) || misaligned(q_g) || misaligned(k_g) ||
       misaligned(v_g))
     return PTENC_EALIGN;
+  ptenc_drop_old_error();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const PtencDev& d = c->dev;
   const size_t wbytes = (size_t)d.r * d.d_kv * d.elt;
@@ -625,6 +629,7 @@ int ptenc_get_scores(ptenc_cache* c, int layer, float* score_out, int32_t* token
   if (c == nullptr || layer < 0 || layer >= c->cfg.n_layers || score_out == nullptr || token_out == nullptr)
     return PTENC_EINVAL;
   if (c->cfg.policy != PTENC_POLICY_SCORE) return PTENC_EINVAL;
+  ptenc_drop_old_error();
   return ptenc_launch_export_scores(c, layer, score_out, token_out, static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? PTENC_OK : PTENC_ECUDA;
 }

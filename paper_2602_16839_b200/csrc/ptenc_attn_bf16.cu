@@ -1189,6 +1189,7 @@ extern "C" int ptenc_attn_rings_static(const ptenc_config* cfg, const void* K, c
     return PTENC_EALIGN;
 
   // Like every other entry point this one leaves the caller's current device alone: cfg->device has to be current.
+  ptenc_drop_old_error();
   int cur_dev = -1;
   if (cudaGetDevice(&cur_dev) != cudaSuccess) return PTENC_ECUDA;
   if (cur_dev != cfg->device) return PTENC_EINVAL;

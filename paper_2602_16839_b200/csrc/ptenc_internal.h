@@ -162,6 +162,11 @@ bool ptenc_attn_bf16_prepare(ptenc_cache* c, cudaError_t* err);
 // The instantiation a launch over `nl` layers would use: consumer warps, tokens per tile, pipeline stages.
 void ptenc_attn_bf16_plan(const ptenc_cache* c, int nl, int* consumer_warps, int* tile_tokens, int* stages);
 
+// The runtime keeps a failed call's error for whoever asks next, and launchers ask after their launch.  Every entry point that
+// launches drops what an earlier call has left, so that each reports its own failures: one that reported its predecessor's would
+// have run all the same, and a caller who repeats it would append twice.
+inline void ptenc_drop_old_error() { (void)cudaGetLastError(); }
+
 // Describing a tensor to the TMA unit is a driver call that wants a current context, and a host thread whose first CUDA call
 // this is has none: the runtime binds one when it is asked for something that needs it.  Encodes; if that fails, makes the
 // thread's current device's context current and encodes once more.

@@ -468,6 +468,7 @@ extern "C" int ptenc_verify_tree(const void* p, const void* q, int dtype, const 
   a.p = p; a.q = q; a.tokens = tokens; a.parent = parent; a.n_nodes = n_nodes; a.u = u; a.active = active;
   a.T = max_nodes; a.V = vocab; a.total = (long long)batch * max_nodes * vocab;
   a.path = path; a.n_path = n_path; a.next = next_token;
+  ptenc_drop_old_error();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int dev = -1, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
