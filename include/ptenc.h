@@ -26,11 +26,15 @@
  * - Return value: PTENC_OK or a negative error code.  Arguments are validated on the host before any
  *   launch; nothing is launched when an error is returned.  Device-side anomalies (a bounded wait that
  *   ran out, an index outside its range) never trap: they set a status word read by ptenc_cache_status.
- * - A handle may be used from one host thread and one stream at a time.  The device the cache was created on
+ * - A handle may be used from one host thread and one stream at a time, different handles from different threads at once.  The device the cache was created on
  *   (ptenc_config.device) must be the calling thread's current CUDA device when an entry point is called;
  *   ptenc_cache_create makes it current.
  * - Storage dtype (ptenc_config.dtype) applies to q, k, v, out, the rings and the encoder weights;
- *   the state S, the latent queries Q_a, lse and all accumulation are fp32.
+ *   the state S, the latent queries Q_a, lse and all accumulation are fp32.  The tensor-core attention kernels (bf16,
+ *   head_dim 64 or 128) take exp2 from the hardware approximation (relative error 2^-22, results below 2^-126
+ *   are zero) and round each softmax weight to bf16 for the product with V, the type of that product's operands;
+ *   the weights' sum is of the unrounded ones.  An output is then off by up to 2^-8 (|out| + max |V|), by about 2.3e-3 of its
+ *   size on ordinary data, of which rounding the output itself makes 1.7e-3.  Other shapes round the output alone.
  */
 #ifndef PTENC_H
 #define PTENC_H
@@ -215,7 +219,9 @@ PTENC_API int ptenc_tree_attn(ptenc_cache* c, int layer, const void* q, const vo
  *   cur = 0, r = p[0].  For i = 1 .. n_nodes-1 with parent[i] == cur, in this order: accepted when
  *   u[i] * q[cur][tokens[i]] < r[tokens[i]]: cur = i, r = p[i].  Otherwise r = max(r - q[cur], 0) / sum (r = p[cur] when
  *   nothing is left).  Then next_token = the first x with r[0] + .. + r[x] > u[0] * (sum of r).
- * The sequence of accepted tokens and next_token is distributed as if sampled from p token by token.  Evaluated in 64 bits.
+ * The sequence of accepted tokens and next_token is distributed as if sampled from p token by token, provided that the children
+ * of a node were drawn from its row of q independently of one another, the same token twice included, or are certain.  Children
+ * that were drawn to be distinct follow another law than q, and the result is then biased.  Evaluated in 64 bits.
  *   path [B, max_nodes] int32: node 0, the accepted nodes, then -1; n_path [B]: how many (1 + accepted); next_token [B].
  * These are what ptenc_commit_path takes.  Entries of p and q are finite and not negative; a row of p that sums to zero gives
  * next_token -1.  A sequence with n_nodes outside 1..max_nodes, a parent or a token out of range gets path -1, n_path 0,

@@ -120,7 +120,10 @@ __device__ __forceinline__ void cm_store(const PtencDev& p, size_t lb, size_t ob
   }
 }
 
-// Shape-generic kernel: a CTA per (layer, sequence), rows one after another.
+// Shape-generic kernel (fp32 storage, Frobenius norm, ranks or rows that k_commit_bf16 does not take): a CTA per (layer, sequence),
+// rows one after another, four block barriers and the weights read anew for each.  That chain is the bound: 28 layers x 32
+// sequences, paths of up to 8 tokens that each evict one, 203 us in fp32 (61 MB, 9 us of copy bandwidth) and 265 us in bf16
+// with the Frobenius norm; chunks of 129 rows in fp32 815 us.  The tiling of k_commit_bf16 has not been carried over to it.
 template <typename T>
 __global__ void __launch_bounds__(CM_THREADS)
 k_commit(PtencDev p, int l0, const T* __restrict__ k_tree, const T* __restrict__ v_tree, int NT,
@@ -465,7 +468,9 @@ k_commit_bf16(PtencDev p, int l0, const __nv_bfloat16* __restrict__ k_tree, cons
               float n2 = (right ? b : a) + __shfl_xor_sync(0xffffffffu, right ? a : b, 8);
 #pragma unroll
               for (int o = 4; o > 0; o >>= 1) n2 += __shfl_xor_sync(0xffffffffu, n2, o);
-              n2 = rsqrtf(fmaxf(n2, 1e-24f));              // 1 / max(|row|, 1e-12)
+              // 1 / max(|row|, 1e-12) by rsqrtf, within two units in the last place of the square root and division, which would
+              // sit in the chain between two events: a state after eight events is off by 6e-7 of its size
+              n2 = rsqrtf(fmaxf(n2, 1e-24f));
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
                 const float sc = __shfl_sync(0xffffffffu, n2, 8 * x);
@@ -568,7 +573,8 @@ cudaError_t ptenc_launch_commit(ptenc_cache* c, int l0, int nl, const void* k_tr
   const PtencDev& p = c->dev;
   if (c->cfg.dtype == PTENC_DTYPE_BF16 && p.r % 8 == 0 && p.d_kv % 32 == 0 && p.norm_mode != PTENC_NORM_FROBENIUS) {
     // Chunks of evicted tokens (E >= 16, a tile of the fold here) are folded by the chunk encoder, which reads them from the
-    // staging area: 192 sequences of which 40 % evict 129 rows 56 us by k_commit_bf16 alone, 29 us with the encoder.
+    // staging area: 192 sequences of which 40 % evict 129 rows 56 us by k_commit_bf16 alone, 29 us with the encoder.  The encoder
+    // loads boxes of up to 128 rows, which the staged rows of the call's layers have to be as many as.
     const bool chunks = p.E >= 16 && c->tc_encode && c->cfg.encode_enabled && (long long)nl * p.B * p.E >= 128;
     int32_t* deferred = c->commit_rows;
     cudaError_t e;

@@ -13,7 +13,9 @@
 //
 // Measured (fp32, head size 64, 16 sequences of 8 nodes, 4 heads over one ring of 1024 slots): 27 us, of which set-up takes 2, the
 // loads' way 4, each pair of a tile's scores and outputs 6, the join 3; 8.7 MB and 0.13 GFLOP would take 2.  With one set per CTA
-// 32 us.
+// 32 us.  Calls that read more are far from the copy bandwidth, because a CTA scores 32 rows however few there are and has one tile
+// of a set on its way: fp32, 36 sequences of 2 nodes, 28 heads over 4 rings of 1024 slots of 128 dims (153 MB) 156 us, 1.0 TB/s;
+// bf16, 32 sequences of 8 nodes, 16 heads over 4 rings of 2048 slots, 198 us at D = 96 (103 MB) and 515 us at D = 256 (274 MB).
 #include <cooperative_groups.h>
 #include <string.h>
 
@@ -344,7 +346,9 @@ cudaError_t launch_tree_j(ptenc_cache* c, int l0, int nl, const void* q, const v
   const PtencDev& p = c->dev;
   const int n_groups = (NT * p.g + TG_ROWS - 1) / TG_ROWS;
   const long long blocks = (long long)nl * p.B * p.Hkv * n_groups;
-  // Tokens over up to eight CTAs while that does not exceed two CTAs per SM and each still has a tile of 64.
+  // Tokens over up to eight CTAs while that does not exceed two CTAs per SM and each still has a tile of 64.  Two CTAs fit an SM
+  // where they take up to 113 KB and 128 registers each (fp32 at D <= 64, bf16 at D <= 128); of the larger ones one fits, and
+  // such a call may be split into two rounds.
   int cs = 1;
   while (cs < TG_CLUSTER && blocks * cs * 2 <= 2 * c->sm_count && cs * 2 * TG_TOK <= p.W) cs *= 2;
   if (blocks * cs > 0x7fffffffll) return cudaErrorInvalidValue;

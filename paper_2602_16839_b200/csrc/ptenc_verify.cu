@@ -432,8 +432,9 @@ k_verify_tree(const VerifyArgs a) {
 template <typename T>
 cudaError_t launch_verify_t(const VerifyArgs& a, int batch, int dev, int sms, cudaStream_t st) {
   // A row over up to eight CTAs: a CTA's share should be worth its start, 2048 entries at least, and the batch should not
-  // need more than two rounds of the eight CTAs that an SM holds.  128 rows of 152000 entries: 53 us with eight CTAs each,
-  // 65 us with four.
+  // need more than two rounds of the four CTAs that an SM holds (64 registers x 256 threads).  128 rows of 152000 entries: 53 us
+  // with eight CTAs each (1.7 rounds), 65 us with four.  The rule steps at whole rounds: 149 sequences on 148 SMs get four CTAs
+  // each, which is one round and four CTAs.
   int cs = 1;
   while (cs < VF_CLUSTER && a.V >= 4096ll * cs && (long long)batch * cs * 2 <= 8 * sms) cs *= 2;
   static PtencOnce once;
