@@ -244,6 +244,114 @@ PTENC_API int ptenc_commit_path(ptenc_cache* c, int layer, const void* k_tree, c
                                 const int32_t* path, const int32_t* n_path, const uint8_t* active,
                                 int32_t* n_evicted_out, void* stream);
 
+/* A training pass over rollouts (the policy update of Sec. 3.1 and 3.2): every token of the rollouts goes through the model once
+ * more, all at the same time, seeing what the cache let it see when it was decoded, and the loss is the clipped ratio of the two
+ * policies with a KL term.  The calls below are what such a pass needs of this library beside dense products: the norms of
+ * queries and keys with the position rotation (which a prompt and a decode step need too), attention over whole sequences, and
+ * the loss.  They take no handle; the tensors' device is to be the calling thread's current one.  Tokens of all sequences lie
+ * packed one after another; a token's rows [heads, head_dim] are contiguous, and `*_stride` counts elements from one token to the
+ * next (a slice of a fused projection has a stride above heads * head_dim): at least heads * head_dim, a multiple of 16 bytes,
+ * PTENC_EALIGN otherwise.  Data pointers are 16-byte aligned unless noted.  head_dim is a multiple of 8 up to 256, n_q_heads a
+ * multiple of n_kv_heads, at most 16384 heads, n_tokens below 2^31 - 512 (PTENC_ESHAPE).  n_tokens == 0 is allowed.  The inputs
+ * are not changed; outputs overlap neither inputs nor one another, except where a call says so. */
+
+typedef struct {
+  int32_t dtype;           /* PTENC_DTYPE_* of queries, keys, weights and their gradients                  */
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t rotary_dim;      /* the first rotary_dim values of a head are rotated: even, 0..head_dim         */
+  int32_t interleaved;     /* 0: value i is paired with value i + rotary_dim / 2; 1: 2i with 2i + 1        */
+  float eps;               /* added to the mean square, >= 0                                               */
+} ptenc_rope_config;
+
+/* Norm of every query and key head and its rotation by the token's position, in one pass:
+ *   y = w * x / sqrt(mean(x^2) + eps)  (y = x where the weight is NULL),  then each pair (a, b) of y turns by
+ *   angle = positions[t] * inv_freq[i]:  (a cos - b sin, b cos + a sin).
+ * The angle is taken in 64 bits, so positions may be far; everything else is fp32, rounded once at the end.  q [n, H_q, D],
+ * k [n, H_kv, D]; q_weight, k_weight [D] in the storage dtype, nullable each; positions [n] int32; inv_freq [rotary_dim / 2] fp32.
+ * q_out may be q and k_out k, with equal strides.  For a decode step n is the batch, q_out and k_out go on to ptenc_decode_step. */
+PTENC_API int ptenc_head_norm_rope(const ptenc_rope_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
+                                   int64_t k_stride, const void* q_weight, const void* k_weight,
+                                   const int32_t* positions, const float* inv_freq, int64_t n_tokens, void* q_out,
+                                   int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/* Gradients of ptenc_head_norm_rope: from dq_out, dk_out (those of its outputs) to dq, dk (dq may be dq_out and dk dk_out, with
+ * equal strides), and dq_weight, dk_weight [D] fp32, summed over tokens and heads in a fixed order.  q and k are the inputs of
+ * the forward call; they are not read for a side whose weight is NULL.  A weight's gradient is wanted where its weight is given
+ * (PTENC_EINVAL where one of the two is missing).  workspace: device, ptenc_head_norm_rope_workspace_bytes, needed with weights
+ * only; its contents do not outlive the call, and calls that share one do not overlap on the GPU. */
+PTENC_API int ptenc_head_norm_rope_workspace_bytes(int32_t head_dim, size_t* bytes /*host, out*/);
+PTENC_API int ptenc_head_norm_rope_backward(const ptenc_rope_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
+                                            int64_t k_stride, const void* q_weight, const void* k_weight,
+                                            const int32_t* positions, const float* inv_freq, int64_t n_tokens,
+                                            const void* dq_out, int64_t dq_out_stride, const void* dk_out,
+                                            int64_t dk_out_stride, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+                                            float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                                            void* stream);
+
+typedef struct {
+  int32_t dtype;           /* PTENC_DTYPE_* of q, k, v, out and their gradients                            */
+  int32_t n_q_heads, n_kv_heads, head_dim;
+  int32_t window;          /* the cache budget W a token was decoded under; 0: no limit                    */
+  int32_t evict_chunk;     /* E, 1..W; read only with a window                                             */
+  float scale;             /* of the scores, > 0; 0: 1 / sqrt(head_dim)                                    */
+} ptenc_seq_config;
+
+/* Attention over whole sequences, causal: out[t,h,:] = softmax(scale * q[t,h,:] . K^T) V over the tokens that token t sees of
+ * its own sequence, KV head floor(h / (H_q/H_kv)).  Sequence b is the rows cu_seqlens[b] .. cu_seqlens[b+1] - 1 of the packed
+ * tensors (device int32 [batch + 1], not decreasing; empty ones are allowed).  Without a window token i of a sequence sees the
+ * tokens 0..i: a prompt before its first decode step.  With one it sees what ptenc_decode_attn would see had the first
+ * n_pinned[b] tokens been pinned by ptenc_prefill and the others been appended one by one to a cache of window W and chunk E
+ * under PTENC_POLICY_FIFO: the pinned tokens up to i and, with C = W - n_pinned[b] and e = min(E, C), from the sliding tokens up to
+ * i those that are not among the e * ceil(max(0, i - n_pinned[b] + 1 - C) / e) oldest.  n_pinned: device int32 [batch], NULL = none;
+ * not read without a window.
+ *   q, out [n, H_q, D]; k, v [n, H_kv, D]; out is contiguous; lse_out [n, H_q] fp32, nullable: the natural logarithm of the sum
+ * of exp of the scaled scores, which the backward call wants.  What a token does not see does not reach its rows, whatever it holds
+ * (NaN and infinities included).  Rows of no sequence are neither read for an answer nor written.  A sequence whose bounds or
+ * n_pinned (0 <= n_pinned < W) are out of range is left alone.  No workspace. */
+PTENC_API int ptenc_seq_attn(const ptenc_seq_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* v, int64_t v_stride, const int32_t* cu_seqlens,
+                             const int32_t* n_pinned, int32_t batch, int64_t n_tokens, void* out, float* lse_out,
+                             void* stream);
+
+/* Gradients of ptenc_seq_attn with respect to q, k and v, from dout [n, H_q, D] (contiguous, like out), the forward call's inputs,
+ * out and lse.  The heads that share a KV head are summed in fp32, in a fixed order: repeated calls give the same bits.
+ * workspace: device, 16-byte aligned, ptenc_seq_attn_workspace_bytes; its contents do not outlive the call, and calls that share
+ * one do not overlap on the GPU. */
+PTENC_API int ptenc_seq_attn_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, size_t* bytes /*host, out*/);
+PTENC_API int ptenc_seq_attn_backward(const ptenc_seq_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
+                                      int64_t k_stride, const void* v, int64_t v_stride, const void* out, const float* lse,
+                                      const void* dout, const int32_t* cu_seqlens, const int32_t* n_pinned, int32_t batch,
+                                      int64_t n_tokens, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, void* dv,
+                                      int64_t dv_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int32_t dtype;           /* PTENC_DTYPE_* of the logits and their gradient                               */
+  int32_t vocab;           /* V, up to 2^28                                                                */
+  float temperature;       /* > 0: the policy is softmax(logits / temperature)                             */
+  float clip_low, clip_high; /* the ratio is clipped to [1 - clip_low, 1 + clip_high], both >= 0           */
+  float kl_coef;           /* of the KL term, >= 0; not read without ref_logp                              */
+} ptenc_policy_config;
+
+/* The clipped policy loss with a KL term, from the logits to their gradient (Sec. 3.1, the GRPO objective, per token).  For token t with
+ * weight[t] != 0 and tokens[t] in [0, vocab):
+ *   lp = log softmax(logits[t] / temperature)[tokens[t]],  r = exp(lp - old_logp[t])  (old_logp NULL: r = 1, as on the policy that
+ *   sampled the token; the gradient still flows through lp),
+ *   loss_t = -min(r A, clip(r) A) + kl_coef (exp(ref_logp[t] - lp) - (ref_logp[t] - lp) - 1),  A = advantage[t],
+ *   loss = sum over t of weight[t] loss_t,  dlogits[t] = weight[t] (d loss_t / d lp) (onehot - softmax) / temperature,
+ * where a ratio beyond the clip border on the side that A favours has no gradient of the first term.  Other tokens: their logits
+ * are not read (whatever they hold), logp, token_loss and token_kl are 0 and the row of dlogits is zero.
+ *   logits, dlogits [n, vocab] with strides of at least vocab elements, the pointers 16-byte aligned, the rows need not be; dlogits
+ * may be logits (then the strides are equal), or NULL: no gradient.  tokens [n] int32; old_logp, ref_logp, advantage, weight [n]
+ * fp32; old_logp, ref_logp, weight (NULL = 1) nullable.  advantage NULL: only logp is wanted (the log-probabilities of the policy
+ * that samples, or of the reference), and everything but tokens, weight and logp is to be NULL.  Outputs logp [n], token_loss
+ * [n] (the loss_t; required with loss), token_kl [n] (the KL estimate without kl_coef; 0 without ref_logp), loss [1], all fp32,
+ * token_loss, token_kl and loss nullable.  Sums over the vocabulary are fp32, what follows from them per token is 64 bits, the sum
+ * over tokens 64 bits in a fixed order.  logits of -inf have no probability.  No workspace. */
+PTENC_API int ptenc_policy_loss(const ptenc_policy_config* cfg /*host*/, const void* logits, int64_t logits_stride,
+                                const int32_t* tokens, const float* old_logp, const float* ref_logp, const float* advantage,
+                                const float* weight, int64_t n_tokens, float* logp, float* token_loss, float* token_kl,
+                                float* loss, void* dlogits, int64_t dlogits_stride, void* stream);
+
 /* a4 with HOST buffers: the same step as ptenc_decode_step, with q, k_new, v_new, active read from host
  * memory and out written to host memory.  The call enqueues the host-to-device copies into `dev_staging`
  * (device, 256-byte aligned, at least ptenc_host_staging_bytes), the step, and the device-to-host copy of out,

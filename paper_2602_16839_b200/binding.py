@@ -28,7 +28,9 @@ EXPORTS = ["ptenc_workspace_bytes", "ptenc_cache_create", "ptenc_cache_destroy",
            "ptenc_host_staging_bytes", "ptenc_decode_step_host",
            "ptenc_get_ring", "ptenc_get_state", "ptenc_get_evicted", "ptenc_get_scores", "ptenc_cache_status", "ptenc_cache_info", "ptenc_attn_launch_info",
            "ptenc_workspace_region", "ptenc_time_next_attn", "ptenc_attn_rings_static", "ptenc_launch_count",
-           "ptenc_tree_attn", "ptenc_verify_tree", "ptenc_commit_path", "ptenc_strerror"]
+           "ptenc_tree_attn", "ptenc_verify_tree", "ptenc_commit_path", "ptenc_strerror",
+           "ptenc_head_norm_rope", "ptenc_head_norm_rope_workspace_bytes", "ptenc_head_norm_rope_backward", "ptenc_seq_attn",
+           "ptenc_seq_attn_workspace_bytes", "ptenc_seq_attn_backward", "ptenc_policy_loss"]
 MAX_TREE = 64
 
 
@@ -36,6 +38,21 @@ class PtencConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "n_layers", "batch", "n_q_heads", "n_kv_heads", "head_dim", "window", "evict_chunk", "n_global",
         "rank", "dtype", "normalize_mode", "encode_enabled", "device", "attn_consumer_warps", "policy", "recent")]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "interleaved")] + [
+        ("eps", ctypes.c_float)]
+
+
+class SeqConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "window", "evict_chunk")] + [
+        ("scale", ctypes.c_float)]
+
+
+class PolicyConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "vocab")] + [
+        (n, ctypes.c_float) for n in ("temperature", "clip_low", "clip_high", "kl_coef")]
 
 
 class PtencError(RuntimeError):
@@ -80,6 +97,16 @@ def _load() -> ctypes.CDLL:
     lib.ptenc_verify_tree.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                       vp, vp, vp, vp]
     lib.ptenc_commit_path.argtypes = [vp, i32, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp]
+    i64 = ctypes.c_int64
+    lib.ptenc_head_norm_rope.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    lib.ptenc_head_norm_rope_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(u64)]
+    lib.ptenc_head_norm_rope_backward.argtypes = [ctypes.POINTER(RopeConfig), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp,
+                                                  i64, vp, i64, vp, i64, vp, vp, vp, u64, vp]
+    lib.ptenc_seq_attn.argtypes = [ctypes.POINTER(SeqConfig), vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_int32, i64, vp, vp, vp]
+    lib.ptenc_seq_attn_workspace_bytes.argtypes = [i64, ctypes.c_int32, ctypes.POINTER(u64)]
+    lib.ptenc_seq_attn_backward.argtypes = [ctypes.POINTER(SeqConfig), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp,
+                                            ctypes.c_int32, i64, vp, i64, vp, i64, vp, i64, vp, u64, vp]
+    lib.ptenc_policy_loss.argtypes = [ctypes.POINTER(PolicyConfig), vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, i64, vp]
     lib.ptenc_launch_count.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
     lib.ptenc_strerror.argtypes = [i32]
     lib.ptenc_strerror.restype = ctypes.c_char_p
@@ -178,6 +205,184 @@ def verify_tree(p, q, tokens, parent, u, path, n_path, next_token, n_nodes=None,
                                path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _stream_of(dev))
     if rc != PTENC_OK:
         raise PtencError(rc, where)
+
+
+def _device_of(where, t) -> int:
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise PtencError(PTENC_EINVAL, f"{where}: the tensors' device is to be the current CUDA device")
+    return dev
+
+
+def _rows(where, name, t, shape, dtype, device) -> int:
+    """Stride from token to token of a [n, heads, D] tensor whose rows are contiguous; refuses others."""
+    if t.dtype != dtype or t.device != device:
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a {dtype} tensor on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise PtencError(PTENC_ESHAPE, f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    n, h, d = shape
+    s0, s1, s2 = t.stride()
+    if n == 0 or h * d == 0:
+        return h * d
+    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to have contiguous [heads, D] rows")
+    return s0 if n > 1 else max(h * d, 8)
+
+
+def _storage(where, t, name):
+    if t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16):
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a [n, heads, D] tensor of fp32 or bf16")
+    return DTYPE_BF16 if t.dtype is torch.bfloat16 else DTYPE_FP32
+
+
+def _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved):
+    dt = _storage(where, q, "q")
+    n, Hq, D = q.shape
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    dev = q.device
+    sq, sk = _rows(where, "q", q, (n, Hq, D), q.dtype, dev), _rows(where, "k", k, (n, Hkv, D), q.dtype, dev)
+    half = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
+    _want(where, dev, ("positions", positions, (n,), torch.int32), ("inv_freq", inv_freq, (half,), torch.float32),
+          ("q_weight", q_weight, (D,), q.dtype), ("k_weight", k_weight, (D,), q.dtype))
+    return RopeConfig(dt, Hq, Hkv, D, 2 * half, 1 if interleaved else 0, eps), n, sq, sk
+
+
+def head_norm_rope(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+    """ptenc_head_norm_rope: norms of query and key heads (weights [D], None = no norm) and the rotation by position.  q, q_out
+    [n, Hq, D], k, k_out [n, Hkv, D] with contiguous rows and any token stride; positions [n] int32; inv_freq [rotary_dim / 2] fp32.
+    q_out may be q and k_out k."""
+    where = "ptenc_head_norm_rope"
+    cfg, n, sq, sk = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    so, sp = _rows(where, "q_out", q_out, q.shape, q.dtype, q.device), _rows(where, "k_out", k_out, k.shape, q.dtype, q.device)
+    dev = _device_of(where, q)
+    rc = lib.ptenc_head_norm_rope(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
+                                  positions.data_ptr(), inv_freq.data_ptr(), n, q_out.data_ptr(), so, k_out.data_ptr(), sp,
+                                  _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
+
+
+def head_norm_rope_workspace_bytes(head_dim) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.ptenc_head_norm_rope_workspace_bytes(head_dim, ctypes.byref(n)), "ptenc_head_norm_rope_workspace_bytes")
+    return int(n.value)
+
+
+def _workspace(where, ws, device):
+    if ws is None:
+        return 0
+    if not ws.is_contiguous() or ws.device != device:
+        raise PtencError(PTENC_EINVAL, f"{where}: workspace is to be a contiguous tensor on {device}")
+    return ws.numel() * ws.element_size()
+
+
+def head_norm_rope_backward(q, k, dq_out, dk_out, positions, inv_freq, dq, dk, q_weight=None, k_weight=None, dq_weight=None,
+                            dk_weight=None, workspace=None, eps=1e-6, interleaved=False):
+    """ptenc_head_norm_rope_backward: gradients dq, dk of the inputs and dq_weight, dk_weight [D] fp32 of the weights, from those of
+    the outputs.  dq may be dq_out and dk dk_out.  workspace (with weights): head_norm_rope_workspace_bytes(D) bytes."""
+    where = "ptenc_head_norm_rope_backward"
+    cfg, n, sq, sk = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    st = [_rows(where, name, t, like.shape, q.dtype, q.device) for name, t, like in
+          (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k))]
+    D = (q.shape[2],)
+    _want(where, q.device, ("dq_weight", dq_weight, D, torch.float32), ("dk_weight", dk_weight, D, torch.float32))
+    size = _workspace(where, workspace, q.device)
+    dev = _device_of(where, q)
+    rc = lib.ptenc_head_norm_rope_backward(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
+                                           positions.data_ptr(), inv_freq.data_ptr(), n, dq_out.data_ptr(), st[0],
+                                           dk_out.data_ptr(), st[1], dq.data_ptr(), st[2], dk.data_ptr(), st[3],
+                                           _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace), size, _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
+
+
+def _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale):
+    dt = _storage(where, q, "q")
+    n, Hq, D = q.shape
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    st = [_rows(where, name, t, (n, h, D), q.dtype, q.device) for name, t, h in (("q", q, Hq), ("k", k, Hkv), ("v", v, Hkv))]
+    batch = cu_seqlens.shape[0] - 1 if cu_seqlens.dim() == 1 else -1
+    _want(where, q.device, ("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32), ("n_pinned", n_pinned, (batch,), torch.int32))
+    return SeqConfig(dt, Hq, Hkv, D, window, evict_chunk, 0.0 if scale is None else scale), n, batch, st
+
+
+def seq_attn(q, k, v, cu_seqlens, out, lse_out=None, n_pinned=None, window=0, evict_chunk=1, scale=None):
+    """ptenc_seq_attn: causal attention over packed sequences; with a window, what a cache of that window let each token see.
+    q [n, Hq, D], k, v [n, Hkv, D] with contiguous rows and any token stride; cu_seqlens [B + 1], n_pinned [B] int32; out
+    [n, Hq, D], lse_out [n, Hq] fp32 contiguous."""
+    where = "ptenc_seq_attn"
+    cfg, n, batch, (sq, sk, sv) = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
+    _want(where, q.device, ("out", out, q.shape, q.dtype), ("lse_out", lse_out, q.shape[:2], torch.float32))
+    dev = _device_of(where, q)
+    rc = lib.ptenc_seq_attn(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, cu_seqlens.data_ptr(),
+                            _ptr(n_pinned), batch, n, out.data_ptr(), _ptr(lse_out), _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
+
+
+def seq_attn_workspace_bytes(n_tokens, n_q_heads) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.ptenc_seq_attn_workspace_bytes(n_tokens, n_q_heads, ctypes.byref(n)), "ptenc_seq_attn_workspace_bytes")
+    return int(n.value)
+
+
+def seq_attn_backward(q, k, v, out, lse, dout, cu_seqlens, dq, dk, dv, workspace, n_pinned=None, window=0, evict_chunk=1,
+                      scale=None):
+    """ptenc_seq_attn_backward: dq, dk, dv (contiguous rows, any token stride) from dout and the forward call's inputs, out and
+    lse.  workspace: seq_attn_workspace_bytes(n, Hq) bytes."""
+    where = "ptenc_seq_attn_backward"
+    cfg, n, batch, (sq, sk, sv) = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
+    _want(where, q.device, ("out", out, q.shape, q.dtype), ("lse", lse, q.shape[:2], torch.float32),
+          ("dout", dout, q.shape, q.dtype))
+    gq, gk, gv = (_rows(where, name, t, like.shape, q.dtype, q.device) for name, t, like in
+                  (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    size = _workspace(where, workspace, q.device)
+    dev = _device_of(where, q)
+    rc = lib.ptenc_seq_attn_backward(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(),
+                                     lse.data_ptr(), dout.data_ptr(), cu_seqlens.data_ptr(), _ptr(n_pinned), batch, n,
+                                     dq.data_ptr(), gq, dk.data_ptr(), gk, dv.data_ptr(), gv, _ptr(workspace), size,
+                                     _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
+
+
+def _logit_rows(where, name, t, shape, dtype, device) -> int:
+    if t.dtype != dtype or t.device != device:
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a {dtype} tensor on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise PtencError(PTENC_ESHAPE, f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if shape[1] > 1 and shape[0] > 0 and t.stride(1) != 1:
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to have contiguous rows")
+    return t.stride(0) if shape[0] > 1 else max(1, shape[1])
+
+
+def policy_loss(logits, tokens, advantage, logp, token_loss=None, loss=None, dlogits=None, old_logp=None, ref_logp=None,
+                weight=None, token_kl=None, temperature=1.0, clip_low=0.2, clip_high=0.2, kl_coef=0.0):
+    """ptenc_policy_loss: the clipped policy loss with a KL term and the gradient of the logits.  logits, dlogits [n, V] fp32 or
+    bf16 (dlogits may be logits); tokens [n] int32; advantage, old_logp, ref_logp, weight, logp, token_loss, token_kl [n] and
+    loss [1] fp32.  advantage None: only logp."""
+    where = "ptenc_policy_loss"
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise PtencError(PTENC_EINVAL, f"{where}: logits is to be a [n, V] tensor of fp32 or bf16")
+    n, V = logits.shape
+    device, f32, row = logits.device, torch.float32, (n,)
+    s_in = _logit_rows(where, "logits", logits, (n, V), logits.dtype, device)
+    s_out = 0 if dlogits is None else _logit_rows(where, "dlogits", dlogits, (n, V), logits.dtype, device)
+    _want(where, device, ("tokens", tokens, row, torch.int32), ("advantage", advantage, row, f32), ("old_logp", old_logp, row, f32),
+          ("ref_logp", ref_logp, row, f32), ("weight", weight, row, f32), ("logp", logp, row, f32),
+          ("token_loss", token_loss, row, f32), ("token_kl", token_kl, row, f32), ("loss", loss, (1,), f32))
+    dev = _device_of(where, logits)
+    cfg = PolicyConfig(DTYPE_BF16 if logits.dtype is torch.bfloat16 else DTYPE_FP32, V, temperature, clip_low, clip_high, kl_coef)
+    rc = lib.ptenc_policy_loss(ctypes.byref(cfg), logits.data_ptr(), s_in, tokens.data_ptr(), _ptr(old_logp), _ptr(ref_logp),
+                               _ptr(advantage), _ptr(weight), n, logp.data_ptr(), _ptr(token_loss), _ptr(token_kl), _ptr(loss),
+                               _ptr(dlogits), s_out, _stream_of(dev))
+    if rc != PTENC_OK:
+        raise PtencError(rc, where)
+
+
+def token_logp(logits, tokens, logp, weight=None, temperature=1.0):
+    """Log-probabilities of tokens [n] under softmax(logits / temperature), logits [n, V]: ptenc_policy_loss without a loss."""
+    policy_loss(logits, tokens, None, logp, weight=weight, temperature=temperature)
 
 
 class Cache:
