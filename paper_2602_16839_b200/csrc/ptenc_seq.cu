@@ -468,7 +468,10 @@ extern "C" int ptenc_seq_attn(const ptenc_seq_config* cfg, const void* q, int64_
   ptenc_drop_old_error();
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) return PTENC_ECUDA;
-  return seq_forward_any(a, cfg->dtype, dev, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (!seq_forward_tc(a, cfg->dtype, dev, st, &e)) e = seq_forward_any(a, cfg->dtype, dev, st);
+  return e == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
 }
 
 extern "C" int ptenc_seq_attn_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, size_t* bytes) {

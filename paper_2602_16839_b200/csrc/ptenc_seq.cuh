@@ -89,3 +89,5 @@ __device__ __forceinline__ bool seq_all(const SeqView& s, int i0, int i1, int j0
 
 cudaError_t seq_forward_any(const SeqArgs& a, int dtype, int dev, cudaStream_t st);
 cudaError_t seq_backward_any(const SeqArgs& a, int dtype, int dev, cudaStream_t st);
+// The tensor-core kernels; false: they do not cover the call.
+bool seq_forward_tc(const SeqArgs& a, int dtype, int dev, cudaStream_t st, cudaError_t* e);
