@@ -12,10 +12,10 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libptenc.so")
 SOURCES = ["ptenc_api.cu", "ptenc_ring.cu", "ptenc_score.cu", "ptenc_encode.cu", "ptenc_encode_tc.cu", "ptenc_step_e1.cu", "ptenc_lora.cu", "ptenc_attn_generic.cu", "ptenc_attn_bf16.cu",
            "ptenc_tree_tc.cu", "ptenc_tree_generic.cu", "ptenc_commit.cu", "ptenc_verify.cu", "ptenc_rope.cu",
-           "ptenc_seq.cu", "ptenc_seq_tc.cu", "ptenc_policy.cu"]
+           "ptenc_seq.cu", "ptenc_seq_tc.cu", "ptenc_seq_bwd_tc.cu", "ptenc_policy.cu"]
 HEADERS = [os.path.join(CSRC, "ptenc_internal.h"), os.path.join(CSRC, "ptenc_once.h"), os.path.join(CSRC, "ptenc_encode_warp.cuh"),
            os.path.join(CSRC, "ptenc_tree.cuh"), os.path.join(CSRC, "ptenc_seq.cuh"),
-           os.path.join(CSRC, "ptenc_tc.cuh"), os.path.join(ROOT, "include", "ptenc.h")]
+           os.path.join(CSRC, "ptenc_tc.cuh"), os.path.join(CSRC, "ptenc_seq_tc.cuh"), os.path.join(ROOT, "include", "ptenc.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
 

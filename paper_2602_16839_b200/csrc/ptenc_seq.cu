@@ -477,7 +477,7 @@ extern "C" int ptenc_seq_attn(const ptenc_seq_config* cfg, const void* q, int64_
 extern "C" int ptenc_seq_attn_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, size_t* bytes) {
   if (bytes == nullptr || n_tokens < 0 || n_q_heads < 1) return PTENC_EINVAL;
   if (n_tokens >= (1ll << 31) - 512 || n_q_heads > 16384) return PTENC_ESHAPE;
-  *bytes = (size_t)n_tokens * n_q_heads * sizeof(float);
+  *bytes = (size_t)n_tokens * n_q_heads * 2 * sizeof(float);
   return PTENC_OK;
 }
 
@@ -511,5 +511,8 @@ extern "C" int ptenc_seq_attn_backward(const ptenc_seq_config* cfg, const void* 
   ptenc_drop_old_error();
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) return PTENC_ECUDA;
-  return seq_backward_any(a, cfg->dtype, dev, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (!seq_backward_tc(a, cfg->dtype, dev, st, &e)) e = seq_backward_any(a, cfg->dtype, dev, st);
+  return e == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
 }

@@ -21,7 +21,7 @@ struct SeqArgs {
   void* dk;
   void* dv;
   long long dqs, dks, dvs;
-  float* delta;                    // backward: [n][Hq] sums of dout * out
+  float* delta;                    // backward scratch, 2 n Hq: sums of dout * out (and lse, in the tensor-core kernels)
 };
 
 // A sequence as its tiles see it.  Token i sees j <= i with j < pin or j >= low(i); token j is seen by i >= j with i <= last(j).
@@ -91,3 +91,4 @@ cudaError_t seq_forward_any(const SeqArgs& a, int dtype, int dev, cudaStream_t s
 cudaError_t seq_backward_any(const SeqArgs& a, int dtype, int dev, cudaStream_t st);
 // The tensor-core kernels; false: they do not cover the call.
 bool seq_forward_tc(const SeqArgs& a, int dtype, int dev, cudaStream_t st, cudaError_t* e);
+bool seq_backward_tc(const SeqArgs& a, int dtype, int dev, cudaStream_t st, cudaError_t* e);

@@ -1,0 +1,738 @@
+// Gradients of attention over whole sequences on the sm_100a tensor cores (bf16, head sizes up to 128).
+//
+//   S = Q K^T, dP = dO V^T, P = exp(scale S - lse), dS = P (dP - delta), delta = rowsum(dO * O);
+//   dQ = scale dS K,  dV = P^T dO,  dK = scale dS^T Q.
+// Two kernels, one per side: k_seq_dq_tc has 128 query rows of a head and goes over their keys (S, dP, dQ: three products per
+// tile), k_seq_dkv_tc has 128 tokens of a KV head and goes over the queries of all heads of its group (S^T, dP^T, dV, dK: four).
+// Seven products instead of the five that one kernel would need, but every sum stays in one CTA's tensor memory: no atomics on
+// results, no fp32 copy of dQ in memory, the heads of a group added for free, and the same bits every time.
+//
+// Both have the forward kernel's roles: a TMA producer, an MMA issuer, two warps that pass the stages on (and patch tiles that some
+// row does not see in full) and eight softmax warps, here two threads per row with half of the columns each.  P and dS are
+// rounded to bf16 and are A operands in tensor memory, over the S and dP they came from; the tile that was K-major for the first
+// products is read MN-major for the second.
+//  * k_seq_dkv_tc, per tile of queries: dV and the next S^T run while dS is computed, dK and the next dP^T while the next P is.
+//    Tensor memory is full (S, dP, dV, dK: 4 x 128 columns), so nothing is buffered twice.  -lse and -delta of a tile's queries, which
+//    run along a thread's columns, lie in shared memory.
+//  * k_seq_dq_tc, per tile of keys: S is buffered twice and dS goes over the S it came from, so that softmax warps never wait.
+// Non-finite values of tokens that a row does not see: they are taken out of the operands of the second products (0 * NaN), and
+// the rows that do see them become NaN through lse, delta or a bit per key.
+#include "ptenc_seq_tc.cuh"
+
+namespace {
+
+enum { B_KIND, B_START, B_LEN, B_PIN, B_CAP, B_E, B_HEAD, B_TILE, B_A, B_B, B_C, B_N, B_WORDS };
+
+__device__ __forceinline__ SeqView bwd_view(volatile int* d) {
+  SeqView s;
+  s.start = d[B_START]; s.len = d[B_LEN]; s.pin = d[B_PIN]; s.cap = d[B_CAP]; s.e = d[B_E];
+  return s;
+}
+__device__ __forceinline__ uint64_t st_mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+template <int D>
+struct BSmem {
+  static constexpr int TILE = (D / 64) * HALF;
+  // Two rings: of the tiles that two products use far apart (K, or Q) and of the others (V, or dO).
+  static constexpr int RA = D == 128 ? 3 : 5, RB = D == 128 ? 2 : 5, STAGES = RA + RB;
+  static constexpr int OFF_AB = STAGES * TILE;                       // the item's own two tiles
+  static constexpr int OFF_STAT = OFF_AB + 2 * TILE;                 // float [2][2][128]
+  static constexpr int OFF_CLC = OFF_STAT + 4 * TM * 4;
+  static constexpr int OFF_BAD = OFF_CLC + 16;                       // uint32 [2][2][4]: rows of patched tiles with non-finite values
+  static constexpr int OFF_DESC = OFF_BAD + 64;
+  static constexpr int OFF_BAR = (OFF_DESC + 2 * B_WORDS * 4 + 7) / 8 * 8;
+  static constexpr int N_BAR = 3 * STAGES + 20;
+  static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
+  static constexpr int TOTAL = OFF_MISC + 16;
+  static_assert(TOTAL <= 232448, "shared memory of one CTA");
+  // where the nt-th tile of a CTA lies, and its barriers' parity
+  __device__ static __forceinline__ uint32_t stage_a(uint32_t nt) { return nt % RA; }
+  __device__ static __forceinline__ uint32_t stage_b(uint32_t nt) { return RA + nt % RB; }
+  __device__ static __forceinline__ uint32_t phase_a(uint32_t nt) { return (nt / RA) & 1; }
+  __device__ static __forceinline__ uint32_t phase_b(uint32_t nt) { return (nt / RB) & 1; }
+};
+
+// Barriers after the stages' full, empty and ready ones.
+enum { X_AB_FULL, X_AB_EMPTY, X_S_FULL, X_S_FULL1, X_DP_FULL, X_P_READY, X_DS_READY, X_ACC_FULL, X_ACC_EMPTY, X_STAT_FULL, X_STAT_FULL1,
+       X_STAT_EMPTY, X_STAT_EMPTY1, X_ITEM_FULL, X_ITEM_FULL1, X_ITEM_EMPTY, X_ITEM_EMPTY1, X_CLC, X_DRAIN };
+
+// What a CTA of either kernel does first; returns the TMEM base.
+template <int D>
+__device__ __forceinline__ uint32_t bwd_begin(uint8_t* smem, uint32_t sb, int tid, int warp) {
+  using SM = BSmem<D>;
+  constexpr int NS = SM::STAGES;
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
+  const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, x = ready + 8 * NS;
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); bar_init(ready + 8 * s, 1); }
+    const int counts[] = {1, 1, 1, 1, 1, 8, 8, 1, 8, 2, 2, 8, 8, 1, 1, 1 + 2 + 8, 1 + 2 + 8, 1, 1};
+    for (int i = 0; i <= X_DRAIN; ++i) bar_init(x + 8 * i, counts[i]);
+    misc[0] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sb + SM::OFF_MISC + 4), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tree_after_previous();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  return (uint32_t)misc[1];
+}
+
+// The producer of either kernel.  find(item, d) fills an item's words (all but the kind) and says whether it is one; own(d, which) and
+// entry(d, tile, which) load the item's own two tiles and its ring entries.
+template <int D, typename FIND, typename OWN, typename ENTRY>
+__device__ __forceinline__ void bwd_produce(uint8_t* smem, uint32_t sb, FIND find, OWN own, ENTRY entry) {
+  using SM = BSmem<D>;
+  constexpr int NS = SM::STAGES, TILE = SM::TILE;
+  volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
+  const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, x = empty + 16 * NS;
+  uint32_t nt = 0, seq = 0, asked = 0;                   // tiles, items and takeovers so far
+  bool half = false;                                     // the last tile's first ring entry alone has been asked for
+  bool okay = true;
+  int item = (int)blockIdx.x;
+  while (okay) {
+    const uint32_t slot = seq & 1;
+    if (item < 0) {
+      if (bar_wait(x + 8 * (X_ITEM_EMPTY + slot), ((seq >> 1) & 1) ^ 1, abort_flag)) {
+        desc[slot * B_WORDS + B_KIND] = 0;
+        bar_arrive(x + 8 * (X_ITEM_FULL + slot));
+      } else {
+        okay = false;
+      }
+      break;
+    }
+    bar_expect(x + 8 * X_CLC, 16);
+    clc_ask(sb + SM::OFF_CLC, x + 8 * X_CLC);
+    int w[B_WORDS];
+    if (find(item, w)) {
+      if (!bar_wait(x + 8 * (X_ITEM_EMPTY + slot), ((seq >> 1) & 1) ^ 1, abort_flag)) { okay = false; break; }
+      volatile int* d = desc + slot * B_WORDS;
+      for (int i = B_START; i < B_WORDS; ++i) d[i] = w[i];
+      d[B_KIND] = 1;
+      bar_arrive(x + 8 * (X_ITEM_FULL + slot));
+      if (!bar_wait(x + 8 * X_AB_EMPTY, (seq & 1) ^ 1, abort_flag)) { okay = false; break; }
+      bar_expect(x + 8 * X_AB_FULL, 2 * TILE);
+      for (int t = 0; t < 2; ++t) own(w, t, sb + SM::OFF_AB + t * TILE, x + 8 * X_AB_FULL);
+      ++seq;
+      for (int t = 0; t < w[B_N] && okay; ++t, ++nt) {
+        uint32_t s = SM::stage_a(nt);
+        if (!bar_wait(empty + 8 * s, SM::phase_a(nt) ^ 1, abort_flag)) { okay = false; break; }
+        bar_expect(full + 8 * s, (uint32_t)TILE);
+        entry(w, t, 0, sb + s * TILE, full + 8 * s);
+        s = SM::stage_b(nt);
+        if (!bar_wait(empty + 8 * s, SM::phase_b(nt) ^ 1, abort_flag)) { okay = false; half = true; break; }
+        bar_expect(full + 8 * s, (uint32_t)TILE);
+        entry(w, t, 1, sb + s * TILE, full + 8 * s);
+      }
+    }
+    if (okay) {
+      if (!bar_wait(x + 8 * X_CLC, asked & 1, abort_flag)) { okay = false; break; }
+      item = clc_answer(sb + SM::OFF_CLC);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      ++asked;
+    }
+  }
+  if (!okay) { *abort_flag = 1; bar_drain(x + 8 * X_CLC, asked & 1); }
+  // whatever the other roles did, copies in flight land before the shared memory goes away
+  const uint32_t na = nt + (half ? 1 : 0);
+  for (uint32_t i = 1; i <= (uint32_t)SM::RA && i <= na; ++i) bar_drain(full + 8 * SM::stage_a(na - i), SM::phase_a(na - i));
+  for (uint32_t i = 1; i <= (uint32_t)SM::RB && i <= nt; ++i) bar_drain(full + 8 * SM::stage_b(nt - i), SM::phase_b(nt - i));
+  if (seq > 0 && !okay) bar_drain(x + 8 * X_AB_FULL, (seq - 1) & 1);
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int h, int row, uint32_t bar) {
+#pragma unroll
+  for (int hf = 0; hf < D / 64; ++hf) tma_3d(dst + hf * HALF, map, hf * 64, h, row, bar);
+}
+
+// D (fp32, 128 x 128) = A B^T, both K-major tiles in shared memory.
+template <int D>
+__device__ __forceinline__ void mma_scores(uint32_t d, uint32_t a, uint32_t b) {
+  const uint64_t da = desc_k(a), db = desc_k(b);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    const uint64_t off = ((k >> 2) * HALF + (k & 3) * 32) >> 4;
+    mma_ss(d, da + off, db + off, tt_idesc(SN, 0), k > 0);
+  }
+}
+// D (fp32, 128 x D) += A B, A bf16 in tensor memory (64 columns of it at the start of each half of `a`), B 128 rows as they lie.
+template <int D>
+__device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, uint32_t b, bool replace) {
+  const uint64_t db = desc_mn(b);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) mma_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (k * 2048 >> 4), tt_idesc(D, 1), k > 0 ? 1u : (replace ? 0u : 1u));
+}
+
+// One row of a gradient, columns [c0, c1), from tensor memory.
+template <int D>
+__device__ __forceinline__ void store_row(uint32_t t, int c0, int c1, float f, __nv_bfloat16* to, int Dr, bool real, bool wide) {
+#pragma unroll 1
+  for (int c = c0; c < c1; c += 16) {
+    float o[16];
+    ld16(t + c, o);
+    wait_ld();
+    uint32_t pk[8];
+#pragma unroll
+    for (int y = 0; y < 16; y += 2) pk[y >> 1] = tt_pack(o[y] * f, o[y + 1] * f);
+    if (!real) continue;
+    if (c + 16 <= Dr) tt_store(to + c, pk, wide);
+    else if (c < Dr) *reinterpret_cast<uint4*>(to + c) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+  }
+}
+
+__device__ __forceinline__ void bwd_end(uint32_t tmem, int warp) {
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ dq
+// Also leaves -lse (base 2) and -delta of every row for the other kernel, [Hq][n] each.
+template <int D>
+__global__ void __launch_bounds__(ST_THREADS, 1)
+k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG) {
+  using SM = BSmem<D>;
+  constexpr int NS = SM::STAGES, TILE = SM::TILE;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sb = tt_u32(smem);
+  volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
+  uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + SM::OFF_BAD);           // [tile & 1][4]: keys with non-finite values
+  const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, X = ready + 8 * NS;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp);
+  const uint32_t tS = tmem, tP = tmem + 2 * SN, tA = tmem + 3 * SN;            // S [2], dP, dQ
+  auto range_of = [](volatile int* d) { SeqRange r; r.np = d[B_A]; r.s0 = d[B_B]; r.s1 = d[B_C]; return r; };
+
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ST_REGS_LOW));
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag)); };
+  if (warp == 0) {
+    if (lane == 0)
+      bwd_produce<D>(smem, sb,
+        [&](int item, int* w) -> bool {
+          const int at = (int)gridDim.x - 1 - item, number = at / a.Hq;
+          SeqView s;
+          int tile;
+          if (!seq_find(a, number, TM, &s, &tile)) return false;
+          const int i0 = tile * TM;
+          const SeqRange r = seq_keys(s, i0, min(i0 + TM, s.len) - 1, SN);
+          w[B_START] = s.start; w[B_LEN] = s.len; w[B_PIN] = s.pin; w[B_CAP] = s.cap; w[B_E] = s.e; w[B_HEAD] = at - number * a.Hq;
+          w[B_TILE] = tile; w[B_A] = r.np; w[B_B] = r.s0; w[B_C] = r.s1; w[B_N] = seq_count(r);
+          return true;
+        },
+        [&](const int* w, int t, uint32_t dst, uint32_t bar) {
+          load_tile<D>(dst, t == 0 ? &tmQ : &tmG, w[B_HEAD], w[B_START] + w[B_TILE] * TM, bar);
+        },
+        [&](const int* w, int t, int which, uint32_t dst, uint32_t bar) {
+          SeqRange r;
+          r.np = w[B_A]; r.s0 = w[B_B]; r.s1 = w[B_C];
+          load_tile<D>(dst, which ? &tmV : &tmK, w[B_HEAD] / a.g, w[B_START] + seq_at(r, t) * SN, bar);
+        });
+  } else if (warp == 1) {
+    // ================================================================ MMA issuer
+    const bool leader = tt_elect();
+    uint32_t seq = 0, nt = 0;                            // items, tiles
+    bool okay = true;
+    auto send = [&](uint32_t bar) { if (leader) commit(bar); __syncwarp(); };
+    while (okay) {
+      const uint32_t slot = seq & 1;
+      if (!wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + slot * B_WORDS;
+      const int kind = __shfl_sync(0xffffffffu, d[B_KIND], 0), n = __shfl_sync(0xffffffffu, d[B_N], 0);
+      if (kind == 0) break;
+      __syncwarp();
+      if (leader) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
+      if (!wait(X + 8 * X_AB_FULL, seq & 1)) { okay = false; break; }
+      auto scores = [&](int t) -> bool {                 // S of tile t
+        const uint32_t s = SM::stage_a(nt + t), buf = (nt + t) & 1;
+        if (!wait(ready + 8 * s, SM::phase_a(nt + t))) return false;
+        if (leader) { mma_scores<D>(tS + buf * SN, sb + SM::OFF_AB, sb + s * TILE); commit(X + 8 * (X_S_FULL + buf)); }
+        __syncwarp();
+        return true;
+      };
+      auto values = [&](int t) -> bool {                 // dP of tile t
+        const uint32_t s = SM::stage_b(nt + t);
+        if (!wait(ready + 8 * s, SM::phase_b(nt + t))) return false;
+        if (leader) {
+          mma_scores<D>(tP, sb + SM::OFF_AB + TILE, sb + s * TILE);
+          commit(X + 8 * X_DP_FULL);
+          commit(empty + 8 * s);
+        }
+        __syncwarp();
+        return true;
+      };
+      okay = scores(0) && values(0) && (n == 1 || scores(1));
+      for (int t = 0; t < n && okay; ++t) {
+        if (!wait(X + 8 * X_DS_READY, (nt + t) & 1)) { okay = false; break; }
+        fence_after();
+        if (t + 1 < n && !values(t + 1)) { okay = false; break; }
+        if (t == 0 && !wait(X + 8 * X_ACC_EMPTY, (seq & 1) ^ 1)) { okay = false; break; }
+        const uint32_t s = SM::stage_a(nt + t);
+        if (leader) {
+          mma_sums<D>(tA, tS + ((nt + t) & 1) * SN, sb + s * TILE, t == 0);
+          commit(empty + 8 * s);
+        }
+        __syncwarp();
+        if (t + 2 < n && !scores(t + 2)) { okay = false; break; }
+      }
+      if (!okay) break;
+      send(X + 8 * X_ACC_FULL);
+      send(X + 8 * X_AB_EMPTY);
+      nt += n;
+      ++seq;
+    }
+    if (leader) {
+      if (!okay) *abort_flag = 1;
+      commit(X + 8 * X_DRAIN);
+      bar_drain(X + 8 * X_DRAIN, 0);
+    }
+    __syncwarp();
+  } else {
+    // ================================================================ passes the stages on: warp 2 the K tiles, warp 3 the V tiles
+    const int me = warp - 2;
+    uint32_t seq = 0, nt = 0;
+    bool okay = true;
+    while (okay) {
+      const uint32_t slot = seq & 1;
+      if (!wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + slot * B_WORDS;
+      if (d[B_KIND] == 0) break;
+      const SeqView s = bwd_view(d);
+      const SeqRange r = range_of(d);
+      const int n = d[B_N], i0 = d[B_TILE] * TM;
+      for (int t = 0; t < n; ++t) {
+        // Each ring has its own warp, which waits for each of its tiles in turn and without which none is used: a wait tells a
+        // stage's phase from the one two rounds before or after.
+        const uint32_t sg = me == 0 ? SM::stage_a(nt + t) : SM::stage_b(nt + t);
+        if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
+        if (me == 0) {
+          const int tile = seq_at(r, t);
+          uint32_t* bad = s_bad + 4 * ((nt + t) & 1);    // read with the tile two before
+          if (!wait(X + 8 * (X_STAT_EMPTY + ((nt + t) & 1)), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
+          if (!seq_all(s, i0, i0 + TM - 1, tile * SN, tile * SN + SN - 1)) {
+            if (lane < 4) bad[lane] = 0;
+            __syncwarp();
+            patch_tile(smem + sg * TILE, D / 64, tile * SN, s.len, 0, 1, bad);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(ready + 8 * sg);
+      }
+      if (!okay) break;
+      __syncwarp();
+      if (lane == 0) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
+      ++seq;
+      nt += n;
+    }
+    if (!okay && lane == 0) *abort_flag = 1;
+  }
+  } else {
+    // ================================================================ softmax: two threads per row, half of a tile's keys each
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ST_REGS_HIGH));
+    const int half = (warp - 4) >> 2, quarter = warp & 3, lrow = 32 * quarter + lane;
+    const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
+    const float sl2 = a.scale * ST_LOG2E;
+    uint32_t seq = 0, nt = 0;
+    bool fine = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (fine && !bar_wait(bar, parity, abort_flag)) { fine = false; *abort_flag = 1; }
+    };
+    while (true) {
+      const uint32_t slot = seq & 1;
+      wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1);
+      if (!__all_sync(0xffffffffu, fine)) break;
+      volatile int* d = desc + slot * B_WORDS;
+      if (d[B_KIND] == 0) break;
+      const SeqView s = bwd_view(d);
+      const SeqRange r = range_of(d);
+      const int n = d[B_N], i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row);
+      const bool real = row < s.len;
+      // delta: both threads of a row form it, so that no barrier stands between the warps
+      const long long orow = (long long)(s.start + row) * a.Hq + h;
+      float sum = 0.f, nlse = 0.f;
+      if (real) {
+        const uint4* o = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.out) + orow * a.D);
+        const uint4* g = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.dout) + orow * a.D);
+#pragma unroll 4
+        for (int c = 0; c < a.D / 8; ++c) {
+          const uint4 u = o[c], v = g[c];
+          const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&u);
+          const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 p = __bfloat1622float2(x[k]), q = __bfloat1622float2(y[k]);
+            sum = fmaf(p.x, q.x, fmaf(p.y, q.y, sum));
+          }
+        }
+        nlse = -a.lse[orow] * ST_LOG2E;
+      }
+      const float ndelta = -sum;
+      if (real && half == 0) {
+        const long long at = (long long)h * a.n + s.start + row;
+        a.delta[at] = ndelta;
+        a.delta[(long long)a.Hq * a.n + at] = nlse;
+      }
+      const uint64_t scl2 = tt_two(sl2, sl2), nlse2 = tt_two(nlse, nlse), nd2 = tt_two(ndelta, ndelta);
+#pragma unroll 1
+      for (int t = 0; t < n; ++t, ++nt) {
+        const uint32_t buf = nt & 1, ts = tS + buf * SN + 64 * half + lane_off, tp = tP + 64 * half + lane_off;
+        const int j0 = seq_at(r, t) * SN;
+        wait(X + 8 * (X_S_FULL + buf), (nt >> 1) & 1);
+        fence_after();
+        float p[64];
+        ld32(ts, p);
+        ld32(ts + 32, p + 32);
+        wait_ld();
+        const bool all = seq_all(s, i0, i0 + TM - 1, j0, j0 + SN - 1);
+#pragma unroll
+        for (int y = 0; y < 64; y += 2) {
+          tt_both(tt_fma2(tt_two(p[y], p[y + 1]), scl2, nlse2), p[y], p[y + 1]);
+          p[y] = tt_ex2(p[y]);
+          p[y + 1] = tt_ex2(p[y + 1]);
+        }
+        if (!all) {
+          const uint32_t* bad = s_bad + 4 * buf + 2 * half;
+          const uint32_t b0 = bad[0], b1 = bad[1];
+          if ((b0 | b1) != 0) {                          // rare: keys with non-finite values
+#pragma unroll
+            for (int y = 0; y < 64; ++y)
+              if (((y < 32 ? b0 : b1) >> (y & 31)) & 1u) p[y] = __int_as_float(0x7fffffff);
+          }
+        }
+        wait(X + 8 * X_DP_FULL, nt & 1);
+        fence_after();
+        const int jh = j0 + 64 * half, hi = row - jh, lo = low - jh, pn = s.pin - jh;
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          float x[32];
+          uint32_t pk[16];
+          ld32(tp + c, x);
+          wait_ld();
+#pragma unroll
+          for (int y = 0; y < 32; y += 2)
+            tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), nd2), tt_two(p[c + y], p[c + y + 1])), x[y], x[y + 1]);
+          if (!all) {
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (c + y > hi || (c + y >= pn && c + y < lo)) x[y] = 0.f;
+          }
+          // dS in bf16, half a step of 2^-8: the product's operands are of one type
+#pragma unroll
+          for (int y = 0; y < 32; y += 2) pk[y >> 1] = tt_pack(x[y], x[y + 1]);
+          st16(ts + c / 2, pk);
+        }
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) { bar_arrive(X + 8 * X_DS_READY); bar_arrive(X + 8 * (X_STAT_EMPTY + buf)); }
+      }
+      wait(X + 8 * X_ACC_FULL, seq & 1);
+      fence_after();
+      const bool wide = (reinterpret_cast<uintptr_t>(a.dq) & 31) == 0 && a.D % 16 == 0 && a.dqs % 16 == 0;
+      store_row<D>(tA + lane_off, half * (D / 2), (half + 1) * (D / 2), fine ? a.scale : __int_as_float(0x7fffffff),
+                   static_cast<__nv_bfloat16*>(a.dq) + (s.start + row) * a.dqs + (long long)h * a.D, a.D, real, wide);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) { bar_arrive(X + 8 * X_ACC_EMPTY); bar_arrive(X + 8 * (X_ITEM_EMPTY + slot)); }
+      ++seq;
+    }
+  }
+  bwd_end(tmem, warp);
+}
+
+// ------------------------------------------------------------------------------------------------ dk, dv
+template <int D>
+__global__ void __launch_bounds__(ST_THREADS, 1)
+k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+             const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG) {
+  using SM = BSmem<D>;
+  constexpr int NS = SM::STAGES, TILE = SM::TILE;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sb = tt_u32(smem);
+  volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
+  uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + SM::OFF_BAD);           // [Q or dO][4], of the warp that patches
+  float* s_stat = reinterpret_cast<float*>(smem + SM::OFF_STAT);               // [buffer][-lse or -delta][128]
+  const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, X = ready + 8 * NS;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp);
+  const uint32_t tS = tmem, tP = tmem + SN, tV = tmem + 2 * SN, tK = tV + D;   // S^T, dP^T, dV, dK
+  // An item's tiles of queries: head by head, tiles B_TILE .. B_TILE + B_A - 1 of each.
+
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ST_REGS_LOW));
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag)); };
+  if (warp == 0) {
+    if (lane == 0)
+      bwd_produce<D>(smem, sb,
+        [&](int item, int* w) -> bool {
+          const int number = item / a.Hkv;               // early tiles, which most rows see, first
+          SeqView s;
+          int tile;
+          if (!seq_find(a, number, TM, &s, &tile)) return false;
+          const int j0 = tile * TM, last = j0 < s.pin ? s.len - 1 : s.last(min(j0 + TM, s.len) - 1);
+          w[B_START] = s.start; w[B_LEN] = s.len; w[B_PIN] = s.pin; w[B_CAP] = s.cap; w[B_E] = s.e; w[B_HEAD] = item - number * a.Hkv;
+          w[B_TILE] = tile; w[B_A] = last / TM - tile + 1; w[B_B] = w[B_C] = 0; w[B_N] = a.g * w[B_A];
+          return true;
+        },
+        [&](const int* w, int t, uint32_t dst, uint32_t bar) {
+          load_tile<D>(dst, t == 0 ? &tmK : &tmV, w[B_HEAD], w[B_START] + w[B_TILE] * TM, bar);
+        },
+        [&](const int* w, int t, int which, uint32_t dst, uint32_t bar) {
+          const int hh = t / w[B_A];
+          load_tile<D>(dst, which ? &tmG : &tmQ, w[B_HEAD] * a.g + hh, w[B_START] + (w[B_TILE] + t - hh * w[B_A]) * TM, bar);
+        });
+  } else if (warp == 1) {
+    // ================================================================ MMA issuer
+    const bool leader = tt_elect();
+    uint32_t seq = 0, nt = 0;
+    bool okay = true;
+    auto send = [&](uint32_t bar) { if (leader) commit(bar); __syncwarp(); };
+    while (okay) {
+      const uint32_t slot = seq & 1;
+      if (!wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + slot * B_WORDS;
+      const int kind = __shfl_sync(0xffffffffu, d[B_KIND], 0), n = __shfl_sync(0xffffffffu, d[B_N], 0);
+      if (kind == 0) break;
+      __syncwarp();
+      if (leader) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
+      if (!wait(X + 8 * X_AB_FULL, seq & 1)) { okay = false; break; }
+      // S^T (which 0) or dP^T (1) of tile t
+      auto product = [&](int t, int which) -> bool {
+        const uint32_t s = which ? SM::stage_b(nt + t) : SM::stage_a(nt + t);
+        if (!wait(ready + 8 * s, which ? SM::phase_b(nt + t) : SM::phase_a(nt + t))) return false;
+        if (leader) {
+          mma_scores<D>(which ? tP : tS, sb + SM::OFF_AB + which * TILE, sb + s * TILE);
+          commit(X + 8 * (which ? X_DP_FULL : X_S_FULL));
+        }
+        __syncwarp();
+        return true;
+      };
+      okay = product(0, 0) && product(0, 1);
+      if (okay && !wait(X + 8 * X_ACC_EMPTY, (seq & 1) ^ 1)) okay = false;
+      for (int t = 0; t < n && okay; ++t) {
+        const uint32_t sq = SM::stage_a(nt + t), sg = SM::stage_b(nt + t);
+        if (!wait(X + 8 * X_P_READY, (nt + t) & 1)) { okay = false; break; }
+        fence_after();
+        if (leader) { mma_sums<D>(tV, tS, sb + sg * TILE, t == 0); commit(empty + 8 * sg); }
+        __syncwarp();
+        if (t + 1 < n && !product(t + 1, 0)) { okay = false; break; }
+        if (!wait(X + 8 * X_DS_READY, (nt + t) & 1)) { okay = false; break; }
+        fence_after();
+        if (leader) { mma_sums<D>(tK, tP, sb + sq * TILE, t == 0); commit(empty + 8 * sq); }
+        __syncwarp();
+        if (t + 1 < n && !product(t + 1, 1)) { okay = false; break; }
+      }
+      if (!okay) break;
+      send(X + 8 * X_ACC_FULL);
+      send(X + 8 * X_AB_EMPTY);
+      nt += n;
+      ++seq;
+    }
+    if (leader) {
+      if (!okay) *abort_flag = 1;
+      commit(X + 8 * X_DRAIN);
+      bar_drain(X + 8 * X_DRAIN, 0);
+    }
+    __syncwarp();
+  } else {
+    // ================================================================ warp 2: Q tiles and -lse; warp 3: dO tiles and -delta
+    const int me = warp - 2;
+    uint32_t seq = 0, nt = 0;
+    uint32_t* bad = s_bad + 4 * me;
+    bool okay = true;
+    while (okay) {
+      const uint32_t slot = seq & 1;
+      if (!wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1)) { okay = false; break; }
+      volatile int* d = desc + slot * B_WORDS;
+      if (d[B_KIND] == 0) break;
+      const SeqView s = bwd_view(d);
+      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM;
+      const float* stat = a.delta + (me == 0 ? (long long)a.Hq * a.n : 0) + (long long)d[B_HEAD] * a.g * a.n + s.start;
+      for (int t = 0; t < n; ++t) {
+        const uint32_t sg = me == 0 ? SM::stage_a(nt + t) : SM::stage_b(nt + t), buf = (nt + t) & 1;
+        const int hh = t / tiles, i0 = (tile0 + t - hh * tiles) * TM;
+        // asked for early: rows past the end are not seen by anybody
+        float v[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int i = i0 + lane + 32 * y;
+          v[y] = i < s.len ? stat[(long long)hh * a.n + i] : 0.f;
+        }
+        if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
+        if (!(i0 + TM <= s.len && seq_all(s, i0, i0 + TM - 1, j0, j0 + TM - 1))) {
+          if (lane < 4) bad[lane] = 0;
+          __syncwarp();
+          if (patch_tile(smem + sg * TILE, D / 64, i0, s.len, 0, 1, bad)) {
+            __syncwarp();
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if ((bad[y] >> lane) & 1u) v[y] = __int_as_float(0x7fffffff);    // whoever sees the row becomes NaN
+          }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(ready + 8 * sg);
+        if (!wait(X + 8 * (X_STAT_EMPTY + buf), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s_stat[buf * 2 * TM + me * TM + lane + 32 * y] = v[y];
+        __syncwarp();
+        if (lane == 0) bar_arrive(X + 8 * (X_STAT_FULL + buf));
+      }
+      if (!okay) break;
+      __syncwarp();
+      if (lane == 0) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
+      ++seq;
+      nt += n;
+    }
+    if (!okay && lane == 0) *abort_flag = 1;
+  }
+  } else {
+    // ================================================================ softmax: two threads per token, half of a tile's queries each
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ST_REGS_HIGH));
+    const int half = (warp - 4) >> 2, quarter = warp & 3, lrow = 32 * quarter + lane;
+    const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
+    const uint32_t ts = tS + 64 * half + lane_off, tp = tP + 64 * half + lane_off;
+    const float sl2 = a.scale * ST_LOG2E;
+    const uint64_t scl2 = tt_two(sl2, sl2);
+    uint32_t seq = 0, nt = 0;
+    bool fine = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (fine && !bar_wait(bar, parity, abort_flag)) { fine = false; *abort_flag = 1; }
+    };
+    while (true) {
+      const uint32_t slot = seq & 1;
+      wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1);
+      if (!__all_sync(0xffffffffu, fine)) break;
+      volatile int* d = desc + slot * B_WORDS;
+      if (d[B_KIND] == 0) break;
+      const SeqView s = bwd_view(d);
+      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM, col = j0 + lrow, last = s.last(col);
+      int i0 = j0, left = tiles;
+#pragma unroll 1
+      for (int t = 0; t < n; ++t, ++nt) {
+        const uint32_t buf = nt & 1;
+        const float* st = s_stat + buf * 2 * TM + 64 * half;
+        const bool all = i0 + TM <= s.len && seq_all(s, i0, i0 + TM - 1, j0, j0 + TM - 1);
+        const int lo = col - i0 - 64 * half, hi = last - i0 - 64 * half;       // columns [lo, hi] see this token
+        wait(X + 8 * (X_STAT_FULL + buf), (nt >> 1) & 1);
+        wait(X + 8 * X_S_FULL, nt & 1);
+        fence_after();
+        float p[64];
+        ld32(ts, p);
+        ld32(ts + 32, p + 32);
+        wait_ld();
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int y = c; y < c + 32; y += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(st + y);
+            tt_both(tt_fma2(tt_two(p[y], p[y + 1]), scl2, tt_two(v.x, v.y)), p[y], p[y + 1]);
+            tt_both(tt_fma2(tt_two(p[y + 2], p[y + 3]), scl2, tt_two(v.z, v.w)), p[y + 2], p[y + 3]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) p[y + z] = tt_ex2(p[y + z]);
+          }
+          if (!all) {
+#pragma unroll
+            for (int y = c; y < c + 32; ++y)             // a non-finite row of dO reaches dV too
+              p[y] = y < lo || y > hi ? 0.f : fmaf(0.f, st[TM + y], p[y]);
+          }
+          // P in bf16, half a step of 2^-8 per weight, as in the forward pass
+#pragma unroll
+          for (int y = 0; y < 32; y += 2) pk[y >> 1] = tt_pack(p[c + y], p[c + y + 1]);
+          st16(ts + c / 2, pk);
+        }
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(X + 8 * X_P_READY);
+        wait(X + 8 * X_DP_FULL, nt & 1);
+        fence_after();
+        float x[64];
+        ld32(tp, x);
+        ld32(tp + 32, x + 32);
+        wait_ld();
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int y = c; y < c + 32; y += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(st + TM + y);
+            tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), tt_two(v.x, v.y)), tt_two(p[y], p[y + 1])), x[y], x[y + 1]);
+            tt_both(st_mul2(tt_add2(tt_two(x[y + 2], x[y + 3]), tt_two(v.z, v.w)), tt_two(p[y + 2], p[y + 3])), x[y + 2], x[y + 3]);
+          }
+          if (!all) {
+#pragma unroll
+            for (int y = c; y < c + 32; ++y)
+              if (y < lo || y > hi) x[y] = 0.f;
+          }
+#pragma unroll
+          for (int y = 0; y < 32; y += 2) pk[y >> 1] = tt_pack(x[c + y], x[c + y + 1]);
+          st16(tp + c / 2, pk);
+        }
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) { bar_arrive(X + 8 * X_DS_READY); bar_arrive(X + 8 * (X_STAT_EMPTY + buf)); }
+        i0 += TM;
+        if (--left == 0) { left = tiles; i0 = j0; }
+      }
+      wait(X + 8 * X_ACC_FULL, seq & 1);
+      fence_after();
+      const bool real = col < s.len;
+      const float f = !fine ? __int_as_float(0x7fffffff) : half == 0 ? 1.f : a.scale;
+      void* base = half == 0 ? a.dv : a.dk;
+      const long long stride = half == 0 ? a.dvs : a.dks;
+      const bool wide = (reinterpret_cast<uintptr_t>(base) & 31) == 0 && a.D % 16 == 0 && stride % 16 == 0;
+      store_row<D>((half == 0 ? tV : tK) + lane_off, 0, D, f,
+                   static_cast<__nv_bfloat16*>(base) + (s.start + col) * stride + (long long)d[B_HEAD] * a.D, a.D, real, wide);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) { bar_arrive(X + 8 * X_ACC_EMPTY); bar_arrive(X + 8 * (X_ITEM_EMPTY + slot)); }
+      ++seq;
+    }
+  }
+  bwd_end(tmem, warp);
+}
+
+template <int D>
+cudaError_t bwd_launch(const SeqArgs& a, int dev, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& g,
+                       unsigned numbers, cudaStream_t st) {
+  static PtencOnce once;
+  cudaError_t e = ptenc_first_use(once, dev, [] {
+    const cudaError_t x = ptenc_allow_smem(k_seq_dq_tc<D>, BSmem<D>::TOTAL);
+    return x != cudaSuccess ? x : ptenc_allow_smem(k_seq_dkv_tc<D>, BSmem<D>::TOTAL);
+  });
+  if (e != cudaSuccess) return e;
+  e = tree_launch(k_seq_dq_tc<D>, dim3(numbers * a.Hq), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
+  if (e != cudaSuccess) return e;
+  return tree_launch(k_seq_dkv_tc<D>, dim3(numbers * a.Hkv), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
+}
+
+}  // namespace
+
+bool seq_backward_tc(const SeqArgs& a, int dtype, int dev, cudaStream_t st, cudaError_t* e) {
+  const long long numbers = seq_numbers(a.n, a.B, TM);
+  if (dtype != PTENC_DTYPE_BF16 || a.D > 128 || numbers * a.Hq >= (1ll << 31)) return false;
+  CUtensorMap q, k, v, g;
+  if (!seq_map(&q, a.q, a.D, a.Hq, a.n, a.qs) || !seq_map(&k, a.k, a.D, a.Hkv, a.n, a.ks) || !seq_map(&v, a.v, a.D, a.Hkv, a.n, a.vs) ||
+      !seq_map(&g, a.dout, a.D, a.Hq, a.n, (long long)a.Hq * a.D))
+    return false;
+  *e = a.D <= 64 ? bwd_launch<64>(a, dev, q, k, v, g, (unsigned)numbers, st) : bwd_launch<128>(a, dev, q, k, v, g, (unsigned)numbers, st);
+  return true;
+}

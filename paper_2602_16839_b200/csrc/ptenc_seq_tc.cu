@@ -14,38 +14,11 @@
 //    fp32 (base 2), P rounded to bf16 and handed over in halves.  O is rescaled only when the maximum has grown by more than 2^8.
 //  * Every wait is bounded: one that runs out raises an abort flag, every role leaves, copies and products in flight are drained and
 //    tensor memory is freed; the item's rows become NaN.
-#include "ptenc_seq.cuh"
-#include "ptenc_tc.cuh"
+#include "ptenc_seq_tc.cuh"
 
 namespace {
 
-constexpr int SN = 128;                        // tokens of a K/V tile
 constexpr int ST_ROWS = 2 * TM;                // query rows of an item
-constexpr int ST_THREADS = 384;                // producer, MMA, two patch warps, 2 x 4 softmax warps
-// Registers: 384 threads are launched with 168 each (64512); the first four warps give up 96 for the softmax threads' scores.
-constexpr int ST_REGS_LOW = 72, ST_REGS_HIGH = 216;
-static_assert(128 * ST_REGS_LOW + 256 * ST_REGS_HIGH <= 384 * 168, "the split waits for registers that do not exist");
-constexpr float ST_LOG2E = 1.4426950408889634f, ST_LN2 = 0.6931471805599453f;
-
-// ------------------------------------------------------------------------------------------------ taking over CTAs
-// Asks for a CTA of the grid that has not started yet; 16 bytes of answer arrive at `to` and count at the barrier.
-__device__ __forceinline__ void clc_ask(uint32_t to, uint32_t bar) {
-  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
-               ::"r"(to), "r"(bar) : "memory");
-}
-// The x coordinate of the CTA that was taken over, or -1: none was left.
-__device__ __forceinline__ int clc_answer(uint32_t at) {
-  int x;
-  asm volatile(
-      "{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t.reg .b32 y;\n\t"
-      "ld.shared.b128 h, [%1];\n\t"
-      "mov.b32 y, -1;\n\t"
-      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
-      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 y, h;\n\t"
-      "mov.b32 %0, y;\n\t}"
-      : "=r"(x) : "r"(at) : "memory");
-  return x;
-}
 
 // ------------------------------------------------------------------------------------------------ layout
 // Item description words in shared memory.
@@ -54,7 +27,7 @@ enum { J_KIND, J_START, J_LEN, J_PIN, J_CAP, J_E, J_HEAD, J_ROW0, J_NP, J_S0, J_
 template <int D>
 struct FSmem {
   static constexpr int TILE = (D / 64) * HALF;                       // bytes of a 128-row tile
-  static constexpr int STAGES = D == 128 ? 5 : 10;
+  static constexpr int RK = D == 128 ? 2 : 5, RV = D == 128 ? 3 : 5, STAGES = RK + RV;       // rings of K and V tiles
   static constexpr int OFF_Q = STAGES * TILE;                        // two Q tiles
   static constexpr int OFF_CLC = OFF_Q + 2 * TILE;                   // 16 bytes of answer
   static constexpr int OFF_DESC = OFF_CLC + 16;                      // int [2][J_WORDS]
@@ -63,6 +36,11 @@ struct FSmem {
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;               // int [4]
   static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
+  // where the nt-th tile of a CTA lies, and its barriers' parity
+  __device__ static __forceinline__ uint32_t stage_k(uint32_t nt) { return nt % RK; }
+  __device__ static __forceinline__ uint32_t stage_v(uint32_t nt) { return RK + nt % RV; }
+  __device__ static __forceinline__ uint32_t phase_k(uint32_t nt) { return (nt / RK) & 1; }
+  __device__ static __forceinline__ uint32_t phase_v(uint32_t nt) { return (nt / RV) & 1; }
 };
 
 // What a stream's 128 rows see of an item's tiles.
@@ -103,34 +81,6 @@ __device__ __noinline__ void add_odd(float* o, const __nv_bfloat16* v, long long
       }
     }
   }
-}
-
-// Rows [row0, row0 + 128) of a 128-row tile of `cols` bf16 columns in shared memory: those past `rows` become zero, non-finite values
-// of the others too.  `me` of `of` warps.  True in every lane if something was taken out.
-__device__ __forceinline__ bool patch_tile(uint8_t* tile, int halves, int row0, int rows, int me, int of) {
-  const int lane = threadIdx.x & 31;
-  bool odd = false;
-  for (int x = me * 32 + lane; x < halves * TM * 8; x += of * 32) {
-    const int r = (x >> 3) & (TM - 1);
-    uint4* at = reinterpret_cast<uint4*>(tile + (x >> 10) * HALF + r * 128 + (x & 7) * 16);
-    if (row0 + r >= rows) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
-    uint4 w = *at;
-    uint32_t* e = reinterpret_cast<uint32_t*>(&w);
-    uint32_t top = 0;                                    // exponent bits all set, infinity or NaN, carry into the sign's place
-#pragma unroll
-    for (int y = 0; y < 4; ++y) top |= (e[y] & 0x7fff7fffu) + 0x00800080u;
-    if ((top & 0x80008000u) != 0) {
-      odd = true;
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
-        if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0x0000ffffu;
-      }
-      *at = w;
-    }
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  return __any_sync(0xffffffffu, odd);
 }
 
 // ------------------------------------------------------------------------------------------------ forward
@@ -186,7 +136,8 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   if (warp == 0) {
     // ================================================================ producer
     if (lane == 0) {
-      uint32_t pos = 0, seq = 0, asked = 0;              // ring entries, items and takeovers so far
+      uint32_t nt = 0, seq = 0, asked = 0;               // tiles, items and takeovers so far
+      bool half = false;                                 // the last tile's K alone has been asked for
       bool okay = true;
       int item = (int)blockIdx.x;
       while (okay) {
@@ -223,12 +174,16 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
               tma_3d(sb + SM::OFF_Q + t * TILE + hf * HALF, &tmQ, hf * 64, h, s.start + row0 + t * TM, q_full);
           ++seq;
           const int hk = h / a.g;
-          for (int k = 0; k < 2 * n; ++k, ++pos) {
-            const uint32_t st = pos % NS, bar = full + 8 * st, dst = sb + st * TILE;
-            if (!bar_wait(empty + 8 * st, ((pos / NS) & 1) ^ 1, abort_flag)) { okay = false; break; }
-            bar_expect(bar, (uint32_t)TILE);
-            const int j = s.start + seq_at(r, k >> 1) * SN;
-            for (int hf = 0; hf < DH; ++hf) tma_3d(dst + hf * HALF, (k & 1) ? &tmV : &tmK, hf * 64, hk, j, bar);
+          for (int i = 0; i < n; ++i, ++nt) {
+            const int j = s.start + seq_at(r, i) * SN;
+            uint32_t sg = SM::stage_k(nt);
+            if (!bar_wait(empty + 8 * sg, SM::phase_k(nt) ^ 1, abort_flag)) { okay = false; break; }
+            bar_expect(full + 8 * sg, (uint32_t)TILE);
+            for (int hf = 0; hf < DH; ++hf) tma_3d(sb + sg * TILE + hf * HALF, &tmK, hf * 64, hk, j, full + 8 * sg);
+            sg = SM::stage_v(nt);
+            if (!bar_wait(empty + 8 * sg, SM::phase_v(nt) ^ 1, abort_flag)) { okay = false; half = true; break; }
+            bar_expect(full + 8 * sg, (uint32_t)TILE);
+            for (int hf = 0; hf < DH; ++hf) tma_3d(sb + sg * TILE + hf * HALF, &tmV, hf * 64, hk, j, full + 8 * sg);
           }
         }
         // the answer is waited for whatever happened: it is a copy in flight
@@ -241,7 +196,9 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       }
       if (!okay) { *abort_flag = 1; bar_drain(clc, asked & 1); }
       // whatever the other roles did, copies in flight land before the shared memory goes away
-      for (uint32_t i = 1; i <= (uint32_t)NS && i <= pos; ++i) bar_drain(full + 8 * ((pos - i) % NS), ((pos - i) / NS) & 1);
+      const uint32_t nk = nt + (half ? 1 : 0);
+      for (uint32_t i = 1; i <= (uint32_t)SM::RK && i <= nk; ++i) bar_drain(full + 8 * SM::stage_k(nk - i), SM::phase_k(nk - i));
+      for (uint32_t i = 1; i <= (uint32_t)SM::RV && i <= nt; ++i) bar_drain(full + 8 * SM::stage_v(nt - i), SM::phase_v(nt - i));
       if (seq > 0 && !okay) bar_drain(q_full, (seq - 1) & 1);
     }
   } else if (warp == 1) {
@@ -252,7 +209,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     };
     auto get = [&](int x) -> int { return __shfl_sync(0xffffffffu, x, 0); };
     constexpr uint32_t ID_QK = tt_idesc(SN, 0), ID_PV = tt_idesc(D, 1);
-    uint32_t base = 0, seq = 0, patched = 0;             // ring entries, items; parity of each stage's patches
+    uint32_t nt = 0, seq = 0;                            // tiles and items
     uint32_t np0 = 0, np1 = 0, ni0 = 0, ni1 = 0;         // tiles and items of the streams
     bool okay = true;
     while (okay) {
@@ -271,7 +228,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       if (!wait(q_full, seq & 1)) { okay = false; break; }
       ++seq;
       auto issue_s = [&](int st, int i) {
-        const uint32_t sg = (base + 2 * i) % NS;
+        const uint32_t sg = SM::stage_k(nt + i);
         const uint64_t dq = desc_k(sb + SM::OFF_Q + st * TILE), dk = desc_k(sb + sg * TILE);
         if (leader) {
 #pragma unroll
@@ -283,25 +240,15 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         }
         __syncwarp();
       };
-      auto wait_k = [&](int i) -> bool {
-        const uint32_t ps = base + 2 * i;
-        return wait(full + 8 * (ps % NS), (ps / NS) & 1);
-      };
-      auto release = [&](int k) {                        // ring entry of the item: free once what has been issued is done
-        if (leader) commit(empty + 8 * ((base + k) % NS));
+      auto wait_k = [&](int i) -> bool { return wait(full + 8 * SM::stage_k(nt + i), SM::phase_k(nt + i)); };
+      auto release = [&](uint32_t stage) {               // free once what has been issued is done
+        if (leader) commit(empty + 8 * stage);
         __syncwarp();
       };
       auto step = [&](int st, int i, int tile, bool& v_there, bool first, uint32_t& np, uint32_t& ni, bool last) -> bool {
-        const uint32_t ps = base + 2 * i + 1, sg = ps % NS;
-        if (!v_there) {
-          if (clean_tile(s, row0, ST_ROWS, tile)) {
-            if (!wait(full + 8 * sg, (ps / NS) & 1)) return false;
-          } else {
-            if (!wait(ready + 8 * sg, (patched >> sg) & 1)) return false;
-            patched ^= 1u << sg;
-          }
-          v_there = true;
-        }
+        const uint32_t sg = SM::stage_v(nt + i);
+        if (!v_there && !wait(ready + 8 * sg, SM::phase_v(nt + i))) return false;
+        v_there = true;
         if (first && !wait(o_empty + 8 * st, (ni & 1) ^ 1)) return false;      // O of the item before is out
         const uint64_t dv = desc_mn(sb + sg * TILE);
 #pragma unroll
@@ -332,7 +279,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         if (leader) commit(q_empty);
         __syncwarp();
       };
-      if (okay) release(0);
+      if (okay) release(SM::stage_k(nt));
       if (okay && n == 1) q_done();
       bool first0 = true, first1 = true;
       for (int i = 0; i < n && okay; ++i) {
@@ -350,12 +297,12 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           first1 = false;
         }
         if (!okay) break;
-        release(2 * i + 1);
+        release(SM::stage_v(nt + i));
         if (k1) issue_s(1, i + 1);
-        if (next >= 0) release(2 * i + 2);
+        if (next >= 0) release(SM::stage_k(nt + i + 1));
         if (i + 2 == n) q_done();
       }
-      base += 2 * n;
+      nt += n;
     }
     if (leader) {
       if (!okay) *abort_flag = 1;
@@ -365,7 +312,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     __syncwarp();
   } else {
     // ================================================================ patch warps
-    uint32_t base = 0, seq = 0;
+    uint32_t nt = 0, seq = 0;
     bool okay = true;
     auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
       return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag));
@@ -380,12 +327,12 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       r.np = d[J_NP]; r.s0 = d[J_S0]; r.s1 = d[J_S1];
       for (int i = 0; i < n; ++i) {
         const int tile = seq_at(r, i);
-        const uint32_t ps = base + 2 * i + 1, sg = ps % NS;
-        // every V tile is waited for, in order: a wait for a stage's phase tells it from the one two rounds before only while this
-        // warp is less than a round ahead
-        if (!wait(full + 8 * sg, (ps / NS) & 1)) { okay = false; break; }
-        if (clean_tile(s, row0, ST_ROWS, tile)) continue;
-        if (patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2) && lane == 0) d[J_ODD] = 1;
+        // These warps wait for each V tile in turn, and none is used without them: a wait tells a stage's phase from the one two
+        // rounds before or after.
+        const uint32_t sg = SM::stage_v(nt + i);
+        if (!wait(full + 8 * sg, SM::phase_v(nt + i))) { okay = false; break; }
+        if (!clean_tile(s, row0, ST_ROWS, tile) && patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2, nullptr) && lane == 0)
+          d[J_ODD] = 1;
         __syncwarp();
         if (lane == 0) bar_arrive(ready + 8 * sg);
       }
@@ -393,7 +340,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       __syncwarp();
       if (lane == 0) bar_arrive(item_empty + 8 * (seq & 1));
       ++seq;
-      base += 2 * n;
+      nt += n;
     }
     if (!okay && lane == 0) *abort_flag = 1;
   }
@@ -547,22 +494,6 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 }
 
 // ------------------------------------------------------------------------------------------------ host
-// bf16 [n][heads][D] with `stride` elements from token to token, box of 128 tokens x 1 head x 64 columns, 128-byte swizzle; what lies
-// outside the tensor reads as zero.
-bool seq_map(CUtensorMap* map, const void* base, int D, int heads, long long n, long long stride) {
-  TtEncodeFn fn = tt_encode_fn();
-  if (fn == nullptr) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)n};
-  cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
-  cuuint32_t box[3] = {64, 1, SN};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return ptenc_encode_map([&] {
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  });
-}
-
 template <int D>
 cudaError_t fwd_launch(const SeqArgs& a, int dev, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, unsigned grid,
                        cudaStream_t st) {

@@ -146,7 +146,7 @@ def test_head_norm_rope_backward_refuses(over, code):
 
 def _seq(back=False, **over):
     a = dict(dtype=1, Hq=4, Hkv=2, D=64, W=0, E=1, scale=0.0, q=P, qs=256, k=P, ks=128, v=P, vs=128, out=P, lse=P, g=P, cu=P, pin=None, B=2, n=10,
-             dq=P, dqs=256, dk=P, dks=128, dv=P, dvs=128, ws=P, size=160)
+             dq=P, dqs=256, dk=P, dks=128, dv=P, dvs=128, ws=P, size=320)
     a.update(over)
     cfg = bd.SeqConfig(a["dtype"], a["Hq"], a["Hkv"], a["D"], a["W"], a["E"], a["scale"])
     cfg = None if a.get("nocfg") else ctypes.byref(cfg)
@@ -170,7 +170,7 @@ def test_seq_attn_refuses(over, code, back):
 
 @pytest.mark.parametrize("over,code", [
     (dict(lse=None), "EINVAL"), (dict(g=None), "EINVAL"), (dict(dq=None), "EINVAL"), (dict(dk=None), "EINVAL"), (dict(dv=None), "EINVAL"),
-    (dict(ws=None), "EINVAL"), (dict(size=159), "EWORKSPACE"), (dict(ws=P + 8), "EALIGN"), (dict(dq=P + 8), "EALIGN"), (dict(g=P + 2), "EALIGN"),
+    (dict(ws=None), "EINVAL"), (dict(size=319), "EWORKSPACE"), (dict(ws=P + 8), "EALIGN"), (dict(dq=P + 8), "EALIGN"), (dict(g=P + 2), "EALIGN"),
     (dict(dqs=128), "ESHAPE"), (dict(dks=132), "EALIGN"), (dict(dvs=100), "ESHAPE")])
 def test_seq_attn_backward_refuses(over, code):
     assert _seq(True, **over) == getattr(bd, "PTENC_" + code)
@@ -202,7 +202,7 @@ def test_nothing_to_do_is_not_an_error():
 
 def test_workspace_sizes():
     n = ctypes.c_size_t(0)
-    assert pt.seq_attn_workspace_bytes(10, 4) == 160 and pt.head_norm_rope_workspace_bytes(128) > 0
+    assert pt.seq_attn_workspace_bytes(10, 4) == 320 and pt.head_norm_rope_workspace_bytes(128) > 0
     assert pt.lib.ptenc_seq_attn_workspace_bytes(-1, 4, ctypes.byref(n)) == bd.PTENC_EINVAL
     assert pt.lib.ptenc_seq_attn_workspace_bytes(1, 4, None) == bd.PTENC_EINVAL
     assert pt.lib.ptenc_seq_attn_workspace_bytes(1 << 31, 4, ctypes.byref(n)) == bd.PTENC_ESHAPE
