@@ -6,6 +6,7 @@
 struct SeqArgs {
   int Hq, Hkv, D, g, B;
   int window, chunk;               // window 0: none
+  int pins;                        // tiles of a sequence that may be pinned and are numbered by themselves (gradients of keys and values)
   float scale;
   long long n;
   const void* q;
@@ -41,6 +42,24 @@ struct SeqView {
   }
 };
 
+// Describes sequence b; false where its bounds or its pinned tokens are out of range.
+__device__ __forceinline__ bool seq_at_start(const SeqArgs& a, int b, SeqView* s) {
+  const int c0 = a.cu[b], c1 = a.cu[b + 1];
+  if (c0 < 0 || c1 < c0 || c1 > a.n) return false;
+  s->start = c0;
+  s->len = c1 - c0;
+  s->pin = s->cap = 0;
+  s->e = 1;
+  if (a.window > 0) {
+    const int pin = a.pinned != nullptr ? a.pinned[b] : 0;
+    if (pin < 0 || pin >= a.window) return false;
+    s->pin = pin;
+    s->cap = a.window - pin;
+    s->e = min(a.chunk, s->cap);
+  }
+  return true;
+}
+
 // Tile numbers.  Tile t of sequence b has number cu[b] / M + b + t: since cu[b + 1] / M + 1 - cu[b] / M is at least the number
 // of tiles of M tokens that sequence b needs, numbers are never shared, and a call has at most n / M + B of them -- the host
 // needs to know no length.  Some numbers belong to no tile.  Finds the sequence by binary search and checks everything read.
@@ -50,21 +69,9 @@ __device__ __forceinline__ bool seq_find(const SeqArgs& a, int number, int M, Se
     const int mid = (lo + hi) >> 1;
     if (a.cu[mid] / M + mid <= number) lo = mid; else hi = mid;
   }
-  const int c0 = a.cu[lo], c1 = a.cu[lo + 1];
-  if (c0 < 0 || c1 < c0 || c1 > a.n) return false;
-  const int t = number - (c0 / M + lo);
-  if (t < 0 || (long long)t * M >= c1 - c0) return false;
-  s->start = c0;
-  s->len = c1 - c0;
-  s->pin = s->cap = 0;
-  s->e = 1;
-  if (a.window > 0) {
-    const int pin = a.pinned != nullptr ? a.pinned[lo] : 0;
-    if (pin < 0 || pin >= a.window) return false;
-    s->pin = pin;
-    s->cap = a.window - pin;
-    s->e = min(a.chunk, s->cap);
-  }
+  if (!seq_at_start(a, lo, s)) return false;
+  const int t = number - (s->start / M + lo);
+  if (t < 0 || (long long)t * M >= s->len) return false;
   *tile = t;
   return true;
 }

@@ -481,12 +481,20 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     if (lane == 0)
       bwd_produce<D>(smem, sb,
         [&](int item, int* w) -> bool {
-          const int number = item / a.Hkv;               // early tiles, which most rows see, first
+          // Pinned tokens are seen by all that follow and cost most, so their tiles come first, by numbers of their own: a.pins
+          // per sequence.
+          int number = item / a.Hkv, tile;
           SeqView s;
-          int tile;
-          if (!seq_find(a, number, TM, &s, &tile)) return false;
+          const int own = a.pins * a.B;
+          if (number < own) {
+            const int b = number / a.pins;
+            tile = number - b * a.pins;
+            if (!seq_at_start(a, b, &s) || tile * TM >= min(s.pin, s.len)) return false;
+          } else {
+            if (!seq_find(a, number - own, TM, &s, &tile) || (a.pins > 0 && tile * TM < s.pin)) return false;
+          }
           const int j0 = tile * TM, last = j0 < s.pin ? s.len - 1 : s.last(min(j0 + TM, s.len) - 1);
-          w[B_START] = s.start; w[B_LEN] = s.len; w[B_PIN] = s.pin; w[B_CAP] = s.cap; w[B_E] = s.e; w[B_HEAD] = item - number * a.Hkv;
+          w[B_START] = s.start; w[B_LEN] = s.len; w[B_PIN] = s.pin; w[B_CAP] = s.cap; w[B_E] = s.e; w[B_HEAD] = item % a.Hkv;
           w[B_TILE] = tile; w[B_A] = last / TM - tile + 1; w[B_B] = w[B_C] = 0; w[B_N] = a.g * w[B_A];
           return true;
         },
@@ -721,14 +729,18 @@ cudaError_t bwd_launch(const SeqArgs& a, int dev, const CUtensorMap& q, const CU
   if (e != cudaSuccess) return e;
   e = tree_launch(k_seq_dq_tc<D>, dim3(numbers * a.Hq), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
   if (e != cudaSuccess) return e;
-  return tree_launch(k_seq_dkv_tc<D>, dim3(numbers * a.Hkv), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
+  return tree_launch(k_seq_dkv_tc<D>, dim3((numbers + (unsigned)(a.pins * a.B)) * a.Hkv), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
 }
 
 }  // namespace
 
-bool seq_backward_tc(const SeqArgs& a, int dtype, int dev, cudaStream_t st, cudaError_t* e) {
+bool seq_backward_tc(const SeqArgs& args, int dtype, int dev, cudaStream_t st, cudaError_t* e) {
+  SeqArgs a = args;
   const long long numbers = seq_numbers(a.n, a.B, TM);
-  if (dtype != PTENC_DTYPE_BF16 || a.D > 128 || numbers * a.Hq >= (1ll << 31)) return false;
+  // Most tiles that may be pinned; where there would be more numbers for them than for all the others, they are not set apart.
+  const long long pins = a.window > 0 && a.pinned != nullptr ? (a.window - 1 + TM - 1ll) / TM : 0;
+  a.pins = pins * a.B <= numbers ? (int)pins : 0;
+  if (dtype != PTENC_DTYPE_BF16 || a.D > 128 || 2 * numbers * a.Hq >= (1ll << 31)) return false;
   CUtensorMap q, k, v, g;
   if (!seq_map(&q, a.q, a.D, a.Hq, a.n, a.qs) || !seq_map(&k, a.k, a.D, a.Hkv, a.n, a.ks) || !seq_map(&v, a.v, a.D, a.Hkv, a.n, a.vs) ||
       !seq_map(&g, a.dout, a.D, a.Hq, a.n, (long long)a.Hq * a.D))

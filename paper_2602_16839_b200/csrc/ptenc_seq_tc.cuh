@@ -33,33 +33,51 @@ __device__ __forceinline__ int clc_answer(uint32_t at) {
   return x;
 }
 
-// Rows [row0, row0 + 128) of a 128-row tile of `cols` bf16 columns in shared memory: those past `rows` become zero, non-finite values
-// of the others too.  `me` of `of` warps.  True in every lane if something was taken out; bad (nullable): a bit per row it was.
+// Rows [row0, row0 + 128) of a 128-row tile of bf16 columns in shared memory: those past `rows` become zero, non-finite values of the
+// others too.  `me` of `of` warps.  True in every lane if something was taken out; bad (nullable): a bit per row it was.
+// A row's products with zero, added up, are NaN exactly if it holds an infinity or a NaN: four packed instructions per 16 bytes, so
+// that the pass hides under a tile's products (tested bit by bit it took 4000 cycles, more than they do, and bounded the kernels).
 __device__ __forceinline__ bool patch_tile(uint8_t* tile, int halves, int row0, int rows, int me, int of, uint32_t* bad) {
   const int lane = threadIdx.x & 31;
-  bool odd = false;
-  for (int x = me * 32 + lane; x < halves * TM * 8; x += of * 32) {
-    const int r = (x >> 3) & (TM - 1);
-    uint4* at = reinterpret_cast<uint4*>(tile + (x >> 10) * HALF + r * 128 + (x & 7) * 16);
-    if (row0 + r >= rows) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
-    uint4 w = *at;
-    uint32_t* e = reinterpret_cast<uint32_t*>(&w);
-    uint32_t top = 0;                                    // exponent bits all set, infinity or NaN, carry into the sign's place
+  auto place = [&](int x) { return reinterpret_cast<uint4*>(tile + (x >> 10) * HALF + ((x >> 3) & (TM - 1)) * 128 + (x & 7) * 16); };
+  const int total = halves * TM * 8;
+  if (row0 + TM > rows)
+    for (int x = me * 32 + lane; x < total; x += of * 32)
+      if (row0 + ((x >> 3) & (TM - 1)) >= rows) *place(x) = make_uint4(0u, 0u, 0u, 0u);
+  const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+  __nv_bfloat162 acc[2] = {zero, zero};
+  for (int x0 = me * 32 + lane; x0 < total; x0 += of * 32 * 8) {       // a multiple of eight steps: 512 or 1024 vectors per warp
+    uint4 w[8];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) top |= (e[y] & 0x7fff7fffu) + 0x00800080u;
-    if ((top & 0x80008000u) != 0) {
-      odd = true;
+    for (int k = 0; k < 8; ++k) w[k] = *place(x0 + k * of * 32);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&w[k]);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) acc[y & 1] = __hfma2(e[y], zero, acc[y & 1]);
+    }
+  }
+  acc[0] = __hadd2(acc[0], acc[1]);
+  const bool odd = __any_sync(0xffffffffu, !(__low2float(acc[0]) == 0.f) || !(__high2float(acc[0]) == 0.f));
+  if (odd) {
+#pragma unroll 1
+    for (int x = me * 32 + lane; x < total; x += of * 32) {
+      uint4 w = *place(x);
+      uint32_t* e = reinterpret_cast<uint32_t*>(&w);
+      bool hit = false;
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        if ((e[y] & 0x7f80u) == 0x7f80u) e[y] &= 0xffff0000u;
-        if ((e[y] & 0x7f800000u) == 0x7f800000u) e[y] &= 0x0000ffffu;
+        if ((e[y] & 0x7f80u) == 0x7f80u) { e[y] &= 0xffff0000u; hit = true; }
+        if ((e[y] & 0x7f800000u) == 0x7f800000u) { e[y] &= 0x0000ffffu; hit = true; }
       }
-      *at = w;
-      if (bad != nullptr) atomicOr(bad + (r >> 5), 1u << (r & 31));
+      if (hit) {
+        *place(x) = w;
+        if (bad != nullptr) atomicOr(bad + ((x >> 8) & 3), 1u << ((x >> 3) & 31));
+      }
     }
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  return __any_sync(0xffffffffu, odd);
+  return odd;
 }
 
 // ------------------------------------------------------------------------------------------------ host
