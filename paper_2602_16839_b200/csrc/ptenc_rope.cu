@@ -3,14 +3,21 @@
 //   n = x / sqrt(mean(x^2) + eps),  y = w n,  (a, b) -> (a cos - b sin, b cos + a sin)  for each pair of the rotated values.
 // Backward, with g the gradient turned back by the same angles (a rotation's inverse is its transpose):
 //   dw = sum g n,  dx = (w g - n mean(w g n)) / sqrt(mean(x^2) + eps).
+//
+// Bound by memory: every value is read and written once, a few operations each.  A CTA takes a few tokens with all their query heads
+// or all their key heads: the angles of a token, in 64 bits, are worked out once for all of them, in the shadow of the first loads.  A head is a group of lanes
+// (a power of two) with two 16-byte vectors each, chosen so that both values of a pair are in the same lane.
 #include <string.h>
 
+#include "ptenc_tc.cuh"
 #include "ptenc_tree.cuh"
 
 namespace {
 
 constexpr int RP_MAX_D = 256;
 constexpr int RP_BLOCKS = 592;                   // most CTAs of a backward launch, each with a partial sum of dw
+constexpr int RP_THREADS = 256;
+constexpr int RP_TOK = 8;                        // most tokens of a CTA at a time
 constexpr int RP_WARPS = 8;
 
 struct RopeArgs {
@@ -30,11 +37,18 @@ struct RopeArgs {
 };
 
 // Cosine and sine of pos * freq.  The product is taken in 64 bits and brought to a fraction of a turn there: in 32 bits the
-// angle of position 60000 would be off by 2e-3.
-__device__ __forceinline__ void rp_angle(int pos, float freq, float* s, float* c) {
+// angle of position 60000 would be off by 2e-3.  `fast`: the hardware's sine and cosine, off by 2^-20.5 at most within half a turn, for
+// results that are rounded to bf16 (2^-8) anyhow.
+__device__ __forceinline__ void rp_angle(int pos, float freq, float* s, float* c, bool fast) {
   double t = (double)pos * (double)freq * 0.15915494309189533577;
   t -= rint(t);
-  sincospif(2.f * (float)t, s, c);
+  if (fast) {
+    const float x = (float)t * 6.2831853071795864769f;
+    *s = __sinf(x);
+    *c = __cosf(x);
+  } else {
+    sincospif(2.f * (float)t, s, c);
+  }
 }
 
 __device__ __forceinline__ float rp_sum(float v) {
@@ -92,7 +106,7 @@ k_rope_any(const __grid_constant__ RopeArgs a) {
           const bool second = a.inter ? (d & 1) != 0 : d >= half;
           const float other = row[a.inter ? d ^ 1 : (second ? d - half : d + half)];
           float sn, cs;
-          rp_angle(pos, a.freq[f], &sn, &cs);
+          rp_angle(pos, a.freq[f], &sn, &cs, false);
           if (BWD) sn = -sn;
           g[i] = fmaf(g[i], cs, second ? other * sn : -other * sn);
         }
@@ -136,19 +150,236 @@ k_rope_any(const __grid_constant__ RopeArgs a) {
   }
 }
 
-// dw of both sides: the CTAs' partial sums, added in order, eight groups of CTAs at a time.
-__global__ void __launch_bounds__(256)
+// ------------------------------------------------------------------------------------------------ vectors
+struct RopeShape {
+  int lanes;                                     // of a head: a power of two up to 32
+  int tok[2];                                    // tokens of a CTA at a time, of the queries' and the keys' CTAs
+  unsigned inv[2];                               // ceil(2^32 / heads): x / heads = umulhi(x, inv) for x heads < 2^32
+};
+
+template <typename T> struct RpVec { static constexpr int N = 16 / sizeof(T); };
+
+// A vector's values, two to a register pair, for packed arithmetic: taken one by one the kernel was bound by its instructions.
+__device__ __forceinline__ void rp_unpack(const uint4& w, uint64_t (&f)[8], int at, __nv_bfloat16) {
+  const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int y = 0; y < 4; ++y) f[at + y] = tt_two(__uint_as_float(e[y] << 16), __uint_as_float(e[y] & 0xffff0000u));
+}
+__device__ __forceinline__ void rp_unpack(const uint4& w, uint64_t (&f)[4], int at, float) {
+  f[at] = tt_two(__uint_as_float(w.x), __uint_as_float(w.y));
+  f[at + 1] = tt_two(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+__device__ __forceinline__ uint4 rp_pack(const uint64_t (&f)[8], int at, __nv_bfloat16) {
+  uint32_t e[4];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    float lo, hi;
+    tt_both(f[at + y], lo, hi);
+    e[y] = tt_pack(lo, hi);
+  }
+  return make_uint4(e[0], e[1], e[2], e[3]);
+}
+__device__ __forceinline__ uint4 rp_pack(const uint64_t (&f)[4], int at, float) {
+  float a, b, c, d;
+  tt_both(f[at], a, b);
+  tt_both(f[at + 1], c, d);
+  return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+}
+__device__ __forceinline__ uint64_t rp_mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float rp_group_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Lane l of a head holds pairs N l .. N l + N - 1 (N = values of a vector) as vectors va and vb: with halves as pairs the same place
+// in both halves, and behind those lanes values that are not rotated, two vectors each; with neighbours as pairs two vectors in a row.
+template <typename T, bool BWD, bool INTER>
+__global__ void __launch_bounds__(RP_THREADS, BWD ? 3 : 4)
+k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh) {
+  constexpr int N = RpVec<T>::N, U = 2;                  // items of a group in flight
+  extern __shared__ __align__(16) float s_trig[];        // [2][tok][cos, sin][lanes * N]
+  __shared__ float s_sum[RP_THREADS / 32][RP_MAX_D];
+  const int tid = threadIdx.x, l = tid & (sh.lanes - 1), groups = RP_THREADS / sh.lanes, grp = tid / sh.lanes;
+  const int D = a.D, half = a.rot >> 1, nv = D / N, P = half / N, np = sh.lanes * N;
+  const int va = INTER || l >= P ? 2 * l : l, vb = INTER || l >= P ? 2 * l + 1 : l + P;
+  const bool ha = va < nv, hb = vb < nv;
+  const bool turns = N * l < half;                       // some of the lane's pairs are rotated: all of them, with halves
+  const float rD = 1.f / (float)D;
+  const int side = blockIdx.y, H = side ? a.Hkv : a.Hq, tok = sh.tok[side];
+  const unsigned inv_h = sh.inv[side];
+  const T* w = static_cast<const T*>(a.w[side]);
+  const bool norm = w != nullptr, need_x = !BWD || norm;
+  const T* X = static_cast<const T*>(a.x[side]);
+  const T* G = static_cast<const T*>(a.g[side]);
+  T* Y = static_cast<T*>(a.y[side]);
+  const long long xs = a.xs[side], gs = a.gs[side], ys = a.ys[side];
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  uint64_t dw[N], w2[N];
+#pragma unroll
+  for (int y = 0; y < N; ++y) dw[y] = w2[y] = 0ull;
+  tree_after_previous();
+  if (norm) {
+    rp_unpack(ha ? reinterpret_cast<const uint4*>(w)[va] : zero, w2, 0, T());
+    rp_unpack(hb ? reinterpret_cast<const uint4*>(w)[vb] : zero, w2, N / 2, T());
+  }
+  int turn = 0;
+  for (long long t0 = (long long)blockIdx.x * tok; t0 < a.n; t0 += (long long)gridDim.x * tok, turn ^= 1) {
+    const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
+    float* trig = s_trig + turn * tok * 2 * np;
+    // every group takes the same number of steps: the sums go over whole warps
+    for (int it0 = 0; it0 < items; it0 += groups * U) {
+      uint4 x[U][2], g[U][2];
+      int tt[U], hd[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int it = it0 + u * groups + grp;
+        tt[u] = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h);
+        hd[u] = it - tt[u] * H;
+        const bool on = it < items;
+        x[u][0] = x[u][1] = g[u][0] = g[u][1] = zero;
+        if (need_x && on) {
+          const uint4* from = reinterpret_cast<const uint4*>(X + (t0 + tt[u]) * xs + (long long)hd[u] * D);
+          if (ha) x[u][0] = from[va];
+          if (hb) x[u][1] = from[vb];
+        }
+        if (BWD && on) {
+          const uint4* from = reinterpret_cast<const uint4*>(G + (t0 + tt[u]) * gs + (long long)hd[u] * D);
+          if (ha) g[u][0] = from[va];
+          if (hb) g[u][1] = from[vb];
+        }
+      }
+      if (it0 == 0) {
+        // cosines and sines of the CTA's tokens; the other copy may still be read
+        for (int i = tid; i < toks * half; i += RP_THREADS) {
+          const int t = i / half, p = i - t * half;
+          float sn, cs;
+          rp_angle(a.pos[t0 + t], a.freq[p], &sn, &cs, sizeof(T) == 2);
+          // four pairs of a lane next to each other, the lanes behind one another: 16-byte reads without bank conflicts
+          const int at = t * 2 * np + (p / N) * 4 + (p & 3) + (N == 8 ? ((p >> 2) & 1) * (np / 2) : 0);
+          trig[at] = cs;
+          trig[at + np] = sn;
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool on = it0 + u * groups + grp < items;
+        uint64_t v[N], o[N];
+        float inv = 1.f;
+        if (need_x) {
+          rp_unpack(x[u][0], v, 0, T());
+          rp_unpack(x[u][1], v, N / 2, T());
+          if (norm) {
+            uint64_t sq = 0ull;
+#pragma unroll
+            for (int y = 0; y < N; ++y) sq = tt_fma2(v[y], v[y], sq);
+            float lo, hi;
+            tt_both(sq, lo, hi);
+            inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);
+            const uint64_t inv2 = tt_two(inv, inv);
+#pragma unroll
+            for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
+          }
+        }
+        if (BWD) {
+          rp_unpack(g[u][0], o, 0, T());
+          rp_unpack(g[u][1], o, N / 2, T());
+        } else {
+#pragma unroll
+          for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
+        }
+        if (turns && on) {
+          const float* at = trig + tt[u] * 2 * np + l * 4;
+#pragma unroll
+          for (int q = 0; q < N; q += 4) {
+            const float4 c4 = *reinterpret_cast<const float4*>(at + q / 4 * (np / 2));
+            float4 s4 = *reinterpret_cast<const float4*>(at + np + q / 4 * (np / 2));
+            if (BWD) s4 = make_float4(-s4.x, -s4.y, -s4.z, -s4.w);
+            if (INTER) {
+              const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+              for (int y = q; y < q + 4; ++y) {
+                if (N * l + y >= half) continue;
+                float p, r;
+                tt_both(o[y], p, r);
+                o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int i = q / 2 + k, j = i + N / 2;
+                const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
+                const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
+                const uint64_t p = o[i], r = o[j];
+                o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
+                o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
+              }
+            }
+          }
+        }
+        if (BWD && norm) {
+          uint64_t dot2 = 0ull;
+#pragma unroll
+          for (int y = 0; y < N; ++y) {
+            dw[y] = tt_fma2(o[y], v[y], dw[y]);
+            o[y] = rp_mul2(o[y], w2[y]);
+            dot2 = tt_fma2(o[y], v[y], dot2);
+          }
+          float lo, hi;
+          tt_both(dot2, lo, hi);
+          const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
+          const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
+#pragma unroll
+          for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
+        }
+        if (on) {
+          uint4* to = reinterpret_cast<uint4*>(Y + (t0 + tt[u]) * ys + (long long)hd[u] * D);
+          if (ha) to[va] = rp_pack(o, 0, T());
+          if (hb) to[vb] = rp_pack(o, N / 2, T());
+        }
+      }
+    }
+  }
+  if (BWD && a.part != nullptr) {
+    // groups of a warp, then the warps, in a fixed order
+#pragma unroll
+    for (int y = 0; y < 2 * N; ++y) {
+      float lo, hi;
+      tt_both(dw[y >> 1], lo, hi);
+      float v = (y & 1) ? hi : lo;
+      for (int o = 16; o >= sh.lanes; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      const int at = (y < N ? va : vb) * N + (y & (N - 1));
+      if ((tid & 31) < sh.lanes && (y < N ? ha : hb)) s_sum[tid >> 5][at] = v;
+    }
+    __syncthreads();
+    for (int d = tid; d < D; d += RP_THREADS) {
+      float sum = 0.f;
+      for (int k = 0; k < RP_THREADS / 32; ++k) sum += s_sum[k][d];
+      a.part[((size_t)blockIdx.x * 2 + side) * D + d] = sum;
+    }
+  }
+}
+
+// dw of both sides: the CTAs' partial sums, each thread those of every 32nd CTA in order, then the threads of a column in order.
+__global__ void __launch_bounds__(1024)
 k_rope_weights(const float* __restrict__ part, int blocks, int D, float* dwq, float* dwk) {
-  __shared__ double s[8][32];
+  __shared__ double s[32][33];
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   tree_after_previous();
   double sum = 0.0;
-  if (c < 2 * D)
-    for (int b = grp; b < blocks; b += 8) sum += (double)part[(size_t)b * 2 * D + c];
+  if (c < 2 * D) {
+#pragma unroll 8
+    for (int b = grp; b < blocks; b += 32) sum += (double)part[(size_t)b * 2 * D + c];
+  }
   s[grp][lane] = sum;
   __syncthreads();
   if (grp == 0 && c < 2 * D) {
-    for (int k = 1; k < 8; ++k) sum += s[k][lane];
+    sum = 0.0;
+    for (int k = 0; k < 32; ++k) sum += s[k][lane];
     float* to = c < D ? dwq : dwk;
     if (to != nullptr) to[c < D ? c : c - D] = (float)sum;
   }
@@ -178,13 +409,41 @@ int check_stride(long long stride, int heads, int D, int dtype) {
 
 template <typename T, bool BWD>
 cudaError_t rope_launch(const RopeArgs& a, int sms, float* dwq, float* dwk, cudaStream_t st) {
-  const long long items = a.n * (a.Hq + a.Hkv);
-  const long long want = (items + RP_WARPS - 1) / RP_WARPS;
-  const int grid = (int)(want < RP_BLOCKS ? want : RP_BLOCKS);
-  (void)sms;
-  cudaError_t e = tree_launch(k_rope_any<T, BWD>, dim3(grid), 32 * RP_WARPS, 0, 0, st, a);
+  const int N = 16 / (int)sizeof(T), H = a.Hq + a.Hkv;
+  cudaError_t e;
+  int grid;
+  if (!a.inter && (a.rot / 2) % N != 0) {
+    // halves that do not start on a vector
+    const long long want = (a.n * H + RP_WARPS - 1) / RP_WARPS;
+    grid = (int)(want < RP_BLOCKS ? want : RP_BLOCKS);
+    e = tree_launch(k_rope_any<T, BWD>, dim3(grid), 32 * RP_WARPS, 0, 0, st, a);
+  } else {
+    RopeShape sh;
+    const int pairs = (a.D / N + 1) / 2;
+    for (sh.lanes = 1; sh.lanes < pairs; sh.lanes *= 2) {}
+    // Tokens of a CTA: as many as its groups have in flight, fewer where that would leave SMs without work.
+    const int fly = RP_THREADS / sh.lanes * 2;
+    long long want = 0;
+    for (int side = 0; side < 2; ++side) {
+      const int heads = side ? a.Hkv : a.Hq;
+      int tok = fly / heads;
+      if (tok > RP_TOK) tok = RP_TOK;
+      while (tok > 1 && a.n / tok < 4ll * sms) tok /= 2;
+      sh.tok[side] = tok < 1 ? 1 : tok;
+      sh.inv[side] = heads > 1 ? (unsigned)(((1ull << 32) + heads - 1) / heads) : 0u;
+      const long long ctas = (a.n + sh.tok[side] - 1) / sh.tok[side];
+      if (ctas > want) want = ctas;
+    }
+    // forward: a CTA per step, so that one's loads run under another's stores; backward: as many CTAs as stay resident, for fewer
+    // partial sums of dw
+    const long long most = BWD ? (3ll * sms < RP_BLOCKS ? 3ll * sms : RP_BLOCKS) : (1ll << 30);
+    grid = (int)(want < most ? want : most);
+    const int tok = sh.tok[0] > sh.tok[1] ? sh.tok[0] : sh.tok[1];
+    const size_t smem = (size_t)2 * tok * 2 * sh.lanes * N * sizeof(float);
+    e = tree_launch(a.inter ? k_rope<T, BWD, true> : k_rope<T, BWD, false>, dim3(grid, 2), RP_THREADS, smem, 0, st, a, sh);
+  }
   if (e != cudaSuccess || !BWD || a.part == nullptr) return e;
-  return tree_launch(k_rope_weights, dim3((2 * a.D + 31) / 32), 256, 0, 0, st, (const float*)a.part, grid, a.D, dwq, dwk);
+  return tree_launch(k_rope_weights, dim3((2 * a.D + 31) / 32), 1024, 0, 0, st, (const float*)a.part, grid, a.D, dwq, dwk);
 }
 
 template <bool BWD>
