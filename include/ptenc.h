@@ -340,8 +340,8 @@ typedef struct {
  *   loss = sum over t of weight[t] loss_t,  dlogits[t] = weight[t] (d loss_t / d lp) (onehot - softmax) / temperature,
  * where a ratio beyond the clip border on the side that A favours has no gradient of the first term.  Other tokens: their logits
  * are not read (whatever they hold), logp, token_loss and token_kl are 0 and the row of dlogits is zero.
- *   logits, dlogits [n, vocab] with strides of at least vocab elements, the pointers 16-byte aligned, the rows need not be; dlogits
- * may be logits (then the strides are equal), or NULL: no gradient.  tokens [n] int32; old_logp, ref_logp, advantage, weight [n]
+ *   logits, dlogits [n, vocab], n below 2^28, with strides of at least vocab elements, the pointers 16-byte aligned, the rows need not
+ * be; dlogits may be logits (then the strides are equal), or NULL: no gradient.  tokens [n] int32; old_logp, ref_logp, advantage, weight [n]
  * fp32; old_logp, ref_logp, weight (NULL = 1) nullable.  advantage NULL: only logp is wanted (the log-probabilities of the policy
  * that samples, or of the reference), and everything but tokens, weight and logp is to be NULL.  Outputs logp [n], token_loss
  * [n] (the loss_t; required with loss), token_kl [n] (the KL estimate without kl_coef; 0 without ref_logp), loss [1], all fp32,

@@ -2,11 +2,25 @@
 //
 // Per token: lp = z_y / T - log sum exp(z / T), r = exp(lp - old), loss = -min(r A, clip(r) A) + beta (exp(ref - lp) - (ref - lp) - 1),
 // d loss / d z_x = (d loss / d lp) / T * ((x == y) - softmax_x).
+//
+// Bound by memory: a row is read once and its gradient written once.  A row's maximum and sum have to be known before any of its
+// gradient is, so the row stays in shared memory in between: a cluster of one to eight CTAs per row holds a slice each (bulk copies
+// in four chunks, the maximum and the sum of a chunk while the next ones arrive), exchanges (maximum, sum) through distributed shared
+// memory, works the loss out in 64 bits, and writes the gradient from shared memory.  Rows need not be aligned: the values in front of
+// the first and behind the last 16-byte boundary are held by the first CTA's threads, one each.  Rows that eight CTAs cannot hold
+// are read twice.
+#include <cooperative_groups.h>
+
+#include "ptenc_tc.cuh"
 #include "ptenc_tree.cuh"
 
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int PL_THREADS = 256;
+constexpr int PL_CHUNKS = 4;
+constexpr int PL_SLICE = 112 * 1024;             // most bytes of a row in a CTA: two CTAs per SM
 
 struct PolicyArgs {
   const void* z;
@@ -53,6 +67,7 @@ __device__ __forceinline__ PolicyRow pl_row(const PolicyArgs& a, long long t, do
   return o;
 }
 
+// Rows of any width, read from memory three times.
 template <typename T>
 __global__ void __launch_bounds__(PL_THREADS)
 k_policy_row(const __grid_constant__ PolicyArgs a) {
@@ -84,9 +99,9 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   if (lane == 0) s_m[warp] = m;
   __syncthreads();
   for (int i = 0; i < PL_THREADS / 32; ++i) m = fmaxf(m, s_m[i]);
-  const float mc = m * a.c2;
+  const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
-  for (int x = tid; x < a.V; x += PL_THREADS) l += exp2f(fmaf(ptenc_to_float(z[x]), a.c2, -mc));
+  for (int x = tid; x < a.V; x += PL_THREADS) l += exp2f((ptenc_to_float(z[x]) - ref) * a.c2);
   l = nan ? __int_as_float(0x7fffffff) : l;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -95,7 +110,7 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   l = 0.f;
   for (int i = 0; i < PL_THREADS / 32; ++i) l += s_l[i];
   if (tid == 0) {
-    const double lp = ((double)zy * (double)a.c2 - (double)mc - log2((double)l)) * 0.69314718055994530942;
+    const double lp = (((double)zy - (double)ref) * (double)a.c2 - log2((double)l)) * 0.69314718055994530942;
     const PolicyRow o = pl_row(a, t, lp, w);
     a.logp[t] = o.lp;
     if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
@@ -106,10 +121,251 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   __syncthreads();                                       // also: everybody has read the row before it may be overwritten
   const float grad = s_out[0], scale = -grad / l;
   for (int x = tid; x < a.V; x += PL_THREADS) {
-    float v = exp2f(fmaf(ptenc_to_float(z[x]), a.c2, -mc)) * scale;
+    float v = exp2f((ptenc_to_float(z[x]) - ref) * a.c2) * scale;
     if (x == y) v += grad;
     dz[x] = ptenc_from_float<T>(v);
   }
+}
+
+// ------------------------------------------------------------------------------------------------ a row per cluster
+__device__ __forceinline__ void pl_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// A vector's values, two to a register pair.
+__device__ __forceinline__ void pl_unpack(const uint4& w, uint64_t (&f)[4], __nv_bfloat16) {
+  const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int y = 0; y < 4; ++y) f[y] = tt_two(__uint_as_float(e[y] << 16), __uint_as_float(e[y] & 0xffff0000u));
+}
+__device__ __forceinline__ void pl_unpack(const uint4& w, uint64_t (&f)[2], float) {
+  f[0] = tt_two(__uint_as_float(w.x), __uint_as_float(w.y));
+  f[1] = tt_two(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+__device__ __forceinline__ uint4 pl_pack(const float (&f)[8], __nv_bfloat16) {
+  return make_uint4(tt_pack(f[0], f[1]), tt_pack(f[2], f[3]), tt_pack(f[4], f[5]), tt_pack(f[6], f[7]));
+}
+__device__ __forceinline__ uint4 pl_pack(const float (&f)[4], float) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+// A vector's largest value, not counting NaN.
+__device__ __forceinline__ float pl_max(const uint4& w, __nv_bfloat16) {
+  const __nv_bfloat162* e = reinterpret_cast<const __nv_bfloat162*>(&w);
+  const __nv_bfloat162 m = __hmax2(__hmax2(e[0], e[1]), __hmax2(e[2], e[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float pl_max(const uint4& w, float) {
+  return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+}
+__device__ __forceinline__ uint64_t pl_mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// 2^((z - ref) c2) of two values.  The difference comes first: ref c2 would pass the range of fp32 in a row of the type's lowest values.
+__device__ __forceinline__ void pl_weights(uint64_t z, uint64_t neg_ref, uint64_t c2, float& lo, float& hi) {
+  tt_both(pl_mul2(tt_add2(z, neg_ref), c2), lo, hi);
+  lo = tt_ex2(lo);
+  hi = tt_ex2(hi);
+}
+// Running maximum and sum of 2^((z - ref) c2), ref the maximum, 0 while nothing but -inf has been seen.
+struct PlSum {
+  float m, l;
+  __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }
+  __device__ __forceinline__ void grow(float mn, float c2) {
+    if (mn > m) {
+      l = l == 0.f ? 0.f : l * tt_ex2((ref() - mn) * c2);          // NaN stays
+      m = mn;
+    }
+  }
+  __device__ __forceinline__ void join(float om, float ol, float c2) {
+    const PlSum o = {om, ol};
+    const float mn = fmaxf(m, om), to = mn == -INFINITY ? 0.f : mn;
+    l = (l == 0.f ? 0.f : l * tt_ex2((ref() - to) * c2)) + (ol == 0.f ? 0.f : ol * tt_ex2((o.ref() - to) * c2));
+    m = mn;
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(PL_THREADS)
+k_policy(const __grid_constant__ PolicyArgs a) {
+  constexpr int N = 16 / sizeof(T);
+  extern __shared__ __align__(16) uint8_t s_row[];
+  __shared__ __align__(8) uint64_t s_bar[PL_CHUNKS];
+  __shared__ float2 s_part[PL_THREADS / 32], s_all;      // s_all: read by the cluster
+  __shared__ float s_out[3];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const long long t = blockIdx.x / cs;
+  const uint32_t bar = tt_u32(s_bar);
+  if (tid == 0) {
+    for (int c = 0; c < PL_CHUNKS; ++c) bar_init(bar + 8 * c, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tree_after_previous();
+  const int y = a.tok[t];
+  const float w = a.weight != nullptr ? a.weight[t] : 1.f;
+  const T* z = static_cast<const T*>(a.z) + t * a.zs;
+  T* dz = a.dz != nullptr ? static_cast<T*>(a.dz) + t * a.dzs : nullptr;
+  // values [0, head) and [head + N nv, V) lie outside the row's 16-byte vectors; this CTA's vectors are [v0, v0 + mine)
+  const int off = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T)), head = min(a.V, off == 0 ? 0 : N - off);
+  const int nv = (a.V - head) / N, per = (nv + cs - 1) / cs, v0 = min(nv, rank * per), mine = min(per, nv - v0);
+  const int loose = a.V - N * nv, lx = tid < head ? tid : tid + N * nv;        // this thread's value outside them: index lx
+  const bool has = rank == 0 && tid < loose;
+  const bool same = dz != nullptr && ((reinterpret_cast<uintptr_t>(dz) ^ reinterpret_cast<uintptr_t>(z)) & 15) == 0;
+  const T* body = z + head + (long long)N * v0;
+  if (w == 0.f || y < 0 || y >= a.V) {                   // the whole cluster agrees
+    if (rank == 0 && tid == 0) {
+      a.logp[t] = 0.f;
+      if (a.token_loss != nullptr) a.token_loss[t] = 0.f;
+      if (a.token_kl != nullptr) a.token_kl[t] = 0.f;
+    }
+    if (dz != nullptr) {
+      if (has) dz[lx] = ptenc_from_float<T>(0.f);
+      T* to = dz + head + (long long)N * v0;
+      if (same)
+        for (int v = tid; v < mine; v += PL_THREADS) reinterpret_cast<uint4*>(to)[v] = make_uint4(0u, 0u, 0u, 0u);
+      else
+        for (int x = tid; x < mine * N; x += PL_THREADS) to[x] = ptenc_from_float<T>(0.f);
+    }
+    return;
+  }
+  const int chunk = (mine + PL_CHUNKS - 1) / PL_CHUNKS;
+  if (tid == 0) {
+    for (int c = 0; c < PL_CHUNKS; ++c) {
+      const int first = min(mine, c * chunk), count = min(chunk, mine - first);
+      if (count == 0) continue;
+      bar_expect(bar + 8 * c, (uint32_t)count * 16);
+      pl_bulk(tt_u32(s_row) + (uint32_t)first * 16, body + (long long)N * first, (uint32_t)count * 16, bar + 8 * c);
+    }
+  }
+  const float zy = ptenc_to_float(z[y]);
+  const float zl = has ? ptenc_to_float(z[lx]) : -INFINITY;
+  const float c2 = a.c2;
+  const uint64_t c22 = tt_two(c2, c2);
+  PlSum sum = {-INFINITY, 0.f};
+  if (has) {
+    sum.grow(zl, c2);
+    sum.l += tt_ex2((zl - sum.ref()) * c2);
+  }
+  __syncthreads();                                       // the barriers are there
+  bool late = false;
+  const uint4* row = reinterpret_cast<const uint4*>(s_row);
+  for (int c = 0; c < PL_CHUNKS; ++c) {
+    const int first = min(mine, c * chunk), end = min(mine, first + chunk);
+    if (first == end) continue;
+    bool there = false;
+    for (uint32_t i = 0; i < TT_POLLS && !there; ++i) there = bar_try(bar + 8 * c, 0) != 0;
+    late |= !there;
+    int v = first + tid;
+    // four vectors at a time: their maximum, then their weights
+    for (; v + 3 * PL_THREADS < end; v += 4 * PL_THREADS) {
+      uint4 r[4];
+      float mx[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { r[k] = row[v + k * PL_THREADS]; mx[k] = pl_max(r[k], T()); }
+      sum.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), c2);
+      const float nr = -sum.ref();
+      const uint64_t nr2 = tt_two(nr, nr);
+      uint64_t add[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint64_t f[N / 2];
+        pl_unpack(r[k], f, T());
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+          float lo, hi;
+          pl_weights(f[e], nr2, c22, lo, hi);
+          add[k] = tt_add2(add[k], tt_two(lo, hi));
+        }
+      }
+      float lo, hi;
+      tt_both(tt_add2(tt_add2(add[0], add[1]), tt_add2(add[2], add[3])), lo, hi);
+      sum.l += lo + hi;
+    }
+    for (; v < end; v += PL_THREADS) {
+      const uint4 r = row[v];
+      sum.grow(pl_max(r, T()), c2);
+      const float nr = -sum.ref();
+      const uint64_t nr2 = tt_two(nr, nr);
+      uint64_t f[N / 2], add = 0ull;
+      pl_unpack(r, f, T());
+      float lo, hi;
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e) {
+        pl_weights(f[e], nr2, c22, lo, hi);
+        add = tt_add2(add, tt_two(lo, hi));
+      }
+      tt_both(add, lo, hi);
+      sum.l += lo + hi;
+    }
+  }
+  if (late) sum.l = __int_as_float(0x7fffffff);          // a copy that did not come: the row becomes NaN
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    sum.join(__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.l, o), c2);
+  if (lane == 0) s_part[warp] = make_float2(sum.m, sum.l);
+  __syncthreads();
+  sum.m = s_part[0].x; sum.l = s_part[0].y;
+#pragma unroll
+  for (int i = 1; i < PL_THREADS / 32; ++i) sum.join(s_part[i].x, s_part[i].y, c2);
+  if (cs > 1) {
+    if (tid == 0) s_all = make_float2(sum.m, sum.l);
+    cluster.sync();                                      // also: every CTA has read what it needs of the row
+  }
+  if (tid == 0) {
+    if (cs > 1) {
+      const float2 f = *cluster.map_shared_rank(&s_all, 0);
+      sum.m = f.x; sum.l = f.y;
+      for (int i = 1; i < cs; ++i) {                     // in the same order everywhere
+        const float2 o = *cluster.map_shared_rank(&s_all, i);
+        sum.join(o.x, o.y, c2);
+      }
+    }
+    const double lp = (((double)zy - (double)sum.ref()) * (double)c2 - log2((double)sum.l)) * 0.69314718055994530942;
+    const PolicyRow o = pl_row(a, t, lp, w);
+    if (rank == 0) {
+      a.logp[t] = o.lp;
+      if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
+      if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
+    }
+    s_out[0] = -sum.ref(); s_out[1] = o.grad; s_out[2] = -o.grad / sum.l;
+  }
+  if (cs > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");      // nobody leaves while its sum may be read
+  __syncthreads();
+  if (dz != nullptr) {
+    const float nr = s_out[0], grad = s_out[1], scale = s_out[2];
+    const uint64_t nr2 = tt_two(nr, nr);
+    if (has) dz[lx] = ptenc_from_float<T>(fmaf(tt_ex2((zl + nr) * c2), scale, lx == y ? grad : 0.f));
+    const int yb = y - head - N * v0;                    // where y lies in this CTA's slice
+    T* to = dz + head + (long long)N * v0;
+    if (same) {
+#pragma unroll 2
+      for (int v = tid; v < mine; v += PL_THREADS) {
+        uint64_t x[N / 2];
+        float f[N];
+        pl_unpack(row[v], x, T());
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          pl_weights(x[e >> 1], nr2, c22, f[e], f[e + 1]);
+          f[e] *= scale;
+          f[e + 1] *= scale;
+        }
+        if ((unsigned)(yb - N * v) < (unsigned)N) {      // one vector of the row
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (yb - N * v == e) f[e] = fmaf(tt_ex2((zy + nr) * c2), scale, grad);
+        }
+        reinterpret_cast<uint4*>(to)[v] = pl_pack(f, T());
+      }
+    } else {
+      const T* from = reinterpret_cast<const T*>(s_row);
+      for (int x = tid; x < mine * N; x += PL_THREADS)
+        to[x] = ptenc_from_float<T>(fmaf(tt_ex2((ptenc_to_float(from[x]) + nr) * c2), scale, x == yb ? grad : 0.f));
+    }
+  }
+  if (cs > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // loss = sum of weight * token_loss, every thread its tokens in order, then the threads in a fixed tree.
@@ -135,8 +391,21 @@ k_policy_sum(const float* __restrict__ token_loss, const float* __restrict__ wei
 }
 
 template <typename T>
-cudaError_t policy_launch(const PolicyArgs& a, float* loss, cudaStream_t st) {
-  cudaError_t e = tree_launch(k_policy_row<T>, dim3((unsigned)a.n), PL_THREADS, 0, 0, st, a);
+cudaError_t policy_launch(const PolicyArgs& a, float* loss, int dev, int sms, cudaStream_t st) {
+  const long long row = (long long)a.V * sizeof(T);
+  int cs = 1;
+  // A slice of at most a third of an SM's shared memory, so that one row's copies run under another's arithmetic; smaller ones, down to
+  // 16 KB, while the call has too few rows to fill the SMs.
+  while (cs < 8 && (row > cs * 72ll * 1024 || (row > cs * 32ll * 1024 && a.n * cs * 2 <= 4ll * sms))) cs *= 2;
+  cudaError_t e;
+  if (row > 8ll * PL_SLICE) {
+    e = tree_launch(k_policy_row<T>, dim3((unsigned)a.n), PL_THREADS, 0, 0, st, a);
+  } else {
+    static PtencOnce once;
+    e = ptenc_first_use(once, dev, [] { return ptenc_allow_smem(k_policy<T>, PL_SLICE + 64); });
+    const size_t smem = (size_t)((row / 16 + cs - 1) / cs * 16);
+    if (e == cudaSuccess) e = tree_launch(k_policy<T>, dim3((unsigned)(a.n * cs)), PL_THREADS, smem, cs, st, a);
+  }
   if (e != cudaSuccess || loss == nullptr) return e;
   return tree_launch(k_policy_sum, dim3(1), 1024, 0, 0, st, (const float*)a.token_loss, a.weight, a.n, loss);
 }
@@ -153,7 +422,7 @@ extern "C" int ptenc_policy_loss(const ptenc_policy_config* cfg, const void* log
   if (cfg == nullptr || n_tokens < 0) return PTENC_EINVAL;
   if (cfg->dtype != PTENC_DTYPE_FP32 && cfg->dtype != PTENC_DTYPE_BF16) return PTENC_EINVAL;
   if (cfg->vocab < 1 || !(cfg->temperature > 0.f) || cfg->temperature > 3e38f) return PTENC_EINVAL;
-  if (cfg->vocab > (1 << 28) || n_tokens >= (1ll << 31) - 512) return PTENC_ESHAPE;
+  if (cfg->vocab > (1 << 28) || n_tokens >= (1ll << 28)) return PTENC_ESHAPE;
   if (advantage != nullptr && (!(cfg->clip_low >= 0.f) || !(cfg->clip_high >= 0.f))) return PTENC_EINVAL;
   if (advantage != nullptr && ref_logp != nullptr && !(cfg->kl_coef >= 0.f)) return PTENC_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -181,6 +450,10 @@ extern "C" int ptenc_policy_loss(const ptenc_policy_config* cfg, const void* log
   a.clip_low = cfg->clip_low; a.clip_high = cfg->clip_high; a.kl = cfg->kl_coef;
   a.logp = logp; a.token_loss = token_loss; a.token_kl = token_kl; a.dz = dlogits; a.dzs = dlogits_stride;
   ptenc_drop_old_error();
-  const cudaError_t e = cfg->dtype == PTENC_DTYPE_FP32 ? policy_launch<float>(a, loss, st) : policy_launch<__nv_bfloat16>(a, loss, st);
+  int dev = -1, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return PTENC_ECUDA;
+  const cudaError_t e = cfg->dtype == PTENC_DTYPE_FP32 ? policy_launch<float>(a, loss, dev, sms, st)
+                                                       : policy_launch<__nv_bfloat16>(a, loss, dev, sms, st);
   return e == cudaSuccess ? PTENC_OK : PTENC_ECUDA;
 }

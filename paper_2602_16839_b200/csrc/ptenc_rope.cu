@@ -5,7 +5,8 @@
 //   dw = sum g n,  dx = (w g - n mean(w g n)) / sqrt(mean(x^2) + eps).
 //
 // Bound by memory: every value is read and written once, a few operations each.  A CTA takes a few tokens with all their query heads
-// or all their key heads: the angles of a token, in 64 bits, are worked out once for all of them, in the shadow of the first loads.  A head is a group of lanes
+// or all their key heads at a step; their angles, in 64 bits, are worked out once for all heads, one by each thread, while the next
+// step's values are on their way.  A head is a group of lanes
 // (a power of two) with two 16-byte vectors each, chosen so that both values of a pair are in the same lane.
 #include <string.h>
 
@@ -18,6 +19,11 @@ constexpr int RP_MAX_D = 256;
 constexpr int RP_BLOCKS = 592;                   // most CTAs of a backward launch, each with a partial sum of dw
 constexpr int RP_THREADS = 256;
 constexpr int RP_TOK = 8;                        // most tokens of a CTA at a time
+// CTAs per SM, forward and backward: what 64 and 128 registers per thread allow.  Each thread has the next step's row in flight, 32 or
+// 64 bytes.  32768 tokens of 28 + 4 heads, forward: 108 us so, 122 with three CTAs, 117 with five (spills), 115 with two rows in
+// flight; without a next step in flight, a CTA per step, 126.  Backward, 16384 tokens of 32 + 8 heads: 110 us; 163 with one CTA per
+// SM, 153 with three (spills).
+constexpr int RP_CTAS_F = 4, RP_CTAS_B = 2;
 constexpr int RP_WARPS = 8;
 
 struct RopeArgs {
@@ -36,11 +42,11 @@ struct RopeArgs {
   float* part;                                   // [CTA][2][D] partial sums of dw
 };
 
-// Cosine and sine of pos * freq.  The product is taken in 64 bits and brought to a fraction of a turn there: in 32 bits the
+// Cosine and sine of pos * freq, turns = freq / (2 pi).  The product is taken in 64 bits and brought to a fraction of a turn there: in 32 bits the
 // angle of position 60000 would be off by 2e-3.  `fast`: the hardware's sine and cosine, off by 2^-20.5 at most within half a turn, for
 // results that are rounded to bf16 (2^-8) anyhow.
-__device__ __forceinline__ void rp_angle(int pos, float freq, float* s, float* c, bool fast) {
-  double t = (double)pos * (double)freq * 0.15915494309189533577;
+__device__ __forceinline__ void rp_angle(int pos, double turns, float* s, float* c, bool fast) {
+  double t = (double)pos * turns;
   t -= rint(t);
   if (fast) {
     const float x = (float)t * 6.2831853071795864769f;
@@ -106,7 +112,7 @@ k_rope_any(const __grid_constant__ RopeArgs a) {
           const bool second = a.inter ? (d & 1) != 0 : d >= half;
           const float other = row[a.inter ? d ^ 1 : (second ? d - half : d + half)];
           float sn, cs;
-          rp_angle(pos, a.freq[f], &sn, &cs, false);
+          rp_angle(pos, (double)a.freq[f] * 0.15915494309189533577, &sn, &cs, false);
           if (BWD) sn = -sn;
           g[i] = fmaf(g[i], cs, second ? other * sn : -other * sn);
         }
@@ -143,7 +149,7 @@ k_rope_any(const __grid_constant__ RopeArgs a) {
       if (threadIdx.x < D) {
         float sum = 0.f;
         for (int k = 0; k < RP_WARPS; ++k) sum += s_sum[k][threadIdx.x];
-        a.part[((size_t)blockIdx.x * 2 + side) * D + threadIdx.x] = sum;
+        a.part[((size_t)side * RP_BLOCKS + blockIdx.x) * D + threadIdx.x] = sum;
       }
       __syncthreads();
     }
@@ -153,7 +159,9 @@ k_rope_any(const __grid_constant__ RopeArgs a) {
 // ------------------------------------------------------------------------------------------------ vectors
 struct RopeShape {
   int lanes;                                     // of a head: a power of two up to 32
-  int tok[2];                                    // tokens of a CTA at a time, of the queries' and the keys' CTAs
+  // of the queries and of the keys: tokens of a step, steps that the heads of a step's tokens are cut into
+  int tok[2], chunks[2];
+  int first[2], ctas[2];                         // and the CTAs that take them: all take both, in small calls each takes one side
   unsigned inv[2];                               // ceil(2^32 / heads): x / heads = umulhi(x, inv) for x heads < 2^32
 };
 
@@ -198,9 +206,9 @@ __device__ __forceinline__ float rp_group_sum(float v, int lanes) {
 // Lane l of a head holds pairs N l .. N l + N - 1 (N = values of a vector) as vectors va and vb: with halves as pairs the same place
 // in both halves, and behind those lanes values that are not rotated, two vectors each; with neighbours as pairs two vectors in a row.
 template <typename T, bool BWD, bool INTER>
-__global__ void __launch_bounds__(RP_THREADS, BWD ? 3 : 4)
+__global__ void __launch_bounds__(RP_THREADS, BWD ? RP_CTAS_B : RP_CTAS_F)
 k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh) {
-  constexpr int N = RpVec<T>::N, U = 2;                  // items of a group in flight
+  constexpr int N = RpVec<T>::N;
   extern __shared__ __align__(16) float s_trig[];        // [2][tok][cos, sin][lanes * N]
   __shared__ float s_sum[RP_THREADS / 32][RP_MAX_D];
   const int tid = threadIdx.x, l = tid & (sh.lanes - 1), groups = RP_THREADS / sh.lanes, grp = tid / sh.lanes;
@@ -209,139 +217,143 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
   const bool ha = va < nv, hb = vb < nv;
   const bool turns = N * l < half;                       // some of the lane's pairs are rotated: all of them, with halves
   const float rD = 1.f / (float)D;
-  const int side = blockIdx.y, H = side ? a.Hkv : a.Hq, tok = sh.tok[side];
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  tree_after_previous();
+  int turn = 0;
+  // first the CTA's share of the queries' steps, then of the keys'
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {
+  const int H = side ? a.Hkv : a.Hq, tok = sh.tok[side], chunks = sh.chunks[side];
   const unsigned inv_h = sh.inv[side];
+  const long long steps = (a.n + tok - 1) / tok * chunks;
+  const int cta = (int)blockIdx.x - sh.first[side], ctas = sh.ctas[side];
+  if (cta < 0 || cta >= ctas) continue;
   const T* w = static_cast<const T*>(a.w[side]);
   const bool norm = w != nullptr, need_x = !BWD || norm;
   const T* X = static_cast<const T*>(a.x[side]);
   const T* G = static_cast<const T*>(a.g[side]);
   T* Y = static_cast<T*>(a.y[side]);
   const long long xs = a.xs[side], gs = a.gs[side], ys = a.ys[side];
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  // this thread's angle of a step: pair my_p of the step's token my_t, in turns; where it goes: four pairs of a lane next to each
+  // other, the lanes behind one another, for 16-byte reads without bank conflicts
+  const int my_t = half > 0 ? tid / half : tok, my_p = half > 0 ? tid - my_t * half : 0;
+  const int my_at = my_t * 2 * np + (my_p / N) * 4 + (my_p & 3) + (N == 8 ? ((my_p >> 2) & 1) * (np / 2) : 0);
   uint64_t dw[N], w2[N];
 #pragma unroll
   for (int y = 0; y < N; ++y) dw[y] = w2[y] = 0ull;
-  tree_after_previous();
+  uint4 x[2], g[2];
+  int my_pos = 0;
+  // asks for the values and the position of step s
+  auto fetch = [&](long long s) {
+    const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
+    const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
+    const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
+    const bool on = it < items;
+    if (my_t < toks) my_pos = a.pos[t0 + my_t];
+    x[0] = x[1] = g[0] = g[1] = zero;
+    if (need_x && on) {
+      const uint4* from = reinterpret_cast<const uint4*>(X + (t0 + t) * xs + (long long)h * D);
+      if (ha) x[0] = from[va];
+      if (hb) x[1] = from[vb];
+    }
+    if (BWD && on) {
+      const uint4* from = reinterpret_cast<const uint4*>(G + (t0 + t) * gs + (long long)h * D);
+      if (ha) g[0] = from[va];
+      if (hb) g[1] = from[vb];
+    }
+  };
+  if (cta < steps) fetch(cta);
+  const double my_freq = my_t < tok ? (double)a.freq[my_p] * 0.15915494309189533577 : 0.0;
   if (norm) {
     rp_unpack(ha ? reinterpret_cast<const uint4*>(w)[va] : zero, w2, 0, T());
     rp_unpack(hb ? reinterpret_cast<const uint4*>(w)[vb] : zero, w2, N / 2, T());
   }
-  int turn = 0;
-  for (long long t0 = (long long)blockIdx.x * tok; t0 < a.n; t0 += (long long)gridDim.x * tok, turn ^= 1) {
+  for (long long s = cta; s < steps; s += ctas, turn ^= 1) {
+    const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
     const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
-    float* trig = s_trig + turn * tok * 2 * np;
-    // every group takes the same number of steps: the sums go over whole warps
-    for (int it0 = 0; it0 < items; it0 += groups * U) {
-      uint4 x[U][2], g[U][2];
-      int tt[U], hd[U];
+    const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
+    const bool on = it < items;
+    float* trig = s_trig + turn * RP_TOK * 2 * np;         // the other copy may still be read
+    if (my_t < toks) {
+      float sn, cs;
+      rp_angle(my_pos, my_freq, &sn, &cs, sizeof(T) == 2);
+      trig[my_at] = cs;
+      trig[my_at + np] = BWD ? -sn : sn;
+    }
+    __syncthreads();
+    const uint4 x0 = x[0], x1 = x[1], g0 = g[0], g1 = g[1];
+    if (s + ctas < steps) fetch(s + ctas);
+    uint64_t v[N], o[N];
+    float inv = 1.f;
+    if (need_x) {
+      rp_unpack(x0, v, 0, T());
+      rp_unpack(x1, v, N / 2, T());
+      if (norm) {
+        uint64_t sq = 0ull;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int it = it0 + u * groups + grp;
-        tt[u] = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h);
-        hd[u] = it - tt[u] * H;
-        const bool on = it < items;
-        x[u][0] = x[u][1] = g[u][0] = g[u][1] = zero;
-        if (need_x && on) {
-          const uint4* from = reinterpret_cast<const uint4*>(X + (t0 + tt[u]) * xs + (long long)hd[u] * D);
-          if (ha) x[u][0] = from[va];
-          if (hb) x[u][1] = from[vb];
-        }
-        if (BWD && on) {
-          const uint4* from = reinterpret_cast<const uint4*>(G + (t0 + tt[u]) * gs + (long long)hd[u] * D);
-          if (ha) g[u][0] = from[va];
-          if (hb) g[u][1] = from[vb];
-        }
+        for (int y = 0; y < N; ++y) sq = tt_fma2(v[y], v[y], sq);
+        float lo, hi;
+        tt_both(sq, lo, hi);
+        inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
+        const uint64_t inv2 = tt_two(inv, inv);
+#pragma unroll
+        for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
       }
-      if (it0 == 0) {
-        // cosines and sines of the CTA's tokens; the other copy may still be read
-        for (int i = tid; i < toks * half; i += RP_THREADS) {
-          const int t = i / half, p = i - t * half;
-          float sn, cs;
-          rp_angle(a.pos[t0 + t], a.freq[p], &sn, &cs, sizeof(T) == 2);
-          // four pairs of a lane next to each other, the lanes behind one another: 16-byte reads without bank conflicts
-          const int at = t * 2 * np + (p / N) * 4 + (p & 3) + (N == 8 ? ((p >> 2) & 1) * (np / 2) : 0);
-          trig[at] = cs;
-          trig[at + np] = sn;
-        }
-        __syncthreads();
-      }
+    }
+    if (BWD) {
+      rp_unpack(g0, o, 0, T());
+      rp_unpack(g1, o, N / 2, T());
+    } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool on = it0 + u * groups + grp < items;
-        uint64_t v[N], o[N];
-        float inv = 1.f;
-        if (need_x) {
-          rp_unpack(x[u][0], v, 0, T());
-          rp_unpack(x[u][1], v, N / 2, T());
-          if (norm) {
-            uint64_t sq = 0ull;
+      for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
+    }
+    if (turns && on) {
+      const float* at = trig + t * 2 * np + l * 4;
 #pragma unroll
-            for (int y = 0; y < N; ++y) sq = tt_fma2(v[y], v[y], sq);
-            float lo, hi;
-            tt_both(sq, lo, hi);
-            inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);
-            const uint64_t inv2 = tt_two(inv, inv);
+      for (int q = 0; q < N; q += 4) {
+        const float4 c4 = *reinterpret_cast<const float4*>(at + q / 4 * (np / 2));
+        const float4 s4 = *reinterpret_cast<const float4*>(at + np + q / 4 * (np / 2));
+        if (INTER) {
+          const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-            for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
+          for (int y = q; y < q + 4; ++y) {
+            if (N * l + y >= half) continue;
+            float p, r;
+            tt_both(o[y], p, r);
+            o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
           }
-        }
-        if (BWD) {
-          rp_unpack(g[u][0], o, 0, T());
-          rp_unpack(g[u][1], o, N / 2, T());
         } else {
 #pragma unroll
-          for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
-        }
-        if (turns && on) {
-          const float* at = trig + tt[u] * 2 * np + l * 4;
-#pragma unroll
-          for (int q = 0; q < N; q += 4) {
-            const float4 c4 = *reinterpret_cast<const float4*>(at + q / 4 * (np / 2));
-            float4 s4 = *reinterpret_cast<const float4*>(at + np + q / 4 * (np / 2));
-            if (BWD) s4 = make_float4(-s4.x, -s4.y, -s4.z, -s4.w);
-            if (INTER) {
-              const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
-#pragma unroll
-              for (int y = q; y < q + 4; ++y) {
-                if (N * l + y >= half) continue;
-                float p, r;
-                tt_both(o[y], p, r);
-                o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
-              }
-            } else {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int i = q / 2 + k, j = i + N / 2;
-                const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
-                const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
-                const uint64_t p = o[i], r = o[j];
-                o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
-                o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
-              }
-            }
+          for (int k = 0; k < 2; ++k) {
+            const int i = q / 2 + k, j = i + N / 2;
+            const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
+            const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
+            const uint64_t p = o[i], r = o[j];
+            o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
+            o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
           }
-        }
-        if (BWD && norm) {
-          uint64_t dot2 = 0ull;
-#pragma unroll
-          for (int y = 0; y < N; ++y) {
-            dw[y] = tt_fma2(o[y], v[y], dw[y]);
-            o[y] = rp_mul2(o[y], w2[y]);
-            dot2 = tt_fma2(o[y], v[y], dot2);
-          }
-          float lo, hi;
-          tt_both(dot2, lo, hi);
-          const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
-          const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
-#pragma unroll
-          for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
-        }
-        if (on) {
-          uint4* to = reinterpret_cast<uint4*>(Y + (t0 + tt[u]) * ys + (long long)hd[u] * D);
-          if (ha) to[va] = rp_pack(o, 0, T());
-          if (hb) to[vb] = rp_pack(o, N / 2, T());
         }
       }
+    }
+    if (BWD && norm) {
+      uint64_t dot2 = 0ull;
+#pragma unroll
+      for (int y = 0; y < N; ++y) {
+        dw[y] = tt_fma2(o[y], v[y], dw[y]);
+        o[y] = rp_mul2(o[y], w2[y]);
+        dot2 = tt_fma2(o[y], v[y], dot2);
+      }
+      float lo, hi;
+      tt_both(dot2, lo, hi);
+      const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
+      const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
+#pragma unroll
+      for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
+    }
+    if (on) {
+      uint4* to = reinterpret_cast<uint4*>(Y + (t0 + t) * ys + (long long)h * D);
+      if (ha) to[va] = rp_pack(o, 0, T());
+      if (hb) to[vb] = rp_pack(o, N / 2, T());
     }
   }
   if (BWD && a.part != nullptr) {
@@ -359,29 +371,34 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
     for (int d = tid; d < D; d += RP_THREADS) {
       float sum = 0.f;
       for (int k = 0; k < RP_THREADS / 32; ++k) sum += s_sum[k][d];
-      a.part[((size_t)blockIdx.x * 2 + side) * D + d] = sum;
+      a.part[((size_t)side * RP_BLOCKS + cta) * D + d] = sum;
     }
+    __syncthreads();
+  }
   }
 }
 
-// dw of both sides: the CTAs' partial sums, each thread those of every 32nd CTA in order, then the threads of a column in order.
+// dw of both sides: the CTAs' partial sums, each thread those of every 32nd CTA in order, then the threads of a column.
 __global__ void __launch_bounds__(1024)
-k_rope_weights(const float* __restrict__ part, int blocks, int D, float* dwq, float* dwk) {
+k_rope_weights(const float* __restrict__ part, int nq, int nk, int D, float* dwq, float* dwk) {
   __shared__ double s[32][33];
-  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, side = blockIdx.y;
+  float* to = side ? dwk : dwq;
   tree_after_previous();
+  if (to == nullptr) return;
+  const float* from = part + (size_t)side * RP_BLOCKS * D;
+  const int n = side ? nk : nq;
   double sum = 0.0;
-  if (c < 2 * D) {
+  if (c < D) {
 #pragma unroll 8
-    for (int b = grp; b < blocks; b += 32) sum += (double)part[(size_t)b * 2 * D + c];
+    for (int b = grp; b < n; b += 32) sum += (double)from[(size_t)b * D + c];
   }
   s[grp][lane] = sum;
   __syncthreads();
-  if (grp == 0 && c < 2 * D) {
+  if (grp == 0 && c < D) {
     sum = 0.0;
     for (int k = 0; k < 32; ++k) sum += s[k][lane];
-    float* to = c < D ? dwq : dwk;
-    if (to != nullptr) to[c < D ? c : c - D] = (float)sum;
+    to[c] = (float)sum;
   }
 }
 
@@ -411,39 +428,42 @@ template <typename T, bool BWD>
 cudaError_t rope_launch(const RopeArgs& a, int sms, float* dwq, float* dwk, cudaStream_t st) {
   const int N = 16 / (int)sizeof(T), H = a.Hq + a.Hkv;
   cudaError_t e;
-  int grid;
+  int ctas[2];
   if (!a.inter && (a.rot / 2) % N != 0) {
     // halves that do not start on a vector
     const long long want = (a.n * H + RP_WARPS - 1) / RP_WARPS;
-    grid = (int)(want < RP_BLOCKS ? want : RP_BLOCKS);
-    e = tree_launch(k_rope_any<T, BWD>, dim3(grid), 32 * RP_WARPS, 0, 0, st, a);
+    ctas[0] = ctas[1] = (int)(want < RP_BLOCKS ? want : RP_BLOCKS);
+    e = tree_launch(k_rope_any<T, BWD>, dim3(ctas[0]), 32 * RP_WARPS, 0, 0, st, a);
   } else {
     RopeShape sh;
     const int pairs = (a.D / N + 1) / 2;
     for (sh.lanes = 1; sh.lanes < pairs; sh.lanes *= 2) {}
-    // Tokens of a CTA: as many as its groups have in flight, fewer where that would leave SMs without work.
-    const int fly = RP_THREADS / sh.lanes * 2;
-    long long want = 0;
+    const int fly = RP_THREADS / sh.lanes, per_sm = BWD ? RP_CTAS_B : RP_CTAS_F;
+    const int resident = per_sm * sms < RP_BLOCKS ? per_sm * sms : RP_BLOCKS;
+    long long steps[2];
     for (int side = 0; side < 2; ++side) {
+      // tokens of a step: as many as its groups have in flight, no more than its threads have angles for, fewer where that would
+      // leave CTAs without work
       const int heads = side ? a.Hkv : a.Hq;
       int tok = fly / heads;
       if (tok > RP_TOK) tok = RP_TOK;
-      while (tok > 1 && a.n / tok < 4ll * sms) tok /= 2;
+      if (a.rot > 0 && tok > RP_THREADS / (a.rot / 2)) tok = RP_THREADS / (a.rot / 2);
+      while (tok > 1 && a.n / tok < resident) tok /= 2;
       sh.tok[side] = tok < 1 ? 1 : tok;
+      sh.chunks[side] = (sh.tok[side] * heads + fly - 1) / fly;
       sh.inv[side] = heads > 1 ? (unsigned)(((1ull << 32) + heads - 1) / heads) : 0u;
-      const long long ctas = (a.n + sh.tok[side] - 1) / sh.tok[side];
-      if (ctas > want) want = ctas;
+      steps[side] = (a.n + sh.tok[side] - 1) / sh.tok[side] * sh.chunks[side];
     }
-    // forward: a CTA per step, so that one's loads run under another's stores; backward: as many CTAs as stay resident, for fewer
-    // partial sums of dw
-    const long long most = BWD ? (3ll * sms < RP_BLOCKS ? 3ll * sms : RP_BLOCKS) : (1ll << 30);
-    grid = (int)(want < most ? want : most);
-    const int tok = sh.tok[0] > sh.tok[1] ? sh.tok[0] : sh.tok[1];
-    const size_t smem = (size_t)2 * tok * 2 * sh.lanes * N * sizeof(float);
-    e = tree_launch(a.inter ? k_rope<T, BWD, true> : k_rope<T, BWD, false>, dim3(grid, 2), RP_THREADS, smem, 0, st, a, sh);
+    const bool small = steps[0] + steps[1] <= resident;  // each step has a CTA of its own: 16 tokens of 16 + 2 heads 3.6 -> 2.8 us
+    for (int side = 0; side < 2; ++side) sh.ctas[side] = ctas[side] = (int)(steps[side] < resident ? steps[side] : resident);
+    sh.first[0] = 0;
+    sh.first[1] = small ? ctas[0] : 0;
+    const int grid = small ? ctas[0] + ctas[1] : ctas[0] > ctas[1] ? ctas[0] : ctas[1];
+    const size_t smem = (size_t)2 * RP_TOK * 2 * sh.lanes * N * sizeof(float);
+    e = tree_launch(a.inter ? k_rope<T, BWD, true> : k_rope<T, BWD, false>, dim3(grid), RP_THREADS, smem, 0, st, a, sh);
   }
   if (e != cudaSuccess || !BWD || a.part == nullptr) return e;
-  return tree_launch(k_rope_weights, dim3((2 * a.D + 31) / 32), 1024, 0, 0, st, (const float*)a.part, grid, a.D, dwq, dwk);
+  return tree_launch(k_rope_weights, dim3((a.D + 31) / 32, 2), 1024, 0, 0, st, (const float*)a.part, ctas[0], ctas[1], a.D, dwq, dwk);
 }
 
 template <bool BWD>

@@ -204,10 +204,13 @@ def test_policy_loss_and_its_gradient(n, V, dtype):
     ref = to.policy_loss(z, tok, kw["advantage"], kw["old_logp"], kw["ref_logp"], kw["weight"], **opt)
     _check_loss(got, ref, dt, V, n, float((ref["token_loss"].abs() * kw["weight"].double()).sum()))
     # in place: the gradient over the logits; and nothing but some of the outputs
-    z2, g2 = z.clone(), got["dlogits"]
-    z3 = z.clone()
+    # (rows that lie alike with respect to 16 bytes are summed in the same order, others need not be)
+    z2, z3, g2 = torch.empty_strided(z.shape, z.stride(), dtype=dt, device=DEV).copy_(z), z.clone(), got["dlogits"]
     pt.policy_loss(z2, tok, **kw, logp=f(), dlogits=z2, **opt)
     assert torch.equal(z2, g2) and torch.equal(z, z3)
+    lp = f()
+    pt.policy_loss(z3, tok, **kw, logp=lp, dlogits=z3, **opt)
+    _check_loss(dict(logp=lp, dlogits=z3), ref, dt, V, n, 0)
     lp = f()
     pt.policy_loss(z, tok, **kw, logp=lp, **opt)
     assert torch.equal(lp, got["logp"])
@@ -218,3 +221,59 @@ def test_policy_loss_and_its_gradient(n, V, dtype):
     lp = f()
     pt.token_logp(z, tok, lp, temperature=0.8)
     _check_loss(dict(logp=lp), to.policy_loss(z, tok, kw["advantage"], temperature=0.8), dt, V, n, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [37, 5003, 65536])
+def test_policy_loss_of_masked_and_extreme_logits(V, dtype):
+    """Logits of -inf have no probability, whole stretches of them included; far offsets do not matter; a row that is not a number is
+    one, and no other row is."""
+    dt, n = TYPES[dtype], 12
+    z, tok, kw = _loss_case(n, V, dt, V, mask=False)
+    z = z.contiguous()
+    z[0, V // 3:] = -math.inf
+    z[1, :V - 1] = -math.inf
+    z[2] -= 20000
+    z[3] += 20000
+    z[4] = -3e38
+    z[5, V // 2] = math.nan
+    z[6] = -math.inf
+    z[7, 5] = math.inf
+    z[8] = math.nan
+    tok[0], tok[1], tok[8] = 1, V - 1, -1
+    kw["old_logp"] = torch.log_softmax(z.double(), -1).gather(1, tok.clamp(min=0).long()[:, None])[:, 0].float() + 0.1
+    kw["ref_logp"] = kw["old_logp"] - 0.3
+    f = lambda: torch.full((n,), 5.0, device=DEV)                   # noqa: E731
+    got = dict(logp=f(), token_loss=f(), token_kl=f(), dlogits=torch.full_like(z, 5.0))
+    pt.policy_loss(z, tok, **kw, **got, kl_coef=0.1)
+    ref = to.policy_loss(z, tok, kw["advantage"], kw["old_logp"], kw["ref_logp"], kw["weight"], kl_coef=0.1)
+    bad = torch.tensor([5, 6, 7], device=DEV)
+    good = torch.tensor([i for i in range(n) if i not in (5, 6, 7)], device=DEV)
+    for k in got:
+        assert got[k][bad].isnan().reshape(3, -1).any(1).all(), k
+    # offsets of 20000 leave 2^-9 (fp32) or 2^6 (bf16) of a logit: both sides read the same values, the exponents are off by 2^-24 of them
+    slack = 20000 * 2.0 ** -22
+    for k in ("logp", "token_loss", "token_kl"):
+        _close(got[k][good], ref[k][good], slack * (1 + ref[k][good].abs()), k)
+    g = ref["dlogits"][good]
+    _close(got["dlogits"][good], g, (to.half_step(dt) + 4 * slack) * g.abs() + 4 * slack * g.abs().amax(-1, keepdim=True) + 1e-37, "dlogits")
+
+
+def test_policy_loss_gradient_against_differences():
+    n, V = 6, 1000
+    z, tok, kw = _loss_case(n, V, torch.float32, 4, mask=False)
+    out = lambda: dict(logp=torch.empty(n, device=DEV), token_loss=torch.empty(n, device=DEV), loss=torch.empty(1, device=DEV))   # noqa: E731
+    d, o = torch.empty_like(z), out()
+    pt.policy_loss(z, tok, **kw, **o, dlogits=d, kl_coef=0.1)
+    for i in range(n):
+        for x in (int(tok[i]), 17):
+            h = 0.05
+            side = []
+            for s in (h, -h):
+                z2, o2 = z.clone(), out()
+                z2[i, x] += s
+                pt.policy_loss(z2, tok, **kw, **o2, kl_coef=0.1)
+                side.append(float(o2["token_loss"][i].double() * kw["weight"][i].double()))
+            slope = (side[0] - side[1]) / (2 * h)
+            # a central difference: h^2 / 6 of the third derivative, below 20 of the gradient's size, and the losses' roundings
+            assert abs(slope - float(d[i, x])) <= h * h / 6 * 20 * float(d[i].abs().max()) + 2.0 ** -20 / h * float(kw["weight"][i]), (i, x)
