@@ -5,7 +5,7 @@
 //
 // Bound by memory: a row is read once and its gradient written once.  A row's maximum and sum have to be known before any of its
 // gradient is, so the row stays in shared memory in between: a cluster of one to eight CTAs per row holds a slice each (bulk copies
-// in four chunks, the maximum and the sum of a chunk while the next ones arrive), exchanges (maximum, sum) through distributed shared
+// in two chunks, the maximum and the sum of a chunk while the next ones arrive), exchanges (maximum, sum) through distributed shared
 // memory, works the loss out in 64 bits, and writes the gradient from shared memory.  Rows need not be aligned: the values in front of
 // the first and behind the last 16-byte boundary are held by the first CTA's threads, one each.  Rows that eight CTAs cannot hold
 // are read twice.
@@ -19,8 +19,10 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int PL_THREADS = 256;
-constexpr int PL_CHUNKS = 4;
-constexpr int PL_SLICE = 112 * 1024;             // most bytes of a row in a CTA: two CTAs per SM
+constexpr int PL_CHUNKS = 2;
+constexpr int PL_CTAS = 3;                       // CTAs per SM
+// Most bytes of a row in a CTA: so that three share an SM (228 KB, of which a CTA takes 1 KB and its static part besides), or two.
+constexpr int PL_SLICE3 = 76544, PL_SLICE2 = 112 * 1024;
 
 struct PolicyArgs {
   const void* z;
@@ -41,14 +43,44 @@ struct PolicyArgs {
   long long dzs;
 };
 
+// exp(x) - 1 in 64 bits: x = k ln 2 + r, the Taylor series of r to its 13th term (|r| <= 0.35: below 2^-53), 2^k (exp(r) - 1) + 2^k - 1.
+// One chain for the ratio and the KL term, in two lanes: with the library's functions a row's arithmetic kept its CTA waiting longer.
+__device__ __forceinline__ double pl_expm1(double x) {
+  const double k = fmin(fmax(rint(x * 1.44269504088896340736), -1000.0), 1023.0);
+  const double r = fma(-k, 0.69314718055994530942, x);
+  double p = 1.0 / 6227020800.0;
+  const double inv[11] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0,
+                          1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5};
+#pragma unroll
+  for (int i = 0; i < 11; ++i) p = fma(p, r, inv[i]);
+  p = fma(p * r, r, r);
+  const double s = __longlong_as_double((long long)(1023 + (int)k) << 52);
+  const double y = fma(s, p, s - 1.0);
+  return x < -690.0 ? -1.0 : x > 709.0 ? (double)INFINITY : y;          // NaN stays
+}
+// log2 of a positive finite number: the fp32 logarithm of its fraction, corrected by what 2^-y0 leaves of it.
+__device__ __forceinline__ double pl_log2(float l) {
+  if (!(l >= 1.17549435e-38f) || l > 3e38f) return log2((double)l);
+  const int e = (int)(__float_as_uint(l) >> 23) - 127;
+  const double m = (double)__uint_as_float((__float_as_uint(l) & 0x7fffffu) | 0x3f800000u);
+  const float y0 = log2f((float)m);
+  const double q = fma(m, pl_expm1(-(double)y0 * 0.69314718055994530942), m - 1.0);
+  return (double)e + (double)y0 + q * 1.44269504088896340736 * (1.0 - 0.5 * q);
+}
+
 struct PolicyRow { float lp, loss, kl, grad; };  // grad: d (weight * loss) / d z_y without the softmax's part
 
-// What follows from a row's log-probability, in 64 bits: a ratio's side of the clip border decides a whole row of the gradient.
+// What follows from a row's log-probability, in 64 bits: a ratio's side of the clip border decides a whole row of the gradient.  A
+// warp calls it; lane 0 has the answer.
 __device__ __forceinline__ PolicyRow pl_row(const PolicyArgs& a, long long t, double lp, float w) {
   PolicyRow o = {(float)lp, 0.f, 0.f, 0.f};
   if (a.adv == nullptr) return o;
-  const double adv = a.adv[t];
-  const double r = a.old_lp != nullptr ? exp(lp - (double)a.old_lp[t]) : 1.0;
+  const int lane = threadIdx.x & 31;
+  const double adv = a.adv[t], ref = a.ref_lp != nullptr ? (double)a.ref_lp[t] : lp, old = a.old_lp != nullptr ? (double)a.old_lp[t] : lp;
+  const double over = ref - lp;
+  const double em1 = pl_expm1(lane == 0 ? lp - old : over);
+  const double rk = __shfl_sync(0xffffffffu, em1, 1);    // exp(ref - lp) - 1
+  const double r = a.old_lp != nullptr ? em1 + 1.0 : 1.0;
   const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
   const double rc = r < lo ? lo : r > hi ? hi : r;       // NaN stays
   const double s0 = r * adv, s1 = rc * adv;
@@ -56,11 +88,10 @@ __device__ __forceinline__ PolicyRow pl_row(const PolicyArgs& a, long long t, do
   const bool cut = (adv > 0.0 && r > hi) || (adv < 0.0 && r < lo);
   double d = cut ? 0.0 : -s0;
   if (a.ref_lp != nullptr) {
-    const double over = (double)a.ref_lp[t] - lp;
-    const double kl = expm1(over) - over;
+    const double kl = rk - over;
     o.kl = (float)kl;
     loss += (double)a.kl * kl;
-    d -= (double)a.kl * expm1(over);
+    d -= (double)a.kl * rk;
   }
   o.loss = (float)loss;
   o.grad = (float)((double)w * d * (double)a.inv_t);
@@ -109,13 +140,15 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   __syncthreads();
   l = 0.f;
   for (int i = 0; i < PL_THREADS / 32; ++i) l += s_l[i];
-  if (tid == 0) {
-    const double lp = (((double)zy - (double)ref) * (double)a.c2 - log2((double)l)) * 0.69314718055994530942;
+  if (warp == 0) {
+    const double lp = (((double)zy - (double)ref) * (double)a.c2 - pl_log2(l)) * 0.69314718055994530942;
     const PolicyRow o = pl_row(a, t, lp, w);
-    a.logp[t] = o.lp;
-    if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
-    if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
-    s_out[0] = o.grad;
+    if (tid == 0) {
+      a.logp[t] = o.lp;
+      if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
+      if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
+      s_out[0] = o.grad;
+    }
   }
   if (dz == nullptr) return;
   __syncthreads();                                       // also: everybody has read the row before it may be overwritten
@@ -187,7 +220,7 @@ struct PlSum {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(PL_THREADS)
+__global__ void __launch_bounds__(PL_THREADS, PL_CTAS)
 k_policy(const __grid_constant__ PolicyArgs a) {
   constexpr int N = 16 / sizeof(T);
   extern __shared__ __align__(16) uint8_t s_row[];
@@ -314,23 +347,25 @@ k_policy(const __grid_constant__ PolicyArgs a) {
     if (tid == 0) s_all = make_float2(sum.m, sum.l);
     cluster.sync();                                      // also: every CTA has read what it needs of the row
   }
-  if (tid == 0) {
+  if (warp == 0) {
     if (cs > 1) {
-      const float2 f = *cluster.map_shared_rank(&s_all, 0);
-      sum.m = f.x; sum.l = f.y;
-      for (int i = 1; i < cs; ++i) {                     // in the same order everywhere
-        const float2 o = *cluster.map_shared_rank(&s_all, i);
-        sum.join(o.x, o.y, c2);
-      }
+      const float2 own = *cluster.map_shared_rank(&s_all, lane < cs ? lane : 0);
+      sum.m = __shfl_sync(0xffffffffu, own.x, 0);
+      sum.l = __shfl_sync(0xffffffffu, own.y, 0);
+      for (int i = 1; i < cs; ++i)                       // in the same order everywhere
+        sum.join(__shfl_sync(0xffffffffu, own.x, i), __shfl_sync(0xffffffffu, own.y, i), c2);
     }
-    const double lp = (((double)zy - (double)sum.ref()) * (double)c2 - log2((double)sum.l)) * 0.69314718055994530942;
+    const double lp = (((double)zy - (double)sum.ref()) * (double)c2 - pl_log2(sum.l)) * 0.69314718055994530942;
     const PolicyRow o = pl_row(a, t, lp, w);
-    if (rank == 0) {
-      a.logp[t] = o.lp;
-      if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
-      if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
+    if (lane == 0) {
+      if (rank == 0) {
+        a.logp[t] = o.lp;
+        if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
+        if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
+      }
+      s_out[0] = -sum.ref(); s_out[1] = o.grad; s_out[2] = -o.grad / sum.l;
     }
-    s_out[0] = -sum.ref(); s_out[1] = o.grad; s_out[2] = -o.grad / sum.l;
+    __syncwarp();
   }
   if (cs > 1) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");      // nobody leaves while its sum may be read
   __syncthreads();
@@ -394,15 +429,16 @@ template <typename T>
 cudaError_t policy_launch(const PolicyArgs& a, float* loss, int dev, int sms, cudaStream_t st) {
   const long long row = (long long)a.V * sizeof(T);
   int cs = 1;
-  // A slice of at most a third of an SM's shared memory, so that one row's copies run under another's arithmetic; smaller ones, down to
-  // 16 KB, while the call has too few rows to fill the SMs.
-  while (cs < 8 && (row > cs * 72ll * 1024 || (row > cs * 32ll * 1024 && a.n * cs * 2 <= 4ll * sms))) cs *= 2;
+  // Slices that let three CTAs share an SM, so that one's copies run under another's arithmetic; smaller ones, down to 16 KB, while
+  // the call has too few rows to fill the SMs.  4096 rows of 152000 bf16: 548 us with clusters of four; 651 to 723 with eight; more
+  // threads per CTA 598 to 1322; clusters that stay and load the next row behind the gradient of the one before 585.
+  while (cs < 8 && (row > (long long)cs * PL_SLICE3 || (row > cs * 32ll * 1024 && a.n * cs * 2 <= 4ll * sms))) cs *= 2;
   cudaError_t e;
-  if (row > 8ll * PL_SLICE) {
+  if (row > 8ll * PL_SLICE2) {
     e = tree_launch(k_policy_row<T>, dim3((unsigned)a.n), PL_THREADS, 0, 0, st, a);
   } else {
     static PtencOnce once;
-    e = ptenc_first_use(once, dev, [] { return ptenc_allow_smem(k_policy<T>, PL_SLICE + 64); });
+    e = ptenc_first_use(once, dev, [] { return ptenc_allow_smem(k_policy<T>, PL_SLICE2); });
     const size_t smem = (size_t)((row / 16 + cs - 1) / cs * 16);
     if (e == cudaSuccess) e = tree_launch(k_policy<T>, dim3((unsigned)(a.n * cs)), PL_THREADS, smem, cs, st, a);
   }
