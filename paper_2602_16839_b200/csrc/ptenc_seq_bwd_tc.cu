@@ -45,7 +45,7 @@ struct BSmem {
   static constexpr int OFF_BAD = OFF_CLC + 16;                       // uint32 [2][2][4]: rows of patched tiles with non-finite values
   static constexpr int OFF_DESC = OFF_BAD + 64;
   static constexpr int OFF_BAR = (OFF_DESC + 2 * B_WORDS * 4 + 7) / 8 * 8;
-  static constexpr int N_BAR = 3 * STAGES + 20;
+  static constexpr int N_BAR = 3 * STAGES + 22;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
@@ -57,19 +57,19 @@ struct BSmem {
 };
 
 // Barriers after the stages' full, empty and ready ones.
-enum { X_AB_FULL, X_AB_EMPTY, X_S_FULL, X_S_FULL1, X_DP_FULL, X_P_READY, X_DS_READY, X_ACC_FULL, X_ACC_EMPTY, X_STAT_FULL, X_STAT_FULL1,
+enum { X_A_FULL, X_A_EMPTY, X_B_FULL, X_B_EMPTY, X_O_READ, X_S_FULL, X_S_FULL1, X_DP_FULL, X_P_READY, X_DS_READY, X_ACC_FULL, X_ACC_EMPTY, X_STAT_FULL, X_STAT_FULL1,
        X_STAT_EMPTY, X_STAT_EMPTY1, X_ITEM_FULL, X_ITEM_FULL1, X_ITEM_EMPTY, X_ITEM_EMPTY1, X_CLC, X_DRAIN };
 
-// What a CTA of either kernel does first; returns the TMEM base.
+// What a CTA of either kernel does first; returns the TMEM base.  b_users: who frees the item's second tile.
 template <int D>
-__device__ __forceinline__ uint32_t bwd_begin(uint8_t* smem, uint32_t sb, int tid, int warp) {
+__device__ __forceinline__ uint32_t bwd_begin(uint8_t* smem, uint32_t sb, int tid, int warp, int b_users) {
   using SM = BSmem<D>;
   constexpr int NS = SM::STAGES;
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, x = ready + 8 * NS;
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); bar_init(ready + 8 * s, 1); }
-    const int counts[] = {1, 1, 1, 1, 1, 8, 8, 1, 8, 2, 2, 8, 8, 1, 1, 1 + 2 + 8, 1 + 2 + 8, 1, 1};
+    const int counts[] = {1, 1, 1, b_users, 8, 1, 1, 1, 8, 8, 1, 8, 2, 2, 8, 8, 1, 1, 1 + 2 + 8, 1 + 2 + 8, 1, 1};
     for (int i = 0; i <= X_DRAIN; ++i) bar_init(x + 8 * i, counts[i]);
     misc[0] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -87,16 +87,17 @@ __device__ __forceinline__ uint32_t bwd_begin(uint8_t* smem, uint32_t sb, int ti
 }
 
 // The producer of either kernel.  find(item, d) fills an item's words (all but the kind) and says whether it is one; own(d, which) and
-// entry(d, tile, which) load the item's own two tiles and its ring entries.
-template <int D, typename FIND, typename OWN, typename ENTRY>
+// entry(d, tile, which) load the item's own two tiles and its ring entries.  EXTRA: one more entry of the second ring in front of an
+// item's, entry(d, 0, 2).  Everything is asked for as soon as its place is free, the next item's tiles under the end of the last one.
+template <int D, bool EXTRA, typename FIND, typename OWN, typename ENTRY>
 __device__ __forceinline__ void bwd_produce(uint8_t* smem, uint32_t sb, FIND find, OWN own, ENTRY entry) {
   using SM = BSmem<D>;
   constexpr int NS = SM::STAGES, TILE = SM::TILE;
   volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, x = empty + 16 * NS;
-  uint32_t nt = 0, seq = 0, asked = 0;                   // tiles, items and takeovers so far
-  bool half = false;                                     // the last tile's first ring entry alone has been asked for
+  uint32_t na = 0, nb = 0, seq = 0, asked = 0;           // ring entries, items and takeovers so far
+  uint32_t got_a = 0, got_b = 0;                         // the items' own tiles
   bool okay = true;
   int item = (int)blockIdx.x;
   while (okay) {
@@ -119,20 +120,34 @@ __device__ __forceinline__ void bwd_produce(uint8_t* smem, uint32_t sb, FIND fin
       for (int i = B_START; i < B_WORDS; ++i) d[i] = w[i];
       d[B_KIND] = 1;
       bar_arrive(x + 8 * (X_ITEM_FULL + slot));
-      if (!bar_wait(x + 8 * X_AB_EMPTY, (seq & 1) ^ 1, abort_flag)) { okay = false; break; }
-      bar_expect(x + 8 * X_AB_FULL, 2 * TILE);
-      for (int t = 0; t < 2; ++t) own(w, t, sb + SM::OFF_AB + t * TILE, x + 8 * X_AB_FULL);
-      ++seq;
-      for (int t = 0; t < w[B_N] && okay; ++t, ++nt) {
-        uint32_t s = SM::stage_a(nt);
-        if (!bar_wait(empty + 8 * s, SM::phase_a(nt) ^ 1, abort_flag)) { okay = false; break; }
+      if (!bar_wait(x + 8 * X_A_EMPTY, (seq & 1) ^ 1, abort_flag)) { okay = false; break; }
+      bar_expect(x + 8 * X_A_FULL, TILE);
+      own(w, 0, sb + SM::OFF_AB, x + 8 * X_A_FULL);
+      ++got_a;
+      auto ring_a = [&](int t) -> bool {
+        const uint32_t s = SM::stage_a(na);
+        if (!bar_wait(empty + 8 * s, SM::phase_a(na) ^ 1, abort_flag)) return false;
         bar_expect(full + 8 * s, (uint32_t)TILE);
         entry(w, t, 0, sb + s * TILE, full + 8 * s);
-        s = SM::stage_b(nt);
-        if (!bar_wait(empty + 8 * s, SM::phase_b(nt) ^ 1, abort_flag)) { okay = false; half = true; break; }
+        ++na;
+        return true;
+      };
+      auto ring_b = [&](int t, int which) -> bool {
+        const uint32_t s = SM::stage_b(nb);
+        if (!bar_wait(empty + 8 * s, SM::phase_b(nb) ^ 1, abort_flag)) return false;
         bar_expect(full + 8 * s, (uint32_t)TILE);
-        entry(w, t, 1, sb + s * TILE, full + 8 * s);
-      }
+        entry(w, t, which, sb + s * TILE, full + 8 * s);
+        ++nb;
+        return true;
+      };
+      if (!ring_a(0) || !bar_wait(x + 8 * X_B_EMPTY, (seq & 1) ^ 1, abort_flag)) { okay = false; break; }
+      bar_expect(x + 8 * X_B_FULL, TILE);
+      own(w, 1, sb + SM::OFF_AB + TILE, x + 8 * X_B_FULL);
+      ++got_b;
+      ++seq;
+      if (EXTRA) okay = ring_b(0, 2);
+      okay = okay && ring_b(0, 1);
+      for (int t = 1; t < w[B_N] && okay; ++t) okay = ring_a(t) && ring_b(t, 1);
     }
     if (okay) {
       if (!bar_wait(x + 8 * X_CLC, asked & 1, abort_flag)) { okay = false; break; }
@@ -143,10 +158,10 @@ __device__ __forceinline__ void bwd_produce(uint8_t* smem, uint32_t sb, FIND fin
   }
   if (!okay) { *abort_flag = 1; bar_drain(x + 8 * X_CLC, asked & 1); }
   // whatever the other roles did, copies in flight land before the shared memory goes away
-  const uint32_t na = nt + (half ? 1 : 0);
   for (uint32_t i = 1; i <= (uint32_t)SM::RA && i <= na; ++i) bar_drain(full + 8 * SM::stage_a(na - i), SM::phase_a(na - i));
-  for (uint32_t i = 1; i <= (uint32_t)SM::RB && i <= nt; ++i) bar_drain(full + 8 * SM::stage_b(nt - i), SM::phase_b(nt - i));
-  if (seq > 0 && !okay) bar_drain(x + 8 * X_AB_FULL, (seq - 1) & 1);
+  for (uint32_t i = 1; i <= (uint32_t)SM::RB && i <= nb; ++i) bar_drain(full + 8 * SM::stage_b(nb - i), SM::phase_b(nb - i));
+  if (!okay && got_a > 0) bar_drain(x + 8 * X_A_FULL, (got_a - 1) & 1);
+  if (!okay && got_b > 0) bar_drain(x + 8 * X_B_FULL, (got_b - 1) & 1);
 }
 
 template <int D>
@@ -171,6 +186,12 @@ __device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, uint32_t b, boo
   const uint64_t db = desc_mn(b);
 #pragma unroll
   for (int k = 0; k < 8; ++k) mma_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (k * 2048 >> 4), tt_idesc(D, 1), k > 0 ? 1u : (replace ? 0u : 1u));
+}
+
+// Bits of positions [lo, hi) in the word of positions [at, at + 32).
+__device__ __forceinline__ uint32_t st_run(int lo, int hi, int at) {
+  const int a = max(lo - at, 0), b = min(hi - at, 32);
+  return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
 }
 
 // One row of a gradient, columns [c0, c1), from tensor memory.
@@ -204,7 +225,7 @@ __device__ __forceinline__ void bwd_end(uint32_t tmem, int warp) {
 template <int D>
 __global__ void __launch_bounds__(ST_THREADS, 1)
 k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG) {
+            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmO) {
   using SM = BSmem<D>;
   constexpr int NS = SM::STAGES, TILE = SM::TILE;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -214,7 +235,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + SM::OFF_BAD);           // [tile & 1][4]: keys with non-finite values
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, X = ready + 8 * NS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp);
+  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp, 2);
   const uint32_t tS = tmem, tP = tmem + 2 * SN, tA = tmem + 3 * SN;            // S [2], dP, dQ
   auto range_of = [](volatile int* d) { SeqRange r; r.np = d[B_A]; r.s0 = d[B_B]; r.s1 = d[B_C]; return r; };
 
@@ -223,7 +244,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag)); };
   if (warp == 0) {
     if (lane == 0)
-      bwd_produce<D>(smem, sb,
+      bwd_produce<D, true>(smem, sb,
         [&](int item, int* w) -> bool {
           const int at = (int)gridDim.x - 1 - item, number = at / a.Hq;
           SeqView s;
@@ -240,6 +261,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         },
         [&](const int* w, int t, int which, uint32_t dst, uint32_t bar) {
           SeqRange r;
+          if (which == 2) { load_tile<D>(dst, &tmO, w[B_HEAD], w[B_START] + w[B_TILE] * TM, bar); return; }
           r.np = w[B_A]; r.s0 = w[B_B]; r.s1 = w[B_C];
           load_tile<D>(dst, which ? &tmV : &tmK, w[B_HEAD] / a.g, w[B_START] + seq_at(r, t) * SN, bar);
         });
@@ -257,21 +279,27 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (kind == 0) break;
       __syncwarp();
       if (leader) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
-      if (!wait(X + 8 * X_AB_FULL, seq & 1)) { okay = false; break; }
+      if (!wait(X + 8 * X_A_FULL, seq & 1)) { okay = false; break; }
       auto scores = [&](int t) -> bool {                 // S of tile t
         const uint32_t s = SM::stage_a(nt + t), buf = (nt + t) & 1;
         if (!wait(ready + 8 * s, SM::phase_a(nt + t))) return false;
-        if (leader) { mma_scores<D>(tS + buf * SN, sb + SM::OFF_AB, sb + s * TILE); commit(X + 8 * (X_S_FULL + buf)); }
+        if (leader) {
+          mma_scores<D>(tS + buf * SN, sb + SM::OFF_AB, sb + s * TILE);
+          commit(X + 8 * (X_S_FULL + buf));
+          if (t == n - 1) commit(X + 8 * X_A_EMPTY);     // the next item's Q may come
+        }
         __syncwarp();
         return true;
       };
       auto values = [&](int t) -> bool {                 // dP of tile t
-        const uint32_t s = SM::stage_b(nt + t);
-        if (!wait(ready + 8 * s, SM::phase_b(nt + t))) return false;
+        const uint32_t at = nt + t + seq + 1, s = SM::stage_b(at);             // an O tile per item is in that ring too
+        if (t == 0 && !wait(X + 8 * X_B_FULL, seq & 1)) return false;
+        if (!wait(ready + 8 * s, SM::phase_b(at))) return false;
         if (leader) {
           mma_scores<D>(tP, sb + SM::OFF_AB + TILE, sb + s * TILE);
           commit(X + 8 * X_DP_FULL);
           commit(empty + 8 * s);
+          if (t == n - 1) commit(X + 8 * X_B_EMPTY);
         }
         __syncwarp();
         return true;
@@ -292,7 +320,6 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       }
       if (!okay) break;
       send(X + 8 * X_ACC_FULL);
-      send(X + 8 * X_AB_EMPTY);
       nt += n;
       ++seq;
     }
@@ -315,11 +342,22 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       const SeqView s = bwd_view(d);
       const SeqRange r = range_of(d);
       const int n = d[B_N], i0 = d[B_TILE] * TM;
+      if (me == 1) {
+        // the O tile is the softmax warps' alone: when they have read it and dO, this warp frees both
+        const uint32_t at = nt + seq, sg = SM::stage_b(at);
+        if (!wait(full + 8 * sg, SM::phase_b(at)) || !wait(X + 8 * X_O_READ, seq & 1)) { okay = false; break; }
+        if (lane == 0) {
+          bar_arrive(ready + 8 * sg);                    // nobody waits for it, but the stage's phases go on
+          bar_arrive(empty + 8 * sg);
+          bar_arrive(X + 8 * X_B_EMPTY);
+        }
+        __syncwarp();
+      }
       for (int t = 0; t < n; ++t) {
         // Each ring has its own warp, which waits for each of its tiles in turn and without which none is used: a wait tells a
         // stage's phase from the one two rounds before or after.
-        const uint32_t sg = me == 0 ? SM::stage_a(nt + t) : SM::stage_b(nt + t);
-        if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
+        const uint32_t at = me == 0 ? nt + t : nt + t + seq + 1, sg = me == 0 ? SM::stage_a(at) : SM::stage_b(at);
+        if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(at) : SM::phase_b(at))) { okay = false; break; }
         if (me == 0) {
           const int tile = seq_at(r, t);
           uint32_t* bad = s_bad + 4 * ((nt + t) & 1);    // read with the tile two before
@@ -362,25 +400,34 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       const SeqRange r = range_of(d);
       const int n = d[B_N], i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row);
       const bool real = row < s.len;
-      // delta: both threads of a row form it, so that no barrier stands between the warps
+      // delta from the O and dO tiles in shared memory: both threads of a row form it, so that no barrier stands between the warps.
+      // (Read from memory, rows far apart, it cost 8000 cycles an item; so 1000.)
       const long long orow = (long long)(s.start + row) * a.Hq + h;
-      float sum = 0.f, nlse = 0.f;
-      if (real) {
-        const uint4* o = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.out) + orow * a.D);
-        const uint4* g = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.dout) + orow * a.D);
+      const float nlse = real ? -a.lse[orow] * ST_LOG2E : 0.f;
+      const uint32_t oat = nt + seq;
+      wait(X + 8 * X_B_FULL, seq & 1);
+      wait(full + 8 * SM::stage_b(oat), SM::phase_b(oat));
+      float sum = 0.f;
+      {
+        const uint8_t* to = smem + SM::stage_b(oat) * TILE + lrow * 128;
+        const uint8_t* tg = smem + SM::OFF_AB + TILE + lrow * 128;
+        float part[2] = {0.f, 0.f};
 #pragma unroll 4
-        for (int c = 0; c < a.D / 8; ++c) {
-          const uint4 u = o[c], v = g[c];
+        for (int c = 0; c < D / 8; ++c) {
+          const int at = (c >> 3) * HALF + (((c & 7) ^ (lrow & 7)) << 4);
+          const uint4 u = *reinterpret_cast<const uint4*>(to + at), v = *reinterpret_cast<const uint4*>(tg + at);
           const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&u);
           const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float2 p = __bfloat1622float2(x[k]), q = __bfloat1622float2(y[k]);
-            sum = fmaf(p.x, q.x, fmaf(p.y, q.y, sum));
+            part[k & 1] = fmaf(p.x, q.x, fmaf(p.y, q.y, part[k & 1]));
           }
         }
-        nlse = -a.lse[orow] * ST_LOG2E;
+        sum = part[0] + part[1];
       }
+      __syncwarp();
+      if (lane == 0) bar_arrive(X + 8 * X_O_READ);
       const float ndelta = -sum;
       if (real && half == 0) {
         const long long at = (long long)h * a.n + s.start + row;
@@ -416,7 +463,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         }
         wait(X + 8 * X_DP_FULL, nt & 1);
         fence_after();
-        const int jh = j0 + 64 * half, hi = row - jh, lo = low - jh, pn = s.pin - jh;
+        const int jh = j0 + 64 * half;
 #pragma unroll
         for (int c = 0; c < 64; c += 32) {
           float x[32];
@@ -427,9 +474,10 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           for (int y = 0; y < 32; y += 2)
             tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), nd2), tt_two(p[c + y], p[c + y + 1])), x[y], x[y + 1]);
           if (!all) {
+            const uint32_t keep = st_run(0, row + 1, jh + c) & ~st_run(s.pin, low, jh + c);
 #pragma unroll
             for (int y = 0; y < 32; ++y)
-              if (c + y > hi || (c + y >= pn && c + y < lo)) x[y] = 0.f;
+              if (!(keep & (1u << y))) x[y] = 0.f;
           }
           // dS in bf16, half a step of 2^-8: the product's operands are of one type
 #pragma unroll
@@ -467,10 +515,11 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(smem + SM::OFF_BAD);           // [Q or dO][4], of the warp that patches
+  volatile uint32_t* s_odd = s_bad + 8;                                        // [buffer]: rows of dO were patched
   float* s_stat = reinterpret_cast<float*>(smem + SM::OFF_STAT);               // [buffer][-lse or -delta][128]
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, X = ready + 8 * NS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp);
+  const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp, 1);
   const uint32_t tS = tmem, tP = tmem + SN, tV = tmem + 2 * SN, tK = tV + D;   // S^T, dP^T, dV, dK
   // An item's tiles of queries: head by head, tiles B_TILE .. B_TILE + B_A - 1 of each.
 
@@ -479,7 +528,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag)); };
   if (warp == 0) {
     if (lane == 0)
-      bwd_produce<D>(smem, sb,
+      bwd_produce<D, false>(smem, sb,
         [&](int item, int* w) -> bool {
           // Pinned tokens are seen by all that follow and cost most, so their tiles come first, by numbers of their own: a.pins
           // per sequence.
@@ -519,14 +568,16 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       if (kind == 0) break;
       __syncwarp();
       if (leader) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
-      if (!wait(X + 8 * X_AB_FULL, seq & 1)) { okay = false; break; }
+      if (!wait(X + 8 * X_A_FULL, seq & 1)) { okay = false; break; }
       // S^T (which 0) or dP^T (1) of tile t
       auto product = [&](int t, int which) -> bool {
         const uint32_t s = which ? SM::stage_b(nt + t) : SM::stage_a(nt + t);
+        if (which && t == 0 && !wait(X + 8 * X_B_FULL, seq & 1)) return false;
         if (!wait(ready + 8 * s, which ? SM::phase_b(nt + t) : SM::phase_a(nt + t))) return false;
         if (leader) {
           mma_scores<D>(which ? tP : tS, sb + SM::OFF_AB + which * TILE, sb + s * TILE);
           commit(X + 8 * (which ? X_DP_FULL : X_S_FULL));
+          if (t == n - 1) commit(X + 8 * (which ? X_B_EMPTY : X_A_EMPTY));     // the next item's V or K may come
         }
         __syncwarp();
         return true;
@@ -548,7 +599,6 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       }
       if (!okay) break;
       send(X + 8 * X_ACC_FULL);
-      send(X + 8 * X_AB_EMPTY);
       nt += n;
       ++seq;
     }
@@ -583,10 +633,12 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           v[y] = i < s.len ? stat[(long long)hh * a.n + i] : 0.f;
         }
         if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
+        bool odd = false;
         if (!(i0 + TM <= s.len && seq_all(s, i0, i0 + TM - 1, j0, j0 + TM - 1))) {
           if (lane < 4) bad[lane] = 0;
           __syncwarp();
-          if (patch_tile(smem + sg * TILE, D / 64, i0, s.len, 0, 1, bad)) {
+          odd = patch_tile(smem + sg * TILE, D / 64, i0, s.len, 0, 1, bad);
+          if (odd) {
             __syncwarp();
 #pragma unroll
             for (int y = 0; y < 4; ++y)
@@ -598,6 +650,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         if (!wait(X + 8 * (X_STAT_EMPTY + buf), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
 #pragma unroll
         for (int y = 0; y < 4; ++y) s_stat[buf * 2 * TM + me * TM + lane + 32 * y] = v[y];
+        if (me == 1 && lane == 0) s_odd[buf] = odd;
         __syncwarp();
         if (lane == 0) bar_arrive(X + 8 * (X_STAT_FULL + buf));
       }
@@ -656,9 +709,14 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             for (int z = 0; z < 4; ++z) p[y + z] = tt_ex2(p[y + z]);
           }
           if (!all) {
+            if (s_odd[buf] != 0) {                       // rare: a non-finite row of dO, whose delta is NaN, reaches dV too
 #pragma unroll
-            for (int y = c; y < c + 32; ++y)             // a non-finite row of dO reaches dV too
-              p[y] = y < lo || y > hi ? 0.f : fmaf(0.f, st[TM + y], p[y]);
+              for (int y = c; y < c + 32; ++y) p[y] = fmaf(0.f, st[TM + y], p[y]);
+            }
+            const uint32_t keep = st_run(lo, hi + 1, c);
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (!(keep & (1u << y))) p[c + y] = 0.f;
           }
           // P in bf16, half a step of 2^-8 per weight, as in the forward pass
 #pragma unroll
@@ -685,9 +743,10 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             tt_both(st_mul2(tt_add2(tt_two(x[y + 2], x[y + 3]), tt_two(v.z, v.w)), tt_two(p[y + 2], p[y + 3])), x[y + 2], x[y + 3]);
           }
           if (!all) {
+            const uint32_t keep = st_run(lo, hi + 1, c);
 #pragma unroll
-            for (int y = c; y < c + 32; ++y)
-              if (y < lo || y > hi) x[y] = 0.f;
+            for (int y = 0; y < 32; ++y)
+              if (!(keep & (1u << y))) x[c + y] = 0.f;
           }
 #pragma unroll
           for (int y = 0; y < 32; y += 2) pk[y >> 1] = tt_pack(x[c + y], x[c + y + 1]);
@@ -720,14 +779,14 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 
 template <int D>
 cudaError_t bwd_launch(const SeqArgs& a, int dev, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& g,
-                       unsigned numbers, cudaStream_t st) {
+                       const CUtensorMap& o, unsigned numbers, cudaStream_t st) {
   static PtencOnce once;
   cudaError_t e = ptenc_first_use(once, dev, [] {
     const cudaError_t x = ptenc_allow_smem(k_seq_dq_tc<D>, BSmem<D>::TOTAL);
     return x != cudaSuccess ? x : ptenc_allow_smem(k_seq_dkv_tc<D>, BSmem<D>::TOTAL);
   });
   if (e != cudaSuccess) return e;
-  e = tree_launch(k_seq_dq_tc<D>, dim3(numbers * a.Hq), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
+  e = tree_launch(k_seq_dq_tc<D>, dim3(numbers * a.Hq), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g, o);
   if (e != cudaSuccess) return e;
   return tree_launch(k_seq_dkv_tc<D>, dim3((numbers + (unsigned)(a.pins * a.B)) * a.Hkv), ST_THREADS, BSmem<D>::TOTAL, 0, st, a, q, k, v, g);
 }
@@ -741,10 +800,10 @@ bool seq_backward_tc(const SeqArgs& args, int dtype, int dev, cudaStream_t st, c
   const long long pins = a.window > 0 && a.pinned != nullptr ? (a.window - 1 + TM - 1ll) / TM : 0;
   a.pins = pins * a.B <= numbers ? (int)pins : 0;
   if (dtype != PTENC_DTYPE_BF16 || a.D > 128 || 2 * numbers * a.Hq >= (1ll << 31)) return false;
-  CUtensorMap q, k, v, g;
+  CUtensorMap q, k, v, g, o;
   if (!seq_map(&q, a.q, a.D, a.Hq, a.n, a.qs) || !seq_map(&k, a.k, a.D, a.Hkv, a.n, a.ks) || !seq_map(&v, a.v, a.D, a.Hkv, a.n, a.vs) ||
-      !seq_map(&g, a.dout, a.D, a.Hq, a.n, (long long)a.Hq * a.D))
+      !seq_map(&g, a.dout, a.D, a.Hq, a.n, (long long)a.Hq * a.D) || !seq_map(&o, a.out, a.D, a.Hq, a.n, (long long)a.Hq * a.D))
     return false;
-  *e = a.D <= 64 ? bwd_launch<64>(a, dev, q, k, v, g, (unsigned)numbers, st) : bwd_launch<128>(a, dev, q, k, v, g, (unsigned)numbers, st);
+  *e = a.D <= 64 ? bwd_launch<64>(a, dev, q, k, v, g, o, (unsigned)numbers, st) : bwd_launch<128>(a, dev, q, k, v, g, o, (unsigned)numbers, st);
   return true;
 }
