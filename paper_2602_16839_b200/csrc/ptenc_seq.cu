@@ -174,14 +174,14 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
     for (int c = 0; c < DP / 16; ++c) o[i][c] = 0.f;
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
-  const int nt = seq_count(r);
+  const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
   for (int t = 0; t < nt; ++t) {
     const int j0 = seq_at(r, t) * S::M;
     __syncthreads();
     sg_load<T, DP>(sK, k, a.ks, j0, s.len, D);
     sg_load<T, DP>(sV, v, a.vs, j0, s.len, D);
     __syncthreads();
-    const bool all = seq_all(s, i0, i0 + S::M - 1, j0, j0 + S::M - 1);
+    const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R];
     sg_dot<DP>(x, sQ, sK, tx, ty, D);
 #pragma unroll
@@ -272,14 +272,14 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
     for (int c = 0; c < DP / 16; ++c) acc[i][c] = 0.f;
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
-  const int nt = seq_count(r);
+  const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
   for (int t = 0; t < nt; ++t) {
     const int j0 = seq_at(r, t) * S::M;
     __syncthreads();
     sg_load<T, DP>(sK, k, a.ks, j0, s.len, D);
     sg_load<T, DP>(sV, v, a.vs, j0, s.len, D);
     __syncthreads();
-    const bool all = seq_all(s, i0, i0 + S::M - 1, j0, j0 + S::M - 1);
+    const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R], y[S::R][S::R];
     sg_dot<DP>(x, sQ, sK, tx, ty, D);
     sg_dot<DP>(y, sG, sV, tx, ty, D);
@@ -333,7 +333,7 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
   for (int i = 0; i < S::R; ++i)
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
-  const int last = j0 < s.pin ? s.len - 1 : s.last(j1);
+  const int last = j0 < s.pin ? s.len - 1 : s.last(j1), until = seq_seen_until(s, j0, j0 + S::M - 1);
   for (int h = hk * a.g; h < (hk + 1) * a.g; ++h) {
     const T* q = static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D;
     const T* go = static_cast<const T*>(a.dout) + s.start * os + (long long)h * D;
@@ -348,7 +348,7 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
         s_delta[threadIdx.x] = row < s.len ? a.delta[at] : 0.f;
       }
       __syncthreads();
-      const bool all = i0 + S::M <= s.len && seq_all(s, i0, i0 + S::M - 1, j0, j0 + S::M - 1);
+      const bool all = i0 + S::M <= s.len && j0 + S::M - 1 <= i0 && i0 + S::M - 1 <= until;
       float x[S::R][S::R], y[S::R][S::R];
       sg_dot<DP>(x, sK, sQ, tx, ty, D);
       sg_dot<DP>(y, sV, sG, tx, ty, D);

@@ -89,9 +89,17 @@ __device__ __forceinline__ SeqRange seq_keys(const SeqView& s, int i0, int i1, i
 }
 __device__ __forceinline__ int seq_count(const SeqRange& r) { return r.np + max(0, r.s1 - r.s0 + 1); }
 __device__ __forceinline__ int seq_at(const SeqRange& r, int k) { return k < r.np ? k : r.s0 + k - r.np; }
-// Whether every row of [i0, i1] sees every key of [j0, j1].
-__device__ __forceinline__ bool seq_all(const SeqView& s, int i0, int i1, int j0, int j1) {
-  return j1 <= i0 && (j1 < s.pin || j0 >= s.low(i1));
+// Whether every row of [i0, i1] sees every key of [j0, j1], low1 = low(i1): a division that is not done once per tile (in the
+// tensor-core kernels it and the tests row by row had cost a third of the time under a window).
+__device__ __forceinline__ bool seq_all(const SeqView& s, int i0, int low1, int j0, int j1) {
+  return j1 <= i0 && (j1 < s.pin || j0 >= low1);
+}
+// The same from the keys' side: every row of [i0, i1] sees every key of [j0, j1] if j1 <= i0 and i1 <= seq_seen_until(j0, j1).
+__device__ __forceinline__ int seq_seen_until(const SeqView& s, int j0, int j1) {
+  if (s.cap == 0 || j1 < s.pin) return 0x7fffffff;
+  if (j0 < s.pin) return s.pin - 1;                // rows of the prompt alone
+  const long long x = (long long)s.pin + s.cap - 1 + (long long)((j0 - s.pin) / s.e) * s.e;
+  return x < 0x7fffffff ? (int)x : 0x7fffffff;
 }
 
 cudaError_t seq_forward_any(const SeqArgs& a, int dtype, int dev, cudaStream_t st);

@@ -188,12 +188,6 @@ __device__ __forceinline__ void mma_sums(uint32_t d, uint32_t a, uint32_t b, boo
   for (int k = 0; k < 8; ++k) mma_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, db + (k * 2048 >> 4), tt_idesc(D, 1), k > 0 ? 1u : (replace ? 0u : 1u));
 }
 
-// Bits of positions [lo, hi) in the word of positions [at, at + 32).
-__device__ __forceinline__ uint32_t st_run(int lo, int hi, int at) {
-  const int a = max(lo - at, 0), b = min(hi - at, 32);
-  return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
-}
-
 // One row of a gradient, columns [c0, c1), from tensor memory.
 template <int D>
 __device__ __forceinline__ void store_row(uint32_t t, int c0, int c1, float f, __nv_bfloat16* to, int Dr, bool real, bool wide) {
@@ -341,7 +335,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
       const SeqRange r = range_of(d);
-      const int n = d[B_N], i0 = d[B_TILE] * TM;
+      const int n = d[B_N], i0 = d[B_TILE] * TM, low1 = s.low(i0 + TM - 1);
       if (me == 1) {
         // the O tile is the softmax warps' alone: when they have read it and dO, this warp frees both
         const uint32_t at = nt + seq, sg = SM::stage_b(at);
@@ -362,7 +356,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           const int tile = seq_at(r, t);
           uint32_t* bad = s_bad + 4 * ((nt + t) & 1);    // read with the tile two before
           if (!wait(X + 8 * (X_STAT_EMPTY + ((nt + t) & 1)), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
-          if (!seq_all(s, i0, i0 + TM - 1, tile * SN, tile * SN + SN - 1)) {
+          if (!seq_all(s, i0, low1, tile * SN, tile * SN + SN - 1)) {
             if (lane < 4) bad[lane] = 0;
             __syncwarp();
             patch_tile(smem + sg * TILE, D / 64, tile * SN, s.len, 0, 1, bad);
@@ -398,7 +392,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
       const SeqRange r = range_of(d);
-      const int n = d[B_N], i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row);
+      const int n = d[B_N], i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row), low1 = s.low(i0 + TM - 1);
       const bool real = row < s.len;
       // delta from the O and dO tiles in shared memory: both threads of a row form it, so that no barrier stands between the warps.
       // (Read from memory, rows far apart, it cost 8000 cycles an item; so 1000.)
@@ -445,7 +439,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         ld32(ts, p);
         ld32(ts + 32, p + 32);
         wait_ld();
-        const bool all = seq_all(s, i0, i0 + TM - 1, j0, j0 + SN - 1);
+        const bool all = seq_all(s, i0, low1, j0, j0 + SN - 1);
 #pragma unroll
         for (int y = 0; y < 64; y += 2) {
           tt_both(tt_fma2(tt_two(p[y], p[y + 1]), scl2, nlse2), p[y], p[y + 1]);
@@ -620,21 +614,22 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       volatile int* d = desc + slot * B_WORDS;
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
-      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM;
+      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM, until = seq_seen_until(s, j0, j0 + TM - 1);
+      int at = 0;                                        // the tile within its head
       const float* stat = a.delta + (me == 0 ? (long long)a.Hq * a.n : 0) + (long long)d[B_HEAD] * a.g * a.n + s.start;
       for (int t = 0; t < n; ++t) {
         const uint32_t sg = me == 0 ? SM::stage_a(nt + t) : SM::stage_b(nt + t), buf = (nt + t) & 1;
-        const int hh = t / tiles, i0 = (tile0 + t - hh * tiles) * TM;
+        const int i0 = (tile0 + at) * TM;
         // asked for early: rows past the end are not seen by anybody
         float v[4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const int i = i0 + lane + 32 * y;
-          v[y] = i < s.len ? stat[(long long)hh * a.n + i] : 0.f;
+          v[y] = i < s.len ? stat[i] : 0.f;
         }
         if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
         bool odd = false;
-        if (!(i0 + TM <= s.len && seq_all(s, i0, i0 + TM - 1, j0, j0 + TM - 1))) {
+        if (!(i0 + TM <= s.len && j0 + TM - 1 <= i0 && i0 + TM - 1 <= until)) {
           if (lane < 4) bad[lane] = 0;
           __syncwarp();
           odd = patch_tile(smem + sg * TILE, D / 64, i0, s.len, 0, 1, bad);
@@ -653,6 +648,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         if (me == 1 && lane == 0) s_odd[buf] = odd;
         __syncwarp();
         if (lane == 0) bar_arrive(X + 8 * (X_STAT_FULL + buf));
+        if (++at == tiles) { at = 0; stat += a.n; }
       }
       if (!okay) break;
       __syncwarp();
@@ -682,13 +678,14 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       volatile int* d = desc + slot * B_WORDS;
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
-      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM, col = j0 + lrow, last = s.last(col);
+      const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM, col = j0 + lrow, last = s.last(col),
+                until = seq_seen_until(s, j0, j0 + TM - 1);
       int i0 = j0, left = tiles;
 #pragma unroll 1
       for (int t = 0; t < n; ++t, ++nt) {
         const uint32_t buf = nt & 1;
         const float* st = s_stat + buf * 2 * TM + 64 * half;
-        const bool all = i0 + TM <= s.len && seq_all(s, i0, i0 + TM - 1, j0, j0 + TM - 1);
+        const bool all = i0 + TM <= s.len && j0 + TM - 1 <= i0 && i0 + TM - 1 <= until;
         const int lo = col - i0 - 64 * half, hi = last - i0 - 64 * half;       // columns [lo, hi] see this token
         wait(X + 8 * (X_STAT_FULL + buf), (nt >> 1) & 1);
         wait(X + 8 * X_S_FULL, nt & 1);

@@ -11,7 +11,7 @@
 //    non-finite values out of the others, since 0 * NaN would carry them into rows that do not see them; rows that do get them back
 //    at the end.
 //  * warps 4..11: softmax, four warps per stream, a row per thread with its 128 scores in registers: mask, maximum, running sum in
-//    fp32 (base 2), P rounded to bf16 and handed over in halves.  O is rescaled only when the maximum has grown by more than 2^8.
+//    fp32 (base 2), P rounded to bf16.  O is rescaled only when the maximum has grown by more than 2^8.
 //  * Every wait is bounded: one that runs out raises an abort flag, every role leaves, copies and products in flight are drained and
 //    tensor memory is freed; the item's rows become NaN.
 #include "ptenc_seq_tc.cuh"
@@ -32,7 +32,7 @@ struct FSmem {
   static constexpr int OFF_CLC = OFF_Q + 2 * TILE;                   // 16 bytes of answer
   static constexpr int OFF_DESC = OFF_CLC + 16;                      // int [2][J_WORDS]
   static constexpr int OFF_BAR = (OFF_DESC + 2 * J_WORDS * 4 + 7) / 8 * 8;
-  static constexpr int N_BAR = 3 * STAGES + 18;
+  static constexpr int N_BAR = 3 * STAGES + 16;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;               // int [4]
   static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
@@ -60,18 +60,13 @@ __device__ __forceinline__ SeqView view_of(volatile int* d) {
   s.start = d[J_START]; s.len = d[J_LEN]; s.pin = d[J_PIN]; s.cap = d[J_CAP]; s.e = d[J_E];
   return s;
 }
-// Whether the whole item sees the whole key tile: nothing to mask, nothing to patch.
-__device__ __forceinline__ bool clean_tile(const SeqView& s, int i0, int rows, int tile) {
-  return seq_all(s, i0, i0 + rows - 1, tile * SN, tile * SN + SN - 1);
-}
-
 // Adds the non-finite values that were taken out of V tiles to 16 columns of a row that sees them.
 __device__ __noinline__ void add_odd(float* o, const __nv_bfloat16* v, long long vs, int c, int D, const SeqView s, int row, int row0,
                                      SeqRange r, int n) {
-  const int lo = s.low(row);
+  const int lo = s.low(row), low1 = s.low(row0 + ST_ROWS - 1);
   for (int u = 0; u < n; ++u) {
     const int tile = seq_at(r, u);
-    if (clean_tile(s, row0, ST_ROWS, tile)) continue;
+    if (seq_all(s, row0, low1, tile * SN, tile * SN + SN - 1)) continue;
     for (int j = tile * SN; j < min(tile * SN + SN, row + 1); ++j) {
       if (j >= s.pin && j < lo) continue;
       for (int y = 0; y < 16; ++y) {
@@ -96,7 +91,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);    // [0] abort, [1] TMEM base, [2] verdict on the next item
   volatile int* abort_flag = misc;
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
-  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16 /* [stream][half] */, o_full = p_full + 32, o_empty = o_full + 16,
+  const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, o_empty = o_full + 16,
                  q_full = o_empty + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16,
                  clc = item_empty + 16, drain = clc + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -105,8 +100,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); bar_init(ready + 8 * s, 2); }
     for (int s = 0; s < 2; ++s) {
       bar_init(s_full + 8 * s, 1);
-      bar_init(p_full + 16 * s, 4);
-      bar_init(p_full + 16 * s + 8, 4);
+      bar_init(p_full + 8 * s, 4);
       bar_init(o_full + 8 * s, 1);
       bar_init(o_empty + 8 * s, 4);
       bar_init(item_full + 8 * s, 1);
@@ -251,17 +245,14 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         v_there = true;
         if (first && !wait(o_empty + 8 * st, (ni & 1) ^ 1)) return false;      // O of the item before is out
         const uint64_t dv = desc_mn(sb + sg * TILE);
+        if (!wait(p_full + 8 * st, np & 1)) return false;
+        fence_after();
+        if (leader) {
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          if (!wait(p_full + 16 * st + 8 * hf, np & 1)) return false;
-          fence_after();
-          if (leader) {
-#pragma unroll
-            for (int k = 4 * hf; k < 4 * hf + 4; ++k)
-              mma_ts(tO + st * D, tS + st * SN + k * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : (first ? 0u : 1u));
-          }
-          __syncwarp();
+          for (int k = 0; k < 8; ++k)
+            mma_ts(tO + st * D, tS + st * SN + k * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : (first ? 0u : 1u));
         }
+        __syncwarp();
         ++np;
         if (last) {
           if (leader) commit(o_full + 8 * st);
@@ -322,7 +313,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       volatile int* d = desc + (seq & 1) * J_WORDS;
       if (d[J_KIND] == 0) break;
       const SeqView s = view_of(d);
-      const int row0 = d[J_ROW0], n = d[J_N];
+      const int row0 = d[J_ROW0], n = d[J_N], low1 = s.low(row0 + ST_ROWS - 1);
       SeqRange r;
       r.np = d[J_NP]; r.s0 = d[J_S0]; r.s1 = d[J_S1];
       for (int i = 0; i < n; ++i) {
@@ -331,7 +322,8 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         // rounds before or after.
         const uint32_t sg = SM::stage_v(nt + i);
         if (!wait(full + 8 * sg, SM::phase_v(nt + i))) { okay = false; break; }
-        if (!clean_tile(s, row0, ST_ROWS, tile) && patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2, nullptr) && lane == 0)
+        if (!seq_all(s, row0, low1, tile * SN, tile * SN + SN - 1) &&
+            patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2, nullptr) && lane == 0)
           d[J_ODD] = 1;
         __syncwarp();
         if (lane == 0) bar_arrive(ready + 8 * sg);
@@ -366,7 +358,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       SeqRange r;
       r.np = d[J_NP]; r.s0 = d[J_S0]; r.s1 = d[J_S1];
       const Stream us(s, row0, st);
-      const int i0 = row0 + TM * st, row = i0 + 32 * quarter + lane, low = s.low(row);
+      const int i0 = row0 + TM * st, row = i0 + 32 * quarter + lane, low = s.low(row), low1 = s.low(i0 + TM - 1);
       const int last = us.last();
       float m = -INFINITY, l = 0.f;                      // running maximum (of the raw scores) and sum
       bool first = true;
@@ -381,11 +373,15 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 #pragma unroll
         for (int c = 0; c < SN; c += 32) ld32(ts + c, x + c);
         wait_ld();
-        if (!seq_all(s, i0, i0 + TM - 1, tile * SN, tile * SN + SN - 1)) {
-          const int j0 = tile * SN, hi = row - j0, lo = low - j0, pn = s.pin - j0;
+        if (!seq_all(s, i0, low1, tile * SN, tile * SN + SN - 1)) {
+          const int j0 = tile * SN;
 #pragma unroll
-          for (int y = 0; y < SN; ++y)
-            if (y > hi || (y >= pn && y < lo)) x[y] = -INFINITY;
+          for (int c = 0; c < SN; c += 32) {
+            const uint32_t keep = st_run(0, row + 1, j0 + c) & ~st_run(s.pin, low, j0 + c);
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (!(keep & (1u << y))) x[c + y] = -INFINITY;
+          }
         }
         float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -432,13 +428,13 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             pk[y >> 1] = tt_pack(e0, e1);                // P in bf16, half a step of 2^-8 per weight; the sum is of the weights as they were
           }
           st16(ts + c / 2, pk);
-          if (c == 32 || c == 96) {
-            wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 16 * st + (c == 32 ? 0 : 8));
-          }
         }
+        // P is handed over in one piece: in halves or quarters its product would start earlier, but each hand-over costs the warp more
+        // (16384 tokens, 28 heads of 128: 1535 us, in halves 1555, in quarters 1760)
+        wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_full + 8 * st);
         float s0, s1;
         tt_both(tt_add2(sum[0], sum[1]), s0, s1);
         l += s0 + s1;

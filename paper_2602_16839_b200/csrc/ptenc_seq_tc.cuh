@@ -13,6 +13,12 @@ constexpr int ST_REGS_LOW = 72, ST_REGS_HIGH = 216;
 static_assert(128 * ST_REGS_LOW + 256 * ST_REGS_HIGH <= 384 * 168, "the split waits for registers that do not exist");
 constexpr float ST_LOG2E = 1.4426950408889634f, ST_LN2 = 0.6931471805599453f;
 
+// Bits of positions [lo, hi) in the word of positions [at, at + 32).
+__device__ __forceinline__ uint32_t st_run(int lo, int hi, int at) {
+  const int a = max(lo - at, 0), b = min(hi - at, 32);
+  return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
+}
+
 // ------------------------------------------------------------------------------------------------ taking over CTAs
 // Asks for a CTA of the grid that has not started yet; 16 bytes of answer arrive at `to` and count at the barrier.
 __device__ __forceinline__ void clc_ask(uint32_t to, uint32_t bar) {
