@@ -5,11 +5,17 @@
 //
 // A CTA has a tile of M rows (64, or 32 where a head is wider than 128) and goes through the tiles of the other side, all in
 // fp32 from shared memory, an (M / 16) x (M / 16) block of scores and (M / 16) x (D / 16) of sums per thread.  The backward pass is
-// two kernels, one per side, each recomputing the scores: seven products instead of five, but no sums across CTAs, so that
-// results have the same bits every time.
+// two kernels, one per side, each recomputing the scores: seven products instead of five, but no sums in an order that changes, so
+// that results have the same bits every time.  The tiles of the other side are copied a tile ahead where shared memory has room for
+// two.  Gradients of keys and values: where there are few tiles the heads of a group are dealt to a cluster of CTAs, which add their
+// sums in order through distributed shared memory.
+#include <cooperative_groups.h>
+
 #include "ptenc_seq.cuh"
 
 namespace {
+
+namespace cg = cooperative_groups;
 
 constexpr int SG_THREADS = 256;
 // In a tile that some rows see in part, what a row does not see is marked by this NaN, which arithmetic does not produce, and
@@ -22,31 +28,42 @@ struct SgShape {
   static constexpr int R = M / 16;               // rows, and columns of scores, of a thread
   static constexpr int LD = DP + 4;              // row pitch: rows 4 banks apart, so 16-byte reads of 8 rows fill all banks
   static constexpr int LP = M + 4;
-  static constexpr int FWD = (3 * M * LD + M * LP) * 4;
-  static constexpr int DQ = (4 * M * LD + M * LP) * 4;
-  static constexpr int DKV = (4 * M * LD + 2 * M * LP + 2 * M) * 4;
+  static constexpr int TILE = M * LD;
+  // floats of shared memory with `bufs` buffers for the tiles of the other side
+  static constexpr int fwd(int bufs) { return (1 + 2 * bufs) * TILE + M * LP; }
+  static constexpr int dq(int bufs) { return (2 + 2 * bufs) * TILE + M * LP; }
+  static constexpr int dkv(int bufs) { return (2 + 2 * bufs) * TILE + 2 * M * LP + bufs * 2 * M; }
+  static constexpr int room = 232448 / 4;
+  static constexpr int BF = fwd(2) <= room ? 2 : 1, BQ = dq(2) <= room ? 2 : 1, BK = dkv(2) <= room ? 2 : 1;
+  static_assert(fwd(BF) <= room && dq(BQ) <= room && dkv(BK) <= room, "shared memory of one CTA");
 };
 
-// Rows [row0, row0 + M) of a sequence's tensor to shared memory; rows past `rows` and columns past D are zero.
+// Rows [row0, row0 + M) of a sequence's tensor to shared memory; rows past `rows` and columns past D are zero.  fp32 is copied
+// asynchronously: sg_arrived() waits for everything asked for.
 template <typename T, int DP>
 __device__ __forceinline__ void sg_load(float* to, const T* base, long long stride, int row0, int rows, int D) {
   using S = SgShape<DP>;
   constexpr int N = 16 / sizeof(T);
   for (int x = threadIdx.x; x < S::M * (DP / N); x += SG_THREADS) {
     const int r = x / (DP / N), c = (x - r * (DP / N)) * N;
-    float f[N];
-    if (row0 + r < rows && c < D) {
-      const uint4 w = *reinterpret_cast<const uint4*>(base + (long long)(row0 + r) * stride + c);
+    const bool there = row0 + r < rows && c < D;
+    const T* from = base + (there ? (long long)(row0 + r) * stride + c : 0);
+    float* at = to + r * S::LD + c;
+    if constexpr (sizeof(T) == 4) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"((uint32_t)__cvta_generic_to_shared(at)), "l"(from), "r"(there ? 16 : 0) : "memory");
+    } else {
+      const uint4 w = there ? *reinterpret_cast<const uint4*>(from) : make_uint4(0u, 0u, 0u, 0u);
       const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
-      for (int y = 0; y < N; ++y) f[y] = ptenc_to_float(e[y]);
-    } else {
-#pragma unroll
-      for (int y = 0; y < N; ++y) f[y] = 0.f;
+      for (int y = 0; y < N; y += 4)
+        *reinterpret_cast<float4*>(at + y) = make_float4(ptenc_to_float(e[y]), ptenc_to_float(e[y + 1]), ptenc_to_float(e[y + 2]), ptenc_to_float(e[y + 3]));
     }
-#pragma unroll
-    for (int y = 0; y < N; y += 4) *reinterpret_cast<float4*>(to + r * S::LD + c + y) = make_float4(f[y], f[y + 1], f[y + 2], f[y + 3]);
   }
+}
+__device__ __forceinline__ void sg_arrived() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
 }
 
 // acc[i][j] = row (ty + 16 i) of A . row (tx + 16 j) of B
@@ -149,9 +166,8 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
   float* sQ = sm;
-  float* sK = sQ + S::M * S::LD;
-  float* sV = sK + S::M * S::LD;
-  float* sP = sV + S::M * S::LD;
+  float* sKV = sQ + S::TILE;                             // [buffer][K, V]
+  float* sP = sKV + 2 * S::BF * S::TILE;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int h = blockIdx.y, hk = h / a.g, D = a.D;
   tree_after_previous();
@@ -175,12 +191,20 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
   const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
+  auto fetch = [&](int t) {
+    const int j0 = seq_at(r, t) * S::M;
+    float* to = sKV + (S::BF == 2 ? (t & 1) * 2 * S::TILE : 0);
+    sg_load<T, DP>(to, k, a.ks, j0, s.len, D);
+    sg_load<T, DP>(to + S::TILE, v, a.vs, j0, s.len, D);
+  };
+  fetch(0);
   for (int t = 0; t < nt; ++t) {
     const int j0 = seq_at(r, t) * S::M;
-    __syncthreads();
-    sg_load<T, DP>(sK, k, a.ks, j0, s.len, D);
-    sg_load<T, DP>(sV, v, a.vs, j0, s.len, D);
-    __syncthreads();
+    if (S::BF == 1 && t > 0) { __syncthreads(); fetch(t); }
+    sg_arrived();                                        // also: the other buffer's tile and P are not needed any more
+    if (S::BF == 2 && t + 1 < nt) fetch(t + 1);
+    const float* sK = sKV + (S::BF == 2 ? (t & 1) * 2 * S::TILE : 0);
+    const float* sV = sK + S::TILE;
     const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R];
     sg_dot<DP>(x, sQ, sK, tx, ty, D);
@@ -234,10 +258,9 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
   float* sQ = sm;
-  float* sG = sQ + S::M * S::LD;
-  float* sK = sG + S::M * S::LD;
-  float* sV = sK + S::M * S::LD;
-  float* sP = sV + S::M * S::LD;
+  float* sG = sQ + S::TILE;
+  float* sKV = sG + S::TILE;                             // [buffer][K, V]; first O
+  float* sP = sKV + 2 * S::BQ * S::TILE;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int h = blockIdx.y, hk = h / a.g, D = a.D;
   tree_after_previous();
@@ -250,8 +273,8 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   const T* v = static_cast<const T*>(a.v) + s.start * a.vs + (long long)hk * D;
   sg_load<T, DP>(sQ, static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D, a.qs, i0, s.len, D);
   sg_load<T, DP>(sG, static_cast<const T*>(a.dout) + first, os, i0, s.len, D);
-  sg_load<T, DP>(sK, static_cast<const T*>(a.out) + first, os, i0, s.len, D);
-  __syncthreads();
+  sg_load<T, DP>(sKV, static_cast<const T*>(a.out) + first, os, i0, s.len, D);
+  sg_arrived();
   const float c2 = a.scale * LOG2E;
   float acc[S::R][DP / 16], lse2[S::R], delta[S::R];
 #pragma unroll
@@ -260,7 +283,7 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
     float sum = 0.f;
     for (int c = 4 * tx; c < D; c += 64)
 #pragma unroll
-      for (int y = 0; y < 4; ++y) sum = fmaf(sG[row * S::LD + c + y], sK[row * S::LD + c + y], sum);
+      for (int y = 0; y < 4; ++y) sum = fmaf(sG[row * S::LD + c + y], sKV[row * S::LD + c + y], sum);
     delta[i] = sg_row_sum(sum);
     const long long at = (long long)(s.start + i0 + row) * a.Hq + h;
     lse2[i] = 0.f;
@@ -273,12 +296,21 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
   const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
+  auto fetch = [&](int t) {
+    const int j0 = seq_at(r, t) * S::M;
+    float* to = sKV + (S::BQ == 2 ? (t & 1) * 2 * S::TILE : 0);
+    sg_load<T, DP>(to, k, a.ks, j0, s.len, D);
+    sg_load<T, DP>(to + S::TILE, v, a.vs, j0, s.len, D);
+  };
+  __syncthreads();                                       // O has been read
+  fetch(0);
   for (int t = 0; t < nt; ++t) {
     const int j0 = seq_at(r, t) * S::M;
-    __syncthreads();
-    sg_load<T, DP>(sK, k, a.ks, j0, s.len, D);
-    sg_load<T, DP>(sV, v, a.vs, j0, s.len, D);
-    __syncthreads();
+    if (S::BQ == 1 && t > 0) { __syncthreads(); fetch(t); }
+    sg_arrived();
+    if (S::BQ == 2 && t + 1 < nt) fetch(t + 1);
+    const float* sK = sKV + (S::BQ == 2 ? (t & 1) * 2 * S::TILE : 0);
+    const float* sV = sK + S::TILE;
     const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R], y[S::R][S::R];
     sg_dot<DP>(x, sQ, sK, tx, ty, D);
@@ -303,26 +335,26 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   sg_store<T, DP>(static_cast<T*>(a.dq) + s.start * a.dqs + (long long)h * D, a.dqs, acc, f, i0, s.len, D, tx, ty);
 }
 
-// dk and dv of a tile of tokens: all heads of the group, one after another.
+// dk and dv of a tile of tokens: the CTA's share of the group's heads, one after another.
 template <typename T, int DP>
 __global__ void __launch_bounds__(SG_THREADS)
 k_seq_dkv(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
   float* sK = sm;
-  float* sV = sK + S::M * S::LD;
-  float* sQ = sV + S::M * S::LD;
-  float* sG = sQ + S::M * S::LD;
-  float* sP = sG + S::M * S::LD;
+  float* sV = sK + S::TILE;
+  float* sQG = sV + S::TILE;                             // [buffer][Q, dO]
+  float* sP = sQG + 2 * S::BK * S::TILE;
   float* sD = sP + S::M * S::LP;
-  float* s_lse = sD + S::M * S::LP;
-  float* s_delta = s_lse + S::M;
+  float* sStat = sD + S::M * S::LP;                      // [buffer][lse (base 2), delta][M]
+  cg::cluster_group cluster = cg::this_cluster();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int hk = blockIdx.y, D = a.D;
+  const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int hk = blockIdx.y, D = a.D, heads = a.g / cs, h0 = hk * a.g + rank * heads;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)blockIdx.x, S::M, &s, &tile)) return;      // early tiles are seen by most
+  if (!seq_find(a, (int)blockIdx.x / cs, S::M, &s, &tile)) return;      // early tiles are seen by most; a cluster agrees
   const int j0 = tile * S::M, j1 = min(j0 + S::M, s.len) - 1;
   sg_load<T, DP>(sK, static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D, a.ks, j0, s.len, D);
   sg_load<T, DP>(sV, static_cast<const T*>(a.v) + s.start * a.vs + (long long)hk * D, a.vs, j0, s.len, D);
@@ -334,42 +366,81 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
   const int last = j0 < s.pin ? s.len - 1 : s.last(j1), until = seq_seen_until(s, j0, j0 + S::M - 1);
-  for (int h = hk * a.g; h < (hk + 1) * a.g; ++h) {
-    const T* q = static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D;
-    const T* go = static_cast<const T*>(a.dout) + s.start * os + (long long)h * D;
-    for (int i0 = j0; i0 <= last; i0 += S::M) {
-      __syncthreads();
-      sg_load<T, DP>(sQ, q, a.qs, i0, s.len, D);
-      sg_load<T, DP>(sG, go, os, i0, s.len, D);
-      if (threadIdx.x < S::M) {
-        const int row = i0 + threadIdx.x;
-        const long long at = (long long)(s.start + row) * a.Hq + h;
-        s_lse[threadIdx.x] = row < s.len ? a.lse[at] * LOG2E : 0.f;
-        s_delta[threadIdx.x] = row < s.len ? a.delta[at] : 0.f;
-      }
-      __syncthreads();
-      const bool all = i0 + S::M <= s.len && j0 + S::M - 1 <= i0 && i0 + S::M - 1 <= until;
-      float x[S::R][S::R], y[S::R][S::R];
-      sg_dot<DP>(x, sK, sQ, tx, ty, D);
-      sg_dot<DP>(y, sV, sG, tx, ty, D);
-#pragma unroll
-      for (int j = 0; j < S::R; ++j) {                   // queries run along the row
-        const int c = tx + 16 * j, row = i0 + c;
-        const float lse2 = s_lse[c], delta = s_delta[c];
-        const int lo = s.low(row);
-#pragma unroll
-        for (int i = 0; i < S::R; ++i) {
-          const int col = j0 + ty + 16 * i;
-          float p = exp2f(fmaf(x[i][j], c2, -lse2)), ds = p * (y[i][j] - delta);
-          if (!all && !(row < s.len && col <= row && (col < s.pin || col >= lo))) p = ds = __uint_as_float(SG_UNSEEN);
-          sP[(ty + 16 * i) * S::LP + c] = p;
-          sD[(ty + 16 * i) * S::LP + c] = ds;
-        }
-      }
-      __syncthreads();
-      sg_add<DP>(dv, sP, sG, tx, ty, all);
-      sg_add<DP>(dk, sD, sQ, tx, ty, all);
+  const int tiles = last / S::M - tile + 1, nt = tiles * heads;
+  auto fetch = [&](int t) {
+    const int hh = t / tiles, i0 = (tile + t - hh * tiles) * S::M, h = h0 + hh;
+    float* to = sQG + (S::BK == 2 ? (t & 1) * 2 * S::TILE : 0);
+    float* st = sStat + (S::BK == 2 ? (t & 1) * 2 * S::M : 0);
+    sg_load<T, DP>(to, static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D, a.qs, i0, s.len, D);
+    sg_load<T, DP>(to + S::TILE, static_cast<const T*>(a.dout) + s.start * os + (long long)h * D, os, i0, s.len, D);
+    if (threadIdx.x < S::M) {
+      const int row = i0 + threadIdx.x;
+      const long long at = (long long)(s.start + row) * a.Hq + h;
+      st[threadIdx.x] = row < s.len ? a.lse[at] * LOG2E : 0.f;
+      st[S::M + threadIdx.x] = row < s.len ? a.delta[at] : 0.f;
     }
+  };
+  fetch(0);
+  for (int t = 0; t < nt; ++t) {
+    const int i0 = (tile + t % tiles) * S::M;
+    if (S::BK == 1 && t > 0) { __syncthreads(); fetch(t); }
+    sg_arrived();
+    if (S::BK == 2 && t + 1 < nt) fetch(t + 1);
+    const float* sQ = sQG + (S::BK == 2 ? (t & 1) * 2 * S::TILE : 0);
+    const float* sG = sQ + S::TILE;
+    const float* st = sStat + (S::BK == 2 ? (t & 1) * 2 * S::M : 0);
+    const bool all = i0 + S::M <= s.len && j0 + S::M - 1 <= i0 && i0 + S::M - 1 <= until;
+    float x[S::R][S::R], y[S::R][S::R];
+    sg_dot<DP>(x, sK, sQ, tx, ty, D);
+    sg_dot<DP>(y, sV, sG, tx, ty, D);
+#pragma unroll
+    for (int j = 0; j < S::R; ++j) {                     // queries run along the row
+      const int c = tx + 16 * j, row = i0 + c;
+      const float lse2 = st[c], delta = st[S::M + c];
+      const int lo = all ? 0 : s.low(row);
+#pragma unroll
+      for (int i = 0; i < S::R; ++i) {
+        const int col = j0 + ty + 16 * i;
+        float p = exp2f(fmaf(x[i][j], c2, -lse2)), ds = p * (y[i][j] - delta);
+        if (!all && !(row < s.len && col <= row && (col < s.pin || col >= lo))) p = ds = __uint_as_float(SG_UNSEEN);
+        sP[(ty + 16 * i) * S::LP + c] = p;
+        sD[(ty + 16 * i) * S::LP + c] = ds;
+      }
+    }
+    __syncthreads();
+    sg_add<DP>(dv, sP, sG, tx, ty, all);
+    sg_add<DP>(dk, sD, sQ, tx, ty, all);
+  }
+  if (cs > 1) {
+    // every CTA's sums to its shared memory, over K and V; each then adds a share of the rows of all, in order
+    __syncthreads();
+    float* mine[2] = {sK, sV};
+#pragma unroll
+    for (int i = 0; i < S::R; ++i)
+#pragma unroll
+      for (int c = 0; c < DP / 64; ++c) {
+        const int at = (ty + 16 * i) * S::LD + 4 * tx + 64 * c;
+        *reinterpret_cast<float4*>(mine[0] + at) = make_float4(dk[i][4 * c], dk[i][4 * c + 1], dk[i][4 * c + 2], dk[i][4 * c + 3]);
+        *reinterpret_cast<float4*>(mine[1] + at) = make_float4(dv[i][4 * c], dv[i][4 * c + 1], dv[i][4 * c + 2], dv[i][4 * c + 3]);
+      }
+    cluster.sync();
+    T* to[2] = {static_cast<T*>(a.dk) + s.start * a.dks + (long long)hk * D, static_cast<T*>(a.dv) + s.start * a.dvs + (long long)hk * D};
+    const int quads = D / 4;
+    for (int x = rank * SG_THREADS + threadIdx.x; x < 2 * S::M * quads; x += cs * SG_THREADS) {
+      const int which = x / (S::M * quads), rem = x - which * S::M * quads, row = rem / quads, c = 4 * (rem - row * quads);
+      if (j0 + row >= s.len) continue;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int q = 0; q < cs; ++q) {
+        const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine[which] + row * S::LD + c, q));
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+      }
+      const float f = which == 0 ? a.scale : 1.f;
+      T* at = to[which] + (long long)(j0 + row) * (which == 0 ? a.dks : a.dvs) + c;
+      at[0] = ptenc_from_float<T>(sum.x * f); at[1] = ptenc_from_float<T>(sum.y * f);
+      at[2] = ptenc_from_float<T>(sum.z * f); at[3] = ptenc_from_float<T>(sum.w * f);
+    }
+    cluster.sync();                                      // nobody leaves while its sums may be read
+    return;
   }
   float one[S::R], f[S::R];
 #pragma unroll
@@ -383,9 +454,9 @@ cudaError_t sg_attributes(int dev) {
   static PtencOnce once;
   return ptenc_first_use(once, dev, [] {
     using S = SgShape<DP>;
-    cudaError_t e = ptenc_allow_smem(k_seq_fwd<T, DP>, S::FWD);
-    if (e == cudaSuccess) e = ptenc_allow_smem(k_seq_dq<T, DP>, S::DQ);
-    return e == cudaSuccess ? ptenc_allow_smem(k_seq_dkv<T, DP>, S::DKV) : e;
+    cudaError_t e = ptenc_allow_smem(k_seq_fwd<T, DP>, S::fwd(S::BF) * 4);
+    if (e == cudaSuccess) e = ptenc_allow_smem(k_seq_dq<T, DP>, S::dq(S::BQ) * 4);
+    return e == cudaSuccess ? ptenc_allow_smem(k_seq_dkv<T, DP>, S::dkv(S::BK) * 4) : e;
   });
 }
 
@@ -394,7 +465,7 @@ cudaError_t sg_fwd(const SeqArgs& a, int dev, cudaStream_t st) {
   using S = SgShape<DP>;
   const cudaError_t e = sg_attributes<T, DP>(dev);
   if (e != cudaSuccess) return e;
-  return tree_launch(k_seq_fwd<T, DP>, dim3((unsigned)seq_numbers(a.n, a.B, S::M), a.Hq), SG_THREADS, S::FWD, 0, st, a);
+  return tree_launch(k_seq_fwd<T, DP>, dim3((unsigned)seq_numbers(a.n, a.B, S::M), a.Hq), SG_THREADS, S::fwd(S::BF) * 4, 0, st, a);
 }
 
 template <typename T, int DP>
@@ -403,8 +474,18 @@ cudaError_t sg_bwd(const SeqArgs& a, int dev, cudaStream_t st) {
   cudaError_t e = sg_attributes<T, DP>(dev);
   if (e != cudaSuccess) return e;
   const unsigned x = (unsigned)seq_numbers(a.n, a.B, S::M);
-  e = tree_launch(k_seq_dq<T, DP>, dim3(x, a.Hq), SG_THREADS, S::DQ, 0, st, a);
-  return e != cudaSuccess ? e : tree_launch(k_seq_dkv<T, DP>, dim3(x, a.Hkv), SG_THREADS, S::DKV, 0, st, a);
+  e = tree_launch(k_seq_dq<T, DP>, dim3(x, a.Hq), SG_THREADS, S::dq(S::BQ) * 4, 0, st, a);
+  if (e != cudaSuccess) return e;
+  int sms = 0;
+  e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  // The heads of a group over a cluster of CTAs, as many as divide it (eight at most), until each SM has two: nine sequences of 3001
+  // tokens, four heads to a KV head: 730 us with one CTA per tile.
+  int cs = 1;
+  for (int d = 2; d <= 8 && (long long)x * a.Hkv * cs < 2ll * sms; ++d)
+    if (a.g % d == 0) cs = d;
+  if ((long long)x * cs >= (1ll << 31)) cs = 1;
+  return tree_launch(k_seq_dkv<T, DP>, dim3(x * cs, a.Hkv), SG_THREADS, S::dkv(S::BK) * 4, cs, st, a);
 }
 
 template <typename T>
