@@ -12,6 +12,7 @@
 #include <cooperative_groups.h>
 
 #include "ptenc_seq.cuh"
+#include "ptenc_tc.cuh"
 
 namespace {
 
@@ -66,35 +67,44 @@ __device__ __forceinline__ void sg_arrived() {
   __syncthreads();
 }
 
-// acc[i][j] = row (ty + 16 i) of A . row (tx + 16 j) of B
+// acc[i][j] = row (ty + 16 i) of A . row (tx + 16 j) of B.  Two multiply-adds per instruction, here and below: with one the kernels
+// were bound by issuing them.
 template <int DP>
 __device__ __forceinline__ void sg_dot(float (&acc)[SgShape<DP>::R][SgShape<DP>::R], const float* A, const float* B, int tx, int ty, int D) {
   using S = SgShape<DP>;
+  uint64_t two[S::R][S::R];                      // sums over the even and over the odd places
 #pragma unroll
   for (int i = 0; i < S::R; ++i)
 #pragma unroll
-    for (int j = 0; j < S::R; ++j) acc[i][j] = 0.f;
+    for (int j = 0; j < S::R; ++j) two[i][j] = 0ull;
 #pragma unroll 4
   for (int c = 0; c < D; c += 4) {
-    float4 x[S::R], y[S::R];
+    ulonglong2 x[S::R], y[S::R];
 #pragma unroll
     for (int i = 0; i < S::R; ++i) {
-      x[i] = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * S::LD + c);
-      y[i] = *reinterpret_cast<const float4*>(B + (tx + 16 * i) * S::LD + c);
+      x[i] = *reinterpret_cast<const ulonglong2*>(A + (ty + 16 * i) * S::LD + c);
+      y[i] = *reinterpret_cast<const ulonglong2*>(B + (tx + 16 * i) * S::LD + c);
     }
 #pragma unroll
     for (int i = 0; i < S::R; ++i)
 #pragma unroll
-      for (int j = 0; j < S::R; ++j)
-        acc[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, acc[i][j]))));
+      for (int j = 0; j < S::R; ++j) two[i][j] = tt_fma2(x[i].x, y[j].x, tt_fma2(x[i].y, y[j].y, two[i][j]));
   }
+#pragma unroll
+  for (int i = 0; i < S::R; ++i)
+#pragma unroll
+    for (int j = 0; j < S::R; ++j) {
+      float lo, hi;
+      tt_both(two[i][j], lo, hi);
+      acc[i][j] = lo + hi;
+    }
 }
 
 // acc[i][4 c + y] += sum_m P[ty + 16 i][m] * B[m][4 tx + 64 c + y]
 template <int DP, bool SOME>
-__device__ __forceinline__ void sg_add_t(float (&acc)[SgShape<DP>::R][DP / 16], const float* P, const float* B, int tx, int ty) {
+__device__ __forceinline__ void sg_add_t(uint64_t (&acc)[SgShape<DP>::R][DP / 32], const float* P, const float* B, int tx, int ty) {
   using S = SgShape<DP>;
-#pragma unroll 1
+#pragma unroll 2
   for (int m = 0; m < S::M; m += 4) {
     float4 p[S::R];
 #pragma unroll
@@ -103,15 +113,14 @@ __device__ __forceinline__ void sg_add_t(float (&acc)[SgShape<DP>::R][DP / 16], 
     for (int k = 0; k < 4; ++k) {
 #pragma unroll
       for (int c = 0; c < DP / 64; ++c) {
-        const float4 b = *reinterpret_cast<const float4*>(B + (m + k) * S::LD + 4 * tx + 64 * c);
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(B + (m + k) * S::LD + 4 * tx + 64 * c);
 #pragma unroll
         for (int i = 0; i < S::R; ++i) {
           const float w = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
           if (SOME && __float_as_uint(w) == SG_UNSEEN) continue;
-          acc[i][4 * c] = fmaf(w, b.x, acc[i][4 * c]);
-          acc[i][4 * c + 1] = fmaf(w, b.y, acc[i][4 * c + 1]);
-          acc[i][4 * c + 2] = fmaf(w, b.z, acc[i][4 * c + 2]);
-          acc[i][4 * c + 3] = fmaf(w, b.w, acc[i][4 * c + 3]);
+          const uint64_t w2 = tt_two(w, w);
+          acc[i][2 * c] = tt_fma2(w2, b.x, acc[i][2 * c]);
+          acc[i][2 * c + 1] = tt_fma2(w2, b.y, acc[i][2 * c + 1]);
         }
       }
     }
@@ -121,16 +130,21 @@ __device__ __forceinline__ void sg_add_t(float (&acc)[SgShape<DP>::R][DP / 16], 
 // keys over four heads of 976 tokens: 1.1e-6 of their size in one chain of additions, and less than the scores' own 6e-7 so).
 template <int DP>
 __device__ __forceinline__ void sg_add(float (&acc)[SgShape<DP>::R][DP / 16], const float* P, const float* B, int tx, int ty, bool all) {
-  float sum[SgShape<DP>::R][DP / 16];
+  uint64_t sum[SgShape<DP>::R][DP / 32];
 #pragma unroll
   for (int i = 0; i < SgShape<DP>::R; ++i)
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) sum[i][c] = 0.f;
+    for (int c = 0; c < DP / 32; ++c) sum[i][c] = 0ull;
   if (all) sg_add_t<DP, false>(sum, P, B, tx, ty); else sg_add_t<DP, true>(sum, P, B, tx, ty);
 #pragma unroll
   for (int i = 0; i < SgShape<DP>::R; ++i)
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) acc[i][c] += sum[i][c];
+    for (int c = 0; c < DP / 32; ++c) {
+      float lo, hi;
+      tt_both(sum[i][c], lo, hi);
+      acc[i][2 * c] += lo;
+      acc[i][2 * c + 1] += hi;
+    }
 }
 
 template <typename T, int DP>
