@@ -331,11 +331,13 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
     sg_dot<DP>(y, sG, sV, tx, ty, D);
 #pragma unroll
     for (int i = 0; i < S::R; ++i) {
-      const int row = i0 + ty + 16 * i, lo = s.low(row);
+      const int row = i0 + ty + 16 * i, lo = all ? 0 : s.low(row);
+      const bool alone = !all && s.alone(row);
 #pragma unroll
       for (int j = 0; j < S::R; ++j) {
         const int col = j0 + tx + 16 * j;
         float ds = exp2f(fmaf(x[i][j], c2, -lse2[i])) * (y[i][j] - delta[i]);
+        if (alone) ds = 0.f;
         if (!all && !(col <= row && (col < s.pin || col >= lo))) ds = __uint_as_float(SG_UNSEEN);
         sP[(ty + 16 * i) * S::LP + tx + 16 * j] = ds;
       }
@@ -412,10 +414,11 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
       const int c = tx + 16 * j, row = i0 + c;
       const float lse2 = st[c], delta = st[S::M + c];
       const int lo = all ? 0 : s.low(row);
+      const bool alone = !all && s.alone(row);
 #pragma unroll
       for (int i = 0; i < S::R; ++i) {
         const int col = j0 + ty + 16 * i;
-        float p = exp2f(fmaf(x[i][j], c2, -lse2)), ds = p * (y[i][j] - delta);
+        float p = exp2f(fmaf(x[i][j], c2, -lse2)), ds = alone ? 0.f : p * (y[i][j] - delta);
         if (!all && !(row < s.len && col <= row && (col < s.pin || col >= lo))) p = ds = __uint_as_float(SG_UNSEEN);
         sP[(ty + 16 * i) * S::LP + c] = p;
         sD[(ty + 16 * i) * S::LP + c] = ds;

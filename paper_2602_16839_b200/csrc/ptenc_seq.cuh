@@ -35,6 +35,9 @@ struct SeqView {
     const int over = i - pin + 1 - cap;
     return pin + (over > 0 ? (over + e - 1) / e * e : 0);      // below i + e, and i < 2^31 - 512
   }
+  // Token i sees itself alone: its weight is one whatever its score, and its score has a gradient of exactly zero, not what the
+  // roundings of two equal sums leave.
+  __device__ __forceinline__ bool alone(int i) const { return i == 0 || (cap != 0 && pin == 0 && low(i) == i); }
   __device__ __forceinline__ int last(int j) const {
     if (cap == 0 || j < pin) return len - 1;
     const long long x = (long long)pin + cap - 1 + (long long)((j - pin) / e) * e;

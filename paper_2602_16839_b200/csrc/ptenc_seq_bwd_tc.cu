@@ -40,12 +40,12 @@ struct BSmem {
   // Two rings: of the tiles that two products use far apart (K, or Q) and of the others (V, or dO).
   static constexpr int RA = D == 128 ? 3 : 5, RB = D == 128 ? 2 : 5, STAGES = RA + RB;
   static constexpr int OFF_AB = STAGES * TILE;                       // the item's own two tiles
-  static constexpr int OFF_STAT = OFF_AB + 2 * TILE;                 // float [2][2][128]
+  static constexpr int OFF_STAT = OFF_AB + 2 * TILE;                 // float [2][2][128], see the kernels
   static constexpr int OFF_CLC = OFF_STAT + 4 * TM * 4;
   static constexpr int OFF_BAD = OFF_CLC + 16;                       // uint32 [2][2][4]: rows of patched tiles with non-finite values
   static constexpr int OFF_DESC = OFF_BAD + 64;
   static constexpr int OFF_BAR = (OFF_DESC + 2 * B_WORDS * 4 + 7) / 8 * 8;
-  static constexpr int N_BAR = 3 * STAGES + 22;
+  static constexpr int N_BAR = 3 * STAGES + 23;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;
   static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
@@ -57,7 +57,7 @@ struct BSmem {
 };
 
 // Barriers after the stages' full, empty and ready ones.
-enum { X_A_FULL, X_A_EMPTY, X_B_FULL, X_B_EMPTY, X_O_READ, X_S_FULL, X_S_FULL1, X_DP_FULL, X_P_READY, X_DS_READY, X_ACC_FULL, X_ACC_EMPTY, X_STAT_FULL, X_STAT_FULL1,
+enum { X_A_FULL, X_A_EMPTY, X_B_FULL, X_B_EMPTY, X_O_READ, X_SUMS, X_S_FULL, X_S_FULL1, X_DP_FULL, X_P_READY, X_DS_READY, X_ACC_FULL, X_ACC_EMPTY, X_STAT_FULL, X_STAT_FULL1,
        X_STAT_EMPTY, X_STAT_EMPTY1, X_ITEM_FULL, X_ITEM_FULL1, X_ITEM_EMPTY, X_ITEM_EMPTY1, X_CLC, X_DRAIN };
 
 // What a CTA of either kernel does first; returns the TMEM base.  b_users: who frees the item's second tile.
@@ -69,7 +69,7 @@ __device__ __forceinline__ uint32_t bwd_begin(uint8_t* smem, uint32_t sb, int ti
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS, x = ready + 8 * NS;
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); bar_init(ready + 8 * s, 1); }
-    const int counts[] = {1, 1, 1, b_users, 8, 1, 1, 1, 8, 8, 1, 8, 2, 2, 8, 8, 1, 1, 1 + 2 + 8, 1 + 2 + 8, 1, 1};
+    const int counts[] = {1, 1, 1, b_users, 8, 8, 1, 1, 1, 8, 8, 1, 8, 2, 2, 8, 8, 1, 1, 1 + 2 + 8, 1 + 2 + 8, 1, 1};
     for (int i = 0; i <= X_DRAIN; ++i) bar_init(x + 8 * i, counts[i]);
     misc[0] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -216,6 +216,14 @@ __device__ __forceinline__ void bwd_end(uint32_t tmem, int warp) {
 
 // ------------------------------------------------------------------------------------------------ dq
 // Also leaves -lse (base 2) and -delta of every row for the other kernel, [Hq][n] each.
+//
+// delta = rowsum(dO * O) is off by the rounding of O to bf16.  Where a row sees many tokens that is little beside the products it
+// is taken from; where it sees few, O has the size of V and dQ comes out at up to 2.5 times the error of its other roundings.  So delta
+// is corrected by what is left of sum_j p_ij (dP_ij - delta), which is zero for the right delta: items of few tiles (DQ_FIRST) go over
+// their tiles twice, the first time for that sum alone; the others form it beside dS, and the other kernel gets the corrected delta.
+// (Error of dQ in the 2-norm, sequences of 8192 tokens / rollouts under a window of 1024: 2.6e-3 without, 2.5e-3 with up to 4 tiles, 2.4e-3
+// with up to 8, both passes of the rollouts 1.77, 1.82 and 2.00 ms.)
+constexpr int DQ_FIRST = 6;
 template <int D>
 __global__ void __launch_bounds__(ST_THREADS, 1)
 k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -247,7 +255,8 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           const int i0 = tile * TM;
           const SeqRange r = seq_keys(s, i0, min(i0 + TM, s.len) - 1, SN);
           w[B_START] = s.start; w[B_LEN] = s.len; w[B_PIN] = s.pin; w[B_CAP] = s.cap; w[B_E] = s.e; w[B_HEAD] = at - number * a.Hq;
-          w[B_TILE] = tile; w[B_A] = r.np; w[B_B] = r.s0; w[B_C] = r.s1; w[B_N] = seq_count(r);
+          w[B_TILE] = tile; w[B_A] = r.np; w[B_B] = r.s0; w[B_C] = r.s1; const int n = seq_count(r);
+          w[B_N] = n <= DQ_FIRST ? 2 * n : n;
           return true;
         },
         [&](const int* w, int t, uint32_t dst, uint32_t bar) {
@@ -257,7 +266,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           SeqRange r;
           if (which == 2) { load_tile<D>(dst, &tmO, w[B_HEAD], w[B_START] + w[B_TILE] * TM, bar); return; }
           r.np = w[B_A]; r.s0 = w[B_B]; r.s1 = w[B_C];
-          load_tile<D>(dst, which ? &tmV : &tmK, w[B_HEAD] / a.g, w[B_START] + seq_at(r, t) * SN, bar);
+          load_tile<D>(dst, which ? &tmV : &tmK, w[B_HEAD] / a.g, w[B_START] + seq_at(r, t < seq_count(r) ? t : t - seq_count(r)) * SN, bar);
         });
   } else if (warp == 1) {
     // ================================================================ MMA issuer
@@ -270,6 +279,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (!wait(X + 8 * (X_ITEM_FULL + slot), (seq >> 1) & 1)) { okay = false; break; }
       volatile int* d = desc + slot * B_WORDS;
       const int kind = __shfl_sync(0xffffffffu, d[B_KIND], 0), n = __shfl_sync(0xffffffffu, d[B_N], 0);
+      const int pre = __shfl_sync(0xffffffffu, seq_count(range_of(d)) < d[B_N] ? d[B_N] / 2 : 0, 0);      // steps without dQ
       if (kind == 0) break;
       __syncwarp();
       if (leader) bar_arrive(X + 8 * (X_ITEM_EMPTY + slot));
@@ -303,10 +313,10 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         if (!wait(X + 8 * X_DS_READY, (nt + t) & 1)) { okay = false; break; }
         fence_after();
         if (t + 1 < n && !values(t + 1)) { okay = false; break; }
-        if (t == 0 && !wait(X + 8 * X_ACC_EMPTY, (seq & 1) ^ 1)) { okay = false; break; }
+        if (t == pre && !wait(X + 8 * X_ACC_EMPTY, (seq & 1) ^ 1)) { okay = false; break; }
         const uint32_t s = SM::stage_a(nt + t);
         if (leader) {
-          mma_sums<D>(tA, tS + ((nt + t) & 1) * SN, sb + s * TILE, t == 0);
+          if (t >= pre) mma_sums<D>(tA, tS + ((nt + t) & 1) * SN, sb + s * TILE, t == pre);
           commit(empty + 8 * s);
         }
         __syncwarp();
@@ -335,7 +345,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
       const SeqRange r = range_of(d);
-      const int n = d[B_N], i0 = d[B_TILE] * TM, low1 = s.low(i0 + TM - 1);
+      const int n = d[B_N], tiles = seq_count(r), i0 = d[B_TILE] * TM, low1 = s.low(i0 + TM - 1);
       if (me == 1) {
         // the O tile is the softmax warps' alone: when they have read it and dO, this warp frees both
         const uint32_t at = nt + seq, sg = SM::stage_b(at);
@@ -353,7 +363,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         const uint32_t at = me == 0 ? nt + t : nt + t + seq + 1, sg = me == 0 ? SM::stage_a(at) : SM::stage_b(at);
         if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(at) : SM::phase_b(at))) { okay = false; break; }
         if (me == 0) {
-          const int tile = seq_at(r, t);
+          const int tile = seq_at(r, t < tiles ? t : t - tiles);
           uint32_t* bad = s_bad + 4 * ((nt + t) & 1);    // read with the tile two before
           if (!wait(X + 8 * (X_STAT_EMPTY + ((nt + t) & 1)), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
           if (!seq_all(s, i0, low1, tile * SN, tile * SN + SN - 1)) {
@@ -379,6 +389,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
     const int half = (warp - 4) >> 2, quarter = warp & 3, lrow = 32 * quarter + lane;
     const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
     const float sl2 = a.scale * ST_LOG2E;
+    float* s_sums = reinterpret_cast<float*>(smem + SM::OFF_STAT);             // [item & 1][half][row]
     uint32_t seq = 0, nt = 0;
     bool fine = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -392,7 +403,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       if (d[B_KIND] == 0) break;
       const SeqView s = bwd_view(d);
       const SeqRange r = range_of(d);
-      const int n = d[B_N], i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row), low1 = s.low(i0 + TM - 1);
+      const int n = d[B_N], tiles = seq_count(r), pre = n - tiles, i0 = d[B_TILE] * TM, h = d[B_HEAD], row = i0 + lrow, low = s.low(row), low1 = s.low(i0 + TM - 1);
       const bool real = row < s.len;
       // delta from the O and dO tiles in shared memory: both threads of a row form it, so that no barrier stands between the warps.
       // (Read from memory, rows far apart, it cost 8000 cycles an item; so 1000.)
@@ -422,17 +433,32 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
       }
       __syncwarp();
       if (lane == 0) bar_arrive(X + 8 * X_O_READ);
-      const float ndelta = -sum;
-      if (real && half == 0) {
-        const long long at = (long long)h * a.n + s.start + row;
-        a.delta[at] = ndelta;
-        a.delta[(long long)a.Hq * a.n + at] = nlse;
-      }
-      const uint64_t scl2 = tt_two(sl2, sl2), nlse2 = tt_two(nlse, nlse), nd2 = tt_two(ndelta, ndelta);
+      float ndelta = -sum;
+      const bool alone = s.alone(row);
+      const uint64_t scl2 = tt_two(sl2, sl2), nlse2 = tt_two(nlse, nlse);
+      uint64_t nd2 = tt_two(ndelta, ndelta), rest = 0ull;
+      // adds both halves' rests to delta and leaves it for the other kernel
+      auto correct = [&]() {
+        float* sums = s_sums + (seq & 1) * 2 * TM;       // of the item before last, which everybody has read
+        float lo, hi;
+        tt_both(rest, lo, hi);
+        sums[half * TM + lrow] = lo + hi;
+        __syncwarp();
+        if (lane == 0) bar_arrive(X + 8 * X_SUMS);
+        wait(X + 8 * X_SUMS, seq & 1);
+        ndelta -= sums[lrow] + sums[TM + lrow];
+        nd2 = tt_two(ndelta, ndelta);
+        if (real && half == 0) {
+          const long long at = (long long)h * a.n + s.start + row;
+          a.delta[at] = ndelta;
+          a.delta[(long long)a.Hq * a.n + at] = nlse;
+        }
+      };
 #pragma unroll 1
       for (int t = 0; t < n; ++t, ++nt) {
         const uint32_t buf = nt & 1, ts = tS + buf * SN + 64 * half + lane_off, tp = tP + 64 * half + lane_off;
-        const int j0 = seq_at(r, t) * SN;
+        const int j0 = seq_at(r, t < tiles ? t : t - tiles) * SN;
+        if (pre > 0 && t == pre) correct();
         wait(X + 8 * (X_S_FULL + buf), (nt >> 1) & 1);
         fence_after();
         float p[64];
@@ -468,11 +494,14 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           for (int y = 0; y < 32; y += 2)
             tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), nd2), tt_two(p[c + y], p[c + y + 1])), x[y], x[y + 1]);
           if (!all) {
-            const uint32_t keep = st_run(0, row + 1, jh + c) & ~st_run(s.pin, low, jh + c);
+            const uint32_t keep = alone ? 0u : st_run(0, row + 1, jh + c) & ~st_run(s.pin, low, jh + c);
 #pragma unroll
             for (int y = 0; y < 32; ++y)
               if (!(keep & (1u << y))) x[y] = 0.f;
           }
+#pragma unroll
+          for (int y = 0; y < 32; y += 2) rest = tt_add2(rest, tt_two(x[y], x[y + 1]));
+          if (t < pre) continue;
           // dS in bf16, half a step of 2^-8: the product's operands are of one type
 #pragma unroll
           for (int y = 0; y < 32; y += 2) pk[y >> 1] = tt_pack(x[y], x[y + 1]);
@@ -483,6 +512,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
         __syncwarp();
         if (lane == 0) { bar_arrive(X + 8 * X_DS_READY); bar_arrive(X + 8 * (X_STAT_EMPTY + buf)); }
       }
+      if (pre == 0) correct();
       wait(X + 8 * X_ACC_FULL, seq & 1);
       fence_after();
       const bool wide = (reinterpret_cast<uintptr_t>(a.dq) & 31) == 0 && a.D % 16 == 0 && a.dqs % 16 == 0;
@@ -680,6 +710,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       const SeqView s = bwd_view(d);
       const int n = d[B_N], tile0 = d[B_TILE], tiles = d[B_A], j0 = tile0 * TM, col = j0 + lrow, last = s.last(col),
                 until = seq_seen_until(s, j0, j0 + TM - 1);
+      const bool alone = s.alone(col);
       int i0 = j0, left = tiles;
 #pragma unroll 1
       for (int t = 0; t < n; ++t, ++nt) {
@@ -740,7 +771,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             tt_both(st_mul2(tt_add2(tt_two(x[y + 2], x[y + 3]), tt_two(v.z, v.w)), tt_two(p[y + 2], p[y + 3])), x[y + 2], x[y + 3]);
           }
           if (!all) {
-            const uint32_t keep = st_run(lo, hi + 1, c);
+            const uint32_t keep = st_run(alone && i0 == j0 ? lo + 1 : lo, hi + 1, c);          // this token's own query is at lo
 #pragma unroll
             for (int y = 0; y < 32; ++y)
               if (!(keep & (1u << y))) x[c + y] = 0.f;
