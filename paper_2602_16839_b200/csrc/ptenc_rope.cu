@@ -8,6 +8,9 @@
 // or all their key heads at a step; their angles, in 64 bits, are worked out once for all heads, one by each thread, while the next
 // step's values are on their way.  A head is a group of lanes
 // (a power of two) with two 16-byte vectors each, chosen so that both values of a pair are in the same lane.
+//
+// bf16: 32768 tokens of 28 + 4 heads of 128, rotation alone, 107 us, 5.0 TB/s; 16384 tokens of 32 + 8 with norms, forward and
+// backward, 179 us, 4.7 TB/s; 16 tokens of 16 + 2 heads 2.9 us.
 #include <string.h>
 
 #include "ptenc_tc.cuh"
@@ -223,158 +226,158 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
   // first the CTA's share of the queries' steps, then of the keys'
 #pragma unroll 1
   for (int side = 0; side < 2; ++side) {
-  const int H = side ? a.Hkv : a.Hq, tok = sh.tok[side], chunks = sh.chunks[side];
-  const unsigned inv_h = sh.inv[side];
-  const long long steps = (a.n + tok - 1) / tok * chunks;
-  const int cta = (int)blockIdx.x - sh.first[side], ctas = sh.ctas[side];
-  if (cta < 0 || cta >= ctas) continue;
-  const T* w = static_cast<const T*>(a.w[side]);
-  const bool norm = w != nullptr, need_x = !BWD || norm;
-  const T* X = static_cast<const T*>(a.x[side]);
-  const T* G = static_cast<const T*>(a.g[side]);
-  T* Y = static_cast<T*>(a.y[side]);
-  const long long xs = a.xs[side], gs = a.gs[side], ys = a.ys[side];
-  // this thread's angle of a step: pair my_p of the step's token my_t, in turns; where it goes: four pairs of a lane next to each
-  // other, the lanes behind one another, for 16-byte reads without bank conflicts
-  const int my_t = half > 0 ? tid / half : tok, my_p = half > 0 ? tid - my_t * half : 0;
-  const int my_at = my_t * 2 * np + (my_p / N) * 4 + (my_p & 3) + (N == 8 ? ((my_p >> 2) & 1) * (np / 2) : 0);
-  uint64_t dw[N], w2[N];
+    const int H = side ? a.Hkv : a.Hq, tok = sh.tok[side], chunks = sh.chunks[side];
+    const unsigned inv_h = sh.inv[side];
+    const long long steps = (a.n + tok - 1) / tok * chunks;
+    const int cta = (int)blockIdx.x - sh.first[side], ctas = sh.ctas[side];
+    if (cta < 0 || cta >= ctas) continue;
+    const T* w = static_cast<const T*>(a.w[side]);
+    const bool norm = w != nullptr, need_x = !BWD || norm;
+    const T* X = static_cast<const T*>(a.x[side]);
+    const T* G = static_cast<const T*>(a.g[side]);
+    T* Y = static_cast<T*>(a.y[side]);
+    const long long xs = a.xs[side], gs = a.gs[side], ys = a.ys[side];
+    // this thread's angle of a step: pair my_p of the step's token my_t, in turns; where it goes: four pairs of a lane next to each
+    // other, the lanes behind one another, for 16-byte reads without bank conflicts
+    const int my_t = half > 0 ? tid / half : tok, my_p = half > 0 ? tid - my_t * half : 0;
+    const int my_at = my_t * 2 * np + (my_p / N) * 4 + (my_p & 3) + (N == 8 ? ((my_p >> 2) & 1) * (np / 2) : 0);
+    uint64_t dw[N], w2[N];
 #pragma unroll
-  for (int y = 0; y < N; ++y) dw[y] = w2[y] = 0ull;
-  uint4 x[2], g[2];
-  int my_pos = 0;
-  // asks for the values and the position of step s
-  auto fetch = [&](long long s) {
-    const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
-    const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
-    const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
-    const bool on = it < items;
-    if (my_t < toks) my_pos = a.pos[t0 + my_t];
-    x[0] = x[1] = g[0] = g[1] = zero;
-    if (need_x && on) {
-      const uint4* from = reinterpret_cast<const uint4*>(X + (t0 + t) * xs + (long long)h * D);
-      if (ha) x[0] = from[va];
-      if (hb) x[1] = from[vb];
-    }
-    if (BWD && on) {
-      const uint4* from = reinterpret_cast<const uint4*>(G + (t0 + t) * gs + (long long)h * D);
-      if (ha) g[0] = from[va];
-      if (hb) g[1] = from[vb];
-    }
-  };
-  if (cta < steps) fetch(cta);
-  const double my_freq = my_t < tok ? (double)a.freq[my_p] * 0.15915494309189533577 : 0.0;
-  if (norm) {
-    rp_unpack(ha ? reinterpret_cast<const uint4*>(w)[va] : zero, w2, 0, T());
-    rp_unpack(hb ? reinterpret_cast<const uint4*>(w)[vb] : zero, w2, N / 2, T());
-  }
-  for (long long s = cta; s < steps; s += ctas, turn ^= 1) {
-    const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
-    const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
-    const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
-    const bool on = it < items;
-    float* trig = s_trig + turn * RP_TOK * 2 * np;         // the other copy may still be read
-    if (my_t < toks) {
-      float sn, cs;
-      rp_angle(my_pos, my_freq, &sn, &cs, sizeof(T) == 2);
-      trig[my_at] = cs;
-      trig[my_at + np] = BWD ? -sn : sn;
-    }
-    __syncthreads();
-    const uint4 x0 = x[0], x1 = x[1], g0 = g[0], g1 = g[1];
-    if (s + ctas < steps) fetch(s + ctas);
-    uint64_t v[N], o[N];
-    float inv = 1.f;
-    if (need_x) {
-      rp_unpack(x0, v, 0, T());
-      rp_unpack(x1, v, N / 2, T());
-      if (norm) {
-        uint64_t sq = 0ull;
-#pragma unroll
-        for (int y = 0; y < N; ++y) sq = tt_fma2(v[y], v[y], sq);
-        float lo, hi;
-        tt_both(sq, lo, hi);
-        inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
-        const uint64_t inv2 = tt_two(inv, inv);
-#pragma unroll
-        for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
+    for (int y = 0; y < N; ++y) dw[y] = w2[y] = 0ull;
+    uint4 x[2], g[2];
+    int my_pos = 0;
+    // asks for the values and the position of step s
+    auto fetch = [&](long long s) {
+      const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
+      const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
+      const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
+      const bool on = it < items;
+      if (my_t < toks) my_pos = a.pos[t0 + my_t];
+      x[0] = x[1] = g[0] = g[1] = zero;
+      if (need_x && on) {
+        const uint4* from = reinterpret_cast<const uint4*>(X + (t0 + t) * xs + (long long)h * D);
+        if (ha) x[0] = from[va];
+        if (hb) x[1] = from[vb];
       }
+      if (BWD && on) {
+        const uint4* from = reinterpret_cast<const uint4*>(G + (t0 + t) * gs + (long long)h * D);
+        if (ha) g[0] = from[va];
+        if (hb) g[1] = from[vb];
+      }
+    };
+    if (cta < steps) fetch(cta);
+    const double my_freq = my_t < tok ? (double)a.freq[my_p] * 0.15915494309189533577 : 0.0;
+    if (norm) {
+      rp_unpack(ha ? reinterpret_cast<const uint4*>(w)[va] : zero, w2, 0, T());
+      rp_unpack(hb ? reinterpret_cast<const uint4*>(w)[vb] : zero, w2, N / 2, T());
     }
-    if (BWD) {
-      rp_unpack(g0, o, 0, T());
-      rp_unpack(g1, o, N / 2, T());
-    } else {
+    for (long long s = cta; s < steps; s += ctas, turn ^= 1) {
+      const long long tg = chunks == 1 ? s : s / chunks, t0 = tg * tok;
+      const int toks = (int)(a.n - t0 < tok ? a.n - t0 : tok), items = toks * H;
+      const int it = (int)(s - tg * chunks) * groups + grp, t = H == 1 ? it : (int)__umulhi((unsigned)it, inv_h), h = it - t * H;
+      const bool on = it < items;
+      float* trig = s_trig + turn * RP_TOK * 2 * np;         // the other copy may still be read
+      if (my_t < toks) {
+        float sn, cs;
+        rp_angle(my_pos, my_freq, &sn, &cs, sizeof(T) == 2);
+        trig[my_at] = cs;
+        trig[my_at + np] = BWD ? -sn : sn;
+      }
+      __syncthreads();
+      const uint4 x0 = x[0], x1 = x[1], g0 = g[0], g1 = g[1];
+      if (s + ctas < steps) fetch(s + ctas);
+      uint64_t v[N], o[N];
+      float inv = 1.f;
+      if (need_x) {
+        rp_unpack(x0, v, 0, T());
+        rp_unpack(x1, v, N / 2, T());
+        if (norm) {
+          uint64_t sq = 0ull;
 #pragma unroll
-      for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
-    }
-    if (turns && on) {
-      const float* at = trig + t * 2 * np + l * 4;
+          for (int y = 0; y < N; ++y) sq = tt_fma2(v[y], v[y], sq);
+          float lo, hi;
+          tt_both(sq, lo, hi);
+          inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
+          const uint64_t inv2 = tt_two(inv, inv);
 #pragma unroll
-      for (int q = 0; q < N; q += 4) {
-        const float4 c4 = *reinterpret_cast<const float4*>(at + q / 4 * (np / 2));
-        const float4 s4 = *reinterpret_cast<const float4*>(at + np + q / 4 * (np / 2));
-        if (INTER) {
-          const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+          for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
+        }
+      }
+      if (BWD) {
+        rp_unpack(g0, o, 0, T());
+        rp_unpack(g1, o, N / 2, T());
+      } else {
 #pragma unroll
-          for (int y = q; y < q + 4; ++y) {
-            if (N * l + y >= half) continue;
-            float p, r;
-            tt_both(o[y], p, r);
-            o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
-          }
-        } else {
+        for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
+      }
+      if (turns && on) {
+        const float* at = trig + t * 2 * np + l * 4;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int i = q / 2 + k, j = i + N / 2;
-            const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
-            const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
-            const uint64_t p = o[i], r = o[j];
-            o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
-            o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
+        for (int q = 0; q < N; q += 4) {
+          const float4 c4 = *reinterpret_cast<const float4*>(at + q / 4 * (np / 2));
+          const float4 s4 = *reinterpret_cast<const float4*>(at + np + q / 4 * (np / 2));
+          if (INTER) {
+            const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+            for (int y = q; y < q + 4; ++y) {
+              if (N * l + y >= half) continue;
+              float p, r;
+              tt_both(o[y], p, r);
+              o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int i = q / 2 + k, j = i + N / 2;
+              const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
+              const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
+              const uint64_t p = o[i], r = o[j];
+              o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
+              o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
+            }
           }
         }
       }
-    }
-    if (BWD && norm) {
-      uint64_t dot2 = 0ull;
+      if (BWD && norm) {
+        uint64_t dot2 = 0ull;
 #pragma unroll
-      for (int y = 0; y < N; ++y) {
-        dw[y] = tt_fma2(o[y], v[y], dw[y]);
-        o[y] = rp_mul2(o[y], w2[y]);
-        dot2 = tt_fma2(o[y], v[y], dot2);
+        for (int y = 0; y < N; ++y) {
+          dw[y] = tt_fma2(o[y], v[y], dw[y]);
+          o[y] = rp_mul2(o[y], w2[y]);
+          dot2 = tt_fma2(o[y], v[y], dot2);
+        }
+        float lo, hi;
+        tt_both(dot2, lo, hi);
+        const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
+        const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
+#pragma unroll
+        for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
       }
-      float lo, hi;
-      tt_both(dot2, lo, hi);
-      const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
-      const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
+      if (on) {
+        uint4* to = reinterpret_cast<uint4*>(Y + (t0 + t) * ys + (long long)h * D);
+        if (ha) to[va] = rp_pack(o, 0, T());
+        if (hb) to[vb] = rp_pack(o, N / 2, T());
+      }
+    }
+    if (BWD && a.part != nullptr) {
+      // groups of a warp, then the warps, in a fixed order
 #pragma unroll
-      for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
+      for (int y = 0; y < 2 * N; ++y) {
+        float lo, hi;
+        tt_both(dw[y >> 1], lo, hi);
+        float v = (y & 1) ? hi : lo;
+        for (int o = 16; o >= sh.lanes; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        const int at = (y < N ? va : vb) * N + (y & (N - 1));
+        if ((tid & 31) < sh.lanes && (y < N ? ha : hb)) s_sum[tid >> 5][at] = v;
+      }
+      __syncthreads();
+      for (int d = tid; d < D; d += RP_THREADS) {
+        float sum = 0.f;
+        for (int k = 0; k < RP_THREADS / 32; ++k) sum += s_sum[k][d];
+        a.part[((size_t)side * RP_BLOCKS + cta) * D + d] = sum;
+      }
+      __syncthreads();
     }
-    if (on) {
-      uint4* to = reinterpret_cast<uint4*>(Y + (t0 + t) * ys + (long long)h * D);
-      if (ha) to[va] = rp_pack(o, 0, T());
-      if (hb) to[vb] = rp_pack(o, N / 2, T());
-    }
-  }
-  if (BWD && a.part != nullptr) {
-    // groups of a warp, then the warps, in a fixed order
-#pragma unroll
-    for (int y = 0; y < 2 * N; ++y) {
-      float lo, hi;
-      tt_both(dw[y >> 1], lo, hi);
-      float v = (y & 1) ? hi : lo;
-      for (int o = 16; o >= sh.lanes; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      const int at = (y < N ? va : vb) * N + (y & (N - 1));
-      if ((tid & 31) < sh.lanes && (y < N ? ha : hb)) s_sum[tid >> 5][at] = v;
-    }
-    __syncthreads();
-    for (int d = tid; d < D; d += RP_THREADS) {
-      float sum = 0.f;
-      for (int k = 0; k < RP_THREADS / 32; ++k) sum += s_sum[k][d];
-      a.part[((size_t)side * RP_BLOCKS + cta) * D + d] = sum;
-    }
-    __syncthreads();
-  }
   }
 }
 
