@@ -6,9 +6,13 @@
 // A CTA has a tile of M rows (64, or 32 where a head is wider than 128) and goes through the tiles of the other side, all in
 // fp32 from shared memory, an (M / 16) x (M / 16) block of scores and (M / 16) x (D / 16) of sums per thread.  The backward pass is
 // two kernels, one per side, each recomputing the scores: seven products instead of five, but no sums in an order that changes, so
-// that results have the same bits every time.  The tiles of the other side are copied a tile ahead where shared memory has room for
-// two.  Gradients of keys and values: where there are few tiles the heads of a group are dealt to a cluster of CTAs, which add their
-// sums in order through distributed shared memory.
+// results have the same bits every time.  The tiles of the other side are copied a tile ahead where shared memory has room for
+// two.  Where there are few tiles of rows, the tiles of the other side (for keys and values: of all heads of the group) are dealt to a
+// cluster of CTAs, which join their sums in order through distributed shared memory.
+//
+// Bound by what a tile takes one CTA alone, 7 us where its multiply-adds are 2 (eight warps do not hide the latencies of shared memory
+// and of the row sums), times the longest sequence's tiles: nine fp32 sequences of 3001 tokens in all, 4 + 1 heads of 64, forward 85 us,
+// dq 111, dk and dv 150.
 #include <cooperative_groups.h>
 
 #include "ptenc_seq.cuh"
@@ -18,7 +22,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int SG_THREADS = 256;
+constexpr int SG_THREADS = 256, SG_MAX_CLUSTER = 8;
 // In a tile that some rows see in part, what a row does not see is marked by this NaN, which arithmetic does not produce, and
 // left out of the sums: a product by zero would carry the infinities and NaN of unseen tokens along.
 constexpr unsigned SG_UNSEEN = 0xFFFFDEADu;
@@ -58,7 +62,8 @@ __device__ __forceinline__ void sg_load(float* to, const T* base, long long stri
       const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
       for (int y = 0; y < N; y += 4)
-        *reinterpret_cast<float4*>(at + y) = make_float4(ptenc_to_float(e[y]), ptenc_to_float(e[y + 1]), ptenc_to_float(e[y + 2]), ptenc_to_float(e[y + 3]));
+        *reinterpret_cast<float4*>(at + y) =
+            make_float4(ptenc_to_float(e[y]), ptenc_to_float(e[y + 1]), ptenc_to_float(e[y + 2]), ptenc_to_float(e[y + 3]));
     }
   }
 }
@@ -172,6 +177,34 @@ __device__ __forceinline__ float sg_row_sum(float v) {           // over the 16 
   return v;
 }
 
+// A CTA's sums to its shared memory, for the cluster.
+template <int DP>
+__device__ __forceinline__ void sg_leave(float* to, const float (&acc)[SgShape<DP>::R][DP / 16], int tx, int ty) {
+  using S = SgShape<DP>;
+#pragma unroll
+  for (int i = 0; i < S::R; ++i)
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c)
+      *reinterpret_cast<float4*>(to + (ty + 16 * i) * S::LD + 4 * tx + 64 * c) =
+          make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]);
+}
+// Four values of a row, summed over the cluster's CTAs in order, each times its factor f[q].
+__device__ __forceinline__ float4 sg_joined(cg::cluster_group& cluster, float* mine, int cs, const float* f) {
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int q = 0; q < SG_MAX_CLUSTER; ++q) {
+    if (q >= cs) break;
+    const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine, q));
+    sum.x = fmaf(v.x, f[q], sum.x); sum.y = fmaf(v.y, f[q], sum.y); sum.z = fmaf(v.z, f[q], sum.z); sum.w = fmaf(v.w, f[q], sum.w);
+  }
+  return sum;
+}
+template <typename T>
+__device__ __forceinline__ void sg_put(T* to, const float4& v, float f) {
+  to[0] = ptenc_from_float<T>(v.x * f); to[1] = ptenc_from_float<T>(v.y * f);
+  to[2] = ptenc_from_float<T>(v.z * f); to[3] = ptenc_from_float<T>(v.w * f);
+}
+
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <typename T, int DP>
@@ -182,12 +215,14 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
   float* sQ = sm;
   float* sKV = sQ + S::TILE;                             // [buffer][K, V]
   float* sP = sKV + 2 * S::BF * S::TILE;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int h = blockIdx.y, hk = h / a.g, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x), S::M, &s, &tile)) return;   // late tiles, which see most, first
+  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x) / cs, S::M, &s, &tile)) return;     // late tiles, which see most, first; a cluster agrees
   const int i0 = tile * S::M, i1 = min(i0 + S::M, s.len) - 1;
   const T* q = static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D;
   const T* k = static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D;
@@ -205,19 +240,20 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
   const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
-  auto fetch = [&](int t) {
+  auto fetch = [&](int t, int buf) {
     const int j0 = seq_at(r, t) * S::M;
-    float* to = sKV + (S::BF == 2 ? (t & 1) * 2 * S::TILE : 0);
+    float* to = sKV + (S::BF == 2 ? buf * 2 * S::TILE : 0);
     sg_load<T, DP>(to, k, a.ks, j0, s.len, D);
     sg_load<T, DP>(to + S::TILE, v, a.vs, j0, s.len, D);
   };
-  fetch(0);
-  for (int t = 0; t < nt; ++t) {
+  int buf = 0;
+  if (rank < nt) fetch(rank, 0);
+  for (int t = rank; t < nt; t += cs, buf ^= 1) {
     const int j0 = seq_at(r, t) * S::M;
-    if (S::BF == 1 && t > 0) { __syncthreads(); fetch(t); }
+    if (S::BF == 1 && t > rank) { __syncthreads(); fetch(t, 0); }
     sg_arrived();                                        // also: the other buffer's tile and P are not needed any more
-    if (S::BF == 2 && t + 1 < nt) fetch(t + 1);
-    const float* sK = sKV + (S::BF == 2 ? (t & 1) * 2 * S::TILE : 0);
+    if (S::BF == 2 && t + cs < nt) fetch(t + cs, buf ^ 1);
+    const float* sK = sKV + (S::BF == 2 ? buf * 2 * S::TILE : 0);
     const float* sV = sK + S::TILE;
     const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R];
@@ -253,6 +289,43 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
     __syncthreads();
     sg_add<DP>(o, sP, sV, tx, ty, all);
   }
+  if (cs > 1) {
+    // sums over Q, and their rows' maxima and weights over P
+    sg_arrived();
+    sg_leave<DP>(sQ, o, tx, ty);
+    float2* sRow = reinterpret_cast<float2*>(sP);
+#pragma unroll
+    for (int i = 0; i < S::R; ++i)
+      if (tx == 0) sRow[ty + 16 * i] = make_float2(m[i], l[i]);
+    cluster.sync();
+    const int quads = D / 4;
+    const long long os = (long long)a.Hq * D;
+    for (int x = rank * SG_THREADS + threadIdx.x; x < S::M * quads; x += cs * SG_THREADS) {
+      const int row = x / quads, c = 4 * (x - row * quads);
+      if (i0 + row >= s.len) continue;
+      float f[SG_MAX_CLUSTER], w[SG_MAX_CLUSTER], mx = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int q = 0; q < SG_MAX_CLUSTER; ++q) {
+        if (q >= cs) break;
+        const float2 ml = *cluster.map_shared_rank(sRow + row, q);
+        f[q] = ml.x;
+        w[q] = ml.y;
+        mx = fmaxf(mx, ml.x);
+      }
+      const float ref = mx == -INFINITY ? 0.f : __fmul_rn(mx, c2);
+#pragma unroll
+      for (int q = 0; q < SG_MAX_CLUSTER; ++q) {
+        if (q >= cs) break;
+        f[q] = f[q] == -INFINITY ? 0.f : exp2f(__fmul_rn(f[q], c2) - ref);
+        sum = fmaf(w[q], f[q], sum);
+      }
+      const float4 v = sg_joined(cluster, sQ + row * S::LD + c, cs, f);
+      sg_put(static_cast<T*>(a.out) + (s.start + i0 + row) * os + (long long)h * D + c, v, 1.f / sum);
+      if (c == 0 && a.lse != nullptr) a.lse[(long long)(s.start + i0 + row) * a.Hq + h] = (__fmul_rn(mx, c2) + log2f(sum)) * LN2;
+    }
+    cluster.sync();                                      // nobody leaves while its sums may be read
+    return;
+  }
   float f[S::R];
 #pragma unroll
   for (int i = 0; i < S::R; ++i) {
@@ -275,12 +348,14 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   float* sG = sQ + S::TILE;
   float* sKV = sG + S::TILE;                             // [buffer][K, V]; first O
   float* sP = sKV + 2 * S::BQ * S::TILE;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int h = blockIdx.y, hk = h / a.g, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x), S::M, &s, &tile)) return;
+  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x) / cs, S::M, &s, &tile)) return;
   const int i0 = tile * S::M, i1 = min(i0 + S::M, s.len) - 1;
   const long long os = (long long)a.Hq * D, first = s.start * os + (long long)h * D;
   const T* k = static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D;
@@ -303,27 +378,28 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
     lse2[i] = 0.f;
     if (i0 + row < s.len) {
       lse2[i] = a.lse[at] * LOG2E;
-      if (tx == 0) a.delta[at] = delta[i];
+      if (tx == 0 && rank == 0) a.delta[at] = delta[i];
     }
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) acc[i][c] = 0.f;
   }
   const SeqRange r = seq_keys(s, i0, i1, S::M);
   const int nt = seq_count(r), low1 = s.low(i0 + S::M - 1);
-  auto fetch = [&](int t) {
+  auto fetch = [&](int t, int buf) {
     const int j0 = seq_at(r, t) * S::M;
-    float* to = sKV + (S::BQ == 2 ? (t & 1) * 2 * S::TILE : 0);
+    float* to = sKV + (S::BQ == 2 ? buf * 2 * S::TILE : 0);
     sg_load<T, DP>(to, k, a.ks, j0, s.len, D);
     sg_load<T, DP>(to + S::TILE, v, a.vs, j0, s.len, D);
   };
   __syncthreads();                                       // O has been read
-  fetch(0);
-  for (int t = 0; t < nt; ++t) {
+  int buf = 0;
+  if (rank < nt) fetch(rank, 0);
+  for (int t = rank; t < nt; t += cs, buf ^= 1) {
     const int j0 = seq_at(r, t) * S::M;
-    if (S::BQ == 1 && t > 0) { __syncthreads(); fetch(t); }
+    if (S::BQ == 1 && t > rank) { __syncthreads(); fetch(t, 0); }
     sg_arrived();
-    if (S::BQ == 2 && t + 1 < nt) fetch(t + 1);
-    const float* sK = sKV + (S::BQ == 2 ? (t & 1) * 2 * S::TILE : 0);
+    if (S::BQ == 2 && t + cs < nt) fetch(t + cs, buf ^ 1);
+    const float* sK = sKV + (S::BQ == 2 ? buf * 2 * S::TILE : 0);
     const float* sV = sK + S::TILE;
     const bool all = seq_all(s, i0, low1, j0, j0 + S::M - 1);
     float x[S::R][S::R], y[S::R][S::R];
@@ -345,13 +421,28 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
     __syncthreads();
     sg_add<DP>(acc, sP, sK, tx, ty, all);
   }
+  if (cs > 1) {
+    sg_arrived();
+    sg_leave<DP>(sQ, acc, tx, ty);
+    cluster.sync();
+    const float one[SG_MAX_CLUSTER] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    const int quads = D / 4;
+    for (int x = rank * SG_THREADS + threadIdx.x; x < S::M * quads; x += cs * SG_THREADS) {
+      const int row = x / quads, c = 4 * (x - row * quads);
+      if (i0 + row >= s.len) continue;
+      const float4 sum = sg_joined(cluster, sQ + row * S::LD + c, cs, one);
+      sg_put(static_cast<T*>(a.dq) + (s.start + i0 + row) * a.dqs + (long long)h * D + c, sum, a.scale);
+    }
+    cluster.sync();
+    return;
+  }
   float f[S::R];
 #pragma unroll
   for (int i = 0; i < S::R; ++i) f[i] = a.scale;
   sg_store<T, DP>(static_cast<T*>(a.dq) + s.start * a.dqs + (long long)h * D, a.dqs, acc, f, i0, s.len, D, tx, ty);
 }
 
-// dk and dv of a tile of tokens: the CTA's share of the group's heads, one after another.
+// dk and dv of a tile of tokens: tiles of queries of the group's heads, one head after another.
 template <typename T, int DP>
 __global__ void __launch_bounds__(SG_THREADS)
 k_seq_dkv(const __grid_constant__ SeqArgs a) {
@@ -366,7 +457,7 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int hk = blockIdx.y, D = a.D, heads = a.g / cs, h0 = hk * a.g + rank * heads;
+  const int hk = blockIdx.y, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
@@ -382,11 +473,11 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
   const int last = j0 < s.pin ? s.len - 1 : s.last(j1), until = seq_seen_until(s, j0, j0 + S::M - 1);
-  const int tiles = last / S::M - tile + 1, nt = tiles * heads;
-  auto fetch = [&](int t) {
-    const int hh = t / tiles, i0 = (tile + t - hh * tiles) * S::M, h = h0 + hh;
-    float* to = sQG + (S::BK == 2 ? (t & 1) * 2 * S::TILE : 0);
-    float* st = sStat + (S::BK == 2 ? (t & 1) * 2 * S::M : 0);
+  const int tiles = last / S::M - tile + 1, nt = tiles * a.g;
+  auto fetch = [&](int t, int buf) {
+    const int hh = t / tiles, i0 = (tile + t - hh * tiles) * S::M, h = hk * a.g + hh;
+    float* to = sQG + (S::BK == 2 ? buf * 2 * S::TILE : 0);
+    float* st = sStat + (S::BK == 2 ? buf * 2 * S::M : 0);
     sg_load<T, DP>(to, static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D, a.qs, i0, s.len, D);
     sg_load<T, DP>(to + S::TILE, static_cast<const T*>(a.dout) + s.start * os + (long long)h * D, os, i0, s.len, D);
     if (threadIdx.x < S::M) {
@@ -396,15 +487,16 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
       st[S::M + threadIdx.x] = row < s.len ? a.delta[at] : 0.f;
     }
   };
-  fetch(0);
-  for (int t = 0; t < nt; ++t) {
+  int buf = 0;
+  if (rank < nt) fetch(rank, 0);
+  for (int t = rank; t < nt; t += cs, buf ^= 1) {
     const int i0 = (tile + t % tiles) * S::M;
-    if (S::BK == 1 && t > 0) { __syncthreads(); fetch(t); }
+    if (S::BK == 1 && t > rank) { __syncthreads(); fetch(t, 0); }
     sg_arrived();
-    if (S::BK == 2 && t + 1 < nt) fetch(t + 1);
-    const float* sQ = sQG + (S::BK == 2 ? (t & 1) * 2 * S::TILE : 0);
+    if (S::BK == 2 && t + cs < nt) fetch(t + cs, buf ^ 1);
+    const float* sQ = sQG + (S::BK == 2 ? buf * 2 * S::TILE : 0);
     const float* sG = sQ + S::TILE;
-    const float* st = sStat + (S::BK == 2 ? (t & 1) * 2 * S::M : 0);
+    const float* st = sStat + (S::BK == 2 ? buf * 2 * S::M : 0);
     const bool all = i0 + S::M <= s.len && j0 + S::M - 1 <= i0 && i0 + S::M - 1 <= until;
     float x[S::R][S::R], y[S::R][S::R];
     sg_dot<DP>(x, sK, sQ, tx, ty, D);
@@ -429,32 +521,20 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
     sg_add<DP>(dk, sD, sQ, tx, ty, all);
   }
   if (cs > 1) {
-    // every CTA's sums to its shared memory, over K and V; each then adds a share of the rows of all, in order
-    __syncthreads();
+    // over K and V; each then adds a share of the rows of all, in order
+    sg_arrived();
     float* mine[2] = {sK, sV};
-#pragma unroll
-    for (int i = 0; i < S::R; ++i)
-#pragma unroll
-      for (int c = 0; c < DP / 64; ++c) {
-        const int at = (ty + 16 * i) * S::LD + 4 * tx + 64 * c;
-        *reinterpret_cast<float4*>(mine[0] + at) = make_float4(dk[i][4 * c], dk[i][4 * c + 1], dk[i][4 * c + 2], dk[i][4 * c + 3]);
-        *reinterpret_cast<float4*>(mine[1] + at) = make_float4(dv[i][4 * c], dv[i][4 * c + 1], dv[i][4 * c + 2], dv[i][4 * c + 3]);
-      }
+    sg_leave<DP>(sK, dk, tx, ty);
+    sg_leave<DP>(sV, dv, tx, ty);
     cluster.sync();
+    const float one[SG_MAX_CLUSTER] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     T* to[2] = {static_cast<T*>(a.dk) + s.start * a.dks + (long long)hk * D, static_cast<T*>(a.dv) + s.start * a.dvs + (long long)hk * D};
     const int quads = D / 4;
     for (int x = rank * SG_THREADS + threadIdx.x; x < 2 * S::M * quads; x += cs * SG_THREADS) {
       const int which = x / (S::M * quads), rem = x - which * S::M * quads, row = rem / quads, c = 4 * (rem - row * quads);
       if (j0 + row >= s.len) continue;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int q = 0; q < cs; ++q) {
-        const float4 v = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine[which] + row * S::LD + c, q));
-        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-      }
-      const float f = which == 0 ? a.scale : 1.f;
-      T* at = to[which] + (long long)(j0 + row) * (which == 0 ? a.dks : a.dvs) + c;
-      at[0] = ptenc_from_float<T>(sum.x * f); at[1] = ptenc_from_float<T>(sum.y * f);
-      at[2] = ptenc_from_float<T>(sum.z * f); at[3] = ptenc_from_float<T>(sum.w * f);
+      const float4 sum = sg_joined(cluster, mine[which] + row * S::LD + c, cs, one);
+      sg_put(to[which] + (long long)(j0 + row) * (which == 0 ? a.dks : a.dvs) + c, sum, which == 0 ? a.scale : 1.f);
     }
     cluster.sync();                                      // nobody leaves while its sums may be read
     return;
@@ -477,39 +557,47 @@ cudaError_t sg_attributes(int dev) {
   });
 }
 
-template <typename T, int DP>
-cudaError_t sg_fwd(const SeqArgs& a, int dev, cudaStream_t st) {
-  using S = SgShape<DP>;
-  const cudaError_t e = sg_attributes<T, DP>(dev);
-  if (e != cudaSuccess) return e;
-  return tree_launch(k_seq_fwd<T, DP>, dim3((unsigned)seq_numbers(a.n, a.B, S::M), a.Hq), SG_THREADS, S::fwd(S::BF) * 4, 0, st, a);
+// CTAs of a cluster: doubled until the SMs have two CTAs each for the tiles of `heads` heads, and never more than the tiles that a CTA
+// could have at most (`most`).  Nine fp32 sequences of 3001 tokens, 4 + 1 heads of 64, forward, dq and dkv: 113, 133 and 606 us without
+// clusters, 85, 111 and 150 so; until one CTA each 112, 133 and 178, four 78, 138 and 150, eight 107, 235 and 150.
+int sg_cluster(long long x, int heads, long long most, int sms) {
+  int cs = 1;
+  while (cs < SG_MAX_CLUSTER && x * heads * cs < 2ll * sms && 2 * cs <= most) cs *= 2;
+  return x * cs < (1ll << 31) ? cs : 1;
 }
 
 template <typename T, int DP>
-cudaError_t sg_bwd(const SeqArgs& a, int dev, cudaStream_t st) {
+cudaError_t sg_fwd(const SeqArgs& a, int dev, int sms, cudaStream_t st) {
+  using S = SgShape<DP>;
+  const cudaError_t e = sg_attributes<T, DP>(dev);
+  if (e != cudaSuccess) return e;
+  const unsigned x = (unsigned)seq_numbers(a.n, a.B, S::M);
+  const int cs = sg_cluster(x, a.Hq, (a.n + S::M - 1) / S::M, sms);
+  return tree_launch(k_seq_fwd<T, DP>, dim3(x * cs, a.Hq), SG_THREADS, S::fwd(S::BF) * 4, cs, st, a);
+}
+
+template <typename T, int DP>
+cudaError_t sg_bwd(const SeqArgs& a, int dev, int sms, cudaStream_t st) {
   using S = SgShape<DP>;
   cudaError_t e = sg_attributes<T, DP>(dev);
   if (e != cudaSuccess) return e;
   const unsigned x = (unsigned)seq_numbers(a.n, a.B, S::M);
-  e = tree_launch(k_seq_dq<T, DP>, dim3(x, a.Hq), SG_THREADS, S::dq(S::BQ) * 4, 0, st, a);
+  const long long tiles = (a.n + S::M - 1) / S::M;
+  int cs = sg_cluster(x, a.Hq, tiles, sms);
+  e = tree_launch(k_seq_dq<T, DP>, dim3(x * cs, a.Hq), SG_THREADS, S::dq(S::BQ) * 4, cs, st, a);
   if (e != cudaSuccess) return e;
-  int sms = 0;
-  e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
-  // The heads of a group over a cluster of CTAs, as many as divide it (eight at most), until each SM has two: nine sequences of 3001
-  // tokens, four heads to a KV head: 730 us with one CTA per tile.
-  int cs = 1;
-  for (int d = 2; d <= 8 && (long long)x * a.Hkv * cs < 2ll * sms; ++d)
-    if (a.g % d == 0) cs = d;
-  if ((long long)x * cs >= (1ll << 31)) cs = 1;
+  cs = sg_cluster(x, a.Hkv, tiles * a.g, sms);
   return tree_launch(k_seq_dkv<T, DP>, dim3(x * cs, a.Hkv), SG_THREADS, S::dkv(S::BK) * 4, cs, st, a);
 }
 
 template <typename T>
 cudaError_t sg_any(const SeqArgs& a, bool back, int dev, cudaStream_t st) {
-  if (a.D <= 64) return back ? sg_bwd<T, 64>(a, dev, st) : sg_fwd<T, 64>(a, dev, st);
-  if (a.D <= 128) return back ? sg_bwd<T, 128>(a, dev, st) : sg_fwd<T, 128>(a, dev, st);
-  return back ? sg_bwd<T, 256>(a, dev, st) : sg_fwd<T, 256>(a, dev, st);
+  int sms = 0;
+  const cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  if (a.D <= 64) return back ? sg_bwd<T, 64>(a, dev, sms, st) : sg_fwd<T, 64>(a, dev, sms, st);
+  if (a.D <= 128) return back ? sg_bwd<T, 128>(a, dev, sms, st) : sg_fwd<T, 128>(a, dev, sms, st);
+  return back ? sg_bwd<T, 256>(a, dev, sms, st) : sg_fwd<T, 256>(a, dev, sms, st);
 }
 
 inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
