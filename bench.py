@@ -441,6 +441,56 @@ def draft_round(args, c: dict, cache, dev) -> dict:
             "how": "medians of 20 rounds, every call over all layers, CUDA events"}
 
 
+def update_pass(args, c: dict, dev) -> dict:
+    """One layer's operators of a training pass over `--update-pass` packed tokens of the workload's head shape, 8 rollouts under its
+    window (and `--prompt-len`, `--evict-chunk`), and the loss over `--update-vocab` logits of each of its tokens, 1024 at most.
+    Medians of 20 rounds, CUDA events; not part of `value`."""
+    import paper_2602_16839_b200 as pt
+
+    n, Hq, Hkv, D, W = args.update_pass, c["n_q_heads"], c["n_kv_heads"], c["head_dim"], c["window"]
+    V, rows, dt = args.update_vocab, min(args.update_pass, 1024), torch.float32 if c["dtype"] == "fp32" else torch.bfloat16
+    gen = torch.Generator(device=dev).manual_seed(0)
+    H = Hq + 2 * Hkv
+    qkv = torch.randn(n, H, D, generator=gen, device=dev).to(dt)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    dout = torch.randn(n, Hq, D, generator=gen, device=dev).to(dt)
+    B = min(8, n)
+    lens = [n // B + (b < n % B) for b in range(B)]
+    cu = torch.tensor([sum(lens[:b]) for b in range(B + 1)], dtype=torch.int32, device=dev)
+    pos = torch.cat([torch.arange(m, dtype=torch.int32, device=dev) for m in lens])
+    pin = torch.full((B,), min(args.prompt_len, W - 1), dtype=torch.int32, device=dev)
+    freq = (10000.0 ** (-torch.arange(0, D, 2, device=dev).double() / D)).float()
+    e = lambda *s, d=dt: torch.empty(*s, dtype=d, device=dev)        # noqa: E731
+    f32 = torch.float32
+    qr, kr, out, lse, dqkv = e(n, Hq, D), e(n, Hkv, D), e(n, Hq, D), e(n, Hq, d=f32), e(n, H, D)
+    dq, dk, dv = dqkv[:, :Hq], dqkv[:, Hq:Hq + Hkv], dqkv[:, Hq + Hkv:]
+    ws = e(pt.seq_attn_workspace_bytes(n, Hq), d=torch.uint8)
+    z = (2.5 * torch.randn(rows, V, generator=gen, device=dev)).to(dt)
+    tok = torch.randint(0, V, (rows,), generator=gen, device=dev, dtype=torch.int32)
+    adv, old, lp, tl, loss = torch.randn(rows, generator=gen, device=dev), e(rows, d=f32), e(rows, d=f32), e(rows, d=f32), e(1, d=f32)
+    dz = torch.empty_like(z)
+    pt.token_logp(z, tok, old)
+    kw = dict(n_pinned=pin, window=W, evict_chunk=min(args.evict_chunk, W))
+    parts = (("head_norm_rope", lambda: pt.head_norm_rope(q, k, pos, freq, qr, kr)),
+             ("seq_attn", lambda: pt.seq_attn(qr, kr, v, cu, out, lse_out=lse, **kw)),
+             ("seq_attn_backward", lambda: pt.seq_attn_backward(qr, kr, v, out, lse, dout, cu, dq, dk, dv, ws, **kw)),
+             ("head_norm_rope_backward", lambda: pt.head_norm_rope_backward(q, k, dq, dk, pos, freq, dq, dk)),
+             ("policy_loss", lambda: pt.policy_loss(z, tok, adv, lp, tl, loss, dz, old_logp=old)))
+    times = {name: [] for name, _ in parts}
+    for _ in range(23):
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(len(parts) + 1)]
+        ev[0].record()
+        for j, (_, call) in enumerate(parts):
+            call()
+            ev[j + 1].record()
+        torch.cuda.synchronize()
+        for j, (name, _) in enumerate(parts):
+            times[name].append(ev[j].elapsed_time(ev[j + 1]))
+    med = {name + "_ms": statistics.median(ts[3:]) for name, ts in times.items()}
+    return {"tokens": n, "sequences": B, "window": W, "loss_rows": rows, "vocab": V, **med,
+            "how": "medians of 20 rounds, one layer, CUDA events"}
+
+
 # ======================================================================================== GPU leg
 def run_gpu(args, c: dict):
     import paper_2602_16839_b200 as pt
@@ -600,6 +650,8 @@ def run_gpu(args, c: dict):
         del Am, Bw, xin, yio, flush
     if rank == 0 and args.draft_tree > 0:
         extras["draft_round"] = draft_round(args, c, cache, dev)
+    if rank == 0 and args.update_pass > 0:
+        extras["update_pass"] = update_pass(args, c, dev)
 
     # ---- max over ranks -------------------------------------------------------------------------------------
     ms_total, ms_e2e = max_over_ranks([ms_total, ms_e2e], dist, dev)
@@ -683,7 +735,13 @@ def main():
                     help="also time a round of speculative decoding with a tree of this many nodes per sequence (1..64; "
                          "sliding-window policy): attention of the tree, verification, commit of the accepted path")
     ap.add_argument("--draft-vocab", type=int, default=32768, help="--draft-tree: probabilities per node")
+    ap.add_argument("--update-pass", type=int, default=0,
+                    help="also time one layer's operators of a training pass over this many packed tokens: norms and rotation, "
+                         "attention under the workload's window and its gradients, the policy loss")
+    ap.add_argument("--update-vocab", type=int, default=152000, help="--update-pass: logits per token")
     args = ap.parse_args()
+    if args.update_pass < 0 or args.update_vocab < 1:
+        ap.error("--update-pass and --update-vocab are counts")
     if args.draft_tree and (not 1 <= args.draft_tree <= 64 or args.policy != "fifo"):
         ap.error("--draft-tree takes 1 to 64 nodes under the sliding-window policy")
     c = workload_cfg(args.workload)
