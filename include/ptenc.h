@@ -307,14 +307,21 @@ typedef struct {
  *   q, out [n, H_q, D]; k, v [n, H_kv, D]; out is contiguous; lse_out [n, H_q] fp32, nullable: the natural logarithm of the sum
  * of exp of the scaled scores, which the backward call wants.  What a token does not see does not reach its rows, whatever it holds
  * (NaN and infinities included).  Rows of no sequence are neither read for an answer nor written.  A sequence whose bounds or
- * n_pinned (0 <= n_pinned < W) are out of range is left alone.  No workspace. */
+ * n_pinned (0 <= n_pinned < W) are out of range is left alone.  (n_tokens / 32 + batch) * n_q_heads is below 2^31, batch at most 2^24
+ * (PTENC_ESHAPE).  No workspace.
+ *   bf16 with head_dim up to 128 runs on the tensor cores: the weights are rounded to bf16 in the product with V, everything else is
+ * fp32 but the results; outputs are off by 1.8e-3 of their size in the 2-norm, where rounding the result alone gives 1.7e-3.  Other
+ * shapes and fp32 are computed in fp32.  A kernel whose waits run out (broken memory) leaves NaN in the rows
+ * that it was at, and rows that it had not come to may keep what they held. */
 PTENC_API int ptenc_seq_attn(const ptenc_seq_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
                              int64_t k_stride, const void* v, int64_t v_stride, const int32_t* cu_seqlens,
                              const int32_t* n_pinned, int32_t batch, int64_t n_tokens, void* out, float* lse_out,
                              void* stream);
 
 /* Gradients of ptenc_seq_attn with respect to q, k and v, from dout [n, H_q, D] (contiguous, like out), the forward call's inputs,
- * out and lse.  The heads that share a KV head are summed in fp32, in a fixed order: repeated calls give the same bits.
+ * out and lse (those of exactly these keys: a token's weights sum to one).  The heads that share a KV head are summed in fp32, in a fixed
+ * order: repeated calls give the same bits.  On the tensor cores weights and score gradients are rounded to bf16 in the products they
+ * enter: gradients are off by 2.5e-3 of their size in the 2-norm.  A token that sees itself alone has score gradients of zero.
  * workspace: device, 16-byte aligned, ptenc_seq_attn_workspace_bytes; its contents do not outlive the call, and calls that share
  * one do not overlap on the GPU. */
 PTENC_API int ptenc_seq_attn_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, size_t* bytes /*host, out*/);

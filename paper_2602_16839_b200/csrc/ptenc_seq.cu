@@ -11,8 +11,8 @@
 // cluster of CTAs, which join their sums in order through distributed shared memory.
 //
 // Bound by what a tile takes one CTA alone, 7 us where its multiply-adds are 2 (eight warps do not hide the latencies of shared memory
-// and of the row sums), times the longest sequence's tiles: nine fp32 sequences of 3001 tokens in all, 4 + 1 heads of 64, forward 85 us,
-// dq 111, dk and dv 150.
+// and of the row sums), times the longest sequence's tiles: nine fp32 sequences of 3001 tokens in all, 4 + 1 heads of 64, forward 68 us,
+// dq 99, dk and dv 150.
 #include <cooperative_groups.h>
 
 #include "ptenc_seq.cuh"
@@ -218,11 +218,11 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int h = blockIdx.y, hk = h / a.g, D = a.D;
+  const int item = (int)(gridDim.x - 1 - blockIdx.x) / cs, h = item % a.Hq, hk = h / a.g, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x) / cs, S::M, &s, &tile)) return;     // late tiles, which see most, first; a cluster agrees
+  if (!seq_find(a, item / a.Hq, S::M, &s, &tile)) return;               // late tiles, which see most, first; a cluster agrees
   const int i0 = tile * S::M, i1 = min(i0 + S::M, s.len) - 1;
   const T* q = static_cast<const T*>(a.q) + s.start * a.qs + (long long)h * D;
   const T* k = static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D;
@@ -351,11 +351,11 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int h = blockIdx.y, hk = h / a.g, D = a.D;
+  const int item = (int)(gridDim.x - 1 - blockIdx.x) / cs, h = item % a.Hq, hk = h / a.g, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)(gridDim.x - 1 - blockIdx.x) / cs, S::M, &s, &tile)) return;
+  if (!seq_find(a, item / a.Hq, S::M, &s, &tile)) return;
   const int i0 = tile * S::M, i1 = min(i0 + S::M, s.len) - 1;
   const long long os = (long long)a.Hq * D, first = s.start * os + (long long)h * D;
   const T* k = static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D;
@@ -457,11 +457,11 @@ k_seq_dkv(const __grid_constant__ SeqArgs a) {
   cg::cluster_group cluster = cg::this_cluster();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int hk = blockIdx.y, D = a.D;
+  const int item = (int)blockIdx.x / cs, hk = item % a.Hkv, D = a.D;
   tree_after_previous();
   SeqView s;
   int tile;
-  if (!seq_find(a, (int)blockIdx.x / cs, S::M, &s, &tile)) return;      // early tiles are seen by most; a cluster agrees
+  if (!seq_find(a, item / a.Hkv, S::M, &s, &tile)) return;      // early tiles are seen by most; a cluster agrees
   const int j0 = tile * S::M, j1 = min(j0 + S::M, s.len) - 1;
   sg_load<T, DP>(sK, static_cast<const T*>(a.k) + s.start * a.ks + (long long)hk * D, a.ks, j0, s.len, D);
   sg_load<T, DP>(sV, static_cast<const T*>(a.v) + s.start * a.vs + (long long)hk * D, a.vs, j0, s.len, D);
@@ -557,13 +557,13 @@ cudaError_t sg_attributes(int dev) {
   });
 }
 
-// CTAs of a cluster: doubled until the SMs have two CTAs each for the tiles of `heads` heads, and never more than the tiles that a CTA
-// could have at most (`most`).  Nine fp32 sequences of 3001 tokens, 4 + 1 heads of 64, forward, dq and dkv: 113, 133 and 606 us without
-// clusters, 85, 111 and 150 so; until one CTA each 112, 133 and 178, four 78, 138 and 150, eight 107, 235 and 150.
-int sg_cluster(long long x, int heads, long long most, int sms) {
+// CTAs of a cluster: doubled until the SMs have two CTAs each for so many items, and never more than the tiles that an item could have
+// at most.  Nine fp32 sequences of 3001 tokens, 4 + 1 heads of 64, forward, dq and dkv: 108, 120 and 608 us without clusters, 68, 99 and
+// 150 so; until one CTA each 108, 120 and 178, four 73, 133 and 150, eight 107, 234 and 150.
+int sg_cluster(long long items, long long most, int sms) {
   int cs = 1;
-  while (cs < SG_MAX_CLUSTER && x * heads * cs < 2ll * sms && 2 * cs <= most) cs *= 2;
-  return x * cs < (1ll << 31) ? cs : 1;
+  while (cs < SG_MAX_CLUSTER && items * cs < 2ll * sms && 2 * cs <= most) cs *= 2;
+  return cs;
 }
 
 template <typename T, int DP>
@@ -571,9 +571,9 @@ cudaError_t sg_fwd(const SeqArgs& a, int dev, int sms, cudaStream_t st) {
   using S = SgShape<DP>;
   const cudaError_t e = sg_attributes<T, DP>(dev);
   if (e != cudaSuccess) return e;
-  const unsigned x = (unsigned)seq_numbers(a.n, a.B, S::M);
-  const int cs = sg_cluster(x, a.Hq, (a.n + S::M - 1) / S::M, sms);
-  return tree_launch(k_seq_fwd<T, DP>, dim3(x * cs, a.Hq), SG_THREADS, S::fwd(S::BF) * 4, cs, st, a);
+  const unsigned items = (unsigned)seq_numbers(a.n, a.B, S::M) * a.Hq;
+  const int cs = sg_cluster(items, (a.n + S::M - 1) / S::M, sms);
+  return tree_launch(k_seq_fwd<T, DP>, dim3(items * cs), SG_THREADS, S::fwd(S::BF) * 4, cs, st, a);
 }
 
 template <typename T, int DP>
@@ -581,13 +581,13 @@ cudaError_t sg_bwd(const SeqArgs& a, int dev, int sms, cudaStream_t st) {
   using S = SgShape<DP>;
   cudaError_t e = sg_attributes<T, DP>(dev);
   if (e != cudaSuccess) return e;
-  const unsigned x = (unsigned)seq_numbers(a.n, a.B, S::M);
+  const unsigned numbers = (unsigned)seq_numbers(a.n, a.B, S::M);
   const long long tiles = (a.n + S::M - 1) / S::M;
-  int cs = sg_cluster(x, a.Hq, tiles, sms);
-  e = tree_launch(k_seq_dq<T, DP>, dim3(x * cs, a.Hq), SG_THREADS, S::dq(S::BQ) * 4, cs, st, a);
+  int cs = sg_cluster((long long)numbers * a.Hq, tiles, sms);
+  e = tree_launch(k_seq_dq<T, DP>, dim3(numbers * a.Hq * cs), SG_THREADS, S::dq(S::BQ) * 4, cs, st, a);
   if (e != cudaSuccess) return e;
-  cs = sg_cluster(x, a.Hkv, tiles * a.g, sms);
-  return tree_launch(k_seq_dkv<T, DP>, dim3(x * cs, a.Hkv), SG_THREADS, S::dkv(S::BK) * 4, cs, st, a);
+  cs = sg_cluster((long long)numbers * a.Hkv, tiles * a.g, sms);
+  return tree_launch(k_seq_dkv<T, DP>, dim3(numbers * a.Hkv * cs), SG_THREADS, S::dkv(S::BK) * 4, cs, st, a);
 }
 
 template <typename T>
@@ -611,6 +611,7 @@ int check_config(const ptenc_seq_config* c, int32_t batch, int64_t n) {
   if (!(c->scale >= 0.f) || c->scale > 3e38f) return PTENC_EINVAL;
   if (c->head_dim % 8 != 0 || c->head_dim > 256 || c->n_q_heads > 16384 || c->n_q_heads % c->n_kv_heads != 0) return PTENC_ESHAPE;
   if (n >= (1ll << 31) - 512 || batch > (1 << 24)) return PTENC_ESHAPE;
+  if ((n / 32 + batch) * c->n_q_heads >= (1ll << 31)) return PTENC_ESHAPE;      // numbers of tiles and heads, of any of the kernels
   return PTENC_OK;
 }
 

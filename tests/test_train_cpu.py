@@ -168,6 +168,13 @@ def test_seq_attn_refuses(over, code, back):
     assert _seq(back, **over) == getattr(bd, "PTENC_" + code)
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_seq_attn_refuses_more_tiles_than_a_launch_has(back):
+    many = dict(Hq=128, Hkv=128, qs=8192, ks=8192, vs=8192, dqs=8192, dks=8192, dvs=8192, size=10240)
+    assert _seq(back, B=1 << 24, **many) == bd.PTENC_ESHAPE
+    assert _seq(back, B=(1 << 24) - 1, n=1 << 30, **many) == bd.PTENC_ESHAPE
+
+
 @pytest.mark.parametrize("over,code", [
     (dict(lse=None), "EINVAL"), (dict(g=None), "EINVAL"), (dict(dq=None), "EINVAL"), (dict(dk=None), "EINVAL"), (dict(dv=None), "EINVAL"),
     (dict(ws=None), "EINVAL"), (dict(size=319), "EWORKSPACE"), (dict(ws=P + 8), "EALIGN"), (dict(dq=P + 8), "EALIGN"), (dict(g=P + 2), "EALIGN"),
