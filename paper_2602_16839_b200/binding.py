@@ -7,6 +7,7 @@ is missing or fails to load, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -209,16 +210,36 @@ def verify_tree(p, q, tokens, parent, u, path, n_path, next_token, n_nodes=None,
 
 def _device_of(where, t) -> int:
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != (torch.cuda.current_device() if _current_device is None else _current_device()):
         raise PtencError(PTENC_EINVAL, f"{where}: the tensors' device is to be the current CUDA device")
     return dev
 
 
-def _rows(where, name, t, shape, dtype, device) -> int:
-    """Stride from token to token of a [n, heads, D] tensor whose rows are contiguous; refuses others."""
-    if t.dtype != dtype or t.device != device:
-        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a {dtype} tensor on {device}")
-    if tuple(t.shape) != tuple(shape):
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+# Calls of a few tokens are bound by the host: what follows asks each tensor as little as it can, the common answer first.
+@functools.lru_cache(maxsize=256)
+def _config(kind, *values):
+    """A configuration as the C side wants it, the same object for the same values."""
+    return ctypes.byref(kind(*values))
+
+
+def _is(t, dtype, shape, index) -> bool:
+    """A contiguous tensor of this type and shape on CUDA device `index`, or None."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous())
+
+
+def _rows(where, name, t, shape, like, dtype, index) -> int:
+    """Stride from token to token of a [n, heads, D] tensor whose rows are contiguous, of `like`'s type and device (`dtype` and
+    `index` again); refuses others."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index:
+        s0, s1, s2 = t.stride()
+        if s2 == 1 and s1 == shape[2] and shape[0] > 1:
+            return s0
+    if t.dtype != dtype or t.device != like.device:
+        raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a {dtype} tensor on {like.device}")
+    if t.shape != shape:
         raise PtencError(PTENC_ESHAPE, f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     n, h, d = shape
     s0, s1, s2 = t.stride()
@@ -236,15 +257,16 @@ def _storage(where, t, name):
 
 
 def _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved):
-    dt = _storage(where, q, "q")
-    n, Hq, D = q.shape
-    Hkv = k.shape[1] if k.dim() == 3 else 0
-    dev = q.device
-    sq, sk = _rows(where, "q", q, (n, Hq, D), q.dtype, dev), _rows(where, "k", k, (n, Hkv, D), q.dtype, dev)
+    code, dtype, index = _storage(where, q, "q"), q.dtype, q.get_device()
+    n, Hq, D = of_q = q.shape
+    of_k = (n, k.shape[1] if k.dim() == 3 else 0, D)
+    sq, sk = _rows(where, "q", q, of_q, q, dtype, index), _rows(where, "k", k, of_k, q, dtype, index)
     half = inv_freq.shape[0] if inv_freq.dim() == 1 else -1
-    _want(where, dev, ("positions", positions, (n,), torch.int32), ("inv_freq", inv_freq, (half,), torch.float32),
-          ("q_weight", q_weight, (D,), q.dtype), ("k_weight", k_weight, (D,), q.dtype))
-    return RopeConfig(dt, Hq, Hkv, D, 2 * half, 1 if interleaved else 0, eps), n, sq, sk
+    if not (_is(positions, torch.int32, (n,), index) and _is(inv_freq, torch.float32, (half,), index) and
+            _is(q_weight, dtype, (D,), index) and _is(k_weight, dtype, (D,), index)):
+        _want(where, q.device, ("positions", positions, (n,), torch.int32), ("inv_freq", inv_freq, (half,), torch.float32),
+              ("q_weight", q_weight, (D,), dtype), ("k_weight", k_weight, (D,), dtype))
+    return _config(RopeConfig, code, Hq, of_k[1], D, 2 * half, 1 if interleaved else 0, eps), n, sq, sk, of_q, of_k, dtype, index
 
 
 def head_norm_rope(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
@@ -252,10 +274,10 @@ def head_norm_rope(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_wei
     [n, Hq, D], k, k_out [n, Hkv, D] with contiguous rows and any token stride; positions [n] int32; inv_freq [rotary_dim / 2] fp32.
     q_out may be q and k_out k."""
     where = "ptenc_head_norm_rope"
-    cfg, n, sq, sk = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
-    so, sp = _rows(where, "q_out", q_out, q.shape, q.dtype, q.device), _rows(where, "k_out", k_out, k.shape, q.dtype, q.device)
+    cfg, n, sq, sk, of_q, of_k, dtype, index = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    so, sp = _rows(where, "q_out", q_out, of_q, q, dtype, index), _rows(where, "k_out", k_out, of_k, q, dtype, index)
     dev = _device_of(where, q)
-    rc = lib.ptenc_head_norm_rope(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
+    rc = lib.ptenc_head_norm_rope(cfg, q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
                                   positions.data_ptr(), inv_freq.data_ptr(), n, q_out.data_ptr(), so, k_out.data_ptr(), sp,
                                   _stream_of(dev))
     if rc != PTENC_OK:
@@ -281,14 +303,14 @@ def head_norm_rope_backward(q, k, dq_out, dk_out, positions, inv_freq, dq, dk, q
     """ptenc_head_norm_rope_backward: gradients dq, dk of the inputs and dq_weight, dk_weight [D] fp32 of the weights, from those of
     the outputs.  dq may be dq_out and dk dk_out.  workspace (with weights): head_norm_rope_workspace_bytes(D) bytes."""
     where = "ptenc_head_norm_rope_backward"
-    cfg, n, sq, sk = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
-    st = [_rows(where, name, t, like.shape, q.dtype, q.device) for name, t, like in
-          (("dq_out", dq_out, q), ("dk_out", dk_out, k), ("dq", dq, q), ("dk", dk, k))]
+    cfg, n, sq, sk, of_q, of_k, dtype, index = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
+    st = [_rows(where, name, t, shape, q, dtype, index) for name, t, shape in
+          (("dq_out", dq_out, of_q), ("dk_out", dk_out, of_k), ("dq", dq, of_q), ("dk", dk, of_k))]
     D = (q.shape[2],)
     _want(where, q.device, ("dq_weight", dq_weight, D, torch.float32), ("dk_weight", dk_weight, D, torch.float32))
     size = _workspace(where, workspace, q.device)
     dev = _device_of(where, q)
-    rc = lib.ptenc_head_norm_rope_backward(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
+    rc = lib.ptenc_head_norm_rope_backward(cfg, q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
                                            positions.data_ptr(), inv_freq.data_ptr(), n, dq_out.data_ptr(), st[0],
                                            dk_out.data_ptr(), st[1], dq.data_ptr(), st[2], dk.data_ptr(), st[3],
                                            _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace), size, _stream_of(dev))
@@ -297,13 +319,15 @@ def head_norm_rope_backward(q, k, dq_out, dk_out, positions, inv_freq, dq, dk, q
 
 
 def _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale):
-    dt = _storage(where, q, "q")
-    n, Hq, D = q.shape
-    Hkv = k.shape[1] if k.dim() == 3 else 0
-    st = [_rows(where, name, t, (n, h, D), q.dtype, q.device) for name, t, h in (("q", q, Hq), ("k", k, Hkv), ("v", v, Hkv))]
+    code, dtype, index = _storage(where, q, "q"), q.dtype, q.get_device()
+    n, Hq, D = of_q = q.shape
+    of_k = (n, k.shape[1] if k.dim() == 3 else 0, D)
+    st = (_rows(where, "q", q, of_q, q, dtype, index), _rows(where, "k", k, of_k, q, dtype, index), _rows(where, "v", v, of_k, q, dtype, index))
     batch = cu_seqlens.shape[0] - 1 if cu_seqlens.dim() == 1 else -1
-    _want(where, q.device, ("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32), ("n_pinned", n_pinned, (batch,), torch.int32))
-    return SeqConfig(dt, Hq, Hkv, D, window, evict_chunk, 0.0 if scale is None else scale), n, batch, st
+    if not (_is(cu_seqlens, torch.int32, (batch + 1,), index) and _is(n_pinned, torch.int32, (batch,), index)):
+        _want(where, q.device, ("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32), ("n_pinned", n_pinned, (batch,), torch.int32))
+    cfg = _config(SeqConfig, code, Hq, of_k[1], D, window, evict_chunk, 0.0 if scale is None else scale)
+    return cfg, n, batch, st, of_q, of_k, dtype, index
 
 
 def seq_attn(q, k, v, cu_seqlens, out, lse_out=None, n_pinned=None, window=0, evict_chunk=1, scale=None):
@@ -311,10 +335,11 @@ def seq_attn(q, k, v, cu_seqlens, out, lse_out=None, n_pinned=None, window=0, ev
     q [n, Hq, D], k, v [n, Hkv, D] with contiguous rows and any token stride; cu_seqlens [B + 1], n_pinned [B] int32; out
     [n, Hq, D], lse_out [n, Hq] fp32 contiguous."""
     where = "ptenc_seq_attn"
-    cfg, n, batch, (sq, sk, sv) = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
-    _want(where, q.device, ("out", out, q.shape, q.dtype), ("lse_out", lse_out, q.shape[:2], torch.float32))
+    cfg, n, batch, (sq, sk, sv), of_q, _, dtype, index = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
+    if not (_is(out, dtype, of_q, index) and _is(lse_out, torch.float32, of_q[:2], index)):
+        _want(where, q.device, ("out", out, of_q, dtype), ("lse_out", lse_out, of_q[:2], torch.float32))
     dev = _device_of(where, q)
-    rc = lib.ptenc_seq_attn(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, cu_seqlens.data_ptr(),
+    rc = lib.ptenc_seq_attn(cfg, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, cu_seqlens.data_ptr(),
                             _ptr(n_pinned), batch, n, out.data_ptr(), _ptr(lse_out), _stream_of(dev))
     if rc != PTENC_OK:
         raise PtencError(rc, where)
@@ -331,14 +356,13 @@ def seq_attn_backward(q, k, v, out, lse, dout, cu_seqlens, dq, dk, dv, workspace
     """ptenc_seq_attn_backward: dq, dk, dv (contiguous rows, any token stride) from dout and the forward call's inputs, out and
     lse.  workspace: seq_attn_workspace_bytes(n, Hq) bytes."""
     where = "ptenc_seq_attn_backward"
-    cfg, n, batch, (sq, sk, sv) = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
-    _want(where, q.device, ("out", out, q.shape, q.dtype), ("lse", lse, q.shape[:2], torch.float32),
-          ("dout", dout, q.shape, q.dtype))
-    gq, gk, gv = (_rows(where, name, t, like.shape, q.dtype, q.device) for name, t, like in
-                  (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    cfg, n, batch, (sq, sk, sv), of_q, of_k, dtype, index = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
+    _want(where, q.device, ("out", out, of_q, dtype), ("lse", lse, of_q[:2], torch.float32), ("dout", dout, of_q, dtype))
+    gq, gk, gv = (_rows(where, name, t, shape, q, dtype, index) for name, t, shape in
+                  (("dq", dq, of_q), ("dk", dk, of_k), ("dv", dv, of_k)))
     size = _workspace(where, workspace, q.device)
     dev = _device_of(where, q)
-    rc = lib.ptenc_seq_attn_backward(ctypes.byref(cfg), q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(),
+    rc = lib.ptenc_seq_attn_backward(cfg, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(),
                                      lse.data_ptr(), dout.data_ptr(), cu_seqlens.data_ptr(), _ptr(n_pinned), batch, n,
                                      dq.data_ptr(), gq, dk.data_ptr(), gk, dv.data_ptr(), gv, _ptr(workspace), size,
                                      _stream_of(dev))
@@ -347,13 +371,14 @@ def seq_attn_backward(q, k, v, out, lse, dout, cu_seqlens, dq, dk, dv, workspace
 
 
 def _logit_rows(where, name, t, shape, dtype, device) -> int:
-    if t.dtype != dtype or t.device != device:
+    if t.dtype is not dtype or t.device != device:
         raise PtencError(PTENC_EINVAL, f"{where}: {name} is to be a {dtype} tensor on {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise PtencError(PTENC_ESHAPE, f"{where}: {name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if shape[1] > 1 and shape[0] > 0 and t.stride(1) != 1:
+    s0, s1 = t.stride()
+    if shape[1] > 1 and shape[0] > 0 and s1 != 1:
         raise PtencError(PTENC_EINVAL, f"{where}: {name} is to have contiguous rows")
-    return t.stride(0) if shape[0] > 1 else max(1, shape[1])
+    return s0 if shape[0] > 1 else max(1, shape[1])
 
 
 def policy_loss(logits, tokens, advantage, logp, token_loss=None, loss=None, dlogits=None, old_logp=None, ref_logp=None,
@@ -364,16 +389,19 @@ def policy_loss(logits, tokens, advantage, logp, token_loss=None, loss=None, dlo
     where = "ptenc_policy_loss"
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
         raise PtencError(PTENC_EINVAL, f"{where}: logits is to be a [n, V] tensor of fp32 or bf16")
-    n, V = logits.shape
-    device, f32, row = logits.device, torch.float32, (n,)
-    s_in = _logit_rows(where, "logits", logits, (n, V), logits.dtype, device)
-    s_out = 0 if dlogits is None else _logit_rows(where, "dlogits", dlogits, (n, V), logits.dtype, device)
-    _want(where, device, ("tokens", tokens, row, torch.int32), ("advantage", advantage, row, f32), ("old_logp", old_logp, row, f32),
-          ("ref_logp", ref_logp, row, f32), ("weight", weight, row, f32), ("logp", logp, row, f32),
-          ("token_loss", token_loss, row, f32), ("token_kl", token_kl, row, f32), ("loss", loss, (1,), f32))
+    n, V = shape = logits.shape
+    dtype, device, index, f32, row = logits.dtype, logits.device, logits.get_device(), torch.float32, (n,)
+    s_in = _logit_rows(where, "logits", logits, shape, dtype, device)
+    s_out = 0 if dlogits is None else _logit_rows(where, "dlogits", dlogits, shape, dtype, device)
+    if not (_is(tokens, torch.int32, row, index) and _is(logp, f32, row, index) and _is(advantage, f32, row, index) and
+            _is(weight, f32, row, index) and _is(old_logp, f32, row, index) and _is(ref_logp, f32, row, index) and
+            _is(token_loss, f32, row, index) and _is(token_kl, f32, row, index) and _is(loss, f32, (1,), index)):
+        _want(where, device, ("tokens", tokens, row, torch.int32), ("advantage", advantage, row, f32), ("old_logp", old_logp, row, f32),
+              ("ref_logp", ref_logp, row, f32), ("weight", weight, row, f32), ("logp", logp, row, f32),
+              ("token_loss", token_loss, row, f32), ("token_kl", token_kl, row, f32), ("loss", loss, (1,), f32))
     dev = _device_of(where, logits)
-    cfg = PolicyConfig(DTYPE_BF16 if logits.dtype is torch.bfloat16 else DTYPE_FP32, V, temperature, clip_low, clip_high, kl_coef)
-    rc = lib.ptenc_policy_loss(ctypes.byref(cfg), logits.data_ptr(), s_in, tokens.data_ptr(), _ptr(old_logp), _ptr(ref_logp),
+    cfg = _config(PolicyConfig, DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_FP32, V, temperature, clip_low, clip_high, kl_coef)
+    rc = lib.ptenc_policy_loss(cfg, logits.data_ptr(), s_in, tokens.data_ptr(), _ptr(old_logp), _ptr(ref_logp),
                                _ptr(advantage), _ptr(weight), n, logp.data_ptr(), _ptr(token_loss), _ptr(token_kl), _ptr(loss),
                                _ptr(dlogits), s_out, _stream_of(dev))
     if rc != PTENC_OK:
