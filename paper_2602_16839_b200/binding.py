@@ -290,11 +290,11 @@ def head_norm_rope_workspace_bytes(head_dim) -> int:
     return int(n.value)
 
 
-def _workspace(where, ws, device):
+def _workspace(where, ws, like, index):
     if ws is None:
         return 0
-    if not ws.is_contiguous() or ws.device != device:
-        raise PtencError(PTENC_EINVAL, f"{where}: workspace is to be a contiguous tensor on {device}")
+    if not ws.is_contiguous() or ws.get_device() != index:
+        raise PtencError(PTENC_EINVAL, f"{where}: workspace is to be a contiguous tensor on {like.device}")
     return ws.numel() * ws.element_size()
 
 
@@ -304,15 +304,16 @@ def head_norm_rope_backward(q, k, dq_out, dk_out, positions, inv_freq, dq, dk, q
     the outputs.  dq may be dq_out and dk dk_out.  workspace (with weights): head_norm_rope_workspace_bytes(D) bytes."""
     where = "ptenc_head_norm_rope_backward"
     cfg, n, sq, sk, of_q, of_k, dtype, index = _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved)
-    st = [_rows(where, name, t, shape, q, dtype, index) for name, t, shape in
-          (("dq_out", dq_out, of_q), ("dk_out", dk_out, of_k), ("dq", dq, of_q), ("dk", dk, of_k))]
-    D = (q.shape[2],)
-    _want(where, q.device, ("dq_weight", dq_weight, D, torch.float32), ("dk_weight", dk_weight, D, torch.float32))
-    size = _workspace(where, workspace, q.device)
+    so, sp = _rows(where, "dq_out", dq_out, of_q, q, dtype, index), _rows(where, "dk_out", dk_out, of_k, q, dtype, index)
+    gq, gk = _rows(where, "dq", dq, of_q, q, dtype, index), _rows(where, "dk", dk, of_k, q, dtype, index)
+    D = of_q[2:]
+    if not (_is(dq_weight, torch.float32, D, index) and _is(dk_weight, torch.float32, D, index)):
+        _want(where, q.device, ("dq_weight", dq_weight, D, torch.float32), ("dk_weight", dk_weight, D, torch.float32))
+    size = _workspace(where, workspace, q, index)
     dev = _device_of(where, q)
     rc = lib.ptenc_head_norm_rope_backward(cfg, q.data_ptr(), sq, k.data_ptr(), sk, _ptr(q_weight), _ptr(k_weight),
-                                           positions.data_ptr(), inv_freq.data_ptr(), n, dq_out.data_ptr(), st[0],
-                                           dk_out.data_ptr(), st[1], dq.data_ptr(), st[2], dk.data_ptr(), st[3],
+                                           positions.data_ptr(), inv_freq.data_ptr(), n, dq_out.data_ptr(), so,
+                                           dk_out.data_ptr(), sp, dq.data_ptr(), gq, dk.data_ptr(), gk,
                                            _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace), size, _stream_of(dev))
     if rc != PTENC_OK:
         raise PtencError(rc, where)
@@ -357,10 +358,11 @@ def seq_attn_backward(q, k, v, out, lse, dout, cu_seqlens, dq, dk, dv, workspace
     lse.  workspace: seq_attn_workspace_bytes(n, Hq) bytes."""
     where = "ptenc_seq_attn_backward"
     cfg, n, batch, (sq, sk, sv), of_q, of_k, dtype, index = _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale)
-    _want(where, q.device, ("out", out, of_q, dtype), ("lse", lse, of_q[:2], torch.float32), ("dout", dout, of_q, dtype))
-    gq, gk, gv = (_rows(where, name, t, shape, q, dtype, index) for name, t, shape in
-                  (("dq", dq, of_q), ("dk", dk, of_k), ("dv", dv, of_k)))
-    size = _workspace(where, workspace, q.device)
+    if not (_is(out, dtype, of_q, index) and _is(lse, torch.float32, of_q[:2], index) and _is(dout, dtype, of_q, index)):
+        _want(where, q.device, ("out", out, of_q, dtype), ("lse", lse, of_q[:2], torch.float32), ("dout", dout, of_q, dtype))
+    gq, gk = _rows(where, "dq", dq, of_q, q, dtype, index), _rows(where, "dk", dk, of_k, q, dtype, index)
+    gv = _rows(where, "dv", dv, of_k, q, dtype, index)
+    size = _workspace(where, workspace, q, index)
     dev = _device_of(where, q)
     rc = lib.ptenc_seq_attn_backward(cfg, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(),
                                      lse.data_ptr(), dout.data_ptr(), cu_seqlens.data_ptr(), _ptr(n_pinned), batch, n,
