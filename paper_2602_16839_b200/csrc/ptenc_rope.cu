@@ -24,8 +24,8 @@ constexpr int RP_THREADS = 256;
 constexpr int RP_TOK = 8;                        // most tokens of a CTA at a time
 // CTAs per SM, forward and backward: what 64 and 128 registers per thread allow.  Each thread has the next step's row in flight, 32 or
 // 64 bytes.  32768 tokens of 28 + 4 heads, forward: 108 us so, 122 with three CTAs, 117 with five (spills), 115 with two rows in
-// flight; without a next step in flight, a CTA per step, 126.  Backward, 16384 tokens of 32 + 8 heads: 110 us; 163 with one CTA per
-// SM, 153 with three (spills).
+// flight; without a next step in flight, a CTA per step, 126; angles of eight steps at a time, one barrier for them, 135.  Backward,
+// 16384 tokens of 32 + 8 heads: 110 us; 163 with one CTA per SM, 153 with three (spills).
 constexpr int RP_CTAS_F = 4, RP_CTAS_B = 2;
 constexpr int RP_WARPS = 8;
 

@@ -12,7 +12,7 @@
 //    at the end.
 //  * warps 4..11: softmax, four warps per stream, a row per thread with its 128 scores in registers: mask, maximum, running sum in
 //    fp32 (base 2), P rounded to bf16.  O is rescaled only when the maximum has grown by more than 2^8.
-//  * Bound by the chain from a tile's scores to its P, two streams deep: the tensor pipe and the exponentials' unit are each busy 47 % of
+//  * Bound by the chain from a tile's scores to its P, two streams deep: the tensor pipe and the exponentials' unit are each busy half of
 //    the time.  16384 tokens, 28 + 4 heads of 128, causal: 1.52 ms, 1.27 PFLOP/s.
 //  * Every wait is bounded: one that runs out raises an abort flag, every role leaves, copies and products in flight are drained and
 //    tensor memory is freed; the item's rows become NaN, those of items that the CTA had not begun may be left as they were.
