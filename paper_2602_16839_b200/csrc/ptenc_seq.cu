@@ -12,7 +12,7 @@
 //
 // Bound by what a tile takes one CTA alone, 7 us where its multiply-adds are 2 (eight warps do not hide the latencies of shared memory
 // and of the row sums), times the longest sequence's tiles: nine fp32 sequences of 3001 tokens in all, 4 + 1 heads of 64, forward 68 us,
-// dq 99, dk and dv 150.
+// dq 90, dk and dv 140.
 #include <cooperative_groups.h>
 
 #include "ptenc_seq.cuh"
@@ -38,8 +38,11 @@ struct SgShape {
   static constexpr int fwd(int bufs) { return (1 + 2 * bufs) * TILE + M * LP; }
   static constexpr int dq(int bufs) { return (2 + 2 * bufs) * TILE + M * LP; }
   static constexpr int dkv(int bufs) { return (2 + 2 * bufs) * TILE + 2 * M * LP + bufs * 2 * M; }
-  static constexpr int room = 232448 / 4;
-  static constexpr int BF = fwd(2) <= room ? 2 : 1, BQ = dq(2) <= room ? 2 : 1, BK = dkv(2) <= room ? 2 : 1;
+  static constexpr int room = 232448 / 4, half = (233472 / 2 - 1024) / 4;
+  // One buffer where two CTAs share an SM then, two otherwise: eight fp32 sequences of 2048 tokens, 8 + 2 heads of 64, dq 1505 us so, 1735
+  // with two buffers, dk and dv 2664 and 2725.
+  static constexpr int bufs(int two, int one) { return two <= half ? 2 : one <= half ? 1 : two <= room ? 2 : 1; }
+  static constexpr int BF = bufs(fwd(2), fwd(1)), BQ = bufs(dq(2), dq(1)), BK = bufs(dkv(2), dkv(1));
   static_assert(fwd(BF) <= room && dq(BQ) <= room && dkv(BK) <= room, "shared memory of one CTA");
 };
 
@@ -207,8 +210,10 @@ __device__ __forceinline__ void sg_put(T* to, const float4& v, float f) {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
+// The last launch bound, here and below: how many CTAs of an SM the registers are to allow where the compiler's own choice (0) was the
+// slower one.  Five fp32 sequences of 8000 tokens, 12 + 4 heads of 128: forward 3395 us with 1, 3834 with 0.
 template <typename T, int DP>
-__global__ void __launch_bounds__(SG_THREADS)
+__global__ void __launch_bounds__(SG_THREADS, SgShape<DP>::fwd(SgShape<DP>::BF) <= SgShape<DP>::half ? 0 : 1)
 k_seq_fwd(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
@@ -340,7 +345,7 @@ k_seq_fwd(const __grid_constant__ SeqArgs a) {
 
 // dq of a tile of rows, and delta for the other kernel.
 template <typename T, int DP>
-__global__ void __launch_bounds__(SG_THREADS)
+__global__ void __launch_bounds__(SG_THREADS, SgShape<DP>::dq(SgShape<DP>::BQ) <= SgShape<DP>::half ? 2 : 1)
 k_seq_dq(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
@@ -444,7 +449,7 @@ k_seq_dq(const __grid_constant__ SeqArgs a) {
 
 // dk and dv of a tile of tokens: tiles of queries of the group's heads, one head after another.
 template <typename T, int DP>
-__global__ void __launch_bounds__(SG_THREADS)
+__global__ void __launch_bounds__(SG_THREADS, SgShape<DP>::dkv(SgShape<DP>::BK) <= SgShape<DP>::half ? 0 : 1)
 k_seq_dkv(const __grid_constant__ SeqArgs a) {
   using S = SgShape<DP>;
   extern __shared__ __align__(16) float sm[];
