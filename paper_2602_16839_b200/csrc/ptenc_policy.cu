@@ -193,14 +193,9 @@ __device__ __forceinline__ float pl_max(const uint4& w, __nv_bfloat16) {
 __device__ __forceinline__ float pl_max(const uint4& w, float) {
   return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
 }
-__device__ __forceinline__ uint64_t pl_mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // 2^((z - ref) c2) of two values.  The difference comes first: ref c2 would pass the range of fp32 in a row of the type's lowest values.
 __device__ __forceinline__ void pl_weights(uint64_t z, uint64_t neg_ref, uint64_t c2, float& lo, float& hi) {
-  tt_both(pl_mul2(tt_add2(z, neg_ref), c2), lo, hi);
+  tt_both(tt_mul2(tt_add2(z, neg_ref), c2), lo, hi);
   lo = tt_ex2(lo);
   hi = tt_ex2(hi);
 }

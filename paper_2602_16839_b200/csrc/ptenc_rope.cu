@@ -196,11 +196,6 @@ __device__ __forceinline__ uint4 rp_pack(const uint64_t (&f)[4], int at, float) 
   tt_both(f[at + 1], c, d);
   return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
 }
-__device__ __forceinline__ uint64_t rp_mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ float rp_group_sum(float v, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
@@ -300,7 +295,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
           inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
           const uint64_t inv2 = tt_two(inv, inv);
 #pragma unroll
-          for (int y = 0; y < N; ++y) v[y] = rp_mul2(v[y], inv2);
+          for (int y = 0; y < N; ++y) v[y] = tt_mul2(v[y], inv2);
         }
       }
       if (BWD) {
@@ -308,7 +303,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
         rp_unpack(g1, o, N / 2, T());
       } else {
 #pragma unroll
-        for (int y = 0; y < N; ++y) o[y] = norm ? rp_mul2(v[y], w2[y]) : v[y];
+        for (int y = 0; y < N; ++y) o[y] = norm ? tt_mul2(v[y], w2[y]) : v[y];
       }
       if (turns && on) {
         const float* at = trig + t * 2 * np + l * 4;
@@ -323,7 +318,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
               if (N * l + y >= half) continue;
               float p, r;
               tt_both(o[y], p, r);
-              o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), rp_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
+              o[y] = tt_fma2(o[y], tt_two(cs[y - q], cs[y - q]), tt_mul2(tt_two(r, p), tt_two(-sn[y - q], sn[y - q])));
             }
           } else {
 #pragma unroll
@@ -332,8 +327,8 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
               const uint64_t cs = k ? tt_two(c4.z, c4.w) : tt_two(c4.x, c4.y), sn = k ? tt_two(s4.z, s4.w) : tt_two(s4.x, s4.y);
               const uint64_t ns = k ? tt_two(-s4.z, -s4.w) : tt_two(-s4.x, -s4.y);
               const uint64_t p = o[i], r = o[j];
-              o[i] = tt_fma2(r, ns, rp_mul2(p, cs));
-              o[j] = tt_fma2(p, sn, rp_mul2(r, cs));
+              o[i] = tt_fma2(r, ns, tt_mul2(p, cs));
+              o[j] = tt_fma2(p, sn, tt_mul2(r, cs));
             }
           }
         }
@@ -343,7 +338,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
 #pragma unroll
         for (int y = 0; y < N; ++y) {
           dw[y] = tt_fma2(o[y], v[y], dw[y]);
-          o[y] = rp_mul2(o[y], w2[y]);
+          o[y] = tt_mul2(o[y], w2[y]);
           dot2 = tt_fma2(o[y], v[y], dot2);
         }
         float lo, hi;
@@ -351,7 +346,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
         const float dot = -rp_group_sum(lo + hi, sh.lanes) * rD * inv;
         const uint64_t d2 = tt_two(dot, dot), inv2 = tt_two(inv, inv);
 #pragma unroll
-        for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, rp_mul2(o[y], inv2));
+        for (int y = 0; y < N; ++y) o[y] = tt_fma2(v[y], d2, tt_mul2(o[y], inv2));
       }
       if (on) {
         uint4* to = reinterpret_cast<uint4*>(Y + (t0 + t) * ys + (long long)h * D);

@@ -33,11 +33,6 @@ __device__ __forceinline__ SeqView bwd_view(volatile int* d) {
   s.start = d[B_START]; s.len = d[B_LEN]; s.pin = d[B_PIN]; s.cap = d[B_CAP]; s.e = d[B_E];
   return s;
 }
-__device__ __forceinline__ uint64_t st_mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 
 template <int D>
 struct BSmem {
@@ -515,7 +510,7 @@ k_seq_dq_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensorM
           wait_ld();
 #pragma unroll
           for (int y = 0; y < 32; y += 2)
-            tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), nd2), tt_two(p[c + y], p[c + y + 1])), x[y], x[y + 1]);
+            tt_both(tt_mul2(tt_add2(tt_two(x[y], x[y + 1]), nd2), tt_two(p[c + y], p[c + y + 1])), x[y], x[y + 1]);
           if (!all) {
             const uint32_t keep = alone ? 0u : st_run(0, row + 1, jh + c) & ~st_run(s.pin, low, jh + c);
 #pragma unroll
@@ -820,8 +815,8 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int y = c; y < c + 32; y += 4) {
             const float4 v = *reinterpret_cast<const float4*>(st + TM + y);
-            tt_both(st_mul2(tt_add2(tt_two(x[y], x[y + 1]), tt_two(v.x, v.y)), tt_two(p[y], p[y + 1])), x[y], x[y + 1]);
-            tt_both(st_mul2(tt_add2(tt_two(x[y + 2], x[y + 3]), tt_two(v.z, v.w)), tt_two(p[y + 2], p[y + 3])), x[y + 2], x[y + 3]);
+            tt_both(tt_mul2(tt_add2(tt_two(x[y], x[y + 1]), tt_two(v.x, v.y)), tt_two(p[y], p[y + 1])), x[y], x[y + 1]);
+            tt_both(tt_mul2(tt_add2(tt_two(x[y + 2], x[y + 3]), tt_two(v.z, v.w)), tt_two(p[y + 2], p[y + 3])), x[y + 2], x[y + 3]);
           }
           if (!all) {
             const uint32_t keep = st_run(alone && i0 == j0 ? lo + 1 : lo, hi + 1, c);          // this token's own query is at lo
