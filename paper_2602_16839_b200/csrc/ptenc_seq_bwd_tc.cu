@@ -12,7 +12,7 @@
 // rounded to bf16 and are A operands in tensor memory, over the S and dP they came from; the tile that was K-major for the first
 // products is read MN-major for the second.
 //  * k_seq_dkv_tc, per tile of queries: dV and the next S^T run while dS is computed, dK and the next dP^T while the next P is.
-//    Tensor memory is full (S, dP, dV, dK: 4 x 128 columns), so nothing is buffered twice.  -lse and -delta of a tile's queries, which
+//    At D = 128 tensor memory is full (S, dP, dV, dK: 4 x 128 columns) and nothing is buffered twice.  -lse and -delta of a tile's queries, which
 //    run along a thread's columns, lie in shared memory.
 //  * k_seq_dq_tc, per tile of keys: S is buffered twice and dS goes over the S it came from, so that softmax warps never wait.
 // Bound by the chain of a step (scores, exponentials, dS, sums), of which tensor memory holds no second: the tensor pipe is busy 56 %
@@ -593,7 +593,12 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   }
   // beside the long items what came before them is over; without them this launch waits for it itself
   const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp, 1, !SPLIT && a.pins == 0);
-  const uint32_t tS = tmem, tP = tmem + SN, tV = tmem + 2 * SN, tK = tV + D;   // S^T, dP^T, dV, dK
+  // S^T, dP^T, dV, dK.  Narrow heads leave tensor memory for a second S^T, which is formed while P is: dK and dV of two sequences of 8192
+  // tokens, 32 + 8 heads of 64, 1.22 ms, 1.40 with one.  At D = 128 there is none; with P in shared memory in its stead, so that
+  // S^T could be overwritten as soon as it had been read, and a Q tile less in its ring, 1.96 ms instead of 1.80.
+  constexpr int BUFS = D == 128 ? 1 : 2;
+  const uint32_t tS = tmem, tP = tmem + BUFS * SN, tV = tP + SN, tK = tV + D;
+  static_assert((BUFS + 1) * SN + 2 * D <= 512, "tensor memory");
   // An item's steps: head by head, tiles B_TILE .. B_TILE + B_A - 1 of each; of them the B_N from B_B on.
 
   if (warp < 4) {
@@ -644,8 +649,8 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           if (which && t == 0 && !wait(X + 8 * X_B_FULL, seq & 1)) return false;
           if (!wait(ready + 8 * s, which ? SM::phase_b(nt + t) : SM::phase_a(nt + t))) return false;
           if (leader) {
-            mma_scores<D>(which ? tP : tS, sb + SM::OFF_AB + which * TILE, sb + s * TILE);
-            commit(X + 8 * (which ? X_DP_FULL : X_S_FULL));
+            mma_scores<D>(which ? tP : tS + (BUFS - 1) * ((nt + t) & 1) * SN, sb + SM::OFF_AB + which * TILE, sb + s * TILE);
+            commit(X + 8 * (which ? X_DP_FULL : X_S_FULL + (BUFS - 1) * ((nt + t) & 1)));
             if (t == n - 1) commit(X + 8 * (which ? X_B_EMPTY : X_A_EMPTY));     // the next item's V or K may come
           }
           __syncwarp();
@@ -655,11 +660,12 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         if (okay && !wait(X + 8 * X_ACC_EMPTY, (seq & 1) ^ 1)) okay = false;
         for (int t = 0; t < n && okay; ++t) {
           const uint32_t sq = SM::stage_a(nt + t), sg = SM::stage_b(nt + t);
+          if (BUFS == 2 && t + 1 < n && !product(t + 1, 0)) { okay = false; break; }
           if (!wait(X + 8 * X_P_READY, (nt + t) & 1)) { okay = false; break; }
           fence_after();
-          if (leader) { mma_sums<D>(tV, tS, sb + sg * TILE, t == 0); commit(empty + 8 * sg); }
+          if (leader) { mma_sums<D>(tV, tS + (BUFS - 1) * ((nt + t) & 1) * SN, sb + sg * TILE, t == 0); commit(empty + 8 * sg); }
           __syncwarp();
-          if (t + 1 < n && !product(t + 1, 0)) { okay = false; break; }
+          if (BUFS == 1 && t + 1 < n && !product(t + 1, 0)) { okay = false; break; }
           if (!wait(X + 8 * X_DS_READY, (nt + t) & 1)) { okay = false; break; }
           fence_after();
           if (leader) { mma_sums<D>(tK, tP, sb + sq * TILE, t == 0); commit(empty + 8 * sq); }
@@ -697,7 +703,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           const int i0 = (tile0 + at) * TM;
           // asked for early: rows past the end are not seen by anybody
           float v[4];
-  #pragma unroll
+#pragma unroll
           for (int y = 0; y < 4; ++y) {
             const int i = i0 + lane + 32 * y;
             v[y] = i < s.len ? stat[i] : 0.f;
@@ -710,7 +716,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             odd = patch_tile(smem + sg * TILE, D / 64, i0, s.len, 0, 1, bad);
             if (odd) {
               __syncwarp();
-  #pragma unroll
+#pragma unroll
               for (int y = 0; y < 4; ++y)
                 if ((bad[y] >> lane) & 1u) v[y] = __int_as_float(0x7fffffff);    // whoever sees the row becomes NaN
             }
@@ -718,7 +724,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           __syncwarp();
           if (lane == 0) bar_arrive(ready + 8 * sg);
           if (!wait(X + 8 * (X_STAT_EMPTY + buf), (((nt + t) >> 1) & 1) ^ 1)) { okay = false; break; }
-  #pragma unroll
+#pragma unroll
           for (int y = 0; y < 4; ++y) s_stat[buf * 2 * TM + me * TM + lane + 32 * y] = v[y];
           if (me == 1 && lane == 0) s_odd[buf] = odd;
           __syncwarp();
@@ -740,7 +746,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ST_REGS_HIGH));
     const int half = (warp - 4) >> 2, quarter = warp & 3, lrow = 32 * quarter + lane;
     const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
-    const uint32_t ts = tS + 64 * half + lane_off, tp = tP + 64 * half + lane_off;
+    const uint32_t tp = tP + 64 * half + lane_off;
     const float sl2 = a.scale * ST_LOG2E;
     const uint64_t scl2 = tt_two(sl2, sl2);
     uint32_t seq = 0, nt = 0;
@@ -762,12 +768,12 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       int i0 = j0 + skip * TM, left = tiles - skip;
 #pragma unroll 1
       for (int t = 0; t < n; ++t, ++nt) {
-        const uint32_t buf = nt & 1;
+        const uint32_t buf = nt & 1, ts = tS + (BUFS - 1) * buf * SN + 64 * half + lane_off;
         const float* st = s_stat + buf * 2 * TM + 64 * half;
         const bool all = i0 + TM <= s.len && j0 + TM - 1 <= i0 && i0 + TM - 1 <= until;
         const int lo = col - i0 - 64 * half, hi = last - i0 - 64 * half;       // columns [lo, hi] see this token
         wait(X + 8 * (X_STAT_FULL + buf), (nt >> 1) & 1);
-        wait(X + 8 * X_S_FULL, nt & 1);
+        wait(X + 8 * (X_S_FULL + (BUFS - 1) * buf), BUFS == 1 ? nt & 1 : (nt >> 1) & 1);
         fence_after();
         float p[64];
         ld32(ts, p);

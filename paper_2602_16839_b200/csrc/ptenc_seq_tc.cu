@@ -34,7 +34,7 @@ struct FSmem {
   static constexpr int OFF_CLC = OFF_Q + 2 * TILE;                   // 16 bytes of answer
   static constexpr int OFF_DESC = OFF_CLC + 16;                      // int [2][J_WORDS]
   static constexpr int OFF_BAR = (OFF_DESC + 2 * J_WORDS * 4 + 7) / 8 * 8;
-  static constexpr int N_BAR = 3 * STAGES + 16;
+  static constexpr int N_BAR = 3 * STAGES + 20;
   static constexpr int OFF_MISC = OFF_BAR + N_BAR * 8;               // int [4]
   static constexpr int TOTAL = OFF_MISC + 16;
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
@@ -95,7 +95,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
   const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, o_empty = o_full + 16,
                  q_full = o_empty + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16,
-                 clc = item_empty + 16, drain = clc + 8;
+                 clc = item_empty + 16, drain = clc + 8, s_read = drain + 8, p_empty = s_read + 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
@@ -105,6 +105,8 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       bar_init(p_full + 8 * s, 4);
       bar_init(o_full + 8 * s, 1);
       bar_init(o_empty + 8 * s, 4);
+      bar_init(s_read + 8 * s, 4);
+      bar_init(p_empty + 8 * s, 1);
       bar_init(item_full + 8 * s, 1);
       bar_init(item_empty + 8 * s, 1 + 2 + 8);           // MMA, patch and softmax warps
     }
@@ -126,6 +128,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   fence_after();
   const uint32_t tmem = (uint32_t)misc[1];
   const uint32_t tS = tmem, tO = tmem + 2 * SN;          // S [stream] of 128 columns, O [stream] of D columns
+  // Narrow heads leave tensor memory for P beside S: the next S is formed as soon as S has been read, under the same tile's weights
+  // (two sequences of 8192 tokens, 32 + 8 heads of 64: 799 us, 837 with P over S, where the next S waits for the product with P).
+  constexpr bool AHEAD = D == 64;
+  const uint32_t tP = AHEAD ? tmem + 2 * SN + 2 * D : tS, P_STEP = AHEAD ? SN / 2 : SN;         // P [stream]
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(ST_REGS_LOW));
@@ -208,6 +214,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       constexpr uint32_t ID_QK = tt_idesc(SN, 0), ID_PV = tt_idesc(D, 1);
       uint32_t nt = 0, seq = 0;                            // tiles and items
       uint32_t np0 = 0, np1 = 0, ni0 = 0, ni1 = 0;         // tiles and items of the streams
+      uint32_t ns0 = 0, ns1 = 0;                           // their scores so far
       bool okay = true;
       while (okay) {
         if (!__all_sync(0xffffffffu, item_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag, misc + 2))) { okay = false; break; }
@@ -224,11 +231,17 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         const int last0 = u0.last(), last1 = u1.last();
         if (!wait(q_full, seq & 1)) { okay = false; break; }
         ++seq;
-        auto issue_s = [&](int st, int i) {
+        auto issue_s = [&](int st, int i) -> bool {
+          if (AHEAD) {                                     // the scores before have been read
+            uint32_t& ns = st ? ns1 : ns0;
+            if (ns > 0 && !wait(s_read + 8 * st, (ns - 1) & 1)) return false;
+            ++ns;
+            fence_after();
+          }
           const uint32_t sg = SM::stage_k(nt + i);
           const uint64_t dq = desc_k(sb + SM::OFF_Q + st * TILE), dk = desc_k(sb + sg * TILE);
           if (leader) {
-  #pragma unroll
+#pragma unroll
             for (int k = 0; k < D / 16; ++k) {
               const uint64_t off = ((k >> 2) * HALF + (k & 3) * 32) >> 4;        // the address field counts 16 bytes
               mma_ss(tS + st * SN, dq + off, dk + off, ID_QK, k > 0);
@@ -236,6 +249,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             commit(s_full + 8 * st);
           }
           __syncwarp();
+          return true;
         };
         auto wait_k = [&](int i) -> bool { return wait(full + 8 * SM::stage_k(nt + i), SM::phase_k(nt + i)); };
         auto release = [&](uint32_t stage) {               // free once what has been issued is done
@@ -251,9 +265,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           if (!wait(p_full + 8 * st, np & 1)) return false;
           fence_after();
           if (leader) {
-  #pragma unroll
+#pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_ts(tO + st * D, tS + st * SN + k * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : (first ? 0u : 1u));
+              mma_ts(tO + st * D, tP + st * P_STEP + k * 8, dv + (k * 2048 >> 4), ID_PV, k > 0 ? 1u : (first ? 0u : 1u));
+            if (AHEAD) commit(p_empty + 8 * st);
           }
           __syncwarp();
           ++np;
@@ -267,8 +282,8 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         okay = wait_k(0);
         fence_after();
         const int t0 = seq_at(r, 0);
-        if (okay && u0.uses(t0)) issue_s(0, 0);
-        if (okay && u1.uses(t0)) issue_s(1, 0);
+        if (okay && u0.uses(t0)) okay = issue_s(0, 0);
+        if (okay && u1.uses(t0)) okay = issue_s(1, 0);
         auto q_done = [&]() {                              // all scores of the item have been issued: the next item's Q may come
           if (leader) commit(q_empty);
           __syncwarp();
@@ -280,19 +295,29 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           const int tile = seq_at(r, i), next = i + 1 < n ? seq_at(r, i + 1) : -1;
           bool v_there = false;
           const bool k0 = next >= 0 && u0.uses(next), k1 = next >= 0 && u1.uses(next);
+          if (AHEAD && next >= 0) {
+            okay = wait_k(i + 1);
+            fence_after();
+            if (okay && k0) okay = issue_s(0, i + 1);
+            if (okay && k1) okay = issue_s(1, i + 1);
+            if (!okay) break;
+            release(SM::stage_k(nt + i + 1));
+            if (i + 2 == n) q_done();
+          }
           if (u0.uses(tile)) {
             okay = step(0, i, tile, v_there, first0, np0, ni0, tile == last0);
             first0 = false;
           }
-          if (okay && next >= 0) { okay = wait_k(i + 1); fence_after(); }
-          if (okay && k0) issue_s(0, i + 1);
+          if (!AHEAD && okay && next >= 0) { okay = wait_k(i + 1); fence_after(); }
+          if (!AHEAD && okay && k0) okay = issue_s(0, i + 1);
           if (okay && u1.uses(tile)) {
             okay = step(1, i, tile, v_there, first1, np1, ni1, tile == last1);
             first1 = false;
           }
           if (!okay) break;
           release(SM::stage_v(nt + i));
-          if (k1) issue_s(1, i + 1);
+          if (AHEAD) continue;
+          if (k1) okay = issue_s(1, i + 1);
           if (next >= 0) release(SM::stage_k(nt + i + 1));
           if (i + 2 == n) q_done();
         }
@@ -344,7 +369,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ST_REGS_HIGH));
     const int st = (warp - 4) >> 2, quarter = warp & 3;
     const uint32_t lane_off = (uint32_t)(32 * quarter) << 16;
-    const uint32_t ts = tS + st * SN + lane_off, to = tO + st * D + lane_off;
+    const uint32_t ts = tS + st * SN + lane_off, to = tO + st * D + lane_off, tp = tP + st * P_STEP + lane_off;
     const float sl2 = a.scale * ST_LOG2E, slack = 8.f / sl2;
     uint32_t seq = 0, ntile = 0, nitem = 0;
     bool fine = true;                                    // false: a wait ran out; go through the motions, never wait again
@@ -376,6 +401,11 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 #pragma unroll
         for (int c = 0; c < SN; c += 32) ld32(ts + c, x + c);
         wait_ld();
+        if (AHEAD) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(s_read + 8 * st);
+        }
         if (!seq_all(s, i0, low1, tile * SN, tile * SN + SN - 1)) {
           const int j0 = tile * SN;
 #pragma unroll
@@ -393,6 +423,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           for (int z = 0; z < 4; ++z) mx[z] = tt_max3(mx[z], x[y + 2 * z], x[y + 2 * z + 1]);
         const float mine = tt_max3(tt_max3(mx[0], mx[1], mx[2]), tt_max3(mx[3], x[SN - 4], x[SN - 3]), fmaxf(x[SN - 2], x[SN - 1]));
         const float mnew = tt_max3(m, mine, mine);
+        if (AHEAD) {                                     // the product with the last P is done: O is at rest, and P may be written
+          wait(p_empty + 8 * st, ntile & 1);
+          fence_after();
+        }
         if (first) {
           m = mnew;
           first = false;
@@ -404,7 +438,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             if (grown) m = mnew;
             l *= corr;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {            // O is at rest: S of this tile came after the products before it
+            for (int c = 0; c < D; c += 16) {            // O is at rest: without AHEAD S of this tile came after the products before it
               float o[16];
               ld16(to + c, o);
               wait_ld();
@@ -430,7 +464,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             sum[(y >> 1) & 1] = tt_add2(sum[(y >> 1) & 1], tt_two(e0, e1));
             pk[y >> 1] = tt_pack(e0, e1);                // P in bf16, half a step of 2^-8 per weight; the sum is of the weights as they were
           }
-          st16(ts + c / 2, pk);
+          st16(tp + c / 2, pk);
         }
         // P is handed over in one piece: in halves or quarters its product would start earlier, but each hand-over costs the warp more
         // (16384 tokens, 28 heads of 128: 1535 us, in halves 1555, in quarters 1760)
