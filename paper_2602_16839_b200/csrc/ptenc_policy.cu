@@ -10,8 +10,8 @@
 // the first and behind the last 16-byte boundary are held by the first CTA's threads, one each.  Rows that eight CTAs cannot hold
 // are read three times.
 //
-// 4096 rows of 152000 bf16, loss and gradient: 540 us, 4.6 TB/s; the exponentials, two per logit, keep their unit busy for half of that.  1001
-// rows of 65537 fp32, none but the first aligned, a third masked: 93 us.  Log-probabilities of 16 rows of 32000 fp32: 6.1 us.
+// 4096 rows of 152000 bf16, loss and gradient: 547 us, 4.55 TB/s; the exponentials, two per logit, keep their unit busy for half of that.  1001
+// rows of 65537 fp32, none but the first aligned, a third masked: 92 us.  Log-probabilities of 16 rows of 32000 fp32: 6.4 us.
 #include <cooperative_groups.h>
 
 #include "ptenc_tc.cuh"
@@ -125,8 +125,8 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
     return;
   }
   const float zy = ptenc_to_float(z[y]);
-  float m = -INFINITY;
-  bool nan = false;
+  float m = zy;
+  bool nan = zy != zy;
   for (int x = tid; x < a.V; x += PL_THREADS) { const float v = ptenc_to_float(z[x]); m = fmaxf(m, v); nan |= v != v; }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -135,14 +135,16 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   for (int i = 0; i < PL_THREADS / 32; ++i) m = fmaxf(m, s_m[i]);
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
-  for (int x = tid; x < a.V; x += PL_THREADS) l += exp2f((ptenc_to_float(z[x]) - ref) * a.c2);
+  for (int x = tid; x < a.V; x += PL_THREADS)
+    if (x != y) l += exp2f((ptenc_to_float(z[x]) - ref) * a.c2);
   l = nan ? __int_as_float(0x7fffffff) : l;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
   if (lane == 0) s_l[warp] = l;
   __syncthreads();
-  l = 0.f;
-  for (int i = 0; i < PL_THREADS / 32; ++i) l += s_l[i];
+  float others = 0.f;                                    // without the token's own weight, see k_policy
+  for (int i = 0; i < PL_THREADS / 32; ++i) others += s_l[i];
+  l = others + exp2f((zy - ref) * a.c2);
   if (warp == 0) {
     const double lp = (((double)zy - (double)ref) * (double)a.c2 - pl_log2(l)) * 0.69314718055994530942;
     const PolicyRow o = pl_row(a, t, lp, w);
@@ -156,11 +158,8 @@ k_policy_row(const __grid_constant__ PolicyArgs a) {
   if (dz == nullptr) return;
   __syncthreads();                                       // also: everybody has read the row before it may be overwritten
   const float grad = s_out[0], scale = -grad / l;
-  for (int x = tid; x < a.V; x += PL_THREADS) {
-    float v = exp2f((ptenc_to_float(z[x]) - ref) * a.c2) * scale;
-    if (x == y) v += grad;
-    dz[x] = ptenc_from_float<T>(v);
-  }
+  for (int x = tid; x < a.V; x += PL_THREADS)
+    dz[x] = ptenc_from_float<T>(x == y ? grad * (others / l) : exp2f((ptenc_to_float(z[x]) - ref) * a.c2) * scale);
 }
 
 // ------------------------------------------------------------------------------------------------ a row per cluster
@@ -183,6 +182,16 @@ __device__ __forceinline__ uint4 pl_pack(const float (&f)[8], __nv_bfloat16) {
 }
 __device__ __forceinline__ uint4 pl_pack(const float (&f)[4], float) {
   return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+// A vector with its e-th value put to -inf.
+__device__ __forceinline__ uint4 pl_without(const uint4& w, int e, __nv_bfloat16) {
+  const uint32_t keep = (e & 1) ? 0xffffu : 0xffff0000u, inf = (e & 1) ? 0xff800000u : 0xff80u;
+  return make_uint4((e >> 1) == 0 ? (w.x & keep) | inf : w.x, (e >> 1) == 1 ? (w.y & keep) | inf : w.y,
+                    (e >> 1) == 2 ? (w.z & keep) | inf : w.z, (e >> 1) == 3 ? (w.w & keep) | inf : w.w);
+}
+__device__ __forceinline__ uint4 pl_without(const uint4& w, int e, float) {
+  const uint32_t inf = 0xff800000u;
+  return make_uint4(e == 0 ? inf : w.x, e == 1 ? inf : w.y, e == 2 ? inf : w.z, e == 3 ? inf : w.w);
 }
 // A vector's largest value, not counting NaN.
 __device__ __forceinline__ float pl_max(const uint4& w, __nv_bfloat16) {
@@ -217,6 +226,9 @@ struct PlSum {
   }
 };
 
+// The token's own weight is left out of the sums and added at the end: where it is nearly one, its gradient, which is the sum of the
+// others over the whole, would be the difference of two numbers that are the same but for their last bits.  (4096 rows of 152000 bf16
+// 547 us so, 539 with one sum.)
 template <typename T>
 __global__ void __launch_bounds__(PL_THREADS, PL_CTAS)
 k_policy(const __grid_constant__ PolicyArgs a) {
@@ -276,7 +288,8 @@ k_policy(const __grid_constant__ PolicyArgs a) {
   const float c2 = a.c2;
   const uint64_t c22 = tt_two(c2, c2);
   PlSum sum = {-INFINITY, 0.f};
-  if (has) {
+  const int yb = y - head - N * v0, yv = yb >= 0 && yb < N * mine ? yb / N : -1, ye = yb & (N - 1);      // where y lies in this CTA's slice
+  if (has && lx != y) {
     sum.grow(zl, c2);
     sum.l += tt_ex2((zl - sum.ref()) * c2);
   }
@@ -295,7 +308,14 @@ k_policy(const __grid_constant__ PolicyArgs a) {
       uint4 r[4];
       float mx[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) { r[k] = row[v + k * PL_THREADS]; mx[k] = pl_max(r[k], T()); }
+      for (int k = 0; k < 4; ++k) r[k] = row[v + k * PL_THREADS];
+      if ((unsigned)(yv - v) < 4u * PL_THREADS) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (v + k * PL_THREADS == yv) r[k] = pl_without(r[k], ye, T());
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) mx[k] = pl_max(r[k], T());
       sum.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), c2);
       const float nr = -sum.ref();
       const uint64_t nr2 = tt_two(nr, nr);
@@ -316,7 +336,8 @@ k_policy(const __grid_constant__ PolicyArgs a) {
       sum.l += lo + hi;
     }
     for (; v < end; v += PL_THREADS) {
-      const uint4 r = row[v];
+      uint4 r = row[v];
+      if (v == yv) r = pl_without(r, ye, T());
       sum.grow(pl_max(r, T()), c2);
       const float nr = -sum.ref();
       const uint64_t nr2 = tt_two(nr, nr);
@@ -357,6 +378,10 @@ k_policy(const __grid_constant__ PolicyArgs a) {
       for (int i = 1; i < cs; ++i)                       // in the same order everywhere
         sum.join(__shfl_sync(0xffffffffu, own.x, i), __shfl_sync(0xffffffffu, own.y, i), c2);
     }
+    // the others' weights and the token's own, by the larger maximum
+    const float m_o = sum.ref(), some = sum.l;
+    sum.join(zy, zy == -INFINITY ? 0.f : zy - zy + 1.f, c2);             // NaN and inf become NaN
+    const float others = some == 0.f ? 0.f : some * tt_ex2((m_o - sum.ref()) * c2);
     const double lp = (((double)zy - (double)sum.ref()) * (double)c2 - pl_log2(sum.l)) * 0.69314718055994530942;
     const PolicyRow o = pl_row(a, t, lp, w);
     if (lane == 0) {
@@ -365,7 +390,7 @@ k_policy(const __grid_constant__ PolicyArgs a) {
         if (a.token_loss != nullptr) a.token_loss[t] = o.loss;
         if (a.token_kl != nullptr) a.token_kl[t] = o.kl;
       }
-      s_out[0] = -sum.ref(); s_out[1] = o.grad; s_out[2] = -o.grad / sum.l;
+      s_out[0] = -sum.ref(); s_out[1] = o.grad * (others / sum.l); s_out[2] = -o.grad / sum.l;
     }
     __syncwarp();
   }
@@ -374,8 +399,7 @@ k_policy(const __grid_constant__ PolicyArgs a) {
   if (dz != nullptr) {
     const float nr = s_out[0], grad = s_out[1], scale = s_out[2];
     const uint64_t nr2 = tt_two(nr, nr);
-    if (has) dz[lx] = ptenc_from_float<T>(fmaf(tt_ex2((zl + nr) * c2), scale, lx == y ? grad : 0.f));
-    const int yb = y - head - N * v0;                    // where y lies in this CTA's slice
+    if (has) dz[lx] = ptenc_from_float<T>(lx == y ? grad : tt_ex2((zl + nr) * c2) * scale);
     T* to = dz + head + (long long)N * v0;
     if (same) {
 #pragma unroll 2
@@ -392,14 +416,14 @@ k_policy(const __grid_constant__ PolicyArgs a) {
         if ((unsigned)(yb - N * v) < (unsigned)N) {      // one vector of the row
 #pragma unroll
           for (int e = 0; e < N; ++e)
-            if (yb - N * v == e) f[e] = fmaf(tt_ex2((zy + nr) * c2), scale, grad);
+            if (yb - N * v == e) f[e] = grad;
         }
         reinterpret_cast<uint4*>(to)[v] = pl_pack(f, T());
       }
     } else {
       const T* from = reinterpret_cast<const T*>(s_row);
       for (int x = tid; x < mine * N; x += PL_THREADS)
-        to[x] = ptenc_from_float<T>(fmaf(tt_ex2((ptenc_to_float(from[x]) + nr) * c2), scale, x == yb ? grad : 0.f));
+        to[x] = ptenc_from_float<T>(x == yb ? grad : tt_ex2((ptenc_to_float(from[x]) + nr) * c2) * scale);
     }
   }
   if (cs > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
