@@ -260,7 +260,7 @@ typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t rotary_dim;      /* the first rotary_dim values of a head are rotated: even, 0..head_dim         */
   int32_t interleaved;     /* 0: value i is paired with value i + rotary_dim / 2; 1: 2i with 2i + 1        */
-  float eps;               /* added to the mean square, >= 0                                               */
+  float eps;               /* added to the mean square, >= 0; with 0 a head of zeros becomes NaN           */
 } ptenc_rope_config;
 
 /* Norm of every query and key head and its rotation by the token's position, in one pass:

@@ -293,6 +293,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
           float lo, hi;
           tt_both(sq, lo, hi);
           inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
+          if (!on) inv = 0.f;                            // no head here: with eps = 0 its zeros would add 0 * inf to the weights' gradients
           const uint64_t inv2 = tt_two(inv, inv);
 #pragma unroll
           for (int y = 0; y < N; ++y) v[y] = tt_mul2(v[y], inv2);
