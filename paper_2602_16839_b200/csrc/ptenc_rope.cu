@@ -293,7 +293,6 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
           float lo, hi;
           tt_both(sq, lo, hi);
           inv = rsqrtf(rp_group_sum(lo + hi, sh.lanes) * rD + a.eps);      // groups of a warp take the same steps
-          if (!on) inv = 0.f;                            // no head here: with eps = 0 its zeros would add 0 * inf to the weights' gradients
           const uint64_t inv2 = tt_two(inv, inv);
 #pragma unroll
           for (int y = 0; y < N; ++y) v[y] = tt_mul2(v[y], inv2);
@@ -338,7 +337,7 @@ k_rope(const __grid_constant__ RopeArgs a, const __grid_constant__ RopeShape sh)
         uint64_t dot2 = 0ull;
 #pragma unroll
         for (int y = 0; y < N; ++y) {
-          dw[y] = tt_fma2(o[y], v[y], dw[y]);
+          if (on) dw[y] = tt_fma2(o[y], v[y], dw[y]);    // with eps = 0 the zeros of a group without a head have the norm 0 * inf
           o[y] = tt_mul2(o[y], w2[y]);
           dot2 = tt_fma2(o[y], v[y], dot2);
         }
