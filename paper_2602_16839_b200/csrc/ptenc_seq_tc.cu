@@ -23,8 +23,8 @@ namespace {
 constexpr int ST_ROWS = 2 * TM;                // query rows of an item
 
 // ------------------------------------------------------------------------------------------------ layout
-// Item description words in shared memory.
-enum { J_KIND, J_START, J_LEN, J_PIN, J_CAP, J_E, J_HEAD, J_ROW0, J_NP, J_S0, J_S1, J_N, J_ODD, J_WORDS };
+// Item description words in shared memory.  J_ODD .. J_ODD_END - 1: its tiles between the first and the last that values were taken out of.
+enum { J_KIND, J_START, J_LEN, J_PIN, J_CAP, J_E, J_HEAD, J_ROW0, J_NP, J_S0, J_S1, J_N, J_ODD, J_ODD_END, J_WORDS };
 
 template <int D>
 struct FSmem {
@@ -62,21 +62,62 @@ __device__ __forceinline__ SeqView view_of(volatile int* d) {
   s.start = d[J_START]; s.len = d[J_LEN]; s.pin = d[J_PIN]; s.cap = d[J_CAP]; s.e = d[J_E];
   return s;
 }
-// Adds the non-finite values that were taken out of V tiles to 16 columns of a row that sees them.
+// Bounded wait of the forward kernel: it lasts for as long as the CTA gets on, and 8 ms more.  The word counts the numbers that the producer has
+// looked at, the tiles that it has asked for, and the tiles that the epilogue has searched; below zero the CTA has given up.  Numbers that
+// belong to no tile (one per empty sequence and head), the tiles that only the other stream sees (a whole chunk, where one leaves inside an
+// item) and a search through a chunk's tiles can each take longer than 8 ms.
+constexpr int F_ABORT = -0x7fffffff - 1;
+__device__ __forceinline__ bool fwd_wait(uint32_t bar, uint32_t parity, volatile int* progress) {
+  if (bar_try(bar, parity)) return true;
+  int seen = -1;
+  for (uint32_t tries = 0; tries < TT_POLLS; ++tries) {
+    if (bar_try(bar, parity)) return true;
+    const int now = *progress;
+    if (now < 0) return false;
+    if (now != seen) tries = 0;
+    seen = now;
+  }
+  return false;
+}
+// Adds the non-finite values that were taken out of V tiles u0 .. u1 - 1 of an item to 16 columns, c < D, of a row that sees them.  The whole
+// warp calls it, each lane with its row: a lane looks at a token's 16 values, what is found goes round.  After an eviction inside an item the tiles that
+// some row does not see are a whole chunk, so the search is counted as getting on, tile by tile, while the other roles wait.
 __device__ __noinline__ void add_odd(float* o, const __nv_bfloat16* v, long long vs, int c, int D, const SeqView s, int row, int row0,
-                                     SeqRange r, int n) {
-  const int lo = s.low(row), low1 = s.low(row0 + ST_ROWS - 1);
-  for (int u = 0; u < n; ++u) {
-    const int tile = seq_at(r, u);
-    if (seq_all(s, row0, low1, tile * SN, tile * SN + SN - 1)) continue;
-    for (int j = tile * SN; j < min(tile * SN + SN, row + 1); ++j) {
-      if (j >= s.pin && j < lo) continue;
-      for (int y = 0; y < 16; ++y) {
-        if (c + y >= D) break;
-        const float x = __bfloat162float(v[(long long)j * vs + c + y]);
-        if (!isfinite(x)) o[y] += x;
+                                     SeqRange r, int u0, int u1, int* progress) {
+  const int lane = threadIdx.x & 31, lo = s.low(row), low1 = s.low(row0 + ST_ROWS - 1);
+  for (int u = u0; u < u1; ++u) {
+    const int j0 = seq_at(r, u) * SN;
+    if (seq_all(s, row0, low1, j0, j0 + SN - 1)) continue;
+    uint4 w[SN / 32][2];
+#pragma unroll
+    for (int k = 0; k < SN / 32; ++k) {
+      const int j = j0 + 32 * k + lane;
+      const uint4* from = reinterpret_cast<const uint4*>(v + (long long)j * vs + c);
+      w[k][0] = w[k][1] = make_uint4(0u, 0u, 0u, 0u);
+      if (j < s.len) {
+        w[k][0] = from[0];
+        if (c + 8 < D) w[k][1] = from[1];
       }
     }
+#pragma unroll
+    for (int k = 0; k < SN / 32; ++k) {
+      const uint32_t e[8] = {w[k][0].x, w[k][0].y, w[k][0].z, w[k][0].w, w[k][1].x, w[k][1].y, w[k][1].z, w[k][1].w};
+      bool hit = false;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) hit |= (e[y] & 0x7f80u) == 0x7f80u || (e[y] & 0x7f800000u) == 0x7f800000u;
+      for (uint32_t hits = __ballot_sync(0xffffffffu, hit); hits != 0; hits &= hits - 1) {
+        const int from = __ffs((int)hits) - 1, j = j0 + 32 * k + from;
+        const bool sees = row < s.len && j <= row && (j < s.pin || j >= lo);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const uint32_t x = __shfl_sync(0xffffffffu, e[y], from);
+          const float x0 = __uint_as_float(x << 16), x1 = __uint_as_float(x & 0xffff0000u);
+          if (sees && !isfinite(x0)) o[2 * y] += x0;
+          if (sees && !isfinite(x1)) o[2 * y + 1] += x1;
+        }
+      }
+    }
+    if (lane == 0) atomicAdd(progress, 1);
   }
 }
 
@@ -90,8 +131,9 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sb = tt_u32(smem);
   volatile int* desc = reinterpret_cast<volatile int*>(smem + SM::OFF_DESC);
-  volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);    // [0] abort, [1] TMEM base, [2] numbers looked at
-  volatile int* abort_flag = misc;
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + SM::OFF_MISC);    // [0] how far the CTA is, [1] TMEM base
+  int* progress = reinterpret_cast<int*>(smem + SM::OFF_MISC);
+  auto st_wait = [&](uint32_t bar, uint32_t parity) -> bool { return fwd_wait(bar, parity, misc); };
   const uint32_t full = sb + SM::OFF_BAR, empty = full + 8 * NS, ready = empty + 8 * NS;
   const uint32_t s_full = ready + 8 * NS, p_full = s_full + 16, o_full = p_full + 16, o_empty = o_full + 16,
                  q_full = o_empty + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16,
@@ -114,7 +156,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     bar_init(q_empty, 1);
     bar_init(clc, 1);
     bar_init(drain, 1);
-    misc[0] = misc[2] = 0;
+    misc[0] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -144,7 +186,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         int item = (int)blockIdx.x;
         while (okay) {
           if (item < 0) {
-            if (bar_wait(item_empty + 8 * (seq & 1), ((seq >> 1) & 1) ^ 1, abort_flag)) {
+            if (st_wait(item_empty + 8 * (seq & 1), ((seq >> 1) & 1) ^ 1)) {
               desc[(seq & 1) * J_WORDS + J_KIND] = 0;
               bar_arrive(item_full + 8 * (seq & 1));
             } else {
@@ -152,7 +194,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             }
             break;
           }
-          misc[2] = misc[2] + 1;
+          atomicAdd(progress, 1);
           bar_expect(clc, 16);
           clc_ask(sb + SM::OFF_CLC, clc);
           const int number = (int)(gridDim.x - 1 - item) / a.Hq, h = (int)(gridDim.x - 1 - item) - number * a.Hq;
@@ -163,14 +205,14 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             const int row0 = tile * ST_ROWS;
             const SeqRange r = seq_keys(s, row0, min(row0 + ST_ROWS, s.len) - 1, SN);
             const int n = seq_count(r);
-            if (!bar_wait(item_empty + 8 * slot, ((seq >> 1) & 1) ^ 1, abort_flag)) { okay = false; break; }
+            if (!st_wait(item_empty + 8 * slot, ((seq >> 1) & 1) ^ 1)) { okay = false; break; }
             volatile int* d = desc + slot * J_WORDS;
             d[J_START] = s.start; d[J_LEN] = s.len; d[J_PIN] = s.pin; d[J_CAP] = s.cap; d[J_E] = s.e; d[J_HEAD] = h;
-            d[J_ROW0] = row0; d[J_NP] = r.np; d[J_S0] = r.s0; d[J_S1] = r.s1; d[J_N] = n; d[J_ODD] = 0;
+            d[J_ROW0] = row0; d[J_NP] = r.np; d[J_S0] = r.s0; d[J_S1] = r.s1; d[J_N] = n; d[J_ODD] = n; d[J_ODD_END] = 0;
             d[J_KIND] = 1;
             bar_arrive(item_full + 8 * slot);
             const bool two = row0 + TM < s.len;
-            if (!bar_wait(q_empty, (seq & 1) ^ 1, abort_flag)) { okay = false; break; }
+            if (!st_wait(q_empty, (seq & 1) ^ 1)) { okay = false; break; }
             bar_expect(q_full, (uint32_t)((two ? 2 : 1) * TILE));
             for (int t = 0; t < (two ? 2 : 1); ++t)
               for (int hf = 0; hf < DH; ++hf)
@@ -178,26 +220,27 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
             ++seq;
             const int hk = h / a.g;
             for (int i = 0; i < n; ++i, ++nt) {
+              atomicAdd(progress, 1);
               const int j = s.start + seq_at(r, i) * SN;
               uint32_t sg = SM::stage_k(nt);
-              if (!bar_wait(empty + 8 * sg, SM::phase_k(nt) ^ 1, abort_flag)) { okay = false; break; }
+              if (!st_wait(empty + 8 * sg, SM::phase_k(nt) ^ 1)) { okay = false; break; }
               bar_expect(full + 8 * sg, (uint32_t)TILE);
               for (int hf = 0; hf < DH; ++hf) tma_3d(sb + sg * TILE + hf * HALF, &tmK, hf * 64, hk, j, full + 8 * sg);
               sg = SM::stage_v(nt);
-              if (!bar_wait(empty + 8 * sg, SM::phase_v(nt) ^ 1, abort_flag)) { okay = false; half = true; break; }
+              if (!st_wait(empty + 8 * sg, SM::phase_v(nt) ^ 1)) { okay = false; half = true; break; }
               bar_expect(full + 8 * sg, (uint32_t)TILE);
               for (int hf = 0; hf < DH; ++hf) tma_3d(sb + sg * TILE + hf * HALF, &tmV, hf * 64, hk, j, full + 8 * sg);
             }
           }
           // the answer is waited for whatever happened: it is a copy in flight
           if (okay) {
-            if (!bar_wait(clc, asked & 1, abort_flag)) { okay = false; break; }
+            if (!st_wait(clc, asked & 1)) { okay = false; break; }
             item = clc_answer(sb + SM::OFF_CLC);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             ++asked;
           }
         }
-        if (!okay) { *abort_flag = 1; bar_drain(clc, asked & 1); }
+        if (!okay) { misc[0] = F_ABORT; bar_drain(clc, asked & 1); }
         // whatever the other roles did, copies in flight land before the shared memory goes away
         const uint32_t nk = nt + (half ? 1 : 0);
         for (uint32_t i = 1; i <= (uint32_t)SM::RK && i <= nk; ++i) bar_drain(full + 8 * SM::stage_k(nk - i), SM::phase_k(nk - i));
@@ -208,7 +251,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       // ================================================================ MMA issuer: the whole warp takes every step, one lane issues
       const bool leader = tt_elect();
       auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag));
+        return __all_sync(0xffffffffu, st_wait(bar, parity));
       };
       auto get = [&](int x) -> int { return __shfl_sync(0xffffffffu, x, 0); };
       constexpr uint32_t ID_QK = tt_idesc(SN, 0), ID_PV = tt_idesc(D, 1);
@@ -217,7 +260,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       uint32_t ns0 = 0, ns1 = 0;                           // their scores so far
       bool okay = true;
       while (okay) {
-        if (!__all_sync(0xffffffffu, item_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag, misc + 2))) { okay = false; break; }
+        if (!__all_sync(0xffffffffu, st_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1))) { okay = false; break; }
         volatile int* d = desc + (seq & 1) * J_WORDS;
         const int kind = get(d[J_KIND]);
         if (kind == 0) break;
@@ -324,7 +367,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         nt += n;
       }
       if (leader) {
-        if (!okay) *abort_flag = 1;
+        if (!okay) misc[0] = F_ABORT;
         commit(drain);                                     // MMAs still in flight finish before tensor memory is freed
         bar_drain(drain, 0);
       }
@@ -334,10 +377,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
       uint32_t nt = 0, seq = 0;
       bool okay = true;
       auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag));
+        return __all_sync(0xffffffffu, st_wait(bar, parity));
       };
       while (okay) {
-        if (!__all_sync(0xffffffffu, item_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag, misc + 2))) { okay = false; break; }
+        if (!__all_sync(0xffffffffu, st_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1))) { okay = false; break; }
         volatile int* d = desc + (seq & 1) * J_WORDS;
         if (d[J_KIND] == 0) break;
         const SeqView s = view_of(d);
@@ -351,8 +394,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           const uint32_t sg = SM::stage_v(nt + i);
           if (!wait(full + 8 * sg, SM::phase_v(nt + i))) { okay = false; break; }
           if (!seq_all(s, row0, low1, tile * SN, tile * SN + SN - 1) &&
-              patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2, nullptr) && lane == 0)
-            d[J_ODD] = 1;
+              patch_tile(smem + sg * TILE, DH, tile * SN, s.len, warp - 2, 2, nullptr) && lane == 0) {
+            atomicMin(const_cast<int*>(d) + J_ODD, i);
+            atomicMax(const_cast<int*>(d) + J_ODD_END, i + 1);
+          }
           __syncwarp();
           if (lane == 0) bar_arrive(ready + 8 * sg);
         }
@@ -362,7 +407,7 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         ++seq;
         nt += n;
       }
-      if (!okay && lane == 0) *abort_flag = 1;
+      if (!okay && lane == 0) misc[0] = F_ABORT;
     }
   } else {
     // ================================================================ softmax: stream st, a row per thread
@@ -374,10 +419,10 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
     uint32_t seq = 0, ntile = 0, nitem = 0;
     bool fine = true;                                    // false: a wait ran out; go through the motions, never wait again
     auto wait = [&](uint32_t bar, uint32_t parity) {
-      if (fine && !bar_wait(bar, parity, abort_flag)) { fine = false; *abort_flag = 1; }
+      if (fine && !st_wait(bar, parity)) { fine = false; misc[0] = F_ABORT; }
     };
     while (true) {
-      if (fine && !item_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1, abort_flag, misc + 2)) { fine = false; *abort_flag = 1; }
+      if (fine && !st_wait(item_full + 8 * (seq & 1), (seq >> 1) & 1)) { fine = false; misc[0] = F_ABORT; }
       if (!__all_sync(0xffffffffu, fine)) break;
       volatile int* d = desc + (seq & 1) * J_WORDS;
       if (d[J_KIND] == 0) break;
@@ -481,7 +526,8 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
         wait(o_full + 8 * st, nitem & 1);
         ++nitem;
         fence_after();
-        const bool odd = d[J_ODD] != 0;
+        // one lane's: tiles that only the other stream sees may still be added
+        const int odd0 = __shfl_sync(0xffffffffu, d[J_ODD], 0), odd1 = __shfl_sync(0xffffffffu, d[J_ODD_END], 0);
         const float inv = !fine || m == -INFINITY ? __int_as_float(0x7fffffff) : 1.f / l;     // every score -inf: NaN
         const long long orow = (long long)(s.start + row) * a.Hq + h;
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + orow * a.D;
@@ -492,11 +538,11 @@ k_seq_fwd_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
           float o[16];
           ld16(to + c, o);
           wait_ld();
-          if (odd && real) {
+          if (odd0 < odd1 && c < a.D) {                  // rare
             float x[16];
 #pragma unroll
             for (int y = 0; y < 16; ++y) x[y] = o[y];
-            add_odd(x, v, a.vs, c, a.D, s, row, row0, r, n);
+            add_odd(x, v, a.vs, c, a.D, s, row, row0, r, odd0, odd1, progress);
 #pragma unroll
             for (int y = 0; y < 16; ++y) o[y] = x[y];
           }

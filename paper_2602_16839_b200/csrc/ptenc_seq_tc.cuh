@@ -86,8 +86,8 @@ __device__ __forceinline__ bool patch_tile(uint8_t* tile, int halves, int row0, 
   return odd;
 }
 
-// Waits for a CTA's next item for as long as its producer, which counts the numbers it has looked at, gets on: a bounded wait lasts some
-// 20 ms, and numbers that belong to no tile (one per empty sequence and head) can take longer than that together.
+// Waits for a CTA's next item for as long as its producer, which counts the numbers it has looked at, gets on: a bounded wait lasts 8 ms,
+// and numbers that belong to no tile (one per empty sequence and head) can take longer than that together.
 __device__ __forceinline__ bool item_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* looks) {
   for (int seen = -1;;) {
     if (bar_wait(bar, parity, abort_flag)) return true;

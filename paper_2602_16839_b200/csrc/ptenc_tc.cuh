@@ -8,7 +8,9 @@
 
 namespace {
 
-constexpr uint32_t TT_POLLS = 2000;             // bounded wait: tries of up to a millisecond each before giving up
+// Bounded wait: tries before giving up.  The hardware lets a try last 4 us (measured; the millisecond that bar_try allows is only its limit), so
+// a wait that runs out has lasted 8 ms.
+constexpr uint32_t TT_POLLS = 2000;
 constexpr int TM = 128;                        // rows of a row tile = TMEM lanes
 constexpr int HALF = 128 * 128;                // bytes of 64 bf16 columns of a 128-row tile
 
@@ -23,8 +25,8 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// Lets the hardware park the thread for up to a millisecond instead of spinning: the waiting warps share their schedulers
-// with the softmax warps.
+// Lets the hardware park the thread instead of spinning, for as long as it sees fit: the waiting warps share their schedulers with the
+// softmax warps.
 __device__ __forceinline__ uint32_t bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(

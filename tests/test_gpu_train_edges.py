@@ -48,3 +48,49 @@ def test_norms_without_eps_whose_heads_do_not_fill_a_step(n, Hq, Hkv, D, rot, in
         terms = min(n * x.shape[1], 8192)
         each = (D / 16 + 48) * to.U
         _close(dw, rw, bw * (each + min(terms, 64) * to.U) / (each + terms * to.U) + to.U * rw.abs(), "dw")
+
+
+# ------------------------------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("D", [128, 64, 8])
+@pytest.mark.parametrize("many", [False, True])
+def test_non_finite_values_where_a_whole_chunk_leaves_inside_a_tile(many, D):
+    """The rows of one tile on both sides of an eviction of 32700 tokens: a value that is no number reaches the rows that see it, in its
+    column, and nothing else changes, however long those rows take to find it."""
+    lens, Hq, Hkv, W = [33100, 700], 8, 2, 32700
+    n, gen = sum(lens), _gen(D)
+    q, k, v = (torch.randn(n, h, D, device=DEV, generator=gen).bfloat16() for h in (Hq, Hkv, Hkv))
+    cu = torch.tensor([0, lens[0], n], dtype=torch.int32, device=DEV)
+
+    def go():
+        out, lse = torch.full((n, Hq, D), 3.0, dtype=torch.bfloat16, device=DEV), torch.full((n, Hq), 3.0, device=DEV)
+        pt.seq_attn(q, k, v, cu, out, lse_out=lse, window=W, evict_chunk=W)
+        return out, lse
+
+    out, lse = go()
+    assert out.isfinite().all() and lse.isfinite().all() and not (lse == 3.0).any()
+    first = 100
+    v[first:(W if many else first + 1), 0, 5] = float("nan")
+    got, lse2 = go()
+    assert torch.equal(lse, lse2)
+    hit = torch.zeros(n, Hq, D, dtype=torch.bool, device=DEV)
+    hit[first:W, :Hq // Hkv, 5] = True                               # rows first .. W - 1 hold what came since the start, the next are empty
+    assert got[hit].isnan().all()
+    assert torch.equal(got[~hit], out[~hit])
+
+
+def test_a_chunk_of_two_million_tokens_that_leaves_between_the_halves_of_a_tile():
+    """The rows behind the eviction wait while the rows before it go through two million keys."""
+    W, Hq, D = 2_000_000, 1, 64                                      # W = 128 modulo 256: the rows of a work item from its second half on
+    n, gen = W + 300, _gen(1)
+    q, k = (torch.randn(n, Hq, D, device=DEV, generator=gen).bfloat16() for _ in range(2))
+    v = torch.ones(n, Hq, D, dtype=torch.bfloat16, device=DEV)
+    v[W:] = torch.randn(n - W, Hq, D, device=DEV, generator=gen).bfloat16()
+    cu = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    out, lse = torch.full_like(q, 3.0), torch.full((n, Hq), -3.0, device=DEV)
+    pt.seq_attn(q, k, v, cu, out, lse_out=lse, window=W, evict_chunk=W)
+    # a row's weights add up to one: half a step of bf16 for each weight and for the result, and two sums over fewer than 2^14 tiles in fp32
+    assert float((out[:W].float() - 1).abs().max()) <= 2 * 2.0 ** -8 + 2 * 2.0 ** 14 * to.U
+    assert not (lse[:W] == -3.0).any() and lse.isfinite().all()
+    r = to.seq_attn(q[W:], k[W:], v[W:], [n - W], dtype=torch.bfloat16, tensor_cores=True)
+    _close(out[W:], r["out"], r["b_out"] + 2.0 ** -108, "out")
+    _close(lse[W:], r["lse"], r["b_lse"], "lse")
