@@ -312,8 +312,8 @@ typedef struct {
  *   bf16 with head_dim up to 128 runs on the tensor cores: the weights are rounded to bf16 in the product with V, everything else is
  * fp32 but the results; outputs are off by 1.8e-3 to 2.2e-3 of their size in the 2-norm, where rounding the result alone gives 1.7e-3.  The
  * tensor cores add 16 tokens at a time to their fp32 sums and cut what does not fit: sums over n tokens, here and in the gradients, come
- * out smaller by some n / 16 * 2^-24 of their size (6e-5 for 16384 tokens, 7e-3 for two million).  Other shapes and fp32 are computed in
- * fp32.  A kernel whose waits run out (broken memory) leaves NaN in the rows
+ * out smaller by up to n / 16 * 2^-23 of their size (below 1.3e-4 for 16384 tokens; 1.05e-2 measured at two million, where the bound is
+ * 1.5e-2).  Other shapes and fp32 are computed in fp32.  A kernel whose waits run out (broken memory) leaves NaN in the rows
  * that it was at, and rows that it had not come to may keep what they held. */
 PTENC_API int ptenc_seq_attn(const ptenc_seq_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
                              int64_t k_stride, const void* v, int64_t v_stride, const int32_t* cu_seqlens,
