@@ -588,10 +588,15 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
   int sv_tile = 0;
   if (SPLIT) {
     tree_after_previous();
+    __threadfence();
     tree_let_next_start();
     if (!dkv_find_long(a, own / a.Hkv, &sv, &sv_tile)) return;                 // the whole cluster agrees
   }
-  // beside the long items what came before them is over; without them this launch waits for it itself
+  // Without long items this launch waits for the gradients of the queries itself.  Beside them it does not: each of their CTAs has waited before it
+  // let this launch start, so that kernel and all before it are over and what they wrote is in L2.  It is not promised to a reader that has
+  // not waited itself, and L1 may hold lines of an earlier call: hence the fences on both sides, and delta and lse are read past L1.  (With a wait
+  // of its own, that is behind the long items: both passes of 19 rollouts 1651 -> 1720 us, the gradients of one of 32768 tokens 1470 -> 1990.)
+  if (!SPLIT && a.pins > 0) __threadfence();
   const uint32_t tmem = bwd_begin<D>(smem, sb, tid, warp, 1, !SPLIT && a.pins == 0);
   // S^T, dP^T, dV, dK.  Narrow heads leave tensor memory for a second S^T, which is formed while P is: dK and dV of two sequences of 8192
   // tokens, 32 + 8 heads of 64, 1.22 ms, 1.40 with one.  At D = 128 there is none; with P in shared memory in its stead, so that
@@ -706,7 +711,7 @@ k_seq_dkv_tc(const __grid_constant__ SeqArgs a, const __grid_constant__ CUtensor
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const int i = i0 + lane + 32 * y;
-            v[y] = i < s.len ? stat[i] : 0.f;
+            v[y] = i < s.len ? __ldcg(stat + i) : 0.f;     // past L1: see the launch of the others
           }
           if (!wait(full + 8 * sg, me == 0 ? SM::phase_a(nt + t) : SM::phase_b(nt + t))) { okay = false; break; }
           bool odd = false;

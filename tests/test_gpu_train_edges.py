@@ -96,3 +96,41 @@ def test_a_chunk_of_two_million_tokens_that_leaves_between_the_halves_of_a_tile(
     r = to.seq_attn(q[W:], k[W:], v[W:], [n - W], dtype=torch.bfloat16, tensor_cores=True)
     _close(out[W:], r["out"], r["b_out"] + 2.0 ** -108, "out")
     _close(lse[W:], r["lse"], r["b_lse"], "lse")
+
+
+@pytest.mark.parametrize("D", [128, 64])
+def test_gradients_of_rollouts_that_follow_one_another_in_the_same_tensors(D):
+    """Other rollouts, bounds and pinned prompts in the same tensors and the same workspace, call after call with nothing in between: the
+    launch of the short items, which starts beside that of the long ones, reads this call's numbers."""
+    n, Hq, Hkv, W, E, dt = 6000, 8, 2, 256, 64, torch.bfloat16
+    kw = dict(window=W, evict_chunk=E)
+    sets = []
+    for seed, lens, pins in ((1, [2500, 3000, 400, 100], [200, 130, 0, 90]), (2, [300, 5000, 0, 700], [0, 255, 3, 129]),
+                             (3, [1500, 1500, 1500, 1500], [128, 1, 250, 64])):
+        gen = _gen(seed)
+        q, k, v, g = (torch.randn(n, h, D, device=DEV, generator=gen).to(dt) for h in (Hq, Hkv, Hkv, Hq))
+        cu = torch.tensor([0] + list(torch.tensor(lens).cumsum(0)), dtype=torch.int32, device=DEV)
+        pin = torch.tensor(pins, dtype=torch.int32, device=DEV)
+        sets.append([q, k, v, g, cu, pin])
+    bufs = [torch.empty_like(t) for t in sets[0]]
+    ws = torch.empty(pt.seq_attn_workspace_bytes(n, Hq), dtype=torch.uint8, device=DEV)
+    out, lse = torch.empty(n, Hq, D, dtype=dt, device=DEV), torch.empty(n, Hq, device=DEV)
+
+    def go(q, k, v, g, cu, pin, work):
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        pt.seq_attn(q, k, v, cu, out, lse_out=lse, n_pinned=pin, **kw)
+        pt.seq_attn_backward(q, k, v, out, lse, g, cu, *grads, work, n_pinned=pin, **kw)
+        return grads
+
+    alone = []
+    for s in sets:
+        alone.append(go(*s, torch.empty_like(ws)))
+        torch.cuda.synchronize()
+    got = []
+    for i in range(30):
+        for b, t in zip(bufs, sets[i % 3]):
+            b.copy_(t)
+        got.append(go(*bufs, ws))
+    torch.cuda.synchronize()
+    for i, grads in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(alone[i % 3], grads)), i
