@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -221,7 +222,8 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None)
 # Calls of a few tokens are bound by the host: what follows asks each tensor as little as it can, the common answer first.
 @functools.lru_cache(maxsize=256)
 def _config(kind, *values):
-    """A configuration as the C side wants it, the same object for the same values."""
+    """A configuration as the C side wants it, the same object for the same values: Python's own numbers, since others (a tensor that a
+    coefficient is kept in) may be found again by what they are and not by what they hold."""
     return ctypes.byref(kind(*values))
 
 
@@ -266,7 +268,7 @@ def _rope_args(where, q, k, positions, inv_freq, q_weight, k_weight, eps, interl
             _is(q_weight, dtype, (D,), index) and _is(k_weight, dtype, (D,), index)):
         _want(where, q.device, ("positions", positions, (n,), torch.int32), ("inv_freq", inv_freq, (half,), torch.float32),
               ("q_weight", q_weight, (D,), dtype), ("k_weight", k_weight, (D,), dtype))
-    return _config(RopeConfig, code, Hq, of_k[1], D, 2 * half, 1 if interleaved else 0, eps), n, sq, sk, of_q, of_k, dtype, index
+    return _config(RopeConfig, code, Hq, of_k[1], D, 2 * half, 1 if interleaved else 0, float(eps)), n, sq, sk, of_q, of_k, dtype, index
 
 
 def head_norm_rope(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
@@ -327,7 +329,7 @@ def _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale):
     batch = cu_seqlens.shape[0] - 1 if cu_seqlens.dim() == 1 else -1
     if not (_is(cu_seqlens, torch.int32, (batch + 1,), index) and _is(n_pinned, torch.int32, (batch,), index)):
         _want(where, q.device, ("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32), ("n_pinned", n_pinned, (batch,), torch.int32))
-    cfg = _config(SeqConfig, code, Hq, of_k[1], D, window, evict_chunk, 0.0 if scale is None else scale)
+    cfg = _config(SeqConfig, code, Hq, of_k[1], D, operator.index(window), operator.index(evict_chunk), 0.0 if scale is None else float(scale))
     return cfg, n, batch, st, of_q, of_k, dtype, index
 
 
@@ -402,7 +404,8 @@ def policy_loss(logits, tokens, advantage, logp, token_loss=None, loss=None, dlo
               ("ref_logp", ref_logp, row, f32), ("weight", weight, row, f32), ("logp", logp, row, f32),
               ("token_loss", token_loss, row, f32), ("token_kl", token_kl, row, f32), ("loss", loss, (1,), f32))
     dev = _device_of(where, logits)
-    cfg = _config(PolicyConfig, DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_FP32, V, temperature, clip_low, clip_high, kl_coef)
+    cfg = _config(PolicyConfig, DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_FP32, V, float(temperature), float(clip_low),
+                  float(clip_high), float(kl_coef))
     rc = lib.ptenc_policy_loss(cfg, logits.data_ptr(), s_in, tokens.data_ptr(), _ptr(old_logp), _ptr(ref_logp),
                                _ptr(advantage), _ptr(weight), n, logp.data_ptr(), _ptr(token_loss), _ptr(token_kl), _ptr(loss),
                                _ptr(dlogits), s_out, _stream_of(dev))

@@ -1,0 +1,69 @@
+"""What the training-pass calls hand to the library, without a GPU: the library is a stand-in that keeps the configurations it gets."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_16839_b200 as pt
+from paper_2602_16839_b200 import binding as bd
+
+
+class _Library:
+    def __init__(self):
+        self.got = []
+
+    def __getattr__(self, name):
+        def call(cfg, *args):
+            self.got.append({field: getattr(cfg._obj, field) for field, _ in cfg._obj._fields_})
+            return bd.PTENC_OK
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    fake = _Library()
+    monkeypatch.setattr(bd, "lib", fake)
+    monkeypatch.setattr(bd, "_device_of", lambda where, t: 0)
+    monkeypatch.setattr(bd, "_stream_of", lambda device: 0)
+    return fake
+
+
+def _calls():
+    q, k = torch.zeros(6, 4, 64, dtype=torch.bfloat16), torch.zeros(6, 2, 64, dtype=torch.bfloat16)
+    cu, pos, freq, w = torch.zeros(3, dtype=torch.int32), torch.zeros(6, dtype=torch.int32), torch.zeros(32), torch.zeros(64, dtype=torch.bfloat16)
+    z, f, dw, lse = torch.zeros(6, 9), torch.zeros(6), torch.zeros(64), torch.zeros(6, 4)
+    return {
+        "rope": lambda **kw: pt.head_norm_rope(q, k, pos, freq, q, k, q_weight=w, k_weight=w, **kw),
+        "rope_bwd": lambda **kw: pt.head_norm_rope_backward(q, k, q, k, pos, freq, q, k, q_weight=w, k_weight=w, dq_weight=dw, dk_weight=dw, **kw),
+        "attn": lambda **kw: pt.seq_attn(q, k, k, cu, q, **kw),
+        "attn_bwd": lambda **kw: pt.seq_attn_backward(q, k, k, q, lse, q, cu, q, k, k, f, **kw),
+        "loss": lambda **kw: pt.policy_loss(z, pos, f, f, f, **kw),
+        "logp": lambda **kw: pt.token_logp(z, pos, f, **kw),
+    }
+
+
+@pytest.mark.parametrize("call,name", [
+    ("rope", "eps"), ("rope_bwd", "eps"), ("attn", "scale"), ("attn_bwd", "scale"), ("loss", "temperature"), ("loss", "clip_low"),
+    ("loss", "clip_high"), ("loss", "kl_coef"), ("logp", "temperature")])
+@pytest.mark.parametrize("number", [torch.tensor, np.float32, float])
+def test_numbers_are_taken_as_they_are_at_the_call(call, name, number, library):
+    """A coefficient that is changed in place between two calls, as an annealed one may be."""
+    t = number(0.5)
+    go = _calls()[call]
+    go(**{name: t})
+    t *= 0.5
+    go(**{name: t})
+    assert [c[name] for c in library.got] == [0.5, 0.25]
+
+
+@pytest.mark.parametrize("call", ["attn", "attn_bwd"])
+@pytest.mark.parametrize("name", ["window", "evict_chunk"])
+def test_whole_numbers_are_taken_as_they_are_at_the_call(call, name, library):
+    go, kw = _calls()[call], dict(window=64, evict_chunk=4)
+    t = torch.tensor(8)
+    go(**{**kw, name: t})
+    t += 3
+    go(**{**kw, name: t})
+    go(**{**kw, name: np.int64(5)})
+    assert [c[name] for c in library.got] == [8, 11, 5]
+    with pytest.raises(TypeError):
+        go(**{**kw, name: 8.0})
