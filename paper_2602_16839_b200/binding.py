@@ -224,6 +224,9 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None)
 def _config(kind, *values):
     """A configuration as the C side wants it, the same object for the same values: Python's own numbers, since others (a tensor that a
     coefficient is kept in) may be found again by what they are and not by what they hold."""
+    for (name, _), v in zip(kind._fields_, values):
+        if isinstance(v, int) and not -2 ** 31 <= v < 2 ** 31:      # a field would keep its last 32 bits
+            raise PtencError(PTENC_ESHAPE, f"{kind.__name__}: {name} = {v} does not fit 32 bits")
     return ctypes.byref(kind(*values))
 
 
@@ -327,6 +330,8 @@ def _seq_args(where, q, k, v, cu_seqlens, n_pinned, window, evict_chunk, scale):
     of_k = (n, k.shape[1] if k.dim() == 3 else 0, D)
     st = (_rows(where, "q", q, of_q, q, dtype, index), _rows(where, "k", k, of_k, q, dtype, index), _rows(where, "v", v, of_k, q, dtype, index))
     batch = cu_seqlens.shape[0] - 1 if cu_seqlens.dim() == 1 else -1
+    if batch >= 2 ** 31:
+        raise PtencError(PTENC_ESHAPE, f"{where}: {batch} sequences do not fit 32 bits")
     if not (_is(cu_seqlens, torch.int32, (batch + 1,), index) and _is(n_pinned, torch.int32, (batch,), index)):
         _want(where, q.device, ("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32), ("n_pinned", n_pinned, (batch,), torch.int32))
     cfg = _config(SeqConfig, code, Hq, of_k[1], D, operator.index(window), operator.index(evict_chunk), 0.0 if scale is None else float(scale))

@@ -67,3 +67,28 @@ def test_whole_numbers_are_taken_as_they_are_at_the_call(call, name, library):
     assert [c[name] for c in library.got] == [8, 11, 5]
     with pytest.raises(TypeError):
         go(**{**kw, name: 8.0})
+
+
+@pytest.mark.parametrize("call", ["attn", "attn_bwd"])
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 32 + 5, 2 ** 70])
+@pytest.mark.parametrize("name", ["window", "evict_chunk"])
+def test_whole_numbers_that_32_bits_do_not_hold_are_refused(call, name, value, library):
+    for _ in range(2):
+        with pytest.raises(pt.PtencError) as e:
+            _calls()[call](**{"window": 64, "evict_chunk": 4, name: value})
+        assert e.value.code == bd.PTENC_ESHAPE
+    assert library.got == []
+
+
+def test_vocabularies_and_batches_that_32_bits_do_not_hold_are_refused(library):
+    """They would arrive as what 32 bits leave of them.  The tensors have a shape and no memory."""
+    meta = dict(device="meta")
+    z, n1 = torch.empty(1, 2 ** 32 + 9, dtype=torch.bfloat16, **meta), torch.empty(1, **meta)
+    q, k = torch.empty(6, 4, 64, **meta), torch.empty(6, 2, 64, **meta)
+    cu, lse, ws = torch.empty(2 ** 32 + 3, dtype=torch.int32, **meta), torch.empty(6, 4, **meta), torch.empty(48, **meta)
+    for go in (lambda: pt.token_logp(z, n1.int(), n1), lambda: pt.policy_loss(z, n1.int(), n1, n1, dlogits=torch.empty_like(z)),
+               lambda: pt.seq_attn(q, k, k, cu, q), lambda: pt.seq_attn_backward(q, k, k, q, lse, q, cu, q, k, k, ws)):
+        with pytest.raises(pt.PtencError) as e:
+            go()
+        assert e.value.code == bd.PTENC_ESHAPE
+    assert library.got == []
