@@ -12,6 +12,9 @@ class _Library:
         self.got = []
 
     def __getattr__(self, name):
+        if name == "ptenc_strerror":
+            return pt.lib.ptenc_strerror
+
         def call(cfg, *args):
             self.got.append({field: getattr(cfg._obj, field) for field, _ in cfg._obj._fields_})
             return bd.PTENC_OK
