@@ -5,6 +5,8 @@ import torch
 import paper_2602_16839_b200 as pt
 from oracle import train_oracle as to
 
+import test_gpu_train as whole
+
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
@@ -134,3 +136,38 @@ def test_gradients_of_rollouts_that_follow_one_another_in_the_same_tensors(D):
     torch.cuda.synchronize()
     for i, grads in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(alone[i % 3], grads)), i
+
+
+# ------------------------------------------------------------------------------------------------------ policy loss
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [500_009, 20_000_003, 1 << 28])
+def test_rows_of_any_width_add_up(V, dtype):
+    """Rows that no cluster holds, of weights that are all alike and of weights that are not: however many there are, their sum is as
+    exact as that of a short row."""
+    dt, gen = TYPES[dtype], _gen(V)
+    z = torch.full((2, V), -0.359375, dtype=dt, device=DEV)          # a weight of 0.698: no sum of them is exact
+    z[0, V // 3] = 0.0
+    z[1] = torch.randn(V, device=DEV, generator=gen, dtype=dt)
+    tok = torch.tensor([5, V - 2], dtype=torch.int32, device=DEV)
+    adv, lp = torch.tensor([1.5, -0.7], device=DEV), torch.empty(2, device=DEV)
+    only = torch.empty(2, device=DEV)
+    pt.token_logp(z, tok, only)
+    zd = z.double()
+    lse = torch.logsumexp(zd, 1)
+    ref = zd[torch.arange(2, device=DEV), tok.long()] - lse
+    # Exponents (of the base 2) below 2^4 are off by their own rounding and the factor's, 2^-24 each: weights by 2^-19 log 2, exp2f by 2^-22,
+    # a sum of at most 32 of them in fp32 by 2^-19; what the log-probability is rounded to comes beside that.
+    rel = 2.0 ** -18
+    _close(only, ref, rel + 4 * to.U * ref.abs(), "logp")
+    pt.policy_loss(z, tok, adv, lp, dlogits=z)                       # in place
+    assert torch.equal(lp, only)
+    for i in range(2):
+        g = zd[i].sub_(lse[i]).exp_().mul_(adv[i].double())          # -A (onehot - softmax)
+        g[int(tok[i])] -= float(adv[i])
+        bound = g.abs().mul_(2 * rel + to.half_step(dt)).add_(2.0 ** -126)
+        assert (z[i].double().sub_(g).abs_() <= bound).all(), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_no_cluster_holds_of_masked_and_extreme_logits(dtype):
+    whole.test_policy_loss_of_masked_and_extreme_logits(500_009, dtype)
