@@ -171,3 +171,35 @@ def test_rows_of_any_width_add_up(V, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_that_no_cluster_holds_of_masked_and_extreme_logits(dtype):
     whole.test_policy_loss_of_masked_and_extreme_logits(500_009, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("opt", [
+    dict(temperature=0.8, clip_low=0.15, clip_high=0.3, kl_coef=0.1), dict(temperature=1.7, kl_coef=2.0), dict(clip_low=0.0, clip_high=0.05)])
+@pytest.mark.parametrize("n,V", [(60, 1000), (30, 32000), (20, 152000), (12, 300001), (6, 700003)])
+def test_every_entry_of_the_gradient_is_relatively_exact(n, V, opt, dtype):
+    """Of the whole loss: old policy, reference, weights, masked tokens.  An entry is compared with its own size, however small a part of
+    its row it is."""
+    dt = TYPES[dtype]
+    z, tok, kw = whole._loss_case(n, V, dt, 3 * n + V)
+    lp, dz = torch.empty(n, device=DEV), torch.full_like(z, 5.0)
+    pt.policy_loss(z, tok, **kw, logp=lp, dlogits=dz, **opt)
+    ref = to.policy_loss(z, tok, kw["advantage"], kw["old_logp"], kw["ref_logp"], kw["weight"], **opt)
+    on = (kw["weight"] != 0) & (tok >= 0) & (tok < V)
+    assert (dz[~on] == 0).all() and on.sum() >= 2
+    T = opt.get("temperature", 1.0)
+    p = torch.softmax(z.double() / T, -1)
+    rows, own = torch.arange(n, device=DEV)[on], tok[on].long()
+    p[rows, own] = 1 - p[rows, own]
+    # A weight's exponent (below 2^6 in the base 2) is off by three roundings of 2^-24, its power and the sum by less than 2^-18: 2^-16 with what
+    # the entry is multiplied by.  The log-probability is off by less than 2^-17, and with it the ratio and the KL term's factor, each
+    # relatively, before one is taken from the other.
+    size = (kw["weight"].abs() / T).double() * (torch.exp(ref["logp"] - kw["old_logp"].double()) * kw["advantage"].double().abs()
+                                                + opt.get("kl_coef", 0.0) * torch.exp(kw["ref_logp"].double() - ref["logp"]))
+    g = ref["dlogits"]
+    bound = (to.half_step(dt) + 2.0 ** -16) * g.abs() + 2.0 ** -17 * (size[:, None] * p) + 2.0 ** -126
+    _close(dz[on], g[on], bound[on], "dlogits")
+    top = g[on].abs().amax(-1, keepdim=True)
+    some = top[:, 0] > 0                                             # not cut off by the clip
+    few = (g[on][some].abs() < 2.0 ** -6 * top[some]).double().mean()
+    assert some.any() and (V < 10000 or few > 0.9)                   # most entries are a small part of their row's largest
