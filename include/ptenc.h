@@ -293,7 +293,7 @@ typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim;
   int32_t window;          /* the cache budget W a token was decoded under; 0: no limit                    */
   int32_t evict_chunk;     /* E, 1..W; read only with a window                                             */
-  float scale;             /* of the scores, > 0; 0: 1 / sqrt(head_dim)                                    */
+  float scale;             /* of the scores, > 0, up to 2e38; 0: 1 / sqrt(head_dim)                        */
 } ptenc_seq_config;
 
 /* Attention over whole sequences, causal: out[t,h,:] = softmax(scale * q[t,h,:] . K^T) V over the tokens that token t sees of
@@ -336,7 +336,7 @@ PTENC_API int ptenc_seq_attn_backward(const ptenc_seq_config* cfg /*host*/, cons
 typedef struct {
   int32_t dtype;           /* PTENC_DTYPE_* of the logits and their gradient                               */
   int32_t vocab;           /* V, up to 2^28                                                                */
-  float temperature;       /* > 0: the policy is softmax(logits / temperature)                             */
+  float temperature;       /* 2^-126 .. 3e38: the policy is softmax(logits / temperature)                  */
   float clip_low, clip_high; /* the ratio is clipped to [1 - clip_low, 1 + clip_high], both >= 0           */
   float kl_coef;           /* of the KL term, >= 0; not read without ref_logp                              */
 } ptenc_policy_config;

@@ -497,7 +497,7 @@ extern "C" int ptenc_policy_loss(const ptenc_policy_config* cfg, const void* log
                                  int64_t dlogits_stride, void* stream) {
   if (cfg == nullptr || n_tokens < 0) return PTENC_EINVAL;
   if (cfg->dtype != PTENC_DTYPE_FP32 && cfg->dtype != PTENC_DTYPE_BF16) return PTENC_EINVAL;
-  if (cfg->vocab < 1 || !(cfg->temperature > 0.f) || cfg->temperature > 3e38f) return PTENC_EINVAL;
+  if (cfg->vocab < 1 || !(cfg->temperature >= 1.17549435e-38f) || cfg->temperature > 3e38f) return PTENC_EINVAL;
   if (cfg->vocab > (1 << 28) || n_tokens >= (1ll << 28)) return PTENC_ESHAPE;
   if (advantage != nullptr && (!(cfg->clip_low >= 0.f) || !(cfg->clip_high >= 0.f))) return PTENC_EINVAL;
   if (advantage != nullptr && ref_logp != nullptr && !(cfg->kl_coef >= 0.f)) return PTENC_EINVAL;

@@ -613,7 +613,7 @@ int check_config(const ptenc_seq_config* c, int32_t batch, int64_t n) {
   if (c->dtype != PTENC_DTYPE_FP32 && c->dtype != PTENC_DTYPE_BF16) return PTENC_EINVAL;
   if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->head_dim < 1 || c->window < 0) return PTENC_EINVAL;
   if (c->window > 0 && (c->evict_chunk < 1 || c->evict_chunk > c->window)) return PTENC_EINVAL;
-  if (!(c->scale >= 0.f) || c->scale > 3e38f) return PTENC_EINVAL;
+  if (!(c->scale >= 0.f) || c->scale > 2e38f) return PTENC_EINVAL;
   if (c->head_dim % 8 != 0 || c->head_dim > 256 || c->n_q_heads > 16384 || c->n_q_heads % c->n_kv_heads != 0) return PTENC_ESHAPE;
   if (n >= (1ll << 31) - 512 || batch > (1 << 24)) return PTENC_ESHAPE;
   if ((n / 32 + batch) * c->n_q_heads >= (1ll << 31)) return PTENC_ESHAPE;      // numbers of tiles and heads, of any of the kernels

@@ -6,6 +6,8 @@ import torch
 import paper_2602_16839_b200 as pt
 from paper_2602_16839_b200 import binding as bd
 
+from test_train_cpu import _loss, _seq
+
 
 class _Library:
     def __init__(self):
@@ -95,3 +97,16 @@ def test_vocabularies_and_batches_that_32_bits_do_not_hold_are_refused(library):
             go()
         assert e.value.code == bd.PTENC_ESHAPE
     assert library.got == []
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 1e-39, 1.1e-38])
+def test_temperatures_below_the_normal_range_are_refused(temperature):
+    """With an inverse that is not finite a row's largest logits would become 0 * inf."""
+    assert _loss(T=temperature) == bd.PTENC_EINVAL
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("scale", [2.4e38, 2.9e38])
+def test_scales_that_pass_the_range_in_base_2_are_refused(scale, back):
+    """A score of zero would become 0 * inf."""
+    assert _seq(back, scale=scale) == bd.PTENC_EINVAL
