@@ -266,7 +266,8 @@ typedef struct {
 /* Norm of every query and key head and its rotation by the token's position, in one pass:
  *   y = w * x / sqrt(mean(x^2) + eps)  (y = x where the weight is NULL),  then each pair (a, b) of y turns by
  *   angle = positions[t] * inv_freq[i]:  (a cos - b sin, b cos + a sin).
- * The angle is taken in 64 bits, so positions may be far; everything else is fp32, rounded once at the end.  q [n, H_q, D],
+ * The angle is taken in 64 bits, so positions may be far; everything else is fp32, rounded once at the end (fp32 results are off by 1.1e-7
+ * of their size in the 2-norm; with bf16 tensors sines and cosines are good to 2^-20.5, in the gradients of the weights too).  q [n, H_q, D],
  * k [n, H_kv, D]; q_weight, k_weight [D] in the storage dtype, nullable each; positions [n] int32; inv_freq [rotary_dim / 2] fp32.
  * q_out may be q and k_out k, with equal strides.  For a decode step n is the batch, q_out and k_out go on to ptenc_decode_step. */
 PTENC_API int ptenc_head_norm_rope(const ptenc_rope_config* cfg /*host*/, const void* q, int64_t q_stride, const void* k,
@@ -323,7 +324,9 @@ PTENC_API int ptenc_seq_attn(const ptenc_seq_config* cfg /*host*/, const void* q
 /* Gradients of ptenc_seq_attn with respect to q, k and v, from dout [n, H_q, D] (contiguous, like out), the forward call's inputs,
  * out and lse (those of exactly these keys: a token's weights sum to one).  The heads that share a KV head are summed in fp32, in a fixed
  * order: repeated calls give the same bits.  On the tensor cores weights and score gradients are rounded to bf16 in the products they
- * enter: gradients are off by 2.5e-3 of their size in the 2-norm.  A token that sees itself alone has score gradients of zero.
+ * enter: gradients are off by 2.5e-3 of their size in the 2-norm.  The sum of dout * out over a row is taken from the rounded out and
+ * corrected by what the row's weights leave of it; the gradient of a query whose 128-row tile reaches more than six tiles of 128 keys takes it
+ * uncorrected, those of keys always corrected.  A token that sees itself alone has score gradients of zero.
  * workspace: device, 16-byte aligned, ptenc_seq_attn_workspace_bytes; its contents do not outlive the call, and calls that share
  * one do not overlap on the GPU. */
 PTENC_API int ptenc_seq_attn_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, size_t* bytes /*host, out*/);
@@ -354,7 +357,8 @@ typedef struct {
  * fp32; old_logp, ref_logp, weight (NULL = 1) nullable.  advantage NULL: only logp is wanted (the log-probabilities of the policy
  * that samples, or of the reference), and everything but tokens, weight and logp is to be NULL.  Outputs logp [n], token_loss
  * [n] (the loss_t; required with loss), token_kl [n] (the KL estimate without kl_coef; 0 without ref_logp), loss [1], all fp32,
- * token_loss, token_kl and loss nullable.  Sums over the vocabulary are fp32, what follows from them per token is 64 bits, the sum
+ * token_loss, token_kl and loss nullable.  Weights are powers of two good to 2^-22, sums over the vocabulary fp32
+ * (in 64 bits across blocks of 16 where a row is above 917504 bytes), what follows from them per token is 64 bits, the sum
  * over tokens 64 bits in a fixed order.  logits of -inf have no probability.  No workspace. */
 PTENC_API int ptenc_policy_loss(const ptenc_policy_config* cfg /*host*/, const void* logits, int64_t logits_stride,
                                 const int32_t* tokens, const float* old_logp, const float* ref_logp, const float* advantage,

@@ -47,7 +47,7 @@ struct RopeArgs {
 
 // Cosine and sine of pos * freq, turns = freq / (2 pi).  The product is taken in 64 bits and brought to a fraction of a turn there: in 32 bits the
 // angle of position 60000 would be off by 2e-3.  `fast`: the hardware's sine and cosine, off by 2^-20.5 at most within half a turn, for
-// results that are rounded to bf16 (2^-8) anyhow.
+// results that are rounded to bf16 (2^-8) anyhow; the weights' gradients, which are fp32 sums over bf16 values, take them too.
 __device__ __forceinline__ void rp_angle(int pos, double turns, float* s, float* c, bool fast) {
   double t = (double)pos * turns;
   t -= rint(t);

@@ -211,7 +211,8 @@ __device__ __forceinline__ void sg_put(T* to, const float4& v, float f) {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // The last launch bound, here and below: how many CTAs of an SM the registers are to allow where the compiler's own choice (0) was the
-// slower one.  Five fp32 sequences of 8000 tokens, 12 + 4 heads of 128: forward 3395 us with 1, 3834 with 0.
+// slower one.  Five fp32 sequences of 8000 tokens in all, 5839 the longest, 12 + 4 heads of
+// 128: forward 3395 us with 1, 3834 with 0.
 template <typename T, int DP>
 __global__ void __launch_bounds__(SG_THREADS, SgShape<DP>::fwd(SgShape<DP>::BF) <= SgShape<DP>::half ? 0 : 1)
 k_seq_fwd(const __grid_constant__ SeqArgs a) {

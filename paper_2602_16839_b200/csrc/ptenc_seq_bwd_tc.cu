@@ -16,8 +16,8 @@
 //    run along a thread's columns, lie in shared memory.
 //  * k_seq_dq_tc, per tile of keys: S is buffered twice and dS goes over the S it came from, so that softmax warps never wait.
 // Bound by the chain of a step (scores, exponentials, dS, sums), of which tensor memory holds no second: the tensor pipe is busy 56 %
-// (dQ) and 62 % (dK, dV) of the time.  Two sequences of 8192 tokens, 32 + 8 heads of 128, full attention: 1.27 ms (1.30 PFLOP/s of its
-// three products) and 1.79 ms (1.23 PFLOP/s of its four).
+// (dQ) and 62 % (dK, dV) of the time.  Two sequences of 8192 tokens, 32 + 8 heads of 128, full attention: 1.32 ms (1.25 PFLOP/s of its
+// three products) and 1.81 ms (1.22 PFLOP/s of its four).
 // Non-finite values of tokens that a row does not see: they are taken out of the operands of the second products (0 * NaN), and
 // the rows that do see them become NaN through lse, delta or a bit per key.
 #include <cooperative_groups.h>

@@ -13,8 +13,9 @@
 //  * warps 4..11: softmax, four warps per stream, a row per thread with its 128 scores in registers: mask, maximum, running sum in
 //    fp32 (base 2), P rounded to bf16.  O is rescaled only when the maximum has grown by more than 2^8.
 //  * Bound by the chain from a tile's scores to its P, two streams deep: the tensor pipe and the exponentials' unit are each busy half of
-//    the time.  16384 tokens, 28 + 4 heads of 128, causal: 1.52 ms, 1.27 PFLOP/s.
-//  * Every wait is bounded: one that runs out raises an abort flag, every role leaves, copies and products in flight are drained and
+//    the time; at D = 64 the exponentials' unit is busy 60 % of it, the tensor pipe 30 %.  16384 tokens, 28 + 4 heads of 128, causal: 1.61 ms
+//    after a rest, 1.20 PFLOP/s, 1.77 ms for seconds on end.
+//  * Every wait is bounded, by 8 ms in which the CTA does not get on at all (fwd_wait): one that runs out raises an abort flag, every role leaves, copies and products in flight are drained and
 //    tensor memory is freed; the item's rows become NaN, those of items that the CTA had not begun may be left as they were.
 #include "ptenc_seq_tc.cuh"
 
